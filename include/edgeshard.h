@@ -58,7 +58,11 @@ typedef enum {
   ES_ERR_UNSUPPORTED = 9
 } es_status_t;
 
-typedef enum { ES_DTYPE_F16 = 0, ES_DTYPE_F32 = 1, ES_DTYPE_I32 = 2 } es_dtype_t;
+typedef enum {
+  ES_DTYPE_F16 = 0, ES_DTYPE_F32 = 1, ES_DTYPE_I32 = 2,
+  ES_DTYPE_BF16 = 3,                       /* operands of the 8-bit cache and sampling operations only */
+  ES_DTYPE_I8 = 4, ES_DTYPE_F8E4M3 = 5     /* codes of an 8-bit cache */
+} es_dtype_t;
 
 /* Model and capacity description.  max_slots = number of sequences whose KV is kept at once;
  * max_seq = longest context (prompt + generated) per slot; max_tokens = largest B*T of one
@@ -358,6 +362,107 @@ ES_API es_status_t es_op_decode_attention_static(const void *q, const void *k_pa
                                                  int32_t B, int32_t Hq, int32_t Hkv, int32_t hd,
                                                  int32_t page_tokens, int32_t pages_per_seq, int32_t max_ctx,
                                                  void *stream);
+
+/* ---- decode loop over a paged cache held in 8 bits ----------------------------------------------
+ * The memory constraint of the paper's placement (Req_i <= Mem_j, Sec. "Optimize LLM Inference") counts the
+ * reserved KV cache; these operations hold it in one byte per value.  They work on pages of the same layout as
+ * es_op_decode_attention: codes [n_pages, Hkv, P, hd] (P = page_tokens, a power of two >= 16) with one fp32 scale
+ * per page and KV head, k_scale / v_scale [n_pages, Hkv]; a cached value is code * scale.  A SLOT is the number
+ * page * P + offset of a token's place in the pool.  code_dtype: ES_DTYPE_I8 (symmetric, -127..127) or
+ * ES_DTYPE_F8E4M3.  hd is 64 or 128.  All pointers dev; every call only enqueues on `stream`, on the current device,
+ * and may be captured into a graph.  No call reads or writes outside its arguments' stated extents, whatever the
+ * contents of tables, lengths and slots. */
+
+/* Block tables and slot maps from request lengths.  Request b holds old_len[b] tokens and is to hold new_len[b]:
+ * more (prompt rows, new tokens), fewer (rejected draft tokens), none (finished), or the same.
+ *   old_len, new_len int32 [B], B <= 8192;   block_table int32 [B, pages_per_seq], in and out;
+ *   free_pages int32 [n_pages] and free_count int32 [1], in and out: a stack of the pages nobody holds.
+ *     Both NULL: the table is taken as it is and only the row outputs are made.
+ *   max_rows: room of the row outputs (>= 1);  pages_per_seq * page_tokens <= 2^31 - 1.
+ * Pages: first the pages of shrinking requests (table entries ceil(new / P) .. ceil(old / P) - 1) are pushed in
+ * ascending order of (b, entry) and their entries become -1; then growing requests, in ascending order, pop the
+ * pages they lack from the top.  A growing request is served whole or not at all: it is refused when the rows up to
+ * and including its own exceed max_rows, or when it lacks pages and the pages lacked up to and including its own
+ * exceed those on the stack.  A length outside [0, pages_per_seq * P] leaves its request as it is, with no rows.
+ * Rows: the gained tokens of all requests, refused ones included, one request after the other, so the layout
+ * follows from the lengths alone:
+ *   row_offsets int32 [B + 1] (capped at max_rows);  positions int32 [max_rows] (place in its sequence);
+ *   row_seq int32 [max_rows] (its request);  slot_map int32 [max_rows] (-1 for rows of a refused request and where
+ *   the table holds no page);  runs int32 [max_runs]: first rows of the served stretches that lie in one page, ascending
+ *   (-1 for one whose page the table does not hold), max_runs = es_op_kv_plan_max_runs(...);
+ *   entries behind the last row or run are -1;
+ *   len_out int32 [B]: new_len where served, else old_len (may be old_len itself).
+ * Entries of the table below a request's length must be distinct pages in [0, n_pages) for the stack to stay
+ * sound. */
+ES_API int32_t es_op_kv_plan_max_runs(int32_t B, int32_t max_rows, int32_t page_tokens);
+ES_API es_status_t es_op_kv_plan(const int32_t *old_len, const int32_t *new_len, int32_t *block_table,
+                                 int32_t *free_pages, int32_t *free_count, int32_t B, int32_t pages_per_seq,
+                                 int32_t page_tokens, int32_t n_pages, int32_t max_rows, int32_t *row_offsets,
+                                 int32_t *slot_map, int32_t *positions, int32_t *row_seq, int32_t *runs,
+                                 int32_t *len_out, void *stream);
+
+/* Writes n_rows new rows of K and V into the cache: k, v (fp16 or bf16) [n_rows, Hkv, hd], row r at k + r * row_stride
+ * elements (heads contiguous; row_stride % 8 == 0, 16-byte aligned, so a slice of a fused QKV product serves);
+ * row r goes to slot_map[r].  Rows with a slot outside [0, n_pages * P) are left out (padding, refused requests).
+ * A page is filled in ascending order: rows that go to one page must be consecutive rows at consecutive slots, and
+ * what lies in front of the first of them is what the page already holds.  `runs` (int32 [n_runs], may be NULL with
+ * n_runs 0) lists the first rows of these stretches, as es_op_kv_plan gives them; entries outside [0, n_rows) are
+ * skipped.  Without it every row is looked at to find them.  One call must not give a page twice.
+ * Scale of a page and head, x = largest magnitude among the new rows: I8 x / 127, F8E4M3 the smallest power of two s
+ * with x <= 448 s, never below 2^-100; a page that holds tokens in front keeps its scale if that is larger, and
+ * otherwise its codes are brought to the new one (round(code * old / new)).  New codes are round(value / scale), to
+ * nearest, ties to even.  If a new value is infinite or NaN the page's scale of that head becomes NaN until the
+ * page is filled again from its offset 0: nothing hides it. */
+ES_API es_status_t es_op_kv8_append(const void *k, const void *v, int32_t dtype, int64_t row_stride, int32_t n_rows,
+                                    const int32_t *slot_map, const int32_t *runs, int32_t n_runs, void *k_pages,
+                                    void *v_pages, int32_t code_dtype, float *k_scale, float *v_scale, int32_t Hkv,
+                                    int32_t hd, int32_t page_tokens, int32_t n_pages, void *stream);
+
+/* Reads cached rows back: k, v [n_rows, Hkv, hd] (fp16, bf16 or fp32, dense) = code * scale of the token at
+ * slot_map[r]; zeros for a slot outside [0, n_pages * P).  For handing a sequence to a shard with another cache
+ * (the paper's hand-over of a device's state) or to es_op_prefill_attention. */
+ES_API es_status_t es_op_kv8_gather(const int32_t *slot_map, int32_t n_rows, const void *k_pages, const void *v_pages,
+                                    int32_t code_dtype, const float *k_scale, const float *v_scale, int32_t Hkv,
+                                    int32_t hd, int32_t page_tokens, int32_t n_pages, void *k, void *v, int32_t dtype,
+                                    void *stream);
+
+/* es_op_decode_attention over the 8-bit cache, for the newest T tokens of every sequence (T = 1: a decode step;
+ * T > 1: draft tokens checked in one pass).
+ *   q (fp16 or bf16) [B, T, Hq, hd], token b * T + t at q + (b * T + t) * q_stride elements (heads contiguous,
+ *   q_stride % 8 == 0, 16-byte aligned);  out [B, T, Hq * hd], dense, of q's type;  Hq a multiple of Hkv;
+ *   block_table int32 [B, pages_per_seq];  ctx_len int32 [B]: cached keys of the sequence, its T newest included.
+ * Query t sees keys 0 .. ctx_len[b] - T + t; a query that sees none gives zeros.  Scale 1/sqrt(hd); scores, softmax
+ * and sums in fp32, probabilities enter the product as two fp16 halves.  Table entries outside [0, n_pages) are
+ * pages that nobody sees; lengths above max_ctx (<= pages_per_seq * page_tokens) are read as max_ctx.
+ *   scratch: dev, 16-byte aligned, es_op_decode_attention_kv8_scratch_bytes(...) bytes of the call's sizes, in use
+ *   until the call's work is done (calls that overlap on the GPU need one each).  Uninitialised is fine. */
+ES_API size_t es_op_decode_attention_kv8_scratch_bytes(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t hd,
+                                                       int32_t page_tokens, int32_t max_ctx);
+ES_API es_status_t es_op_decode_attention_kv8(const void *q, int32_t dtype, int64_t q_stride, const void *k_pages,
+                                              const void *v_pages, int32_t code_dtype, const float *k_scale,
+                                              const float *v_scale, const int32_t *block_table,
+                                              const int32_t *ctx_len, void *out, int32_t B, int32_t T, int32_t Hq,
+                                              int32_t Hkv, int32_t hd, int32_t page_tokens, int32_t pages_per_seq,
+                                              int32_t n_pages, int32_t max_ctx, void *scratch, size_t scratch_bytes,
+                                              void *stream);
+
+/* The next token of every row of logits, drawn with a given random number (the sampled counterpart of the shard's
+ * greedy ids; `logits` may be the view es_shard_handoff returns, `tokens` feeds es_shard_decode_step).
+ *   logits (fp32, fp16 or bf16) [B, V], row b at logits + b * row_stride elements;  u fp32 [B], in [0, 1);
+ *   temperature, top_p, min_p fp32 [B] and top_k int32 [B], each may be NULL (1, off, off, off);
+ *   tokens int32 [B] out;  logprobs fp32 [B] out or NULL: log of the drawn token's probability among those kept.
+ * Per row: weights w_i = exp((logit_i - max) / temperature); tokens rank by logit, equal ones by index.  Kept are
+ * the top_k first (top_k <= 0: all), of those the fewest first whose mass reaches top_p of theirs (top_p >= 1: all),
+ * of those the ones with w_i >= min_p (clamped to [0, 1]); the first token is always kept.  The result is the
+ * lowest index at which the running kept mass, in order of index, exceeds u times the whole.  A temperature that is
+ * not above 0 takes the first token.  NaN logits count as -infinity, which is never drawn; a row that has nothing
+ * else gives -1 (and -infinity).  u is clamped to [0, 1].  Weights are held as integers in units of 2^-44, so every
+ * sum is exact and the result depends on nothing but the inputs; tokens of weight below 2^-45 have none.
+ * V <= 262144. */
+ES_API es_status_t es_op_sample(const void *logits, int32_t dtype, int64_t row_stride, const float *u,
+                                const float *temperature, const int32_t *top_k, const float *top_p,
+                                const float *min_p, int32_t *tokens, float *logprobs, int32_t B, int32_t V,
+                                void *stream);
 
 #ifdef __cplusplus
 }

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
@@ -21,7 +21,7 @@ STATUS_NAMES = {
     5: "ES_ERR_KV_FULL", 6: "ES_ERR_WORKSPACE", 7: "ES_ERR_CUDA", 8: "ES_ERR_DEVICE_TIMEOUT",
     9: "ES_ERR_UNSUPPORTED",
 }
-ES_DTYPE_F16, ES_DTYPE_F32, ES_DTYPE_I32 = 0, 1, 2
+ES_DTYPE_F16, ES_DTYPE_F32, ES_DTYPE_I32, ES_DTYPE_BF16, ES_DTYPE_I8, ES_DTYPE_F8E4M3 = 0, 1, 2, 3, 4, 5
 KERNEL_CATEGORIES = ("embed", "rmsnorm", "qkv", "attention", "o", "gate_up", "down", "lm_head", "argmax", "set_ctx",
                      "splitk_finish", "splitk_reduce")
 LAYER_KEYS = ("attn_norm", "wq", "wk", "wv", "wo", "ffn_norm", "w_gate", "w_up", "w_down")
@@ -99,6 +99,13 @@ def _load() -> C.CDLL:
         "es_op_prefill_attention": (i32, [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp]),
         "es_op_decode_attention_scratch_bytes": (sz, [i32, i32, i32, i32, i32]),
         "es_op_decode_attention": (i32, [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, sz, vp]),
+        "es_op_kv_plan_max_runs": (i32, [i32, i32, i32]),
+        "es_op_kv_plan": (i32, [vp] * 5 + [i32] * 5 + [vp] * 7),
+        "es_op_kv8_append": (i32, [vp, vp, i32, C.c_int64, i32, vp, vp, i32, vp, vp, i32, vp, vp, i32, i32, i32, i32, vp]),
+        "es_op_kv8_gather": (i32, [vp, i32, vp, vp, i32, vp, vp, i32, i32, i32, i32, vp, vp, i32, vp]),
+        "es_op_decode_attention_kv8_scratch_bytes": (sz, [i32] * 7),
+        "es_op_decode_attention_kv8": (i32, [vp, i32, C.c_int64, vp, vp, i32] + [vp] * 5 + [i32] * 9 + [vp, sz, vp]),
+        "es_op_sample": (i32, [vp, i32, C.c_int64] + [vp] * 7 + [i32, i32, vp]),
         "es_op_decode_attention_static_capacity": (sz, []),
         "es_op_decode_attention_static": (i32, [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp]),
     }
@@ -114,7 +121,8 @@ EXPORTS = ("es_shard_workspace_bytes es_shard_create es_shard_prefill es_shard_p
            "es_layer_profile es_shard_set_profiling es_shard_reset_slots es_shard_set_page_table es_shard_set_graphs "
            "es_partition_latency es_partition_throughput es_shard_device_status es_shard_wait_probe es_shard_launch_count es_shard_set_kernel_timing es_shard_kernel_timing es_shard_kernel_timing_detail es_shard_set_step_timing es_shard_step_timing es_shard_destroy es_last_error es_version es_op_rmsnorm "
            "es_op_linear es_op_linear_splitk_workspace_bytes es_op_linear_splitk es_op_prefill_attention es_op_decode_attention_scratch_bytes es_op_decode_attention "
-           "es_op_decode_attention_static_capacity es_op_decode_attention_static").split()
+           "es_op_decode_attention_static_capacity es_op_decode_attention_static es_op_kv_plan_max_runs es_op_kv_plan es_op_kv8_append "
+           "es_op_kv8_gather es_op_decode_attention_kv8_scratch_bytes es_op_decode_attention_kv8 es_op_sample").split()
 
 
 def es_last_error() -> str:
@@ -414,6 +422,206 @@ def es_op_decode_attention_static(q: torch.Tensor, k_pages: torch.Tensor, v_page
     _check(lib.es_op_decode_attention_static(_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(block_table), _ptr(ctx_len),
                                              _ptr(out), B, Hq, Hkv, hd, P, block_table.shape[1], max_ctx,
                                              _stream_ptr(stream)))
+    return out
+
+
+# ---- decode loop over a paged cache held in 8 bits -------------------------------------------
+
+_VALUE_DTYPES = {torch.float16: ES_DTYPE_F16, torch.bfloat16: ES_DTYPE_BF16, torch.float32: ES_DTYPE_F32}
+_CODE_DTYPES = {torch.int8: ES_DTYPE_I8, torch.float8_e4m3fn: ES_DTYPE_F8E4M3}
+
+
+def _need(ok: bool, message: str) -> None:
+    if not ok:
+        raise EsError(1, message)
+
+
+def _on_device(stream, **tensors) -> None:
+    """All tensors on the current device (the library launches there) and the stream too."""
+    for name, t in tensors.items():
+        _need(isinstance(t, torch.Tensor) and t.is_cuda, f"{name} must be a CUDA tensor")
+    dev = torch.cuda.current_device()
+    for name, t in tensors.items():
+        _need(t.device.index == dev, f"{name} is on {t.device}, the current device is cuda:{dev}")
+    if stream is not None:
+        _need(stream.device.index == dev, f"the stream is on {stream.device}, the current device is cuda:{dev}")
+
+
+def _ints(**tensors) -> None:
+    for name, t in tensors.items():
+        _need(t.dtype == torch.int32 and t.is_contiguous(), f"{name} must be a contiguous int32 tensor")
+
+
+def _empty(stream, *shape, dtype, device) -> torch.Tensor:
+    """Memory for a call on `stream`: the allocator must know the stream it is used on."""
+    with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream()):
+        return torch.empty(*shape, dtype=dtype, device=device)
+
+
+def _check_pool(k_pages, v_pages, k_scale, v_scale) -> Tuple[int, int, int, int]:
+    _need(k_pages.dim() == 4 and k_pages.shape == v_pages.shape, "k_pages and v_pages must be [n_pages, Hkv, P, hd] of one shape")
+    _need(k_pages.dtype in _CODE_DTYPES and v_pages.dtype == k_pages.dtype, "pages must be int8 or float8_e4m3fn, both the same")
+    _need(k_pages.is_contiguous() and v_pages.is_contiguous(), "pages must be contiguous")
+    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+        _need(t.dtype == torch.float32 and t.is_contiguous() and t.shape == k_pages.shape[:2], f"{name} must be contiguous fp32 [n_pages, Hkv]")
+    return tuple(k_pages.shape)
+
+
+def _row_stride(t: torch.Tensor, name: str) -> int:
+    """Elements from row to row of [..., heads, hd] whose last two dimensions are dense and whose leading ones, if
+    several, step evenly: a slice of a fused projection's output is such a tensor."""
+    heads, hd = t.shape[-2:]
+    _need(t.stride(-1) == 1 and (t.stride(-2) == hd or heads == 1), f"the heads of a row of {name} must be contiguous")
+    lead = [(n, s) for n, s in zip(t.shape[:-2], t.stride()[:-2]) if n != 1]
+    for (_, outer), (n, inner) in zip(lead, lead[1:]):
+        _need(outer == n * inner, f"the rows of {name} must be evenly spaced")
+    return lead[-1][1] if lead else heads * hd
+
+
+class KvPlan(NamedTuple):
+    """Row layout of a batch (all int32, on the device); see es_op_kv_plan."""
+    row_offsets: torch.Tensor      # [B + 1]
+    slot_map: torch.Tensor         # [max_rows], -1 = no place
+    positions: torch.Tensor        # [max_rows]
+    row_seq: torch.Tensor          # [max_rows]
+    runs: torch.Tensor             # [max_runs], first rows of the stretches that lie in one page
+    len_out: torch.Tensor          # [B]
+
+
+def es_op_kv_plan_max_runs(B: int, max_rows: int, page_tokens: int) -> int:
+    return int(lib.es_op_kv_plan_max_runs(B, max_rows, page_tokens))
+
+
+def es_op_kv_plan(old_len: torch.Tensor, new_len: torch.Tensor, block_table: torch.Tensor, page_tokens: int, max_rows: int,
+                  free_pages: Optional[torch.Tensor] = None, free_count: Optional[torch.Tensor] = None,
+                  n_pages: Optional[int] = None, out: Optional[KvPlan] = None, stream=None) -> KvPlan:
+    """Pages and slots for requests that are to hold new_len tokens instead of old_len.  block_table, free_pages and
+    free_count are brought up to date in place; without the latter two the table is taken as it is and n_pages says
+    which of its entries are pages (default: any that is not negative).  `out`: a KvPlan of the same sizes to write
+    into; its len_out may be old_len itself."""
+    given = {"free_pages": free_pages, "free_count": free_count}
+    given = {k: v for k, v in given.items() if v is not None}
+    _need(len(given) != 1, "free_pages and free_count go together")
+    _on_device(stream, old_len=old_len, new_len=new_len, block_table=block_table, **given)
+    _ints(old_len=old_len, new_len=new_len, block_table=block_table, **given)
+    _need(block_table.dim() == 2 and old_len.shape == new_len.shape == block_table.shape[:1], "lengths must be [B], block_table [B, pages]")
+    B, pps = block_table.shape
+    if given:
+        _need(free_pages.dim() == 1 and free_count.numel() == 1, "free_pages must be [n_pages], free_count one number")
+        _need(n_pages is None or n_pages == free_pages.numel(), "n_pages must be the size of free_pages")
+        n_pages = free_pages.numel()
+    elif n_pages is None:
+        n_pages = (2 ** 31 - 1) // max(1, page_tokens)
+    shapes = ((B + 1,), (max_rows,), (max_rows,), (max_rows,), (es_op_kv_plan_max_runs(B, max_rows, page_tokens),), (B,))
+    if out is None:
+        _need(max_rows > 0 and B > 0, "bad sizes")
+        out = KvPlan(*[_empty(stream, *s, dtype=torch.int32, device=old_len.device) for s in shapes])
+    else:
+        _on_device(stream, **out._asdict())
+        _ints(**out._asdict())
+        _need(all(t.shape == s for t, s in zip(out, shapes)), f"out must hold tensors of the shapes {shapes}")
+    _check(lib.es_op_kv_plan(_ptr(old_len), _ptr(new_len), _ptr(block_table), _ptr(free_pages), _ptr(free_count), B, pps,
+                             page_tokens, n_pages, max_rows, *[_ptr(t) for t in out], _stream_ptr(stream)))
+    return out
+
+
+def es_op_kv8_append(k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                     k_scale: torch.Tensor, v_scale: torch.Tensor, runs: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Writes rows k, v [n, Hkv, hd] (fp16 or bf16; evenly spaced, e.g. slices of a fused projection) into the 8-bit pages
+    at slot_map (at least n entries); `runs` as es_op_kv_plan gives it."""
+    extra = {} if runs is None else {"runs": runs}
+    _on_device(stream, k=k, v=v, slot_map=slot_map, k_pages=k_pages, v_pages=v_pages, k_scale=k_scale, v_scale=v_scale, **extra)
+    n_pages, Hkv, P, hd = _check_pool(k_pages, v_pages, k_scale, v_scale)
+    _ints(slot_map=slot_map, **extra)
+    _need(k.dim() == 3 and k.shape == v.shape and tuple(k.shape[1:]) == (Hkv, hd), "k and v must be [n, Hkv, hd]")
+    _need(k.dtype == v.dtype and k.dtype in (torch.float16, torch.bfloat16), "k and v must be fp16 or bf16, both the same")
+    n = k.shape[0]
+    _need(slot_map.numel() >= n, "slot_map must have an entry for every row")
+    stride = _row_stride(k, "k")
+    _need(n <= 1 or stride == _row_stride(v, "v"), "k and v must have the same row stride")
+    _row_stride(v, "v")
+    _check(lib.es_op_kv8_append(_ptr(k), _ptr(v), _VALUE_DTYPES[k.dtype], stride, n, _ptr(slot_map), _ptr(runs),
+                                0 if runs is None else runs.numel(), _ptr(k_pages), _ptr(v_pages), _CODE_DTYPES[k_pages.dtype],
+                                _ptr(k_scale), _ptr(v_scale), Hkv, hd, P, n_pages, _stream_ptr(stream)))
+
+
+def es_op_kv8_gather(slot_map: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scale: torch.Tensor,
+                     v_scale: torch.Tensor, dtype: torch.dtype = torch.float16, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
+                     stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(k, v) [n, Hkv, hd]: the cached rows at slot_map [n], zeros where a slot is no place."""
+    _on_device(stream, slot_map=slot_map, k_pages=k_pages, v_pages=v_pages, k_scale=k_scale, v_scale=v_scale)
+    n_pages, Hkv, P, hd = _check_pool(k_pages, v_pages, k_scale, v_scale)
+    _ints(slot_map=slot_map)
+    _need(dtype in _VALUE_DTYPES, "dtype must be fp16, bf16 or fp32")
+    n = slot_map.numel()
+    if out is None:
+        out = tuple(_empty(stream, n, Hkv, hd, dtype=dtype, device=k_pages.device) for _ in range(2))
+    else:
+        _on_device(stream, out_k=out[0], out_v=out[1])
+        for t in out:
+            _need(t.dtype == dtype and t.is_contiguous() and tuple(t.shape) == (n, Hkv, hd), "out must be two contiguous [n, Hkv, hd] tensors of dtype")
+    _check(lib.es_op_kv8_gather(_ptr(slot_map), n, _ptr(k_pages), _ptr(v_pages), _CODE_DTYPES[k_pages.dtype], _ptr(k_scale),
+                                _ptr(v_scale), Hkv, hd, P, n_pages, _ptr(out[0]), _ptr(out[1]), _VALUE_DTYPES[dtype], _stream_ptr(stream)))
+    return out
+
+
+def es_op_decode_attention_kv8_scratch_bytes(B: int, T: int, Hq: int, Hkv: int, hd: int, page_tokens: int, max_ctx: int) -> int:
+    return int(lib.es_op_decode_attention_kv8_scratch_bytes(B, T, Hq, Hkv, hd, page_tokens, max_ctx))
+
+
+def es_op_decode_attention_kv8(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scale: torch.Tensor,
+                               v_scale: torch.Tensor, block_table: torch.Tensor, ctx_len: torch.Tensor, max_ctx: int,
+                               scratch: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Attention of q [B, T, Hq, hd] (the T newest tokens of every sequence; [B, Hq, hd] for one) over the 8-bit pages;
+    returns [B, T, Hq * hd] (or [B, Hq * hd]) of q's type.  q's tokens may be evenly spaced slices of larger rows."""
+    _on_device(stream, q=q, k_pages=k_pages, v_pages=v_pages, k_scale=k_scale, v_scale=v_scale, block_table=block_table, ctx_len=ctx_len)
+    n_pages, Hkv, P, hd = _check_pool(k_pages, v_pages, k_scale, v_scale)
+    _ints(block_table=block_table, ctx_len=ctx_len)
+    _need(q.dim() in (3, 4) and q.shape[-1] == hd and q.dtype in (torch.float16, torch.bfloat16), "q must be fp16 or bf16 [B, T, Hq, hd] or [B, Hq, hd]")
+    B, T, Hq = q.shape[0], 1 if q.dim() == 3 else q.shape[1], q.shape[-2]
+    _need(block_table.dim() == 2 and block_table.shape[0] == B and tuple(ctx_len.shape) == (B,), "block_table must be [B, pages], ctx_len [B]")
+    stride = _row_stride(q, "q")
+    shape = (B, Hq * hd) if q.dim() == 3 else (B, T, Hq * hd)
+    extra = {k: t for k, t in (("scratch", scratch), ("out", out)) if t is not None}
+    _on_device(stream, **extra)
+    if scratch is None:
+        n = es_op_decode_attention_kv8_scratch_bytes(B, T, Hq, Hkv, hd, P, max_ctx)
+        scratch = _empty(stream, n, dtype=torch.uint8, device=q.device) if n else None
+    else:
+        _need(scratch.is_contiguous(), "scratch must be contiguous")
+    if out is None:
+        out = _empty(stream, *shape, dtype=q.dtype, device=q.device)
+    else:
+        _need(out.dtype == q.dtype and out.is_contiguous() and tuple(out.shape) == shape, f"out must be contiguous {shape} of q's type")
+    _check(lib.es_op_decode_attention_kv8(_ptr(q), _VALUE_DTYPES[q.dtype], stride, _ptr(k_pages), _ptr(v_pages), _CODE_DTYPES[k_pages.dtype],
+                                          _ptr(k_scale), _ptr(v_scale), _ptr(block_table), _ptr(ctx_len), _ptr(out), B, T, Hq, Hkv, hd, P,
+                                          block_table.shape[1], n_pages, max_ctx, _ptr(scratch),
+                                          0 if scratch is None else scratch.numel() * scratch.element_size(), _stream_ptr(stream)))
+    return out
+
+
+def es_op_sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+                 top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
+                 out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(tokens int32 [B], logprobs fp32 [B]) drawn from logits [B, V] (fp32, fp16 or bf16; rows may be spaced) with the random
+    numbers u [B] in [0, 1) and per-row settings [B]: temperature, top_p, min_p fp32, top_k int32; None = off."""
+    settings = {"temperature": temperature, "top_k": top_k, "top_p": top_p, "min_p": min_p}
+    given = {k: t for k, t in settings.items() if t is not None}
+    _on_device(stream, logits=logits, u=u, **given)
+    _need(logits.dim() == 2 and logits.dtype in _VALUE_DTYPES and (logits.stride(1) == 1 or logits.shape[1] == 1), "logits must be fp32, fp16 or bf16 [B, V] with dense rows")
+    B, V = logits.shape
+    for name, t in {"u": u, **given}.items():
+        want = torch.int32 if name == "top_k" else torch.float32
+        _need(t.dtype == want and t.is_contiguous() and tuple(t.shape) == (B,), f"{name} must be contiguous {want} [B]")
+    if out is None:
+        _need(B > 0, "bad sizes")
+        out = (_empty(stream, B, dtype=torch.int32, device=logits.device), _empty(stream, B, dtype=torch.float32, device=logits.device))
+    else:
+        _on_device(stream, out_tokens=out[0], out_logprobs=out[1])
+        for t, want in zip(out, (torch.int32, torch.float32)):
+            _need(t.dtype == want and t.is_contiguous() and tuple(t.shape) == (B,), f"out must be contiguous int32 [B] and fp32 [B]")
+    _check(lib.es_op_sample(_ptr(logits), _VALUE_DTYPES[logits.dtype], logits.stride(0) if B > 1 else V, _ptr(u), _ptr(temperature),
+                            _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(out[0]), _ptr(out[1]), B, V, _stream_ptr(stream)))
     return out
 
 

@@ -256,4 +256,8 @@ es_status_t launch_decode_attention(const DecodeAttnParams& p, cudaStream_t s, i
 bool decode_attention_mma_supported(const DecodeAttnParams& p);
 es_status_t launch_decode_attention_mma(const DecodeAttnParams& p, cudaStream_t s, bool pdl = false);
 
+// ---- 8-bit cache -----------------------------------------------------------------------------
+// Checks what all operations over an 8-bit page pool share; *code = CODE_I8 or CODE_E4M3 (kv8.cuh).
+es_status_t kv8_check_pool(int32_t code_dtype, int32_t Hkv, int32_t hd, int32_t page_tokens, int32_t n_pages, int* code);
+
 }  // namespace es

@@ -1,0 +1,357 @@
+// Writing K and V rows into the paged 8-bit cache, and reading them back.
+//
+// append: an item is one stretch of consecutive rows in one page, for one KV head and one of K / V.  A group of warps
+// takes an item: it finds the stretch's length in the slot map, takes the largest magnitude of its rows (as integers:
+// the bits of |x| order like the numbers, infinities and NaN above all), settles the page's scale, brings the codes in
+// front to it if it grew, and writes the new codes.  One group owns the page and head for the whole call, so nothing is
+// atomic and the result does not depend on scheduling.
+#include "es_internal.cuh"
+#include "kv8.cuh"
+#include "launch.cuh"
+
+namespace es {
+namespace {
+
+constexpr int APPEND_THREADS = 256;
+
+struct AppendParams {
+  const uint16_t *k, *v;
+  int64_t row_stride;
+  const int *slots, *runs;
+  int n_rows, n_items;             // n_items: runs, or rows where there are none
+  uint8_t *k_pages, *v_pages;
+  float *k_scale, *v_scale;
+  int Hkv, P, n_pages;
+};
+
+template <bool BF16>
+__device__ __forceinline__ float2 to_float2(uint32_t w) {
+  if (BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  return __half22float2(bits_h2(w));
+}
+
+// round(x / s) to nearest, ties to even, exactly: x * (1 / s) is within one of it, and the remainder x - q s is a
+// multiple of the last place of s no larger than s, so one fused multiply-add gives it without rounding.
+__device__ __forceinline__ int quotient_code(float x, float s, float inv) {
+  float q = rintf(x * inv);
+  const float r = fmaf(-q, s, x), twice = 2.f * fabsf(r);
+  if (twice > s || (twice == s && (((int)q) & 1))) q += r > 0.f ? 1.f : -1.f;
+  return (int)q;
+}
+
+__device__ __forceinline__ uint32_t e4m3_of(float x) { return __nv_cvt_float_to_fp8(x, __NV_SATFINITE, __NV_E4M3); }
+
+// 8 values at scale s -> 8 codes
+template <int CODE, bool BF16>
+__device__ __forceinline__ uint2 encode(const uint4& x, float s, float inv) {
+  const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+  uint32_t out[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float2 a = to_float2<BF16>(in[2 * i]), b = to_float2<BF16>(in[2 * i + 1]);
+    if (CODE == CODE_I8) {
+      const int c0 = quotient_code(a.x, s, inv), c1 = quotient_code(a.y, s, inv), c2 = quotient_code(b.x, s, inv),
+                c3 = quotient_code(b.y, s, inv);
+      out[i] = (c0 & 255) | ((c1 & 255) << 8) | ((c2 & 255) << 16) | ((uint32_t)c3 << 24);
+    } else {
+      const __nv_fp8x2_storage_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a.x * inv, a.y * inv), __NV_SATFINITE, __NV_E4M3);
+      const __nv_fp8x2_storage_t hi = __nv_cvt_float2_to_fp8x2(make_float2(b.x * inv, b.y * inv), __NV_SATFINITE, __NV_E4M3);
+      out[i] = (uint32_t)lo | ((uint32_t)hi << 16);
+    }
+  }
+  return make_uint2(out[0], out[1]);
+}
+
+// four codes at the old scale -> four codes at the new one
+template <int CODE>
+__device__ __forceinline__ uint32_t rescale(uint32_t w, double ratio) {
+  uint32_t out = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t c = (w >> (8 * i)) & 255u;
+    uint32_t n;
+    if (CODE == CODE_I8) {
+      n = (uint32_t)__double2int_rn((double)(int)(int8_t)c * ratio) & 255u;
+    } else {
+      const __half_raw h = __nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)c, __NV_E4M3);
+      n = e4m3_of(__half2float(__half(h)) * (float)ratio);
+    }
+    out |= n << (8 * i);
+  }
+  return out;
+}
+
+// the scale that a largest magnitude asks for
+template <int CODE>
+__device__ __forceinline__ float wanted_scale(float amax) {
+  if (CODE == CODE_I8) return fmaxf(__fdiv_rn(amax, 127.f), KV8_MIN_SCALE);
+  // smallest power of two s with amax <= 448 s = 1.75 * 2^8 s
+  const uint32_t bits = __float_as_uint(amax);
+  int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u);
+  e = e < -100 ? -100 : e;         // zero and subnormal magnitudes end here too
+  return __uint_as_float((uint32_t)(e + 127) << 23);
+}
+
+template <int WARPS>
+__device__ __forceinline__ void group_sync() { if (WARPS == 1) __syncwarp(); else __syncthreads(); }
+
+template <int HD, int CODE, bool BF16, int WARPS>
+__global__ void __launch_bounds__(APPEND_THREADS) kv8_append_kernel(const AppendParams p) {
+  constexpr int GROUP = 32 * WARPS;                // threads of an item
+  constexpr int CPR = HD / 8;                      // 16-byte pieces of a row
+  constexpr int KEEP = 4;                          // pieces a thread holds in registers between the two uses
+  __shared__ uint32_t s_max[APPEND_THREADS / 32];
+  __shared__ int s_len[APPEND_THREADS / 32];
+  const int tid = threadIdx.x % GROUP, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t item = (int64_t)blockIdx.x * (APPEND_THREADS / GROUP) + threadIdx.x / GROUP;
+  // heads change fastest: the groups of a CTA share rows of the slot map and read one row's heads side by side
+  const int h = (int)(item % p.Hkv);
+  const int64_t which = item / p.Hkv;
+  if (which >= p.n_items) return;                  // uniform over the group
+  const int r0 = p.runs ? p.runs[which] : (int)which;
+  if (r0 < 0 || r0 >= p.n_rows) return;
+  const int slot = p.slots[r0];
+  if (slot < 0 || slot >= p.n_pages * p.P) return;
+  const int page = slot / p.P, off = slot - page * p.P;
+  if (!p.runs && r0 > 0 && off > 0 && p.slots[r0 - 1] == slot - 1) return;      // inside a stretch
+
+  // ---- length of the stretch: the first row that does not follow on ----
+  const int most = min(p.P - off, p.n_rows - r0);
+  int len = most;
+  if (WARPS == 1) {
+    for (int i = 1; i < most; i += 32) {
+      const bool stop = i + lane < most && p.slots[r0 + i + lane] != slot + i + lane;
+      const unsigned m = __ballot_sync(~0u, stop);
+      if (m) { len = i + __ffs(m) - 1; break; }
+    }
+  } else {
+    if (tid == 0) s_len[0] = most;
+    __syncthreads();
+    for (int i = tid; i < most; i += GROUP)
+      if (p.slots[r0 + i] != slot + i) { atomicMin(s_len, i); break; }
+    __syncthreads();
+    len = s_len[0];
+  }
+
+  const uint16_t* src = (blockIdx.y ? p.v : p.k) + (int64_t)r0 * p.row_stride + (int64_t)h * HD;
+  uint8_t* dst = (blockIdx.y ? p.v_pages : p.k_pages) + ((int64_t)page * p.Hkv + h) * ((int64_t)p.P * HD);
+  float* scale = (blockIdx.y ? p.v_scale : p.k_scale) + (int64_t)page * p.Hkv + h;
+  const float s_old = off > 0 ? *scale : 0.f;
+  const int pieces = len * CPR;
+  auto piece = [&](int i) { return *reinterpret_cast<const uint4*>(src + (int64_t)(i / CPR) * p.row_stride + (i % CPR) * 8); };
+
+  // ---- largest magnitude ----
+  uint4 keep[KEEP];
+  uint32_t mx = 0;                                 // two 16-bit magnitudes
+  auto take = [&](const uint4& x) {
+    mx = __vmaxu2(mx, __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
+  };
+#pragma unroll
+  for (int j = 0; j < KEEP; ++j) {
+    keep[j] = make_uint4(0, 0, 0, 0);
+    if (tid + j * GROUP < pieces) keep[j] = piece(tid + j * GROUP);
+  }
+#pragma unroll
+  for (int j = 0; j < KEEP; ++j) take(keep[j]);
+  for (int i = tid + KEEP * GROUP; i < pieces; i += GROUP) take(piece(i));
+  mx = max(mx & 0xffffu, mx >> 16);
+  mx = __reduce_max_sync(~0u, mx);
+  if (WARPS > 1) {
+    if (lane == 0) s_max[warp] = mx;
+    __syncthreads();
+    mx = __reduce_max_sync(~0u, s_max[lane % WARPS]);
+  }
+
+  // ---- the page's scale ----
+  const bool finite = mx < (BF16 ? 0x7f80u : 0x7c00u);
+  const float amax = BF16 ? __uint_as_float(mx << 16) : __half2float(__ushort_as_half((unsigned short)mx));
+  const float want = wanted_scale<CODE>(amax);
+  float s = off > 0 ? (s_old >= want || isnan(s_old) ? s_old : want) : want;
+  if (!finite) s = __int_as_float(0x7fffffff);
+  const bool bad = isnan(s);
+  const float inv = bad ? 0.f : 1.f / s;
+
+  // ---- codes in front ----
+  if (off > 0 && !bad && s != s_old) {
+    const double ratio = (double)s_old / (double)s;
+    uint4* front = reinterpret_cast<uint4*>(dst);
+    for (int i = tid; i < off * HD / 16; i += GROUP) {
+      uint4 w = front[i];
+      w.x = rescale<CODE>(w.x, ratio); w.y = rescale<CODE>(w.y, ratio);
+      w.z = rescale<CODE>(w.z, ratio); w.w = rescale<CODE>(w.w, ratio);
+      front[i] = w;
+    }
+  }
+
+  // ---- new codes ----
+  uint2* to = reinterpret_cast<uint2*>(dst + (int64_t)off * HD);
+#pragma unroll
+  for (int j = 0; j < KEEP; ++j)
+    if (tid + j * GROUP < pieces) to[tid + j * GROUP] = bad ? make_uint2(0, 0) : encode<CODE, BF16>(keep[j], s, inv);
+  for (int i = tid + KEEP * GROUP; i < pieces; i += GROUP) to[i] = bad ? make_uint2(0, 0) : encode<CODE, BF16>(piece(i), s, inv);
+  group_sync<WARPS>();                             // every thread has read the old scale
+  if (tid == 0) *scale = s;
+}
+
+template <int HD, int CODE, bool BF16>
+es_status_t launch_append(const AppendParams& p, bool wide, cudaStream_t s) {
+  const int64_t items = (int64_t)p.n_items * p.Hkv;
+  const int64_t blocks = wide ? items : (items + APPEND_THREADS / 32 - 1) / (APPEND_THREADS / 32);
+  if (blocks > INT32_MAX) return fail(ES_ERR_RANGE, "too many (run, head) items for one launch");
+  const dim3 grid((unsigned)blocks, 2);
+  if (wide) kv8_append_kernel<HD, CODE, BF16, 8><<<grid, APPEND_THREADS, 0, s>>>(p);
+  else kv8_append_kernel<HD, CODE, BF16, 1><<<grid, APPEND_THREADS, 0, s>>>(p);
+  ES_CUDA_CHECK(cudaGetLastError());
+  return ES_OK;
+}
+
+// ---- reading back ----------------------------------------------------------------------------------------------
+
+constexpr int GATHER_THREADS = 256;
+
+struct GatherParams {
+  const int* slots;
+  const uint8_t *k_pages, *v_pages;
+  const float *k_scale, *v_scale;
+  void *k, *v;
+  int64_t n_items;                 // rows * Hkv * hd / 16
+  int Hkv, P, n_pages;
+};
+
+
+// 16 codes -> 16 values of the output type at dst + 16 * item
+template <int CODE, int OUT>
+__device__ __forceinline__ void store_values(void* dst, int64_t item, const uint4& w, float s) {
+  const uint32_t in[4] = {w.x, w.y, w.z, w.w};
+  float f[16];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t lo, hi;
+    codes_to_h2<CODE>(in[i], lo, hi);
+    const float2 a = __half22float2(bits_h2(lo)), b = __half22float2(bits_h2(hi));
+    f[4 * i] = a.x * s; f[4 * i + 1] = a.y * s; f[4 * i + 2] = b.x * s; f[4 * i + 3] = b.y * s;
+  }
+  if (OUT == ES_DTYPE_F32) {
+    float4* o = reinterpret_cast<float4*>(dst) + item * 4;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+  } else {
+    uint32_t r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (OUT == ES_DTYPE_F16) {
+        r[i] = h2_bits(__floats2half2_rn(f[2 * i], f[2 * i + 1]));
+      } else {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+        r[i] = *reinterpret_cast<const uint32_t*>(&b);
+      }
+    }
+    uint4* o = reinterpret_cast<uint4*>(dst) + item * 2;
+    o[0] = make_uint4(r[0], r[1], r[2], r[3]);
+    o[1] = make_uint4(r[4], r[5], r[6], r[7]);
+  }
+}
+
+// A thread takes 16 values of K and of V: 16-byte loads out of the pages (a row of a head is contiguous there), 32 bytes
+// out, neighbouring threads side by side in the output.
+template <int HD, int CODE, int OUT>
+__global__ void __launch_bounds__(GATHER_THREADS) kv8_gather_kernel(const GatherParams p) {
+  constexpr int PPR = HD / 16;
+  const int64_t item = (int64_t)blockIdx.x * GATHER_THREADS + threadIdx.x;
+  if (item >= p.n_items) return;
+  const int64_t rh = item / PPR;
+  const int part = (int)(item - rh * PPR);
+  const int64_t r = rh / p.Hkv;
+  const int h = (int)(rh - r * p.Hkv);
+  const int slot = p.slots[r];
+  uint4 a = make_uint4(0, 0, 0, 0), b = a;
+  float sa = 0.f, sb = 0.f;
+  if (slot >= 0 && slot < p.n_pages * p.P) {
+    const int page = slot / p.P, off = slot - page * p.P;
+    const int64_t ph = (int64_t)page * p.Hkv + h;
+    const int64_t at = (ph * p.P + off) * HD + part * 16;
+    a = __ldcs(reinterpret_cast<const uint4*>(p.k_pages + at));
+    b = __ldcs(reinterpret_cast<const uint4*>(p.v_pages + at));
+    sa = p.k_scale[ph];
+    sb = p.v_scale[ph];
+  }
+  store_values<CODE, OUT>(p.k, item, a, sa);
+  store_values<CODE, OUT>(p.v, item, b, sb);
+}
+
+template <int HD, int CODE>
+es_status_t launch_gather(const GatherParams& p, int out, cudaStream_t s) {
+  const int64_t blocks = (p.n_items + GATHER_THREADS - 1) / GATHER_THREADS;
+  if (blocks > INT32_MAX) return fail(ES_ERR_RANGE, "too many rows for one launch");
+  const dim3 grid((unsigned)blocks);
+  switch (out) {
+    case ES_DTYPE_F16: kv8_gather_kernel<HD, CODE, ES_DTYPE_F16><<<grid, GATHER_THREADS, 0, s>>>(p); break;
+    case ES_DTYPE_BF16: kv8_gather_kernel<HD, CODE, ES_DTYPE_BF16><<<grid, GATHER_THREADS, 0, s>>>(p); break;
+    default: kv8_gather_kernel<HD, CODE, ES_DTYPE_F32><<<grid, GATHER_THREADS, 0, s>>>(p);
+  }
+  ES_CUDA_CHECK(cudaGetLastError());
+  return ES_OK;
+}
+
+}  // namespace
+
+es_status_t kv8_check_pool(int32_t code_dtype, int32_t Hkv, int32_t hd, int32_t page_tokens, int32_t n_pages, int* code) {
+  if (!kv8_code_of(code_dtype, code)) return fail(ES_ERR_INVALID_ARG, "code_dtype must be ES_DTYPE_I8 or ES_DTYPE_F8E4M3");
+  if (Hkv <= 0 || hd <= 0 || page_tokens <= 0 || n_pages <= 0) return fail(ES_ERR_INVALID_ARG, "bad sizes");
+  if (hd != 64 && hd != 128) return fail(ES_ERR_SHAPE, "head_dim must be 64 or 128");
+  if (page_tokens < 16 || (page_tokens & (page_tokens - 1))) return fail(ES_ERR_SHAPE, "page_tokens must be a power of two >= 16");
+  if ((long long)n_pages * page_tokens > INT32_MAX) return fail(ES_ERR_RANGE, "n_pages * page_tokens exceeds 2^31 - 1");
+  return ES_OK;
+}
+
+}  // namespace es
+
+extern "C" {
+
+es_status_t es_op_kv8_append(const void* k, const void* v, int32_t dtype, int64_t row_stride, int32_t n_rows,
+                             const int32_t* slot_map, const int32_t* runs, int32_t n_runs, void* k_pages, void* v_pages,
+                             int32_t code_dtype, float* k_scale, float* v_scale, int32_t Hkv, int32_t hd,
+                             int32_t page_tokens, int32_t n_pages, void* stream) {
+  using namespace es;
+  int code = 0;
+  if (n_rows < 0 || n_runs < 0) return fail(ES_ERR_INVALID_ARG, "bad sizes");
+  if (dtype != ES_DTYPE_F16 && dtype != ES_DTYPE_BF16) return fail(ES_ERR_INVALID_ARG, "k and v must be fp16 or bf16");
+  ES_TRY(kv8_check_pool(code_dtype, Hkv, hd, page_tokens, n_pages, &code));
+  if (n_rows == 0 || (runs && n_runs == 0)) return ES_OK;
+  if (!k || !v || !slot_map || !k_pages || !v_pages || !k_scale || !v_scale) return fail(ES_ERR_INVALID_ARG, "null argument");
+  if (row_stride < (int64_t)Hkv * hd || row_stride % 8) return fail(ES_ERR_INVALID_ARG, "row_stride must be a multiple of 8, at least Hkv * hd");
+  if (((uintptr_t)k | (uintptr_t)v | (uintptr_t)k_pages | (uintptr_t)v_pages) % 16) return fail(ES_ERR_INVALID_ARG, "rows and pages must be 16-byte aligned");
+  AppendParams p{(const uint16_t*)k, (const uint16_t*)v, row_stride, slot_map, runs, n_rows, runs ? n_runs : n_rows,
+                 (uint8_t*)k_pages, (uint8_t*)v_pages, k_scale, v_scale, Hkv, page_tokens, n_pages};
+  // a warp per item where stretches are short on average (a decode step: one row each), eight warps where they are long
+  const bool wide = runs ? n_rows >= 8 * (int64_t)n_runs : false;
+  const bool bf16 = dtype == ES_DTYPE_BF16;
+  cudaStream_t s = (cudaStream_t)stream;
+  if (hd == 128) {
+    if (code == CODE_I8) return bf16 ? launch_append<128, CODE_I8, true>(p, wide, s) : launch_append<128, CODE_I8, false>(p, wide, s);
+    return bf16 ? launch_append<128, CODE_E4M3, true>(p, wide, s) : launch_append<128, CODE_E4M3, false>(p, wide, s);
+  }
+  if (code == CODE_I8) return bf16 ? launch_append<64, CODE_I8, true>(p, wide, s) : launch_append<64, CODE_I8, false>(p, wide, s);
+  return bf16 ? launch_append<64, CODE_E4M3, true>(p, wide, s) : launch_append<64, CODE_E4M3, false>(p, wide, s);
+}
+
+es_status_t es_op_kv8_gather(const int32_t* slot_map, int32_t n_rows, const void* k_pages, const void* v_pages,
+                             int32_t code_dtype, const float* k_scale, const float* v_scale, int32_t Hkv, int32_t hd,
+                             int32_t page_tokens, int32_t n_pages, void* k, void* v, int32_t dtype, void* stream) {
+  using namespace es;
+  int code = 0;
+  if (n_rows < 0) return fail(ES_ERR_INVALID_ARG, "bad sizes");
+  if (dtype != ES_DTYPE_F16 && dtype != ES_DTYPE_BF16 && dtype != ES_DTYPE_F32)
+    return fail(ES_ERR_INVALID_ARG, "k and v must be fp16, bf16 or fp32");
+  ES_TRY(kv8_check_pool(code_dtype, Hkv, hd, page_tokens, n_pages, &code));
+  if (n_rows == 0) return ES_OK;
+  if (!slot_map || !k_pages || !v_pages || !k_scale || !v_scale || !k || !v) return fail(ES_ERR_INVALID_ARG, "null argument");
+  if (((uintptr_t)k | (uintptr_t)v | (uintptr_t)k_pages | (uintptr_t)v_pages) % 16) return fail(ES_ERR_INVALID_ARG, "rows and pages must be 16-byte aligned");
+  GatherParams p{slot_map, (const uint8_t*)k_pages, (const uint8_t*)v_pages, k_scale, v_scale, k, v,
+                 (int64_t)n_rows * Hkv * (hd / 16), Hkv, page_tokens, n_pages};
+  cudaStream_t s = (cudaStream_t)stream;
+  if (hd == 128) return code == CODE_I8 ? launch_gather<128, CODE_I8>(p, dtype, s) : launch_gather<128, CODE_E4M3>(p, dtype, s);
+  return code == CODE_I8 ? launch_gather<64, CODE_I8>(p, dtype, s) : launch_gather<64, CODE_E4M3>(p, dtype, s);
+}
+
+}  // extern "C"

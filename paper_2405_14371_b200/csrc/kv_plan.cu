@@ -1,0 +1,276 @@
+// Block tables and slot maps from request lengths: page allocation, page return and the row layout of a batch in one
+// launch, without the host knowing any result.
+//
+// Everything is a prefix sum over the requests followed by independent writes:
+//   rows_b = max(new - old, 0), need_b / give_b = pages gained / given up, and with R = sum(give), `have` pages on the
+//   stack and avail = have + R:  b is served iff its inclusive row sum fits max_rows and its inclusive need sum fits avail.
+// Both sums only grow with b, so the served requests that take pages are a prefix and the pop number of a page is
+// the exclusive sum itself.  Pop i is entry avail - 1 - i of "the stack with the returned pages on it": a stack entry
+// below `have`, else a returned page, found by a search in the sums of give.  When pops exceed returns no stack entry
+// is written, and otherwise no stack entry is read, so pops and pushes need no order between them.
+//
+// One cluster does it all: every CTA scans the lengths for itself (a few KB out of L2, cheaper than handing sums around),
+// then the CTAs share the page work, meet once, and share the rows.  The meeting orders table writes before the rows
+// that read them, and the reads of returned entries before their clearing.  Small calls are bound by latency and run as
+// one CTA without remote barriers.
+#include <cooperative_groups.h>
+#include <limits.h>
+
+#include "es_internal.cuh"
+#include "launch.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace es {
+namespace {
+
+constexpr int PLAN_THREADS = 1024;
+constexpr int PLAN_WARPS = PLAN_THREADS / 32;
+constexpr int PLAN_MAX_B = 8192;
+
+struct PlanParams {
+  const int *old_len, *new_len;
+  int *table, *free_pages, *free_count;
+  int B, pps, P, n_pages, max_rows, max_runs;
+  int *row_offsets, *slot_map, *positions, *row_seq, *runs, *len_out;
+};
+
+struct Sums { long long give, rows, need; };
+
+__device__ __forceinline__ Sums add(const Sums& a, const Sums& b) { return {a.give + b.give, a.rows + b.rows, a.need + b.need}; }
+
+// inclusive scan over the block; `total` is the block's sum.  All threads call.
+__device__ __forceinline__ Sums block_scan(Sums v, Sums* warp_sums, Sums* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const Sums o = {__shfl_up_sync(~0u, v.give, d), __shfl_up_sync(~0u, v.rows, d), __shfl_up_sync(~0u, v.need, d)};
+    if (lane >= d) v = add(v, o);
+  }
+  if (lane == 31) warp_sums[warp] = v;
+  __syncthreads();
+  if (warp == 0) {
+    Sums w = warp_sums[lane];
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const Sums o = {__shfl_up_sync(~0u, w.give, d), __shfl_up_sync(~0u, w.rows, d), __shfl_up_sync(~0u, w.need, d)};
+      if (lane >= d) w = add(w, o);
+    }
+    warp_sums[lane] = w;
+  }
+  __syncthreads();
+  if (warp > 0) v = add(v, warp_sums[warp - 1]);
+  *total = warp_sums[PLAN_WARPS - 1];
+  __syncthreads();
+  return v;
+}
+
+__device__ __forceinline__ int block_scan_int(int v, int* warp_sums, int* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int o = __shfl_up_sync(~0u, v, d);
+    if (lane >= d) v += o;
+  }
+  if (lane == 31) warp_sums[warp] = v;
+  __syncthreads();
+  if (warp == 0) {
+    int w = warp_sums[lane];
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int o = __shfl_up_sync(~0u, w, d);
+      if (lane >= d) w += o;
+    }
+    warp_sums[lane] = w;
+  }
+  __syncthreads();
+  if (warp > 0) v += warp_sums[warp - 1];
+  *total = warp_sums[PLAN_WARPS - 1];
+  __syncthreads();
+  return v;
+}
+
+// the request that owns item i: the b with off[b] <= i < off[b + 1]; off[0] = 0, i < off[B]
+__device__ __forceinline__ int owner(const int* off, int B, int i) {
+  int lo = 0, hi = B;            // off[lo] <= i < off[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (off[mid] <= i) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+__device__ __forceinline__ int clip(long long v, int most) { return v < most ? (int)v : most; }
+
+__global__ void __launch_bounds__(PLAN_THREADS, 1) kv_plan_kernel(const PlanParams p) {
+  extern __shared__ int sm[];
+  __shared__ Sums warp_sums[PLAN_WARPS];
+  __shared__ int warp_ints[PLAN_WARPS];
+  const int B = p.B, P = p.P, tid = threadIdx.x;
+  int* s_old = sm;                 // [B]
+  int* s_new = s_old + B;          // [B]   the length to hold: the request's, or the old one when refused
+  int* row_off = s_new + B;        // [B + 1]
+  int* need_off = row_off + B + 1; // [B + 1]   served requests only
+  int* give_off = need_off + B + 1;
+  int* run_off = give_off + B + 1;
+  const int ranks = gridDim.x, rank = blockIdx.x;
+  const bool alloc = p.free_pages != nullptr;
+  const long long cap = (long long)p.pps * P;
+
+  // ---- the sums (every CTA for itself) ----
+  int have = 0;
+  if (alloc) { have = __ldcg(p.free_count); have = have < 0 ? 0 : min(have, p.n_pages); }
+  Sums carry = {0, 0, 0};
+  if (tid == 0) { row_off[0] = 0; need_off[0] = 0; give_off[0] = 0; run_off[0] = 0; }
+  for (int base = 0; base < B; base += PLAN_THREADS) {
+    const int b = base + tid;
+    int o = 0, n = 0;
+    if (b < B) { o = __ldcg(p.old_len + b); n = __ldcg(p.new_len + b); }
+    const bool ok = o >= 0 && o <= cap && n >= 0 && n <= cap;
+    const int oo = ok ? o : 0, nn = ok ? n : 0;
+    const int po = (int)(((long long)oo + P - 1) / P), pn = (int)(((long long)nn + P - 1) / P);
+    Sums v = {max(po - pn, 0), max(nn - oo, 0), max(pn - po, 0)}, total;
+    v = add(block_scan(v, warp_sums, &total), carry);
+    if (b < B) {
+      s_old[b] = o;
+      s_new[b] = ok ? n : o;
+      give_off[b + 1] = alloc ? clip(v.give, INT_MAX) : 0;
+      row_off[b + 1] = clip(v.rows, p.max_rows + 1);        // one more than there is room marks "does not fit"
+      need_off[b + 1] = clip(v.need, INT_MAX);
+    }
+    carry = add(carry, total);
+  }
+  const int given = alloc ? clip(carry.give, INT_MAX) : 0;
+  const long long avail = (long long)have + given;
+  __syncthreads();
+
+  // ---- who is served; the runs of the served ----
+  int runs_before = 0, taken = 0;
+  for (int base = 0; base < B; base += PLAN_THREADS) {
+    const int b = base + tid;
+    int n_runs = 0;
+    if (b < B) {
+      const int o = s_old[b], n = s_new[b];
+      if (n > o) {                                          // gains rows (a request with lengths out of range has n == o)
+        const bool need = (n - 1) / P > (o - 1 + P) / P - 1;       // last page wanted against last page held
+        const bool fits = row_off[b + 1] <= p.max_rows && (!alloc || !need || need_off[b + 1] <= avail);
+        if (fits) n_runs = (n - 1) / P - o / P + 1;
+        else s_new[b] = o;
+      }
+    }
+    int total;
+    n_runs = block_scan_int(n_runs, warp_ints, &total);
+    if (b < B) run_off[b + 1] = runs_before + n_runs;
+    runs_before += total;
+  }
+  __syncthreads();
+  // from here row_off is capped, and need_off counts the served only: they are a prefix of those that need pages
+  // (need sums beyond avail belong to refused requests; so do all needs behind the first row sum beyond max_rows)
+  {
+    int most = 0;
+    for (int b = tid; b < B; b += PLAN_THREADS)
+      if (s_new[b] > s_old[b] && need_off[b + 1] > need_off[b]) most = max(most, need_off[b + 1]);
+    most = __reduce_max_sync(~0u, most);
+    if ((tid & 31) == 0) warp_ints[tid >> 5] = most;
+    __syncthreads();
+    taken = alloc ? __reduce_max_sync(~0u, warp_ints[tid & 31]) : 0;
+  }
+  const int rows_all = min(row_off[B], p.max_rows);
+  const int stride = PLAN_THREADS * ranks, first = rank * PLAN_THREADS + tid;
+
+  // ---- pages: pops into the table, left-over returns onto the stack ----
+  auto returned = [&](int i) -> int {
+    const int b = owner(give_off, B, i);
+    const int entry = (int)(((long long)s_new[b] + P - 1) / P) + i - give_off[b];
+    return __ldcg(p.table + (int64_t)b * p.pps + entry);
+  };
+  if (alloc) {
+    for (int i = first; i < taken; i += stride) {
+      const long long v = avail - 1 - i;
+      const int page = v < have ? __ldcg(p.free_pages + v) : returned((int)(v - have));
+      const int b = owner(need_off, B, i);
+      const int entry = (int)(((long long)s_old[b] + P - 1) / P) + i - need_off[b];
+      p.table[(int64_t)b * p.pps + entry] = page;
+    }
+    for (int i = first; i < given - taken; i += stride)
+      if (have + (long long)i < p.n_pages) p.free_pages[have + i] = returned(i);
+  }
+
+  // ---- the CTAs meet: table entries written above are read below, returned entries read above are cleared below ----
+  if (ranks > 1) cg::this_cluster().sync(); else __syncthreads();
+
+  for (int i = first; i < given; i += stride) {
+    const int b = owner(give_off, B, i);
+    p.table[(int64_t)b * p.pps + (int)(((long long)s_new[b] + P - 1) / P) + i - give_off[b]] = -1;
+  }
+  if (alloc && first == 0) *p.free_count = (int)min(avail - taken, (long long)p.n_pages);
+  for (int b = first; b <= B; b += stride) p.row_offsets[b] = min(row_off[b], p.max_rows);
+  for (int b = first; b < B; b += stride) p.len_out[b] = s_new[b];
+  for (int i = first; i < p.max_runs; i += stride)
+    if (i >= runs_before) p.runs[i] = -1;
+  for (int r = first; r < p.max_rows; r += stride) {
+    int slot = -1, pos = -1, seq = -1;
+    if (r < rows_all) {
+      seq = owner(row_off, B, r);
+      const int o = s_old[seq];
+      pos = o + (r - row_off[seq]);
+      if (s_new[seq] > o) {
+        const int lp = pos / P, page = __ldcg(p.table + (int64_t)seq * p.pps + lp);
+        if (page >= 0 && page < p.n_pages) slot = page * P + (pos - lp * P);
+        if (pos == o || pos == lp * P) p.runs[run_off[seq] + lp - o / P] = slot >= 0 ? r : -1;
+      }
+    }
+    p.slot_map[r] = slot;
+    p.positions[r] = pos;
+    p.row_seq[r] = seq;
+  }
+}
+
+}  // namespace
+}  // namespace es
+
+extern "C" {
+
+int32_t es_op_kv_plan_max_runs(int32_t B, int32_t max_rows, int32_t page_tokens) {
+  if (B <= 0 || max_rows <= 0 || page_tokens <= 0) return 0;
+  const long long n = (long long)max_rows / page_tokens + 2LL * B;      // n rows of a request touch at most n / P + 2 pages
+  return (int32_t)(n < max_rows ? n : max_rows);
+}
+
+es_status_t es_op_kv_plan(const int32_t* old_len, const int32_t* new_len, int32_t* block_table, int32_t* free_pages,
+                          int32_t* free_count, int32_t B, int32_t pages_per_seq, int32_t page_tokens, int32_t n_pages,
+                          int32_t max_rows, int32_t* row_offsets, int32_t* slot_map, int32_t* positions,
+                          int32_t* row_seq, int32_t* runs, int32_t* len_out, void* stream) {
+  using namespace es;
+  if (!old_len || !new_len || !block_table || !row_offsets || !slot_map || !positions || !row_seq || !runs || !len_out)
+    return fail(ES_ERR_INVALID_ARG, "null argument");
+  if (!free_pages != !free_count) return fail(ES_ERR_INVALID_ARG, "free_pages and free_count go together");
+  if (B <= 0 || pages_per_seq <= 0 || page_tokens <= 0 || n_pages <= 0 || max_rows <= 0)
+    return fail(ES_ERR_INVALID_ARG, "bad sizes");
+  if (page_tokens < 16 || (page_tokens & (page_tokens - 1))) return fail(ES_ERR_SHAPE, "page_tokens must be a power of two >= 16");
+  if (B > PLAN_MAX_B) return fail(ES_ERR_RANGE, "B = %d exceeds %d requests", B, PLAN_MAX_B);
+  if ((long long)pages_per_seq * page_tokens > INT32_MAX || (long long)n_pages * page_tokens > INT32_MAX)
+    return fail(ES_ERR_RANGE, "pages_per_seq or n_pages times page_tokens exceeds 2^31 - 1");
+  if (max_rows == INT32_MAX) return fail(ES_ERR_RANGE, "max_rows must be below 2^31 - 1");
+  PlanParams p{old_len, new_len, block_table, free_pages, free_count, B, pages_per_seq, page_tokens, n_pages, max_rows,
+               es_op_kv_plan_max_runs(B, max_rows, page_tokens), row_offsets, slot_map, positions, row_seq, runs, len_out};
+  const size_t smem = (size_t)(6 * B + 4) * sizeof(int);
+  if (smem > 48 * 1024)
+    ES_CUDA_CHECK(cudaFuncSetAttribute(kv_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)((6 * PLAN_MAX_B + 4) * sizeof(int))));
+  const int ranks = max_rows <= 4096 ? 1 : 8;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ranks);
+  cfg.blockDim = dim3(PLAN_THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = (cudaStream_t)stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = ranks;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = ranks > 1 ? 1 : 0;
+  ES_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_plan_kernel, p));
+  return ES_OK;
+}
+
+}  // extern "C"
