@@ -1,15 +1,18 @@
 // Sampling the next token of every row of logits: temperature, top-k, top-p, min-p, one given random number per row.
 //
-// Nothing is sorted.  All three restrictions keep a prefix of the ranking, so each is a threshold (a key and, among equal
-// keys, a last index), found by descending the bits of the keys with sums over the elements of a bin: counts for top-k,
-// weights for top-p.  The draw is a search for a running weight in order of index.
+// No row is sorted.  Every restriction keeps a prefix of the ranking (by logit, equal ones by index), so each is a
+// threshold in that order, held as one 64-bit number, the logit's order-preserving bits above the complement of the
+// index.  A histogram over the distance from the largest logit (counts, and weights where top-p asks for them) says in
+// which bin a threshold lies; the few elements of that bin are collected, ranked and searched.  A bin with more elements
+// than the list takes (many equal logits) is descended by the bits of its keys instead.  The draw is a search for a
+// running weight in order of index.
 //
-// Weights are integers, w = round(2^44 exp2((x - max) log2(e) / temperature)) out of a 64-bit exponential, so every sum
-// is exact whatever its order: thresholds and tokens depend on the inputs alone, and the borders are as sharp as 2^-45
-// of the largest weight.
+// Weights are integers, w = round(2^44 exp2((x - max) log2(e) / temperature)) out of 64-bit arithmetic, so every sum
+// is exact whatever its order: thresholds and tokens depend on the inputs alone, and the borders are as sharp as the
+// exponential (2^-39).
 //
-// A row belongs to one CTA or to a cluster of 2, 4 or 8, each holding a slice of the row in shared memory as fp32: the
-// logits are read from HBM once, whatever the number of passes.
+// A row belongs to a cluster of 1 to 8 CTAs, each holding a slice of the row in shared memory as fp32: the logits are read
+// from HBM once, whatever the number of passes.
 #include <cooperative_groups.h>
 #include <limits.h>
 
@@ -28,8 +31,12 @@ constexpr int ST = 512;                       // threads of a CTA
 constexpr int SW = ST / 32;
 constexpr int CHUNK = 128;                    // elements a warp sums at a time: the grain of the search
 constexpr int MAX_CLUSTER = 8;
-constexpr int MAX_SLICE = 48 * 1024;          // elements of a slice: 192 KB and its chunk sums fit the 227 KB of a CTA
 constexpr int MAX_V = 262144;                 // 2^18 weights of 2^44 stay below 2^63
+constexpr int MAX_SLICE = MAX_V / MAX_CLUSTER;
+constexpr int NB = 1024;                      // bins of the histogram
+constexpr int LIST = 1024;                    // elements of a bin that are ranked directly
+constexpr double UNIT = 17592186044416.0;     // 2^44, the largest weight
+constexpr float REACH = 46.f;                 // weights further than this (log2) below the largest round to zero
 
 struct SampleParams {
   const void* logits;
@@ -42,16 +49,23 @@ struct SampleParams {
 };
 
 struct Shared {
-  u64 hist[256];
-  u64 comb[256];
   u64 total;                                  // this CTA's, read by the cluster
   u64 best;                                   // this CTA's largest (key, index)
   u64 warp_u64[SW];
+  uint32_t warp_u32[SW];
+  float least;                                // smallest finite logit
   int found;                                  // a chosen index, written into every CTA by the one that finds it
-  int pick_bin;
-  u64 pick_above, pick_here;
+  // written into every CTA by the first one
+  int pick_bin, pick_count;                   // a bin, and how many elements it holds
+  uint32_t pick_rank;                         // elements to keep of the bin
+  u64 pick_mass;                              // mass to reach within the bin
+  u64 pick_pair;                              // threshold found in the list
+  u64 all_mass;
+  int list_n;
+  u64 hist[256], comb[256];                   // descent by key bits
+  int digit;
+  u64 digit_above, digit_here;
 };
-
 // order-preserving integer of a float that is not NaN
 __device__ __forceinline__ uint32_t key_of(float x) {
   const uint32_t b = __float_as_uint(x);
@@ -74,25 +88,61 @@ __device__ __forceinline__ u64 warp_scan(u64 v) {        // inclusive
   return v;
 }
 
+// 2^f on [-1/2, 1/2] by the polynomial through 9 Chebyshev nodes: relative error below 2^-39.7.
+__device__ __forceinline__ double exp2_poly(double f) {
+  double v = 1.3255224878668817e-6;
+  v = fma(v, f, 1.53100794022492974e-5);
+  v = fma(v, f, 1.54034558524538394e-4);
+  v = fma(v, f, 1.33334505680006457e-3);
+  v = fma(v, f, 9.61812915940255819e-3);
+  v = fma(v, f, 5.55041094120593299e-2);
+  v = fma(v, f, 2.40226506958129882e-1);
+  v = fma(v, f, 6.93147180545933455e-1);
+  return fma(v, f, 1.0);
+}
+
+// f of the whole, f in [0, 1): the integer part of f * all, exactly, and whether something was left (f * 2^64 is an
+// integer for every fp32 f from 2^-40 on; a double cannot hold `all`)
+__device__ __forceinline__ u64 share_of(float f, u64 all, bool* more) {
+  const u64 fixed = (u64)((double)f * 18446744073709551616.0);
+  *more = fixed * all != 0;
+  return __umul64hi(fixed, all);
+}
+
+__device__ __forceinline__ u64 pair_key(uint32_t key, int index) { return ((u64)key << 32) | (uint32_t)~index; }
+
 // One row's working state; every method is called by all threads of the cluster.
 struct Row {
   float* x;                                   // slice in shared memory, padded with -infinity to a multiple of CHUNK
-  u64* csum;
+  u64* csum;                                  // [slice / CHUNK]
+  uint32_t *cnt, *part;                       // [NB] counts, [3][NB] weights in three fields of 15 bits
+  uint32_t* ccnt;                             // [NB] the cluster's counts   (first CTA)
+  u64* cmass;                                 // [NB] ... and weights
+  u64* list;                                  // [LIST] elements of a bin, over cnt and part (first CTA)
   Shared* sm;
   int n, first, ranks, rank;                  // padded elements, global index of the first, CTAs
-  float xmax;
+  float xmax, bin_scale;
   double c;                                   // log2(e) / temperature
-  uint32_t key;                               // kept: keys above `key`, and those equal to it up to index `cut`
-  int cut;
+  float cf;
+  u64 keep;                                   // kept: elements not below this in the ranking
   u64 least;                                  // ... whose weight is at least this
 
   __device__ __forceinline__ u64 weight(float v) const {
     if (v == xmax) return 1ull << 44;
+    // far below: zero without 64-bit work (also -infinity, and anything finite below an infinite maximum)
+    if (!(fmaf(v, 0.5f, -0.5f * xmax) * cf > -0.5f * REACH)) return 0;
     const double t = ((double)v - (double)xmax) * c;
-    if (!(t > -46.0)) return 0;               // also -infinity, and anything finite below an infinite maximum
-    return __double2ull_rn(exp2(t) * 17592186044416.0);
+    const double magic = 6755399441055744.0;  // 1.5 * 2^52: adding it rounds to an integer, which its low bits hold
+    const double r = t + magic;
+    const double f = t - (r - magic);
+    const double scale = __hiloint2double((1023 + 44 + __double2loint(r)) << 20, 0);      // -47 <= r <= 0
+    return (u64)__double_as_longlong(fma(exp2_poly(f), scale, 4503599627370496.0)) - 0x4330000000000000ull;
   }
-  __device__ __forceinline__ bool kept(uint32_t k, int i) const { return k > key || (k == key && i <= cut); }
+  __device__ __forceinline__ bool kept(float v, int i) const { return pair_key(key_of(v), i) >= keep; }
+  // bins grow with the distance from the largest logit; equal logits share one
+  __device__ __forceinline__ int bin_of(float v) const {
+    return v == xmax ? 0 : (int)fminf((xmax - v) * bin_scale, (float)(NB - 1));
+  }
 
   // chunk sums of f(value, index) in csum, the CTA's in sm->total; returns the cluster's
   template <class F>
@@ -193,19 +243,107 @@ struct Row {
           u64 r = inc - s;
           int j = 0;
           while (j < 7 && r + v[j] < target) r += v[j++];
-          sm->pick_bin = 255 - 8 * lane - j;
-          sm->pick_above = r;
-          sm->pick_here = v[j];
+          sm->digit = 255 - 8 * lane - j;
+          sm->digit_above = r;
+          sm->digit_here = v[j];
         }
       }
       __syncthreads();
-      prefix = (prefix << 8) | (uint32_t)sm->pick_bin;
-      run = sm->pick_above;
-      *here = sm->pick_here;
+      prefix = (prefix << 8) | (uint32_t)sm->digit;
+      run = sm->digit_above;
+      *here = sm->digit_here;
       __syncthreads();
     }
     *above = run;
     return prefix;
+  }
+
+  // Counts per bin, and weights where asked, summed over the cluster in the first CTA.
+  __device__ void histogram(bool mass) {
+    cg::cluster_group cl = cg::this_cluster();
+    for (int i = threadIdx.x; i < (mass ? 4 : 1) * NB; i += ST) cnt[i] = 0;         // part follows cnt
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += ST) {
+      const float v = x[i];
+      const int b = bin_of(v);
+      atomicAdd(&cnt[b], 1u);
+      if (mass) {
+        const u64 w = weight(v);
+        if (w) {
+          atomicAdd(&part[b], (uint32_t)w & 0x7fffu);
+          atomicAdd(&part[NB + b], (uint32_t)(w >> 15) & 0x7fffu);
+          atomicAdd(&part[2 * NB + b], (uint32_t)(w >> 30));
+        }
+      }
+    }
+    cl.sync();
+    uint32_t* to_cnt = cl.map_shared_rank(ccnt, 0);
+    u64* to_mass = cl.map_shared_rank(cmass, 0);
+    const int share = NB / ranks;
+    for (int i = threadIdx.x; i < share; i += ST) {
+      const int b = rank * share + i;
+      uint32_t k = 0;
+      u64 m = 0;
+      for (int r = 0; r < ranks; ++r) {
+        const uint32_t* c0 = cl.map_shared_rank(cnt, r);
+        k += c0[b];
+        if (mass) m += (u64)c0[NB + b] + ((u64)c0[2 * NB + b] << 15) + ((u64)c0[3 * NB + b] << 30);
+      }
+      to_cnt[b] = k;
+      to_mass[b] = m;
+    }
+    cl.sync();
+  }
+
+  // The first CTA: inclusive sums of its two bins a thread (bins 2 tid and 2 tid + 1).
+  __device__ __forceinline__ u64 scan_bins(u64 a) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    u64 inc = warp_scan(a);
+    if (lane == 31) sm->warp_u64[warp] = inc;
+    __syncthreads();
+    u64 before = 0;
+    for (int w = 0; w < warp; ++w) before += sm->warp_u64[w];
+    __syncthreads();
+    return before + inc;
+  }
+
+  __device__ __forceinline__ void publish(int bin, int count, uint32_t r, u64 mass) {       // by one thread
+    cg::cluster_group cl = cg::this_cluster();
+    for (int i = 0; i < ranks; ++i) {
+      Shared* to = cl.map_shared_rank(sm, i);
+      to->pick_bin = bin; to->pick_count = count; to->pick_rank = r; to->pick_mass = mass;
+    }
+  }
+
+  // The elements of bin `pick_bin` in the first CTA's list, in ranking order, padded with zeros to a power of two.
+  __device__ void collect() {
+    cg::cluster_group cl = cg::this_cluster();
+    const int bin = sm->pick_bin;
+    u64* to = cl.map_shared_rank(list, 0);
+    int* count = cl.map_shared_rank(&sm->list_n, 0);
+    for (int i = threadIdx.x; i < n; i += ST) {
+      const float v = x[i];
+      if (bin_of(v) == bin) {
+        const int at = atomicAdd(count, 1);
+        if (at < LIST) to[at] = pair_key(key_of(v), first + i);
+      }
+    }
+    cl.sync();
+    if (rank != 0) return;
+    const int m = min(sm->pick_count, LIST);
+    int size = 32;
+    while (size < m) size *= 2;
+    for (int i = m + threadIdx.x; i < size; i += ST) list[i] = 0;
+    __syncthreads();
+    for (int k = 2; k <= size; k *= 2)        // bitonic, descending
+      for (int j = k / 2; j > 0; j /= 2) {
+        for (int i = threadIdx.x; i < size / 2; i += ST) {
+          const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
+          const u64 a = list[lo], b = list[hi];
+          if ((a < b) == ((lo & k) == 0)) { list[lo] = b; list[hi] = a; }
+        }
+        __syncthreads();
+      }
   }
 };
 
@@ -218,8 +356,13 @@ __device__ __forceinline__ float load_logit(const void* p, int64_t i) {
   return isnan(x) ? -INFINITY : x + 0.f;      // -0 becomes +0: equal numbers have equal keys
 }
 
+__host__ __device__ constexpr size_t sample_smem(int slice) {
+  // logits, chunk sums, the CTA's histogram (later the list), the cluster's counts and weights
+  return (size_t)slice * 4 + (size_t)(slice / CHUNK) * 8 + (size_t)NB * 16 + (size_t)NB * 12;
+}
+
 template <int DT>
-__global__ void __launch_bounds__(ST) sample_kernel(const SampleParams p) {
+__global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
   extern __shared__ __align__(16) unsigned char dyn[];
   __shared__ Shared shared;
   cg::cluster_group cl = cg::this_cluster();
@@ -227,7 +370,12 @@ __global__ void __launch_bounds__(ST) sample_kernel(const SampleParams p) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   Row R;
   R.x = reinterpret_cast<float*>(dyn);
-  R.csum = reinterpret_cast<u64*>(dyn + (size_t)p.slice * sizeof(float));
+  R.cmass = reinterpret_cast<u64*>(dyn + (size_t)p.slice * 4);
+  R.list = R.cmass + NB;
+  R.cnt = reinterpret_cast<uint32_t*>(R.list);
+  R.part = R.cnt + NB;
+  R.ccnt = R.part + 3 * NB;
+  R.csum = reinterpret_cast<u64*>(R.ccnt + NB);
   R.sm = &shared;
   R.ranks = ranks;
   R.rank = rank;
@@ -235,107 +383,219 @@ __global__ void __launch_bounds__(ST) sample_kernel(const SampleParams p) {
   const int real = max(0, min(p.V - R.first, p.slice));
   R.n = (real + CHUNK - 1) / CHUNK * CHUNK;
 
-  // ---- the slice comes in; largest logit, lowest index ----
+  // ---- the slice comes in; largest logit at the lowest index, smallest finite one ----
   u64 best = 0;
-  for (int i = tid; i < R.n; i += ST) {
-    const float v = i < real ? load_logit<DT>(p.logits, (int64_t)row * p.row_stride + R.first + i) : -INFINITY;
-    R.x[i] = v;
-    const u64 b = ((u64)key_of(v) << 32) | (uint32_t)~(R.first + i);
-    best = b > best ? b : best;
+  float least = INFINITY;
+  const int64_t row_at = (int64_t)row * p.row_stride + R.first;
+  constexpr int FLIGHT = 8;                   // loads of a thread under way at a time
+  for (int base = 0; base < R.n; base += ST * FLIGHT) {
+    float v[FLIGHT];
+#pragma unroll
+    for (int j = 0; j < FLIGHT; ++j) {
+      const int i = base + j * ST + tid;
+      v[j] = i < real ? load_logit<DT>(p.logits, row_at + i) : -INFINITY;
+    }
+#pragma unroll
+    for (int j = 0; j < FLIGHT; ++j) {
+      const int i = base + j * ST + tid;
+      if (i < R.n) {
+        R.x[i] = v[j];
+        const u64 b = pair_key(key_of(v[j]), R.first + i);
+        best = b > best ? b : best;
+        if (v[j] > -INFINITY) least = fminf(least, v[j]);
+      }
+    }
   }
 #pragma unroll
-  for (int d = 16; d; d >>= 1) { const u64 o = __shfl_xor_sync(~0u, best, d); best = o > best ? o : best; }
-  if (lane == 0) shared.warp_u64[warp] = best;
+  for (int d = 16; d; d >>= 1) {
+    const u64 o = __shfl_xor_sync(~0u, best, d);
+    best = o > best ? o : best;
+    least = fminf(least, __shfl_xor_sync(~0u, least, d));
+  }
+  if (lane == 0) { shared.warp_u64[warp] = best; shared.warp_u32[warp] = __float_as_uint(least); }
   __syncthreads();
   if (warp == 0) {
     best = lane < SW ? shared.warp_u64[lane] : 0;
+    least = lane < SW ? __uint_as_float(shared.warp_u32[lane]) : INFINITY;
 #pragma unroll
-    for (int d = 16; d; d >>= 1) { const u64 o = __shfl_xor_sync(~0u, best, d); best = o > best ? o : best; }
-    if (lane == 0) shared.best = best;
+    for (int d = 16; d; d >>= 1) {
+      const u64 o = __shfl_xor_sync(~0u, best, d);
+      best = o > best ? o : best;
+      least = fminf(least, __shfl_xor_sync(~0u, least, d));
+    }
+    if (lane == 0) {
+      shared.best = best; shared.least = least; shared.list_n = 0;
+      shared.pick_bin = 0; shared.pick_count = 0; shared.pick_rank = 1; shared.pick_mass = 1; shared.pick_pair = 0;
+    }
   }
   cl.sync();
   best = 0;
-  for (int r = 0; r < ranks; ++r) { const u64 o = cl.map_shared_rank(&shared, r)->best; best = o > best ? o : best; }
+  least = INFINITY;
+  for (int r = 0; r < ranks; ++r) {
+    const Shared* o = cl.map_shared_rank(&shared, r);
+    best = o->best > best ? o->best : best;
+    least = fminf(least, o->least);
+  }
 
   R.xmax = of_key((uint32_t)(best >> 32));
   const int top = (int)~(uint32_t)best;
   const float T = p.temperature ? p.temperature[row] : 1.f;
-  int token = top;
-  float logprob = 0.f;
-  if (R.xmax == -INFINITY) {
-    token = -1;
-    logprob = -INFINITY;
-  } else if (T > 0.f) {
-    R.c = 1.4426950408889634 / (double)T;
-    R.key = 0; R.cut = INT_MAX; R.least = 1;
-    const int k = p.top_k ? p.top_k[row] : 0;
-    if (k > 0 && k < p.V) {
-      // padding is -infinity behind the last real index: it ranks last among equals
-      u64 above, here;
-      R.key = R.descend([](float, int) { return (u64)1; }, (u64)k, &above, &here);
-      const u64 want = (u64)k - above;
-      if (here > want) {
-        auto f = [&](float v, int) { return (u64)(key_of(v) == R.key); };
-        R.sums(f);
-        R.cut = R.find(f, want - 1);
-      }
-    }
-    auto f = [&](float v, int i) { return R.kept(key_of(v), i) ? R.weight(v) : 0ull; };
-    const float tp = p.top_p ? p.top_p[row] : 1.f;
-    if (tp < 1.f) {
-      const u64 all = R.sums(f);
-      cl.sync();
-      u64 target = (u64)ceil((double)fmaxf(tp, 0.f) * (double)all);
-      target = target < 1 ? 1 : target > all ? all : target;
-      u64 above, here;
-      const uint32_t key = R.descend(f, target, &above, &here);
-      const u64 w = R.weight(of_key(key));
-      const u64 want = (target - above + w - 1) / w;              // of the here / w kept ones with this key
-      int cut = key == R.key ? R.cut : INT_MAX;
-      if (want < here / w) {
-        auto tie = [&](float v, int i) { return (u64)(key_of(v) == key && i <= cut); };
-        R.sums(tie);
-        cut = R.find(tie, want - 1);
-      }
-      R.key = key;
-      R.cut = cut;
-    }
-    if (p.min_p) {
-      const float m = fminf(fmaxf(p.min_p[row], 0.f), 1.f);
-      const u64 w = (u64)ceil((double)m * 17592186044416.0);
-      R.least = w < 1 ? 1 : w;
-    }
-    auto last = [&](float v, int i) { const u64 w = R.kept(key_of(v), i) ? R.weight(v) : 0ull; return w >= R.least ? w : 0ull; };
-    const u64 all = R.sums(last);
-    const float u = fminf(fmaxf(p.u[row], 0.f), 1.f);
-    u64 target = (u64)((double)u * (double)all);
-    if (target >= all) target = all - 1;
-    token = R.find(last, target);
-    // the drawn token's own logit, from whichever CTA holds it
-    if (token >= R.first && token < R.first + real && tid == 0) {
-      const double t = R.x[token - R.first] == R.xmax ? 0.0 : ((double)R.x[token - R.first] - (double)R.xmax) * R.c;
-      logprob = (float)((t - log2((double)all) + 44.0) * 0.6931471805599453);
-      p.tokens[row] = token;
-      if (p.logprobs) p.logprobs[row] = logprob;
+  if (R.xmax == -INFINITY || !(T > 0.f)) {    // nothing to draw from, or no drawing
+    if (rank == 0 && tid == 0) {
+      p.tokens[row] = R.xmax == -INFINITY ? -1 : top;
+      if (p.logprobs) p.logprobs[row] = R.xmax == -INFINITY ? -INFINITY : 0.f;
     }
     cl.sync();                                // no CTA leaves while another may still read its shared memory
     return;
   }
-  if (rank == 0 && tid == 0) {
-    p.tokens[row] = token;
-    if (p.logprobs) p.logprobs[row] = logprob;
+  R.c = 1.4426950408889634 / (double)T;
+  R.cf = (float)R.c;
+  R.keep = 0;
+  R.least = 1;
+  const int k = p.top_k ? p.top_k[row] : 0;
+  const float tp = p.top_p ? p.top_p[row] : 1.f;
+  const bool by_count = k > 0 && k < p.V, by_mass = tp < 1.f;
+  if (by_count || by_mass) {
+    const float span = fminf(R.xmax - least, REACH / R.cf);
+    R.bin_scale = span > 0.f ? fminf((NB - 1) / span, 1e37f) : 0.f;
+    R.histogram(by_mass);
+    u64 counts = 0, masses = 0;               // first CTA: inclusive sums up to this thread's second bin
+    uint32_t c0 = 0, c1 = 0;
+    u64 m0 = 0, m1 = 0;
+    if (rank == 0) {
+      c0 = R.ccnt[2 * tid]; c1 = R.ccnt[2 * tid + 1];
+      counts = R.scan_bins((u64)c0 + c1);
+      if (by_mass) {
+        m0 = R.cmass[2 * tid]; m1 = R.cmass[2 * tid + 1];
+        masses = R.scan_bins(m0 + m1);
+        if (!by_count && tid == ST - 1) shared.all_mass = masses;
+      }
+    }
+    bool listed = false;                      // the list holds bin `pick_bin`
+    int listed_bin = -1;
+    if (by_count) {
+      if (rank == 0) {
+        const u64 a = counts - c0 - c1, b = counts - c1;
+        const bool one = a < (u64)k && (u64)k <= b, two = b < (u64)k && (u64)k <= counts;
+        if (one) { R.publish(2 * tid, (int)c0, (uint32_t)(k - a), 0); if (by_mass) shared.all_mass = masses - m0 - m1; }
+        if (two) { R.publish(2 * tid + 1, (int)c1, (uint32_t)(k - b), 0); if (by_mass) shared.all_mass = masses - m1; }
+      }
+      cl.sync();
+      const uint32_t want = shared.pick_rank;
+      if (shared.pick_count <= LIST) {
+        listed = true;
+        listed_bin = shared.pick_bin;
+        R.collect();
+        if (rank == 0) {
+          if (by_mass) {                      // mass of the first `want` of the bin joins that of the bins before
+            u64 s = 0;
+            for (uint32_t i = tid; i < want; i += ST) s += R.weight(of_key((uint32_t)(R.list[i] >> 32)));
+            s = warp_sum(s);
+            if (lane == 0) shared.warp_u64[warp] = s;
+            __syncthreads();
+            if (tid == 0) for (int w = 0; w < SW; ++w) shared.all_mass += shared.warp_u64[w];
+          }
+          if (tid < ranks) cl.map_shared_rank(&shared, tid)->pick_pair = R.list[want - 1];
+        }
+        cl.sync();
+        R.keep = shared.pick_pair;
+      } else {                                // too many for the list: by the bits of their keys
+        const int bin = shared.pick_bin;
+        u64 above, here;
+        const uint32_t key = R.descend([&](float v, int) { return (u64)(R.bin_of(v) == bin); }, want, &above, &here);
+        int cut = INT_MAX;
+        if (here > want - above) {
+          auto tie = [&](float v, int) { return (u64)(key_of(v) == key); };
+          R.sums(tie);
+          cut = R.find(tie, want - above - 1);
+        }
+        R.keep = ((u64)key << 32) | (cut == INT_MAX ? 0u : (uint32_t)~cut);
+        if (by_mass) {
+          const u64 s = R.sums([&](float v, int i) { return R.bin_of(v) == bin && R.kept(v, i) ? R.weight(v) : 0ull; });
+          cl.sync();
+          if (rank == 0 && tid == 0) shared.all_mass += s;
+        }
+      }
+    }
+    if (by_mass) {
+      if (rank == 0) {
+        __syncthreads();
+        const u64 all = shared.all_mass;
+        bool more;
+        u64 target = share_of(fmaxf(tp, 0.f), all, &more);
+        target += more;
+        target = target < 1 ? 1 : target > all ? all : target;
+        const u64 a = masses - m0 - m1, b = masses - m1;
+        if (a < target && target <= b) R.publish(2 * tid, (int)c0, 0, target - a);
+        if (b < target && target <= masses) R.publish(2 * tid + 1, (int)c1, 0, target - b);
+        if (tid == 0) shared.list_n = 0;
+      }
+      cl.sync();
+      const u64 target = shared.pick_mass;
+      if (shared.pick_count <= LIST) {
+        if (!listed || listed_bin != shared.pick_bin) R.collect();
+        if (rank == 0) {
+          u64 run = 0;
+          for (int base = 0; base < LIST; base += ST) {
+            const int i = base + tid;
+            const u64 pr = i < shared.pick_count ? R.list[i] : 0;
+            const u64 w = i < shared.pick_count ? R.weight(of_key((uint32_t)(pr >> 32))) : 0;
+            const u64 inc = run + R.scan_bins(w);
+            if (inc - w < target && target <= inc)
+              for (int r = 0; r < ranks; ++r) cl.map_shared_rank(&shared, r)->pick_pair = pr;
+            if (tid == ST - 1) shared.total = inc;
+            __syncthreads();
+            run = shared.total;
+            __syncthreads();
+          }
+        }
+        cl.sync();
+        R.keep = shared.pick_pair > R.keep ? shared.pick_pair : R.keep;
+      } else {
+        const int bin = shared.pick_bin;
+        u64 above, here;
+        const uint32_t key = R.descend([&](float v, int) { return R.bin_of(v) == bin ? R.weight(v) : 0ull; }, target, &above, &here);
+        const u64 w = R.weight(of_key(key));
+        const u64 want = (target - above + w - 1) / w;            // of the here / w elements with this key
+        int cut = INT_MAX;
+        if (want < here / w) {
+          auto tie = [&](float v, int) { return (u64)(key_of(v) == key); };
+          R.sums(tie);
+          cut = R.find(tie, want - 1);
+        }
+        const u64 pr = ((u64)key << 32) | (cut == INT_MAX ? 0u : (uint32_t)~cut);
+        R.keep = pr > R.keep ? pr : R.keep;
+      }
+    }
   }
-  cl.sync();
+  if (p.min_p) {
+    const float m = fminf(fmaxf(p.min_p[row], 0.f), 1.f);
+    const u64 w = (u64)ceil((double)m * UNIT);
+    R.least = w < 1 ? 1 : w;
+  }
+  auto last = [&](float v, int i) { const u64 w = R.kept(v, i) ? R.weight(v) : 0ull; return w >= R.least ? w : 0ull; };
+  const u64 all = R.sums(last);
+  const float u = fminf(fmaxf(p.u[row], 0.f), 1.f);
+  bool more;
+  u64 target = u < 1.f ? share_of(u, all, &more) : all;
+  if (target >= all) target = all - 1;
+  const int token = R.find(last, target);
+  // the drawn token's own logit, from whichever CTA holds it
+  if (token >= R.first && token < R.first + real && tid == 0) {
+    const float v = R.x[token - R.first];
+    const double t = v == R.xmax ? 0.0 : ((double)v - (double)R.xmax) * R.c;
+    p.tokens[row] = token;
+    if (p.logprobs) p.logprobs[row] = (float)((t - log2((double)all) + 44.0) * 0.6931471805599453);
+  }
 }
 
 template <int DT>
 es_status_t launch_sample(const SampleParams& p, int B, int ranks, cudaStream_t s) {
-  const size_t smem = (size_t)p.slice * sizeof(float) + (size_t)(p.slice / CHUNK) * sizeof(u64);
-  ES_CUDA_CHECK(cudaFuncSetAttribute(sample_kernel<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SLICE * 4 + MAX_SLICE / CHUNK * 8));
+  ES_CUDA_CHECK(cudaFuncSetAttribute(sample_kernel<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sample_smem(MAX_SLICE)));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((long long)B * ranks));
   cfg.blockDim = dim3(ST);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = sample_smem(p.slice);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -362,10 +622,10 @@ es_status_t es_op_sample(const void* logits, int32_t dtype, int64_t row_stride, 
   if (row_stride < V) return fail(ES_ERR_INVALID_ARG, "row_stride is smaller than V");
   if (V > MAX_V) return fail(ES_ERR_RANGE, "V = %d exceeds %d", V, MAX_V);
   if (B > (1 << 24)) return fail(ES_ERR_RANGE, "too many rows");
-  // a cluster per row while the machine has CTAs to spare and slices stay above 4096 elements, or where one CTA cannot
-  // hold the row
+  // slices of at most 16384 elements (two CTAs share an SM then: one works while the other's logits arrive), and smaller
+  // ones while the machine has room for more CTAs
   int ranks = 1;
-  while (ranks < MAX_CLUSTER && (V > (long long)ranks * MAX_SLICE || (2LL * B * ranks <= sm_count() && V > 4096 * ranks))) ranks *= 2;
+  while (ranks < MAX_CLUSTER && (V > 16384LL * ranks || ((long long)B * ranks < sm_count() && V > 2048 * ranks))) ranks *= 2;
   const int slice = ((V + ranks - 1) / ranks + CHUNK - 1) / CHUNK * CHUNK;
   SampleParams p{logits, row_stride, u, temperature, top_p, min_p, top_k, tokens, logprobs, V, slice};
   cudaStream_t s = (cudaStream_t)stream;
