@@ -430,52 +430,76 @@ def es_op_decode_attention_static(q: torch.Tensor, k_pages: torch.Tensor, v_page
 _VALUE_DTYPES = {torch.float16: ES_DTYPE_F16, torch.bfloat16: ES_DTYPE_BF16, torch.float32: ES_DTYPE_F32}
 _CODE_DTYPES = {torch.int8: ES_DTYPE_I8, torch.float8_e4m3fn: ES_DTYPE_F8E4M3}
 
-
-def _need(ok: bool, message: str) -> None:
-    if not ok:
-        raise EsError(1, message)
+# A decode step calls these once per layer, so their checks run on what costs least to ask of a tensor, and messages are
+# put together only once something is wrong.
 
 
-def _on_device(stream, **tensors) -> None:
-    """All tensors on the current device (the library launches there) and the stream too."""
-    for name, t in tensors.items():
-        _need(isinstance(t, torch.Tensor) and t.is_cuda, f"{name} must be a CUDA tensor")
-    dev = torch.cuda.current_device()
-    for name, t in tensors.items():
-        _need(t.device.index == dev, f"{name} is on {t.device}, the current device is cuda:{dev}")
-    if stream is not None:
-        _need(stream.device.index == dev, f"the stream is on {stream.device}, the current device is cuda:{dev}")
+def _refuse(message: str):
+    raise EsError(1, message)
 
 
-def _ints(**tensors) -> None:
-    for name, t in tensors.items():
-        _need(t.dtype == torch.int32 and t.is_contiguous(), f"{name} must be a contiguous int32 tensor")
+def _launch_on(stream, names: str, *tensors) -> int:
+    """The raw stream to launch on.  All tensors (None = not given) and the stream must be on the current device, where
+    the library launches."""
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            dev = -1
+    if dev < 0:
+        listed = ", ".join(f"{n}: {t.device}" for n, t in zip(names.split(), tensors) if t is not None)
+        _refuse(f"all tensors must be on one CUDA device ({listed})")
+    if dev != torch.cuda.current_device():
+        _refuse(f"{names.split()[0]} is on cuda:{dev}, the current device is cuda:{torch.cuda.current_device()}")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device.index != dev:
+        _refuse(f"the stream is on {stream.device}, the current device is cuda:{dev}")
+    return int(stream.cuda_stream)
 
 
-def _empty(stream, *shape, dtype, device) -> torch.Tensor:
+def _ints(names: str, *tensors) -> None:
+    for i, t in enumerate(tensors):
+        if t is not None and not (t.dtype is torch.int32 and t.is_contiguous()):
+            _refuse(f"{names.split()[i]} must be a contiguous int32 tensor")
+
+
+def _empty(stream, shape, dtype, like) -> torch.Tensor:
     """Memory for a call on `stream`: the allocator must know the stream it is used on."""
-    with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream()):
-        return torch.empty(*shape, dtype=dtype, device=device)
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
 
 
-def _check_pool(k_pages, v_pages, k_scale, v_scale) -> Tuple[int, int, int, int]:
-    _need(k_pages.dim() == 4 and k_pages.shape == v_pages.shape, "k_pages and v_pages must be [n_pages, Hkv, P, hd] of one shape")
-    _need(k_pages.dtype in _CODE_DTYPES and v_pages.dtype == k_pages.dtype, "pages must be int8 or float8_e4m3fn, both the same")
-    _need(k_pages.is_contiguous() and v_pages.is_contiguous(), "pages must be contiguous")
-    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
-        _need(t.dtype == torch.float32 and t.is_contiguous() and t.shape == k_pages.shape[:2], f"{name} must be contiguous fp32 [n_pages, Hkv]")
-    return tuple(k_pages.shape)
+def _check_pool(k_pages, v_pages, k_scale, v_scale):
+    shape = k_pages.shape
+    if len(shape) != 4 or v_pages.shape != shape:
+        _refuse("k_pages and v_pages must be [n_pages, Hkv, P, hd] of one shape")
+    if k_pages.dtype not in _CODE_DTYPES or v_pages.dtype is not k_pages.dtype:
+        _refuse("pages must be int8 or float8_e4m3fn, both the same")
+    if not (k_pages.is_contiguous() and v_pages.is_contiguous()):
+        _refuse("pages must be contiguous")
+    for t in (k_scale, v_scale):
+        if t.dtype is not torch.float32 or not t.is_contiguous() or t.shape != shape[:2]:
+            _refuse("k_scale and v_scale must be contiguous fp32 [n_pages, Hkv]")
+    return shape
 
 
 def _row_stride(t: torch.Tensor, name: str) -> int:
     """Elements from row to row of [..., heads, hd] whose last two dimensions are dense and whose leading ones, if
     several, step evenly: a slice of a fused projection's output is such a tensor."""
-    heads, hd = t.shape[-2:]
-    _need(t.stride(-1) == 1 and (t.stride(-2) == hd or heads == 1), f"the heads of a row of {name} must be contiguous")
-    lead = [(n, s) for n, s in zip(t.shape[:-2], t.stride()[:-2]) if n != 1]
-    for (_, outer), (n, inner) in zip(lead, lead[1:]):
-        _need(outer == n * inner, f"the rows of {name} must be evenly spaced")
-    return lead[-1][1] if lead else heads * hd
+    shape, stride = t.shape, t.stride()
+    if stride[-1] != 1 or (stride[-2] != shape[-1] and shape[-2] != 1):
+        _refuse(f"the heads of a row of {name} must be contiguous")
+    step = 0                        # of the innermost leading dimension with more than one entry
+    span = 0                        # what the next one outwards has to step by
+    for i in range(len(shape) - 3, -1, -1):
+        if shape[i] != 1:
+            if span and stride[i] != span:
+                _refuse(f"the rows of {name} must be evenly spaced")
+            step = step or stride[i]
+            span = stride[i] * shape[i]
+    return step or shape[-1] * shape[-2]
 
 
 class KvPlan(NamedTuple):
@@ -499,29 +523,35 @@ def es_op_kv_plan(old_len: torch.Tensor, new_len: torch.Tensor, block_table: tor
     free_count are brought up to date in place; without the latter two the table is taken as it is and n_pages says
     which of its entries are pages (default: any that is not negative).  `out`: a KvPlan of the same sizes to write
     into; its len_out may be old_len itself."""
-    given = {"free_pages": free_pages, "free_count": free_count}
-    given = {k: v for k, v in given.items() if v is not None}
-    _need(len(given) != 1, "free_pages and free_count go together")
-    _on_device(stream, old_len=old_len, new_len=new_len, block_table=block_table, **given)
-    _ints(old_len=old_len, new_len=new_len, block_table=block_table, **given)
-    _need(block_table.dim() == 2 and old_len.shape == new_len.shape == block_table.shape[:1], "lengths must be [B], block_table [B, pages]")
-    B, pps = block_table.shape
-    if given:
-        _need(free_pages.dim() == 1 and free_count.numel() == 1, "free_pages must be [n_pages], free_count one number")
-        _need(n_pages is None or n_pages == free_pages.numel(), "n_pages must be the size of free_pages")
+    if (free_pages is None) != (free_count is None):
+        _refuse("free_pages and free_count go together")
+    raw = _launch_on(stream, "old_len new_len block_table free_pages free_count", old_len, new_len, block_table, free_pages, free_count)
+    _ints("old_len new_len block_table free_pages free_count", old_len, new_len, block_table, free_pages, free_count)
+    shape = block_table.shape
+    if len(shape) != 2 or old_len.shape != shape[:1] or new_len.shape != shape[:1]:
+        _refuse("lengths must be [B], block_table [B, pages]")
+    B, pps = shape
+    if free_pages is not None:
+        if free_pages.dim() != 1 or free_count.numel() != 1:
+            _refuse("free_pages must be [n_pages], free_count one number")
+        if n_pages is not None and n_pages != free_pages.numel():
+            _refuse("n_pages must be the size of free_pages")
         n_pages = free_pages.numel()
     elif n_pages is None:
         n_pages = (2 ** 31 - 1) // max(1, page_tokens)
-    shapes = ((B + 1,), (max_rows,), (max_rows,), (max_rows,), (es_op_kv_plan_max_runs(B, max_rows, page_tokens),), (B,))
+    max_runs = es_op_kv_plan_max_runs(B, max_rows, page_tokens)
     if out is None:
-        _need(max_rows > 0 and B > 0, "bad sizes")
-        out = KvPlan(*[_empty(stream, *s, dtype=torch.int32, device=old_len.device) for s in shapes])
+        if max_rows <= 0 or B <= 0:
+            _refuse("bad sizes")
+        sizes = [B + 1, max_rows, max_rows, max_rows, max_runs, B]
+        out = KvPlan(*_empty(stream, sum(sizes), torch.int32, old_len).split(sizes))
     else:
-        _on_device(stream, **out._asdict())
-        _ints(**out._asdict())
-        _need(all(t.shape == s for t, s in zip(out, shapes)), f"out must hold tensors of the shapes {shapes}")
-    _check(lib.es_op_kv_plan(_ptr(old_len), _ptr(new_len), _ptr(block_table), _ptr(free_pages), _ptr(free_count), B, pps,
-                             page_tokens, n_pages, max_rows, *[_ptr(t) for t in out], _stream_ptr(stream)))
+        _launch_on(stream, " ".join(KvPlan._fields), *out)
+        _ints(" ".join(KvPlan._fields), *out)
+        if [tuple(t.shape) for t in out] != [(B + 1,), (max_rows,), (max_rows,), (max_rows,), (max_runs,), (B,)]:
+            _refuse(f"out must hold tensors of {B + 1}, {max_rows}, {max_rows}, {max_rows}, {max_runs} and {B} entries")
+    _check(lib.es_op_kv_plan(old_len.data_ptr(), new_len.data_ptr(), block_table.data_ptr(), _ptr(free_pages), _ptr(free_count), B, pps,
+                             page_tokens, n_pages, max_rows, *[t.data_ptr() for t in out], raw))
     return out
 
 
@@ -529,39 +559,43 @@ def es_op_kv8_append(k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor, k
                      k_scale: torch.Tensor, v_scale: torch.Tensor, runs: Optional[torch.Tensor] = None, stream=None) -> None:
     """Writes rows k, v [n, Hkv, hd] (fp16 or bf16; evenly spaced, e.g. slices of a fused projection) into the 8-bit pages
     at slot_map (at least n entries); `runs` as es_op_kv_plan gives it."""
-    extra = {} if runs is None else {"runs": runs}
-    _on_device(stream, k=k, v=v, slot_map=slot_map, k_pages=k_pages, v_pages=v_pages, k_scale=k_scale, v_scale=v_scale, **extra)
+    raw = _launch_on(stream, "k v slot_map k_pages v_pages k_scale v_scale runs", k, v, slot_map, k_pages, v_pages, k_scale, v_scale, runs)
     n_pages, Hkv, P, hd = _check_pool(k_pages, v_pages, k_scale, v_scale)
-    _ints(slot_map=slot_map, **extra)
-    _need(k.dim() == 3 and k.shape == v.shape and tuple(k.shape[1:]) == (Hkv, hd), "k and v must be [n, Hkv, hd]")
-    _need(k.dtype == v.dtype and k.dtype in (torch.float16, torch.bfloat16), "k and v must be fp16 or bf16, both the same")
-    n = k.shape[0]
-    _need(slot_map.numel() >= n, "slot_map must have an entry for every row")
+    _ints("slot_map runs", slot_map, runs)
+    n = k.shape[0] if k.dim() else 0
+    if k.shape != (n, Hkv, hd) or v.shape != k.shape:
+        _refuse("k and v must be [n, Hkv, hd]")
+    if k.dtype not in _VALUE_DTYPES or k.dtype is torch.float32 or v.dtype is not k.dtype:
+        _refuse("k and v must be fp16 or bf16, both the same")
+    if slot_map.numel() < n:
+        _refuse("slot_map must have an entry for every row")
     stride = _row_stride(k, "k")
-    _need(n <= 1 or stride == _row_stride(v, "v"), "k and v must have the same row stride")
-    _row_stride(v, "v")
-    _check(lib.es_op_kv8_append(_ptr(k), _ptr(v), _VALUE_DTYPES[k.dtype], stride, n, _ptr(slot_map), _ptr(runs),
-                                0 if runs is None else runs.numel(), _ptr(k_pages), _ptr(v_pages), _CODE_DTYPES[k_pages.dtype],
-                                _ptr(k_scale), _ptr(v_scale), Hkv, hd, P, n_pages, _stream_ptr(stream)))
+    if stride != _row_stride(v, "v"):
+        _refuse("k and v must have the same row stride")
+    _check(lib.es_op_kv8_append(k.data_ptr(), v.data_ptr(), _VALUE_DTYPES[k.dtype], stride, n, slot_map.data_ptr(), _ptr(runs),
+                                0 if runs is None else runs.numel(), k_pages.data_ptr(), v_pages.data_ptr(), _CODE_DTYPES[k_pages.dtype],
+                                k_scale.data_ptr(), v_scale.data_ptr(), Hkv, hd, P, n_pages, raw))
 
 
 def es_op_kv8_gather(slot_map: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scale: torch.Tensor,
                      v_scale: torch.Tensor, dtype: torch.dtype = torch.float16, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
                      stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(k, v) [n, Hkv, hd]: the cached rows at slot_map [n], zeros where a slot is no place."""
-    _on_device(stream, slot_map=slot_map, k_pages=k_pages, v_pages=v_pages, k_scale=k_scale, v_scale=v_scale)
+    raw = _launch_on(stream, "slot_map k_pages v_pages k_scale v_scale", slot_map, k_pages, v_pages, k_scale, v_scale)
     n_pages, Hkv, P, hd = _check_pool(k_pages, v_pages, k_scale, v_scale)
-    _ints(slot_map=slot_map)
-    _need(dtype in _VALUE_DTYPES, "dtype must be fp16, bf16 or fp32")
+    _ints("slot_map", slot_map)
+    if dtype not in _VALUE_DTYPES:
+        _refuse("dtype must be fp16, bf16 or fp32")
     n = slot_map.numel()
     if out is None:
-        out = tuple(_empty(stream, n, Hkv, hd, dtype=dtype, device=k_pages.device) for _ in range(2))
+        out = tuple(_empty(stream, (2, n, Hkv, hd), dtype, k_pages).unbind())
     else:
-        _on_device(stream, out_k=out[0], out_v=out[1])
+        _launch_on(stream, "out[0] out[1]", *out)
         for t in out:
-            _need(t.dtype == dtype and t.is_contiguous() and tuple(t.shape) == (n, Hkv, hd), "out must be two contiguous [n, Hkv, hd] tensors of dtype")
-    _check(lib.es_op_kv8_gather(_ptr(slot_map), n, _ptr(k_pages), _ptr(v_pages), _CODE_DTYPES[k_pages.dtype], _ptr(k_scale),
-                                _ptr(v_scale), Hkv, hd, P, n_pages, _ptr(out[0]), _ptr(out[1]), _VALUE_DTYPES[dtype], _stream_ptr(stream)))
+            if t.dtype is not dtype or not t.is_contiguous() or t.shape != (n, Hkv, hd):
+                _refuse("out must be two contiguous [n, Hkv, hd] tensors of dtype")
+    _check(lib.es_op_kv8_gather(slot_map.data_ptr(), n, k_pages.data_ptr(), v_pages.data_ptr(), _CODE_DTYPES[k_pages.dtype], k_scale.data_ptr(),
+                                v_scale.data_ptr(), Hkv, hd, P, n_pages, out[0].data_ptr(), out[1].data_ptr(), _VALUE_DTYPES[dtype], raw))
     return out
 
 
@@ -574,29 +608,31 @@ def es_op_decode_attention_kv8(q: torch.Tensor, k_pages: torch.Tensor, v_pages: 
                                scratch: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention of q [B, T, Hq, hd] (the T newest tokens of every sequence; [B, Hq, hd] for one) over the 8-bit pages;
     returns [B, T, Hq * hd] (or [B, Hq * hd]) of q's type.  q's tokens may be evenly spaced slices of larger rows."""
-    _on_device(stream, q=q, k_pages=k_pages, v_pages=v_pages, k_scale=k_scale, v_scale=v_scale, block_table=block_table, ctx_len=ctx_len)
+    raw = _launch_on(stream, "q k_pages v_pages k_scale v_scale block_table ctx_len scratch out", q, k_pages, v_pages, k_scale, v_scale, block_table,
+                     ctx_len, scratch, out)
     n_pages, Hkv, P, hd = _check_pool(k_pages, v_pages, k_scale, v_scale)
-    _ints(block_table=block_table, ctx_len=ctx_len)
-    _need(q.dim() in (3, 4) and q.shape[-1] == hd and q.dtype in (torch.float16, torch.bfloat16), "q must be fp16 or bf16 [B, T, Hq, hd] or [B, Hq, hd]")
-    B, T, Hq = q.shape[0], 1 if q.dim() == 3 else q.shape[1], q.shape[-2]
-    _need(block_table.dim() == 2 and block_table.shape[0] == B and tuple(ctx_len.shape) == (B,), "block_table must be [B, pages], ctx_len [B]")
+    _ints("block_table ctx_len", block_table, ctx_len)
+    shape = q.shape
+    if len(shape) not in (3, 4) or shape[-1] != hd or q.dtype not in _VALUE_DTYPES or q.dtype is torch.float32:
+        _refuse("q must be fp16 or bf16 [B, T, Hq, hd] or [B, Hq, hd]")
+    B, Hq = shape[0], shape[-2]
+    T, result = (1, (B, Hq * hd)) if len(shape) == 3 else (shape[1], (B, shape[1], Hq * hd))
+    if block_table.dim() != 2 or block_table.shape[0] != B or ctx_len.shape != (B,):
+        _refuse("block_table must be [B, pages], ctx_len [B]")
     stride = _row_stride(q, "q")
-    shape = (B, Hq * hd) if q.dim() == 3 else (B, T, Hq * hd)
-    extra = {k: t for k, t in (("scratch", scratch), ("out", out)) if t is not None}
-    _on_device(stream, **extra)
     if scratch is None:
-        n = es_op_decode_attention_kv8_scratch_bytes(B, T, Hq, Hkv, hd, P, max_ctx)
-        scratch = _empty(stream, n, dtype=torch.uint8, device=q.device) if n else None
-    else:
-        _need(scratch.is_contiguous(), "scratch must be contiguous")
+        n = lib.es_op_decode_attention_kv8_scratch_bytes(B, T, Hq, Hkv, hd, P, max_ctx)
+        scratch = _empty(stream, n, torch.uint8, q) if n else None
+    elif not scratch.is_contiguous():
+        _refuse("scratch must be contiguous")
     if out is None:
-        out = _empty(stream, *shape, dtype=q.dtype, device=q.device)
-    else:
-        _need(out.dtype == q.dtype and out.is_contiguous() and tuple(out.shape) == shape, f"out must be contiguous {shape} of q's type")
-    _check(lib.es_op_decode_attention_kv8(_ptr(q), _VALUE_DTYPES[q.dtype], stride, _ptr(k_pages), _ptr(v_pages), _CODE_DTYPES[k_pages.dtype],
-                                          _ptr(k_scale), _ptr(v_scale), _ptr(block_table), _ptr(ctx_len), _ptr(out), B, T, Hq, Hkv, hd, P,
-                                          block_table.shape[1], n_pages, max_ctx, _ptr(scratch),
-                                          0 if scratch is None else scratch.numel() * scratch.element_size(), _stream_ptr(stream)))
+        out = _empty(stream, result, q.dtype, q)
+    elif out.dtype is not q.dtype or not out.is_contiguous() or out.shape != result:
+        _refuse(f"out must be contiguous {result} of q's type")
+    _check(lib.es_op_decode_attention_kv8(q.data_ptr(), _VALUE_DTYPES[q.dtype], stride, k_pages.data_ptr(), v_pages.data_ptr(), _CODE_DTYPES[k_pages.dtype],
+                                          k_scale.data_ptr(), v_scale.data_ptr(), block_table.data_ptr(), ctx_len.data_ptr(), out.data_ptr(), B, T, Hq, Hkv,
+                                          hd, P, block_table.shape[1], n_pages, max_ctx, _ptr(scratch),
+                                          0 if scratch is None else scratch.numel() * scratch.element_size(), raw))
     return out
 
 
@@ -605,23 +641,28 @@ def es_op_sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[to
                  out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(tokens int32 [B], logprobs fp32 [B]) drawn from logits [B, V] (fp32, fp16 or bf16; rows may be spaced) with the random
     numbers u [B] in [0, 1) and per-row settings [B]: temperature, top_p, min_p fp32, top_k int32; None = off."""
-    settings = {"temperature": temperature, "top_k": top_k, "top_p": top_p, "min_p": min_p}
-    given = {k: t for k, t in settings.items() if t is not None}
-    _on_device(stream, logits=logits, u=u, **given)
-    _need(logits.dim() == 2 and logits.dtype in _VALUE_DTYPES and (logits.stride(1) == 1 or logits.shape[1] == 1), "logits must be fp32, fp16 or bf16 [B, V] with dense rows")
-    B, V = logits.shape
-    for name, t in {"u": u, **given}.items():
-        want = torch.int32 if name == "top_k" else torch.float32
-        _need(t.dtype == want and t.is_contiguous() and tuple(t.shape) == (B,), f"{name} must be contiguous {want} [B]")
+    raw = _launch_on(stream, "logits u temperature top_k top_p min_p", logits, u, temperature, top_k, top_p, min_p)
+    shape = logits.shape
+    if len(shape) != 2 or logits.dtype not in _VALUE_DTYPES or (logits.stride(1) != 1 and shape[1] != 1):
+        _refuse("logits must be fp32, fp16 or bf16 [B, V] with dense rows")
+    B, V = shape
+    for t in (u, temperature, top_p, min_p):
+        if t is not None and not (t.dtype is torch.float32 and t.is_contiguous() and t.shape == (B,)):
+            _refuse("u, temperature, top_p and min_p must be contiguous fp32 [B]")
+    if top_k is not None and not (top_k.dtype is torch.int32 and top_k.is_contiguous() and top_k.shape == (B,)):
+        _refuse("top_k must be contiguous int32 [B]")
     if out is None:
-        _need(B > 0, "bad sizes")
-        out = (_empty(stream, B, dtype=torch.int32, device=logits.device), _empty(stream, B, dtype=torch.float32, device=logits.device))
+        if B <= 0:
+            _refuse("bad sizes")
+        tokens, logprobs = _empty(stream, (2, B), torch.int32, logits).unbind()
+        out = (tokens, logprobs.view(torch.float32))
     else:
-        _on_device(stream, out_tokens=out[0], out_logprobs=out[1])
+        _launch_on(stream, "out[0] out[1]", *out)
         for t, want in zip(out, (torch.int32, torch.float32)):
-            _need(t.dtype == want and t.is_contiguous() and tuple(t.shape) == (B,), f"out must be contiguous int32 [B] and fp32 [B]")
-    _check(lib.es_op_sample(_ptr(logits), _VALUE_DTYPES[logits.dtype], logits.stride(0) if B > 1 else V, _ptr(u), _ptr(temperature),
-                            _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(out[0]), _ptr(out[1]), B, V, _stream_ptr(stream)))
+            if t.dtype is not want or not t.is_contiguous() or t.shape != (B,):
+                _refuse("out must be contiguous int32 [B] and fp32 [B]")
+    _check(lib.es_op_sample(logits.data_ptr(), _VALUE_DTYPES[logits.dtype], logits.stride(0) if B > 1 else V, u.data_ptr(), _ptr(temperature),
+                            _ptr(top_k), _ptr(top_p), _ptr(min_p), out[0].data_ptr(), out[1].data_ptr(), B, V, raw))
     return out
 
 
