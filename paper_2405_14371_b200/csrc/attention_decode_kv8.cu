@@ -1,46 +1,58 @@
-// Split-KV decode attention over the paged 8-bit cache (mma.sync m16n8k16), for one or a few query tokens per sequence.
+// Decode attention over the paged 8-bit cache (TMA + mma.sync m16n8k16), for one or a few query tokens per sequence.
 //
-// The bound is reading every code of K and V once.  A KV head's query rows (T tokens x G heads of the group) form row
-// tiles of 8 (NT = 1) or 16 (NT = 2); a CTA takes one split of one sequence's keys for one row tile, its four warps
-// every fourth block of 16 tokens each:
+// The bound is reading every code of K and V once, so the work is cut for an even and unbroken stream of bytes: the keys of
+// all (sequence, KV head) items, in tiles of 64 tokens, form one line, and every warp of the machine (8 per SM, one CTA
+// per SM) takes an equal stretch of it, whatever the lengths.  A warp feeds itself: one lane asks for a tile's K and V
+// through TMA into the warp's own ring of three half tiles (24 KB), so up to 192 KB per SM are on their way while it computes,
+// and nothing between the warps waits until they are done.  An item whose tiles lie in one stretch is finished by its
+// warp; the others leave (o, max, sum), which a second kernel merges in order of the stretches.
 //
-//   * codes go from global memory to registers with 16-byte loads and become fp16 there, which holds every code of both
-//     types exactly; the contraction visits the head's dimensions in whatever order the bytes arrive in, and the query
-//     fragments are gathered with the same permutation, so nothing passes through shared memory;
+// For a tile and a tile of 8 (NT = 1) or 16 (NT = 2) query rows (T tokens x G heads of the KV head's group):
+//   * codes become fp16, which holds every code of both types exactly, on their way from shared memory into the
+//     fragments.  The contraction visits the head's dimensions in the order in which a thread's 16-byte pieces hold them;
+//     the query fragments are gathered with the same permutation.  The 128-byte swizzle keeps both the K reads (8 rows,
+//     4 pieces) and the V reads (4 rows, 8 pieces) free of bank conflicts;
 //   * scores S[row, token]: A = query rows, B = K.  The scale of K's page, 1/sqrt(hd) and the query's own exponent are
 //     factors of the finished score;
-//   * softmax per block against the block's own maximum, in fp32: the probabilities lie in [0, 1] whatever the other
-//     pages hold, and enter the next product as two fp16 halves (hi + lo, together 22 bits), so that rounding them costs
-//     the output nothing next to its own;
-//   * O^T[dim, row] = V^T P^T into a block accumulator, which joins the running sum with the factor
-//     (scale of V's page) * exp(block maximum - new maximum): pages of very different scales cannot wash each other out.
+//   * softmax in sub-tiles (SUB tokens of one page) against the sub-tile's own maximum, in fp32: the probabilities lie in
+//     [0, 1] whatever the other pages hold, and enter the next product as two fp16 halves (hi + lo, together 22 bits), so
+//     that rounding them costs the output nothing next to its own;
+//   * O^T[dim, row] = V^T P^T into a sub-tile accumulator, which joins the running sum with the factor
+//     (scale of V's page) * exp(sub-tile maximum - new maximum): pages of very different scales cannot wash each other out.
 //
 // bf16 queries are brought to fp16 by a power of two per row (largest magnitude to [1, 2)): 11 bits hold bf16's 8, and
 // what underflows is below 2^-24 of the row's largest.
 //
-// A block lies in one page (P >= 16).  Codes behind the context are zeroed in V and masked by selection in the scores, so
-// that garbage (NaN codes among it) never meets a product; a page whose scale is NaN makes the rows that see it NaN.
-// Splits are merged in order by a second kernel.
+// Codes behind the context are zeroed in V and masked by selection in the scores, so that garbage (NaN codes among it)
+// never meets a product; a page whose scale is NaN makes the rows that see it NaN.
+#include <cuda.h>
+
 #include "es_internal.cuh"
 #include "kv8.cuh"
 #include "launch.cuh"
+#include "sm100.cuh"
 
 namespace es {
 namespace {
 
-constexpr int AW = 4;                    // warps of a CTA
+constexpr int AW = 8;                    // warps of a CTA
+constexpr int TILE = 64;                 // tokens of a tile
+constexpr int SLOTS = 3;                 // half tiles of a warp's ring
+constexpr int KV8_MAX_B = 4096;          // sequences whose tile sums fit beside the rings
 
 struct Kv8AttnParams {
   const void* q;
   int64_t q_stride;
-  const uint8_t *k, *v;
   const float *ks, *vs;
   const int *table, *ctx_len;
   void* out;
-  float *part_o, *part_ml;               // [B * T * Hq][n_splits][hd], [..][n_splits][2]
+  float *part_o, *part_ml;               // [2 * warps][rows][hd], [..][rows][2]
+  int* plan;                             // tiles before each sequence [B + 1], written for the merge
   int B, T, Hq, Hkv, G, P, log2P, pps, n_pages, max_ctx;
-  int row_tiles, n_splits, tokens_per_split;
+  int row_tiles, rows, bf16;             // rows = rows of a row tile that are stored
 };
+
+struct alignas(64) Kv8Maps { CUtensorMap k, v; };
 
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -54,354 +66,499 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-__device__ __forceinline__ uint4 ld16(const uint8_t* p) {
+__device__ __forceinline__ uint4 lds16(uint32_t addr) {
   uint4 v;
-  asm volatile("ld.global.cg.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
   return v;
 }
-__device__ __forceinline__ uint2 ld8(const uint8_t* p) {
+__device__ __forceinline__ uint2 lds8(uint32_t addr) {
   uint2 v;
-  asm volatile("ld.global.cg.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
   return v;
 }
 
-template <bool BF16>
-__device__ __forceinline__ float2 pair_of(uint32_t w) {
-  if (BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
-  return __half22float2(bits_h2(w));
+__device__ __forceinline__ uint32_t two_outputs(float a, float b, int bf16) {
+  if (bf16) {
+    const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&r);
+  }
+  return h2_bits(__floats2half2_rn(a, b));
 }
 
-template <bool BF16>
-__device__ __forceinline__ void store_out(void* out, int64_t i, float x) {
-  if (BF16) reinterpret_cast<__nv_bfloat16*>(out)[i] = __float2bfloat16_rn(x);
-  else reinterpret_cast<__half*>(out)[i] = __float2half_rn(x);
-}
+// A place on the line of tiles: sequence b, item (kv head, row tile) of it, tile of the item.
+struct Cursor {
+  int b, item, tile, tiles;
+  __device__ __forceinline__ void seek(int at, const int* pre, int B, int items) {
+    int lo = 0, hi = B;                  // pre[lo] * items <= at < pre[hi] * items
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (pre[mid] * items <= at) lo = mid; else hi = mid;
+    }
+    b = lo;
+    tiles = pre[b + 1] - pre[b];
+    const int r = at - pre[b] * items;
+    item = r / tiles;
+    tile = r - item * tiles;
+  }
+  __device__ __forceinline__ void next(const int* pre, int B, int items) {
+    if (++tile < tiles) return;
+    tile = 0;
+    if (++item < items) return;
+    item = 0;
+    if (++b < B) tiles = pre[b + 1] - pre[b];
+  }
+};
 
-template <int HD, int CODE, bool BF16, int NT>
-__global__ void __launch_bounds__(AW * 32, NT == 1 ? 3 : 2) kv8_attn_kernel(const Kv8AttnParams p) {
+// Tiles of a warp's stretch.
+__device__ __forceinline__ int stretch_of(int total, int warps) { return (total + warps - 1) / warps; }
+
+template <int HD, int CODE, int NT, int SUB>
+__global__ void __launch_bounds__(AW * 32, 1) kv8_attn_kernel(const __grid_constant__ Kv8Maps maps, const Kv8AttnParams p) {
   pdl_launch_dependents();
   constexpr int J = HD / 64;             // 16-byte pieces of a K row per thread
   constexpr int D = HD / 8;              // dimensions of V per thread
-  constexpr int NM = D / 2;              // output MMAs
+  constexpr int NM = D / 2;              // output MMAs of 16 tokens
   constexpr int ROWS = 8 * NT;
+  constexpr int HALF = TILE * HD;        // bytes of a half tile
+  constexpr int NSUB = TILE / SUB, KK = SUB / 16;
   constexpr float LOG2E = 1.4426950408889634f;
-  __shared__ float sm_o[AW][ROWS][HD];
-  __shared__ float sm_m[AW][ROWS], sm_l[AW][ROWS];
+  extern __shared__ __align__(1024) unsigned char dyn[];
+  unsigned char* ring = dyn + ((1024 - (smem_u32(dyn) & 1023)) & 1023);  // the swizzle goes by address bits 7 to 9
+  __shared__ __align__(8) uint64_t bars[AW * SLOTS];
+  __shared__ int s_warp[AW];
+  __shared__ int s_abort;
+  int* pre = reinterpret_cast<int*>(ring + AW * SLOTS * HALF);          // [B + 1] tiles before each sequence
 
-  const int split = blockIdx.x;
-  const int kvh = blockIdx.y / p.row_tiles, tile = blockIdx.y - kvh * p.row_tiles, b = blockIdx.z;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int n_rows = p.T * p.G;
-  const int ctx = max(0, min(p.ctx_len[b], p.max_ctx));
-  const int t_begin = split * p.tokens_per_split;
-  if (t_begin >= ctx && split > 0) return;               // nothing to read and nobody reads its part (split 0 answers for empty contexts)
-  const int t_end = (int)min((long long)ctx, (long long)t_begin + p.tokens_per_split);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const int items = p.Hkv * p.row_tiles, n_rows = p.T * p.G;
 
-  // row r of the tile: query token (r / G), head kvh * G + r % G; it sees keys below `limit`
-  auto row_of = [&](int r, int& token, int& head) { const int i = tile * ROWS + r; token = i / p.G; head = kvh * p.G + i - token * p.G; return i < n_rows; };
+  if (tid == 0) {
+    s_abort = 0;
+    for (int i = 0; i < AW * SLOTS; ++i) mbar_init(smem_u32(bars + i), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    prefetch_tmap(&maps.k);
+    prefetch_tmap(&maps.v);
+  }
+  // ---- tiles of every sequence; an empty one has a tile without keys, so that somebody writes its rows ----
+  {
+    int before = 0;
+    for (int base = 0; base < p.B; base += AW * 32) {
+      const int b = base + tid;
+      int v = 0;
+      if (b < p.B) { const int n = min(max(p.ctx_len[b], 1), p.max_ctx); v = (n + TILE - 1) / TILE; }
+      int inc = v;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) { const int o = __shfl_up_sync(~0u, inc, d); if (lane >= d) inc += o; }
+      if (lane == 31) s_warp[warp] = inc;
+      __syncthreads();
+      int sum = 0, off = 0;
+#pragma unroll
+      for (int w = 0; w < AW; ++w) { if (w < warp) off += s_warp[w]; sum += s_warp[w]; }
+      if (b < p.B) pre[b + 1] = before + off + inc;
+      before += sum;
+      __syncthreads();
+    }
+    if (tid == 0) pre[0] = 0;
+    __syncthreads();
+  }
+  if (blockIdx.x == 0 && p.plan)
+    for (int i = tid; i <= p.B; i += AW * 32) p.plan[i] = pre[i];
+  const int total = pre[p.B] * items;
+  // stretches go round the SMs first: few tiles spread over all of them
+  const int me = warp * gridDim.x + blockIdx.x;
+  const int per_warp = stretch_of(total, AW * gridDim.x);
+  const int begin = min((int64_t)me * per_warp, (int64_t)total), end = min(begin + per_warp, total);
+  if (begin >= end) return;
+
+  const uint32_t my_ring = smem_u32(ring) + warp * SLOTS * HALF, my_bars = smem_u32(bars) + warp * SLOTS * 8;
+  const int box = min(p.P, TILE), log2box = min(p.log2P, 6), boxes = TILE >> log2box;        // tokens that lie together
+  Cursor c, ahead;
+  c.seek(begin, pre, p.B, items);
+  ahead = c;
+  const int n_half = 2 * (end - begin);
+  int asked = 0;                         // half tiles asked for: K, V, K, V, ...
+  float ks_a = 0.f, vs_a = 0.f;          // lane i: scales of box i of the tile asked for last, and whether its page exists
+  int row_a = -1;                        // its first 128-byte line, or -1
+  float ks_c = 0.f, vs_c = 0.f;
+  unsigned ok_a = 0, ok_c = 0;
+
+  auto ask = [&]() {
+    const int slot = asked % SLOTS;
+    const bool is_v = asked & 1;
+    if (!is_v) {
+      row_a = -1;
+      const int tok = ahead.tile * TILE + (lane << log2box);
+      const int n = min(p.ctx_len[ahead.b], p.max_ctx);
+      if (lane < boxes && tok < n) {
+        const int page = p.table[(int64_t)ahead.b * p.pps + (tok >> p.log2P)];
+        if (page >= 0 && page < p.n_pages) {
+          const int64_t ph = (int64_t)page * p.Hkv + ahead.item / p.row_tiles;
+          ks_a = p.ks[ph];
+          vs_a = p.vs[ph];
+          row_a = (int)((ph * p.P + (tok & (p.P - 1))) * HD / 128);
+        }
+      }
+      ok_a = __ballot_sync(~0u, row_a >= 0);
+    }
+    const uint32_t bar = my_bars + slot * 8;
+    if (lane == 0) mbar_expect_tx(bar, __popc(ok_a) * (HD << log2box));
+    __syncwarp();
+    if (row_a >= 0) tma_load_2d(my_ring + slot * HALF + lane * (HD << log2box), is_v ? &maps.v : &maps.k, 0, row_a, bar);
+    if (is_v) ahead.next(pre, p.B, items);
+    ++asked;
+  };
+  int used = 0;
+  auto arrived = [&]() -> bool {         // the oldest half tile that was not yet used
+    return __all_sync(~0u, mbar_wait(my_bars + (used % SLOTS) * 8, (used / SLOTS) & 1, &s_abort, nullptr, 1));
+  };
+
+  ask();                                 // the first tile's K
+  ks_c = ks_a; vs_c = vs_a; ok_c = ok_a;
+  ask();                                 // its V
+  if (asked < n_half) ask();             // the second tile's K
+
   int limit[NT];
   float qscale[NT];
   uint32_t qa[NT][8 * J];
+  float o[NT][NM][4], m_run[NT], l_run[NT];
+  int ctx = 0, item_begin = 0;
+  bool fresh = true, running = true;
+
+  for (int at = begin; at < end && running; ++at) {
+    if (fresh) {
+      // ---- a new item: its query rows; row r of the row tile is token r / G, head kv_head * G + r % G ----
+      fresh = false;
+      ctx = max(0, min(p.ctx_len[c.b], p.max_ctx));
+      item_begin = at - c.tile;
+      const int kvh = c.item / p.row_tiles, rt = c.item - kvh * p.row_tiles;
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    int token, head;
-    const bool real = row_of(8 * n + g, token, head);
-    limit[n] = real ? ctx - p.T + token + 1 : 0;
-    qscale[n] = 1.f;
-    const uint16_t* row = reinterpret_cast<const uint16_t*>(p.q) + ((int64_t)b * p.T + token) * p.q_stride + (int64_t)head * HD;
+      for (int n = 0; n < NT; ++n) {
+        const int i = rt * ROWS + 8 * n + g, token = i / p.G;
+        const bool real = i < n_rows;
+        limit[n] = real ? ctx - p.T + token + 1 : 0;
+        qscale[n] = 1.f;
+        const uint16_t* row = reinterpret_cast<const uint16_t*>(p.q) + ((int64_t)c.b * p.T + token) * p.q_stride + (int64_t)(kvh * p.G + i - token * p.G) * HD + t * (HD / 4);
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-      uint4 x = make_uint4(0, 0, 0, 0), y = x;
-      if (real) { x = *reinterpret_cast<const uint4*>(row + (4 * j + t) * 16); y = *reinterpret_cast<const uint4*>(row + (4 * j + t) * 16 + 8); }
-      qa[n][8 * j] = x.x; qa[n][8 * j + 1] = x.y; qa[n][8 * j + 2] = x.z; qa[n][8 * j + 3] = x.w;
-      qa[n][8 * j + 4] = y.x; qa[n][8 * j + 5] = y.y; qa[n][8 * j + 6] = y.z; qa[n][8 * j + 7] = y.w;
-    }
-    if (BF16) {
-      uint32_t mx = 0;
+        for (int j = 0; j < 2 * J; ++j) {
+          const uint4 x = real ? *reinterpret_cast<const uint4*>(row + 8 * j) : make_uint4(0, 0, 0, 0);
+          qa[n][4 * j] = x.x; qa[n][4 * j + 1] = x.y; qa[n][4 * j + 2] = x.z; qa[n][4 * j + 3] = x.w;
+        }
+        if (p.bf16) {
+          uint32_t mx = 0;
 #pragma unroll
-      for (int i = 0; i < 8 * J; ++i) mx = __vmaxu2(mx, qa[n][i] & 0x7fff7fffu);
-      mx = max(mx & 0xffffu, mx >> 16);
-      mx = max(mx, __shfl_xor_sync(~0u, mx, 1));
-      mx = max(mx, __shfl_xor_sync(~0u, mx, 2));
-      // 2^-e and 2^e with e the exponent of the largest magnitude, kept where both are normal numbers
-      const int e = min(max((int)(mx >> 7) - 127, -126), 126);
-      const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-      qscale[n] = __uint_as_float((uint32_t)(127 + e) << 23);
+          for (int i2 = 0; i2 < 8 * J; ++i2) mx = __vmaxu2(mx, qa[n][i2] & 0x7fff7fffu);
+          mx = max(mx & 0xffffu, mx >> 16);
+          mx = max(mx, __shfl_xor_sync(~0u, mx, 1));
+          mx = max(mx, __shfl_xor_sync(~0u, mx, 2));
+          // 2^-e and 2^e with e the exponent of the largest magnitude, kept where both are normal numbers
+          const int e = min(max((int)(mx >> 7) - 127, -126), 126);
+          const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+          qscale[n] = __uint_as_float((uint32_t)(127 + e) << 23);
 #pragma unroll
-      for (int i = 0; i < 8 * J; ++i) {
-        const float2 f = pair_of<true>(qa[n][i]);
-        qa[n][i] = h2_bits(__floats2half2_rn(f.x * down, f.y * down));
+          for (int i2 = 0; i2 < 8 * J; ++i2)
+            qa[n][i2] = h2_bits(__floats2half2_rn(__uint_as_float(qa[n][i2] << 16) * down, __uint_as_float(qa[n][i2] & 0xffff0000u) * down));
+        }
+        qscale[n] *= rsqrtf((float)HD) * LOG2E;            // scores in units of log2
+        m_run[n] = -INFINITY;
+        l_run[n] = 0.f;
+#pragma unroll
+        for (int i2 = 0; i2 < NM; ++i2) o[n][i2][0] = o[n][i2][1] = o[n][i2][2] = o[n][i2][3] = 0.f;
       }
     }
-    qscale[n] *= rsqrtf((float)HD) * LOG2E;                // scores in units of log2
-  }
-
-  const int64_t head_bytes = (int64_t)p.P * HD;
-  const int* table = p.table + (int64_t)b * p.pps;
-  uint4 kreg[2][J];
-  uint32_t vreg[4][D / 4];
-  float k_s = 0.f, v_s = 0.f, k_n = 0.f, v_n = 0.f;        // scales of the block at hand and of the one being loaded
-  bool ok = false, ok_n = false;                           // whether their pages exist
-
-  auto page_of = [&](int T0) -> int { return T0 < t_end ? table[T0 >> p.log2P] : -1; };
-  auto load_k = [&](int T0, int page) {
-    ok_n = page >= 0 && page < p.n_pages;
-    if (!ok_n) return;
-    const int64_t ph = (int64_t)page * p.Hkv + kvh;
-    const uint8_t* base = p.k + ph * head_bytes + (int64_t)(T0 & (p.P - 1)) * HD;
+    // ---- scores: rows g (and 8 + g), tokens 8 nt + 2 t + {0, 1} of the tile ----
+    if (!arrived()) { running = false; break; }
+    float s[TILE / 8][4];
+    {
+      const uint32_t base = my_ring + (used % SLOTS) * HALF;
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt)
+      for (int nt = 0; nt < TILE / 8; ++nt) {
+        s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
 #pragma unroll
-      for (int j = 0; j < J; ++j) kreg[nt][j] = ld16(base + (8 * nt + g) * HD + (4 * j + t) * 16);
-    k_n = p.ks[ph];
-    v_n = p.vs[ph];
-  };
-  auto load_v = [&](int T0, int page) {
-    if (page < 0 || page >= p.n_pages) return;
-    const uint8_t* base = p.v + ((int64_t)page * p.Hkv + kvh) * head_bytes + (int64_t)(T0 & (p.P - 1)) * HD;
-    const int left = ctx - T0;
+        for (int j = 0; j < J; ++j) {
+          // the 16-byte pieces of token 8 nt + g: J t + j of its row, moved by the swizzle of its 128-byte line
+          const uint32_t line = HD == 128 ? 8 * nt + g : 4 * nt + (g >> 1);
+          const uint32_t piece = HD == 128 ? 2 * t + j : 4 * (g & 1) + t;
+          const uint4 k = lds16(base + line * 128 + ((piece ^ (line & 7)) << 4));
+          const uint32_t w[4] = {k.x, k.y, k.z, k.w};
 #pragma unroll
-    for (int q4 = 0; q4 < 4; ++q4) {
-      const int r = 2 * t + (q4 & 1) + 8 * (q4 >> 1);
-      if constexpr (HD == 128) {
-        const uint4 x = r < left ? ld16(base + r * HD + g * 16) : make_uint4(0, 0, 0, 0);
-        vreg[q4][0] = x.x; vreg[q4][1] = x.y; vreg[q4][2] = x.z; vreg[q4][3] = x.w;
-      } else {
-        const uint2 x = r < left ? ld8(base + r * HD + g * 8) : make_uint2(0, 0);
-        vreg[q4][0] = x.x; vreg[q4][1] = x.y;
-      }
-    }
-  };
-
-  float o[NT][NM][4];
-  float m_run[NT], l_run[NT];
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    m_run[n] = -INFINITY; l_run[n] = 0.f;
-#pragma unroll
-    for (int i = 0; i < NM; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
-  }
-
-  constexpr int STEP = AW * 16;
-  int T0 = t_begin + warp * 16;
-  int page = page_of(T0), page_next = page_of(T0 + STEP);
-  load_k(T0, page);
-  load_v(T0, page);
-  for (; T0 < t_end; T0 += STEP) {
-    ok = ok_n; k_s = k_n; v_s = v_n;
-    page = page_next;
-    page_next = page_of(T0 + 2 * STEP);
-    if (!ok) {                                             // a page nobody sees (uniform over the warp)
-      load_k(T0 + STEP, page);
-      load_v(T0 + STEP, page);
-      continue;
-    }
-    // ---- scores: rows g (and 8 + g), tokens T0 + 8 nt + 2 t + {0, 1} ----
-    float s[2][4];
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
-      s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
-#pragma unroll
-      for (int j = 0; j < J; ++j) {
-        const uint32_t w[4] = {kreg[nt][j].x, kreg[nt][j].y, kreg[nt][j].z, kreg[nt][j].w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t lo, hi;
-          codes_to_h2<CODE>(w[i], lo, hi);
-          mma(s[nt], qa[0][8 * j + 2 * i], NT == 2 ? qa[NT - 1][8 * j + 2 * i] : 0u, qa[0][8 * j + 2 * i + 1],
-              NT == 2 ? qa[NT - 1][8 * j + 2 * i + 1] : 0u, lo, hi);
+          for (int i = 0; i < 4; ++i) {
+            uint32_t lo, hi;
+            codes_to_h2<CODE>(w[i], lo, hi);
+            mma(s[nt], qa[0][8 * j + 2 * i], NT == 2 ? qa[NT - 1][8 * j + 2 * i] : 0u, qa[0][8 * j + 2 * i + 1],
+                NT == 2 ? qa[NT - 1][8 * j + 2 * i + 1] : 0u, lo, hi);
+          }
         }
       }
     }
-    load_k(T0 + STEP, page);
-    // ---- softmax of the block ----
-    uint32_t ph[NT][2], pl[NT][2];                         // probabilities, hi and lo halves: the B fragments of the output MMAs
-    float alpha[NT], beta[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      float x[4], mx = -INFINITY;
-      const float f = qscale[n] * k_s;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int tok = T0 + 8 * (e >> 1) + 2 * t + (e & 1);
-        x[e] = tok < limit[n] ? s[e >> 1][2 * n + (e & 1)] * f : -INFINITY;
-        mx = fmaxf(mx, x[e]);
-      }
-      mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 1));
-      mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 2));
-      const bool sees = T0 < limit[n];
-      const float ref = mx == -INFINITY ? 0.f : mx;
-      float sum = 0.f;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) { x[e] = ex2(x[e] - ref); sum += x[e]; }
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const __half2 h = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
-        const float2 back = __half22float2(h);
-        ph[n][i] = h2_bits(h);
-        pl[n][i] = h2_bits(__floats2half2_rn(x[2 * i] - back.x, x[2 * i + 1] - back.y));
-      }
-      sum += __shfl_xor_sync(~0u, sum, 1);
-      sum += __shfl_xor_sync(~0u, sum, 2);
-      const float mn = fmaxf(m_run[n], mx);
-      const float to = mn == -INFINITY ? 0.f : mn;
-      alpha[n] = ex2(m_run[n] - to);
-      const float join = sees ? ex2(ref - to) : 0.f;       // NaN scores pass through: they are in `sum` and in the product
-      beta[n] = sees ? join * v_s : 0.f;
-      l_run[n] = sees ? l_run[n] * alpha[n] + sum * join : l_run[n];
-      m_run[n] = mn;
-    }
-    // ---- output: MMA i gives dimensions D g + i (rows 0..7) and D g + D / 2 + i (rows 8..15) ----
-    float al[NT][2], be[NT][2];                            // factors of rows 2 t and 2 t + 1
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        al[n][i] = __shfl_sync(~0u, alpha[n], (2 * t + i) * 4);
-        be[n][i] = __shfl_sync(~0u, beta[n], (2 * t + i) * 4);
-      }
-    #pragma unroll
-    for (int w = 0; w < D / 8; ++w) {
-      uint32_t a[4][4];                                    // A registers 0..3 of four MMAs
-#pragma unroll
-      for (int q2 = 0; q2 < 2; ++q2)
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const uint32_t x = vreg[2 * q2][w + half * (D / 8)], y = vreg[2 * q2 + 1][w + half * (D / 8)];
-          codes_to_h2<CODE>(__byte_perm(x, y, 0x5140), a[2 * q2 + half][0], a[2 * q2 + half][1]);
-          codes_to_h2<CODE>(__byte_perm(x, y, 0x7362), a[2 * q2 + half][2], a[2 * q2 + half][3]);
-        }
-#pragma unroll
-      for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          float c[4] = {0.f, 0.f, 0.f, 0.f};
-          mma(c, a[0][d], a[1][d], a[2][d], a[3][d], ph[n][0], ph[n][1]);
-          mma(c, a[0][d], a[1][d], a[2][d], a[3][d], pl[n][0], pl[n][1]);
-          float (&acc)[4] = o[n][4 * w + d];
-          acc[0] = acc[0] * al[n][0] + c[0] * be[n][0];
-          acc[1] = acc[1] * al[n][1] + c[1] * be[n][1];
-          acc[2] = acc[2] * al[n][0] + c[2] * be[n][0];
-          acc[3] = acc[3] * al[n][1] + c[3] * be[n][1];
-        }
-    }
-    load_v(T0 + STEP, page);
-  }
+    __syncwarp();
+    ++used;
+    if (asked < n_half) ask();           // in the place of the half tile just read: the next tile's V
 
-  // ---- the warps' parts join in warp order ----
+    const uint32_t vbase = my_ring + (used % SLOTS) * HALF;
+    bool v_here = false;
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
+    for (int sub = 0; sub < NSUB; ++sub) {
+      const int T0 = c.tile * TILE + sub * SUB;
+      const int bx = (sub * SUB) >> log2box;
+      if (T0 >= ctx || !((ok_c >> bx) & 1)) continue;      // nothing there, or a page nobody sees
+      const float k_s = __shfl_sync(~0u, ks_c, bx), v_s = __shfl_sync(~0u, vs_c, bx);
+      // ---- softmax of the sub-tile ----
+      uint32_t ph[NT][KK][2], pl[NT][KK][2];               // probabilities, hi and lo halves: B fragments of the output MMAs
+      float al[NT][2], be[NT][2];                          // factors of rows 2 t and 2 t + 1
 #pragma unroll
-    for (int i = 0; i < NM; ++i) {
-      sm_o[warp][8 * n + 2 * t][D * g + i] = o[n][i][0];
-      sm_o[warp][8 * n + 2 * t + 1][D * g + i] = o[n][i][1];
-      sm_o[warp][8 * n + 2 * t][D * g + D / 2 + i] = o[n][i][2];
-      sm_o[warp][8 * n + 2 * t + 1][D * g + D / 2 + i] = o[n][i][3];
+      for (int n = 0; n < NT; ++n) {
+        float x[2 * KK][2], mx = -INFINITY;
+        const float f = qscale[n] * k_s;
+#pragma unroll
+        for (int nt = 0; nt < 2 * KK; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            x[nt][e] = T0 + 8 * nt + 2 * t + e < limit[n] ? s[sub * 2 * KK + nt][2 * n + e] * f : -INFINITY;
+            mx = fmaxf(mx, x[nt][e]);
+          }
+        mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 1));
+        mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 2));
+        const bool sees = T0 < limit[n];
+        const float ref = mx == -INFINITY ? 0.f : mx;
+        float sum = 0.f;
+#pragma unroll
+        for (int nt = 0; nt < 2 * KK; ++nt) {
+          x[nt][0] = ex2(x[nt][0] - ref);
+          x[nt][1] = ex2(x[nt][1] - ref);
+          sum += x[nt][0] + x[nt][1];
+          const __half2 h = __floats2half2_rn(x[nt][0], x[nt][1]);
+          const float2 back = __half22float2(h);
+          ph[n][nt >> 1][nt & 1] = h2_bits(h);
+          pl[n][nt >> 1][nt & 1] = h2_bits(__floats2half2_rn(x[nt][0] - back.x, x[nt][1] - back.y));
+        }
+        sum += __shfl_xor_sync(~0u, sum, 1);
+        sum += __shfl_xor_sync(~0u, sum, 2);
+        const float mn = fmaxf(m_run[n], mx);
+        const float to = mn == -INFINITY ? 0.f : mn;
+        const float alpha = ex2(m_run[n] - to);
+        const float join = sees ? ex2(ref - to) : 0.f;     // NaN scores pass through: they are in `sum` and in the product
+        const float beta = sees ? join * v_s : 0.f;
+        l_run[n] = sees ? l_run[n] * alpha + sum * join : l_run[n];
+        m_run[n] = mn;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          al[n][i] = __shfl_sync(~0u, alpha, (2 * t + i) * 4);
+          be[n][i] = __shfl_sync(~0u, beta, (2 * t + i) * 4);
+        }
+      }
+      if (!v_here) {
+        v_here = true;
+        if (!arrived()) { running = false; break; }
+      }
+      // ---- output: MMA i gives dimensions D g + i (rows 0..7) and D g + D / 2 + i (rows 8..15) ----
+      uint32_t v[KK][4][D / 4];
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          // token 16 kk + 2 t + {0, 1} (+ 8) of the sub-tile: its dimensions D g ..
+          const int e = q4 & 1, up = q4 >> 1;
+          if constexpr (HD == 128) {
+            const uint32_t line = sub * SUB + 16 * kk + 8 * up + 2 * t + e;
+            const uint4 x = lds16(vbase + line * 128 + ((g ^ (line & 7)) << 4));
+            v[kk][q4][0] = x.x; v[kk][q4][1] = x.y; v[kk][q4][2] = x.z; v[kk][q4][3] = x.w;
+          } else {
+            const uint32_t line = sub * (SUB / 2) + 8 * kk + 4 * up + t;
+            const uint2 x = lds8(vbase + line * 128 + (((4 * e + (g >> 1)) ^ (line & 7)) << 4) + 8 * (g & 1));
+            v[kk][q4][0] = x.x; v[kk][q4][1] = x.y;
+          }
+        }
+      if (T0 + SUB > ctx) {              // the last tokens' sub-tile: nothing behind them enters a product
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4)
+            if (T0 + 16 * kk + 8 * (q4 >> 1) + 2 * t + (q4 & 1) >= ctx)
+#pragma unroll
+              for (int w = 0; w < D / 4; ++w) v[kk][q4][w] = 0;
+      }
+#pragma unroll
+      for (int w = 0; w < D / 8; ++w) {
+        float acc[4][NT][4];
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) acc[d][n][0] = acc[d][n][1] = acc[d][n][2] = acc[d][n][3] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          uint32_t a[4][4];              // A registers 0..3 of four MMAs
+#pragma unroll
+          for (int q2 = 0; q2 < 2; ++q2)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              const uint32_t x = v[kk][2 * q2][w + half * (D / 8)], y = v[kk][2 * q2 + 1][w + half * (D / 8)];
+              codes_to_h2<CODE>(__byte_perm(x, y, 0x5140), a[2 * q2 + half][0], a[2 * q2 + half][1]);
+              codes_to_h2<CODE>(__byte_perm(x, y, 0x7362), a[2 * q2 + half][2], a[2 * q2 + half][3]);
+            }
+#pragma unroll
+          for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              mma(acc[d][n], a[0][d], a[1][d], a[2][d], a[3][d], ph[n][kk][0], ph[n][kk][1]);
+              mma(acc[d][n], a[0][d], a[1][d], a[2][d], a[3][d], pl[n][kk][0], pl[n][kk][1]);
+            }
+        }
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[n][4 * w + d][i] = o[n][4 * w + d][i] * al[n][i & 1] + acc[d][n][i] * be[n][i & 1];
+      }
     }
-    if (t == 0) { sm_m[warp][8 * n + g] = m_run[n]; sm_l[warp][8 * n + g] = l_run[n]; }
+    if (!running) break;
+    if (!v_here && !arrived()) { running = false; break; }
+    __syncwarp();
+    ++used;
+    ks_c = ks_a; vs_c = vs_a; ok_c = ok_a;                 // the next tile's
+    if (asked < n_half) ask();                             // the K of the one after
+
+    // ---- the item's end, or the stretch's ----
+    const bool item_ends = c.tile + 1 == c.tiles;
+    if (item_ends || at + 1 == end) {
+      const int kvh = c.item / p.row_tiles, rt = c.item - kvh * p.row_tiles;
+      const bool whole = item_ends && item_begin >= begin;
+      const int64_t part = 2 * (int64_t)me + (item_begin >= begin);       // a stretch has two split items at most
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {                      // this thread holds dimensions D g .. D g + D - 1 of row 8 n + 2 t + e
+          const int r = 8 * n + 2 * t + e, i = rt * ROWS + r, token = i / p.G;
+          const float m = __shfl_sync(~0u, m_run[n], (2 * t + e) * 4), l = __shfl_sync(~0u, l_run[n], (2 * t + e) * 4);
+          if (i >= n_rows) continue;
+          if (whole) {
+            const int64_t row = ((int64_t)c.b * p.T + token) * p.Hq + kvh * p.G + (i - token * p.G);
+            uint32_t* to = reinterpret_cast<uint32_t*>(p.out) + (row * HD + D * g) / 2;
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int k = 0; k < NM; k += 2) to[(h * NM + k) / 2] = two_outputs(o[n][k][2 * h + e] * inv, o[n][k + 1][2 * h + e] * inv, p.bf16);
+          } else {
+            float* to = p.part_o + (part * p.rows + r) * HD + D * g;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int k = 0; k < NM; k += 4)
+                *reinterpret_cast<float4*>(to + h * NM + k) = make_float4(o[n][k][2 * h + e], o[n][k + 1][2 * h + e], o[n][k + 2][2 * h + e], o[n][k + 3][2 * h + e]);
+            if (g == 0) *reinterpret_cast<float2*>(p.part_ml + (part * p.rows + r) * 2) = make_float2(m, l);
+          }
+        }
+      fresh = true;
+    }
+    c.next(pre, p.B, items);
   }
-  __syncthreads();
-  for (int i = threadIdx.x; i < ROWS * HD; i += AW * 32) {
-    const int r = i / HD, c = i - r * HD;
-    int token, head;
-    if (!row_of(r, token, head)) break;
-    float mm = sm_m[0][r];
-#pragma unroll
-    for (int w = 1; w < AW; ++w) mm = fmaxf(mm, sm_m[w][r]);
-    const float ref = mm == -INFINITY ? 0.f : mm;
-    float acc = 0.f, ll = 0.f;
-#pragma unroll
-    for (int w = 0; w < AW; ++w) {
-      const float f = ex2(sm_m[w][r] - ref);
-      acc += sm_o[w][r][c] * f;
-      ll += sm_l[w][r] * f;
+  // a wait that ran out: let this warp's copies that are under way land before its shared memory goes
+  if (!running)
+    for (; used < asked; ++used) {
+      int dummy = 0;
+      mbar_wait(my_bars + (used % SLOTS) * 8, (used / SLOTS) & 1, &dummy, nullptr, 1);
     }
-    const int64_t row = ((int64_t)b * p.T + token) * p.Hq + head;
-    if (p.n_splits == 1) {
-      store_out<BF16>(p.out, row * HD + c, ll == 0.f ? 0.f : acc / ll);
-    } else {
-      p.part_o[(row * p.n_splits + split) * HD + c] = acc;
-      if (c == 0) *reinterpret_cast<float2*>(p.part_ml + (row * p.n_splits + split) * 2) = make_float2(mm, ll);
-    }
-  }
 }
 
-// One warp per output row: the splits that hold keys, in ascending order.
-template <int HD, bool BF16>
-__global__ void __launch_bounds__(128) kv8_merge_kernel(const Kv8AttnParams p) {
+// One CTA per output row of an item that was split: its warps take every fourth part, in order, and join in order.
+template <int HD>
+__global__ void __launch_bounds__(128) kv8_merge_kernel(const Kv8AttnParams p, int warps) {
   constexpr int V = HD / 32;
-  const int lane = threadIdx.x & 31;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+  __shared__ float sm_o[4][HD];
+  __shared__ float sm_l[4];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int h = blockIdx.x, token = blockIdx.y, b = blockIdx.z;
+  const int kvh = h / p.G, i = token * p.G + h - kvh * p.G;
+  const int nt_rows = p.row_tiles > 1 || p.rows > 8 ? 16 : 8, rt = i / nt_rows, r = i - rt * nt_rows;
+  const int items = p.Hkv * p.row_tiles;
   pdl_wait();
-  if (row >= (int64_t)p.B * p.T * p.Hq) return;
-  const int b = (int)(row / ((int64_t)p.T * p.Hq));
-  const int ctx = max(0, min(p.ctx_len[b], p.max_ctx));
-  const int active = max(1, (ctx + p.tokens_per_split - 1) / p.tokens_per_split);
-  const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + row * p.n_splits;
-  const float* po = p.part_o + row * p.n_splits * HD + lane * V;
+  const int per_warp = stretch_of(p.plan[p.B] * items, warps);
+  const int first = p.plan[b], tiles = p.plan[b + 1] - first;
+  const int begin = first * items + (kvh * p.row_tiles + rt) * tiles;
+  const int w0 = begin / per_warp, w1 = (begin + tiles - 1) / per_warp;
+  if (w0 == w1) return;                  // finished by its warp
+  auto part_of = [&](int w) { return (2 * (int64_t)w + (w == w0)) * p.rows + r; };
+  const int n = w1 - w0 + 1;
   float mm = -INFINITY;
-  for (int i = lane; i < active; i += 32) mm = fmaxf(mm, __ldcg(&ml[i]).x);
+  for (int k = lane; k < n; k += 32) mm = fmaxf(mm, __ldcg(p.part_ml + part_of(w0 + k) * 2));
 #pragma unroll
   for (int d = 16; d; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(~0u, mm, d));
   const float ref = mm == -INFINITY ? 0.f : mm;
   float acc[V], ll = 0.f;
 #pragma unroll
   for (int c = 0; c < V; ++c) acc[c] = 0.f;
-#pragma unroll 4
-  for (int i = 0; i < active; ++i) {
-    const float2 x = __ldcg(&ml[i]);
-    const float f = ex2(x.x - ref);
-    ll += x.y * f;
+#pragma unroll 8
+  for (int k = warp; k < n; k += 4) {
+    const int64_t part = part_of(w0 + k);
+    const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.part_ml + part * 2));
+    const float f = ex2(ml.x - ref);
+    ll += ml.y * f;
 #pragma unroll
-    for (int c = 0; c < V; ++c) acc[c] += __ldcg(po + (int64_t)i * HD + c) * f;
+    for (int c = 0; c < V; ++c) acc[c] += __ldcg(p.part_o + part * HD + c * 32 + lane) * f;
   }
 #pragma unroll
-  for (int c = 0; c < V; ++c) store_out<BF16>(p.out, row * HD + lane * V + c, ll == 0.f ? 0.f : acc[c] / ll);
+  for (int c = 0; c < V; ++c) sm_o[warp][c * 32 + lane] = acc[c];
+  if (lane == 0) sm_l[warp] = ll;
+  __syncthreads();
+  const float l = sm_l[0] + sm_l[1] + sm_l[2] + sm_l[3], inv = l == 0.f ? 0.f : 1.f / l;
+  const int64_t row = ((int64_t)b * p.T + token) * p.Hq + h;
+  if (threadIdx.x < HD / 2) {
+    const int c = 2 * threadIdx.x;
+    const float x = sm_o[0][c] + sm_o[1][c] + sm_o[2][c] + sm_o[3][c], y = sm_o[0][c + 1] + sm_o[1][c + 1] + sm_o[2][c + 1] + sm_o[3][c + 1];
+    reinterpret_cast<uint32_t*>(p.out)[(row * HD + c) / 2] = two_outputs(x * inv, y * inv, p.bf16);
+  }
 }
 
-struct Split { int row_tiles, nt, n_splits, tokens; };
+struct Shape { int nt, row_tiles, rows; };
 
-Split choose_kv8_split(int B, int T, int Hq, int Hkv, int max_ctx) {
-  Split s;
-  const int rows = T * (Hq / Hkv);
+Shape row_shape(int T, int G) {
+  Shape s;
+  const int rows = T * G;
   s.nt = rows > 8 ? 2 : 1;
   s.row_tiles = (rows + 8 * s.nt - 1) / (8 * s.nt);
-  const long long items = (long long)B * Hkv * s.row_tiles;
-  long long n = (3LL * sm_count() + items - 1) / items;
-  const int unit = AW * 16;
-  long long tokens = (max_ctx + n - 1) / n;
-  if (tokens < 256) tokens = 256;
-  tokens = (tokens + unit - 1) / unit * unit;
-  if (tokens > max_ctx) tokens = (max_ctx + unit - 1) / unit * unit;
-  s.tokens = (int)tokens;
-  s.n_splits = (int)((max_ctx + tokens - 1) / tokens);
+  s.rows = rows < 8 * s.nt ? rows : 8 * s.nt;
   return s;
 }
 
-size_t part_bytes(const Split& s, int B, int T, int Hq, int hd) {
-  return s.n_splits > 1 ? (size_t)B * T * Hq * s.n_splits * (hd + 2) * sizeof(float) : 0;
+size_t parts_of(const Shape& s) { return (size_t)2 * AW * sm_count() * s.rows; }
+
+size_t scratch_of(const Shape& s, int B, int hd, int max_ctx) {
+  if (max_ctx <= TILE) return 0;         // no item has a second tile
+  return (parts_of(s) * (hd + 2) + (size_t)B + 1) * sizeof(float);
 }
 
-template <int HD, int CODE, bool BF16>
-es_status_t launch(const Kv8AttnParams& p, int nt, cudaStream_t s) {
-  const dim3 grid(p.n_splits, p.Hkv * p.row_tiles, p.B);
-  if (nt == 1) ES_CUDA_CHECK(launch_kernel(kv8_attn_kernel<HD, CODE, BF16, 1>, grid, dim3(AW * 32), 0, s, false, p));
-  else ES_CUDA_CHECK(launch_kernel(kv8_attn_kernel<HD, CODE, BF16, 2>, grid, dim3(AW * 32), 0, s, false, p));
-  if (p.n_splits > 1) {
-    const long long rows = (long long)p.B * p.T * p.Hq;
-    ES_CUDA_CHECK(launch_kernel(kv8_merge_kernel<HD, BF16>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, s, true, p));
-  }
+template <int HD, int CODE, int NT, int SUB>
+es_status_t launch_sub(const Kv8Maps& maps, const Kv8AttnParams& p, cudaStream_t s) {
+  constexpr int RINGS = AW * SLOTS * TILE * HD + 1024;     // and room to align them
+  const size_t smem = RINGS + (size_t)(p.B + 1) * sizeof(int);
+  auto kern = kv8_attn_kernel<HD, CODE, NT, SUB>;
+  ES_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, RINGS + (KV8_MAX_B + 1) * (int)sizeof(int)));
+  ES_CUDA_CHECK(launch_kernel(kern, dim3(sm_count()), dim3(AW * 32), smem, s, false, maps, p));
+  if (p.plan)
+    ES_CUDA_CHECK(launch_kernel(kv8_merge_kernel<HD>, dim3(p.Hq, p.T, p.B), dim3(128), 0, s, true, p, AW * sm_count()));
   return ES_OK;
+}
+
+template <int HD, int CODE>
+es_status_t launch(const Kv8Maps& maps, const Kv8AttnParams& p, int nt, cudaStream_t s) {
+  if (nt == 1) {
+    if (p.P >= 64) return launch_sub<HD, CODE, 1, 64>(maps, p, s);
+    return p.P == 32 ? launch_sub<HD, CODE, 1, 32>(maps, p, s) : launch_sub<HD, CODE, 1, 16>(maps, p, s);
+  }
+  return p.P >= 32 ? launch_sub<HD, CODE, 2, 32>(maps, p, s) : launch_sub<HD, CODE, 2, 16>(maps, p, s);
 }
 
 es_status_t check_heads(int B, int T, int Hq, int Hkv, int hd, int page_tokens, int max_ctx) {
   if (B <= 0 || T <= 0 || Hq <= 0 || Hkv <= 0 || hd <= 0 || page_tokens <= 0 || max_ctx <= 0) return fail(ES_ERR_INVALID_ARG, "bad sizes");
   if (Hq % Hkv != 0) return fail(ES_ERR_SHAPE, "Hq must be a multiple of Hkv");
   if (hd != 64 && hd != 128) return fail(ES_ERR_SHAPE, "head_dim must be 64 or 128");
-  const long long rows = (long long)T * (Hq / Hkv);
   if (max_ctx > (1 << 30)) return fail(ES_ERR_RANGE, "max_ctx exceeds 2^30");
-  if (B > 65535 || rows > 65535 || (rows + 15) / 16 * Hkv > 32767 || (long long)B * T * Hq > (1LL << 30))
-    return fail(ES_ERR_RANGE, "B, T or the head counts exceed one launch");
+  if (B > KV8_MAX_B) return fail(ES_ERR_RANGE, "B = %d exceeds %d sequences", B, KV8_MAX_B);
+  if (T > 65535 || (long long)T * (Hq / Hkv) > 65535) return fail(ES_ERR_RANGE, "T * (Hq / Hkv) exceeds one launch");
+  const Shape s = row_shape(T, Hq / Hkv);
+  if ((long long)B * Hkv * s.row_tiles * ((max_ctx + TILE - 1) / TILE) > (1LL << 30))
+    return fail(ES_ERR_RANGE, "B * heads * max_ctx exceeds one launch");
   return ES_OK;
 }
 
@@ -414,7 +571,7 @@ size_t es_op_decode_attention_kv8_scratch_bytes(int32_t B, int32_t T, int32_t Hq
                                                 int32_t page_tokens, int32_t max_ctx) {
   using namespace es;
   if (check_heads(B, T, Hq, Hkv, hd, page_tokens, max_ctx) != ES_OK) return 0;
-  return part_bytes(choose_kv8_split(B, T, Hq, Hkv, max_ctx), B, T, Hq, hd);
+  return scratch_of(row_shape(T, Hq / Hkv), B, hd, max_ctx);
 }
 
 es_status_t es_op_decode_attention_kv8(const void* q, int32_t dtype, int64_t q_stride, const void* k_pages,
@@ -432,25 +589,29 @@ es_status_t es_op_decode_attention_kv8(const void* q, int32_t dtype, int64_t q_s
   if (pages_per_seq <= 0) return fail(ES_ERR_INVALID_ARG, "bad sizes");
   if ((long long)max_ctx > (long long)page_tokens * pages_per_seq) return fail(ES_ERR_RANGE, "max_ctx exceeds the block table");
   if (q_stride < (int64_t)Hq * hd || q_stride % 8) return fail(ES_ERR_INVALID_ARG, "q_stride must be a multiple of 8, at least Hq * hd");
-  if (((uintptr_t)q | (uintptr_t)k_pages | (uintptr_t)v_pages | (uintptr_t)scratch) % 16)
+  if (((uintptr_t)q | (uintptr_t)k_pages | (uintptr_t)v_pages | (uintptr_t)scratch) % 16 || (uintptr_t)out % 4)
     return fail(ES_ERR_INVALID_ARG, "q, pages and scratch must be 16-byte aligned");
-  const Split sp = choose_kv8_split(B, T, Hq, Hkv, max_ctx);
-  const size_t need = part_bytes(sp, B, T, Hq, hd);
+  const Shape sh = row_shape(T, Hq / Hkv);
+  const size_t need = scratch_of(sh, B, hd, max_ctx);
   if (scratch_bytes < need || (need && !scratch)) return fail(ES_ERR_WORKSPACE, "scratch: %zu bytes given, %zu needed", scratch ? scratch_bytes : (size_t)0, need);
   int log2P = 0;
   while ((1 << log2P) < page_tokens) ++log2P;
-  const size_t rows = (size_t)B * T * Hq;
-  Kv8AttnParams p{q, q_stride, (const uint8_t*)k_pages, (const uint8_t*)v_pages, k_scale, v_scale, block_table, ctx_len, out,
-                  (float*)scratch, (float*)scratch + rows * sp.n_splits * hd, B, T, Hq, Hkv, Hq / Hkv, page_tokens, log2P,
-                  pages_per_seq, n_pages, max_ctx, sp.row_tiles, sp.n_splits, sp.tokens};
-  const bool bf16 = dtype == ES_DTYPE_BF16;
+  // pages as 128-byte lines (of one token, or of two when hd is 64); a copy takes what lies together of a tile.  The
+  // helper's matrix of 64 fp16 columns moves bytes as they are
+  Kv8Maps maps;
+  const int64_t lines = (int64_t)n_pages * Hkv * page_tokens * hd / 128;
+  const int box_lines = (page_tokens < TILE ? page_tokens : TILE) * hd / 128;
+  if (lines > INT32_MAX) return fail(ES_ERR_RANGE, "a page pool exceeds 2^31 lines of 128 bytes");
+  ES_TRY(tma_encode_2d_f16(&maps.k, k_pages, lines, 64, 64, box_lines));
+  ES_TRY(tma_encode_2d_f16(&maps.v, v_pages, lines, 64, 64, box_lines));
+  float* part = (float*)scratch;
+  const size_t parts = parts_of(sh);
+  Kv8AttnParams p{q, q_stride, k_scale, v_scale, block_table, ctx_len, out, part, part + parts * hd,
+                  need ? (int*)(part + parts * (hd + 2)) : nullptr, B, T, Hq, Hkv, Hq / Hkv, page_tokens, log2P, pages_per_seq,
+                  n_pages, max_ctx, sh.row_tiles, sh.rows, dtype == ES_DTYPE_BF16};
   cudaStream_t s = (cudaStream_t)stream;
-  if (hd == 128) {
-    if (code == CODE_I8) return bf16 ? launch<128, CODE_I8, true>(p, sp.nt, s) : launch<128, CODE_I8, false>(p, sp.nt, s);
-    return bf16 ? launch<128, CODE_E4M3, true>(p, sp.nt, s) : launch<128, CODE_E4M3, false>(p, sp.nt, s);
-  }
-  if (code == CODE_I8) return bf16 ? launch<64, CODE_I8, true>(p, sp.nt, s) : launch<64, CODE_I8, false>(p, sp.nt, s);
-  return bf16 ? launch<64, CODE_E4M3, true>(p, sp.nt, s) : launch<64, CODE_E4M3, false>(p, sp.nt, s);
+  if (hd == 128) return code == CODE_I8 ? launch<128, CODE_I8>(maps, p, sh.nt, s) : launch<128, CODE_E4M3>(maps, p, sh.nt, s);
+  return code == CODE_I8 ? launch<64, CODE_I8>(maps, p, sh.nt, s) : launch<64, CODE_E4M3>(maps, p, sh.nt, s);
 }
 
 }  // extern "C"
