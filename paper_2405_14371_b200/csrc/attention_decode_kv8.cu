@@ -1,10 +1,10 @@
 // Decode attention over the paged 8-bit cache (TMA + mma.sync m16n8k16), for one or a few query tokens per sequence.
 //
 // The bound is reading every code of K and V once, so the work is cut for an even and unbroken stream of bytes: the keys of
-// all (sequence, KV head) items, in tiles of 64 tokens, form one line, and every warp of the machine (8 per SM, one CTA
-// per SM) takes an equal stretch of it, whatever the lengths.  A warp feeds itself: one lane asks for a tile's K and V
-// through TMA into the warp's own ring of three half tiles (24 KB), so up to 192 KB per SM are on their way while it computes,
-// and nothing between the warps waits until they are done.  An item whose tiles lie in one stretch is finished by its
+// all (sequence, KV head) items, in tiles of 64 tokens, form one line, and every warp of the machine (8 or 12 in a CTA,
+// one CTA per SM) takes an equal stretch of it, whatever the lengths.  A warp feeds itself: it asks for a tile's K and V
+// through TMA into a ring of its own, so that up to 192 KB per SM are on their way while it computes, and no warp waits for
+// another.  An item whose tiles lie in one stretch is finished by its
 // warp; the others leave (o, max, sum), which a second kernel merges in order of the stretches.
 //
 // For a tile and a tile of 8 (NT = 1) or 16 (NT = 2) query rows (T tokens x G heads of the KV head's group):
@@ -35,9 +35,11 @@
 namespace es {
 namespace {
 
-constexpr int AW = 8;                    // warps of a CTA
 constexpr int TILE = 64;                 // tokens of a tile
-constexpr int SLOTS = 3;                 // half tiles of a warp's ring
+// Warps of a CTA and half tiles of a warp's ring.  8 query rows leave registers for 12 warps, whose latencies hide one
+// another's better than 8 warps' do; two half tiles each are then what 192 KB hold.
+template <int HD, int NT> constexpr int WARPS = NT == 1 ? 12 : 8;
+template <int HD, int NT> constexpr int SLOTS = HD == 128 && NT == 1 ? 2 : 3;
 constexpr int KV8_MAX_B = 4096;          // sequences whose tile sums fit beside the rings
 
 struct Kv8AttnParams {
@@ -58,6 +60,13 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// the same with nothing to add to
+__device__ __forceinline__ void mma_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+               : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 
 __device__ __forceinline__ float ex2(float x) {
@@ -85,10 +94,11 @@ __device__ __forceinline__ uint32_t two_outputs(float a, float b, int bf16) {
   return h2_bits(__floats2half2_rn(a, b));
 }
 
-// A place on the line of tiles: sequence b, item (kv head, row tile) of it, tile of the item.
+// A place on the line of tiles: sequence b, KV head and row tile in it, tile of that item.
 struct Cursor {
-  int b, item, tile, tiles;
-  __device__ __forceinline__ void seek(int at, const int* pre, int B, int items) {
+  int b, kvh, rt, tile, tiles;
+  __device__ __forceinline__ void seek(int at, const int* pre, int B, int Hkv, int row_tiles) {
+    const int items = Hkv * row_tiles;
     int lo = 0, hi = B;                  // pre[lo] * items <= at < pre[hi] * items
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -96,15 +106,18 @@ struct Cursor {
     }
     b = lo;
     tiles = pre[b + 1] - pre[b];
-    const int r = at - pre[b] * items;
-    item = r / tiles;
+    const int r = at - pre[b] * items, item = r / tiles;
     tile = r - item * tiles;
+    kvh = item / row_tiles;
+    rt = item - kvh * row_tiles;
   }
-  __device__ __forceinline__ void next(const int* pre, int B, int items) {
+  __device__ __forceinline__ void next(const int* pre, int B, int Hkv, int row_tiles) {
     if (++tile < tiles) return;
     tile = 0;
-    if (++item < items) return;
-    item = 0;
+    if (++rt < row_tiles) return;
+    rt = 0;
+    if (++kvh < Hkv) return;
+    kvh = 0;
     if (++b < B) tiles = pre[b + 1] - pre[b];
   }
 };
@@ -113,8 +126,9 @@ struct Cursor {
 __device__ __forceinline__ int stretch_of(int total, int warps) { return (total + warps - 1) / warps; }
 
 template <int HD, int CODE, int NT, int SUB>
-__global__ void __launch_bounds__(AW * 32, 1) kv8_attn_kernel(const __grid_constant__ Kv8Maps maps, const Kv8AttnParams p) {
+__global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const __grid_constant__ Kv8Maps maps, const Kv8AttnParams p) {
   pdl_launch_dependents();
+  constexpr int AW = WARPS<HD, NT>, SL = SLOTS<HD, NT>;
   constexpr int J = HD / 64;             // 16-byte pieces of a K row per thread
   constexpr int D = HD / 8;              // dimensions of V per thread
   constexpr int NM = D / 2;              // output MMAs of 16 tokens
@@ -124,17 +138,17 @@ __global__ void __launch_bounds__(AW * 32, 1) kv8_attn_kernel(const __grid_const
   constexpr float LOG2E = 1.4426950408889634f;
   extern __shared__ __align__(1024) unsigned char dyn[];
   unsigned char* ring = dyn + ((1024 - (smem_u32(dyn) & 1023)) & 1023);  // the swizzle goes by address bits 7 to 9
-  __shared__ __align__(8) uint64_t bars[AW * SLOTS];
+  __shared__ __align__(8) uint64_t bars[AW * SL];
   __shared__ int s_warp[AW];
   __shared__ int s_abort;
-  int* pre = reinterpret_cast<int*>(ring + AW * SLOTS * HALF);          // [B + 1] tiles before each sequence
+  int* pre = reinterpret_cast<int*>(ring + AW * SL * HALF);          // [B + 1] tiles before each sequence
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int items = p.Hkv * p.row_tiles, n_rows = p.T * p.G;
 
   if (tid == 0) {
     s_abort = 0;
-    for (int i = 0; i < AW * SLOTS; ++i) mbar_init(smem_u32(bars + i), 1);
+    for (int i = 0; i < AW * SL; ++i) mbar_init(smem_u32(bars + i), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     prefetch_tmap(&maps.k);
     prefetch_tmap(&maps.v);
@@ -170,52 +184,54 @@ __global__ void __launch_bounds__(AW * 32, 1) kv8_attn_kernel(const __grid_const
   const int begin = min((int64_t)me * per_warp, (int64_t)total), end = min(begin + per_warp, total);
   if (begin >= end) return;
 
-  const uint32_t my_ring = smem_u32(ring) + warp * SLOTS * HALF, my_bars = smem_u32(bars) + warp * SLOTS * 8;
+  const uint32_t my_ring = smem_u32(ring) + warp * SL * HALF, my_bars = smem_u32(bars) + warp * SL * 8;
   const int box = min(p.P, TILE), log2box = min(p.log2P, 6), boxes = TILE >> log2box;        // tokens that lie together
   Cursor c, ahead;
-  c.seek(begin, pre, p.B, items);
+  c.seek(begin, pre, p.B, p.Hkv, p.row_tiles);
   ahead = c;
   const int n_half = 2 * (end - begin);
-  int asked = 0;                         // half tiles asked for: K, V, K, V, ...
-  float ks_a = 0.f, vs_a = 0.f;          // lane i: scales of box i of the tile asked for last, and whether its page exists
-  int row_a = -1;                        // its first 128-byte line, or -1
+  int asked = 0, ask_slot = 0;           // half tiles asked for: K, V, K, V, ...
+  float ks_a = 0.f, vs_a = 0.f;          // lane i: scales of box i of the tile asked for last, and its first 128-byte line
+  int row_a = -1;                        // (-1: nothing there)
   float ks_c = 0.f, vs_c = 0.f;
   unsigned ok_a = 0, ok_c = 0;
-
   auto ask = [&]() {
-    const int slot = asked % SLOTS;
     const bool is_v = asked & 1;
     if (!is_v) {
       row_a = -1;
       const int tok = ahead.tile * TILE + (lane << log2box);
-      const int n = min(p.ctx_len[ahead.b], p.max_ctx);
-      if (lane < boxes && tok < n) {
+      if (lane < boxes && tok < min(p.ctx_len[ahead.b], p.max_ctx)) {
         const int page = p.table[(int64_t)ahead.b * p.pps + (tok >> p.log2P)];
-        if (page >= 0 && page < p.n_pages) {
-          const int64_t ph = (int64_t)page * p.Hkv + ahead.item / p.row_tiles;
+        if ((unsigned)page < (unsigned)p.n_pages) {
+          const int ph = page * p.Hkv + ahead.kvh;         // the pool has less than 2^31 lines, so this fits
           ks_a = p.ks[ph];
           vs_a = p.vs[ph];
-          row_a = (int)((ph * p.P + (tok & (p.P - 1))) * HD / 128);
+          row_a = (int)((((unsigned)ph << p.log2P) + (tok & (p.P - 1))) / (128 / HD));
         }
       }
       ok_a = __ballot_sync(~0u, row_a >= 0);
     }
-    const uint32_t bar = my_bars + slot * 8;
+    const uint32_t bar = my_bars + ask_slot * 8;
     if (lane == 0) mbar_expect_tx(bar, __popc(ok_a) * (HD << log2box));
     __syncwarp();
-    if (row_a >= 0) tma_load_2d(my_ring + slot * HALF + lane * (HD << log2box), is_v ? &maps.v : &maps.k, 0, row_a, bar);
-    if (is_v) ahead.next(pre, p.B, items);
+    if (row_a >= 0) tma_load_2d(my_ring + ask_slot * HALF + lane * (HD << log2box), is_v ? &maps.v : &maps.k, 0, row_a, bar);
+    if (is_v) ahead.next(pre, p.B, p.Hkv, p.row_tiles);
     ++asked;
+    if (++ask_slot == SL) ask_slot = 0;
   };
-  int used = 0;
-  auto arrived = [&]() -> bool {         // the oldest half tile that was not yet used
-    return __all_sync(~0u, mbar_wait(my_bars + (used % SLOTS) * 8, (used / SLOTS) & 1, &s_abort, nullptr, 1));
+  int used = 0, slot = 0, parity = 0;    // half tiles used, the place of the next and the phase that it completes
+  auto arrived = [&]() -> bool { return __all_sync(~0u, mbar_wait(my_bars + slot * 8, parity, &s_abort, nullptr, 1)); };
+  auto release = [&]() {
+    __syncwarp();
+    ++used;
+    if (++slot == SL) { slot = 0; parity ^= 1; }
+    if (asked < n_half) ask();
   };
 
   ask();                                 // the first tile's K
   ks_c = ks_a; vs_c = vs_a; ok_c = ok_a;
   ask();                                 // its V
-  if (asked < n_half) ask();             // the second tile's K
+  if (SL == 3 && asked < n_half) ask();  // the second tile's K, whose scales wait in ks_a, vs_a
 
   int limit[NT];
   float qscale[NT];
@@ -230,14 +246,13 @@ __global__ void __launch_bounds__(AW * 32, 1) kv8_attn_kernel(const __grid_const
       fresh = false;
       ctx = max(0, min(p.ctx_len[c.b], p.max_ctx));
       item_begin = at - c.tile;
-      const int kvh = c.item / p.row_tiles, rt = c.item - kvh * p.row_tiles;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const int i = rt * ROWS + 8 * n + g, token = i / p.G;
+        const int i = c.rt * ROWS + 8 * n + g, token = i / p.G;
         const bool real = i < n_rows;
-        limit[n] = real ? ctx - p.T + token + 1 : 0;
+        limit[n] = real ? ctx - p.T + token + 1 : ctx;     // rows that do not exist have zero queries and are not stored
         qscale[n] = 1.f;
-        const uint16_t* row = reinterpret_cast<const uint16_t*>(p.q) + ((int64_t)c.b * p.T + token) * p.q_stride + (int64_t)(kvh * p.G + i - token * p.G) * HD + t * (HD / 4);
+        const uint16_t* row = reinterpret_cast<const uint16_t*>(p.q) + ((int64_t)c.b * p.T + token) * p.q_stride + (int64_t)(c.kvh * p.G + i - token * p.G) * HD + t * (HD / 4);
 #pragma unroll
         for (int j = 0; j < 2 * J; ++j) {
           const uint4 x = real ? *reinterpret_cast<const uint4*>(row + 8 * j) : make_uint4(0, 0, 0, 0);
@@ -269,10 +284,9 @@ __global__ void __launch_bounds__(AW * 32, 1) kv8_attn_kernel(const __grid_const
     if (!arrived()) { running = false; break; }
     float s[TILE / 8][4];
     {
-      const uint32_t base = my_ring + (used % SLOTS) * HALF;
+      const uint32_t base = my_ring + slot * HALF;
 #pragma unroll
       for (int nt = 0; nt < TILE / 8; ++nt) {
-        s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
           // the 16-byte pieces of token 8 nt + g: J t + j of its row, moved by the swizzle of its 128-byte line
@@ -284,17 +298,16 @@ __global__ void __launch_bounds__(AW * 32, 1) kv8_attn_kernel(const __grid_const
           for (int i = 0; i < 4; ++i) {
             uint32_t lo, hi;
             codes_to_h2<CODE>(w[i], lo, hi);
-            mma(s[nt], qa[0][8 * j + 2 * i], NT == 2 ? qa[NT - 1][8 * j + 2 * i] : 0u, qa[0][8 * j + 2 * i + 1],
-                NT == 2 ? qa[NT - 1][8 * j + 2 * i + 1] : 0u, lo, hi);
+            const uint32_t a1 = NT == 2 ? qa[NT - 1][8 * j + 2 * i] : 0u, a3 = NT == 2 ? qa[NT - 1][8 * j + 2 * i + 1] : 0u;
+            if (j == 0 && i == 0) mma_first(s[nt], qa[0][0], a1, qa[0][1], a3, lo, hi);
+            else mma(s[nt], qa[0][8 * j + 2 * i], a1, qa[0][8 * j + 2 * i + 1], a3, lo, hi);
           }
         }
       }
     }
-    __syncwarp();
-    ++used;
-    if (asked < n_half) ask();           // in the place of the half tile just read: the next tile's V
+    release();                           // a ring of two takes this tile's successor only now; a longer one has it already
 
-    const uint32_t vbase = my_ring + (used % SLOTS) * HALF;
+    const uint32_t vbase = my_ring + slot * HALF;
     bool v_here = false;
 #pragma unroll
     for (int sub = 0; sub < NSUB; ++sub) {
@@ -305,6 +318,8 @@ __global__ void __launch_bounds__(AW * 32, 1) kv8_attn_kernel(const __grid_const
       // ---- softmax of the sub-tile ----
       uint32_t ph[NT][KK][2], pl[NT][KK][2];               // probabilities, hi and lo halves: B fragments of the output MMAs
       float al[NT][2], be[NT][2];                          // factors of rows 2 t and 2 t + 1
+      const bool inner = T0 + SUB <= ctx - p.T + 1;        // every row sees all of it
+      bool same = true;                                    // no row's maximum changes
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         float x[2 * KK][2], mx = -INFINITY;
@@ -313,7 +328,8 @@ __global__ void __launch_bounds__(AW * 32, 1) kv8_attn_kernel(const __grid_const
         for (int nt = 0; nt < 2 * KK; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            x[nt][e] = T0 + 8 * nt + 2 * t + e < limit[n] ? s[sub * 2 * KK + nt][2 * n + e] * f : -INFINITY;
+            x[nt][e] = s[sub * 2 * KK + nt][2 * n + e] * f;
+            if (!inner && T0 + 8 * nt + 2 * t + e >= limit[n]) x[nt][e] = -INFINITY;
             mx = fmaxf(mx, x[nt][e]);
           }
         mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 1));
@@ -340,6 +356,7 @@ __global__ void __launch_bounds__(AW * 32, 1) kv8_attn_kernel(const __grid_const
         const float beta = sees ? join * v_s : 0.f;
         l_run[n] = sees ? l_run[n] * alpha + sum * join : l_run[n];
         m_run[n] = mn;
+        same = same && alpha == 1.f;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           al[n][i] = __shfl_sync(~0u, alpha, (2 * t + i) * 4);
@@ -350,10 +367,14 @@ __global__ void __launch_bounds__(AW * 32, 1) kv8_attn_kernel(const __grid_const
         v_here = true;
         if (!arrived()) { running = false; break; }
       }
-      // ---- output: MMA i gives dimensions D g + i (rows 0..7) and D g + D / 2 + i (rows 8..15) ----
-      uint32_t v[KK][4][D / 4];
+      if (!__all_sync(~0u, same)) {
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk)
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < NM; ++i) { o[n][i][0] *= al[n][0]; o[n][i][1] *= al[n][1]; o[n][i][2] *= al[n][0]; o[n][i][3] *= al[n][1]; }
+      }
+      // ---- output: MMA i gives dimensions D g + i (rows 0..7) and D g + D / 2 + i (rows 8..15) ----
+      auto load_v = [&](int kk, uint32_t (&v)[4][D / 4]) {
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) {
           // token 16 kk + 2 t + {0, 1} (+ 8) of the sub-tile: its dimensions D g ..
@@ -361,78 +382,107 @@ __global__ void __launch_bounds__(AW * 32, 1) kv8_attn_kernel(const __grid_const
           if constexpr (HD == 128) {
             const uint32_t line = sub * SUB + 16 * kk + 8 * up + 2 * t + e;
             const uint4 x = lds16(vbase + line * 128 + ((g ^ (line & 7)) << 4));
-            v[kk][q4][0] = x.x; v[kk][q4][1] = x.y; v[kk][q4][2] = x.z; v[kk][q4][3] = x.w;
+            v[q4][0] = x.x; v[q4][1] = x.y; v[q4][2] = x.z; v[q4][3] = x.w;
           } else {
             const uint32_t line = sub * (SUB / 2) + 8 * kk + 4 * up + t;
             const uint2 x = lds8(vbase + line * 128 + (((4 * e + (g >> 1)) ^ (line & 7)) << 4) + 8 * (g & 1));
-            v[kk][q4][0] = x.x; v[kk][q4][1] = x.y;
+            v[q4][0] = x.x; v[q4][1] = x.y;
           }
         }
-      if (T0 + SUB > ctx) {              // the last tokens' sub-tile: nothing behind them enters a product
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk)
+        if (T0 + SUB > ctx) {            // the last tokens' sub-tile: nothing behind them enters a product
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4)
             if (T0 + 16 * kk + 8 * (q4 >> 1) + 2 * t + (q4 & 1) >= ctx)
 #pragma unroll
-              for (int w = 0; w < D / 4; ++w) v[kk][q4][w] = 0;
-      }
+              for (int w = 0; w < D / 4; ++w) v[q4][w] = 0;
+        }
+      };
+      // A registers 0..3 of the four MMAs that words w and w + D / 8 of the four tokens make
+      auto fragments = [&](const uint32_t (&v)[4][D / 4], int w, uint32_t (&a)[4][4]) {
 #pragma unroll
-      for (int w = 0; w < D / 8; ++w) {
-        float acc[4][NT][4];
+        for (int q2 = 0; q2 < 2; ++q2)
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-          for (int n = 0; n < NT; ++n) acc[d][n][0] = acc[d][n][1] = acc[d][n][2] = acc[d][n][3] = 0.f;
+          for (int half = 0; half < 2; ++half) {
+            const uint32_t x = v[2 * q2][w + half * (D / 8)], y = v[2 * q2 + 1][w + half * (D / 8)];
+            codes_to_h2<CODE>(__byte_perm(x, y, 0x5140), a[2 * q2 + half][0], a[2 * q2 + half][1]);
+            codes_to_h2<CODE>(__byte_perm(x, y, 0x7362), a[2 * q2 + half][2], a[2 * q2 + half][3]);
+          }
+      };
+      if constexpr (NT == 1) {           // accumulators of the whole sub-tile, V as it is needed
+        float acc[NM][4];
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
-          uint32_t a[4][4];              // A registers 0..3 of four MMAs
+          uint32_t v[4][D / 4], a[4][4];
+          load_v(kk, v);
 #pragma unroll
-          for (int q2 = 0; q2 < 2; ++q2)
+          for (int w = 0; w < D / 8; ++w) {
+            fragments(v, w, a);
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              const uint32_t x = v[kk][2 * q2][w + half * (D / 8)], y = v[kk][2 * q2 + 1][w + half * (D / 8)];
-              codes_to_h2<CODE>(__byte_perm(x, y, 0x5140), a[2 * q2 + half][0], a[2 * q2 + half][1]);
-              codes_to_h2<CODE>(__byte_perm(x, y, 0x7362), a[2 * q2 + half][2], a[2 * q2 + half][3]);
+            for (int d = 0; d < 4; ++d) {
+              if (kk == 0) mma_first(acc[4 * w + d], a[0][d], a[1][d], a[2][d], a[3][d], ph[0][kk][0], ph[0][kk][1]);
+              else mma(acc[4 * w + d], a[0][d], a[1][d], a[2][d], a[3][d], ph[0][kk][0], ph[0][kk][1]);
             }
+#pragma unroll
+            for (int d = 0; d < 4; ++d) mma(acc[4 * w + d], a[0][d], a[1][d], a[2][d], a[3][d], pl[0][kk][0], pl[0][kk][1]);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < NM; ++i)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) o[0][i][k] += acc[i][k] * be[0][k & 1];
+      } else {                           // two row blocks: accumulators of four MMAs, all of V held
+        uint32_t v[KK][4][D / 4];
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) load_v(kk, v[kk]);
+#pragma unroll
+        for (int w = 0; w < D / 8; ++w) {
+          float acc[4][NT][4];
+#pragma unroll
+          for (int kk = 0; kk < KK; ++kk) {
+            uint32_t a[4][4];
+            fragments(v[kk], w, a);
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+              for (int n = 0; n < NT; ++n) {
+                if (kk == 0) mma_first(acc[d][n], a[0][d], a[1][d], a[2][d], a[3][d], ph[n][kk][0], ph[n][kk][1]);
+                else mma(acc[d][n], a[0][d], a[1][d], a[2][d], a[3][d], ph[n][kk][0], ph[n][kk][1]);
+                mma(acc[d][n], a[0][d], a[1][d], a[2][d], a[3][d], pl[n][kk][0], pl[n][kk][1]);
+              }
+          }
 #pragma unroll
           for (int d = 0; d < 4; ++d)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              mma(acc[d][n], a[0][d], a[1][d], a[2][d], a[3][d], ph[n][kk][0], ph[n][kk][1]);
-              mma(acc[d][n], a[0][d], a[1][d], a[2][d], a[3][d], pl[n][kk][0], pl[n][kk][1]);
-            }
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) o[n][4 * w + d][k] += acc[d][n][k] * be[n][k & 1];
         }
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[n][4 * w + d][i] = o[n][4 * w + d][i] * al[n][i & 1] + acc[d][n][i] * be[n][i & 1];
       }
     }
     if (!running) break;
     if (!v_here && !arrived()) { running = false; break; }
-    __syncwarp();
-    ++used;
-    ks_c = ks_a; vs_c = vs_a; ok_c = ok_a;                 // the next tile's
-    if (asked < n_half) ask();                             // the K of the one after
+    if (SL == 2) {                       // the next tile's K was asked for above or is asked for now: its scales come then
+      release();
+      ks_c = ks_a; vs_c = vs_a; ok_c = ok_a;
+    } else {                             // they wait in ks_a, vs_a until the K after it is asked for
+      ks_c = ks_a; vs_c = vs_a; ok_c = ok_a;
+      release();
+    }
 
     // ---- the item's end, or the stretch's ----
     const bool item_ends = c.tile + 1 == c.tiles;
     if (item_ends || at + 1 == end) {
-      const int kvh = c.item / p.row_tiles, rt = c.item - kvh * p.row_tiles;
       const bool whole = item_ends && item_begin >= begin;
       const int64_t part = 2 * (int64_t)me + (item_begin >= begin);       // a stretch has two split items at most
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {                      // this thread holds dimensions D g .. D g + D - 1 of row 8 n + 2 t + e
-          const int r = 8 * n + 2 * t + e, i = rt * ROWS + r, token = i / p.G;
+          const int r = 8 * n + 2 * t + e, i = c.rt * ROWS + r, token = i / p.G;
           const float m = __shfl_sync(~0u, m_run[n], (2 * t + e) * 4), l = __shfl_sync(~0u, l_run[n], (2 * t + e) * 4);
           if (i >= n_rows) continue;
           if (whole) {
-            const int64_t row = ((int64_t)c.b * p.T + token) * p.Hq + kvh * p.G + (i - token * p.G);
+            const int64_t row = ((int64_t)c.b * p.T + token) * p.Hq + c.kvh * p.G + (i - token * p.G);
             uint32_t* to = reinterpret_cast<uint32_t*>(p.out) + (row * HD + D * g) / 2;
             const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
@@ -451,13 +501,14 @@ __global__ void __launch_bounds__(AW * 32, 1) kv8_attn_kernel(const __grid_const
         }
       fresh = true;
     }
-    c.next(pre, p.B, items);
+    c.next(pre, p.B, p.Hkv, p.row_tiles);
   }
   // a wait that ran out: let this warp's copies that are under way land before its shared memory goes
   if (!running)
     for (; used < asked; ++used) {
-      int dummy = 0;
-      mbar_wait(my_bars + (used % SLOTS) * 8, (used / SLOTS) & 1, &dummy, nullptr, 1);
+      int nobody = 0;
+      mbar_wait(my_bars + slot * 8, parity, &nobody, nullptr, 1);
+      if (++slot == SL) { slot = 0; parity ^= 1; }
     }
 }
 
@@ -521,7 +572,9 @@ Shape row_shape(int T, int G) {
   return s;
 }
 
-size_t parts_of(const Shape& s) { return (size_t)2 * AW * sm_count() * s.rows; }
+int warps_of(const Shape& s) { return (s.nt == 1 ? WARPS<128, 1> : WARPS<128, 2>) * sm_count(); }
+
+size_t parts_of(const Shape& s) { return (size_t)2 * warps_of(s) * s.rows; }
 
 size_t scratch_of(const Shape& s, int B, int hd, int max_ctx) {
   if (max_ctx <= TILE) return 0;         // no item has a second tile
@@ -530,7 +583,8 @@ size_t scratch_of(const Shape& s, int B, int hd, int max_ctx) {
 
 template <int HD, int CODE, int NT, int SUB>
 es_status_t launch_sub(const Kv8Maps& maps, const Kv8AttnParams& p, cudaStream_t s) {
-  constexpr int RINGS = AW * SLOTS * TILE * HD + 1024;     // and room to align them
+  constexpr int AW = WARPS<HD, NT>;
+  constexpr int RINGS = AW * SLOTS<HD, NT> * TILE * HD + 1024;       // and room to align them
   const size_t smem = RINGS + (size_t)(p.B + 1) * sizeof(int);
   auto kern = kv8_attn_kernel<HD, CODE, NT, SUB>;
   ES_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, RINGS + (KV8_MAX_B + 1) * (int)sizeof(int)));
