@@ -1,11 +1,16 @@
 // Decode attention over the paged 8-bit cache (TMA + mma.sync m16n8k16), for one or a few query tokens per sequence.
 //
-// The bound is reading every code of K and V once, so the work is cut for an even and unbroken stream of bytes: the keys of
-// all (sequence, KV head) items, in tiles of 64 tokens, form one line, and every warp of the machine (8 or 12 in a CTA,
-// one CTA per SM) takes an equal stretch of it, whatever the lengths.  A warp feeds itself: it asks for a tile's K and V
-// through TMA into a ring of its own, so that up to 192 KB per SM are on their way while it computes, and no warp waits for
-// another.  An item whose tiles lie in one stretch is finished by its
-// warp; the others leave (o, max, sum), which a second kernel merges in order of the stretches.
+// The bound is reading every code of K and V once, so the work is cut for an even and unbroken stream of bytes.  An item is
+// one sequence and KV head (and row tile, below); its keys come in tiles of 64 or 32 tokens.  A warp feeds itself: it asks
+// for a tile's K and V through TMA into a ring of its own, so that up to 192 KB per SM are on their way while it computes,
+// and no warp waits for another.  Two ways of handing out the tiles:
+//
+//   * stretches: the tiles of all items form one line, and every warp of the machine (8 or 12 in a CTA, one CTA per SM)
+//     takes an equal stretch of it, whatever the lengths.  An item that lies in one stretch is finished by its warp; the
+//     others leave (o, max, sum), which a second kernel merges in order of the stretches;
+//   * groups: where there are no more items than SMs and little to read for each, an item belongs to a CTA or a cluster of
+//     2 to 8, whose warps share its tiles and join through (distributed) shared memory.  That saves the second kernel,
+//     which is what such calls spend most of their time on.
 //
 // For a tile and a tile of 8 (NT = 1) or 16 (NT = 2) query rows (T tokens x G heads of the KV head's group):
 //   * codes become fp16, which holds every code of both types exactly, on their way from shared memory into the
@@ -15,8 +20,8 @@
 //   * scores S[row, token]: A = query rows, B = K.  The scale of K's page, 1/sqrt(hd) and the query's own exponent are
 //     factors of the finished score;
 //   * softmax in sub-tiles (SUB tokens of one page) against the sub-tile's own maximum, in fp32: the probabilities lie in
-//     [0, 1] whatever the other pages hold, and enter the next product as two fp16 halves (hi + lo, together 22 bits), so
-//     that rounding them costs the output nothing next to its own;
+//     [0, 2^15] whatever the other pages hold, and enter the next product as two fp16 halves (hi + lo: 22 bits, and nothing
+//     lost above 2^-40 of the largest), so that rounding them costs the output nothing next to its own;
 //   * O^T[dim, row] = V^T P^T into a sub-tile accumulator, which joins the running sum with the factor
 //     (scale of V's page) * exp(sub-tile maximum - new maximum): pages of very different scales cannot wash each other out.
 //
@@ -25,6 +30,7 @@
 //
 // Codes behind the context are zeroed in V and masked by selection in the scores, so that garbage (NaN codes among it)
 // never meets a product; a page whose scale is NaN makes the rows that see it NaN.
+#include <cooperative_groups.h>
 #include <cuda.h>
 
 #include "es_internal.cuh"
@@ -32,14 +38,15 @@
 #include "launch.cuh"
 #include "sm100.cuh"
 
+namespace cg = cooperative_groups;
+
 namespace es {
 namespace {
 
-constexpr int TILE = 64;                 // tokens of a tile
 // Warps of a CTA and half tiles of a warp's ring.  8 query rows leave registers for 12 warps, whose latencies hide one
 // another's better than 8 warps' do; two half tiles each are then what 192 KB hold.
 template <int HD, int NT> constexpr int WARPS = NT == 1 ? 12 : 8;
-template <int HD, int NT> constexpr int SLOTS = HD == 128 && NT == 1 ? 2 : 3;
+template <int HD, int NT, int TILE> constexpr int SLOTS = HD == 128 && NT == 1 && TILE == 64 ? 2 : 3;
 constexpr int KV8_MAX_B = 4096;          // sequences whose tile sums fit beside the rings
 
 struct Kv8AttnParams {
@@ -49,9 +56,9 @@ struct Kv8AttnParams {
   const int *table, *ctx_len;
   void* out;
   float *part_o, *part_ml;               // [2 * warps][rows][hd], [..][rows][2]
-  int* plan;                             // tiles before each sequence [B + 1], written for the merge
   int B, T, Hq, Hkv, G, P, log2P, pps, n_pages, max_ctx;
   int row_tiles, rows, bf16;             // rows = rows of a row tile that are stored
+  int group;                             // CTAs of an item (groups)
 };
 
 struct alignas(64) Kv8Maps { CUtensorMap k, v; };
@@ -125,10 +132,14 @@ struct Cursor {
 // Tiles of a warp's stretch.
 __device__ __forceinline__ int stretch_of(int total, int warps) { return (total + warps - 1) / warps; }
 
-template <int HD, int CODE, int NT, int SUB>
+// Tiles of a sequence; an empty one has a tile without keys, so that somebody writes its rows.
+template <int TILE>
+__device__ __forceinline__ int tiles_of(int ctx, int max_ctx) { return (min(max(ctx, 1), max_ctx) + TILE - 1) / TILE; }
+
+template <int HD, int CODE, int NT, int TILE, int SUB, bool GROUPED>
 __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const __grid_constant__ Kv8Maps maps, const Kv8AttnParams p) {
   pdl_launch_dependents();
-  constexpr int AW = WARPS<HD, NT>, SL = SLOTS<HD, NT>;
+  constexpr int AW = WARPS<HD, NT>, SL = SLOTS<HD, NT, TILE>;
   constexpr int J = HD / 64;             // 16-byte pieces of a K row per thread
   constexpr int D = HD / 8;              // dimensions of V per thread
   constexpr int NM = D / 2;              // output MMAs of 16 tokens
@@ -140,6 +151,7 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
   unsigned char* ring = dyn + ((1024 - (smem_u32(dyn) & 1023)) & 1023);  // the swizzle goes by address bits 7 to 9
   __shared__ __align__(8) uint64_t bars[AW * SL];
   __shared__ int s_warp[AW];
+  __shared__ float2 s_ml[GROUPED ? AW : 1][ROWS];
   __shared__ int s_abort;
   int* pre = reinterpret_cast<int*>(ring + AW * SL * HALF);          // [B + 1] tiles before each sequence
 
@@ -153,13 +165,24 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
     prefetch_tmap(&maps.k);
     prefetch_tmap(&maps.v);
   }
-  // ---- tiles of every sequence; an empty one has a tile without keys, so that somebody writes its rows ----
-  {
+  Cursor c, ahead;
+  int begin, end, me = 0;                // tiles of this warp, and its place among the warps
+  if constexpr (GROUPED) {
+    const int item = blockIdx.x / p.group, in_b = item % items;
+    c.b = item / items;
+    c.kvh = in_b / p.row_tiles;
+    c.rt = in_b - c.kvh * p.row_tiles;
+    c.tiles = tiles_of<TILE>(p.ctx_len[c.b], p.max_ctx);
+    const int workers = p.group * AW, per_warp = stretch_of(c.tiles, workers);
+    begin = min((warp * p.group + (int)blockIdx.x % p.group) * per_warp, c.tiles);
+    end = min(begin + per_warp, c.tiles);
+    c.tile = begin;
+    __syncthreads();
+  } else {
     int before = 0;
     for (int base = 0; base < p.B; base += AW * 32) {
       const int b = base + tid;
-      int v = 0;
-      if (b < p.B) { const int n = min(max(p.ctx_len[b], 1), p.max_ctx); v = (n + TILE - 1) / TILE; }
+      const int v = b < p.B ? tiles_of<TILE>(p.ctx_len[b], p.max_ctx) : 0;
       int inc = v;
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) { const int o = __shfl_up_sync(~0u, inc, d); if (lane >= d) inc += o; }
@@ -174,20 +197,18 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
     }
     if (tid == 0) pre[0] = 0;
     __syncthreads();
+    const int total = pre[p.B] * items;
+    // stretches go round the SMs first: few tiles spread over all of them
+    me = warp * gridDim.x + blockIdx.x;
+    const int per_warp = stretch_of(total, AW * gridDim.x);
+    begin = min((int64_t)me * per_warp, (int64_t)total);
+    end = min(begin + per_warp, total);
+    if (begin >= end) return;
+    c.seek(begin, pre, p.B, p.Hkv, p.row_tiles);
   }
-  if (blockIdx.x == 0 && p.plan)
-    for (int i = tid; i <= p.B; i += AW * 32) p.plan[i] = pre[i];
-  const int total = pre[p.B] * items;
-  // stretches go round the SMs first: few tiles spread over all of them
-  const int me = warp * gridDim.x + blockIdx.x;
-  const int per_warp = stretch_of(total, AW * gridDim.x);
-  const int begin = min((int64_t)me * per_warp, (int64_t)total), end = min(begin + per_warp, total);
-  if (begin >= end) return;
 
   const uint32_t my_ring = smem_u32(ring) + warp * SL * HALF, my_bars = smem_u32(bars) + warp * SL * 8;
-  const int box = min(p.P, TILE), log2box = min(p.log2P, 6), boxes = TILE >> log2box;        // tokens that lie together
-  Cursor c, ahead;
-  c.seek(begin, pre, p.B, p.Hkv, p.row_tiles);
+  const int log2box = min(p.log2P, TILE == 64 ? 6 : 5), boxes = TILE >> log2box;             // tokens that lie together
   ahead = c;
   const int n_half = 2 * (end - begin);
   int asked = 0, ask_slot = 0;           // half tiles asked for: K, V, K, V, ...
@@ -215,7 +236,9 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
     if (lane == 0) mbar_expect_tx(bar, __popc(ok_a) * (HD << log2box));
     __syncwarp();
     if (row_a >= 0) tma_load_2d(my_ring + ask_slot * HALF + lane * (HD << log2box), is_v ? &maps.v : &maps.k, 0, row_a, bar);
-    if (is_v) ahead.next(pre, p.B, p.Hkv, p.row_tiles);
+    if (is_v) {
+      if (GROUPED) ++ahead.tile; else ahead.next(pre, p.B, p.Hkv, p.row_tiles);
+    }
     ++asked;
     if (++ask_slot == SL) ask_slot = 0;
   };
@@ -228,9 +251,11 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
     if (asked < n_half) ask();
   };
 
-  ask();                                 // the first tile's K
-  ks_c = ks_a; vs_c = vs_a; ok_c = ok_a;
-  ask();                                 // its V
+  if (asked < n_half) {
+    ask();                               // the first tile's K
+    ks_c = ks_a; vs_c = vs_a; ok_c = ok_a;
+    ask();                               // its V
+  }
   if (SL == 3 && asked < n_half) ask();  // the second tile's K, whose scales wait in ks_a, vs_a
 
   int limit[NT];
@@ -335,12 +360,13 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
         mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 1));
         mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 2));
         const bool sees = T0 < limit[n];
-        const float ref = mx == -INFINITY ? 0.f : mx;
+        // the reference is a whole number, so that taking it off 15 is exact and factors between references are powers of two
+        const float ref = mx == -INFINITY ? 0.f : ceilf(mx), shift = 15.f - ref;
         float sum = 0.f;
 #pragma unroll
         for (int nt = 0; nt < 2 * KK; ++nt) {
-          x[nt][0] = ex2(x[nt][0] - ref);
-          x[nt][1] = ex2(x[nt][1] - ref);
+          x[nt][0] = ex2(x[nt][0] + shift);
+          x[nt][1] = ex2(x[nt][1] + shift);
           sum += x[nt][0] + x[nt][1];
           const __half2 h = __floats2half2_rn(x[nt][0], x[nt][1]);
           const float2 back = __half22float2(h);
@@ -349,10 +375,10 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
         }
         sum += __shfl_xor_sync(~0u, sum, 1);
         sum += __shfl_xor_sync(~0u, sum, 2);
-        const float mn = fmaxf(m_run[n], mx);
+        const float mn = fmaxf(m_run[n], mx == -INFINITY ? mx : ref);
         const float to = mn == -INFINITY ? 0.f : mn;
         const float alpha = ex2(m_run[n] - to);
-        const float join = sees ? ex2(ref - to) : 0.f;     // NaN scores pass through: they are in `sum` and in the product
+        const float join = sees ? ex2(ref - to - 15.f) : 0.f;        // NaN scores pass through: they are in `sum` and in the product
         const float beta = sees ? join * v_s : 0.f;
         l_run[n] = sees ? l_run[n] * alpha + sum * join : l_run[n];
         m_run[n] = mn;
@@ -469,6 +495,10 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
       release();
     }
 
+    if constexpr (GROUPED) {
+      ++c.tile;
+      continue;
+    }
     // ---- the item's end, or the stretch's ----
     const bool item_ends = c.tile + 1 == c.tiles;
     if (item_ends || at + 1 == end) {
@@ -510,65 +540,203 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
       mbar_wait(my_bars + slot * 8, parity, &nobody, nullptr, 1);
       if (++slot == SL) { slot = 0; parity ^= 1; }
     }
+  if constexpr (GROUPED) {
+    // ---- the warps of the CTA, then the CTAs of the item, join in order ----
+    // a warp's part goes over its ring, which nothing writes any more: o [ROWS][HD]
+    float* mine = reinterpret_cast<float*>(ring + warp * SL * HALF);
+    if (begin < end) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int k = 0; k < NM; k += 4)
+              *reinterpret_cast<float4*>(mine + (8 * n + 2 * t + e) * HD + D * g + h * NM + k) =
+                  make_float4(o[n][k][2 * h + e], o[n][k + 1][2 * h + e], o[n][k + 2][2 * h + e], o[n][k + 3][2 * h + e]);
+    }
+    if (t == 0)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) s_ml[warp][8 * n + g] = begin < end ? make_float2(m_run[n], l_run[n]) : make_float2(-INFINITY, 0.f);
+    __syncthreads();
+    constexpr int PER = (ROWS * HD / 2 + AW * 32 - 1) / (AW * 32);        // pairs of outputs a thread
+    float2 sum[PER];
+    float mx[PER], l[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int at = tid + i * AW * 32, r = at / (HD / 2), d = at - r * (HD / 2);
+      if (at >= ROWS * HD / 2) break;
+      mx[i] = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < AW; ++w) mx[i] = fmaxf(mx[i], s_ml[w][r].x);
+      const float ref = mx[i] == -INFINITY ? 0.f : mx[i];
+      sum[i] = make_float2(0.f, 0.f);
+      l[i] = 0.f;
+#pragma unroll
+      for (int w = 0; w < AW; ++w) {
+        const float2 ml = s_ml[w][r];
+        if (ml.y == 0.f) continue;       // nothing seen, nothing written
+        const float f = ex2(ml.x - ref);
+        const float2 x = *reinterpret_cast<const float2*>(ring + w * SL * HALF + (r * HD + 2 * d) * 4);
+        sum[i].x += x.x * f;
+        sum[i].y += x.y * f;
+        l[i] += ml.y * f;
+      }
+    }
+    if (p.group > 1) {
+      // every CTA leaves its part in its own memory; the CTAs share the outputs, each reading all parts
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int at = tid + i * AW * 32;
+        if (at < ROWS * HD / 2) *reinterpret_cast<float4*>(ring + at * 16) = make_float4(sum[i].x, sum[i].y, mx[i], l[i]);
+      }
+      cg::cluster_group cl = cg::this_cluster();
+      cl.sync();
+      const int rank = (int)cl.block_rank();
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int at = tid + i * AW * 32;
+        if (at >= ROWS * HD / 2) break;
+        if (at % p.group != rank) { l[i] = -1.f; continue; }              // another CTA's output
+        float4 x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (k < p.group) x[k] = *reinterpret_cast<const float4*>(cl.map_shared_rank(ring, k) + at * 16);
+        float m = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) if (k < p.group) m = fmaxf(m, x[k].z);
+        const float ref = m == -INFINITY ? 0.f : m;
+        sum[i] = make_float2(0.f, 0.f);
+        l[i] = 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (k < p.group) {
+            const float f = ex2(x[k].z - ref);
+            sum[i].x += x[k].x * f;
+            sum[i].y += x[k].y * f;
+            l[i] += x[k].w * f;
+          }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int at = tid + i * AW * 32, r = at / (HD / 2), d = at - r * (HD / 2);
+      if (at >= ROWS * HD / 2) break;
+      const int row_i = c.rt * ROWS + r, token = row_i / p.G;
+      if (row_i >= n_rows || l[i] < 0.f) continue;
+      const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
+      const int64_t row = ((int64_t)c.b * p.T + token) * p.Hq + c.kvh * p.G + (row_i - token * p.G);
+      reinterpret_cast<uint32_t*>(p.out)[(row * HD) / 2 + d] = two_outputs(sum[i].x * inv, sum[i].y * inv, p.bf16);
+    }
+    if (p.group > 1) cg::this_cluster().sync();            // nobody leaves while another reads
+  }
 }
 
-// One CTA per output row of an item that was split: its warps take every fourth part, in order, and join in order.
-template <int HD>
+// One CTA per output row of an item that was split: its warps take every fourth part, in order, and join in order.  Where the
+// parts lie follows from the lengths alone, so that is worked out while the first kernel still runs.
+template <int HD, int TILE>
 __global__ void __launch_bounds__(128) kv8_merge_kernel(const Kv8AttnParams p, int warps) {
-  constexpr int V = HD / 32;
+  constexpr int V = HD / 32, AHEAD = 4;
   __shared__ float sm_o[4][HD];
-  __shared__ float sm_l[4];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __shared__ float2 sm_ml[4];
+  __shared__ int sm_n[4][2];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int h = blockIdx.x, token = blockIdx.y, b = blockIdx.z;
   const int kvh = h / p.G, i = token * p.G + h - kvh * p.G;
-  const int nt_rows = p.row_tiles > 1 || p.rows > 8 ? 16 : 8, rt = i / nt_rows, r = i - rt * nt_rows;
+  const int nt_rows = p.rows > 8 ? 16 : 8, rt = i / nt_rows, r = i - rt * nt_rows;
   const int items = p.Hkv * p.row_tiles;
-  pdl_wait();
-  const int per_warp = stretch_of(p.plan[p.B] * items, warps);
-  const int first = p.plan[b], tiles = p.plan[b + 1] - first;
-  const int begin = first * items + (kvh * p.row_tiles + rt) * tiles;
+  int before = 0, all = 0;
+  for (int k = tid; k < p.B; k += 128) {
+    const int v = tiles_of<TILE>(p.ctx_len[k], p.max_ctx);
+    all += v;
+    if (k < b) before += v;
+  }
+  all = __reduce_add_sync(~0u, all);
+  before = __reduce_add_sync(~0u, before);
+  if (lane == 0) { sm_n[warp][0] = all; sm_n[warp][1] = before; }
+  __syncthreads();
+  all = sm_n[0][0] + sm_n[1][0] + sm_n[2][0] + sm_n[3][0];
+  before = sm_n[0][1] + sm_n[1][1] + sm_n[2][1] + sm_n[3][1];
+  const int per_warp = stretch_of(all * items, warps);
+  const int tiles = tiles_of<TILE>(p.ctx_len[b], p.max_ctx);
+  const int begin = before * items + (kvh * p.row_tiles + rt) * tiles;
   const int w0 = begin / per_warp, w1 = (begin + tiles - 1) / per_warp;
   if (w0 == w1) return;                  // finished by its warp
-  auto part_of = [&](int w) { return (2 * (int64_t)w + (w == w0)) * p.rows + r; };
   const int n = w1 - w0 + 1;
-  float mm = -INFINITY;
-  for (int k = lane; k < n; k += 32) mm = fmaxf(mm, __ldcg(p.part_ml + part_of(w0 + k) * 2));
-#pragma unroll
-  for (int d = 16; d; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(~0u, mm, d));
-  const float ref = mm == -INFINITY ? 0.f : mm;
-  float acc[V], ll = 0.f;
+  pdl_wait();
+  float acc[V], mm = -INFINITY, ll = 0.f;
 #pragma unroll
   for (int c = 0; c < V; ++c) acc[c] = 0.f;
-#pragma unroll 8
-  for (int k = warp; k < n; k += 4) {
-    const int64_t part = part_of(w0 + k);
-    const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.part_ml + part * 2));
-    const float f = ex2(ml.x - ref);
-    ll += ml.y * f;
+  for (int k0 = warp; k0 < n; k0 += 4 * AHEAD) {           // several parts' loads under way at a time
+    float2 ml[AHEAD];
+    float x[AHEAD][V];
 #pragma unroll
-    for (int c = 0; c < V; ++c) acc[c] += __ldcg(p.part_o + part * HD + c * 32 + lane) * f;
+    for (int j = 0; j < AHEAD; ++j) {
+      const int k = min(k0 + 4 * j, n - 1);
+      const int64_t part = (2 * (int64_t)(w0 + k) + (k == 0)) * p.rows + r;
+      ml[j] = __ldcg(reinterpret_cast<const float2*>(p.part_ml + part * 2));
+#pragma unroll
+      for (int c = 0; c < V; ++c) x[j][c] = __ldcg(p.part_o + part * HD + c * 32 + lane);
+    }
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      if (k0 + 4 * j >= n) break;
+      const float mn = fmaxf(mm, ml[j].x), ref = mn == -INFINITY ? 0.f : mn;
+      const float a = ex2(mm - ref), f = ex2(ml[j].x - ref);
+      ll = ll * a + ml[j].y * f;
+#pragma unroll
+      for (int c = 0; c < V; ++c) acc[c] = acc[c] * a + x[j][c] * f;
+      mm = mn;
+    }
   }
 #pragma unroll
   for (int c = 0; c < V; ++c) sm_o[warp][c * 32 + lane] = acc[c];
-  if (lane == 0) sm_l[warp] = ll;
+  if (lane == 0) sm_ml[warp] = make_float2(mm, ll);
   __syncthreads();
-  const float l = sm_l[0] + sm_l[1] + sm_l[2] + sm_l[3], inv = l == 0.f ? 0.f : 1.f / l;
-  const int64_t row = ((int64_t)b * p.T + token) * p.Hq + h;
-  if (threadIdx.x < HD / 2) {
-    const int c = 2 * threadIdx.x;
-    const float x = sm_o[0][c] + sm_o[1][c] + sm_o[2][c] + sm_o[3][c], y = sm_o[0][c + 1] + sm_o[1][c + 1] + sm_o[2][c + 1] + sm_o[3][c + 1];
-    reinterpret_cast<uint32_t*>(p.out)[(row * HD + c) / 2] = two_outputs(x * inv, y * inv, p.bf16);
+  if (tid < HD / 2) {
+    float m = fmaxf(fmaxf(sm_ml[0].x, sm_ml[1].x), fmaxf(sm_ml[2].x, sm_ml[3].x));
+    m = m == -INFINITY ? 0.f : m;
+    float l = 0.f, x = 0.f, y = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = ex2(sm_ml[w].x - m);
+      l += sm_ml[w].y * f;
+      x += sm_o[w][2 * tid] * f;
+      y += sm_o[w][2 * tid + 1] * f;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int64_t row = ((int64_t)b * p.T + token) * p.Hq + h;
+    reinterpret_cast<uint32_t*>(p.out)[(row * HD) / 2 + tid] = two_outputs(x * inv, y * inv, p.bf16);
   }
 }
 
-struct Shape { int nt, row_tiles, rows; };
+// How a call is cut: query rows of a KV head, and tiles handed out as stretches or to groups.
+struct Shape { int nt, row_tiles, rows, group, tile; };
 
-Shape row_shape(int T, int G) {
+constexpr int MIN_TILE = 32, MAX_TILE = 64;
+constexpr int MAX_GROUP = 8;
+constexpr int GROUP_BYTES = 512 << 10;
+
+Shape shape_of(int B, int T, int Hq, int Hkv, int hd, int max_ctx) {
   Shape s;
-  const int rows = T * G;
+  const int rows = T * (Hq / Hkv);
   s.nt = rows > 8 ? 2 : 1;
   s.row_tiles = (rows + 8 * s.nt - 1) / (8 * s.nt);
   s.rows = rows < 8 * s.nt ? rows : 8 * s.nt;
+  // Groups: all items at once, one wave of clusters as large as the SMs allow (no larger than the tiles can use), and not
+  // more than half a megabyte for a CTA to read, so that an uneven batch, whose longest sequence then sets the time,
+  // loses less than the second kernel costs.
+  const long long items = (long long)B * Hkv * s.row_tiles;
+  const int warps = s.nt == 1 ? WARPS<128, 1> : WARPS<128, 2>;
+  int group = 1;
+  while (group < MAX_GROUP && items * group * 2 <= sm_count() && (long long)group * warps * MIN_TILE < max_ctx) group *= 2;
+  const bool grouped = items <= sm_count() && 2LL * max_ctx * hd <= (long long)GROUP_BYTES * group;
+  s.group = grouped ? group : 0;
+  // Stretches: smaller tiles where a warp would get few of them, and the odd one too many would show.
+  const long long tiles = items * ((max_ctx + MAX_TILE - 1) / MAX_TILE);
+  s.tile = grouped || (s.nt == 1 && tiles < 4LL * warps * sm_count()) ? MIN_TILE : MAX_TILE;
   return s;
 }
 
@@ -576,31 +744,49 @@ int warps_of(const Shape& s) { return (s.nt == 1 ? WARPS<128, 1> : WARPS<128, 2>
 
 size_t parts_of(const Shape& s) { return (size_t)2 * warps_of(s) * s.rows; }
 
-size_t scratch_of(const Shape& s, int B, int hd, int max_ctx) {
-  if (max_ctx <= TILE) return 0;         // no item has a second tile
-  return (parts_of(s) * (hd + 2) + (size_t)B + 1) * sizeof(float);
+size_t scratch_of(const Shape& s, int hd, int max_ctx) {
+  if (s.group > 0 || max_ctx <= s.tile) return 0;          // joined in the first kernel, or no item has a second tile
+  return parts_of(s) * (hd + 2) * sizeof(float);
 }
 
-template <int HD, int CODE, int NT, int SUB>
+template <int HD, int CODE, int NT, int TILE, int SUB, bool GROUPED>
 es_status_t launch_sub(const Kv8Maps& maps, const Kv8AttnParams& p, cudaStream_t s) {
   constexpr int AW = WARPS<HD, NT>;
-  constexpr int RINGS = AW * SLOTS<HD, NT> * TILE * HD + 1024;       // and room to align them
-  const size_t smem = RINGS + (size_t)(p.B + 1) * sizeof(int);
-  auto kern = kv8_attn_kernel<HD, CODE, NT, SUB>;
+  constexpr int RINGS = AW * SLOTS<HD, NT, TILE> * TILE * HD + 1024; // and room to align them
+  auto kern = kv8_attn_kernel<HD, CODE, NT, TILE, SUB, GROUPED>;
   ES_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, RINGS + (KV8_MAX_B + 1) * (int)sizeof(int)));
-  ES_CUDA_CHECK(launch_kernel(kern, dim3(sm_count()), dim3(AW * 32), smem, s, false, maps, p));
-  if (p.plan)
-    ES_CUDA_CHECK(launch_kernel(kv8_merge_kernel<HD>, dim3(p.Hq, p.T, p.B), dim3(128), 0, s, true, p, AW * sm_count()));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(GROUPED ? p.B * p.Hkv * p.row_tiles * p.group : sm_count());
+  cfg.blockDim = dim3(AW * 32);
+  cfg.dynamicSmemBytes = RINGS + (GROUPED ? 0 : (size_t)(p.B + 1) * sizeof(int));
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = p.group;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = GROUPED && p.group > 1 ? 1 : 0;
+  ES_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kern, maps, p));
+  if (!GROUPED && p.max_ctx > TILE)
+    ES_CUDA_CHECK(launch_kernel(kv8_merge_kernel<HD, TILE>, dim3(p.Hq, p.T, p.B), dim3(128), 0, s, true, p, AW * sm_count()));
   return ES_OK;
 }
 
-template <int HD, int CODE>
-es_status_t launch(const Kv8Maps& maps, const Kv8AttnParams& p, int nt, cudaStream_t s) {
-  if (nt == 1) {
-    if (p.P >= 64) return launch_sub<HD, CODE, 1, 64>(maps, p, s);
-    return p.P == 32 ? launch_sub<HD, CODE, 1, 32>(maps, p, s) : launch_sub<HD, CODE, 1, 16>(maps, p, s);
+// Sub-tiles of the softmax: as much of a tile as lies in one page (two row blocks: 32 tokens at most, for registers).
+template <int HD, int CODE, int NT>
+es_status_t launch_tile(const Kv8Maps& maps, const Kv8AttnParams& p, const Shape& sh, cudaStream_t s) {
+  const bool small = p.P == 16;
+  if (sh.group > 0) return small ? launch_sub<HD, CODE, NT, 32, 16, true>(maps, p, s) : launch_sub<HD, CODE, NT, 32, 32, true>(maps, p, s);
+  if constexpr (NT == 1) {
+    if (sh.tile == 32) return small ? launch_sub<HD, CODE, 1, 32, 16, false>(maps, p, s) : launch_sub<HD, CODE, 1, 32, 32, false>(maps, p, s);
+    if (p.P >= 64) return launch_sub<HD, CODE, 1, 64, 64, false>(maps, p, s);
   }
-  return p.P >= 32 ? launch_sub<HD, CODE, 2, 32>(maps, p, s) : launch_sub<HD, CODE, 2, 16>(maps, p, s);
+  return small ? launch_sub<HD, CODE, NT, 64, 16, false>(maps, p, s) : launch_sub<HD, CODE, NT, 64, 32, false>(maps, p, s);
+}
+
+template <int HD, int CODE>
+es_status_t launch(const Kv8Maps& maps, const Kv8AttnParams& p, const Shape& sh, cudaStream_t s) {
+  return sh.nt == 1 ? launch_tile<HD, CODE, 1>(maps, p, sh, s) : launch_tile<HD, CODE, 2>(maps, p, sh, s);
 }
 
 es_status_t check_heads(int B, int T, int Hq, int Hkv, int hd, int page_tokens, int max_ctx) {
@@ -610,8 +796,8 @@ es_status_t check_heads(int B, int T, int Hq, int Hkv, int hd, int page_tokens, 
   if (max_ctx > (1 << 30)) return fail(ES_ERR_RANGE, "max_ctx exceeds 2^30");
   if (B > KV8_MAX_B) return fail(ES_ERR_RANGE, "B = %d exceeds %d sequences", B, KV8_MAX_B);
   if (T > 65535 || (long long)T * (Hq / Hkv) > 65535) return fail(ES_ERR_RANGE, "T * (Hq / Hkv) exceeds one launch");
-  const Shape s = row_shape(T, Hq / Hkv);
-  if ((long long)B * Hkv * s.row_tiles * ((max_ctx + TILE - 1) / TILE) > (1LL << 30))
+  const Shape s = shape_of(B, T, Hq, Hkv, hd, max_ctx);
+  if ((long long)B * Hkv * s.row_tiles * ((max_ctx + MIN_TILE - 1) / MIN_TILE) > (1LL << 30))
     return fail(ES_ERR_RANGE, "B * heads * max_ctx exceeds one launch");
   return ES_OK;
 }
@@ -625,7 +811,7 @@ size_t es_op_decode_attention_kv8_scratch_bytes(int32_t B, int32_t T, int32_t Hq
                                                 int32_t page_tokens, int32_t max_ctx) {
   using namespace es;
   if (check_heads(B, T, Hq, Hkv, hd, page_tokens, max_ctx) != ES_OK) return 0;
-  return scratch_of(row_shape(T, Hq / Hkv), B, hd, max_ctx);
+  return scratch_of(shape_of(B, T, Hq, Hkv, hd, max_ctx), hd, max_ctx);
 }
 
 es_status_t es_op_decode_attention_kv8(const void* q, int32_t dtype, int64_t q_stride, const void* k_pages,
@@ -645,8 +831,8 @@ es_status_t es_op_decode_attention_kv8(const void* q, int32_t dtype, int64_t q_s
   if (q_stride < (int64_t)Hq * hd || q_stride % 8) return fail(ES_ERR_INVALID_ARG, "q_stride must be a multiple of 8, at least Hq * hd");
   if (((uintptr_t)q | (uintptr_t)k_pages | (uintptr_t)v_pages | (uintptr_t)scratch) % 16 || (uintptr_t)out % 4)
     return fail(ES_ERR_INVALID_ARG, "q, pages and scratch must be 16-byte aligned");
-  const Shape sh = row_shape(T, Hq / Hkv);
-  const size_t need = scratch_of(sh, B, hd, max_ctx);
+  const Shape sh = shape_of(B, T, Hq, Hkv, hd, max_ctx);
+  const size_t need = scratch_of(sh, hd, max_ctx);
   if (scratch_bytes < need || (need && !scratch)) return fail(ES_ERR_WORKSPACE, "scratch: %zu bytes given, %zu needed", scratch ? scratch_bytes : (size_t)0, need);
   int log2P = 0;
   while ((1 << log2P) < page_tokens) ++log2P;
@@ -654,18 +840,17 @@ es_status_t es_op_decode_attention_kv8(const void* q, int32_t dtype, int64_t q_s
   // helper's matrix of 64 fp16 columns moves bytes as they are
   Kv8Maps maps;
   const int64_t lines = (int64_t)n_pages * Hkv * page_tokens * hd / 128;
-  const int box_lines = (page_tokens < TILE ? page_tokens : TILE) * hd / 128;
+  const int box_lines = (page_tokens < sh.tile ? page_tokens : sh.tile) * hd / 128;
   if (lines > INT32_MAX) return fail(ES_ERR_RANGE, "a page pool exceeds 2^31 lines of 128 bytes");
   ES_TRY(tma_encode_2d_f16(&maps.k, k_pages, lines, 64, 64, box_lines));
   ES_TRY(tma_encode_2d_f16(&maps.v, v_pages, lines, 64, 64, box_lines));
   float* part = (float*)scratch;
   const size_t parts = parts_of(sh);
-  Kv8AttnParams p{q, q_stride, k_scale, v_scale, block_table, ctx_len, out, part, part + parts * hd,
-                  need ? (int*)(part + parts * (hd + 2)) : nullptr, B, T, Hq, Hkv, Hq / Hkv, page_tokens, log2P, pages_per_seq,
-                  n_pages, max_ctx, sh.row_tiles, sh.rows, dtype == ES_DTYPE_BF16};
+  Kv8AttnParams p{q, q_stride, k_scale, v_scale, block_table, ctx_len, out, part, part + parts * hd, B, T, Hq, Hkv, Hq / Hkv,
+                  page_tokens, log2P, pages_per_seq, n_pages, max_ctx, sh.row_tiles, sh.rows, dtype == ES_DTYPE_BF16, sh.group};
   cudaStream_t s = (cudaStream_t)stream;
-  if (hd == 128) return code == CODE_I8 ? launch<128, CODE_I8>(maps, p, sh.nt, s) : launch<128, CODE_E4M3>(maps, p, sh.nt, s);
-  return code == CODE_I8 ? launch<64, CODE_I8>(maps, p, sh.nt, s) : launch<64, CODE_E4M3>(maps, p, sh.nt, s);
+  if (hd == 128) return code == CODE_I8 ? launch<128, CODE_I8>(maps, p, sh, s) : launch<128, CODE_E4M3>(maps, p, sh, s);
+  return code == CODE_I8 ? launch<64, CODE_I8>(maps, p, sh, s) : launch<64, CODE_E4M3>(maps, p, sh, s);
 }
 
 }  // extern "C"

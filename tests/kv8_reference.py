@@ -138,7 +138,9 @@ def attend(q, kc, vc, ks, vs, table, ctx, P, max_ctx):
     A = sum |q k| / sqrt(hd), the 4 for the factors and the exponent's multiplication.  bf16 queries scaled to fp16
     lose at most 2^-24 of the row's largest an element.  exp turns an error d of a score into a factor 1 + d, it shifts
     numerator and denominator, and is itself within 2^-21: 2 (d + 2^-20) sum(p |v|) in all, with the two fp16 halves of
-    a probability (2^-22) and the sums in it.  Then the result is rounded once."""
+    a probability (2^-22) and the sums in it.  A half has no bits below 2^-24, and the probabilities of up to 64 tokens
+    (a stretch of positions 64 i .. 64 i + 63 at most) are scaled so that the largest lies in (2^14, 2^15]: what is lost
+    of each is below 2^-25 / 2^14 = 2^-39 of the largest.  Then the result is rounded once."""
     B, T, Hq, hd = q.shape
     Hkv, n_pages = kc.shape[1], kc.shape[0]
     G = Hq // Hkv
@@ -165,6 +167,10 @@ def attend(q, kc, vc, ks, vs, table, ctx, P, max_ctx):
                 if q.dtype == torch.bfloat16:
                     d = d + 2.0 ** -24 * qq.abs().amax(-1) * float(k.abs().sum(-1).max()) / math.sqrt(hd)
                 bound[b, t, h * G:(h + 1) * G] = 2 * (d[:, None] + 2.0 ** -20) * (p @ v.abs())
+                group = torch.tensor([i // 64 for i in pos[:m]])
+                for i in group.unique().tolist():
+                    at = group == i
+                    bound[b, t, h * G:(h + 1) * G] += 2.0 ** -39 * p[:, at].amax(-1, keepdim=True) * v[at].abs().sum(0)
     eps = torch.finfo(q.dtype).eps / 2
     return want, bound * (1 + eps) + eps * want.abs() + TINY[q.dtype]
 

@@ -296,7 +296,10 @@ def _check_attn(B, case, got=None, P=None):
         got = B.es_op_decode_attention_kv8(*[t.cuda() for t in (q, kc, vc, ks, vs, table, ctx)], max_ctx)
     want, bound = R.attend(q, kc, vc, ks, vs, table, ctx, P, max_ctx)
     got = got.cpu().double().reshape(want.shape)
-    assert bool(((got - want).abs() <= bound).all()), float(((got - want).abs() / bound).max())
+    over = (got - want).abs() / bound
+    worst = float(over.max())
+    where = [int(i) for i in torch.unravel_index(over.argmax(), over.shape)]
+    assert worst <= 1.0, f"{worst} of what is allowed at [b, t, head, dim] {where}, {int((over > 1).sum())} places"
     return got
 
 
@@ -309,6 +312,20 @@ def _check_attn(B, case, got=None, P=None):
 ])
 def test_attention(B, Bn, T, Hq, Hkv, hd, P, ctxs, code, dtype):
     _check_attn(B, _attn_case(Bn, T, Hq, Hkv, hd, P, ctxs, code, dtype, 31))
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("P,hd,Hq,T", [(16, 64, 8, 1), (32, 128, 16, 1), (64, 128, 8, 3), (128, 64, 24, 2), (16, 128, 24, 4), (64, 128, 40, 3)])
+@pytest.mark.parametrize("longest", [400, 3000])
+def test_attention_many_items_share_the_machine(B, P, hd, Hq, T, longest, code):
+    """More (sequence, head) items than SMs: stretches of tiles that begin and end inside items, tiles of both sizes, one and
+    two row blocks, several row tiles, sequences without keys among them."""
+    rng = random.Random(P * T + Hq)
+    ctxs = [rng.choice([0, 1, 15, 31, 32, 33, 63, 64, 65, 130, 200]) for _ in range(20)]
+    ctxs[7], ctxs[13] = longest, longest // 2
+    case = _attn_case(20, T, Hq, 8, hd, P, ctxs, code, "bf16" if T == 3 else "fp16", 71)
+    assert B.es_op_decode_attention_kv8_scratch_bytes(20, T, Hq, 8, hd, P, longest) > 0
+    _check_attn(B, case)
 
 
 @pytest.mark.parametrize("code", ["int8", "e4m3"])
@@ -387,7 +404,7 @@ def test_attention_shows_a_page_without_a_number_to_the_rows_that_see_it(B):
 def test_attention_long_context_many_splits_and_sliced_queries(B):
     """One sequence cut into many splits, q a slice of a fused projection's rows, both result layouts, the same bits from a
     caller's scratch full of garbage and from run to run."""
-    case = _attn_case(1, 1, 8, 2, 128, 64, [9001], "int8", "fp16", 53)
+    case = _attn_case(1, 1, 8, 2, 128, 64, [20001], "int8", "fp16", 53)
     q, kc, vc, ks, vs, table, ctx, max_ctx = case
     dev = [t.cuda() for t in (kc, vc, ks, vs, table, ctx)]
     fused = torch.full((1, 12, 128), math.nan, dtype=torch.float16, device="cuda")
