@@ -47,6 +47,7 @@ namespace {
 // another's better than 8 warps' do; two half tiles each are then what 192 KB hold.
 template <int HD, int NT> constexpr int WARPS = NT == 1 ? 12 : 8;
 template <int HD, int NT, int TILE> constexpr int SLOTS = HD == 128 && NT == 1 && TILE == 64 ? 2 : 3;
+constexpr int MAX_GROUP = 8;             // CTAs of an item (groups)
 constexpr int KV8_MAX_B = 4096;          // sequences whose tile sums fit beside the rings
 
 struct Kv8AttnParams {
@@ -151,17 +152,23 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
   unsigned char* ring = dyn + ((1024 - (smem_u32(dyn) & 1023)) & 1023);  // the swizzle goes by address bits 7 to 9
   __shared__ __align__(8) uint64_t bars[AW * SL];
   __shared__ int s_warp[AW];
-  __shared__ float2 s_ml[GROUPED ? AW : 1][ROWS];
+  __shared__ float2 s_ml[GROUPED ? AW : 1][ROWS];          // groups: maximum and sum of every warp, its factor, the CTAs'
+  __shared__ float s_f[GROUPED ? AW : 1][ROWS];
+  __shared__ float2 s_all[GROUPED ? MAX_GROUP : 1][ROWS];
   __shared__ int s_abort;
   int* pre = reinterpret_cast<int*>(ring + AW * SL * HALF);          // [B + 1] tiles before each sequence
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int items = p.Hkv * p.row_tiles, n_rows = p.T * p.G;
+  const uint32_t my_ring = smem_u32(ring) + warp * SL * HALF, my_bars = smem_u32(bars) + warp * SL * 8;
 
+  if (GROUPED && p.group > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");      // "this CTA runs"
+  if (lane < SL) {                       // a warp's barriers are its own
+    mbar_init(my_bars + lane * 8, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
   if (tid == 0) {
     s_abort = 0;
-    for (int i = 0; i < AW * SL; ++i) mbar_init(smem_u32(bars + i), 1);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     prefetch_tmap(&maps.k);
     prefetch_tmap(&maps.v);
   }
@@ -207,7 +214,6 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
     c.seek(begin, pre, p.B, p.Hkv, p.row_tiles);
   }
 
-  const uint32_t my_ring = smem_u32(ring) + warp * SL * HALF, my_bars = smem_u32(bars) + warp * SL * 8;
   const int log2box = min(p.log2P, TILE == 64 ? 6 : 5), boxes = TILE >> log2box;             // tokens that lie together
   ahead = c;
   const int n_half = 2 * (end - begin);
@@ -251,59 +257,70 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
     if (asked < n_half) ask();
   };
 
+  int limit[NT];
+  float qscale[NT];
+  uint32_t qa[NT][8 * J];
+  float o[NT][NM][4], m_run[NT], l_run[NT];
+  int ctx = 0, item_begin = 0;
+  bool fresh = false, running = true;
+  // query rows of the item at hand; row r of the row tile is token r / G, head kv_head * G + r % G
+  auto load_q = [&]() {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int i = c.rt * ROWS + 8 * n + g, token = i / p.G;
+      const uint16_t* row = reinterpret_cast<const uint16_t*>(p.q) + ((int64_t)c.b * p.T + token) * p.q_stride + (int64_t)(c.kvh * p.G + i - token * p.G) * HD + t * (HD / 4);
+#pragma unroll
+      for (int j = 0; j < 2 * J; ++j) {
+        const uint4 x = i < n_rows ? *reinterpret_cast<const uint4*>(row + 8 * j) : make_uint4(0, 0, 0, 0);
+        qa[n][4 * j] = x.x; qa[n][4 * j + 1] = x.y; qa[n][4 * j + 2] = x.z; qa[n][4 * j + 3] = x.w;
+      }
+    }
+  };
+  auto start_item = [&](int at) {
+    ctx = max(0, min(p.ctx_len[c.b], p.max_ctx));
+    item_begin = at - c.tile;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int i = c.rt * ROWS + 8 * n + g;
+      limit[n] = i < n_rows ? ctx - p.T + i / p.G + 1 : ctx;         // rows that do not exist have zero queries and are not stored
+      qscale[n] = 1.f;
+      if (p.bf16) {
+        uint32_t mx = 0;
+#pragma unroll
+        for (int k = 0; k < 8 * J; ++k) mx = __vmaxu2(mx, qa[n][k] & 0x7fff7fffu);
+        mx = max(mx & 0xffffu, mx >> 16);
+        mx = max(mx, __shfl_xor_sync(~0u, mx, 1));
+        mx = max(mx, __shfl_xor_sync(~0u, mx, 2));
+        // 2^-e and 2^e with e the exponent of the largest magnitude, kept where both are normal numbers
+        const int e = min(max((int)(mx >> 7) - 127, -126), 126);
+        const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+        qscale[n] = __uint_as_float((uint32_t)(127 + e) << 23);
+#pragma unroll
+        for (int k = 0; k < 8 * J; ++k)
+          qa[n][k] = h2_bits(__floats2half2_rn(__uint_as_float(qa[n][k] << 16) * down, __uint_as_float(qa[n][k] & 0xffff0000u) * down));
+      }
+      qscale[n] *= rsqrtf((float)HD) * LOG2E;              // scores in units of log2
+      m_run[n] = -INFINITY;
+      l_run[n] = 0.f;
+#pragma unroll
+      for (int k = 0; k < NM; ++k) o[n][k][0] = o[n][k][1] = o[n][k][2] = o[n][k][3] = 0.f;
+    }
+  };
+
+  load_q();                              // before the first tiles are asked for: behind them it would wait for their bytes
   if (asked < n_half) {
     ask();                               // the first tile's K
     ks_c = ks_a; vs_c = vs_a; ok_c = ok_a;
     ask();                               // its V
   }
   if (SL == 3 && asked < n_half) ask();  // the second tile's K, whose scales wait in ks_a, vs_a
-
-  int limit[NT];
-  float qscale[NT];
-  uint32_t qa[NT][8 * J];
-  float o[NT][NM][4], m_run[NT], l_run[NT];
-  int ctx = 0, item_begin = 0;
-  bool fresh = true, running = true;
+  start_item(begin);
 
   for (int at = begin; at < end && running; ++at) {
     if (fresh) {
-      // ---- a new item: its query rows; row r of the row tile is token r / G, head kv_head * G + r % G ----
       fresh = false;
-      ctx = max(0, min(p.ctx_len[c.b], p.max_ctx));
-      item_begin = at - c.tile;
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const int i = c.rt * ROWS + 8 * n + g, token = i / p.G;
-        const bool real = i < n_rows;
-        limit[n] = real ? ctx - p.T + token + 1 : ctx;     // rows that do not exist have zero queries and are not stored
-        qscale[n] = 1.f;
-        const uint16_t* row = reinterpret_cast<const uint16_t*>(p.q) + ((int64_t)c.b * p.T + token) * p.q_stride + (int64_t)(c.kvh * p.G + i - token * p.G) * HD + t * (HD / 4);
-#pragma unroll
-        for (int j = 0; j < 2 * J; ++j) {
-          const uint4 x = real ? *reinterpret_cast<const uint4*>(row + 8 * j) : make_uint4(0, 0, 0, 0);
-          qa[n][4 * j] = x.x; qa[n][4 * j + 1] = x.y; qa[n][4 * j + 2] = x.z; qa[n][4 * j + 3] = x.w;
-        }
-        if (p.bf16) {
-          uint32_t mx = 0;
-#pragma unroll
-          for (int i2 = 0; i2 < 8 * J; ++i2) mx = __vmaxu2(mx, qa[n][i2] & 0x7fff7fffu);
-          mx = max(mx & 0xffffu, mx >> 16);
-          mx = max(mx, __shfl_xor_sync(~0u, mx, 1));
-          mx = max(mx, __shfl_xor_sync(~0u, mx, 2));
-          // 2^-e and 2^e with e the exponent of the largest magnitude, kept where both are normal numbers
-          const int e = min(max((int)(mx >> 7) - 127, -126), 126);
-          const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-          qscale[n] = __uint_as_float((uint32_t)(127 + e) << 23);
-#pragma unroll
-          for (int i2 = 0; i2 < 8 * J; ++i2)
-            qa[n][i2] = h2_bits(__floats2half2_rn(__uint_as_float(qa[n][i2] << 16) * down, __uint_as_float(qa[n][i2] & 0xffff0000u) * down));
-        }
-        qscale[n] *= rsqrtf((float)HD) * LOG2E;            // scores in units of log2
-        m_run[n] = -INFINITY;
-        l_run[n] = 0.f;
-#pragma unroll
-        for (int i2 = 0; i2 < NM; ++i2) o[n][i2][0] = o[n][i2][1] = o[n][i2][2] = o[n][i2][3] = 0.f;
-      }
+      load_q();
+      start_item(at);
     }
     // ---- scores: rows g (and 8 + g), tokens 8 nt + 2 t + {0, 1} of the tile ----
     if (!arrived()) { running = false; break; }
@@ -542,82 +559,79 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
     }
   if constexpr (GROUPED) {
     // ---- the warps of the CTA, then the CTAs of the item, join in order ----
-    // a warp's part goes over its ring, which nothing writes any more: o [ROWS][HD]
+    // a warp's part goes over its ring, which nothing writes any more: o [ROWS][HD] (zero where it had no tile)
     float* mine = reinterpret_cast<float*>(ring + warp * SL * HALF);
-    if (begin < end) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+      for (int e = 0; e < 2; ++e)
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int k = 0; k < NM; k += 4)
-              *reinterpret_cast<float4*>(mine + (8 * n + 2 * t + e) * HD + D * g + h * NM + k) =
-                  make_float4(o[n][k][2 * h + e], o[n][k + 1][2 * h + e], o[n][k + 2][2 * h + e], o[n][k + 3][2 * h + e]);
+          for (int k = 0; k < NM; k += 4)
+            *reinterpret_cast<float4*>(mine + (8 * n + 2 * t + e) * HD + D * g + h * NM + k) =
+                make_float4(o[n][k][2 * h + e], o[n][k + 1][2 * h + e], o[n][k + 2][2 * h + e], o[n][k + 3][2 * h + e]);
+      if (t == 0) s_ml[warp][8 * n + g] = make_float2(m_run[n], l_run[n]);
     }
-    if (t == 0)
+    __syncthreads();
+    if (tid < AW * ROWS) {               // the factor of every warp's part of a row
+      const int w = tid / ROWS, r = tid - w * ROWS;
+      float2 ml[AW];
+      float m = -INFINITY;
 #pragma unroll
-      for (int n = 0; n < NT; ++n) s_ml[warp][8 * n + g] = begin < end ? make_float2(m_run[n], l_run[n]) : make_float2(-INFINITY, 0.f);
+      for (int k = 0; k < AW; ++k) { ml[k] = s_ml[k][r]; m = fmaxf(m, ml[k].x); }
+      const float ref = m == -INFINITY ? 0.f : m;
+      s_f[w][r] = ex2(s_ml[w][r].x - ref);
+      if (w == 0) {
+        float l = 0.f;
+#pragma unroll
+        for (int k = 0; k < AW; ++k) l += ml[k].y * ex2(ml[k].x - ref);
+        s_all[0][r] = make_float2(m, l);
+      }
+    }
     __syncthreads();
     constexpr int PER = (ROWS * HD / 2 + AW * 32 - 1) / (AW * 32);        // pairs of outputs a thread
     float2 sum[PER];
-    float mx[PER], l[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int at = tid + i * AW * 32, r = at / (HD / 2), d = at - r * (HD / 2);
-      if (at >= ROWS * HD / 2) break;
-      mx[i] = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < AW; ++w) mx[i] = fmaxf(mx[i], s_ml[w][r].x);
-      const float ref = mx[i] == -INFINITY ? 0.f : mx[i];
+      const int at = min(tid + i * AW * 32, ROWS * HD / 2 - 1), r = at / (HD / 2);
       sum[i] = make_float2(0.f, 0.f);
-      l[i] = 0.f;
 #pragma unroll
       for (int w = 0; w < AW; ++w) {
-        const float2 ml = s_ml[w][r];
-        if (ml.y == 0.f) continue;       // nothing seen, nothing written
-        const float f = ex2(ml.x - ref);
-        const float2 x = *reinterpret_cast<const float2*>(ring + w * SL * HALF + (r * HD + 2 * d) * 4);
-        sum[i].x += x.x * f;
-        sum[i].y += x.y * f;
-        l[i] += ml.y * f;
+        const float2 x = *reinterpret_cast<const float2*>(ring + w * SL * HALF + at * 8);
+        sum[i].x += x.x * s_f[w][r];
+        sum[i].y += x.y * s_f[w][r];
       }
     }
     if (p.group > 1) {
-      // every CTA leaves its part in its own memory; the CTAs share the outputs, each reading all parts
-      __syncthreads();
+      // the CTAs leave their parts with the first one, behind its rings; before that, all of them run
+      asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+      const int rank = (int)cluster_ctarank();
+      float2* inbox = reinterpret_cast<float2*>(ring + AW * SL * HALF);
+      if (rank > 0) {
+        cg::cluster_group cl = cg::this_cluster();
+        float2* to = cl.map_shared_rank(inbox, 0) + (rank - 1) * (ROWS * HD / 2);
 #pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const int at = tid + i * AW * 32;
-        if (at < ROWS * HD / 2) *reinterpret_cast<float4*>(ring + at * 16) = make_float4(sum[i].x, sum[i].y, mx[i], l[i]);
+        for (int i = 0; i < PER; ++i)
+          if (tid + i * AW * 32 < ROWS * HD / 2) to[tid + i * AW * 32] = sum[i];
+        if (tid < ROWS) cl.map_shared_rank(&s_all[0][0], 0)[rank * ROWS + tid] = s_all[0][tid];
       }
-      cg::cluster_group cl = cg::this_cluster();
-      cl.sync();
-      const int rank = (int)cl.block_rank();
+      cluster_sync_all();
+      if (rank > 0) return;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        const int at = tid + i * AW * 32;
-        if (at >= ROWS * HD / 2) break;
-        if (at % p.group != rank) { l[i] = -1.f; continue; }              // another CTA's output
-        float4 x[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (k < p.group) x[k] = *reinterpret_cast<const float4*>(cl.map_shared_rank(ring, k) + at * 16);
-        float m = -INFINITY;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) if (k < p.group) m = fmaxf(m, x[k].z);
-        const float ref = m == -INFINITY ? 0.f : m;
-        sum[i] = make_float2(0.f, 0.f);
-        l[i] = 0.f;
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (k < p.group) {
-            const float f = ex2(x[k].z - ref);
-            sum[i].x += x[k].x * f;
-            sum[i].y += x[k].y * f;
-            l[i] += x[k].w * f;
-          }
+        const int at = min(tid + i * AW * 32, ROWS * HD / 2 - 1), r = at / (HD / 2);
+        float m = s_all[0][r].x;
+        for (int k = 1; k < p.group; ++k) m = fmaxf(m, s_all[k][r].x);
+        const float ref = m == -INFINITY ? 0.f : m, f0 = ex2(s_all[0][r].x - ref);
+        sum[i].x *= f0;
+        sum[i].y *= f0;
+        for (int k = 1; k < p.group; ++k) {
+          const float f = ex2(s_all[k][r].x - ref);
+          const float2 x = inbox[(k - 1) * (ROWS * HD / 2) + at];
+          sum[i].x += x.x * f;
+          sum[i].y += x.y * f;
+        }
       }
     }
 #pragma unroll
@@ -625,12 +639,15 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
       const int at = tid + i * AW * 32, r = at / (HD / 2), d = at - r * (HD / 2);
       if (at >= ROWS * HD / 2) break;
       const int row_i = c.rt * ROWS + r, token = row_i / p.G;
-      if (row_i >= n_rows || l[i] < 0.f) continue;
-      const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
+      if (row_i >= n_rows) continue;
+      float m = s_all[0][r].x, l = 0.f;
+      for (int k = 1; k < p.group; ++k) m = fmaxf(m, s_all[k][r].x);
+      const float ref = m == -INFINITY ? 0.f : m;
+      for (int k = 0; k < p.group; ++k) l += s_all[k][r].y * ex2(s_all[k][r].x - ref);
+      const float inv = l == 0.f ? 0.f : 1.f / l;
       const int64_t row = ((int64_t)c.b * p.T + token) * p.Hq + c.kvh * p.G + (row_i - token * p.G);
       reinterpret_cast<uint32_t*>(p.out)[(row * HD) / 2 + d] = two_outputs(sum[i].x * inv, sum[i].y * inv, p.bf16);
     }
-    if (p.group > 1) cg::this_cluster().sync();            // nobody leaves while another reads
   }
 }
 
@@ -716,7 +733,6 @@ __global__ void __launch_bounds__(128) kv8_merge_kernel(const Kv8AttnParams p, i
 struct Shape { int nt, row_tiles, rows, group, tile; };
 
 constexpr int MIN_TILE = 32, MAX_TILE = 64;
-constexpr int MAX_GROUP = 8;
 constexpr int GROUP_BYTES = 512 << 10;
 
 Shape shape_of(int B, int T, int Hq, int Hkv, int hd, int max_ctx) {
@@ -753,12 +769,14 @@ template <int HD, int CODE, int NT, int TILE, int SUB, bool GROUPED>
 es_status_t launch_sub(const Kv8Maps& maps, const Kv8AttnParams& p, cudaStream_t s) {
   constexpr int AW = WARPS<HD, NT>;
   constexpr int RINGS = AW * SLOTS<HD, NT, TILE> * TILE * HD + 1024; // and room to align them
+  constexpr int INBOX = (MAX_GROUP - 1) * 8 * NT * HD * 4; // parts of the other CTAs of a group
   auto kern = kv8_attn_kernel<HD, CODE, NT, TILE, SUB, GROUPED>;
-  ES_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, RINGS + (KV8_MAX_B + 1) * (int)sizeof(int)));
+  ES_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     RINGS + (GROUPED ? INBOX : (KV8_MAX_B + 1) * (int)sizeof(int))));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(GROUPED ? p.B * p.Hkv * p.row_tiles * p.group : sm_count());
   cfg.blockDim = dim3(AW * 32);
-  cfg.dynamicSmemBytes = RINGS + (GROUPED ? 0 : (size_t)(p.B + 1) * sizeof(int));
+  cfg.dynamicSmemBytes = RINGS + (GROUPED ? (p.group > 1 ? INBOX : 0) : (size_t)(p.B + 1) * sizeof(int));
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
