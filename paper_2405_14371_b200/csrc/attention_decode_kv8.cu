@@ -187,7 +187,16 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
     __syncthreads();
   } else {
     int before = 0;
-    for (int base = 0; base < p.B; base += AW * 32) {
+    if (p.B <= 32) {                     // every warp for itself, all writing the same
+      const int v = lane < p.B ? tiles_of<TILE>(p.ctx_len[lane], p.max_ctx) : 0;
+      int inc = v;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) { const int o = __shfl_up_sync(~0u, inc, d); if (lane >= d) inc += o; }
+      if (lane < p.B) pre[lane + 1] = inc;
+      if (lane == 0) pre[0] = 0;
+      __syncthreads();                   // also: s_abort is set
+    }
+    for (int base = 0; p.B > 32 && base < p.B; base += AW * 32) {
       const int b = base + tid;
       const int v = b < p.B ? tiles_of<TILE>(p.ctx_len[b], p.max_ctx) : 0;
       int inc = v;
@@ -202,8 +211,10 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
       before += sum;
       __syncthreads();
     }
-    if (tid == 0) pre[0] = 0;
-    __syncthreads();
+    if (p.B > 32) {
+      if (tid == 0) pre[0] = 0;
+      __syncthreads();
+    }
     const int total = pre[p.B] * items;
     // stretches go round the SMs first: few tiles spread over all of them
     me = warp * gridDim.x + blockIdx.x;
@@ -222,7 +233,7 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
   int row_a = -1;                        // (-1: nothing there)
   float ks_c = 0.f, vs_c = 0.f;
   unsigned ok_a = 0, ok_c = 0;
-  auto ask = [&]() {
+  auto ask = [&](float& ks_to, float& vs_to) {
     const bool is_v = asked & 1;
     if (!is_v) {
       row_a = -1;
@@ -231,8 +242,8 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
         const int page = p.table[(int64_t)ahead.b * p.pps + (tok >> p.log2P)];
         if ((unsigned)page < (unsigned)p.n_pages) {
           const int ph = page * p.Hkv + ahead.kvh;         // the pool has less than 2^31 lines, so this fits
-          ks_a = p.ks[ph];
-          vs_a = p.vs[ph];
+          ks_to = p.ks[ph];
+          vs_to = p.vs[ph];
           row_a = (int)((((unsigned)ph << p.log2P) + (tok & (p.P - 1))) / (128 / HD));
         }
       }
@@ -254,7 +265,7 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
     __syncwarp();
     ++used;
     if (++slot == SL) { slot = 0; parity ^= 1; }
-    if (asked < n_half) ask();
+    if (asked < n_half) ask(ks_a, vs_a);
   };
 
   int limit[NT];
@@ -309,11 +320,11 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
 
   load_q();                              // before the first tiles are asked for: behind them it would wait for their bytes
   if (asked < n_half) {
-    ask();                               // the first tile's K
-    ks_c = ks_a; vs_c = vs_a; ok_c = ok_a;
-    ask();                               // its V
+    ask(ks_c, vs_c);                     // the first tile's K
+    ok_c = ok_a;
+    ask(ks_c, vs_c);                     // its V
   }
-  if (SL == 3 && asked < n_half) ask();  // the second tile's K, whose scales wait in ks_a, vs_a
+  if (SL == 3 && asked < n_half) ask(ks_a, vs_a);          // the second tile's K, whose scales wait in ks_a, vs_a
   start_item(begin);
 
   for (int at = begin; at < end && running; ++at) {
@@ -574,6 +585,7 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
       if (t == 0) s_ml[warp][8 * n + g] = make_float2(m_run[n], l_run[n]);
     }
     __syncthreads();
+    const int live = min(ROWS, n_rows - c.rt * ROWS);                     // rows that exist
     if (tid < AW * ROWS) {               // the factor of every warp's part of a row
       const int w = tid / ROWS, r = tid - w * ROWS;
       float2 ml[AW];
@@ -591,10 +603,12 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
     }
     __syncthreads();
     constexpr int PER = (ROWS * HD / 2 + AW * 32 - 1) / (AW * 32);        // pairs of outputs a thread
+    const int pairs = live * (HD / 2);
     float2 sum[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int at = min(tid + i * AW * 32, ROWS * HD / 2 - 1), r = at / (HD / 2);
+      const int at = tid + i * AW * 32, r = at / (HD / 2);
+      if (at >= pairs) break;
       sum[i] = make_float2(0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < AW; ++w) {
@@ -613,40 +627,44 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
         float2* to = cl.map_shared_rank(inbox, 0) + (rank - 1) * (ROWS * HD / 2);
 #pragma unroll
         for (int i = 0; i < PER; ++i)
-          if (tid + i * AW * 32 < ROWS * HD / 2) to[tid + i * AW * 32] = sum[i];
-        if (tid < ROWS) cl.map_shared_rank(&s_all[0][0], 0)[rank * ROWS + tid] = s_all[0][tid];
+          if (tid + i * AW * 32 < pairs) to[tid + i * AW * 32] = sum[i];
+        if (tid < live) cl.map_shared_rank(&s_all[0][0], 0)[rank * ROWS + tid] = s_all[0][tid];
       }
       cluster_sync_all();
       if (rank > 0) return;
-#pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const int at = min(tid + i * AW * 32, ROWS * HD / 2 - 1), r = at / (HD / 2);
-        float m = s_all[0][r].x;
-        for (int k = 1; k < p.group; ++k) m = fmaxf(m, s_all[k][r].x);
-        const float ref = m == -INFINITY ? 0.f : m, f0 = ex2(s_all[0][r].x - ref);
-        sum[i].x *= f0;
-        sum[i].y *= f0;
-        for (int k = 1; k < p.group; ++k) {
-          const float f = ex2(s_all[k][r].x - ref);
-          const float2 x = inbox[(k - 1) * (ROWS * HD / 2) + at];
-          sum[i].x += x.x * f;
-          sum[i].y += x.y * f;
-        }
-      }
     }
+    if (tid < ROWS && tid < live) {      // factors of the CTAs' parts, the sum's reciprocal in them
+      float2 ml[MAX_GROUP];
+      float m = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int k = 0; k < MAX_GROUP; ++k)
+        if (k < p.group) { ml[k] = s_all[k][tid]; m = fmaxf(m, ml[k].x); }
+      const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int k = 0; k < MAX_GROUP; ++k)
+        if (k < p.group) { ml[k].x = ex2(ml[k].x - ref); l += ml[k].y * ml[k].x; }
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+      for (int k = 0; k < MAX_GROUP; ++k)
+        if (k < p.group) s_all[k][tid].x = ml[k].x * inv;
+    }
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int at = tid + i * AW * 32, r = at / (HD / 2), d = at - r * (HD / 2);
-      if (at >= ROWS * HD / 2) break;
+      if (at >= pairs) break;
+      const float2* inbox = reinterpret_cast<const float2*>(ring + AW * SL * HALF);
+      float x = sum[i].x * s_all[0][r].x, y = sum[i].y * s_all[0][r].x;
+#pragma unroll
+      for (int k = 1; k < MAX_GROUP; ++k)
+        if (k < p.group) {
+          const float2 part = inbox[(k - 1) * (ROWS * HD / 2) + at];
+          x += part.x * s_all[k][r].x;
+          y += part.y * s_all[k][r].x;
+        }
       const int row_i = c.rt * ROWS + r, token = row_i / p.G;
-      if (row_i >= n_rows) continue;
-      float m = s_all[0][r].x, l = 0.f;
-      for (int k = 1; k < p.group; ++k) m = fmaxf(m, s_all[k][r].x);
-      const float ref = m == -INFINITY ? 0.f : m;
-      for (int k = 0; k < p.group; ++k) l += s_all[k][r].y * ex2(s_all[k][r].x - ref);
-      const float inv = l == 0.f ? 0.f : 1.f / l;
       const int64_t row = ((int64_t)c.b * p.T + token) * p.Hq + c.kvh * p.G + (row_i - token * p.G);
-      reinterpret_cast<uint32_t*>(p.out)[(row * HD) / 2 + d] = two_outputs(sum[i].x * inv, sum[i].y * inv, p.bf16);
+      reinterpret_cast<uint32_t*>(p.out)[(row * HD) / 2 + d] = two_outputs(x, y, p.bf16);
     }
   }
 }
