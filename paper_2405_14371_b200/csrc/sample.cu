@@ -49,23 +49,28 @@ struct SampleParams {
 };
 
 struct Shared {
-  u64 total;                                  // this CTA's, read by the cluster
-  u64 best;                                   // this CTA's largest (key, index)
-  u64 warp_u64[SW];
-  uint32_t warp_u32[SW];
-  float least;                                // smallest finite logit
-  int found;                                  // a chosen index, written into every CTA by the one that finds it
-  // written into every CTA by the first one
+  // one entry per CTA of the cluster, written by that CTA into everybody's copy: after the next cluster barrier each reads
+  // its own memory
+  u64 total[MAX_CLUSTER];
+  u64 best[MAX_CLUSTER];                      // largest (key, index)
+  float least[MAX_CLUSTER];                   // smallest finite logit
+  int found;                                  // a chosen index, from the CTA that found it
+  // from the first CTA
   int pick_bin, pick_count;                   // a bin, and how many elements it holds
-  uint32_t pick_rank;                         // elements to keep of the bin
-  u64 pick_mass;                              // mass to reach within the bin
+  u64 pick_target;                            // rank (counts) or mass to reach within the bin
   u64 pick_pair;                              // threshold found in the list
+  // this CTA's own
   u64 all_mass;
   int list_n;
+  u64 warp_a[SW], warp_b[SW];
   u64 hist[256], comb[256];                   // descent by key bits
   int digit;
   u64 digit_above, digit_here;
 };
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
 // order-preserving integer of a float that is not NaN
 __device__ __forceinline__ uint32_t key_of(float x) {
   const uint32_t b = __float_as_uint(x);
@@ -118,7 +123,7 @@ struct Row {
   uint32_t *cnt, *part;                       // [NB] counts, [3][NB] weights in three fields of 15 bits
   uint32_t* ccnt;                             // [NB] the cluster's counts   (first CTA)
   u64* cmass;                                 // [NB] ... and weights
-  u64* list;                                  // [LIST] elements of a bin, over cnt and part (first CTA)
+  u64 *list, *lweight;                        // [LIST] elements of a bin and, over `part`, their weights (first CTA)
   Shared* sm;
   int n, first, ranks, rank;                  // padded elements, global index of the first, CTAs
   float xmax, bin_scale;
@@ -144,9 +149,10 @@ struct Row {
     return v == xmax ? 0 : (int)fminf((xmax - v) * bin_scale, (float)(NB - 1));
   }
 
-  // chunk sums of f(value, index) in csum, the CTA's in sm->total; returns the cluster's
+  // chunk sums of f(value, index) in csum, every CTA's sum in sm->total; returns the cluster's
   template <class F>
   __device__ u64 sums(F f) {
+    cg::cluster_group cl = cg::this_cluster();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int ch = warp; ch < n / CHUNK; ch += SW) {
       const float4 v = *reinterpret_cast<const float4*>(x + ch * CHUNK + lane * 4);
@@ -159,47 +165,51 @@ struct Row {
       u64 s = 0;
       for (int ch = lane; ch < n / CHUNK; ch += 32) s += csum[ch];
       s = warp_sum(s);
-      if (lane == 0) sm->total = s;
+      if (lane < ranks) cl.map_shared_rank(sm, lane)->total[rank] = s;
     }
-    cg::cluster_group cl = cg::this_cluster();
     cl.sync();
     u64 all = 0;
-    for (int r = 0; r < ranks; ++r) all += cl.map_shared_rank(sm, r)->total;
+    for (int r = 0; r < ranks; ++r) all += sm->total[r];
     return all;
   }
 
-  // after sums(f): the first index at which the running sum of f exceeds `target` (< the cluster's sum), in every CTA
+  // after sums(f), in one warp: the first index of this CTA at which the running sum of f exceeds `target`, or -1 where
+  // that is in another CTA
+  template <class F>
+  __device__ int find_here(F f, u64 target) {
+    const int lane = threadIdx.x & 31;
+    u64 run = 0;
+    for (int r = 0; r < rank; ++r) run += sm->total[r];
+    if (run > target || target >= run + sm->total[rank]) return -1;
+    int ch = 0;
+    for (int base = 0; base < n / CHUNK; base += 32) {
+      const u64 v = base + lane < n / CHUNK ? csum[base + lane] : 0;
+      const u64 inc = run + warp_scan(v);
+      const unsigned hit = __ballot_sync(~0u, inc > target);
+      if (hit) {
+        const int l = __ffs(hit) - 1;
+        ch = base + l;
+        run = __shfl_sync(~0u, inc - v, l);
+        break;
+      }
+      run = __shfl_sync(~0u, inc, 31);
+    }
+    const float4 v = *reinterpret_cast<const float4*>(x + ch * CHUNK + lane * 4);
+    const int i = first + ch * CHUNK + lane * 4;
+    const u64 a = f(v.x, i), b = a + f(v.y, i + 1), d = b + f(v.z, i + 2), e = d + f(v.w, i + 3);
+    const u64 inc = run + warp_scan(e), base = inc - e;
+    const unsigned hit = __ballot_sync(~0u, inc > target);
+    const int at = i + (base + a > target ? 0 : base + b > target ? 1 : base + d > target ? 2 : 3);
+    return __shfl_sync(~0u, at, __ffs(hit) - 1);
+  }
+
+  // the same, in every CTA
   template <class F>
   __device__ int find(F f, u64 target) {
     cg::cluster_group cl = cg::this_cluster();
-    const int lane = threadIdx.x & 31;
     if (threadIdx.x < 32) {
-      u64 before = 0;
-      for (int r = 0; r < rank; ++r) before += cl.map_shared_rank(sm, r)->total;
-      if (before <= target && target < before + sm->total) {
-        u64 run = before;
-        int ch = 0;
-        for (int base = 0; base < n / CHUNK; base += 32) {
-          const u64 v = base + lane < n / CHUNK ? csum[base + lane] : 0;
-          const u64 inc = run + warp_scan(v);
-          const unsigned hit = __ballot_sync(~0u, inc > target);
-          if (hit) {
-            const int l = __ffs(hit) - 1;
-            ch = base + l;
-            run = __shfl_sync(~0u, inc - v, l);
-            break;
-          }
-          run = __shfl_sync(~0u, inc, 31);
-        }
-        const float4 v = *reinterpret_cast<const float4*>(x + ch * CHUNK + lane * 4);
-        const int i = first + ch * CHUNK + lane * 4;
-        const u64 a = f(v.x, i), b = a + f(v.y, i + 1), d = b + f(v.z, i + 2), e = d + f(v.w, i + 3);
-        const u64 inc = run + warp_scan(e), base = inc - e;
-        const unsigned hit = __ballot_sync(~0u, inc > target);
-        const int at = i + (base + a > target ? 0 : base + b > target ? 1 : base + d > target ? 2 : 3);
-        const int got = __shfl_sync(~0u, at, __ffs(hit) - 1);
-        if (lane < ranks) cl.map_shared_rank(sm, lane)->found = got;
-      }
+      const int got = find_here(f, target);
+      if (got >= 0 && threadIdx.x < ranks) cl.map_shared_rank(sm, threadIdx.x)->found = got;
     }
     cl.sync();
     const int got = sm->found;
@@ -261,91 +271,165 @@ struct Row {
   // Counts per bin, and weights where asked, summed over the cluster in the first CTA.
   __device__ void histogram(bool mass) {
     cg::cluster_group cl = cg::this_cluster();
-    for (int i = threadIdx.x; i < (mass ? 4 : 1) * NB; i += ST) cnt[i] = 0;         // part follows cnt
+    for (int i = threadIdx.x; i < (mass ? NB : NB / 4); i += ST) reinterpret_cast<uint4*>(cnt)[i] = make_uint4(0, 0, 0, 0);     // part follows cnt
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += ST) {
-      const float v = x[i];
-      const int b = bin_of(v);
-      atomicAdd(&cnt[b], 1u);
+    for (int i = threadIdx.x * 4; i < n; i += ST * 4) {
+      const float4 v4 = *reinterpret_cast<const float4*>(x + i);
+      const float v[4] = {v4.x, v4.y, v4.z, v4.w};
+      int b[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { b[j] = bin_of(v[j]); atomicAdd(&cnt[b[j]], 1u); }
       if (mass) {
-        const u64 w = weight(v);
-        if (w) {
-          atomicAdd(&part[b], (uint32_t)w & 0x7fffu);
-          atomicAdd(&part[NB + b], (uint32_t)(w >> 15) & 0x7fffu);
-          atomicAdd(&part[2 * NB + b], (uint32_t)(w >> 30));
-        }
+        u64 w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = weight(v[j]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (w[j]) {
+            atomicAdd(&part[b[j]], (uint32_t)w[j] & 0x7fffu);
+            atomicAdd(&part[NB + b[j]], (uint32_t)(w[j] >> 15) & 0x7fffu);
+            atomicAdd(&part[2 * NB + b[j]], (uint32_t)(w[j] >> 30));
+          }
       }
     }
     cl.sync();
+    // each CTA adds up its share of the bins, all copies of a bin under way at a time
     uint32_t* to_cnt = cl.map_shared_rank(ccnt, 0);
     u64* to_mass = cl.map_shared_rank(cmass, 0);
     const int share = NB / ranks;
     for (int i = threadIdx.x; i < share; i += ST) {
       const int b = rank * share + i;
-      uint32_t k = 0;
-      u64 m = 0;
-      for (int r = 0; r < ranks; ++r) {
-        const uint32_t* c0 = cl.map_shared_rank(cnt, r);
-        k += c0[b];
-        if (mass) m += (u64)c0[NB + b] + ((u64)c0[2 * NB + b] << 15) + ((u64)c0[3 * NB + b] << 30);
+      uint32_t c[MAX_CLUSTER], m[MAX_CLUSTER][3];
+#pragma unroll
+      for (int r = 0; r < MAX_CLUSTER; ++r) {
+        c[r] = m[r][0] = m[r][1] = m[r][2] = 0;
+        if (r < ranks) {
+          const uint32_t* from = cl.map_shared_rank(cnt, r);
+          c[r] = from[b];
+          if (mass) { m[r][0] = from[NB + b]; m[r][1] = from[2 * NB + b]; m[r][2] = from[3 * NB + b]; }
+        }
       }
+      uint32_t k = 0;
+      u64 w = 0;
+#pragma unroll
+      for (int r = 0; r < MAX_CLUSTER; ++r) { k += c[r]; w += m[r][0] + ((u64)m[r][1] << 15) + ((u64)m[r][2] << 30); }
       to_cnt[b] = k;
-      to_mass[b] = m;
+      if (mass) to_mass[b] = w;
     }
     cl.sync();
   }
 
-  // The first CTA: inclusive sums of its two bins a thread (bins 2 tid and 2 tid + 1).
-  __device__ __forceinline__ u64 scan_bins(u64 a) {
+  // Inclusive block sums of a and b.
+  __device__ __forceinline__ void scan2(u64& a, u64& b) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    u64 inc = warp_scan(a);
-    if (lane == 31) sm->warp_u64[warp] = inc;
+    a = warp_scan(a);
+    b = warp_scan(b);
+    if (lane == 31) { sm->warp_a[warp] = a; sm->warp_b[warp] = b; }
     __syncthreads();
-    u64 before = 0;
-    for (int w = 0; w < warp; ++w) before += sm->warp_u64[w];
+    u64 wa = lane < warp ? sm->warp_a[lane & (SW - 1)] : 0, wb = lane < warp ? sm->warp_b[lane & (SW - 1)] : 0;      // SW = 16 <= 32
+    a += warp_sum(wa);
+    b += warp_sum(wb);
     __syncthreads();
-    return before + inc;
   }
 
-  __device__ __forceinline__ void publish(int bin, int count, uint32_t r, u64 mass) {       // by one thread
+  __device__ __forceinline__ void publish(int bin, int count, u64 target) {                 // by one thread
     cg::cluster_group cl = cg::this_cluster();
     for (int i = 0; i < ranks; ++i) {
       Shared* to = cl.map_shared_rank(sm, i);
-      to->pick_bin = bin; to->pick_count = count; to->pick_rank = r; to->pick_mass = mass;
+      to->pick_bin = bin; to->pick_count = count; to->pick_target = target;
     }
   }
+  __device__ __forceinline__ void publish_pair(u64 pair) {
+    cg::cluster_group cl = cg::this_cluster();
+    for (int i = 0; i < ranks; ++i) cl.map_shared_rank(sm, i)->pick_pair = pair;
+  }
 
-  // The elements of bin `pick_bin` in the first CTA's list, in ranking order, padded with zeros to a power of two.
+  // The elements of bin `pick_bin` go to the first CTA's list, each CTA's behind those of the CTAs before it.
   __device__ void collect() {
     cg::cluster_group cl = cg::this_cluster();
-    const int bin = sm->pick_bin;
-    u64* to = cl.map_shared_rank(list, 0);
-    int* count = cl.map_shared_rank(&sm->list_n, 0);
-    for (int i = threadIdx.x; i < n; i += ST) {
-      const float v = x[i];
-      if (bin_of(v) == bin) {
-        const int at = atomicAdd(count, 1);
-        if (at < LIST) to[at] = pair_key(key_of(v), first + i);
+    const int bin = sm->pick_bin, lane = threadIdx.x & 31;
+    const uint32_t c = lane < ranks ? cl.map_shared_rank(cnt, lane)[bin] : 0;
+    const int base = (int)__reduce_add_sync(~0u, lane < rank ? c : 0u);
+    if (threadIdx.x == 0) sm->list_n = 0;
+    __syncthreads();
+    if (cnt[bin]) {
+      u64* to = cl.map_shared_rank(list, 0) + base;
+      for (int i = threadIdx.x * 4; i < n; i += ST * 4) {
+        const float4 v4 = *reinterpret_cast<const float4*>(x + i);
+        const float v[4] = {v4.x, v4.y, v4.z, v4.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (bin_of(v[j]) == bin) to[atomicAdd(&sm->list_n, 1)] = pair_key(key_of(v[j]), first + i + j);
       }
     }
     cl.sync();
-    if (rank != 0) return;
-    const int m = min(sm->pick_count, LIST);
-    int size = 32;
+  }
+
+  // First CTA, list of m elements: the one at which, in ranking order, the running count (or, by_mass, weight) reaches
+  // `target` is handed to `chosen` with the running weight up to and including it.
+  template <class G>
+  __device__ void choose(int m, bool by_mass, bool weights, u64 target, G chosen) {
+    if (weights) {
+      for (int i = threadIdx.x; i < m; i += ST) lweight[i] = weight(of_key((uint32_t)(list[i] >> 32)));
+      __syncthreads();
+    }
+    if (m <= ST / 2) {                        // every element against every other, several threads an element
+      int q = 2;
+      while (q < 16 && m * q * 2 <= ST) q *= 2;
+      const int e = threadIdx.x / q;
+      const u64 mine = e < m ? list[e] : ~0ull;
+      u64 before = 0, mass = 0;
+#pragma unroll 4
+      for (int j = threadIdx.x & (q - 1); j < m; j += q) {
+        const u64 other = list[j];
+        before += other > mine;
+        if (weights && other >= mine) mass += lweight[j];
+      }
+      for (int d = 1; d < q; d <<= 1) {
+        before += __shfl_xor_sync(~0u, before, d);
+        mass += __shfl_xor_sync(~0u, mass, d);
+      }
+      if (e < m && (threadIdx.x & (q - 1)) == 0) {
+        const bool hit = by_mass ? mass >= target && mass - lweight[e] < target : before + 1 == target;
+        if (hit) chosen(mine, mass);
+      }
+      __syncthreads();
+      return;
+    }
+    int size = ST;                            // many: bitonic, descending, padded with zeros
     while (size < m) size *= 2;
-    for (int i = m + threadIdx.x; i < size; i += ST) list[i] = 0;
+    for (int i = m + threadIdx.x; i < size; i += ST) { list[i] = 0; lweight[i] = 0; }
     __syncthreads();
-    for (int k = 2; k <= size; k *= 2)        // bitonic, descending
+    for (int k = 2; k <= size; k *= 2)
       for (int j = k / 2; j > 0; j /= 2) {
         for (int i = threadIdx.x; i < size / 2; i += ST) {
           const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
           const u64 a = list[lo], b = list[hi];
-          if ((a < b) == ((lo & k) == 0)) { list[lo] = b; list[hi] = a; }
+          if ((a < b) == ((lo & k) == 0)) {
+            list[lo] = b; list[hi] = a;
+            const u64 wa = lweight[lo];
+            lweight[lo] = lweight[hi]; lweight[hi] = wa;
+          }
         }
         __syncthreads();
       }
+    const int each = size / ST, at = threadIdx.x * each;          // 1 or 2 elements a thread
+    u64 w = 0, nothing = 0;
+    if (weights) for (int i = 0; i < each; ++i) w += lweight[at + i];
+    u64 run = w;
+    scan2(run, nothing);
+    run -= w;
+    for (int i = 0; i < each; ++i) {
+      const u64 wi = weights ? lweight[at + i] : 0;
+      const bool hit = at + i < m && (by_mass ? run < target && target <= run + wi : (u64)(at + i) + 1 == target);
+      run += wi;
+      if (hit) chosen(list[at + i], run);
+    }
+    __syncthreads();
   }
 };
+
+static_assert(SW == 16 && LIST == 2 * ST && NB == 2 * ST && LIST * 8 <= 3 * NB * 4, "scan2, choose and the bins of a thread");
 
 template <int DT>
 __device__ __forceinline__ float load_logit(const void* p, int64_t i) {
@@ -357,8 +441,8 @@ __device__ __forceinline__ float load_logit(const void* p, int64_t i) {
 }
 
 __host__ __device__ constexpr size_t sample_smem(int slice) {
-  // logits, chunk sums, the CTA's histogram (later the list), the cluster's counts and weights
-  return (size_t)slice * 4 + (size_t)(slice / CHUNK) * 8 + (size_t)NB * 16 + (size_t)NB * 12;
+  // logits, chunk sums, the CTA's histogram, the cluster's weights and counts, the list
+  return (size_t)slice * 4 + (size_t)(slice / CHUNK) * 8 + (size_t)NB * (16 + 8 + 4) + (size_t)LIST * 8;
 }
 
 template <int DT>
@@ -366,16 +450,18 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
   extern __shared__ __align__(16) unsigned char dyn[];
   __shared__ Shared shared;
   cg::cluster_group cl = cg::this_cluster();
+  cluster_arrive();                           // "this CTA runs": nobody writes into it before
   const int ranks = (int)cl.num_blocks(), rank = (int)cl.block_rank(), row = blockIdx.x / ranks;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   Row R;
   R.x = reinterpret_cast<float*>(dyn);
-  R.cmass = reinterpret_cast<u64*>(dyn + (size_t)p.slice * 4);
-  R.list = R.cmass + NB;
-  R.cnt = reinterpret_cast<uint32_t*>(R.list);
+  R.cnt = reinterpret_cast<uint32_t*>(dyn + (size_t)p.slice * 4);
   R.part = R.cnt + NB;
-  R.ccnt = R.part + 3 * NB;
-  R.csum = reinterpret_cast<u64*>(R.ccnt + NB);
+  R.cmass = reinterpret_cast<u64*>(R.part + 3 * NB);
+  R.list = R.cmass + NB;
+  R.lweight = reinterpret_cast<u64*>(R.part);  // read by nobody once the cluster's sums are made
+  R.csum = R.list + LIST;
+  R.ccnt = reinterpret_cast<uint32_t*>(R.csum + p.slice / CHUNK);
   R.sm = &shared;
   R.ranks = ranks;
   R.rank = rank;
@@ -387,7 +473,7 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
   u64 best = 0;
   float least = INFINITY;
   const int64_t row_at = (int64_t)row * p.row_stride + R.first;
-  constexpr int FLIGHT = 8;                   // loads of a thread under way at a time
+  constexpr int FLIGHT = 16;                  // loads of a thread under way at a time
   for (int base = 0; base < R.n; base += ST * FLIGHT) {
     float v[FLIGHT];
 #pragma unroll
@@ -412,29 +498,31 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
     best = o > best ? o : best;
     least = fminf(least, __shfl_xor_sync(~0u, least, d));
   }
-  if (lane == 0) { shared.warp_u64[warp] = best; shared.warp_u32[warp] = __float_as_uint(least); }
+  if (lane == 0) { shared.warp_a[warp] = best; shared.warp_b[warp] = __float_as_uint(least); }
   __syncthreads();
+  cluster_wait();
   if (warp == 0) {
-    best = lane < SW ? shared.warp_u64[lane] : 0;
-    least = lane < SW ? __uint_as_float(shared.warp_u32[lane]) : INFINITY;
+    best = lane < SW ? shared.warp_a[lane] : 0;
+    least = lane < SW ? __uint_as_float((uint32_t)shared.warp_b[lane]) : INFINITY;
 #pragma unroll
     for (int d = 16; d; d >>= 1) {
       const u64 o = __shfl_xor_sync(~0u, best, d);
       best = o > best ? o : best;
       least = fminf(least, __shfl_xor_sync(~0u, least, d));
     }
-    if (lane == 0) {
-      shared.best = best; shared.least = least; shared.list_n = 0;
-      shared.pick_bin = 0; shared.pick_count = 0; shared.pick_rank = 1; shared.pick_mass = 1; shared.pick_pair = 0;
+    if (lane < ranks) {
+      Shared* to = cl.map_shared_rank(&shared, lane);
+      to->best[rank] = best;
+      to->least[rank] = least;
     }
+    if (lane == 0) { shared.pick_bin = 0; shared.pick_count = 0; shared.pick_target = 1; shared.pick_pair = 0; }
   }
   cl.sync();
   best = 0;
   least = INFINITY;
   for (int r = 0; r < ranks; ++r) {
-    const Shared* o = cl.map_shared_rank(&shared, r);
-    best = o->best > best ? o->best : best;
-    least = fminf(least, o->least);
+    best = shared.best[r] > best ? shared.best[r] : best;
+    least = fminf(least, shared.least[r]);
   }
 
   R.xmax = of_key((uint32_t)(best >> 32));
@@ -445,7 +533,6 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
       p.tokens[row] = R.xmax == -INFINITY ? -1 : top;
       if (p.logprobs) p.logprobs[row] = R.xmax == -INFINITY ? -INFINITY : 0.f;
     }
-    cl.sync();                                // no CTA leaves while another may still read its shared memory
     return;
   }
   R.c = 1.4426950408889634 / (double)T;
@@ -459,48 +546,49 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
     const float span = fminf(R.xmax - least, REACH / R.cf);
     R.bin_scale = span > 0.f ? fminf((NB - 1) / span, 1e37f) : 0.f;
     R.histogram(by_mass);
-    u64 counts = 0, masses = 0;               // first CTA: inclusive sums up to this thread's second bin
+    // first CTA: inclusive sums up to this thread's second bin (bins 2 tid and 2 tid + 1)
+    u64 counts = 0, masses = 0, m0 = 0, m1 = 0;
     uint32_t c0 = 0, c1 = 0;
-    u64 m0 = 0, m1 = 0;
+    auto pick_mass = [&]() {                  // first CTA: the bin in which the mass is reached, of the kept mass so far
+      const u64 all = shared.all_mass;
+      bool more;
+      u64 target = share_of(fmaxf(tp, 0.f), all, &more);
+      target += more;
+      target = target < 1 ? 1 : target > all ? all : target;
+      const u64 a = masses - m0 - m1, b = masses - m1;
+      if (a < target && target <= b) R.publish(2 * tid, (int)c0, target - a);
+      if (b < target && target <= masses) R.publish(2 * tid + 1, (int)c1, target - b);
+    };
     if (rank == 0) {
       c0 = R.ccnt[2 * tid]; c1 = R.ccnt[2 * tid + 1];
-      counts = R.scan_bins((u64)c0 + c1);
-      if (by_mass) {
-        m0 = R.cmass[2 * tid]; m1 = R.cmass[2 * tid + 1];
-        masses = R.scan_bins(m0 + m1);
-        if (!by_count && tid == ST - 1) shared.all_mass = masses;
+      counts = (u64)c0 + c1;
+      if (by_mass) { m0 = R.cmass[2 * tid]; m1 = R.cmass[2 * tid + 1]; masses = m0 + m1; }
+      R.scan2(counts, masses);
+      if (by_count) {
+        const u64 a = counts - c0 - c1, b = counts - c1;
+        if (a < (u64)k && (u64)k <= b) { R.publish(2 * tid, (int)c0, k - a); shared.all_mass = masses - m0 - m1; }
+        if (b < (u64)k && (u64)k <= counts) { R.publish(2 * tid + 1, (int)c1, k - b); shared.all_mass = masses - m1; }
+      } else {
+        if (tid == ST - 1) shared.all_mass = masses;
+        __syncthreads();
+        pick_mass();
       }
     }
-    bool listed = false;                      // the list holds bin `pick_bin`
-    int listed_bin = -1;
+    cl.sync();
+    int listed = -1;                          // the bin that the list holds
     if (by_count) {
-      if (rank == 0) {
-        const u64 a = counts - c0 - c1, b = counts - c1;
-        const bool one = a < (u64)k && (u64)k <= b, two = b < (u64)k && (u64)k <= counts;
-        if (one) { R.publish(2 * tid, (int)c0, (uint32_t)(k - a), 0); if (by_mass) shared.all_mass = masses - m0 - m1; }
-        if (two) { R.publish(2 * tid + 1, (int)c1, (uint32_t)(k - b), 0); if (by_mass) shared.all_mass = masses - m1; }
-      }
-      cl.sync();
-      const uint32_t want = shared.pick_rank;
-      if (shared.pick_count <= LIST) {
-        listed = true;
-        listed_bin = shared.pick_bin;
+      const u64 want = shared.pick_target;
+      const int bin = shared.pick_bin, m = shared.pick_count;
+      if (m <= LIST) {
+        listed = bin;
         R.collect();
-        if (rank == 0) {
-          if (by_mass) {                      // mass of the first `want` of the bin joins that of the bins before
-            u64 s = 0;
-            for (uint32_t i = tid; i < want; i += ST) s += R.weight(of_key((uint32_t)(R.list[i] >> 32)));
-            s = warp_sum(s);
-            if (lane == 0) shared.warp_u64[warp] = s;
-            __syncthreads();
-            if (tid == 0) for (int w = 0; w < SW; ++w) shared.all_mass += shared.warp_u64[w];
-          }
-          if (tid < ranks) cl.map_shared_rank(&shared, tid)->pick_pair = R.list[want - 1];
+        if (rank == 0) {                      // the mass of the bin's kept elements joins that of the bins before
+          R.choose(m, false, by_mass, want, [&](u64 pair, u64 mass) { R.publish_pair(pair); shared.all_mass += mass; });
+          if (by_mass) pick_mass();
         }
         cl.sync();
         R.keep = shared.pick_pair;
       } else {                                // too many for the list: by the bits of their keys
-        const int bin = shared.pick_bin;
         u64 above, here;
         const uint32_t key = R.descend([&](float v, int) { return (u64)(R.bin_of(v) == bin); }, want, &above, &here);
         int cut = INT_MAX;
@@ -512,47 +600,24 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
         R.keep = ((u64)key << 32) | (cut == INT_MAX ? 0u : (uint32_t)~cut);
         if (by_mass) {
           const u64 s = R.sums([&](float v, int i) { return R.bin_of(v) == bin && R.kept(v, i) ? R.weight(v) : 0ull; });
+          if (rank == 0) {
+            if (tid == 0) shared.all_mass += s;
+            __syncthreads();
+            pick_mass();
+          }
           cl.sync();
-          if (rank == 0 && tid == 0) shared.all_mass += s;
         }
       }
     }
     if (by_mass) {
-      if (rank == 0) {
-        __syncthreads();
-        const u64 all = shared.all_mass;
-        bool more;
-        u64 target = share_of(fmaxf(tp, 0.f), all, &more);
-        target += more;
-        target = target < 1 ? 1 : target > all ? all : target;
-        const u64 a = masses - m0 - m1, b = masses - m1;
-        if (a < target && target <= b) R.publish(2 * tid, (int)c0, 0, target - a);
-        if (b < target && target <= masses) R.publish(2 * tid + 1, (int)c1, 0, target - b);
-        if (tid == 0) shared.list_n = 0;
-      }
-      cl.sync();
-      const u64 target = shared.pick_mass;
-      if (shared.pick_count <= LIST) {
-        if (!listed || listed_bin != shared.pick_bin) R.collect();
-        if (rank == 0) {
-          u64 run = 0;
-          for (int base = 0; base < LIST; base += ST) {
-            const int i = base + tid;
-            const u64 pr = i < shared.pick_count ? R.list[i] : 0;
-            const u64 w = i < shared.pick_count ? R.weight(of_key((uint32_t)(pr >> 32))) : 0;
-            const u64 inc = run + R.scan_bins(w);
-            if (inc - w < target && target <= inc)
-              for (int r = 0; r < ranks; ++r) cl.map_shared_rank(&shared, r)->pick_pair = pr;
-            if (tid == ST - 1) shared.total = inc;
-            __syncthreads();
-            run = shared.total;
-            __syncthreads();
-          }
-        }
+      const u64 target = shared.pick_target;
+      const int bin = shared.pick_bin, m = shared.pick_count;
+      if (m <= LIST) {
+        if (listed != bin) R.collect();
+        if (rank == 0) R.choose(m, true, true, target, [&](u64 pair, u64) { R.publish_pair(pair); });
         cl.sync();
         R.keep = shared.pick_pair > R.keep ? shared.pick_pair : R.keep;
       } else {
-        const int bin = shared.pick_bin;
         u64 above, here;
         const uint32_t key = R.descend([&](float v, int) { return R.bin_of(v) == bin ? R.weight(v) : 0ull; }, target, &above, &here);
         const u64 w = R.weight(of_key(key));
@@ -575,13 +640,13 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
   }
   auto last = [&](float v, int i) { const u64 w = R.kept(v, i) ? R.weight(v) : 0ull; return w >= R.least ? w : 0ull; };
   const u64 all = R.sums(last);
+  if (warp > 0) return;                       // nothing is read from another CTA any more
   const float u = fminf(fmaxf(p.u[row], 0.f), 1.f);
   bool more;
   u64 target = u < 1.f ? share_of(u, all, &more) : all;
   if (target >= all) target = all - 1;
-  const int token = R.find(last, target);
-  // the drawn token's own logit, from whichever CTA holds it
-  if (token >= R.first && token < R.first + real && tid == 0) {
+  const int token = R.find_here(last, target);
+  if (token >= 0 && lane == 0) {
     const float v = R.x[token - R.first];
     const double t = v == R.xmax ? 0.0 : ((double)v - (double)R.xmax) * R.c;
     p.tokens[row] = token;
