@@ -117,6 +117,11 @@ def _load() -> C.CDLL:
 
 
 lib = _load()
+try:
+    from . import _native_binding as _native
+except ImportError as e:
+    raise ImportError(f"{os.path.join(_HERE, '_native_binding.so')} is missing or does not fit this torch ({e}): build it "
+                      "with `python -m paper_2405_14371_b200.build`") from e
 EXPORTS = ("es_shard_workspace_bytes es_shard_create es_shard_prefill es_shard_prefill_ragged es_shard_prefill_packed es_shard_decode_step es_shard_handoff "
            "es_layer_profile es_shard_set_profiling es_shard_reset_slots es_shard_set_page_table es_shard_set_graphs "
            "es_partition_latency es_partition_throughput es_shard_device_status es_shard_wait_probe es_shard_launch_count es_shard_set_kernel_timing es_shard_kernel_timing es_shard_kernel_timing_detail es_shard_set_step_timing es_shard_step_timing es_shard_destroy es_last_error es_version es_op_rmsnorm "
@@ -428,78 +433,18 @@ def es_op_decode_attention_static(q: torch.Tensor, k_pages: torch.Tensor, v_page
 # ---- decode loop over a paged cache held in 8 bits -------------------------------------------
 
 _VALUE_DTYPES = {torch.float16: ES_DTYPE_F16, torch.bfloat16: ES_DTYPE_BF16, torch.float32: ES_DTYPE_F32}
-_CODE_DTYPES = {torch.int8: ES_DTYPE_I8, torch.float8_e4m3fn: ES_DTYPE_F8E4M3}
 
-# A decode step calls these once per layer, so their checks run on what costs least to ask of a tensor, and messages are
-# put together only once something is wrong.
-
-
-def _refuse(message: str):
-    raise EsError(1, message)
+# A decode step makes these calls once per layer, so their checks, result memory and stream are handled in the compiled
+# module (csrc_py/native_binding.cpp); every refusal is an EsError with the C ABI's status.
+_native.set_errors(EsError, torch.cuda.OutOfMemoryError)
 
 
-def _launch_on(stream, names: str, *tensors) -> int:
-    """The raw stream to launch on.  All tensors (None = not given) and the stream must be on the current device, where
-    the library launches."""
-    dev = tensors[0].get_device()
-    for t in tensors:
-        if t is not None and t.get_device() != dev:
-            dev = -1
-    if dev < 0:
-        listed = ", ".join(f"{n}: {t.device}" for n, t in zip(names.split(), tensors) if t is not None)
-        _refuse(f"all tensors must be on one CUDA device ({listed})")
-    if dev != torch.cuda.current_device():
-        _refuse(f"{names.split()[0]} is on cuda:{dev}, the current device is cuda:{torch.cuda.current_device()}")
+def _call(stream, f, *args):
+    """On the current stream, or on `stream` (its device becomes current and results belong to it for the allocator)."""
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(dev)
-    if stream.device.index != dev:
-        _refuse(f"the stream is on {stream.device}, the current device is cuda:{dev}")
-    return int(stream.cuda_stream)
-
-
-def _ints(names: str, *tensors) -> None:
-    for i, t in enumerate(tensors):
-        if t is not None and not (t.dtype is torch.int32 and t.is_contiguous()):
-            _refuse(f"{names.split()[i]} must be a contiguous int32 tensor")
-
-
-def _empty(stream, shape, dtype, like) -> torch.Tensor:
-    """Memory for a call on `stream`: the allocator must know the stream it is used on."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return f(*args)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=like.device)
-
-
-def _check_pool(k_pages, v_pages, k_scale, v_scale):
-    shape = k_pages.shape
-    if len(shape) != 4 or v_pages.shape != shape:
-        _refuse("k_pages and v_pages must be [n_pages, Hkv, P, hd] of one shape")
-    if k_pages.dtype not in _CODE_DTYPES or v_pages.dtype is not k_pages.dtype:
-        _refuse("pages must be int8 or float8_e4m3fn, both the same")
-    if not (k_pages.is_contiguous() and v_pages.is_contiguous()):
-        _refuse("pages must be contiguous")
-    for t in (k_scale, v_scale):
-        if t.dtype is not torch.float32 or not t.is_contiguous() or t.shape != shape[:2]:
-            _refuse("k_scale and v_scale must be contiguous fp32 [n_pages, Hkv]")
-    return shape
-
-
-def _row_stride(t: torch.Tensor, name: str) -> int:
-    """Elements from row to row of [..., heads, hd] whose last two dimensions are dense and whose leading ones, if
-    several, step evenly: a slice of a fused projection's output is such a tensor."""
-    shape, stride = t.shape, t.stride()
-    if stride[-1] != 1 or (stride[-2] != shape[-1] and shape[-2] != 1):
-        _refuse(f"the heads of a row of {name} must be contiguous")
-    step = 0                        # of the innermost leading dimension with more than one entry
-    span = 0                        # what the next one outwards has to step by
-    for i in range(len(shape) - 3, -1, -1):
-        if shape[i] != 1:
-            if span and stride[i] != span:
-                _refuse(f"the rows of {name} must be evenly spaced")
-            step = step or stride[i]
-            span = stride[i] * shape[i]
-    return step or shape[-1] * shape[-2]
+        return f(*args)
 
 
 class KvPlan(NamedTuple):
@@ -523,80 +468,21 @@ def es_op_kv_plan(old_len: torch.Tensor, new_len: torch.Tensor, block_table: tor
     free_count are brought up to date in place; without the latter two the table is taken as it is and n_pages says
     which of its entries are pages (default: any that is not negative).  `out`: a KvPlan of the same sizes to write
     into; its len_out may be old_len itself."""
-    if (free_pages is None) != (free_count is None):
-        _refuse("free_pages and free_count go together")
-    raw = _launch_on(stream, "old_len new_len block_table free_pages free_count", old_len, new_len, block_table, free_pages, free_count)
-    _ints("old_len new_len block_table free_pages free_count", old_len, new_len, block_table, free_pages, free_count)
-    shape = block_table.shape
-    if len(shape) != 2 or old_len.shape != shape[:1] or new_len.shape != shape[:1]:
-        _refuse("lengths must be [B], block_table [B, pages]")
-    B, pps = shape
-    if free_pages is not None:
-        if free_pages.dim() != 1 or free_count.numel() != 1:
-            _refuse("free_pages must be [n_pages], free_count one number")
-        if n_pages is not None and n_pages != free_pages.numel():
-            _refuse("n_pages must be the size of free_pages")
-        n_pages = free_pages.numel()
-    elif n_pages is None:
-        n_pages = (2 ** 31 - 1) // max(1, page_tokens)
-    max_runs = es_op_kv_plan_max_runs(B, max_rows, page_tokens)
-    if out is None:
-        if max_rows <= 0 or B <= 0:
-            _refuse("bad sizes")
-        sizes = [B + 1, max_rows, max_rows, max_rows, max_runs, B]
-        out = KvPlan(*_empty(stream, sum(sizes), torch.int32, old_len).split(sizes))
-    else:
-        _launch_on(stream, " ".join(KvPlan._fields), *out)
-        _ints(" ".join(KvPlan._fields), *out)
-        if [tuple(t.shape) for t in out] != [(B + 1,), (max_rows,), (max_rows,), (max_rows,), (max_runs,), (B,)]:
-            _refuse(f"out must hold tensors of {B + 1}, {max_rows}, {max_rows}, {max_rows}, {max_runs} and {B} entries")
-    _check(lib.es_op_kv_plan(old_len.data_ptr(), new_len.data_ptr(), block_table.data_ptr(), _ptr(free_pages), _ptr(free_count), B, pps,
-                             page_tokens, n_pages, max_rows, *[t.data_ptr() for t in out], raw))
-    return out
+    return KvPlan._make(_call(stream, _native.kv_plan, old_len, new_len, block_table, page_tokens, max_rows, free_pages, free_count, n_pages, out))
 
 
 def es_op_kv8_append(k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
                      k_scale: torch.Tensor, v_scale: torch.Tensor, runs: Optional[torch.Tensor] = None, stream=None) -> None:
     """Writes rows k, v [n, Hkv, hd] (fp16 or bf16; evenly spaced, e.g. slices of a fused projection) into the 8-bit pages
     at slot_map (at least n entries); `runs` as es_op_kv_plan gives it."""
-    raw = _launch_on(stream, "k v slot_map k_pages v_pages k_scale v_scale runs", k, v, slot_map, k_pages, v_pages, k_scale, v_scale, runs)
-    n_pages, Hkv, P, hd = _check_pool(k_pages, v_pages, k_scale, v_scale)
-    _ints("slot_map runs", slot_map, runs)
-    n = k.shape[0] if k.dim() else 0
-    if k.shape != (n, Hkv, hd) or v.shape != k.shape:
-        _refuse("k and v must be [n, Hkv, hd]")
-    if k.dtype not in _VALUE_DTYPES or k.dtype is torch.float32 or v.dtype is not k.dtype:
-        _refuse("k and v must be fp16 or bf16, both the same")
-    if slot_map.numel() < n:
-        _refuse("slot_map must have an entry for every row")
-    stride = _row_stride(k, "k")
-    if stride != _row_stride(v, "v"):
-        _refuse("k and v must have the same row stride")
-    _check(lib.es_op_kv8_append(k.data_ptr(), v.data_ptr(), _VALUE_DTYPES[k.dtype], stride, n, slot_map.data_ptr(), _ptr(runs),
-                                0 if runs is None else runs.numel(), k_pages.data_ptr(), v_pages.data_ptr(), _CODE_DTYPES[k_pages.dtype],
-                                k_scale.data_ptr(), v_scale.data_ptr(), Hkv, hd, P, n_pages, raw))
+    _call(stream, _native.kv8_append, k, v, slot_map, k_pages, v_pages, k_scale, v_scale, runs)
 
 
 def es_op_kv8_gather(slot_map: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scale: torch.Tensor,
                      v_scale: torch.Tensor, dtype: torch.dtype = torch.float16, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
                      stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(k, v) [n, Hkv, hd]: the cached rows at slot_map [n], zeros where a slot is no place."""
-    raw = _launch_on(stream, "slot_map k_pages v_pages k_scale v_scale", slot_map, k_pages, v_pages, k_scale, v_scale)
-    n_pages, Hkv, P, hd = _check_pool(k_pages, v_pages, k_scale, v_scale)
-    _ints("slot_map", slot_map)
-    if dtype not in _VALUE_DTYPES:
-        _refuse("dtype must be fp16, bf16 or fp32")
-    n = slot_map.numel()
-    if out is None:
-        out = tuple(_empty(stream, (2, n, Hkv, hd), dtype, k_pages).unbind())
-    else:
-        _launch_on(stream, "out[0] out[1]", *out)
-        for t in out:
-            if t.dtype is not dtype or not t.is_contiguous() or t.shape != (n, Hkv, hd):
-                _refuse("out must be two contiguous [n, Hkv, hd] tensors of dtype")
-    _check(lib.es_op_kv8_gather(slot_map.data_ptr(), n, k_pages.data_ptr(), v_pages.data_ptr(), _CODE_DTYPES[k_pages.dtype], k_scale.data_ptr(),
-                                v_scale.data_ptr(), Hkv, hd, P, n_pages, out[0].data_ptr(), out[1].data_ptr(), _VALUE_DTYPES[dtype], raw))
-    return out
+    return _call(stream, _native.kv8_gather, slot_map, k_pages, v_pages, k_scale, v_scale, _VALUE_DTYPES.get(dtype, -1), out)
 
 
 def es_op_decode_attention_kv8_scratch_bytes(B: int, T: int, Hq: int, Hkv: int, hd: int, page_tokens: int, max_ctx: int) -> int:
@@ -608,32 +494,7 @@ def es_op_decode_attention_kv8(q: torch.Tensor, k_pages: torch.Tensor, v_pages: 
                                scratch: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention of q [B, T, Hq, hd] (the T newest tokens of every sequence; [B, Hq, hd] for one) over the 8-bit pages;
     returns [B, T, Hq * hd] (or [B, Hq * hd]) of q's type.  q's tokens may be evenly spaced slices of larger rows."""
-    raw = _launch_on(stream, "q k_pages v_pages k_scale v_scale block_table ctx_len scratch out", q, k_pages, v_pages, k_scale, v_scale, block_table,
-                     ctx_len, scratch, out)
-    n_pages, Hkv, P, hd = _check_pool(k_pages, v_pages, k_scale, v_scale)
-    _ints("block_table ctx_len", block_table, ctx_len)
-    shape = q.shape
-    if len(shape) not in (3, 4) or shape[-1] != hd or q.dtype not in _VALUE_DTYPES or q.dtype is torch.float32:
-        _refuse("q must be fp16 or bf16 [B, T, Hq, hd] or [B, Hq, hd]")
-    B, Hq = shape[0], shape[-2]
-    T, result = (1, (B, Hq * hd)) if len(shape) == 3 else (shape[1], (B, shape[1], Hq * hd))
-    if block_table.dim() != 2 or block_table.shape[0] != B or ctx_len.shape != (B,):
-        _refuse("block_table must be [B, pages], ctx_len [B]")
-    stride = _row_stride(q, "q")
-    if scratch is None:
-        n = lib.es_op_decode_attention_kv8_scratch_bytes(B, T, Hq, Hkv, hd, P, max_ctx)
-        scratch = _empty(stream, n, torch.uint8, q) if n else None
-    elif not scratch.is_contiguous():
-        _refuse("scratch must be contiguous")
-    if out is None:
-        out = _empty(stream, result, q.dtype, q)
-    elif out.dtype is not q.dtype or not out.is_contiguous() or out.shape != result:
-        _refuse(f"out must be contiguous {result} of q's type")
-    _check(lib.es_op_decode_attention_kv8(q.data_ptr(), _VALUE_DTYPES[q.dtype], stride, k_pages.data_ptr(), v_pages.data_ptr(), _CODE_DTYPES[k_pages.dtype],
-                                          k_scale.data_ptr(), v_scale.data_ptr(), block_table.data_ptr(), ctx_len.data_ptr(), out.data_ptr(), B, T, Hq, Hkv,
-                                          hd, P, block_table.shape[1], n_pages, max_ctx, _ptr(scratch),
-                                          0 if scratch is None else scratch.numel() * scratch.element_size(), raw))
-    return out
+    return _call(stream, _native.decode_attention_kv8, q, k_pages, v_pages, k_scale, v_scale, block_table, ctx_len, max_ctx, scratch, out)
 
 
 def es_op_sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
@@ -641,29 +502,7 @@ def es_op_sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[to
                  out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(tokens int32 [B], logprobs fp32 [B]) drawn from logits [B, V] (fp32, fp16 or bf16; rows may be spaced) with the random
     numbers u [B] in [0, 1) and per-row settings [B]: temperature, top_p, min_p fp32, top_k int32; None = off."""
-    raw = _launch_on(stream, "logits u temperature top_k top_p min_p", logits, u, temperature, top_k, top_p, min_p)
-    shape = logits.shape
-    if len(shape) != 2 or logits.dtype not in _VALUE_DTYPES or (logits.stride(1) != 1 and shape[1] != 1):
-        _refuse("logits must be fp32, fp16 or bf16 [B, V] with dense rows")
-    B, V = shape
-    for t in (u, temperature, top_p, min_p):
-        if t is not None and not (t.dtype is torch.float32 and t.is_contiguous() and t.shape == (B,)):
-            _refuse("u, temperature, top_p and min_p must be contiguous fp32 [B]")
-    if top_k is not None and not (top_k.dtype is torch.int32 and top_k.is_contiguous() and top_k.shape == (B,)):
-        _refuse("top_k must be contiguous int32 [B]")
-    if out is None:
-        if B <= 0:
-            _refuse("bad sizes")
-        tokens, logprobs = _empty(stream, (2, B), torch.int32, logits).unbind()
-        out = (tokens, logprobs.view(torch.float32))
-    else:
-        _launch_on(stream, "out[0] out[1]", *out)
-        for t, want in zip(out, (torch.int32, torch.float32)):
-            if t.dtype is not want or not t.is_contiguous() or t.shape != (B,):
-                _refuse("out must be contiguous int32 [B] and fp32 [B]")
-    _check(lib.es_op_sample(logits.data_ptr(), _VALUE_DTYPES[logits.dtype], logits.stride(0) if B > 1 else V, u.data_ptr(), _ptr(temperature),
-                            _ptr(top_k), _ptr(top_p), _ptr(min_p), out[0].data_ptr(), out[1].data_ptr(), B, V, raw))
-    return out
+    return _call(stream, _native.sample, logits, u, temperature, top_k, top_p, min_p, out)
 
 
 def _partition(fn, t_comp, O, Req, Mem, Bw):

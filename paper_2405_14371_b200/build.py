@@ -1,4 +1,4 @@
-"""Builds libedgeshard.so in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
+"""Builds libedgeshard.so (nvcc, sm_100a, cross-compiles without a GPU) and _native_binding.so (g++) in-tree."""
 from __future__ import annotations
 
 import concurrent.futures
@@ -12,6 +12,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libedgeshard.so")
+NATIVE_SRC = os.path.join(HERE, "csrc_py", "native_binding.cpp")
+NATIVE = os.path.join(HERE, "_native_binding.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
@@ -58,8 +60,36 @@ def _compile(src: str, verbose: bool) -> str:
     return obj
 
 
+def _build_native(force: bool) -> None:
+    """The Python entry points of the per-layer calls, against the headers of the torch that is installed."""
+    import sysconfig
+
+    import torch
+
+    t = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(_nvcc())) if os.path.isabs(_nvcc()) else "/usr/local/cuda"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include"),
+           "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(t, "include"),
+           "-isystem", os.path.join(t, "include", "torch", "csrc", "api", "include"), "-isystem", os.path.join(cuda, "include"),
+           NATIVE_SRC, "-o", NATIVE, "-L", os.path.join(t, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python",
+           "-L", HERE, "-ledgeshard", "-Wl,-rpath,$ORIGIN"]
+    h = hashlib.sha256(" ".join(cmd + [torch.__version__]).encode())
+    for f in (NATIVE_SRC, os.path.join(ROOT, "include", "edgeshard.h")):
+        with open(f, "rb") as fh:
+            h.update(fh.read())
+    stamp_file = os.path.join(OBJ_DIR, "native_binding.stamp")
+    if not force and os.path.exists(NATIVE) and os.path.exists(stamp_file) and open(stamp_file).read() == h.hexdigest():
+        return
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{cmd[0]} failed for {NATIVE_SRC}:\n{r.stdout}\n{r.stderr}")
+    with open(stamp_file, "w") as f:
+        f.write(h.hexdigest())
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compiles every .cu under csrc/ and links libedgeshard.so; returns its path."""
+    """Compiles every .cu under csrc/, links libedgeshard.so and builds the Python entry points; returns the library's path."""
     os.makedirs(OBJ_DIR, exist_ok=True)
     if force:
         for f in os.listdir(OBJ_DIR):
@@ -74,6 +104,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
+    _build_native(force)
     return LIB
 
 

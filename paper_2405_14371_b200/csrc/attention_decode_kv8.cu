@@ -789,8 +789,8 @@ es_status_t launch_sub(const Kv8Maps& maps, const Kv8AttnParams& p, cudaStream_t
   constexpr int RINGS = AW * SLOTS<HD, NT, TILE> * TILE * HD + 1024; // and room to align them
   constexpr int INBOX = (MAX_GROUP - 1) * 8 * NT * HD * 4; // parts of the other CTAs of a group
   auto kern = kv8_attn_kernel<HD, CODE, NT, TILE, SUB, GROUPED>;
-  ES_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                     RINGS + (GROUPED ? INBOX : (KV8_MAX_B + 1) * (int)sizeof(int))));
+  static std::atomic<uint64_t> allowed{0};
+  ES_CUDA_CHECK(allow_shared_memory(kern, RINGS + (GROUPED ? INBOX : (KV8_MAX_B + 1) * (int)sizeof(int)), &allowed));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(GROUPED ? p.B * p.Hkv * p.row_tiles * p.group : sm_count());
   cfg.blockDim = dim3(AW * 32);

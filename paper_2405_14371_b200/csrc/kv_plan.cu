@@ -255,8 +255,9 @@ es_status_t es_op_kv_plan(const int32_t* old_len, const int32_t* new_len, int32_
   PlanParams p{old_len, new_len, block_table, free_pages, free_count, B, pages_per_seq, page_tokens, n_pages, max_rows,
                es_op_kv_plan_max_runs(B, max_rows, page_tokens), row_offsets, slot_map, positions, row_seq, runs, len_out};
   const size_t smem = (size_t)(6 * B + 4) * sizeof(int);
+  static std::atomic<uint64_t> allowed{0};
   if (smem > 48 * 1024)
-    ES_CUDA_CHECK(cudaFuncSetAttribute(kv_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)((6 * PLAN_MAX_B + 4) * sizeof(int))));
+    ES_CUDA_CHECK(allow_shared_memory(kv_plan_kernel, (int)((6 * PLAN_MAX_B + 4) * sizeof(int)), &allowed));
   const int ranks = max_rows <= 4096 ? 1 : 8;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ranks);

@@ -656,7 +656,8 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
 
 template <int DT>
 es_status_t launch_sample(const SampleParams& p, int B, int ranks, cudaStream_t s) {
-  ES_CUDA_CHECK(cudaFuncSetAttribute(sample_kernel<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sample_smem(MAX_SLICE)));
+  static std::atomic<uint64_t> allowed{0};
+  ES_CUDA_CHECK(allow_shared_memory(sample_kernel<DT>, (int)sample_smem(MAX_SLICE), &allowed));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((long long)B * ranks));
   cfg.blockDim = dim3(ST);
