@@ -35,6 +35,7 @@ constexpr int MAX_V = 262144;                 // 2^18 weights of 2^44 stay below
 constexpr int MAX_SLICE = MAX_V / MAX_CLUSTER;
 constexpr int NB = 1024;                      // bins of the histogram
 constexpr int LIST = 1024;                    // elements of a bin that are ranked directly
+constexpr int FEW = 256;                      // candidates that the first CTA finishes by itself
 constexpr double UNIT = 17592186044416.0;     // 2^44, the largest weight
 constexpr float REACH = 46.f;                 // weights further than this (log2) below the largest round to zero
 
@@ -57,14 +58,16 @@ struct Shared {
   int found;                                  // a chosen index, from the CTA that found it
   // from the first CTA
   int pick_bin, pick_count;                   // a bin, and how many elements it holds
+  u64 pick_up_to;                             // elements up to and including that bin
   u64 pick_target;                            // rank (counts) or mass to reach within the bin
   u64 pick_pair;                              // threshold found in the list
   // this CTA's own
   u64 all_mass;
   int list_n;
+  int few_n;                                  // first CTA: candidates that have arrived
+  int base;
   u64 warp_a[SW], warp_b[SW];
-  u64 hist[256], comb[256];                   // descent by key bits
-  int digit;
+  int digit;                                  // descent by key bits
   u64 digit_above, digit_here;
 };
 
@@ -117,15 +120,18 @@ __device__ __forceinline__ u64 share_of(float f, u64 all, bool* more) {
 __device__ __forceinline__ u64 pair_key(uint32_t key, int index) { return ((u64)key << 32) | (uint32_t)~index; }
 
 // One row's working state; every method is called by all threads of the cluster.
+template <int ranks>
 struct Row {
   float* x;                                   // slice in shared memory, padded with -infinity to a multiple of CHUNK
   u64* csum;                                  // [slice / CHUNK]
   uint32_t *cnt, *part;                       // [NB] counts, [3][NB] weights in three fields of 15 bits
+  uint4* inbox;                               // [ranks][NB / ranks] this CTA's share of the bins, from every CTA
   uint32_t* ccnt;                             // [NB] the cluster's counts   (first CTA)
   u64* cmass;                                 // [NB] ... and weights
-  u64 *list, *lweight;                        // [LIST] elements of a bin and, over `part`, their weights (first CTA)
+  u64 *list, *lweight;                        // [LIST] elements of a bin and their weights (first CTA)
+  u64 *mine, *dhist, *dcomb;                  // this CTA's elements of a bin; sums of a descent by key bits
   Shared* sm;
-  int n, first, ranks, rank;                  // padded elements, global index of the first, CTAs
+  int n, first, rank;                         // padded elements, global index of the first, this CTA
   float xmax, bin_scale;
   double c;                                   // log2(e) / temperature
   float cf;
@@ -169,6 +175,7 @@ struct Row {
     }
     cl.sync();
     u64 all = 0;
+#pragma unroll
     for (int r = 0; r < ranks; ++r) all += sm->total[r];
     return all;
   }
@@ -225,28 +232,28 @@ struct Row {
     uint32_t prefix = 0;
     u64 run = 0;
     for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = threadIdx.x; i < 256; i += ST) sm->hist[i] = 0;
+      for (int i = threadIdx.x; i < 256; i += ST) dhist[i] = 0;
       __syncthreads();
       for (int i = threadIdx.x; i < n; i += ST) {
         const float v = x[i];
         const uint32_t k = key_of(v);
         if (shift == 24 || (k >> (shift + 8)) == prefix) {
           const u64 w = f(v, first + i);
-          if (w) atomicAdd(&sm->hist[(k >> shift) & 255], w);
+          if (w) atomicAdd(&dhist[(k >> shift) & 255], w);
         }
       }
       cl.sync();
       for (int i = threadIdx.x; i < 256; i += ST) {
         u64 s = 0;
-        for (int r = 0; r < ranks; ++r) s += cl.map_shared_rank(sm, r)->hist[i];
-        sm->comb[i] = s;
+        for (int r = 0; r < ranks; ++r) s += cl.map_shared_rank(dhist, r)[i];
+        dcomb[i] = s;
       }
       cl.sync();
       if (threadIdx.x < 32) {                 // lane l holds bins 255 - 8 l down to 248 - 8 l
         const int lane = threadIdx.x;
         u64 v[8], s = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) { v[j] = sm->comb[255 - 8 * lane - j]; s += v[j]; }
+        for (int j = 0; j < 8; ++j) { v[j] = dcomb[255 - 8 * lane - j]; s += v[j]; }
         const u64 inc = run + warp_scan(s);
         const unsigned hit = __ballot_sync(~0u, inc >= target);
         if (hit && lane == __ffs(hit) - 1) {
@@ -292,29 +299,34 @@ struct Row {
           }
       }
     }
-    cl.sync();
-    // each CTA adds up its share of the bins, all copies of a bin under way at a time
+    __syncthreads();
+    // every CTA hands the bins out, each share to the CTA that adds it up; the sums go to the first CTA
+    constexpr int share = NB / ranks;
+    if (ranks > 1) {
+      for (int b = threadIdx.x; b < NB; b += ST) {
+        uint4* to = cl.map_shared_rank(inbox, b / share) + rank * share + b % share;
+        *to = mass ? make_uint4(cnt[b], part[b], part[NB + b], part[2 * NB + b]) : make_uint4(cnt[b], 0, 0, 0);
+      }
+      cl.sync();
+    }
     uint32_t* to_cnt = cl.map_shared_rank(ccnt, 0);
     u64* to_mass = cl.map_shared_rank(cmass, 0);
-    const int share = NB / ranks;
     for (int i = threadIdx.x; i < share; i += ST) {
-      const int b = rank * share + i;
-      uint32_t c[MAX_CLUSTER], m[MAX_CLUSTER][3];
-#pragma unroll
-      for (int r = 0; r < MAX_CLUSTER; ++r) {
-        c[r] = m[r][0] = m[r][1] = m[r][2] = 0;
-        if (r < ranks) {
-          const uint32_t* from = cl.map_shared_rank(cnt, r);
-          c[r] = from[b];
-          if (mass) { m[r][0] = from[NB + b]; m[r][1] = from[2 * NB + b]; m[r][2] = from[3 * NB + b]; }
-        }
-      }
       uint32_t k = 0;
       u64 w = 0;
+      if (ranks == 1) {
+        k = cnt[i];
+        if (mass) w = part[i] + ((u64)part[NB + i] << 15) + ((u64)part[2 * NB + i] << 30);
+      } else {
 #pragma unroll
-      for (int r = 0; r < MAX_CLUSTER; ++r) { k += c[r]; w += m[r][0] + ((u64)m[r][1] << 15) + ((u64)m[r][2] << 30); }
-      to_cnt[b] = k;
-      if (mass) to_mass[b] = w;
+        for (int r = 0; r < ranks; ++r) {
+          const uint4 v = inbox[r * share + i];
+          k += v.x;
+          w += v.y + ((u64)v.z << 15) + ((u64)v.w << 30);
+        }
+      }
+      to_cnt[rank * share + i] = k;
+      if (mass) to_mass[rank * share + i] = w;
     }
     cl.sync();
   }
@@ -332,11 +344,12 @@ struct Row {
     __syncthreads();
   }
 
-  __device__ __forceinline__ void publish(int bin, int count, u64 target) {                 // by one thread
+  __device__ __forceinline__ void publish(int bin, int count, u64 target, u64 up_to) {      // by one thread
     cg::cluster_group cl = cg::this_cluster();
+#pragma unroll
     for (int i = 0; i < ranks; ++i) {
       Shared* to = cl.map_shared_rank(sm, i);
-      to->pick_bin = bin; to->pick_count = count; to->pick_target = target;
+      to->pick_bin = bin; to->pick_count = count; to->pick_target = target; to->pick_up_to = up_to;
     }
   }
   __device__ __forceinline__ void publish_pair(u64 pair) {
@@ -344,25 +357,89 @@ struct Row {
     for (int i = 0; i < ranks; ++i) cl.map_shared_rank(sm, i)->pick_pair = pair;
   }
 
-  // The elements of bin `pick_bin` go to the first CTA's list, each CTA's behind those of the CTAs before it.
-  __device__ void collect() {
+  // The elements whose bin lies in [lo, hi] (at most LIST in all) go to the first CTA's list: each CTA gathers its own, then
+  // takes room for them there with one remote addition to `counter`.
+  __device__ void collect(int lo, int hi, int* counter) {
     cg::cluster_group cl = cg::this_cluster();
-    const int bin = sm->pick_bin, lane = threadIdx.x & 31;
-    const uint32_t c = lane < ranks ? cl.map_shared_rank(cnt, lane)[bin] : 0;
-    const int base = (int)__reduce_add_sync(~0u, lane < rank ? c : 0u);
     if (threadIdx.x == 0) sm->list_n = 0;
     __syncthreads();
-    if (cnt[bin]) {
-      u64* to = cl.map_shared_rank(list, 0) + base;
-      for (int i = threadIdx.x * 4; i < n; i += ST * 4) {
-        const float4 v4 = *reinterpret_cast<const float4*>(x + i);
-        const float v[4] = {v4.x, v4.y, v4.z, v4.w};
+    for (int i = threadIdx.x * 4; i < n; i += ST * 4) {
+      const float4 v4 = *reinterpret_cast<const float4*>(x + i);
+      const float v[4] = {v4.x, v4.y, v4.z, v4.w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (bin_of(v[j]) == bin) to[atomicAdd(&sm->list_n, 1)] = pair_key(key_of(v[j]), first + i + j);
+      for (int j = 0; j < 4; ++j) {
+        const int b = bin_of(v[j]);
+        if (b >= lo && b <= hi) mine[atomicAdd(&sm->list_n, 1)] = pair_key(key_of(v[j]), first + i + j);
       }
     }
+    __syncthreads();
+    const int m = sm->list_n;
+    if (m > 0) {                              // uniform over the CTA
+      if (threadIdx.x == 0) sm->base = atomicAdd(cl.map_shared_rank(counter, 0), m);
+      __syncthreads();
+      u64* to = cl.map_shared_rank(list, 0) + sm->base;
+      for (int i = threadIdx.x; i < m; i += ST) to[i] = mine[i];
+    }
     cl.sync();
+  }
+
+  __device__ __forceinline__ u64 block_sum(u64 v) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    v = warp_sum(v);
+    if (lane == 0) sm->warp_a[warp] = v;
+    __syncthreads();
+    const u64 all = warp_sum(lane < SW ? sm->warp_a[lane] : 0);
+    __syncthreads();
+    return all;
+  }
+
+  // First CTA, all m <= FEW candidates in the list: thresholds and draw, every element against every other.
+  // `whole`: the mass that top_p is a share of, or 0: that of the top_k first.
+  __device__ void finish_few(int m, u64 top_k, bool by_mass, float top_p, u64 whole, float u, int* token, float* logprob) {
+    int q = 2;                                // threads of an element
+    while (q < 16 && m * q * 2 <= ST) q *= 2;
+    const int e = threadIdx.x / q, part_of = threadIdx.x & (q - 1);
+    if (threadIdx.x < m) lweight[threadIdx.x] = weight(of_key((uint32_t)(list[threadIdx.x] >> 32)));
+    __syncthreads();
+    const u64 pair = e < m ? list[e] : 0, w = e < m ? lweight[e] : 0;
+    u64 above = 0;                            // weight of what ranks before
+    int before = 0;
+#pragma unroll 4
+    for (int j = part_of; j < m; j += q)
+      if (list[j] > pair) { ++before; above += lweight[j]; }
+    for (int d = 1; d < q; d <<= 1) {
+      before += __shfl_xor_sync(~0u, before, d);
+      above += __shfl_xor_sync(~0u, above, d);
+    }
+    const bool first_of = e < m && part_of == 0;
+    bool keep = e < m && (u64)before < top_k;
+    if (by_mass) {
+      const u64 all = whole ? whole : block_sum(first_of && keep ? w : 0);
+      bool more;
+      u64 target = share_of(fmaxf(top_p, 0.f), all, &more);
+      target += more;
+      keep = keep && (above < target || before == 0);
+    }
+    keep = keep && w >= least;
+    const u64 all = block_sum(first_of && keep ? w : 0);
+    u64* kept_weight = lweight;
+    __syncthreads();
+    if (first_of) kept_weight[e] = keep ? w : 0;
+    __syncthreads();
+    bool more;
+    u64 target = u < 1.f ? share_of(u, all, &more) : all;
+    if (target >= all) target = all - 1;
+    u64 run = 0;                              // weight up to and including this index: the low word orders downwards
+#pragma unroll 4
+    for (int j = part_of; j < m; j += q)
+      if ((uint32_t)list[j] >= (uint32_t)pair) run += kept_weight[j];
+    for (int d = 1; d < q; d <<= 1) run += __shfl_xor_sync(~0u, run, d);
+    if (first_of && keep && run > target && run - w <= target) {
+      *token = (int)~(uint32_t)pair;
+      const float v = of_key((uint32_t)(pair >> 32));
+      const double t = v == xmax ? 0.0 : ((double)v - (double)xmax) * c;
+      if (logprob) *logprob = (float)((t - log2((double)all) + 44.0) * 0.6931471805599453);
+    }
   }
 
   // First CTA, list of m elements: the one at which, in ranking order, the running count (or, by_mass, weight) reaches
@@ -429,7 +506,7 @@ struct Row {
   }
 };
 
-static_assert(SW == 16 && LIST == 2 * ST && NB == 2 * ST && LIST * 8 <= 3 * NB * 4, "scan2, choose and the bins of a thread");
+static_assert(SW == 16 && LIST == 2 * ST && NB == 2 * ST && 2 * LIST * 8 <= NB * 16, "scan2, choose and the bins of a thread");
 
 template <int DT>
 __device__ __forceinline__ float load_logit(const void* p, int64_t i) {
@@ -441,29 +518,36 @@ __device__ __forceinline__ float load_logit(const void* p, int64_t i) {
 }
 
 __host__ __device__ constexpr size_t sample_smem(int slice) {
-  // logits, chunk sums, the CTA's histogram, the cluster's weights and counts, the list
-  return (size_t)slice * 4 + (size_t)(slice / CHUNK) * 8 + (size_t)NB * (16 + 8 + 4) + (size_t)LIST * 8;
+  return (size_t)slice * 4 + (size_t)(slice / CHUNK) * 8 + (size_t)NB * (16 + 16 + 8 + 4);
 }
 
-template <int DT>
+template <int DT, int ranks>
 __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
   extern __shared__ __align__(16) unsigned char dyn[];
   __shared__ Shared shared;
   cg::cluster_group cl = cg::this_cluster();
   cluster_arrive();                           // "this CTA runs": nobody writes into it before
-  const int ranks = (int)cl.num_blocks(), rank = (int)cl.block_rank(), row = blockIdx.x / ranks;
+  const int rank = (int)cl.block_rank(), row = blockIdx.x / ranks;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  Row R;
+  // the row's settings, wanted after the logits: their latencies pass together
+  const float T = p.temperature ? p.temperature[row] : 1.f, tp = p.top_p ? p.top_p[row] : 1.f;
+  const float mp = p.min_p ? fminf(fmaxf(p.min_p[row], 0.f), 1.f) : 0.f, u = fminf(fmaxf(p.u[row], 0.f), 1.f);
+  const int k = p.top_k ? p.top_k[row] : 0;
+  Row<ranks> R;
   R.x = reinterpret_cast<float*>(dyn);
+  // [slice] logits | [4][NB] the CTA's histogram, later its own elements of a bin and the list's weights, or the sums of a
+  // descent | [NB] uint4 inbox of the histograms, later the list | the cluster's weights and counts | chunk sums
   R.cnt = reinterpret_cast<uint32_t*>(dyn + (size_t)p.slice * 4);
   R.part = R.cnt + NB;
-  R.cmass = reinterpret_cast<u64*>(R.part + 3 * NB);
-  R.list = R.cmass + NB;
-  R.lweight = reinterpret_cast<u64*>(R.part);  // read by nobody once the cluster's sums are made
-  R.csum = R.list + LIST;
+  R.mine = R.dhist = reinterpret_cast<u64*>(R.cnt);
+  R.dcomb = R.dhist + 256;
+  R.lweight = R.mine + LIST;
+  R.inbox = reinterpret_cast<uint4*>(R.part + 3 * NB);
+  R.list = reinterpret_cast<u64*>(R.inbox);
+  R.cmass = reinterpret_cast<u64*>(R.inbox + NB);
+  R.csum = R.cmass + NB;
   R.ccnt = reinterpret_cast<uint32_t*>(R.csum + p.slice / CHUNK);
   R.sm = &shared;
-  R.ranks = ranks;
   R.rank = rank;
   R.first = rank * p.slice;
   const int real = max(0, min(p.V - R.first, p.slice));
@@ -515,11 +599,12 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
       to->best[rank] = best;
       to->least[rank] = least;
     }
-    if (lane == 0) { shared.pick_bin = 0; shared.pick_count = 0; shared.pick_target = 1; shared.pick_pair = 0; }
+    if (lane == 0) { shared.few_n = 0; shared.pick_bin = 0; shared.pick_count = 0; shared.pick_target = 1; shared.pick_pair = 0; }
   }
   cl.sync();
   best = 0;
   least = INFINITY;
+#pragma unroll
   for (int r = 0; r < ranks; ++r) {
     best = shared.best[r] > best ? shared.best[r] : best;
     least = fminf(least, shared.least[r]);
@@ -527,7 +612,6 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
 
   R.xmax = of_key((uint32_t)(best >> 32));
   const int top = (int)~(uint32_t)best;
-  const float T = p.temperature ? p.temperature[row] : 1.f;
   if (R.xmax == -INFINITY || !(T > 0.f)) {    // nothing to draw from, or no drawing
     if (rank == 0 && tid == 0) {
       p.tokens[row] = R.xmax == -INFINITY ? -1 : top;
@@ -538,14 +622,18 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
   R.c = 1.4426950408889634 / (double)T;
   R.cf = (float)R.c;
   R.keep = 0;
-  R.least = 1;
-  const int k = p.top_k ? p.top_k[row] : 0;
-  const float tp = p.top_p ? p.top_p[row] : 1.f;
+  {
+    const u64 w = (u64)ceil((double)mp * UNIT);
+    R.least = w < 1 ? 1 : w;
+  }
   const bool by_count = k > 0 && k < p.V, by_mass = tp < 1.f;
   if (by_count || by_mass) {
     const float span = fminf(R.xmax - least, REACH / R.cf);
     R.bin_scale = span > 0.f ? fminf((NB - 1) / span, 1e37f) : 0.f;
-    R.histogram(by_mass);
+    // weights are left out of the histogram where the count alone is likely to leave few candidates; if it does not, a
+    // second one makes up for it
+    const bool count_first = by_count && by_mass && k <= FEW;
+    R.histogram(by_mass && !count_first);
     // first CTA: inclusive sums up to this thread's second bin (bins 2 tid and 2 tid + 1)
     u64 counts = 0, masses = 0, m0 = 0, m1 = 0;
     uint32_t c0 = 0, c1 = 0;
@@ -556,35 +644,54 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
       target += more;
       target = target < 1 ? 1 : target > all ? all : target;
       const u64 a = masses - m0 - m1, b = masses - m1;
-      if (a < target && target <= b) R.publish(2 * tid, (int)c0, target - a);
-      if (b < target && target <= masses) R.publish(2 * tid + 1, (int)c1, target - b);
+      if (a < target && target <= b) R.publish(2 * tid, (int)c0, target - a, counts - c1);
+      if (b < target && target <= masses) R.publish(2 * tid + 1, (int)c1, target - b, counts);
     };
     if (rank == 0) {
       c0 = R.ccnt[2 * tid]; c1 = R.ccnt[2 * tid + 1];
       counts = (u64)c0 + c1;
-      if (by_mass) { m0 = R.cmass[2 * tid]; m1 = R.cmass[2 * tid + 1]; masses = m0 + m1; }
+      if (by_mass && !count_first) { m0 = R.cmass[2 * tid]; m1 = R.cmass[2 * tid + 1]; masses = m0 + m1; }
       R.scan2(counts, masses);
+      if (tid == ST - 1) shared.all_mass = masses;
+      __syncthreads();
       if (by_count) {
         const u64 a = counts - c0 - c1, b = counts - c1;
-        if (a < (u64)k && (u64)k <= b) { R.publish(2 * tid, (int)c0, k - a); shared.all_mass = masses - m0 - m1; }
-        if (b < (u64)k && (u64)k <= counts) { R.publish(2 * tid + 1, (int)c1, k - b); shared.all_mass = masses - m1; }
+        if (a < (u64)k && (u64)k <= b) { R.publish(2 * tid, (int)c0, k - a, b); shared.all_mass = masses - m0 - m1; }
+        if (b < (u64)k && (u64)k <= counts) { R.publish(2 * tid + 1, (int)c1, k - b, counts); shared.all_mass = masses - m1; }
       } else {
-        if (tid == ST - 1) shared.all_mass = masses;
-        __syncthreads();
         pick_mass();
       }
     }
     cl.sync();
+    if (shared.pick_up_to <= FEW) {           // the other CTAs hand over their candidates and are done
+      const int m = (int)shared.pick_up_to, last_bin = shared.pick_bin;
+      R.collect(0, last_bin, &shared.few_n);
+      if (rank == 0) R.finish_few(m, by_count ? (u64)k : ~0ull, by_mass, tp, by_count ? 0 : shared.all_mass, u, p.tokens + row, p.logprobs ? p.logprobs + row : nullptr);
+      return;
+    }
+    if (count_first) {
+      const int bin = shared.pick_bin;
+      R.histogram(true);
+      if (rank == 0) {
+        m0 = R.cmass[2 * tid]; m1 = R.cmass[2 * tid + 1];
+        masses = m0 + m1;
+        u64 nothing = 0;
+        R.scan2(masses, nothing);
+        if (tid == bin / 2) shared.all_mass = masses - m1 - (bin & 1 ? 0 : m0);
+        __syncthreads();
+      }
+    }
     int listed = -1;                          // the bin that the list holds
     if (by_count) {
       const u64 want = shared.pick_target;
       const int bin = shared.pick_bin, m = shared.pick_count;
       if (m <= LIST) {
         listed = bin;
-        R.collect();
+        R.collect(bin, bin, &shared.few_n);
         if (rank == 0) {                      // the mass of the bin's kept elements joins that of the bins before
           R.choose(m, false, by_mass, want, [&](u64 pair, u64 mass) { R.publish_pair(pair); shared.all_mass += mass; });
           if (by_mass) pick_mass();
+          if (tid == 0) shared.few_n = 0;
         }
         cl.sync();
         R.keep = shared.pick_pair;
@@ -613,7 +720,7 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
       const u64 target = shared.pick_target;
       const int bin = shared.pick_bin, m = shared.pick_count;
       if (m <= LIST) {
-        if (listed != bin) R.collect();
+        if (listed != bin) R.collect(bin, bin, &shared.few_n);
         if (rank == 0) R.choose(m, true, true, target, [&](u64 pair, u64) { R.publish_pair(pair); });
         cl.sync();
         R.keep = shared.pick_pair > R.keep ? shared.pick_pair : R.keep;
@@ -633,15 +740,9 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
       }
     }
   }
-  if (p.min_p) {
-    const float m = fminf(fmaxf(p.min_p[row], 0.f), 1.f);
-    const u64 w = (u64)ceil((double)m * UNIT);
-    R.least = w < 1 ? 1 : w;
-  }
   auto last = [&](float v, int i) { const u64 w = R.kept(v, i) ? R.weight(v) : 0ull; return w >= R.least ? w : 0ull; };
   const u64 all = R.sums(last);
   if (warp > 0) return;                       // nothing is read from another CTA any more
-  const float u = fminf(fmaxf(p.u[row], 0.f), 1.f);
   bool more;
   u64 target = u < 1.f ? share_of(u, all, &more) : all;
   if (target >= all) target = all - 1;
@@ -654,12 +755,12 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
   }
 }
 
-template <int DT>
-es_status_t launch_sample(const SampleParams& p, int B, int ranks, cudaStream_t s) {
+template <int DT, int ranks>
+es_status_t launch_ranks(const SampleParams& p, int B, cudaStream_t s) {
   static std::atomic<uint64_t> allowed{0};
-  ES_CUDA_CHECK(allow_shared_memory(sample_kernel<DT>, (int)sample_smem(MAX_SLICE), &allowed));
+  ES_CUDA_CHECK(allow_shared_memory(sample_kernel<DT, ranks>, (int)sample_smem(MAX_SLICE), &allowed));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((long long)B * ranks));
+  cfg.gridDim = dim3((unsigned)(B * ranks));
   cfg.blockDim = dim3(ST);
   cfg.dynamicSmemBytes = sample_smem(p.slice);
   cfg.stream = s;
@@ -669,8 +770,18 @@ es_status_t launch_sample(const SampleParams& p, int B, int ranks, cudaStream_t 
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  ES_CUDA_CHECK(cudaLaunchKernelEx(&cfg, sample_kernel<DT>, p));
+  ES_CUDA_CHECK(cudaLaunchKernelEx(&cfg, sample_kernel<DT, ranks>, p));
   return ES_OK;
+}
+
+template <int DT>
+es_status_t launch_sample(const SampleParams& p, int B, int ranks, cudaStream_t s) {
+  switch (ranks) {
+    case 1: return launch_ranks<DT, 1>(p, B, s);
+    case 2: return launch_ranks<DT, 2>(p, B, s);
+    case 4: return launch_ranks<DT, 4>(p, B, s);
+    default: return launch_ranks<DT, 8>(p, B, s);
+  }
 }
 
 }  // namespace
