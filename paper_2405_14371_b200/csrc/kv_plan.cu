@@ -10,9 +10,9 @@
 // is written, and otherwise no stack entry is read, so pops and pushes need no order between them.
 //
 // One cluster does it all: every CTA scans the lengths for itself (a few KB out of L2, cheaper than handing sums around),
-// then the CTAs share the page work, meet once, and share the rows.  The meeting orders table writes before the rows
-// that read them, and the reads of returned entries before their clearing.  Small calls are bound by latency and run as
-// one CTA without remote barriers.
+// then the CTAs share the page work, meet once, and share the rest.  The meeting orders table writes before the rows that
+// read them, and the reads of returned entries before their clearing.  Small calls are bound by latency and run as one CTA
+// that makes the rows too; large ones leave the rows (12 bytes each) to a second kernel over the whole machine.
 #include <cooperative_groups.h>
 #include <limits.h>
 
@@ -102,7 +102,15 @@ __device__ __forceinline__ int owner(const int* off, int B, int i) {
 
 __device__ __forceinline__ int clip(long long v, int most) { return v < most ? (int)v : most; }
 
+// slot of a position, -1 where the table holds no page
+__device__ __forceinline__ int slot_of(const PlanParams& p, int seq, int pos) {
+  const int lp = pos / p.P, page = __ldcg(p.table + (int64_t)seq * p.pps + lp);
+  return page >= 0 && page < p.n_pages ? page * p.P + (pos - lp * p.P) : -1;
+}
+
+template <bool ROWS>
 __global__ void __launch_bounds__(PLAN_THREADS, 1) kv_plan_kernel(const PlanParams p) {
+  pdl_launch_dependents();
   extern __shared__ int sm[];
   __shared__ Sums warp_sums[PLAN_WARPS];
   __shared__ int warp_ints[PLAN_WARPS];
@@ -206,19 +214,49 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) kv_plan_kernel(const PlanPara
   if (alloc && first == 0) *p.free_count = (int)min(avail - taken, (long long)p.n_pages);
   for (int b = first; b <= B; b += stride) p.row_offsets[b] = min(row_off[b], p.max_rows);
   for (int b = first; b < B; b += stride) p.len_out[b] = s_new[b];
-  for (int i = first; i < p.max_runs; i += stride)
-    if (i >= runs_before) p.runs[i] = -1;
-  for (int r = first; r < p.max_rows; r += stride) {
+  for (int i = first; i < p.max_runs; i += stride) {       // run i: a page of its request, from the row that begins it
+    int row = -1;
+    if (i < runs_before) {
+      const int b = owner(run_off, B, i), o = s_old[b], lp = o / P + (i - run_off[b]);
+      const int page = __ldcg(p.table + (int64_t)b * p.pps + lp);
+      if (page >= 0 && page < p.n_pages) row = row_off[b] + max(lp * P - o, 0);
+    }
+    p.runs[i] = row;
+  }
+  if (ROWS)
+    for (int r = first; r < p.max_rows; r += stride) {
+      int slot = -1, pos = -1, seq = -1;
+      if (r < rows_all) {
+        seq = owner(row_off, B, r);
+        const int o = s_old[seq];
+        pos = o + (r - row_off[seq]);
+        if (s_new[seq] > o) slot = slot_of(p, seq, pos);
+      }
+      p.slot_map[r] = slot;
+      p.positions[r] = pos;
+      p.row_seq[r] = seq;
+    }
+}
+
+// The rows of a large call.  A request was served exactly if its length became the new one; where it began follows.
+__global__ void __launch_bounds__(PLAN_THREADS, 1) kv_plan_rows_kernel(const PlanParams p) {
+  extern __shared__ int sm[];
+  int* row_off = sm;               // [B + 1]
+  const int B = p.B;
+  pdl_wait();
+  for (int b = threadIdx.x; b <= B; b += PLAN_THREADS) row_off[b] = __ldcg(p.row_offsets + b);
+  __syncthreads();
+  const int rows_all = row_off[B];
+  // neighbouring threads take neighbouring rows, four rounds under way at a time
+  for (int64_t base = (int64_t)blockIdx.x * PLAN_THREADS + threadIdx.x; base < p.max_rows; base += (int64_t)gridDim.x * PLAN_THREADS) {
+    const int r = (int)base;
     int slot = -1, pos = -1, seq = -1;
     if (r < rows_all) {
       seq = owner(row_off, B, r);
-      const int o = s_old[seq];
-      pos = o + (r - row_off[seq]);
-      if (s_new[seq] > o) {
-        const int lp = pos / P, page = __ldcg(p.table + (int64_t)seq * p.pps + lp);
-        if (page >= 0 && page < p.n_pages) slot = page * P + (pos - lp * P);
-        if (pos == o || pos == lp * P) p.runs[run_off[seq] + lp - o / P] = slot >= 0 ? r : -1;
-      }
+      const int held = __ldcg(p.len_out + seq), want = __ldcg(p.new_len + seq);
+      const bool served = held == want;
+      pos = served ? held - (row_off[seq + 1] - r) : held + (r - row_off[seq]);
+      if (served) slot = slot_of(p, seq, pos);
     }
     p.slot_map[r] = slot;
     p.positions[r] = pos;
@@ -255,10 +293,12 @@ es_status_t es_op_kv_plan(const int32_t* old_len, const int32_t* new_len, int32_
   PlanParams p{old_len, new_len, block_table, free_pages, free_count, B, pages_per_seq, page_tokens, n_pages, max_rows,
                es_op_kv_plan_max_runs(B, max_rows, page_tokens), row_offsets, slot_map, positions, row_seq, runs, len_out};
   const size_t smem = (size_t)(6 * B + 4) * sizeof(int);
-  static std::atomic<uint64_t> allowed{0};
-  if (smem > 48 * 1024)
-    ES_CUDA_CHECK(allow_shared_memory(kv_plan_kernel, (int)((6 * PLAN_MAX_B + 4) * sizeof(int)), &allowed));
-  const int ranks = max_rows <= 4096 ? 1 : 8;
+  // one CTA as long as it writes the rows in about the time that a second launch costs
+  const bool small = max_rows <= 4096;
+  auto kern = small ? kv_plan_kernel<true> : kv_plan_kernel<false>;
+  static std::atomic<uint64_t> allowed[2];
+  if (smem > 48 * 1024) ES_CUDA_CHECK(allow_shared_memory(kern, (int)((6 * PLAN_MAX_B + 4) * sizeof(int)), &allowed[small]));
+  const int ranks = small ? 1 : 8;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ranks);
   cfg.blockDim = dim3(PLAN_THREADS);
@@ -270,7 +310,13 @@ es_status_t es_op_kv_plan(const int32_t* old_len, const int32_t* new_len, int32_
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = ranks > 1 ? 1 : 0;
-  ES_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_plan_kernel, p));
+  ES_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kern, p));
+  if (!small) {
+    const int blocks = (int)((max_rows + (long long)PLAN_THREADS - 1) / PLAN_THREADS);
+    const int most = 2 * sm_count();
+    ES_CUDA_CHECK(launch_kernel(kv_plan_rows_kernel, dim3(blocks < most ? blocks : most), dim3(PLAN_THREADS), (size_t)(B + 1) * sizeof(int),
+                                (cudaStream_t)stream, true, p));
+  }
   return ES_OK;
 }
 

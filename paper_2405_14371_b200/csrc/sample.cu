@@ -369,16 +369,19 @@ struct Row {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int b = bin_of(v[j]);
-        if (b >= lo && b <= hi) mine[atomicAdd(&sm->list_n, 1)] = pair_key(key_of(v[j]), first + i + j);
+        if (b >= lo && b <= hi) {
+          const int at = atomicAdd(&sm->list_n, 1);
+          if (at < LIST) mine[at] = pair_key(key_of(v[j]), first + i + j);
+        }
       }
     }
     __syncthreads();
-    const int m = sm->list_n;
+    const int m = min(sm->list_n, LIST);
     if (m > 0) {                              // uniform over the CTA
       if (threadIdx.x == 0) sm->base = atomicAdd(cl.map_shared_rank(counter, 0), m);
       __syncthreads();
       u64* to = cl.map_shared_rank(list, 0) + sm->base;
-      for (int i = threadIdx.x; i < m; i += ST) to[i] = mine[i];
+      for (int i = threadIdx.x; i < m && sm->base + i < LIST; i += ST) to[i] = mine[i];
     }
     cl.sync();
   }

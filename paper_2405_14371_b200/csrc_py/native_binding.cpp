@@ -4,6 +4,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <ATen/core/LegacyTypeDispatch.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAFunctions.h>
@@ -358,6 +359,8 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
     return nullptr;
   }
   try {
+    // results are plain memory: views and allocations go past autograd
+    at::AutoDispatchBelowADInplaceOrView no_autograd;
     return F(args);
   } catch (const Refusal& r) {
     raise_refusal(r.status, r.message);
