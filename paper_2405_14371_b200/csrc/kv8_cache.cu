@@ -21,13 +21,23 @@ struct AppendParams {
   int n_rows, n_items;             // n_items: runs, or rows where there are none
   uint8_t *k_pages, *v_pages;
   float *k_scale, *v_scale;
-  int Hkv, P, n_pages;
+  int Hkv, P, log2P, n_pages;
 };
 
 template <bool BF16>
 __device__ __forceinline__ float2 to_float2(uint32_t w) {
   if (BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
   return __half22float2(bits_h2(w));
+}
+
+// larger magnitudes of two pairs; NaN wins
+template <bool BF16>
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+  if (BF16) {
+    const __nv_bfloat162 r = __hmax2_nan(__habs2(*reinterpret_cast<const __nv_bfloat162*>(&a)), __habs2(*reinterpret_cast<const __nv_bfloat162*>(&b)));
+    return *reinterpret_cast<const uint32_t*>(&r);
+  }
+  return h2_bits(__hmax2_nan(__habs2(bits_h2(a)), __habs2(bits_h2(b))));
 }
 
 // round(x / s) to nearest, ties to even, exactly: x * (1 / s) is within one of it, and the remainder x - q s is a
@@ -119,30 +129,32 @@ __device__ __forceinline__ void group_sync() {
 }
 
 template <int HD, int CODE, bool BF16, int WARPS>
-__global__ void __launch_bounds__(APPEND_THREADS) kv8_append_kernel(const AppendParams p) {
+__global__ void __launch_bounds__(APPEND_THREADS, 4) kv8_append_kernel(const AppendParams p) {
   constexpr int GROUP = 32 * WARPS;                // threads of an item
   constexpr int CPR = HD / 8;                      // 16-byte pieces of a row
-  constexpr int KEEP = 4;                          // pieces a thread holds in registers between the two uses
+  constexpr int KEEP = 8;                          // pieces a thread holds in registers between the two uses
   __shared__ uint32_t s_max[APPEND_THREADS / 32];
   __shared__ int s_len[APPEND_THREADS / 32];
   const int tid = threadIdx.x % GROUP, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t item = (int64_t)blockIdx.x * (APPEND_THREADS / GROUP) + threadIdx.x / GROUP;
   // heads change fastest: the groups of a CTA share rows of the slot map and read one row's heads side by side
-  const int h = (int)(item % p.Hkv);
-  const int64_t which = item / p.Hkv;
+  const unsigned item = blockIdx.x * (APPEND_THREADS / GROUP) + threadIdx.x / GROUP;
+  const int which = item / (unsigned)p.Hkv, h = item - which * p.Hkv;
   if (which >= p.n_items) return;                  // uniform over the group
-  const int r0 = p.runs ? p.runs[which] : (int)which;
+  const int r0 = p.runs ? p.runs[which] : which;
   if (r0 < 0 || r0 >= p.n_rows) return;
   const int slot = p.slots[r0];
   if (slot < 0 || slot >= p.n_pages * p.P) return;
-  const int page = slot / p.P, off = slot - page * p.P;
+  const int page = slot >> p.log2P, off = slot & (p.P - 1);
   if (!p.runs && r0 > 0 && off > 0 && p.slots[r0 - 1] == slot - 1) return;      // inside a stretch
 
   const uint16_t* src = (blockIdx.y ? p.v : p.k) + (int64_t)r0 * p.row_stride + (int64_t)h * HD;
   uint8_t* dst = (blockIdx.y ? p.v_pages : p.k_pages) + ((int64_t)page * p.Hkv + h) * ((int64_t)p.P * HD);
   float* scale = (blockIdx.y ? p.v_scale : p.k_scale) + (int64_t)page * p.Hkv + h;
   const float s_old = off > 0 ? *scale : 0.f;
-  auto piece = [&](int i) { return *reinterpret_cast<const uint4*>(src + (int64_t)(i / CPR) * p.row_stride + (i % CPR) * 8); };
+  // this thread's pieces: tid, tid + GROUP, ... of the stretch, row after row
+  const uint16_t* at = src + (int64_t)(tid / CPR) * p.row_stride + (tid % CPR) * 8;
+  const int64_t step = (int64_t)(GROUP / CPR) * p.row_stride;
+  auto piece = [&](int j) { return *reinterpret_cast<const uint4*>(at + j * step); };
 
   // ---- the first rows are on their way while the length of the stretch is found: the first row that does not follow on ----
   const int most = min(p.P - off, p.n_rows - r0);
@@ -150,7 +162,7 @@ __global__ void __launch_bounds__(APPEND_THREADS) kv8_append_kernel(const Append
 #pragma unroll
   for (int j = 0; j < KEEP; ++j) {
     keep[j] = make_uint4(0, 0, 0, 0);
-    if (tid + j * GROUP < most * CPR) keep[j] = piece(tid + j * GROUP);
+    if (tid + j * GROUP < most * CPR) keep[j] = piece(j);
   }
   int len = most;
   if (WARPS == 1) {
@@ -171,15 +183,14 @@ __global__ void __launch_bounds__(APPEND_THREADS) kv8_append_kernel(const Append
   const int pieces = len * CPR;
 
   // ---- largest magnitude ----
-  uint32_t mx = 0;                                 // two 16-bit magnitudes
-  auto take = [&](const uint4& x) {
-    mx = __vmaxu2(mx, __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
-  };
+  uint32_t pair = 0;                               // two magnitudes
+  auto take = [&](const uint4& x) { pair = larger<BF16>(larger<BF16>(larger<BF16>(pair, x.x), larger<BF16>(x.y, x.z)), x.w); };
 #pragma unroll
   for (int j = 0; j < KEEP; ++j)
     if (tid + j * GROUP < pieces) take(keep[j]);
-  for (int i = tid + KEEP * GROUP; i < pieces; i += GROUP) take(piece(i));
-  mx = max(mx & 0xffffu, mx >> 16);
+  for (int j = KEEP; tid + j * GROUP < pieces; ++j) take(piece(j));
+  // as integers the bits of magnitudes order like the numbers, infinities and NaN above all
+  uint32_t mx = max(pair & 0x7fffu, (pair >> 16) & 0x7fffu);
   mx = __reduce_max_sync(~0u, mx);
   if (WARPS > 1) {
     if (lane == 0) s_max[warp] = mx;
@@ -213,8 +224,8 @@ __global__ void __launch_bounds__(APPEND_THREADS) kv8_append_kernel(const Append
 #pragma unroll
   for (int j = 0; j < KEEP; ++j)
     if (tid + j * GROUP < pieces) to[tid + j * GROUP] = bad ? make_uint2(0, 0) : encode<CODE, BF16>(keep[j], s, inv);
-  for (int i = tid + KEEP * GROUP; i < pieces; i += GROUP) to[i] = bad ? make_uint2(0, 0) : encode<CODE, BF16>(piece(i), s, inv);
-  group_sync<WARPS>();                             // every thread has read the old scale
+  for (int j = KEEP; tid + j * GROUP < pieces; ++j) to[tid + j * GROUP] = bad ? make_uint2(0, 0) : encode<CODE, BF16>(piece(j), s, inv);
+  if (WARPS == 1) __syncwarp();                    // every thread has read the old scale (several warps have met since)
   if (tid == 0) *scale = s;
 }
 
@@ -228,11 +239,11 @@ es_status_t launch_append_warps(const AppendParams& p, cudaStream_t s) {
   return ES_OK;
 }
 
-// A warp per item where stretches are short on average (a decode step: one row each); else as many as give a thread four
+// A warp per item where stretches are short on average (a decode step: one row each); else as many as give a thread eight
 // 16-byte pieces of a whole page, up to eight.
 template <int HD, int CODE, bool BF16>
 es_status_t launch_append(const AppendParams& p, bool whole_pages, cudaStream_t s) {
-  const int warps = whole_pages ? p.P * (HD / 8) / 128 : 1;
+  const int warps = whole_pages ? p.P * (HD / 8) / 256 : 1;
   if (warps >= 8) return launch_append_warps<HD, CODE, BF16, 8>(p, s);
   if (warps >= 4) return launch_append_warps<HD, CODE, BF16, 4>(p, s);
   if (warps >= 2) return launch_append_warps<HD, CODE, BF16, 2>(p, s);
@@ -249,7 +260,7 @@ struct GatherParams {
   const float *k_scale, *v_scale;
   void *k, *v;
   int64_t n_items;                 // rows * Hkv * hd / 16
-  int Hkv, P, n_pages;
+  int Hkv, P, log2P, n_pages;
 };
 
 
@@ -293,15 +304,15 @@ __global__ void __launch_bounds__(GATHER_THREADS) kv8_gather_kernel(const Gather
   constexpr int PPR = HD / 16;
   const int64_t item = (int64_t)blockIdx.x * GATHER_THREADS + threadIdx.x;
   if (item >= p.n_items) return;
-  const int64_t rh = item / PPR;
-  const int part = (int)(item - rh * PPR);
-  const int64_t r = rh / p.Hkv;
+  const unsigned rh = (unsigned)(item / PPR);               // rows * heads fit 32 bits
+  const int part = (int)(item % PPR);
+  const unsigned r = rh / (unsigned)p.Hkv;
   const int h = (int)(rh - r * p.Hkv);
   const int slot = p.slots[r];
   uint4 a = make_uint4(0, 0, 0, 0), b = a;
   float sa = 0.f, sb = 0.f;
   if (slot >= 0 && slot < p.n_pages * p.P) {
-    const int page = slot / p.P, off = slot - page * p.P;
+    const int page = slot >> p.log2P, off = slot & (p.P - 1);
     const int64_t ph = (int64_t)page * p.Hkv + h;
     const int64_t at = (ph * p.P + off) * HD + part * 16;
     a = __ldcs(reinterpret_cast<const uint4*>(p.k_pages + at));
@@ -316,7 +327,7 @@ __global__ void __launch_bounds__(GATHER_THREADS) kv8_gather_kernel(const Gather
 template <int HD, int CODE>
 es_status_t launch_gather(const GatherParams& p, int out, cudaStream_t s) {
   const int64_t blocks = (p.n_items + GATHER_THREADS - 1) / GATHER_THREADS;
-  if (blocks > INT32_MAX) return fail(ES_ERR_RANGE, "too many rows for one launch");
+  if (blocks > INT32_MAX || p.n_items / (HD / 16) > UINT32_MAX) return fail(ES_ERR_RANGE, "too many rows for one launch");
   const dim3 grid((unsigned)blocks);
   switch (out) {
     case ES_DTYPE_F16: kv8_gather_kernel<HD, CODE, ES_DTYPE_F16><<<grid, GATHER_THREADS, 0, s>>>(p); break;
@@ -356,7 +367,8 @@ es_status_t es_op_kv8_append(const void* k, const void* v, int32_t dtype, int64_
   if (row_stride < (int64_t)Hkv * hd || row_stride % 8) return fail(ES_ERR_INVALID_ARG, "row_stride must be a multiple of 8, at least Hkv * hd");
   if (((uintptr_t)k | (uintptr_t)v | (uintptr_t)k_pages | (uintptr_t)v_pages) % 16) return fail(ES_ERR_INVALID_ARG, "rows and pages must be 16-byte aligned");
   AppendParams p{(const uint16_t*)k, (const uint16_t*)v, row_stride, slot_map, runs, n_rows, runs ? n_runs : n_rows,
-                 (uint8_t*)k_pages, (uint8_t*)v_pages, k_scale, v_scale, Hkv, page_tokens, n_pages};
+                 (uint8_t*)k_pages, (uint8_t*)v_pages, k_scale, v_scale, Hkv, page_tokens, 0, n_pages};
+  while ((1 << p.log2P) < page_tokens) ++p.log2P;
   const bool wide = runs ? n_rows >= 8 * (int64_t)n_runs : false;
   const bool bf16 = dtype == ES_DTYPE_BF16;
   cudaStream_t s = (cudaStream_t)stream;
@@ -381,7 +393,8 @@ es_status_t es_op_kv8_gather(const int32_t* slot_map, int32_t n_rows, const void
   if (!slot_map || !k_pages || !v_pages || !k_scale || !v_scale || !k || !v) return fail(ES_ERR_INVALID_ARG, "null argument");
   if (((uintptr_t)k | (uintptr_t)v | (uintptr_t)k_pages | (uintptr_t)v_pages) % 16) return fail(ES_ERR_INVALID_ARG, "rows and pages must be 16-byte aligned");
   GatherParams p{slot_map, (const uint8_t*)k_pages, (const uint8_t*)v_pages, k_scale, v_scale, k, v,
-                 (int64_t)n_rows * Hkv * (hd / 16), Hkv, page_tokens, n_pages};
+                 (int64_t)n_rows * Hkv * (hd / 16), Hkv, page_tokens, 0, n_pages};
+  while ((1 << p.log2P) < page_tokens) ++p.log2P;
   cudaStream_t s = (cudaStream_t)stream;
   if (hd == 128) return code == CODE_I8 ? launch_gather<128, CODE_I8>(p, dtype, s) : launch_gather<128, CODE_E4M3>(p, dtype, s);
   return code == CODE_I8 ? launch_gather<64, CODE_I8>(p, dtype, s) : launch_gather<64, CODE_E4M3>(p, dtype, s);
