@@ -259,31 +259,31 @@ struct GatherParams {
   const uint8_t *k_pages, *v_pages;
   const float *k_scale, *v_scale;
   void *k, *v;
-  int64_t n_items;                 // rows * Hkv * hd / 16
+  int64_t n_items;                 // rows * Hkv * hd / 8
   int Hkv, P, log2P, n_pages;
 };
 
 
-// 16 codes -> 16 values of the output type at dst + 16 * item
+// 8 codes -> 8 values of the output type at dst + 8 * item
 template <int CODE, int OUT>
-__device__ __forceinline__ void store_values(void* dst, int64_t item, const uint4& w, float s) {
-  const uint32_t in[4] = {w.x, w.y, w.z, w.w};
-  float f[16];
+__device__ __forceinline__ void store_values(void* dst, int64_t item, const uint2& w, float s) {
+  const uint32_t in[2] = {w.x, w.y};
+  float f[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 2; ++i) {
     uint32_t lo, hi;
     codes_to_h2<CODE>(in[i], lo, hi);
     const float2 a = __half22float2(bits_h2(lo)), b = __half22float2(bits_h2(hi));
     f[4 * i] = a.x * s; f[4 * i + 1] = a.y * s; f[4 * i + 2] = b.x * s; f[4 * i + 3] = b.y * s;
   }
   if (OUT == ES_DTYPE_F32) {
-    float4* o = reinterpret_cast<float4*>(dst) + item * 4;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+    float4* o = reinterpret_cast<float4*>(dst) + item * 2;
+    __stcs(o, make_float4(f[0], f[1], f[2], f[3]));
+    __stcs(o + 1, make_float4(f[4], f[5], f[6], f[7]));
   } else {
-    uint32_t r[8];
+    uint32_t r[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4; ++i) {
       if (OUT == ES_DTYPE_F16) {
         r[i] = h2_bits(__floats2half2_rn(f[2 * i], f[2 * i + 1]));
       } else {
@@ -291,43 +291,54 @@ __device__ __forceinline__ void store_values(void* dst, int64_t item, const uint
         r[i] = *reinterpret_cast<const uint32_t*>(&b);
       }
     }
-    uint4* o = reinterpret_cast<uint4*>(dst) + item * 2;
-    o[0] = make_uint4(r[0], r[1], r[2], r[3]);
-    o[1] = make_uint4(r[4], r[5], r[6], r[7]);
+    __stcs(reinterpret_cast<uint4*>(dst) + item, make_uint4(r[0], r[1], r[2], r[3]));
   }
 }
 
-// A thread takes 16 values of K and of V: 16-byte loads out of the pages (a row of a head is contiguous there), 32 bytes
-// out, neighbouring threads side by side in the output.
+// A thread takes 8 values of K and of V at ROUNDS places a block apart, all loads under way together: 8 bytes in, 16 out,
+// neighbouring threads side by side in the output and, within a row of a head, in the page.
 template <int HD, int CODE, int OUT>
 __global__ void __launch_bounds__(GATHER_THREADS) kv8_gather_kernel(const GatherParams p) {
-  constexpr int PPR = HD / 16;
-  const int64_t item = (int64_t)blockIdx.x * GATHER_THREADS + threadIdx.x;
-  if (item >= p.n_items) return;
-  const unsigned rh = (unsigned)(item / PPR);               // rows * heads fit 32 bits
-  const int part = (int)(item % PPR);
-  const unsigned r = rh / (unsigned)p.Hkv;
-  const int h = (int)(rh - r * p.Hkv);
-  const int slot = p.slots[r];
-  uint4 a = make_uint4(0, 0, 0, 0), b = a;
-  float sa = 0.f, sb = 0.f;
-  if (slot >= 0 && slot < p.n_pages * p.P) {
-    const int page = slot >> p.log2P, off = slot & (p.P - 1);
-    const int64_t ph = (int64_t)page * p.Hkv + h;
-    const int64_t at = (ph * p.P + off) * HD + part * 16;
-    a = __ldcs(reinterpret_cast<const uint4*>(p.k_pages + at));
-    b = __ldcs(reinterpret_cast<const uint4*>(p.v_pages + at));
-    sa = p.k_scale[ph];
-    sb = p.v_scale[ph];
+  constexpr int PPR = HD / 8, ROUNDS = 2;
+  uint2 a[ROUNDS], b[ROUNDS];
+  float sa[ROUNDS], sb[ROUNDS];
+  int slot[ROUNDS];
+  const int64_t first = (int64_t)blockIdx.x * (ROUNDS * GATHER_THREADS) + threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < ROUNDS; ++i) {
+    const int64_t item = first + i * GATHER_THREADS;
+    slot[i] = item < p.n_items ? p.slots[(unsigned)(item / PPR) / (unsigned)p.Hkv] : -1;
   }
-  store_values<CODE, OUT>(p.k, item, a, sa);
-  store_values<CODE, OUT>(p.v, item, b, sb);
+#pragma unroll
+  for (int i = 0; i < ROUNDS; ++i) {
+    const int64_t item = first + i * GATHER_THREADS;
+    const unsigned rh = (unsigned)(item / PPR);             // rows * heads fit 32 bits
+    const int part = (int)(item % PPR), h = (int)(rh % (unsigned)p.Hkv);
+    a[i] = b[i] = make_uint2(0, 0);
+    sa[i] = sb[i] = 0.f;
+    if (slot[i] >= 0 && slot[i] < p.n_pages * p.P) {
+      const int page = slot[i] >> p.log2P, off = slot[i] & (p.P - 1);
+      const int64_t ph = (int64_t)page * p.Hkv + h;
+      const int64_t at = (ph * p.P + off) * HD + part * 8;
+      a[i] = __ldcs(reinterpret_cast<const uint2*>(p.k_pages + at));
+      b[i] = __ldcs(reinterpret_cast<const uint2*>(p.v_pages + at));
+      sa[i] = p.k_scale[ph];
+      sb[i] = p.v_scale[ph];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < ROUNDS; ++i) {
+    const int64_t item = first + i * GATHER_THREADS;
+    if (item >= p.n_items) break;
+    store_values<CODE, OUT>(p.k, item, a[i], sa[i]);
+    store_values<CODE, OUT>(p.v, item, b[i], sb[i]);
+  }
 }
 
 template <int HD, int CODE>
 es_status_t launch_gather(const GatherParams& p, int out, cudaStream_t s) {
-  const int64_t blocks = (p.n_items + GATHER_THREADS - 1) / GATHER_THREADS;
-  if (blocks > INT32_MAX || p.n_items / (HD / 16) > UINT32_MAX) return fail(ES_ERR_RANGE, "too many rows for one launch");
+  const int64_t blocks = (p.n_items + 2 * GATHER_THREADS - 1) / (2 * GATHER_THREADS);
+  if (blocks > INT32_MAX || p.n_items / (HD / 8) > UINT32_MAX) return fail(ES_ERR_RANGE, "too many rows for one launch");
   const dim3 grid((unsigned)blocks);
   switch (out) {
     case ES_DTYPE_F16: kv8_gather_kernel<HD, CODE, ES_DTYPE_F16><<<grid, GATHER_THREADS, 0, s>>>(p); break;
@@ -393,7 +404,7 @@ es_status_t es_op_kv8_gather(const int32_t* slot_map, int32_t n_rows, const void
   if (!slot_map || !k_pages || !v_pages || !k_scale || !v_scale || !k || !v) return fail(ES_ERR_INVALID_ARG, "null argument");
   if (((uintptr_t)k | (uintptr_t)v | (uintptr_t)k_pages | (uintptr_t)v_pages) % 16) return fail(ES_ERR_INVALID_ARG, "rows and pages must be 16-byte aligned");
   GatherParams p{slot_map, (const uint8_t*)k_pages, (const uint8_t*)v_pages, k_scale, v_scale, k, v,
-                 (int64_t)n_rows * Hkv * (hd / 16), Hkv, page_tokens, 0, n_pages};
+                 (int64_t)n_rows * Hkv * (hd / 8), Hkv, page_tokens, 0, n_pages};
   while ((1 << p.log2P) < page_tokens) ++p.log2P;
   cudaStream_t s = (cudaStream_t)stream;
   if (hd == 128) return code == CODE_I8 ? launch_gather<128, CODE_I8>(p, dtype, s) : launch_gather<128, CODE_E4M3>(p, dtype, s);

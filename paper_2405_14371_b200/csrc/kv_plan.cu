@@ -25,7 +25,7 @@ namespace es {
 namespace {
 
 constexpr int PLAN_THREADS = 1024;
-constexpr int PLAN_WARPS = PLAN_THREADS / 32;
+constexpr int PLAN_FEW = 128;      // threads of a call with few requests and rows: barriers and launch cost less
 constexpr int PLAN_MAX_B = 8192;
 
 struct PlanParams {
@@ -40,6 +40,7 @@ struct Sums { long long give, rows, need; };
 __device__ __forceinline__ Sums add(const Sums& a, const Sums& b) { return {a.give + b.give, a.rows + b.rows, a.need + b.need}; }
 
 // inclusive scan over the block; `total` is the block's sum.  All threads call.
+template <int WARPS>
 __device__ __forceinline__ Sums block_scan(Sums v, Sums* warp_sums, Sums* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
@@ -50,21 +51,22 @@ __device__ __forceinline__ Sums block_scan(Sums v, Sums* warp_sums, Sums* total)
   if (lane == 31) warp_sums[warp] = v;
   __syncthreads();
   if (warp == 0) {
-    Sums w = warp_sums[lane];
+    Sums w = lane < WARPS ? warp_sums[lane] : Sums{0, 0, 0};
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
       const Sums o = {__shfl_up_sync(~0u, w.give, d), __shfl_up_sync(~0u, w.rows, d), __shfl_up_sync(~0u, w.need, d)};
       if (lane >= d) w = add(w, o);
     }
-    warp_sums[lane] = w;
+    if (lane < WARPS) warp_sums[lane] = w;
   }
   __syncthreads();
   if (warp > 0) v = add(v, warp_sums[warp - 1]);
-  *total = warp_sums[PLAN_WARPS - 1];
+  *total = warp_sums[WARPS - 1];
   __syncthreads();
   return v;
 }
 
+template <int WARPS>
 __device__ __forceinline__ int block_scan_int(int v, int* warp_sums, int* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
@@ -75,17 +77,17 @@ __device__ __forceinline__ int block_scan_int(int v, int* warp_sums, int* total)
   if (lane == 31) warp_sums[warp] = v;
   __syncthreads();
   if (warp == 0) {
-    int w = warp_sums[lane];
+    int w = lane < WARPS ? warp_sums[lane] : 0;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
       const int o = __shfl_up_sync(~0u, w, d);
       if (lane >= d) w += o;
     }
-    warp_sums[lane] = w;
+    if (lane < WARPS) warp_sums[lane] = w;
   }
   __syncthreads();
   if (warp > 0) v += warp_sums[warp - 1];
-  *total = warp_sums[PLAN_WARPS - 1];
+  *total = warp_sums[WARPS - 1];
   __syncthreads();
   return v;
 }
@@ -108,12 +110,13 @@ __device__ __forceinline__ int slot_of(const PlanParams& p, int seq, int pos) {
   return page >= 0 && page < p.n_pages ? page * p.P + (pos - lp * p.P) : -1;
 }
 
-template <bool ROWS>
-__global__ void __launch_bounds__(PLAN_THREADS, 1) kv_plan_kernel(const PlanParams p) {
+template <bool ROWS, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1) kv_plan_kernel(const PlanParams p) {
   pdl_launch_dependents();
+  constexpr int WARPS = THREADS / 32;
   extern __shared__ int sm[];
-  __shared__ Sums warp_sums[PLAN_WARPS];
-  __shared__ int warp_ints[PLAN_WARPS];
+  __shared__ Sums warp_sums[WARPS];
+  __shared__ int warp_ints[WARPS];
   const int B = p.B, P = p.P, tid = threadIdx.x;
   int* s_old = sm;                 // [B]
   int* s_new = s_old + B;          // [B]   the length to hold: the request's, or the old one when refused
@@ -130,7 +133,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) kv_plan_kernel(const PlanPara
   if (alloc) { have = __ldcg(p.free_count); have = have < 0 ? 0 : min(have, p.n_pages); }
   Sums carry = {0, 0, 0};
   if (tid == 0) { row_off[0] = 0; need_off[0] = 0; give_off[0] = 0; run_off[0] = 0; }
-  for (int base = 0; base < B; base += PLAN_THREADS) {
+  for (int base = 0; base < B; base += THREADS) {
     const int b = base + tid;
     int o = 0, n = 0;
     if (b < B) { o = __ldcg(p.old_len + b); n = __ldcg(p.new_len + b); }
@@ -138,7 +141,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) kv_plan_kernel(const PlanPara
     const int oo = ok ? o : 0, nn = ok ? n : 0;
     const int po = (int)(((long long)oo + P - 1) / P), pn = (int)(((long long)nn + P - 1) / P);
     Sums v = {max(po - pn, 0), max(nn - oo, 0), max(pn - po, 0)}, total;
-    v = add(block_scan(v, warp_sums, &total), carry);
+    v = add(block_scan<WARPS>(v, warp_sums, &total), carry);
     if (b < B) {
       s_old[b] = o;
       s_new[b] = ok ? n : o;
@@ -154,7 +157,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) kv_plan_kernel(const PlanPara
 
   // ---- who is served; the runs of the served ----
   int runs_before = 0, taken = 0;
-  for (int base = 0; base < B; base += PLAN_THREADS) {
+  for (int base = 0; base < B; base += THREADS) {
     const int b = base + tid;
     int n_runs = 0;
     if (b < B) {
@@ -167,7 +170,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) kv_plan_kernel(const PlanPara
       }
     }
     int total;
-    n_runs = block_scan_int(n_runs, warp_ints, &total);
+    n_runs = block_scan_int<WARPS>(n_runs, warp_ints, &total);
     if (b < B) run_off[b + 1] = runs_before + n_runs;
     runs_before += total;
   }
@@ -176,15 +179,15 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) kv_plan_kernel(const PlanPara
   // (need sums beyond avail belong to refused requests; so do all needs behind the first row sum beyond max_rows)
   {
     int most = 0;
-    for (int b = tid; b < B; b += PLAN_THREADS)
+    for (int b = tid; b < B; b += THREADS)
       if (s_new[b] > s_old[b] && need_off[b + 1] > need_off[b]) most = max(most, need_off[b + 1]);
     most = __reduce_max_sync(~0u, most);
     if ((tid & 31) == 0) warp_ints[tid >> 5] = most;
     __syncthreads();
-    taken = alloc ? __reduce_max_sync(~0u, warp_ints[tid & 31]) : 0;
+    taken = alloc ? __reduce_max_sync(~0u, warp_ints[tid & (WARPS - 1)]) : 0;
   }
   const int rows_all = min(row_off[B], p.max_rows);
-  const int stride = PLAN_THREADS * ranks, first = rank * PLAN_THREADS + tid;
+  const int stride = THREADS * ranks, first = rank * THREADS + tid;
 
   // ---- pages: pops into the table, left-over returns onto the stack ----
   auto returned = [&](int i) -> int {
@@ -295,13 +298,14 @@ es_status_t es_op_kv_plan(const int32_t* old_len, const int32_t* new_len, int32_
   const size_t smem = (size_t)(6 * B + 4) * sizeof(int);
   // one CTA as long as it writes the rows in about the time that a second launch costs
   const bool small = max_rows <= 4096;
-  auto kern = small ? kv_plan_kernel<true> : kv_plan_kernel<false>;
+  const bool few = small && max_rows <= 4 * PLAN_FEW && B <= PLAN_FEW;
+  auto kern = few ? kv_plan_kernel<true, PLAN_FEW> : small ? kv_plan_kernel<true, PLAN_THREADS> : kv_plan_kernel<false, PLAN_THREADS>;
   static std::atomic<uint64_t> allowed[2];
   if (smem > 48 * 1024) ES_CUDA_CHECK(allow_shared_memory(kern, (int)((6 * PLAN_MAX_B + 4) * sizeof(int)), &allowed[small]));
   const int ranks = small ? 1 : 8;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ranks);
-  cfg.blockDim = dim3(PLAN_THREADS);
+  cfg.blockDim = dim3(few ? PLAN_FEW : PLAN_THREADS);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = (cudaStream_t)stream;
   cudaLaunchAttribute attr[1];

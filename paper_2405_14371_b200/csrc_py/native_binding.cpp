@@ -6,6 +6,7 @@
 
 #include <ATen/core/LegacyTypeDispatch.h>
 #include <ATen/core/Tensor.h>
+#include <ATen/ops/as_strided_native.h>
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
@@ -166,10 +167,10 @@ PyObject* kv_plan(PyObject* const* a) {
   at::Tensor out[6];
   if (a[8] == Py_None) {
     if (max_rows <= 0 || B <= 0) refuse("bad sizes");
-    int64_t all = 0, at = 0;
+    int64_t all = 0, begin = 0;
     for (int64_t s : sizes) all += s;
     const at::Tensor flat = empty({all}, at::kInt, old_len);
-    for (int i = 0; i < 6; ++i) { out[i] = flat.narrow(0, at, sizes[i]); at += sizes[i]; }
+    for (int i = 0; i < 6; ++i) { out[i] = at::native::as_strided_tensorimpl(flat, {sizes[i]}, {1}, begin); begin += sizes[i]; }
   } else {
     if (!PyTuple_Check(a[8]) || PyTuple_GET_SIZE(a[8]) != 6) refuse("out must be a KvPlan");
     for (int i = 0; i < 6; ++i) {
@@ -229,8 +230,8 @@ PyObject* kv8_gather(PyObject* const* a) {
   at::Tensor out[2];
   if (a[6] == Py_None) {
     const at::Tensor both = empty({2, n, p.Hkv, p.hd}, scalar_of(dtype), kp);
-    out[0] = both.select(0, 0);
-    out[1] = both.select(0, 1);
+    const int64_t head = p.hd, row = head * p.Hkv;
+    for (int i = 0; i < 2; ++i) out[i] = at::native::as_strided_tensorimpl(both, {n, p.Hkv, p.hd}, {row, head, 1}, i * n * row);
   } else {
     if (!PyTuple_Check(a[6]) || PyTuple_GET_SIZE(a[6]) != 2) refuse("out must be two tensors");
     for (int i = 0; i < 2; ++i) {
