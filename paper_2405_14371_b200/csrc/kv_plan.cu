@@ -92,15 +92,18 @@ __device__ __forceinline__ int block_scan_int(int v, int* warp_sums, int* total)
   return v;
 }
 
-// the request that owns item i: the b with off[b] <= i < off[b + 1]; off[0] = 0, i < off[B]
-__device__ __forceinline__ int owner(const int* off, int B, int i) {
-  int lo = 0, hi = B;            // off[lo] <= i < off[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (off[mid] <= i) lo = mid; else hi = mid;
+// The request that owns item i: the b with off[b] <= i < off[b + 1]; off[0] = 0, i < off[B].  A fixed number of steps
+// without branches, so that the searches of several items overlap; `top` is the largest power of two not above B.
+__device__ __forceinline__ int owner(const int* off, int B, int top, int i) {
+  int b = 0;
+  for (int step = top; step; step >>= 1) {
+    const int mid = b + step;
+    if (mid < B && off[mid] <= i) b = mid;
   }
-  return lo;
+  return b;
 }
+
+constexpr int FLIGHT = 4;          // items of a thread under way at a time
 
 __device__ __forceinline__ int clip(long long v, int most) { return v < most ? (int)v : most; }
 
@@ -124,6 +127,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_plan_kernel(const PlanParams p)
   int* need_off = row_off + B + 1; // [B + 1]   served requests only
   int* give_off = need_off + B + 1;
   int* run_off = give_off + B + 1;
+  const int top = 1 << (31 - __clz(B));
   const int ranks = gridDim.x, rank = blockIdx.x;
   const bool alloc = p.free_pages != nullptr;
   const long long cap = (long long)p.pps * P;
@@ -191,17 +195,26 @@ __global__ void __launch_bounds__(THREADS, 1) kv_plan_kernel(const PlanParams p)
 
   // ---- pages: pops into the table, left-over returns onto the stack ----
   auto returned = [&](int i) -> int {
-    const int b = owner(give_off, B, i);
+    const int b = owner(give_off, B, top, i);
     const int entry = (int)(((long long)s_new[b] + P - 1) / P) + i - give_off[b];
     return __ldcg(p.table + (int64_t)b * p.pps + entry);
   };
   if (alloc) {
-    for (int i = first; i < taken; i += stride) {
-      const long long v = avail - 1 - i;
-      const int page = v < have ? __ldcg(p.free_pages + v) : returned((int)(v - have));
-      const int b = owner(need_off, B, i);
-      const int entry = (int)(((long long)s_old[b] + P - 1) / P) + i - need_off[b];
-      p.table[(int64_t)b * p.pps + entry] = page;
+    for (int base = first; base < taken; base += FLIGHT * stride) {
+      int page[FLIGHT];
+#pragma unroll
+      for (int j = 0; j < FLIGHT; ++j) {
+        const int i = base + j * stride;
+        const long long v = avail - 1 - i;
+        page[j] = i >= taken ? -1 : v < have ? __ldcg(p.free_pages + v) : returned((int)(v - have));
+      }
+#pragma unroll
+      for (int j = 0; j < FLIGHT; ++j) {
+        const int i = base + j * stride;
+        if (i >= taken) break;
+        const int b = owner(need_off, B, top, i);
+        p.table[(int64_t)b * p.pps + (int)(((long long)s_old[b] + P - 1) / P) + i - need_off[b]] = page[j];
+      }
     }
     for (int i = first; i < given - taken; i += stride)
       if (have + (long long)i < p.n_pages) p.free_pages[have + i] = returned(i);
@@ -211,26 +224,33 @@ __global__ void __launch_bounds__(THREADS, 1) kv_plan_kernel(const PlanParams p)
   if (ranks > 1) cg::this_cluster().sync(); else __syncthreads();
 
   for (int i = first; i < given; i += stride) {
-    const int b = owner(give_off, B, i);
+    const int b = owner(give_off, B, top, i);
     p.table[(int64_t)b * p.pps + (int)(((long long)s_new[b] + P - 1) / P) + i - give_off[b]] = -1;
   }
   if (alloc && first == 0) *p.free_count = (int)min(avail - taken, (long long)p.n_pages);
   for (int b = first; b <= B; b += stride) p.row_offsets[b] = min(row_off[b], p.max_rows);
   for (int b = first; b < B; b += stride) p.len_out[b] = s_new[b];
-  for (int i = first; i < p.max_runs; i += stride) {       // run i: a page of its request, from the row that begins it
-    int row = -1;
-    if (i < runs_before) {
-      const int b = owner(run_off, B, i), o = s_old[b], lp = o / P + (i - run_off[b]);
-      const int page = __ldcg(p.table + (int64_t)b * p.pps + lp);
-      if (page >= 0 && page < p.n_pages) row = row_off[b] + max(lp * P - o, 0);
+  for (int base = first; base < p.max_runs; base += FLIGHT * stride) {            // run i: a page of its request, from the row that begins it
+    int row[FLIGHT], page[FLIGHT];
+#pragma unroll
+    for (int j = 0; j < FLIGHT; ++j) {
+      const int i = base + j * stride;
+      row[j] = page[j] = -1;
+      if (i < runs_before) {
+        const int b = owner(run_off, B, top, i), o = s_old[b], lp = o / P + (i - run_off[b]);
+        page[j] = __ldcg(p.table + (int64_t)b * p.pps + lp);
+        row[j] = row_off[b] + max(lp * P - o, 0);
+      }
     }
-    p.runs[i] = row;
+#pragma unroll
+    for (int j = 0; j < FLIGHT; ++j)
+      if (base + j * stride < p.max_runs) p.runs[base + j * stride] = page[j] >= 0 && page[j] < p.n_pages ? row[j] : -1;
   }
   if (ROWS)
     for (int r = first; r < p.max_rows; r += stride) {
       int slot = -1, pos = -1, seq = -1;
       if (r < rows_all) {
-        seq = owner(row_off, B, r);
+        seq = owner(row_off, B, top, r);
         const int o = s_old[seq];
         pos = o + (r - row_off[seq]);
         if (s_new[seq] > o) slot = slot_of(p, seq, pos);
@@ -245,7 +265,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_plan_kernel(const PlanParams p)
 __global__ void __launch_bounds__(PLAN_THREADS, 1) kv_plan_rows_kernel(const PlanParams p) {
   extern __shared__ int sm[];
   int* row_off = sm;               // [B + 1]
-  const int B = p.B;
+  const int B = p.B, top = 1 << (31 - __clz(B));
   pdl_wait();
   for (int b = threadIdx.x; b <= B; b += PLAN_THREADS) row_off[b] = __ldcg(p.row_offsets + b);
   __syncthreads();
@@ -255,7 +275,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) kv_plan_rows_kernel(const Pla
     const int r = (int)base;
     int slot = -1, pos = -1, seq = -1;
     if (r < rows_all) {
-      seq = owner(row_off, B, r);
+      seq = owner(row_off, B, top, r);
       const int held = __ldcg(p.len_out + seq), want = __ldcg(p.new_len + seq);
       const bool served = held == want;
       pos = served ? held - (row_off[seq + 1] - r) : held + (r - row_off[seq]);
