@@ -287,6 +287,35 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) kv_plan_rows_kernel(const Pla
   }
 }
 
+// CTAs of a large call's cluster: 16 where the device places such clusters (their shared work is bound by issue slots; a
+// call that returns 25 000 pages takes 20 us with 8), else the portable 8.
+int plan_cluster() {
+  static std::atomic<int> known[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 8;
+  int n = known[dev].load(std::memory_order_relaxed);
+  if (n) return n;
+  const auto kern = kv_plan_kernel<false, PLAN_THREADS>;
+  const size_t smem = (6 * PLAN_MAX_B + 4) * sizeof(int);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(16);
+  cfg.blockDim = dim3(PLAN_THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 16;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int fit = 0;
+  n = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+              cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) == cudaSuccess &&
+              cudaOccupancyMaxActiveClusters(&fit, kern, &cfg) == cudaSuccess && fit > 0 ? 16 : 8;
+  cudaGetLastError();                // a refusal of the size is an answer, not an error of this call
+  known[dev].store(n, std::memory_order_relaxed);
+  return n;
+}
+
 }  // namespace
 }  // namespace es
 
@@ -322,7 +351,7 @@ es_status_t es_op_kv_plan(const int32_t* old_len, const int32_t* new_len, int32_
   auto kern = few ? kv_plan_kernel<true, PLAN_FEW> : small ? kv_plan_kernel<true, PLAN_THREADS> : kv_plan_kernel<false, PLAN_THREADS>;
   static std::atomic<uint64_t> allowed[2];
   if (smem > 48 * 1024) ES_CUDA_CHECK(allow_shared_memory(kern, (int)((6 * PLAN_MAX_B + 4) * sizeof(int)), &allowed[small]));
-  const int ranks = small ? 1 : 8;
+  const int ranks = small ? 1 : plan_cluster();
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ranks);
   cfg.blockDim = dim3(few ? PLAN_FEW : PLAN_THREADS);
