@@ -70,9 +70,16 @@ class ShardPipeline:
     shards: binding.Shard objects covering consecutive layer ranges, the first holding the embedding.
     For the pipelined schedules each shard must have been created on its own stream.  Every
     micro-batch owns the KV slots `slots[mb]` in every shard.
+
+    sampling: None feeds the greedy tokens back.  Otherwise a dict of device tensors: "u" fp32
+    [iterations, micro_batches, batch], the random number of every token (row 0 = the prefill's), and
+    any of "temperature", "top_p", "min_p" (fp32) and "top_k" (int32), each [micro_batches, batch];
+    the tokens are then drawn by es_op_sample on the last shard's stream, and `logprobs`
+    [micro_batches, batch] holds their log probabilities.
     """
 
-    def __init__(self, shards: Sequence, slots: Sequence[Sequence[int]], batch: int, schedule: str = "no_bubbles"):
+    def __init__(self, shards: Sequence, slots: Sequence[Sequence[int]], batch: int, schedule: str = "no_bubbles",
+                 sampling: Optional[dict] = None):
         import torch
 
         if schedule not in SCHEDULES:
@@ -88,6 +95,17 @@ class ShardPipeline:
         self.has_head = self.shards[-1].layer_end == self.shards[-1].desc.n_layers_total
         dev = self.streams[0].device
         self.tokens = torch.zeros(len(self.slots), batch, dtype=torch.int32, device=dev)   # token fed to the first shard
+        self.logprobs = torch.zeros(len(self.slots), batch, dtype=torch.float32, device=dev)
+        self.sampling = sampling
+        if sampling is not None:
+            if not self.has_head:
+                raise ValueError("sampling needs a last shard with the LM head")
+            known = {"u", "temperature", "top_k", "top_p", "min_p"}
+            if "u" not in sampling or set(sampling) - known:
+                raise ValueError(f"sampling must hold 'u' and may hold {sorted(known - {'u'})}")
+            for name, t in sampling.items():
+                if tuple(t.shape[-2:]) != (len(self.slots), batch) or t.dim() != (3 if name == "u" else 2):
+                    raise ValueError(f"sampling[{name!r}] must be [{'iterations, ' if name == 'u' else ''}micro_batches, batch]")
         self.events = {}
         self.iteration = 0
         self.outputs = [None] * len(self.slots)        # (hidden, logits, next_ids) views of the last shard, per micro-batch
@@ -117,7 +135,9 @@ class ShardPipeline:
                                                self.slots[p.micro_batch])
                 if p.shard == n_sh - 1:
                     out = shard.es_shard_handoff()
-                    if self.has_head:
+                    if self.sampling is not None:
+                        self._draw(p, out[1])
+                    elif self.has_head:
                         self.tokens[p.micro_batch].copy_(out[2], non_blocking=True)      # greedy feedback stays on the device
                     self.outputs[p.micro_batch] = out
                     if on_output is not None:
@@ -131,6 +151,14 @@ class ShardPipeline:
         keep = self.iteration - 2
         self.events = {k: v for k, v in self.events.items() if k.iteration >= keep}
 
+    def _draw(self, p: Pass, logits) -> None:
+        """The tokens of one pass, drawn from its logits into the row that the first shard reads."""
+        from . import binding
+
+        s, mb = self.sampling, p.micro_batch
+        settings = [s[n][mb] if n in s else None for n in ("temperature", "top_k", "top_p", "min_p")]
+        binding.es_op_sample(logits, s["u"][p.iteration, mb], *settings, out=(self.tokens[mb], self.logprobs[mb]))
+
     def prefill(self, ids, prompt_len: int, on_output=None) -> None:
         """ids: [micro_batches, batch, prompt_len] int32 on the device."""
         if self.iteration != 0:
@@ -139,11 +167,14 @@ class ShardPipeline:
 
     def decode(self, steps: int, forced=None, on_output=None) -> None:
         """`steps` token iterations.  forced: [>= steps done so far, micro_batches, batch] int32 device tensor of
-        teacher-forced inputs indexed by decode step, or None to feed the last shard's greedy token back."""
+        teacher-forced inputs indexed by decode step, or None to feed the last shard's token back (greedy, or drawn where
+        the pipeline has `sampling`)."""
         if self.iteration == 0:
             raise RuntimeError("decode before prefill")
         if forced is None and not self.has_head:
             raise RuntimeError("the last shard has no LM head: pass forced token ids")
+        if self.sampling is not None and self.iteration + steps > self.sampling["u"].shape[0]:
+            raise RuntimeError(f"random numbers for {self.sampling['u'].shape[0]} iterations, {self.iteration + steps} asked for")
         self._run(steps, 0, forced=forced, on_output=on_output)
 
     def join(self, stream) -> None:
