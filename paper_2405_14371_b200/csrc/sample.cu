@@ -2,17 +2,25 @@
 //
 // No row is sorted.  Every restriction keeps a prefix of the ranking (by logit, equal ones by index), so each is a
 // threshold in that order, held as one 64-bit number, the logit's order-preserving bits above the complement of the
-// index.  A histogram over the distance from the largest logit (counts, and weights where top-p asks for them) says in
-// which bin a threshold lies; the few elements of that bin are collected, ranked and searched.  A bin with more elements
-// than the list takes (many equal logits) is descended by the bits of its keys instead.  The draw is a search for a
-// running weight in order of index.
+// index.  Three ways to it, from the cheapest:
+//
+//   * a small top-k: the k largest maxima of groups of 16 are k elements, so whatever ranks among the first k lies no lower
+//     than the smallest of them.  A histogram of the maxima says where that is, the few elements from there up are
+//     collected (only groups whose maximum reaches it are read), and one CTA finishes the row;
+//   * few candidates after all: a histogram over the distance from the largest logit (counts, and weights where top-p
+//     asks for them) says in which bin the threshold lies; up to 256 elements down to that bin are finished the same way;
+//   * else the elements of that bin alone are collected, ranked and searched.  A bin with more elements than the list
+//     takes (many equal logits) is descended by the bits of its keys instead.
+//
+// The draw is a search for a running weight in order of index.
 //
 // Weights are integers, w = round(2^44 exp2((x - max) log2(e) / temperature)) out of 64-bit arithmetic, so every sum
 // is exact whatever its order: thresholds and tokens depend on the inputs alone, and the borders are as sharp as the
 // exponential (2^-39).
 //
-// A row belongs to a cluster of 1 to 8 CTAs, each holding a slice of the row in shared memory as fp32: the logits are read
-// from HBM once, whatever the number of passes.
+// A row belongs to a cluster of 1 to 8 CTAs.  Where all CTAs of a call run at once, each holds its slice of the row in
+// shared memory as fp32: latency counts there.  Larger calls read the slice again from L2, which leaves room for four
+// CTAs on an SM, one's barriers under another's sums.
 #include <cooperative_groups.h>
 #include <limits.h>
 
@@ -27,9 +35,10 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int ST = 512;                       // threads of a CTA
-constexpr int SW = ST / 32;
-constexpr int CHUNK = 128;                    // elements a warp sums at a time: the grain of the search
+constexpr int MAX_WARPS = 16;
+constexpr int GROUP = 16;                     // elements that a thread loads together; their largest is kept
+constexpr int TOP_FEW = 200;                  // largest top_k that goes by the maxima
+constexpr int CHUNK = 128;                    // neighbours a warp sums at a time: the grain of the search
 constexpr int MAX_CLUSTER = 8;
 constexpr int MAX_V = 262144;                 // 2^18 weights of 2^44 stay below 2^63
 constexpr int MAX_SLICE = MAX_V / MAX_CLUSTER;
@@ -53,8 +62,7 @@ struct Shared {
   // one entry per CTA of the cluster, written by that CTA into everybody's copy: after the next cluster barrier each reads
   // its own memory
   u64 total[MAX_CLUSTER];
-  u64 best[MAX_CLUSTER];                      // largest (key, index)
-  float least[MAX_CLUSTER];                   // smallest finite logit
+  float best[MAX_CLUSTER], least[MAX_CLUSTER];  // largest logit, about the smallest finite one
   int found;                                  // a chosen index, from the CTA that found it
   // from the first CTA
   int pick_bin, pick_count;                   // a bin, and how many elements it holds
@@ -65,8 +73,9 @@ struct Shared {
   u64 all_mass;
   int list_n;
   int few_n;                                  // first CTA: candidates that have arrived
+  int top;                                    // first CTA: lowest index of the largest
   int base;
-  u64 warp_a[SW], warp_b[SW];
+  u64 warp_a[MAX_WARPS], warp_b[MAX_WARPS];
   int digit;                                  // descent by key bits
   u64 digit_above, digit_here;
 };
@@ -119,10 +128,26 @@ __device__ __forceinline__ u64 share_of(float f, u64 all, bool* more) {
 
 __device__ __forceinline__ u64 pair_key(uint32_t key, int index) { return ((u64)key << 32) | (uint32_t)~index; }
 
+template <int DT>
+__device__ __forceinline__ float load_logit(const void* p, int64_t i) {
+  float x;
+  if (DT == ES_DTYPE_F32) x = __ldg(reinterpret_cast<const float*>(p) + i);
+  else if (DT == ES_DTYPE_F16) x = __half2float(reinterpret_cast<const __half*>(p)[i]);
+  else x = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p)[i]);
+  return fmaxf(x, -INFINITY) + 0.f;           // NaN becomes -infinity; -0 becomes +0: equal numbers have equal keys
+}
+
 // One row's working state; every method is called by all threads of the cluster.
-template <int ranks>
+template <int DT, int ranks, bool RESIDENT>
 struct Row {
-  float* x;                                   // slice in shared memory, padded with -infinity to a multiple of CHUNK
+  static constexpr int ST = RESIDENT ? 512 : 256, SW = ST / 32;       // threads and warps of a CTA
+  static constexpr int BPT = NB / ST;         // bins of a thread in the first CTA
+  float* x;                                   // RESIDENT: slice in shared memory, padded with -infinity to a multiple of CHUNK
+  const void* logits;                         // else the row, from the slice's first element at `at`
+  int64_t at;
+  int real;                                   // elements of the slice
+  float* gmax;                                // largest of every group: group (round, thread) holds the elements
+                                              // (GROUP round + j) ST + thread, j < GROUP
   u64* csum;                                  // [slice / CHUNK]
   uint32_t *cnt, *part;                       // [NB] counts, [3][NB] weights in three fields of 15 bits
   uint4* inbox;                               // [ranks][NB / ranks] this CTA's share of the bins, from every CTA
@@ -138,32 +163,99 @@ struct Row {
   u64 keep;                                   // kept: elements not below this in the ranking
   u64 least;                                  // ... whose weight is at least this
 
+  static __host__ __device__ constexpr int groups(int elements) { return (elements + ST * GROUP - 1) / (ST * GROUP) * ST; }
+  __device__ __forceinline__ float get(int i) const {
+    if (RESIDENT) return x[i];
+    return i < real ? load_logit<DT>(logits, at + i) : -INFINITY;
+  }
+  // t = (v - max) c as r + f, r whole (in the low bits of the result's first word) and |f| <= 1/2.  Roundings spelled out:
+  // every use has to give the same weight to the last bit.
+  __device__ __forceinline__ double split(float v, double x0, double* f) const {
+    const double magic = 6755399441055744.0;  // 1.5 * 2^52: adding it rounds to an integer, which its low bits hold
+    const double t = __dmul_rn(__dsub_rn((double)v, x0), c), r = __dadd_rn(t, magic);
+    *f = __dsub_rn(t, __dsub_rn(r, magic));
+    return __hiloint2double((1023 + 44 + __double2loint(r)) << 20, 0);            // 2^(44 + r), -47 <= r <= 0
+  }
+  static __device__ __forceinline__ u64 scaled(double poly, double scale) {
+    return (u64)__double_as_longlong(fma(poly, scale, 4503599627370496.0)) - 0x4330000000000000ull;
+  }
+  // not so far below the largest that the weight rounds to zero (false for -infinity, and for anything finite below an
+  // infinite largest)
+  __device__ __forceinline__ bool near(float v) const { return fmaf(v, 0.5f, -0.5f * xmax) * cf > -0.5f * REACH; }
   __device__ __forceinline__ u64 weight(float v) const {
     if (v == xmax) return 1ull << 44;
-    // far below: zero without 64-bit work (also -infinity, and anything finite below an infinite maximum)
-    if (!(fmaf(v, 0.5f, -0.5f * xmax) * cf > -0.5f * REACH)) return 0;
-    const double t = ((double)v - (double)xmax) * c;
-    const double magic = 6755399441055744.0;  // 1.5 * 2^52: adding it rounds to an integer, which its low bits hold
-    const double r = t + magic;
-    const double f = t - (r - magic);
-    const double scale = __hiloint2double((1023 + 44 + __double2loint(r)) << 20, 0);      // -47 <= r <= 0
-    return (u64)__double_as_longlong(fma(exp2_poly(f), scale, 4503599627370496.0)) - 0x4330000000000000ull;
+    if (!near(v)) return 0;
+    double f;
+    const double scale = split(v, (double)xmax, &f);
+    return scaled(exp2_poly(f), scale);
+  }
+  // the weights of four elements at once, without branches between them: the 64-bit chains of one fill the other's gaps
+  __device__ __forceinline__ void weights(const float (&v)[4], u64 (&w)[4]) const {
+    if (isinf(xmax)) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = v[j] == xmax ? 1ull << 44 : 0;
+      return;
+    }
+    bool in[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) in[j] = near(v[j]) || v[j] == xmax;
+    if (!__any_sync(~0u, in[0] || in[1] || in[2] || in[3])) {
+      w[0] = w[1] = w[2] = w[3] = 0;
+      return;
+    }
+    const double x0 = (double)xmax;
+    double f[4], scale[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) scale[j] = split(v[j], x0, &f[j]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] = exp2_poly(f[j]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = in[j] ? scaled(f[j], scale[j]) : 0;
   }
   __device__ __forceinline__ bool kept(float v, int i) const { return pair_key(key_of(v), i) >= keep; }
   // bins grow with the distance from the largest logit; equal logits share one
   __device__ __forceinline__ int bin_of(float v) const {
-    return v == xmax ? 0 : (int)fminf((xmax - v) * bin_scale, (float)(NB - 1));
+    // adding 2^23 leaves the whole number (rounded, as good as cut off) in the low bits
+    const float d = fminf((xmax - v) * bin_scale, (float)(NB - 1));
+    return v == xmax ? 0 : __float_as_int(d + 8388608.f) & (2 * NB - 1);
+  }
+
+  // f of four elements, 32 apart
+  template <class F>
+  __device__ __forceinline__ u64 sum4(const F& f, const float (&v)[4], int i) const {
+    return f(v[0], i) + f(v[1], i + 32) + f(v[2], i + 64) + f(v[3], i + 96);
+  }
+  // weight of what is kept
+  struct Kept {
+    const Row& r;
+    __device__ __forceinline__ u64 operator()(float v, int i) const {
+      const u64 w = r.kept(v, i) ? r.weight(v) : 0ull;
+      return w >= r.least ? w : 0;
+    }
+  };
+  __device__ __forceinline__ u64 sum4(const Kept&, const float (&v)[4], int i) const {
+    u64 w[4];
+    weights(v, w);
+    if (keep) {                               // uniform, as the next
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = kept(v[j], i + 32 * j) ? w[j] : 0;
+    }
+    if (least > 1) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = w[j] >= least ? w[j] : 0;
+    }
+    return w[0] + w[1] + w[2] + w[3];
   }
 
   // chunk sums of f(value, index) in csum, every CTA's sum in sm->total; returns the cluster's
   template <class F>
-  __device__ u64 sums(F f) {
+  __device__ u64 sums(const F& f) {
     cg::cluster_group cl = cg::this_cluster();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int ch = warp; ch < n / CHUNK; ch += SW) {
-      const float4 v = *reinterpret_cast<const float4*>(x + ch * CHUNK + lane * 4);
-      const int i = first + ch * CHUNK + lane * 4;
-      const u64 s = warp_sum(f(v.x, i) + f(v.y, i + 1) + f(v.z, i + 2) + f(v.w, i + 3));
+      const int i = ch * CHUNK + lane;
+      const float v[4] = {get(i), get(i + 32), get(i + 64), get(i + 96)};
+      const u64 s = warp_sum(sum4(f, v, first + i));
       if (lane == 0) csum[ch] = s;
     }
     __syncthreads();
@@ -201,13 +293,17 @@ struct Row {
       }
       run = __shfl_sync(~0u, inc, 31);
     }
-    const float4 v = *reinterpret_cast<const float4*>(x + ch * CHUNK + lane * 4);
-    const int i = first + ch * CHUNK + lane * 4;
-    const u64 a = f(v.x, i), b = a + f(v.y, i + 1), d = b + f(v.z, i + 2), e = d + f(v.w, i + 3);
-    const u64 inc = run + warp_scan(e), base = inc - e;
-    const unsigned hit = __ballot_sync(~0u, inc > target);
-    const int at = i + (base + a > target ? 0 : base + b > target ? 1 : base + d > target ? 2 : 3);
-    return __shfl_sync(~0u, at, __ffs(hit) - 1);
+    int at_index = ch * CHUNK;                // in steps of 32: ends where the chunk's sum passes the target
+    unsigned hit = 0;
+#pragma unroll 1
+    for (int j = 0; j < CHUNK / 32; ++j) {
+      const u64 inc = run + warp_scan(f(get(at_index + lane), first + at_index + lane));
+      hit = __ballot_sync(~0u, inc > target);
+      if (hit) break;
+      run = __shfl_sync(~0u, inc, 31);
+      at_index += 32;
+    }
+    return first + at_index + (hit ? __ffs(hit) - 1 : -1);
   }
 
   // the same, in every CTA
@@ -235,7 +331,7 @@ struct Row {
       for (int i = threadIdx.x; i < 256; i += ST) dhist[i] = 0;
       __syncthreads();
       for (int i = threadIdx.x; i < n; i += ST) {
-        const float v = x[i];
+        const float v = get(i);
         const uint32_t k = key_of(v);
         if (shift == 24 || (k >> (shift + 8)) == prefix) {
           const u64 w = f(v, first + i);
@@ -275,28 +371,34 @@ struct Row {
     return prefix;
   }
 
-  // Counts per bin, and weights where asked, summed over the cluster in the first CTA.
-  __device__ void histogram(bool mass) {
+  // Counts per bin, and weights where asked, summed over the cluster in the first CTA; of all elements, or of the maxima.
+  __device__ void histogram(bool mass, bool of_maxima) {
     cg::cluster_group cl = cg::this_cluster();
     for (int i = threadIdx.x; i < (mass ? NB : NB / 4); i += ST) reinterpret_cast<uint4*>(cnt)[i] = make_uint4(0, 0, 0, 0);     // part follows cnt
     __syncthreads();
-    for (int i = threadIdx.x * 4; i < n; i += ST * 4) {
-      const float4 v4 = *reinterpret_cast<const float4*>(x + i);
-      const float v[4] = {v4.x, v4.y, v4.z, v4.w};
-      int b[4];
+    if (of_maxima) {
+      for (int i = threadIdx.x; i < groups(n); i += ST) atomicAdd(&cnt[bin_of(gmax[i])], 1u);
+    } else {
+      for (int base = 0; base < n; base += ST * 4) {       // n is a multiple of CHUNK: a warp is inside or outside
+        float v[4];
+        int b[4];
+        const int i = base + (threadIdx.x >> 5) * CHUNK + (threadIdx.x & 31);
+        if (i >= n) continue;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) { b[j] = bin_of(v[j]); atomicAdd(&cnt[b[j]], 1u); }
-      if (mass) {
-        u64 w[4];
+        for (int j = 0; j < 4; ++j) v[j] = get(i + 32 * j);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = weight(v[j]);
+        for (int j = 0; j < 4; ++j) { b[j] = bin_of(v[j]); atomicAdd(&cnt[b[j]], 1u); }
+        if (mass) {
+          u64 w[4];
+          weights(v, w);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (w[j]) {
-            atomicAdd(&part[b[j]], (uint32_t)w[j] & 0x7fffu);
-            atomicAdd(&part[NB + b[j]], (uint32_t)(w[j] >> 15) & 0x7fffu);
-            atomicAdd(&part[2 * NB + b[j]], (uint32_t)(w[j] >> 30));
-          }
+          for (int j = 0; j < 4; ++j)
+            if (w[j]) {
+              atomicAdd(&part[b[j]], (uint32_t)w[j] & 0x7fffu);
+              atomicAdd(&part[NB + b[j]], (uint32_t)(w[j] >> 15) & 0x7fffu);
+              atomicAdd(&part[2 * NB + b[j]], (uint32_t)(w[j] >> 30));
+            }
+        }
       }
     }
     __syncthreads();
@@ -338,7 +440,7 @@ struct Row {
     b = warp_scan(b);
     if (lane == 31) { sm->warp_a[warp] = a; sm->warp_b[warp] = b; }
     __syncthreads();
-    u64 wa = lane < warp ? sm->warp_a[lane & (SW - 1)] : 0, wb = lane < warp ? sm->warp_b[lane & (SW - 1)] : 0;      // SW = 16 <= 32
+    const u64 wa = lane < warp ? sm->warp_a[lane] : 0, wb = lane < warp ? sm->warp_b[lane] : 0;      // SW <= 16
     a += warp_sum(wa);
     b += warp_sum(wb);
     __syncthreads();
@@ -357,31 +459,34 @@ struct Row {
     for (int i = 0; i < ranks; ++i) cl.map_shared_rank(sm, i)->pick_pair = pair;
   }
 
-  // The elements whose bin lies in [lo, hi] (at most LIST in all) go to the first CTA's list: each CTA gathers its own, then
-  // takes room for them there with one remote addition to `counter`.
+  // The elements whose bin lies in [lo, hi] go to the first CTA's list: each CTA gathers its own out of the groups whose
+  // largest reaches bin hi, then takes room for them there with one remote addition to `counter`.  Counts beyond LIST
+  // are kept, elements beyond it are not.
   __device__ void collect(int lo, int hi, int* counter) {
     cg::cluster_group cl = cg::this_cluster();
     if (threadIdx.x == 0) sm->list_n = 0;
     __syncthreads();
-    for (int i = threadIdx.x * 4; i < n; i += ST * 4) {
-      const float4 v4 = *reinterpret_cast<const float4*>(x + i);
-      const float v[4] = {v4.x, v4.y, v4.z, v4.w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int b = bin_of(v[j]);
-        if (b >= lo && b <= hi) {
-          const int at = atomicAdd(&sm->list_n, 1);
-          if (at < LIST) mine[at] = pair_key(key_of(v[j]), first + i + j);
+    for (int round = 0; round * ST * GROUP < n; ++round) {
+      if (bin_of(gmax[round * ST + threadIdx.x]) > hi) continue;
+#pragma unroll 4
+      for (int j = 0; j < GROUP; ++j) {
+        const int i = (round * GROUP + j) * ST + threadIdx.x;
+        const float v = i < n ? get(i) : -INFINITY;
+        const int b = bin_of(v);
+        if (i < n && b >= lo && b <= hi) {
+          const int place = atomicAdd(&sm->list_n, 1);
+          if (place < LIST) mine[place] = pair_key(key_of(v), first + i);
         }
       }
     }
     __syncthreads();
-    const int m = min(sm->list_n, LIST);
+    const int m = sm->list_n;
     if (m > 0) {                              // uniform over the CTA
       if (threadIdx.x == 0) sm->base = atomicAdd(cl.map_shared_rank(counter, 0), m);
       __syncthreads();
-      u64* to = cl.map_shared_rank(list, 0) + sm->base;
-      for (int i = threadIdx.x; i < m && sm->base + i < LIST; i += ST) to[i] = mine[i];
+      u64* to = cl.map_shared_rank(list, 0);
+      for (int i = threadIdx.x; i < min(m, LIST); i += ST)
+        if (sm->base + i < LIST) to[sm->base + i] = mine[i];
     }
     cl.sync();
   }
@@ -399,7 +504,7 @@ struct Row {
   // First CTA, all m <= FEW candidates in the list: thresholds and draw, every element against every other.
   // `whole`: the mass that top_p is a share of, or 0: that of the top_k first.
   __device__ void finish_few(int m, u64 top_k, bool by_mass, float top_p, u64 whole, float u, int* token, float* logprob) {
-    int q = 2;                                // threads of an element
+    int q = 1;                                // threads of an element
     while (q < 16 && m * q * 2 <= ST) q *= 2;
     const int e = threadIdx.x / q, part_of = threadIdx.x & (q - 1);
     if (threadIdx.x < m) lweight[threadIdx.x] = weight(of_key((uint32_t)(list[threadIdx.x] >> 32)));
@@ -509,23 +614,17 @@ struct Row {
   }
 };
 
-static_assert(SW == 16 && LIST == 2 * ST && NB == 2 * ST && 2 * LIST * 8 <= NB * 16, "scan2, choose and the bins of a thread");
+static_assert(FEW <= 256 && LIST % 512 == 0 && NB % 512 == 0 && 2 * LIST * 8 <= NB * 16 && CHUNK == 128, "choose, finish_few, sum4 and the bins of a thread");
 
-template <int DT>
-__device__ __forceinline__ float load_logit(const void* p, int64_t i) {
-  float x;
-  if (DT == ES_DTYPE_F32) x = __ldg(reinterpret_cast<const float*>(p) + i);
-  else if (DT == ES_DTYPE_F16) x = __half2float(reinterpret_cast<const __half*>(p)[i]);
-  else x = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p)[i]);
-  return isnan(x) ? -INFINITY : x + 0.f;      // -0 becomes +0: equal numbers have equal keys
+__host__ __device__ constexpr size_t sample_smem(int slice, bool resident) {
+  const int round = (resident ? 512 : 256) * GROUP;
+  return (resident ? (size_t)slice * 4 : 0) + (size_t)((slice + round - 1) / round) * (round / GROUP) * 4 + (size_t)(slice / CHUNK) * 8 + (size_t)NB * (16 + 16 + 8 + 4);
 }
 
-__host__ __device__ constexpr size_t sample_smem(int slice) {
-  return (size_t)slice * 4 + (size_t)(slice / CHUNK) * 8 + (size_t)NB * (16 + 16 + 8 + 4);
-}
-
-template <int DT, int ranks>
-__global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
+template <int DT, int ranks, bool RESIDENT>
+__global__ void __launch_bounds__(RESIDENT ? 512 : 256, RESIDENT ? 2 : 4) sample_kernel(const SampleParams p) {
+  using RowT = Row<DT, ranks, RESIDENT>;
+  constexpr int ST = RowT::ST, SW = RowT::SW, BPT = RowT::BPT;
   extern __shared__ __align__(16) unsigned char dyn[];
   __shared__ Shared shared;
   cg::cluster_group cl = cg::this_cluster();
@@ -536,11 +635,12 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
   const float T = p.temperature ? p.temperature[row] : 1.f, tp = p.top_p ? p.top_p[row] : 1.f;
   const float mp = p.min_p ? fminf(fmaxf(p.min_p[row], 0.f), 1.f) : 0.f, u = fminf(fmaxf(p.u[row], 0.f), 1.f);
   const int k = p.top_k ? p.top_k[row] : 0;
-  Row<ranks> R;
+  RowT R;
+  // [slice] logits where resident | [4][NB] the CTA's histogram, later its own elements of a bin and the list's weights, or
+  // the sums of a descent | [NB] uint4 inbox of the histograms, later the list | the cluster's weights | largest of groups | chunk
+  // sums | the cluster's counts
   R.x = reinterpret_cast<float*>(dyn);
-  // [slice] logits | [4][NB] the CTA's histogram, later its own elements of a bin and the list's weights, or the sums of a
-  // descent | [NB] uint4 inbox of the histograms, later the list | the cluster's weights and counts | chunk sums
-  R.cnt = reinterpret_cast<uint32_t*>(dyn + (size_t)p.slice * 4);
+  R.cnt = reinterpret_cast<uint32_t*>(dyn + (RESIDENT ? (size_t)p.slice * 4 : 0));
   R.part = R.cnt + NB;
   R.mine = R.dhist = reinterpret_cast<u64*>(R.cnt);
   R.dcomb = R.dhist + 256;
@@ -548,53 +648,50 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
   R.inbox = reinterpret_cast<uint4*>(R.part + 3 * NB);
   R.list = reinterpret_cast<u64*>(R.inbox);
   R.cmass = reinterpret_cast<u64*>(R.inbox + NB);
-  R.csum = R.cmass + NB;
+  R.gmax = reinterpret_cast<float*>(R.cmass + NB);
+  R.csum = reinterpret_cast<u64*>(R.gmax + RowT::groups(p.slice));
   R.ccnt = reinterpret_cast<uint32_t*>(R.csum + p.slice / CHUNK);
   R.sm = &shared;
   R.rank = rank;
   R.first = rank * p.slice;
-  const int real = max(0, min(p.V - R.first, p.slice));
+  const int real = R.real = max(0, min(p.V - R.first, p.slice));
   R.n = (real + CHUNK - 1) / CHUNK * CHUNK;
+  R.logits = p.logits;
+  R.at = (int64_t)row * p.row_stride + R.first;
 
-  // ---- the slice comes in; largest logit at the lowest index, smallest finite one ----
-  u64 best = 0;
-  float least = INFINITY;
-  const int64_t row_at = (int64_t)row * p.row_stride + R.first;
-  constexpr int FLIGHT = 16;                  // loads of a thread under way at a time
-  for (int base = 0; base < R.n; base += ST * FLIGHT) {
-    float v[FLIGHT];
+  // ---- the slice comes in; largest logit, and about the smallest (one of every group) ----
+  float best = -INFINITY, least = INFINITY;
+  for (int base = 0; base < R.n; base += ST * GROUP) {
+    float v[GROUP], most = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < FLIGHT; ++j) {
+    for (int j = 0; j < GROUP; ++j) {
       const int i = base + j * ST + tid;
-      v[j] = i < real ? load_logit<DT>(p.logits, row_at + i) : -INFINITY;
+      v[j] = i < real ? load_logit<DT>(p.logits, R.at + i) : -INFINITY;
     }
 #pragma unroll
-    for (int j = 0; j < FLIGHT; ++j) {
+    for (int j = 0; j < GROUP; ++j) {
       const int i = base + j * ST + tid;
-      if (i < R.n) {
-        R.x[i] = v[j];
-        const u64 b = pair_key(key_of(v[j]), R.first + i);
-        best = b > best ? b : best;
-        if (v[j] > -INFINITY) least = fminf(least, v[j]);
-      }
+      if (RESIDENT && i < R.n) R.x[i] = v[j];
+      most = fmaxf(most, v[j]);
     }
+    R.gmax[base / GROUP + tid] = most;
+    best = fmaxf(best, most);
+    if (v[0] > -INFINITY) least = fminf(least, v[0]);
   }
 #pragma unroll
   for (int d = 16; d; d >>= 1) {
-    const u64 o = __shfl_xor_sync(~0u, best, d);
-    best = o > best ? o : best;
+    best = fmaxf(best, __shfl_xor_sync(~0u, best, d));
     least = fminf(least, __shfl_xor_sync(~0u, least, d));
   }
-  if (lane == 0) { shared.warp_a[warp] = best; shared.warp_b[warp] = __float_as_uint(least); }
+  if (lane == 0) { shared.warp_a[warp] = __float_as_uint(best); shared.warp_b[warp] = __float_as_uint(least); }
   __syncthreads();
   cluster_wait();
   if (warp == 0) {
-    best = lane < SW ? shared.warp_a[lane] : 0;
+    best = lane < SW ? __uint_as_float((uint32_t)shared.warp_a[lane]) : -INFINITY;
     least = lane < SW ? __uint_as_float((uint32_t)shared.warp_b[lane]) : INFINITY;
 #pragma unroll
     for (int d = 16; d; d >>= 1) {
-      const u64 o = __shfl_xor_sync(~0u, best, d);
-      best = o > best ? o : best;
+      best = fmaxf(best, __shfl_xor_sync(~0u, best, d));
       least = fminf(least, __shfl_xor_sync(~0u, least, d));
     }
     if (lane < ranks) {
@@ -602,23 +699,39 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
       to->best[rank] = best;
       to->least[rank] = least;
     }
-    if (lane == 0) { shared.few_n = 0; shared.pick_bin = 0; shared.pick_count = 0; shared.pick_target = 1; shared.pick_pair = 0; }
+    if (lane == 0) { shared.few_n = 0; shared.pick_bin = 0; shared.pick_count = 0; shared.pick_target = 1; shared.pick_pair = 0; shared.top = INT_MAX; }
   }
   cl.sync();
-  best = 0;
+  best = -INFINITY;
   least = INFINITY;
 #pragma unroll
   for (int r = 0; r < ranks; ++r) {
-    best = shared.best[r] > best ? shared.best[r] : best;
+    best = fmaxf(best, shared.best[r]);
     least = fminf(least, shared.least[r]);
   }
 
-  R.xmax = of_key((uint32_t)(best >> 32));
-  const int top = (int)~(uint32_t)best;
-  if (R.xmax == -INFINITY || !(T > 0.f)) {    // nothing to draw from, or no drawing
+  R.xmax = best;
+  if (R.xmax == -INFINITY) {                  // nothing to draw from
     if (rank == 0 && tid == 0) {
-      p.tokens[row] = R.xmax == -INFINITY ? -1 : top;
-      if (p.logprobs) p.logprobs[row] = R.xmax == -INFINITY ? -INFINITY : 0.f;
+      p.tokens[row] = -1;
+      if (p.logprobs) p.logprobs[row] = -INFINITY;
+    }
+    return;
+  }
+  if (!(T > 0.f)) {                           // no drawing: the lowest index of the largest
+    int top = INT_MAX;
+    for (int round = 0; round * ST * GROUP < R.n; ++round)
+      if (R.gmax[round * ST + tid] == R.xmax)
+        for (int j = GROUP - 1; j >= 0; --j) {
+          const int i = (round * GROUP + j) * ST + tid;
+          if (i < real && R.get(i) == R.xmax) top = min(top, R.first + i);
+        }
+    top = __reduce_min_sync(~0u, top);
+    if (lane == 0 && top < INT_MAX) atomicMin(cl.map_shared_rank(&shared.top, 0), top);
+    cl.sync();
+    if (rank == 0 && tid == 0) {
+      p.tokens[row] = shared.top;
+      if (p.logprobs) p.logprobs[row] = 0.f;
     }
     return;
   }
@@ -633,34 +746,74 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
   if (by_count || by_mass) {
     const float span = fminf(R.xmax - least, REACH / R.cf);
     R.bin_scale = span > 0.f ? fminf((NB - 1) / span, 1e37f) : 0.f;
-    // weights are left out of the histogram where the count alone is likely to leave few candidates; if it does not, a
-    // second one makes up for it
-    const bool count_first = by_count && by_mass && k <= FEW;
-    R.histogram(by_mass && !count_first);
-    // first CTA: inclusive sums up to this thread's second bin (bins 2 tid and 2 tid + 1)
-    u64 counts = 0, masses = 0, m0 = 0, m1 = 0;
-    uint32_t c0 = 0, c1 = 0;
+    if (by_count && k <= TOP_FEW) {           // by the maxima
+      R.histogram(false, true);
+      if (rank == 0) {
+        u64 run = 0, nothing = 0;
+        uint32_t c[BPT];
+#pragma unroll
+        for (int j = 0; j < BPT; ++j) { c[j] = R.ccnt[BPT * tid + j]; run += c[j]; }
+        R.scan2(run, nothing);
+        if (tid == ST - 1 && run < (u64)k) R.publish(NB - 1, 0, 0, 0);       // fewer maxima than that: everything is a candidate
+#pragma unroll
+        for (int j = BPT - 1; j >= 0; --j) {
+          if (run - c[j] < (u64)k && (u64)k <= run) R.publish(BPT * tid + j, 0, 0, 0);
+          run -= c[j];
+        }
+      }
+      cl.sync();
+      R.collect(0, shared.pick_bin, &shared.few_n);
+      const int m = *cl.map_shared_rank(&shared.few_n, 0);
+      cluster_arrive();
+      if (m <= FEW) {
+        if (rank == 0) R.finish_few(m, (u64)k, by_mass, tp, 0, u, p.tokens + row, p.logprobs ? p.logprobs + row : nullptr);
+        __syncwarp();
+        cluster_wait();                       // the first CTA's count has been read by all
+        return;
+      }
+      cluster_wait();
+      if (rank == 0 && tid == 0) shared.few_n = 0;         // (seen by all after the next barrier)
+    }
+    R.histogram(by_mass, false);
+    // first CTA: inclusive sums up to this thread's last bin
+    u64 counts = 0, masses = 0, mb[BPT];
+    uint32_t cb[BPT];
     auto pick_mass = [&]() {                  // first CTA: the bin in which the mass is reached, of the kept mass so far
       const u64 all = shared.all_mass;
       bool more;
       u64 target = share_of(fmaxf(tp, 0.f), all, &more);
       target += more;
       target = target < 1 ? 1 : target > all ? all : target;
-      const u64 a = masses - m0 - m1, b = masses - m1;
-      if (a < target && target <= b) R.publish(2 * tid, (int)c0, target - a, counts - c1);
-      if (b < target && target <= masses) R.publish(2 * tid + 1, (int)c1, target - b, counts);
+      u64 run = masses, up_to = counts;
+#pragma unroll
+      for (int j = BPT - 1; j >= 0; --j) {
+        if (run - mb[j] < target && target <= run) R.publish(BPT * tid + j, (int)cb[j], target - (run - mb[j]), up_to);
+        run -= mb[j];
+        up_to -= cb[j];
+      }
     };
     if (rank == 0) {
-      c0 = R.ccnt[2 * tid]; c1 = R.ccnt[2 * tid + 1];
-      counts = (u64)c0 + c1;
-      if (by_mass && !count_first) { m0 = R.cmass[2 * tid]; m1 = R.cmass[2 * tid + 1]; masses = m0 + m1; }
+#pragma unroll
+      for (int j = 0; j < BPT; ++j) {
+        cb[j] = R.ccnt[BPT * tid + j];
+        counts += cb[j];
+        mb[j] = by_mass ? R.cmass[BPT * tid + j] : 0;
+        masses += mb[j];
+      }
       R.scan2(counts, masses);
       if (tid == ST - 1) shared.all_mass = masses;
       __syncthreads();
       if (by_count) {
-        const u64 a = counts - c0 - c1, b = counts - c1;
-        if (a < (u64)k && (u64)k <= b) { R.publish(2 * tid, (int)c0, k - a, b); shared.all_mass = masses - m0 - m1; }
-        if (b < (u64)k && (u64)k <= counts) { R.publish(2 * tid + 1, (int)c1, k - b, counts); shared.all_mass = masses - m1; }
+        u64 run = counts, mass_run = masses;
+#pragma unroll
+        for (int j = BPT - 1; j >= 0; --j) {
+          if (run - cb[j] < (u64)k && (u64)k <= run) {
+            R.publish(BPT * tid + j, (int)cb[j], k - (run - cb[j]), run);
+            shared.all_mass = mass_run - mb[j];            // the mass of the bins before
+          }
+          run -= cb[j];
+          mass_run -= mb[j];
+        }
       } else {
         pick_mass();
       }
@@ -671,18 +824,6 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
       R.collect(0, last_bin, &shared.few_n);
       if (rank == 0) R.finish_few(m, by_count ? (u64)k : ~0ull, by_mass, tp, by_count ? 0 : shared.all_mass, u, p.tokens + row, p.logprobs ? p.logprobs + row : nullptr);
       return;
-    }
-    if (count_first) {
-      const int bin = shared.pick_bin;
-      R.histogram(true);
-      if (rank == 0) {
-        m0 = R.cmass[2 * tid]; m1 = R.cmass[2 * tid + 1];
-        masses = m0 + m1;
-        u64 nothing = 0;
-        R.scan2(masses, nothing);
-        if (tid == bin / 2) shared.all_mass = masses - m1 - (bin & 1 ? 0 : m0);
-        __syncthreads();
-      }
     }
     int listed = -1;                          // the bin that the list holds
     if (by_count) {
@@ -743,7 +884,7 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
       }
     }
   }
-  auto last = [&](float v, int i) { const u64 w = R.kept(v, i) ? R.weight(v) : 0ull; return w >= R.least ? w : 0ull; };
+  const typename RowT::Kept last{R};
   const u64 all = R.sums(last);
   if (warp > 0) return;                       // nothing is read from another CTA any more
   bool more;
@@ -751,21 +892,21 @@ __global__ void __launch_bounds__(ST, 2) sample_kernel(const SampleParams p) {
   if (target >= all) target = all - 1;
   const int token = R.find_here(last, target);
   if (token >= 0 && lane == 0) {
-    const float v = R.x[token - R.first];
+    const float v = R.get(token - R.first);
     const double t = v == R.xmax ? 0.0 : ((double)v - (double)R.xmax) * R.c;
     p.tokens[row] = token;
     if (p.logprobs) p.logprobs[row] = (float)((t - log2((double)all) + 44.0) * 0.6931471805599453);
   }
 }
 
-template <int DT, int ranks>
-es_status_t launch_ranks(const SampleParams& p, int B, cudaStream_t s) {
+template <int DT, int ranks, bool RESIDENT>
+es_status_t launch_kind(const SampleParams& p, int B, cudaStream_t s) {
   static std::atomic<uint64_t> allowed{0};
-  ES_CUDA_CHECK(allow_shared_memory(sample_kernel<DT, ranks>, (int)sample_smem(MAX_SLICE), &allowed));
+  ES_CUDA_CHECK(allow_shared_memory(sample_kernel<DT, ranks, RESIDENT>, (int)sample_smem(MAX_SLICE, RESIDENT), &allowed));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(B * ranks));
-  cfg.blockDim = dim3(ST);
-  cfg.dynamicSmemBytes = sample_smem(p.slice);
+  cfg.blockDim = dim3(Row<DT, ranks, RESIDENT>::ST);
+  cfg.dynamicSmemBytes = sample_smem(p.slice, RESIDENT);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -773,8 +914,15 @@ es_status_t launch_ranks(const SampleParams& p, int B, cudaStream_t s) {
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  ES_CUDA_CHECK(cudaLaunchKernelEx(&cfg, sample_kernel<DT, ranks>, p));
+  ES_CUDA_CHECK(cudaLaunchKernelEx(&cfg, sample_kernel<DT, ranks, RESIDENT>, p));
   return ES_OK;
+}
+
+template <int DT, int ranks>
+es_status_t launch_ranks(const SampleParams& p, int B, cudaStream_t s) {
+  // resident slices as long as all CTAs of the call run at once
+  const int per_sm = sample_smem(p.slice, true) <= 112 * 1024 ? 2 : 1;
+  return (long long)B * ranks <= (long long)per_sm * sm_count() ? launch_kind<DT, ranks, true>(p, B, s) : launch_kind<DT, ranks, false>(p, B, s);
 }
 
 template <int DT>
@@ -802,8 +950,7 @@ es_status_t es_op_sample(const void* logits, int32_t dtype, int64_t row_stride, 
   if (row_stride < V) return fail(ES_ERR_INVALID_ARG, "row_stride is smaller than V");
   if (V > MAX_V) return fail(ES_ERR_RANGE, "V = %d exceeds %d", V, MAX_V);
   if (B > (1 << 24)) return fail(ES_ERR_RANGE, "too many rows");
-  // slices of at most 16384 elements (two CTAs share an SM then: one works while the other's logits arrive), and smaller
-  // ones while the machine has room for more CTAs
+  // slices of at most 16384 elements, and smaller ones while the machine has room for more CTAs
   int ranks = 1;
   while (ranks < MAX_CLUSTER && (V > 16384LL * ranks || ((long long)B * ranks < sm_count() && V > 2048 * ranks))) ranks *= 2;
   const int slice = ((V + ranks - 1) / ranks + CHUNK - 1) / CHUNK * CHUNK;
