@@ -468,14 +468,18 @@ struct Row {
     __syncthreads();
     for (int round = 0; round * ST * GROUP < n; ++round) {
       if (bin_of(gmax[round * ST + threadIdx.x]) > hi) continue;
-#pragma unroll 4
-      for (int j = 0; j < GROUP; ++j) {
-        const int i = (round * GROUP + j) * ST + threadIdx.x;
-        const float v = i < n ? get(i) : -INFINITY;
-        const int b = bin_of(v);
-        if (i < n && b >= lo && b <= hi) {
-          const int place = atomicAdd(&sm->list_n, 1);
-          if (place < LIST) mine[place] = pair_key(key_of(v), first + i);
+      for (int at = 0; at < GROUP; at += 8) {
+        float v[8];
+        const int i = (round * GROUP + at) * ST + threadIdx.x;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = i + j * ST < n ? get(i + j * ST) : -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int b = bin_of(v[j]);
+          if (i + j * ST < n && b >= lo && b <= hi) {
+            const int place = atomicAdd(&sm->list_n, 1);
+            if (place < LIST) mine[place] = pair_key(key_of(v[j]), first + i + j * ST);
+          }
         }
       }
     }
@@ -558,8 +562,8 @@ struct Row {
       for (int i = threadIdx.x; i < m; i += ST) lweight[i] = weight(of_key((uint32_t)(list[i] >> 32)));
       __syncthreads();
     }
-    if (m <= ST / 2) {                        // every element against every other, several threads an element
-      int q = 2;
+    if (m <= FEW) {                           // every element against every other, several threads an element
+      int q = 1;
       while (q < 16 && m * q * 2 <= ST) q *= 2;
       const int e = threadIdx.x / q;
       const u64 mine = e < m ? list[e] : ~0ull;
