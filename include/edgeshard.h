@@ -378,7 +378,8 @@ ES_API es_status_t es_op_decode_attention_static(const void *q, const void *k_pa
  *   old_len, new_len int32 [B], B <= 8192;   block_table int32 [B, pages_per_seq], in and out;
  *   free_pages int32 [n_pages] and free_count int32 [1], in and out: a stack of the pages nobody holds.
  *     Both NULL: the table is taken as it is and only the row outputs are made.
- *   max_rows: room of the row outputs (>= 1);  pages_per_seq * page_tokens <= 2^31 - 1.
+ *   max_rows: room of the row outputs (1 to 2^30);  n_pages and pages_per_seq times page_tokens <= 2^31 - 1;
+ *   B * pages_per_seq <= 2^30.
  * Pages: first the pages of shrinking requests (table entries ceil(new / P) .. ceil(old / P) - 1) are pushed in
  * ascending order of (b, entry) and their entries become -1; then growing requests, in ascending order, pop the
  * pages they lack from the top.  A growing request is served whole or not at all: it is refused when the rows up to
@@ -429,7 +430,9 @@ ES_API es_status_t es_op_kv8_gather(const int32_t *slot_map, int32_t n_rows, con
 /* es_op_decode_attention over the 8-bit cache, for the newest T tokens of every sequence (T = 1: a decode step;
  * T > 1: draft tokens checked in one pass).
  *   q (fp16 or bf16) [B, T, Hq, hd], token b * T + t at q + (b * T + t) * q_stride elements (heads contiguous,
- *   q_stride % 8 == 0, 16-byte aligned);  out [B, T, Hq * hd], dense, of q's type;  Hq a multiple of Hkv;
+ *   q_stride % 8 == 0, 16-byte aligned);  out [B, T, Hq * hd], dense, of q's type, 4-byte aligned;  Hq a multiple
+ *   of Hkv;  B <= 4096, T * Hq / Hkv <= 65535, max_ctx <= 2^30, and B * Hkv * ceil(T * Hq / Hkv / 8) *
+ *   ceil(max_ctx / 32) <= 2^30;
  *   block_table int32 [B, pages_per_seq];  ctx_len int32 [B]: cached keys of the sequence, its T newest included.
  * Query t sees keys 0 .. ctx_len[b] - T + t; a query that sees none gives zeros.  Scale 1/sqrt(hd); scores, softmax
  * and sums in fp32, probabilities enter the product as two fp16 halves.  Table entries outside [0, n_pages) are
@@ -458,7 +461,7 @@ ES_API es_status_t es_op_decode_attention_kv8(const void *q, int32_t dtype, int6
  * not above 0 takes the first token.  NaN logits count as -infinity, which is never drawn; a row that has nothing
  * else gives -1 (and -infinity).  u is clamped to [0, 1].  Weights are held as integers in units of 2^-44, so every
  * sum is exact and the result depends on nothing but the inputs; tokens of weight below 2^-45 have none.
- * V <= 262144. */
+ * V <= 262144, B <= 2^24. */
 ES_API es_status_t es_op_sample(const void *logits, int32_t dtype, int64_t row_stride, const float *u,
                                 const float *temperature, const int32_t *top_k, const float *top_p,
                                 const float *min_p, int32_t *tokens, float *logprobs, int32_t B, int32_t V,

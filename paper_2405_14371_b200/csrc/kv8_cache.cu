@@ -233,7 +233,7 @@ template <int HD, int CODE, bool BF16, int WARPS>
 es_status_t launch_append_warps(const AppendParams& p, cudaStream_t s) {
   constexpr int per = APPEND_THREADS / (32 * WARPS);
   const int64_t blocks = ((int64_t)p.n_items * p.Hkv + per - 1) / per;
-  if (blocks > INT32_MAX) return fail(ES_ERR_RANGE, "too many (run, head) items for one launch");
+  if ((int64_t)p.n_items * p.Hkv > INT32_MAX) return fail(ES_ERR_RANGE, "too many (run, head) items for one launch");
   kv8_append_kernel<HD, CODE, BF16, WARPS><<<dim3((unsigned)blocks, 2), APPEND_THREADS, 0, s>>>(p);
   ES_CUDA_CHECK(cudaGetLastError());
   return ES_OK;

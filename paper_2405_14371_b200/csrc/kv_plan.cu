@@ -341,7 +341,8 @@ es_status_t es_op_kv_plan(const int32_t* old_len, const int32_t* new_len, int32_
   if (B > PLAN_MAX_B) return fail(ES_ERR_RANGE, "B = %d exceeds %d requests", B, PLAN_MAX_B);
   if ((long long)pages_per_seq * page_tokens > INT32_MAX || (long long)n_pages * page_tokens > INT32_MAX)
     return fail(ES_ERR_RANGE, "pages_per_seq or n_pages times page_tokens exceeds 2^31 - 1");
-  if (max_rows == INT32_MAX) return fail(ES_ERR_RANGE, "max_rows must be below 2^31 - 1");
+  if (max_rows > (1 << 30)) return fail(ES_ERR_RANGE, "max_rows exceeds 2^30");
+  if ((long long)B * pages_per_seq > (1 << 30)) return fail(ES_ERR_RANGE, "the block table has more than 2^30 entries");
   PlanParams p{old_len, new_len, block_table, free_pages, free_count, B, pages_per_seq, page_tokens, n_pages, max_rows,
                es_op_kv_plan_max_runs(B, max_rows, page_tokens), row_offsets, slot_map, positions, row_seq, runs, len_out};
   const size_t smem = (size_t)(6 * B + 4) * sizeof(int);

@@ -26,6 +26,7 @@ def _plan(binding, **kw):
     ({"old": None}, 1), ({"new": None}, 1), ({"table": None}, 1), ({"free": None}, 1), ({"count": None}, 1), ({"out": None}, 1), ({"runs": None}, 1),
     ({"B": 0}, 1), ({"pps": 0}, 1), ({"P": 0}, 1), ({"P": 8}, 2), ({"P": 48}, 2), ({"n_pages": 0}, 1), ({"max_rows": 0}, 1), ({"B": 8193}, 3),
     ({"pps": 1 << 27}, 3), ({"n_pages": 1 << 27}, 3), ({"max_rows": 2 ** 31 - 1}, 3),
+    ({"max_rows": 2 ** 30 + 1}, 3), ({"B": 8192, "pps": 1 << 18}, 3),
 ])
 def test_plan(B, kw, status):
     assert _plan(B, **kw) == status and B.es_last_error()
@@ -40,6 +41,7 @@ def _append(binding, **kw):
 @pytest.mark.parametrize("kw,status", [
     ({"k": None}, 1), ({"slots": None}, 1), ({"kp": None}, 1), ({"vs": None}, 1), ({"dtype": 1}, 1), ({"dtype": 9}, 1), ({"code": 0}, 1), ({"stride": 255}, 1),
     ({"stride": 260}, 1), ({"n": -1}, 1), ({"n_runs": -1}, 1), ({"Hkv": 0}, 1), ({"hd": 96}, 2), ({"P": 12}, 2), ({"n_pages": 1 << 27}, 3), ({"k": A + 8}, 1), ({"vp": A + 1}, 1),
+    ({"n": 2 ** 31 - 1, "Hkv": 2}, 3),
     ({"n": 0}, 0), ({"n": 0, "k": None}, 0), ({"runs": A, "n_runs": 0}, 0),
 ])
 def test_append(B, kw, status):
