@@ -44,7 +44,8 @@ namespace es {
 namespace {
 
 // Warps of a CTA and half tiles of a warp's ring.  8 query rows leave registers for 12 warps, whose latencies hide one
-// another's better than 8 warps' do; two half tiles each are then what 192 KB hold.
+// another's better than 8 warps' do; two half tiles each are then what 192 KB hold (64 ragged sequences: 59.6 us, with
+// 8 warps 65 us).
 template <int HD, int NT> constexpr int WARPS = NT == 1 ? 12 : 8;
 template <int HD, int NT, int TILE> constexpr int SLOTS = HD == 128 && NT == 1 && TILE == 64 ? 2 : 3;
 constexpr int MAX_GROUP = 8;             // CTAs of an item (groups)
@@ -761,16 +762,20 @@ Shape shape_of(int B, int T, int Hq, int Hkv, int hd, int max_ctx) {
   s.rows = rows < 8 * s.nt ? rows : 8 * s.nt;
   // Groups: all items at once, one wave of clusters as large as the SMs allow (no larger than the tiles can use), and not
   // more than half a megabyte for a CTA to read, so that an uneven batch, whose longest sequence then sets the time,
-  // loses less than the second kernel costs.
+  // loses about what the second kernel costs.  With 32 KV heads of 128, groups and stretches take: 1 sequence of 700
+  // 6.7 and 10.0 us, of 8192 (512 KB a CTA) 20.7 and 27.5 us; 4 of 2048 (512 KB) 20.2 and 23.1 us, of 1 to 2048 19.8 and
+  // 18.0 us; 4 of 4096 (1 MB) 32.9 and 32.6 us, of 1 to 4096 32.4 and 23.0 us.
   const long long items = (long long)B * Hkv * s.row_tiles;
   const int warps = s.nt == 1 ? WARPS<128, 1> : WARPS<128, 2>;
   int group = 1;
   while (group < MAX_GROUP && items * group * 2 <= sm_count() && (long long)group * warps * MIN_TILE < max_ctx) group *= 2;
   const bool grouped = items <= sm_count() && 2LL * max_ctx * hd <= (long long)GROUP_BYTES * group;
   s.group = grouped ? group : 0;
-  // Stretches: smaller tiles where a warp would get few of them, and the odd one too many would show.
+  // Stretches: smaller tiles where a warp would get few of them, and the odd one too many would show.  With 32 KV heads,
+  // tiles of 32 and 64 take: 8 sequences of 640 (1.4 tiles of 64 a warp) 16.7 and 17.3 us, 8 of 1280 24.7 and 23.3 us,
+  // 16 of 1280 41.1 and 36.4 us.
   const long long tiles = items * ((max_ctx + MAX_TILE - 1) / MAX_TILE);
-  s.tile = grouped || (s.nt == 1 && tiles < 4LL * warps * sm_count()) ? MIN_TILE : MAX_TILE;
+  s.tile = grouped || (s.nt == 1 && tiles < 2LL * warps * sm_count()) ? MIN_TILE : MAX_TILE;
   return s;
 }
 

@@ -240,7 +240,8 @@ es_status_t launch_append_warps(const AppendParams& p, cudaStream_t s) {
 }
 
 // A warp per item where stretches are short on average (a decode step: one row each); else as many as give a thread eight
-// 16-byte pieces of a whole page, up to eight.
+// 16-byte pieces of a whole page, up to eight.  Pages of 64 tokens, 1 / 2 / 4 / 8 warps: 8 prompts of 2600 tokens, 32 heads,
+// 139 / 118 / 103 / 118 us; a decode step of 64 sequences 8.9 / 9.3 / 10.0 / 11.3 us (append and gather together).
 template <int HD, int CODE, bool BF16>
 es_status_t launch_append(const AppendParams& p, bool whole_pages, cudaStream_t s) {
   const int warps = whole_pages ? p.P * (HD / 8) / 256 : 1;

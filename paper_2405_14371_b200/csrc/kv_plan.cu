@@ -288,7 +288,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) kv_plan_rows_kernel(const Pla
 }
 
 // CTAs of a large call's cluster: 16 where the device places such clusters (their shared work is bound by issue slots; a
-// call that returns 25 000 pages takes 20 us with 8), else the portable 8.
+// call that returns 25 000 pages and one that takes as many: 33 us with 16, 39 us with 8), else the portable 8.
 int plan_cluster() {
   static std::atomic<int> known[64];
   int dev = 0;
@@ -346,8 +346,10 @@ es_status_t es_op_kv_plan(const int32_t* old_len, const int32_t* new_len, int32_
   PlanParams p{old_len, new_len, block_table, free_pages, free_count, B, pages_per_seq, page_tokens, n_pages, max_rows,
                es_op_kv_plan_max_runs(B, max_rows, page_tokens), row_offsets, slot_map, positions, row_seq, runs, len_out};
   const size_t smem = (size_t)(6 * B + 4) * sizeof(int);
-  // one CTA as long as it writes the rows in about the time that a second launch costs
-  const bool small = max_rows <= 4096;
+  // One CTA as long as it writes the rows in about the time that a second launch costs: 1024 rows take 5.5 - 6.0 us by
+  // themselves and 6.9 - 7.4 us with the second kernel, 4096 rows 7.7 - 9.3 us and 7.2 - 8.2 us.  128 threads for the
+  // smallest: 64 requests of one row 4.8 us, with 1024 threads 6.0 us.
+  const bool small = max_rows <= 2048;
   const bool few = small && max_rows <= 4 * PLAN_FEW && B <= PLAN_FEW;
   auto kern = few ? kv_plan_kernel<true, PLAN_FEW> : small ? kv_plan_kernel<true, PLAN_THREADS> : kv_plan_kernel<false, PLAN_THREADS>;
   static std::atomic<uint64_t> allowed[2];

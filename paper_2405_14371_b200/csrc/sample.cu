@@ -37,7 +37,9 @@ typedef unsigned long long u64;
 
 constexpr int MAX_WARPS = 16;
 constexpr int GROUP = 16;                     // elements that a thread loads together; their largest is kept
-constexpr int TOP_FEW = 200;                  // largest top_k that goes by the maxima
+// Largest top_k that goes by the maxima: about k + k^2 / groups of them end up in the list that takes 256.  On 256 rows of
+// 128001, top_k 200 takes 94 us this way, 201 by the histogram of all elements 120 us; on 64 rows of 32000 both take 20 us.
+constexpr int TOP_FEW = 200;
 constexpr int CHUNK = 128;                    // neighbours a warp sums at a time: the grain of the search
 constexpr int MAX_CLUSTER = 8;
 constexpr int MAX_V = 262144;                 // 2^18 weights of 2^44 stay below 2^63
@@ -924,7 +926,8 @@ es_status_t launch_kind(const SampleParams& p, int B, cudaStream_t s) {
 
 template <int DT, int ranks>
 es_status_t launch_ranks(const SampleParams& p, int B, cudaStream_t s) {
-  // resident slices as long as all CTAs of the call run at once
+  // resident slices as long as all CTAs of the call run at once (64 rows of 32000, unrestricted / top_k 50 / top_p 0.9:
+  // resident 10.2 / 12.2 / 24.3 us, from L2 12.9 / 12.9 / 29.3; 256 rows of 128001: 118 / 113 / 306 and 119 / 87 / 274)
   const int per_sm = sample_smem(p.slice, true) <= 112 * 1024 ? 2 : 1;
   return (long long)B * ranks <= (long long)per_sm * sm_count() ? launch_kind<DT, ranks, true>(p, B, s) : launch_kind<DT, ranks, false>(p, B, s);
 }
@@ -954,9 +957,14 @@ es_status_t es_op_sample(const void* logits, int32_t dtype, int64_t row_stride, 
   if (row_stride < V) return fail(ES_ERR_INVALID_ARG, "row_stride is smaller than V");
   if (V > MAX_V) return fail(ES_ERR_RANGE, "V = %d exceeds %d", V, MAX_V);
   if (B > (1 << 24)) return fail(ES_ERR_RANGE, "too many rows");
-  // slices of at most 16384 elements, and smaller ones while the machine has room for more CTAs
+  // Slices of at most 16384 elements, and smaller ones while the machine has room for more CTAs (one row of 32000: 8 CTAs
+  // 6.0 us, 4 7.7, 2 10.6, 1 16.3); then larger ones where that saves waves of four CTAs an SM, each of which costs about as
+  // much again as 8192 elements (256 rows of 128001, unrestricted / top_k 50 / top_p 0.9: 4 CTAs a row 110 / 65 / 262 us, 8
+  // 119 / 88 / 274; 600 rows of 32000: 2 CTAs 70 / 61 / 155, 1 81 / 59 / 172).
   int ranks = 1;
   while (ranks < MAX_CLUSTER && (V > 16384LL * ranks || ((long long)B * ranks < sm_count() && V > 2048 * ranks))) ranks *= 2;
+  const auto cost = [&](int r) { return ((long long)B * r + 4 * sm_count() - 1) / (4 * sm_count()) * ((V + r - 1) / r + 8192); };
+  while (ranks > 1 && V <= (long long)MAX_SLICE * (ranks / 2) && cost(ranks / 2) < cost(ranks)) ranks /= 2;
   const int slice = ((V + ranks - 1) / ranks + CHUNK - 1) / CHUNK * CHUNK;
   SampleParams p{logits, row_stride, u, temperature, top_p, min_p, top_k, tokens, logprobs, V, slice};
   cudaStream_t s = (cudaStream_t)stream;
