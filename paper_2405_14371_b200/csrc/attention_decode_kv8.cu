@@ -44,8 +44,8 @@ namespace es {
 namespace {
 
 // Warps of a CTA and half tiles of a warp's ring.  8 query rows leave registers for 12 warps, whose latencies hide one
-// another's better than 8 warps' do; two half tiles each are then what 192 KB hold (64 ragged sequences: 59.6 us, with
-// 8 warps 65 us).
+// another's better than 8 warps' do; two half tiles each are then what 192 KB hold (32 sequences of 64/8 heads, 500 to 8191
+// tokens: 59.6 us, with 8 warps 65 us).
 template <int HD, int NT> constexpr int WARPS = NT == 1 ? 12 : 8;
 template <int HD, int NT, int TILE> constexpr int SLOTS = HD == 128 && NT == 1 && TILE == 64 ? 2 : 3;
 constexpr int MAX_GROUP = 8;             // CTAs of an item (groups)
@@ -699,7 +699,10 @@ __global__ void __launch_bounds__(128) kv8_merge_kernel(const Kv8AttnParams p, i
   const int tiles = tiles_of<TILE>(p.ctx_len[b], p.max_ctx);
   const int begin = before * items + (kvh * p.row_tiles + rt) * tiles;
   const int w0 = begin / per_warp, w1 = (begin + tiles - 1) / per_warp;
-  if (w0 == w1) return;                  // finished by its warp
+  if (w0 == w1) {                        // finished by its warp; one CTA keeps this kernel from ending before the first one
+    if (h + token + b == 0) pdl_wait();
+    return;
+  }
   const int n = w1 - w0 + 1;
   pdl_wait();
   float acc[V], mm = -INFINITY, ll = 0.f;

@@ -328,6 +328,19 @@ def test_attention_many_items_share_the_machine(B, P, hd, Hq, T, longest, code):
     _check_attn(B, case)
 
 
+def test_attention_short_sequences_in_a_long_table(B):
+    """Every sequence lies in one tile, so nothing is left to merge; what follows on the stream still finds the outputs."""
+    case = _attn_case(40, 1, 16, 8, 128, 16, [1 + i % 16 for i in range(40)], "int8", "fp16", 73, max_ctx=8000)
+    dev = [t.cuda() for t in case[:7]]
+    out = torch.zeros(40, 1, 16 * 128, dtype=torch.float16, device="cuda")
+    for _ in range(20):
+        out.fill_(math.nan)
+        B.es_op_decode_attention_kv8(*dev, 8000, out=out)
+        last = out.clone()
+        assert not bool(last.isnan().any())
+    _check_attn(B, case, got=last)
+
+
 @pytest.mark.parametrize("code", ["int8", "e4m3"])
 def test_attention_never_meets_what_lies_behind_the_context(B, code):
     """Garbage codes (NaN among them) behind the last token, in pages of nobody and NaN scales on pages out of sight do not
