@@ -28,6 +28,12 @@
 // bf16 queries are brought to fp16 by a power of two per row (largest magnitude to [1, 2)): 11 bits hold bf16's 8, and
 // what underflows is below 2^-24 of the row's largest.
 //
+// Measured: 32 sequences of 500 to 8191 tokens, 64 / 8 heads of 128 (286 MB): 59.4 us = 4.8 TB/s, of which the merge kernel
+// 6.4 us; in the loop an SM takes in 23.4 bytes a clock, the rate at which memory feeds it (with the multiplications of the
+// low halves and the conversions left out it took no less).  8 sequences of 3 to 2500 with 4 draft tokens, 40 heads (103 MB):
+// 30.1 us.  16 of 1025 to 1152 (36 MB): 14.4 us.  One of 1000, 32 heads (8 MB): 6.4 us, of which about 3 us are the launch
+// and the chain from length to table to the first tile.
+//
 // Codes behind the context are zeroed in V and masked by selection in the scores, so that garbage (NaN codes among it)
 // never meets a product; a page whose scale is NaN makes the rows that see it NaN.
 #include <cooperative_groups.h>
@@ -670,7 +676,8 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
   }
 }
 
-// One CTA per output row of an item that was split: its warps take every fourth part, in order, and join in order.  Where the
+// One CTA per output row of an item that was split (2048 rows: 6.4 us; a thread for four dimensions of a row, or a CTA for
+// an item's rows, brought fewer bytes under way and took 2 to 4 us longer): its warps take every fourth part, in order, and join in order.  Where the
 // parts lie follows from the lengths alone, so that is worked out while the first kernel still runs.
 template <int HD, int TILE>
 __global__ void __launch_bounds__(128) kv8_merge_kernel(const Kv8AttnParams p, int warps) {

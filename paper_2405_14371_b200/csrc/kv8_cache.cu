@@ -5,6 +5,11 @@
 // the bits of |x| order like the numbers, infinities and NaN above all), settles the page's scale, brings the codes in
 // front to it if it grew, and writes the new codes.  One group owns the page and head for the whole call, so nothing is
 // atomic and the result does not depend on scheduling.
+//
+// Bound: append reads two bytes and writes one per value, gather the reverse.  8 prompts of up to 2600 tokens behind up to 300,
+// 32 heads of 128 (256 MB for append, 285 MB for gather), take 103 us together, 5.2 TB/s; append fills 60 % of the issue
+// slots beside that (two conversions, the scaling and the rounding of every value).  The newest token of 64 sequences of 8
+// heads, and all 3900 of theirs read back (24 MB), take 9.2 us: two launches and a chain of slot, scale and codes each.
 #include "es_internal.cuh"
 #include "kv8.cuh"
 #include "launch.cuh"
@@ -240,7 +245,7 @@ es_status_t launch_append_warps(const AppendParams& p, cudaStream_t s) {
 }
 
 // A warp per item where stretches are short on average (a decode step: one row each); else as many as give a thread eight
-// 16-byte pieces of a whole page, up to eight.  Pages of 64 tokens, 1 / 2 / 4 / 8 warps: 8 prompts of 2600 tokens, 32 heads,
+// 16-byte pieces of a whole page, up to eight.  Pages of 64 tokens, 1 / 2 / 4 / 8 warps: 8 prompts of up to 2600 tokens, 32 heads,
 // 139 / 118 / 103 / 118 us; a decode step of 64 sequences 8.9 / 9.3 / 10.0 / 11.3 us (append and gather together).
 template <int HD, int CODE, bool BF16>
 es_status_t launch_append(const AppendParams& p, bool whole_pages, cudaStream_t s) {
