@@ -120,6 +120,7 @@ int64_t row_stride(const at::Tensor& t, const char* name) {
   int64_t step = 0, span = 0;
   for (int i = n - 3; i >= 0; --i) {
     if (size[i] == 1) continue;
+    if (stride[i] <= 0) refuse(std::string("the rows of ") + name + " must lie one after the other (no expanded dimensions)");
     if (span && stride[i] != span) refuse(std::string("the rows of ") + name + " must be evenly spaced");
     if (!step) step = stride[i];
     span = stride[i] * size[i];

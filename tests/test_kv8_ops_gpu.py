@@ -608,6 +608,66 @@ def test_calls_refuse_what_they_cannot_take(B):
     refused(B.es_op_kv_plan, _i32([0] * 8193).cuda(), _i32([0] * 8193).cuda(), _i32([[0]] * 8193).cuda(), 16, 4, status=3)
 
 
+def test_calls_refuse_expanded_rows(B):
+    """Rows that all lie in one place have no row stride: taken for dense they would be read beyond the tensor's end."""
+    q, kc, vc, ks, vs, table, ctx, max_ctx = [t.cuda() if torch.is_tensor(t) else t for t in _attn_case(2, 3, 4, 2, 64, 16, [20, 30], "int8", "fp16", 61)]
+    slots = _i32([0, 1, 2]).cuda()
+    k = torch.zeros(3, 2, 64, dtype=torch.float16, device="cuda")
+    for bad in (q[:1].expand(2, 3, 4, 64), q[:, :1].expand(2, 3, 4, 64), q[:1, :1].expand(2, 3, 4, 64), q[:1, 0].expand(2, 4, 64)):
+        with pytest.raises(B.EsError):
+            B.es_op_decode_attention_kv8(bad, kc, vc, ks, vs, table, ctx, max_ctx)
+    for a, b in ((k[:1].expand(3, 2, 64), k[:1].expand(3, 2, 64)), (k, k[:1].expand(3, 2, 64)), (k[:, :1].expand(3, 2, 64), k)):
+        with pytest.raises(B.EsError):
+            B.es_op_kv8_append(a, b, slots, kc, vc, ks, vs)
+    B.es_op_decode_attention_kv8(q[:1].expand(1, 3, 4, 64), kc, vc, ks, vs, table[:1], ctx[:1], max_ctx)      # one of them is no expansion
+
+
+def test_pools_beyond_32_bit_offsets(B):
+    """4.6 GB of codes each: pages on both sides of 2^31 and 2^32 bytes."""
+    n_pages, Hkv, P, hd = 70000, 8, 64, 128
+    pages = [69999, 2, 65536, 32768, 65535, 32767]
+    g = _gen(83)
+    kp, vp = (torch.empty(n_pages, Hkv, P, hd, dtype=torch.int8, device="cuda") for _ in range(2))
+    ks, vs = (torch.zeros(n_pages, Hkv, device="cuda") for _ in range(2))
+    n = 6 * P - 7
+    k, v = (torch.randn(n, Hkv, hd, generator=g).half() for _ in range(2))
+    place = [(pages[i // P], i % P) for i in range(n)]
+    slots = _i32([p * P + o for p, o in place])
+    B.es_op_kv8_append(k.cuda(), v.cuda(), slots.cuda(), kp, vp, ks, vs)
+    small = [(torch.zeros(6, Hkv, P, hd, dtype=torch.int8), torch.zeros(6, Hkv)) for _ in range(2)]
+    local = list(range(n))
+    back = B.es_op_kv8_gather(slots.cuda(), kp, vp, ks, vs, dtype=torch.float32)
+    for x, (c, s), dc, ds, got in zip((k, v), small, (kp, vp), (ks, vs), back):
+        R.append(x, local, c, s, P)
+        at = torch.tensor(pages, device="cuda")
+        rows = lambda t: t.transpose(1, 2).reshape(6 * P, Hkv, hd)[:n]
+        assert torch.equal(rows(dc[at].cpu()), rows(c)) and torch.equal(ds[at].cpu(), s)
+        assert torch.equal(got.cpu(), rows(c.float() * s[:, :, None, None]))
+    q = torch.randn(1, 1, 16, hd, generator=g).half()
+    got = B.es_op_decode_attention_kv8(q.cuda(), kp, vp, ks, vs, _i32([pages]).cuda(), _i32([n]).cuda(), 6 * P)
+    _check_attn(B, (q, small[0][0], small[1][0], small[0][1], small[1][1], _i32([list(range(6))]), _i32([n]), 6 * P), got=got)
+
+
+def test_calls_of_two_streams_at_once(B):
+    """Attention with and without a second kernel and sampling, under way on two streams at a time: the results of one at a time."""
+    cases = [_attn_case(40, 1, 8, 8, 64, 16, [100 + 13 * i for i in range(40)], "int8", "fp16", 85), _attn_case(1, 1, 8, 2, 128, 64, [5000], "e4m3", "fp16", 86)]
+    dev = [[t.cuda() for t in c[:7]] + [c[7]] for c in cases]
+    x = [torch.randn(n, 33000, generator=_gen(87 + n)).cuda() for n in (3, 200)]
+    u = [torch.rand(t.shape[0], generator=_gen(89)).cuda() for t in x]
+    top = [torch.full((t.shape[0],), 0.9, device="cuda") for t in x]
+    want = [(B.es_op_decode_attention_kv8(*d), B.es_op_sample(y, r, top_p=p)) for d, y, r, p in zip(dev, x, u, top)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], [[], []]
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append((B.es_op_decode_attention_kv8(*dev[i]), B.es_op_sample(x[i], u[i], top_p=top[i])))
+    torch.cuda.synchronize()
+    for w, all_got in zip(want, got):
+        for a, (t, lp) in all_got:
+            assert torch.equal(a, w[0]) and torch.equal(t, w[1][0]) and torch.equal(lp, w[1][1])
+
+
 # ---- a run of them together --------------------------------------------------------------------------------------
 
 class _Loop:
