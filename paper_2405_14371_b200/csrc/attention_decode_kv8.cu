@@ -146,7 +146,6 @@ __device__ __forceinline__ int tiles_of(int ctx, int max_ctx) { return (min(max(
 
 template <int HD, int CODE, int NT, int TILE, int SUB, bool GROUPED>
 __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const __grid_constant__ Kv8Maps maps, const Kv8AttnParams p) {
-  pdl_launch_dependents();
   constexpr int AW = WARPS<HD, NT>, SL = SLOTS<HD, NT, TILE>;
   constexpr int J = HD / 64;             // 16-byte pieces of a K row per thread
   constexpr int D = HD / 8;              // dimensions of V per thread
@@ -179,6 +178,8 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
     prefetch_tmap(&maps.k);
     prefetch_tmap(&maps.v);
   }
+  pdl_wait();
+  pdl_launch_dependents();               // only now: the merge kernel reads the lengths before it waits
   Cursor c, ahead;
   int begin, end, me = 0;                // tiles of this warp, and its place among the warps
   if constexpr (GROUPED) {
@@ -712,6 +713,7 @@ __global__ void __launch_bounds__(128) kv8_merge_kernel(const Kv8AttnParams p, i
   }
   const int n = w1 - w0 + 1;
   pdl_wait();
+  pdl_launch_dependents();
   float acc[V], mm = -INFINITY, ll = 0.f;
 #pragma unroll
   for (int c = 0; c < V; ++c) acc[c] = 0.f;
@@ -806,18 +808,8 @@ es_status_t launch_sub(const Kv8Maps& maps, const Kv8AttnParams& p, cudaStream_t
   auto kern = kv8_attn_kernel<HD, CODE, NT, TILE, SUB, GROUPED>;
   static std::atomic<uint64_t> allowed{0};
   ES_CUDA_CHECK(allow_shared_memory(kern, RINGS + (GROUPED ? INBOX : (KV8_MAX_B + 1) * (int)sizeof(int)), &allowed));
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(GROUPED ? p.B * p.Hkv * p.row_tiles * p.group : sm_count());
-  cfg.blockDim = dim3(AW * 32);
-  cfg.dynamicSmemBytes = RINGS + (GROUPED ? (p.group > 1 ? INBOX : 0) : (size_t)(p.B + 1) * sizeof(int));
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = p.group;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = GROUPED && p.group > 1 ? 1 : 0;
-  ES_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kern, maps, p));
+  ES_CUDA_CHECK(launch_clusters(kern, GROUPED && p.group > 1 ? p.group : 0, dim3(GROUPED ? p.B * p.Hkv * p.row_tiles * p.group : sm_count()), dim3(AW * 32),
+                                RINGS + (GROUPED ? (p.group > 1 ? INBOX : 0) : (size_t)(p.B + 1) * sizeof(int)), s, true, maps, p));
   if (!GROUPED && p.max_ctx > TILE)
     ES_CUDA_CHECK(launch_kernel(kv8_merge_kernel<HD, TILE>, dim3(p.Hq, p.T, p.B), dim3(128), 0, s, true, p, AW * sm_count()));
   return ES_OK;

@@ -9,7 +9,7 @@
 // Bound: append reads two bytes and writes one per value, gather the reverse.  8 prompts of up to 2600 tokens behind up to 300,
 // 32 heads of 128 (256 MB for append, 285 MB for gather), take 103 us together, 5.2 TB/s; append fills 60 % of the issue
 // slots beside that (two conversions, the scaling and the rounding of every value).  The newest token of 64 sequences of 8
-// heads, and all 3900 of theirs read back (24 MB), take 9.2 us: two launches and a chain of slot, scale and codes each.
+// heads, and all 3900 of theirs read back (24 MB), take 8.4 us: two launches and a chain of slot, scale and codes each.
 #include "es_internal.cuh"
 #include "kv8.cuh"
 #include "launch.cuh"
@@ -144,6 +144,7 @@ __global__ void __launch_bounds__(APPEND_THREADS, 4) kv8_append_kernel(const App
   // heads change fastest: the groups of a CTA share rows of the slot map and read one row's heads side by side
   const unsigned item = blockIdx.x * (APPEND_THREADS / GROUP) + threadIdx.x / GROUP;
   const int which = item / (unsigned)p.Hkv, h = item - which * p.Hkv;
+  pdl_launch_dependents();
   if (which >= p.n_items) return;                  // uniform over the group
   const int r0 = p.runs ? p.runs[which] : which;
   if (r0 < 0 || r0 >= p.n_rows) return;
@@ -239,14 +240,15 @@ es_status_t launch_append_warps(const AppendParams& p, cudaStream_t s) {
   constexpr int per = APPEND_THREADS / (32 * WARPS);
   const int64_t blocks = ((int64_t)p.n_items * p.Hkv + per - 1) / per;
   if ((int64_t)p.n_items * p.Hkv > INT32_MAX) return fail(ES_ERR_RANGE, "too many (run, head) items for one launch");
-  kv8_append_kernel<HD, CODE, BF16, WARPS><<<dim3((unsigned)blocks, 2), APPEND_THREADS, 0, s>>>(p);
-  ES_CUDA_CHECK(cudaGetLastError());
+  // not before the kernel in front has ended: CTAs of this one that wait early cost the 64 sequences and the gather in front of
+  // them 1.2 us (9.6 and 8.4 us for both; the gather itself begins early, which saves 0.6 us)
+  ES_CUDA_CHECK(launch_kernel(kv8_append_kernel<HD, CODE, BF16, WARPS>, dim3((unsigned)blocks, 2), dim3(APPEND_THREADS), 0, s, false, p));
   return ES_OK;
 }
 
 // A warp per item where stretches are short on average (a decode step: one row each); else as many as give a thread eight
 // 16-byte pieces of a whole page, up to eight.  Pages of 64 tokens, 1 / 2 / 4 / 8 warps: 8 prompts of up to 2600 tokens, 32 heads,
-// 139 / 118 / 103 / 118 us; a decode step of 64 sequences 8.9 / 9.3 / 10.0 / 11.3 us (append and gather together).
+// 139 / 118 / 103 / 118 us; a decode step of 64 sequences 8.9 / 9.3 / 10.0 / 11.3 us (with the gather that follows).
 template <int HD, int CODE, bool BF16>
 es_status_t launch_append(const AppendParams& p, bool whole_pages, cudaStream_t s) {
   const int warps = whole_pages ? p.P * (HD / 8) / 256 : 1;
@@ -310,6 +312,8 @@ __global__ void __launch_bounds__(GATHER_THREADS) kv8_gather_kernel(const Gather
   float sa[ROUNDS], sb[ROUNDS];
   int slot[ROUNDS];
   const int64_t first = (int64_t)blockIdx.x * (ROUNDS * GATHER_THREADS) + threadIdx.x;
+  pdl_wait();
+  pdl_launch_dependents();
 #pragma unroll
   for (int i = 0; i < ROUNDS; ++i) {
     const int64_t item = first + i * GATHER_THREADS;
@@ -347,9 +351,9 @@ es_status_t launch_gather(const GatherParams& p, int out, cudaStream_t s) {
   if (blocks > INT32_MAX || p.n_items / (HD / 8) > UINT32_MAX) return fail(ES_ERR_RANGE, "too many rows for one launch");
   const dim3 grid((unsigned)blocks);
   switch (out) {
-    case ES_DTYPE_F16: kv8_gather_kernel<HD, CODE, ES_DTYPE_F16><<<grid, GATHER_THREADS, 0, s>>>(p); break;
-    case ES_DTYPE_BF16: kv8_gather_kernel<HD, CODE, ES_DTYPE_BF16><<<grid, GATHER_THREADS, 0, s>>>(p); break;
-    default: kv8_gather_kernel<HD, CODE, ES_DTYPE_F32><<<grid, GATHER_THREADS, 0, s>>>(p);
+    case ES_DTYPE_F16: ES_CUDA_CHECK(launch_kernel(kv8_gather_kernel<HD, CODE, ES_DTYPE_F16>, grid, dim3(GATHER_THREADS), 0, s, true, p)); break;
+    case ES_DTYPE_BF16: ES_CUDA_CHECK(launch_kernel(kv8_gather_kernel<HD, CODE, ES_DTYPE_BF16>, grid, dim3(GATHER_THREADS), 0, s, true, p)); break;
+    default: ES_CUDA_CHECK(launch_kernel(kv8_gather_kernel<HD, CODE, ES_DTYPE_F32>, grid, dim3(GATHER_THREADS), 0, s, true, p));
   }
   ES_CUDA_CHECK(cudaGetLastError());
   return ES_OK;

@@ -120,6 +120,7 @@ __device__ __forceinline__ int slot_of(const PlanParams& p, int seq, int pos) {
 
 template <bool ROWS, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1) kv_plan_kernel(const PlanParams p) {
+  pdl_wait();
   pdl_launch_dependents();
   constexpr int WARPS = THREADS / 32;
   extern __shared__ int sm[];
@@ -272,6 +273,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) kv_plan_rows_kernel(const Pla
   int* row_off = sm;               // [B + 1]
   const int B = p.B, top = 1 << (31 - __clz(B));
   pdl_wait();
+  pdl_launch_dependents();
   for (int b = threadIdx.x; b <= B; b += PLAN_THREADS) row_off[b] = __ldcg(p.row_offsets + b);
   __syncthreads();
   const int rows_all = row_off[B];
@@ -360,18 +362,7 @@ es_status_t es_op_kv_plan(const int32_t* old_len, const int32_t* new_len, int32_
   static std::atomic<uint64_t> allowed[2];
   if (smem > 48 * 1024) ES_CUDA_CHECK(allow_shared_memory(kern, (int)((6 * PLAN_MAX_B + 4) * sizeof(int)), &allowed[small]));
   const int ranks = small ? 1 : plan_cluster();
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(ranks);
-  cfg.blockDim = dim3(few ? PLAN_FEW : PLAN_THREADS);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = (cudaStream_t)stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = ranks;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = ranks > 1 ? 1 : 0;
-  ES_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kern, p));
+  ES_CUDA_CHECK(launch_clusters(kern, small ? 0 : ranks, dim3(ranks), dim3(few ? PLAN_FEW : PLAN_THREADS), smem, (cudaStream_t)stream, true, p));
   if (!small) {
     const int blocks = (int)((max_rows + (long long)PLAN_THREADS - 1) / PLAN_THREADS);
     const int most = 2 * sm_count();

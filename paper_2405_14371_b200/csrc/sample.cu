@@ -642,6 +642,8 @@ __global__ void __launch_bounds__(RESIDENT ? 512 : 256, RESIDENT ? 2 : 4) sample
   cluster_arrive();                           // "this CTA runs": nobody writes into it before
   const int rank = (int)cl.block_rank(), row = blockIdx.x / ranks;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  pdl_wait();
+  pdl_launch_dependents();
   // the row's settings, wanted after the logits: their latencies pass together
   const float T = p.temperature ? p.temperature[row] : 1.f, tp = p.top_p ? p.top_p[row] : 1.f;
   const float mp = p.min_p ? fminf(fmaxf(p.min_p[row], 0.f), 1.f) : 0.f, u = fminf(fmaxf(p.u[row], 0.f), 1.f);
@@ -914,18 +916,8 @@ template <int DT, int ranks, bool RESIDENT>
 es_status_t launch_kind(const SampleParams& p, int B, cudaStream_t s) {
   static std::atomic<uint64_t> allowed{0};
   ES_CUDA_CHECK(allow_shared_memory(sample_kernel<DT, ranks, RESIDENT>, (int)sample_smem(MAX_SLICE, RESIDENT), &allowed));
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(B * ranks));
-  cfg.blockDim = dim3(Row<DT, ranks, RESIDENT>::ST);
-  cfg.dynamicSmemBytes = sample_smem(p.slice, RESIDENT);
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = ranks;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  ES_CUDA_CHECK(cudaLaunchKernelEx(&cfg, sample_kernel<DT, ranks, RESIDENT>, p));
+  ES_CUDA_CHECK(launch_clusters(sample_kernel<DT, ranks, RESIDENT>, ranks, dim3((unsigned)(B * ranks)), dim3(Row<DT, ranks, RESIDENT>::ST),
+                                sample_smem(p.slice, RESIDENT), s, true, p));
   return ES_OK;
 }
 

@@ -489,6 +489,28 @@ def test_sampling_matches_the_definition(B, n, V, dtype):
     _check_sample(B, x, u, T, k, p, m)
 
 
+@pytest.mark.parametrize("dtype,n,V", [(torch.float32, 700, 1100), (torch.bfloat16, 310, 20001), (torch.float16, 160, 30000), (torch.float32, 80, 60001),
+                                        (torch.bfloat16, 40, 130003), (torch.float32, 300, 17000)])
+def test_sampling_many_rows(B, n, V, dtype):
+    """More CTAs than run at once, so slices are read again from L2: clusters of 1 to 8 and the larger slices of large calls; rows
+    of ties among them (plateaus longer than any list, across the borders of top-k and top-p)."""
+    g, rng = _gen(n + V), random.Random(n * V)
+    x = torch.randn(n, V, generator=g) * (0.5 + 4 * torch.rand(n, 1, generator=g))
+    x[::7] = (x[::7] * 2).round() / 2
+    x[3::11] = (torch.arange(V) % 3).float()
+    x[5::13] = 0.0
+    x[8::17, V // 3:] = -math.inf
+    x = x.to(dtype)
+    u = torch.rand(n, generator=g).tolist()
+    T = [rng.choice([0.0, 0.3, 0.7, 1.0, 1.7]) for _ in range(n)]
+    k = [rng.choice([0, 1, 2, 50, 190, 300, 5000, V - 1, V + 3]) for _ in range(n)]
+    p = [rng.choice([0.1, 0.5, 0.9, 0.99, 1.0]) for _ in range(n)]
+    m = [rng.choice([0.0, 0.01, 0.2]) for _ in range(n)]
+    _check_sample(B, x, u, k=k)
+    _check_sample(B, x, u, p=p)
+    _check_sample(B, x, u, T, k, p, m)
+
+
 @pytest.mark.parametrize("V", [7, 1000, 40000])
 def test_sampling_ties_go_to_the_lowest_index(B, V):
     """All logits equal, two values, a plateau across the border of top-k and of top-p."""
@@ -666,6 +688,62 @@ def test_calls_of_two_streams_at_once(B):
     for w, all_got in zip(want, got):
         for a, (t, lp) in all_got:
             assert torch.equal(a, w[0]) and torch.equal(t, w[1][0]) and torch.equal(lp, w[1][1])
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_calls_wait_for_what_another_stream_made(B, captured):
+    """Every call follows one of its own kind on its stream and an event of another stream, on which its input is still being
+    made: called one by one and as a captured fork and join."""
+    case = _attn_case(3, 1, 8, 2, 128, 64, [900, 40, 3000], "int8", "fp16", 93)
+    dev = [t.cuda() for t in case[:7]]
+    n = 3000
+    fresh = [t.clone() for t in dev]
+    rows = torch.randn(64, 2, 128, generator=_gen(94)).half().cuda()
+    logits, u = torch.randn(5, 40000, generator=_gen(95)).cuda(), torch.rand(5, generator=_gen(96)).cuda()
+    slots, lens, table = _i32(list(range(64, 128))).cuda(), _i32([5, 6]).cuda(), _i32([[0], [1]]).cuda()
+    slow, pages = torch.zeros(64 << 20, device="cuda"), [torch.zeros_like(dev[1][:3]) for _ in range(2)]
+    scales = [torch.zeros_like(dev[3][:3]) for _ in range(2)]
+    made = [torch.zeros_like(t) for t in (dev[0], rows, logits, lens)]
+
+    def work():
+        main, side = torch.cuda.current_stream(), torch.cuda.Stream()
+        out = []
+        for i, call in enumerate((lambda x: B.es_op_decode_attention_kv8(x, *dev[1:], n), lambda x: B.es_op_kv8_append(x, x, slots, *pages, *scales),
+                                  lambda x: B.es_op_sample(x, u), lambda x: B.es_op_kv_plan(x, x + 3, table, 16, 8, n_pages=2))):
+            source = (fresh[0], rows, logits, lens)[i]
+            side.wait_stream(main)
+            with torch.cuda.stream(side):
+                for _ in range(8):
+                    slow.add_(1.0)
+                made[i].copy_(source)
+            call(source)
+            main.wait_stream(side)
+            out.append(call(made[i]))
+        out.append(B.es_op_kv8_gather(slots, *pages, *scales))
+        for _ in range(4):
+            slow.add_(1.0)
+        return out
+
+    flat = lambda out: [t for o in out if o is not None for t in ((o,) if torch.is_tensor(o) else o)]  # noqa: E731
+    for t in made:
+        t.zero_()
+    want = flat(work())                                 # warm; every call here is made on equal inputs, so its result is what counts
+    torch.cuda.synchronize()
+    want = [t.clone() for t in want]
+    assert torch.equal(want[0], B.es_op_decode_attention_kv8(*dev, n)) and torch.equal(want[1], B.es_op_sample(logits, u)[0])
+    if captured:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = flat(work())
+    for _ in range(5):
+        for t in made:
+            t.zero_()
+        if captured:
+            graph.replay()
+        else:
+            got = flat(work())
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
 # ---- a run of them together --------------------------------------------------------------------------------------
