@@ -36,22 +36,27 @@ constexpr int PLAN_MAX_B = 8192;
 struct PlanParams {
   const int *old_len, *new_len;
   int *table, *free_pages, *free_count;
-  int B, pps, P, n_pages, max_rows, max_runs;
+  int B, pps, P, log2P, n_pages, max_rows, max_runs;
   int *row_offsets, *slot_map, *positions, *row_seq, *runs, *len_out;
 };
 
-struct Sums { long long give, rows, need; };
+// Pages given up and gained are entries of the table, at most 2^30.  Rows stop counting at `full`, one more than there is
+// room for; sums of such numbers are the same in any order.
+struct Sums { uint32_t give, rows, need; };
 
-__device__ __forceinline__ Sums add(const Sums& a, const Sums& b) { return {a.give + b.give, a.rows + b.rows, a.need + b.need}; }
+__device__ __forceinline__ Sums add(const Sums& a, const Sums& b, uint32_t full) { return {a.give + b.give, min(a.rows + b.rows, full), a.need + b.need}; }
+
+// pages of a sequence
+__device__ __forceinline__ int pages_of(const PlanParams& p, int len) { return (int)(((uint32_t)len + (uint32_t)p.P - 1) >> p.log2P); }
 
 // inclusive scan over the block; `total` is the block's sum.  All threads call.
 template <int WARPS>
-__device__ __forceinline__ Sums block_scan(Sums v, Sums* warp_sums, Sums* total) {
+__device__ __forceinline__ Sums block_scan(Sums v, Sums* warp_sums, Sums* total, uint32_t full) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
     const Sums o = {__shfl_up_sync(~0u, v.give, d), __shfl_up_sync(~0u, v.rows, d), __shfl_up_sync(~0u, v.need, d)};
-    if (lane >= d) v = add(v, o);
+    if (lane >= d) v = add(v, o, full);
   }
   if (lane == 31) warp_sums[warp] = v;
   __syncthreads();
@@ -60,12 +65,12 @@ __device__ __forceinline__ Sums block_scan(Sums v, Sums* warp_sums, Sums* total)
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
       const Sums o = {__shfl_up_sync(~0u, w.give, d), __shfl_up_sync(~0u, w.rows, d), __shfl_up_sync(~0u, w.need, d)};
-      if (lane >= d) w = add(w, o);
+      if (lane >= d) w = add(w, o, full);
     }
     if (lane < WARPS) warp_sums[lane] = w;
   }
   __syncthreads();
-  if (warp > 0) v = add(v, warp_sums[warp - 1]);
+  if (warp > 0) v = add(v, warp_sums[warp - 1], full);
   *total = warp_sums[WARPS - 1];
   __syncthreads();
   return v;
@@ -110,12 +115,10 @@ __device__ __forceinline__ int owner(const int* off, int B, int top, int i) {
 
 constexpr int FLIGHT = 4;          // items of a thread under way at a time
 
-__device__ __forceinline__ int clip(long long v, int most) { return v < most ? (int)v : most; }
-
 // slot of a position, -1 where the table holds no page
 __device__ __forceinline__ int slot_of(const PlanParams& p, int seq, int pos) {
-  const int lp = pos / p.P, page = __ldcg(p.table + (int64_t)seq * p.pps + lp);
-  return page >= 0 && page < p.n_pages ? page * p.P + (pos - lp * p.P) : -1;
+  const int lp = pos >> p.log2P, page = __ldcg(p.table + (int64_t)seq * p.pps + lp);
+  return page >= 0 && page < p.n_pages ? page * p.P + (pos & (p.P - 1)) : -1;
 }
 
 template <bool ROWS, int THREADS>
@@ -141,6 +144,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_plan_kernel(const PlanParams p)
   // ---- the sums (every CTA for itself) ----
   int have = 0;
   if (alloc) { have = __ldcg(p.free_count); have = have < 0 ? 0 : min(have, p.n_pages); }
+  const uint32_t full = (uint32_t)p.max_rows + 1;
   Sums carry = {0, 0, 0};
   if (tid == 0) { row_off[0] = 0; need_off[0] = 0; give_off[0] = 0; run_off[0] = 0; }
   for (int base = 0; base < B; base += THREADS) {
@@ -149,19 +153,19 @@ __global__ void __launch_bounds__(THREADS, 1) kv_plan_kernel(const PlanParams p)
     if (b < B) { o = __ldcg(p.old_len + b); n = __ldcg(p.new_len + b); }
     const bool ok = o >= 0 && o <= cap && n >= 0 && n <= cap;
     const int oo = ok ? o : 0, nn = ok ? n : 0;
-    const int po = (int)(((long long)oo + P - 1) / P), pn = (int)(((long long)nn + P - 1) / P);
-    Sums v = {max(po - pn, 0), max(nn - oo, 0), max(pn - po, 0)}, total;
-    v = add(block_scan<WARPS>(v, warp_sums, &total), carry);
+    const int po = pages_of(p, oo), pn = pages_of(p, nn);
+    Sums v = {(uint32_t)max(po - pn, 0), min((uint32_t)max(nn - oo, 0), full), (uint32_t)max(pn - po, 0)}, total;
+    v = add(block_scan<WARPS>(v, warp_sums, &total, full), carry, full);
     if (b < B) {
       s_old[b] = o;
       s_new[b] = ok ? n : o;
-      give_off[b + 1] = alloc ? clip(v.give, INT_MAX) : 0;
-      row_off[b + 1] = clip(v.rows, p.max_rows + 1);        // one more than there is room marks "does not fit"
-      need_off[b + 1] = clip(v.need, INT_MAX);
+      give_off[b + 1] = alloc ? (int)v.give : 0;
+      row_off[b + 1] = (int)v.rows;
+      need_off[b + 1] = (int)v.need;
     }
-    carry = add(carry, total);
+    carry = add(carry, total, full);
   }
-  const int given = alloc ? clip(carry.give, INT_MAX) : 0;
+  const int given = alloc ? (int)carry.give : 0;
   const long long avail = (long long)have + given;
   __syncthreads();
 
@@ -173,9 +177,9 @@ __global__ void __launch_bounds__(THREADS, 1) kv_plan_kernel(const PlanParams p)
     if (b < B) {
       const int o = s_old[b], n = s_new[b];
       if (n > o) {                                          // gains rows (a request with lengths out of range has n == o)
-        const bool need = (n - 1) / P > (o - 1 + P) / P - 1;       // last page wanted against last page held
+        const bool need = pages_of(p, n) > pages_of(p, o);
         const bool fits = row_off[b + 1] <= p.max_rows && (!alloc || !need || need_off[b + 1] <= avail);
-        if (fits) n_runs = (n - 1) / P - o / P + 1;
+        if (fits) n_runs = ((n - 1) >> p.log2P) - (o >> p.log2P) + 1;
         else s_new[b] = o;
       }
     }
@@ -202,7 +206,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_plan_kernel(const PlanParams p)
   // ---- pages: pops into the table, left-over returns onto the stack ----
   auto returned = [&](int i) -> int {
     const int b = owner(give_off, B, top, i);
-    const int entry = (int)(((long long)s_new[b] + P - 1) / P) + i - give_off[b];
+    const int entry = pages_of(p, s_new[b]) + i - give_off[b];
     return __ldcg(p.table + (int64_t)b * p.pps + entry);
   };
   if (alloc) {
@@ -219,7 +223,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_plan_kernel(const PlanParams p)
         const int i = base + j * stride;
         if (i >= taken) break;
         const int b = owner(need_off, B, top, i);
-        p.table[(int64_t)b * p.pps + (int)(((long long)s_old[b] + P - 1) / P) + i - need_off[b]] = page[j];
+        p.table[(int64_t)b * p.pps + pages_of(p, s_old[b]) + i - need_off[b]] = page[j];
       }
     }
     for (int i = first; i < given - taken; i += stride)
@@ -231,7 +235,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_plan_kernel(const PlanParams p)
 
   for (int i = first; i < given; i += stride) {
     const int b = owner(give_off, B, top, i);
-    p.table[(int64_t)b * p.pps + (int)(((long long)s_new[b] + P - 1) / P) + i - give_off[b]] = -1;
+    p.table[(int64_t)b * p.pps + pages_of(p, s_new[b]) + i - give_off[b]] = -1;
   }
   if (alloc && first == 0) *p.free_count = (int)min(avail - taken, (long long)p.n_pages);
   for (int b = first; b <= B; b += stride) p.row_offsets[b] = min(row_off[b], p.max_rows);
@@ -243,7 +247,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_plan_kernel(const PlanParams p)
       const int i = base + j * stride;
       row[j] = page[j] = -1;
       if (i < runs_before) {
-        const int b = owner(run_off, B, top, i), o = s_old[b], lp = o / P + (i - run_off[b]);
+        const int b = owner(run_off, B, top, i), o = s_old[b], lp = (o >> p.log2P) + (i - run_off[b]);
         page[j] = __ldcg(p.table + (int64_t)b * p.pps + lp);
         row[j] = row_off[b] + max(lp * P - o, 0);
       }
@@ -350,7 +354,9 @@ es_status_t es_op_kv_plan(const int32_t* old_len, const int32_t* new_len, int32_
     return fail(ES_ERR_RANGE, "pages_per_seq or n_pages times page_tokens exceeds 2^31 - 1");
   if (max_rows > (1 << 30)) return fail(ES_ERR_RANGE, "max_rows exceeds 2^30");
   if ((long long)B * pages_per_seq > (1 << 30)) return fail(ES_ERR_RANGE, "the block table has more than 2^30 entries");
-  PlanParams p{old_len, new_len, block_table, free_pages, free_count, B, pages_per_seq, page_tokens, n_pages, max_rows,
+  int log2P = 0;
+  while ((1 << log2P) < page_tokens) ++log2P;
+  PlanParams p{old_len, new_len, block_table, free_pages, free_count, B, pages_per_seq, page_tokens, log2P, n_pages, max_rows,
                es_op_kv_plan_max_runs(B, max_rows, page_tokens), row_offsets, slot_map, positions, row_seq, runs, len_out};
   const size_t smem = (size_t)(6 * B + 4) * sizeof(int);
   // One CTA as long as it writes the rows in about the time that a second launch costs: 1024 rows take 5.5 - 6.0 us by
