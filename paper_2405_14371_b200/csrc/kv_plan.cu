@@ -11,7 +11,7 @@
 //
 // One cluster does it all: every CTA scans the lengths for itself (a few KB out of L2, cheaper than handing sums around),
 // then the CTAs share the page work, meet once, and share the rest.  The meeting orders table writes before the rows that
-// read them, and the reads of returned entries before their clearing.  Small calls are bound by latency and run as one CTA
+// read them.  Small calls are bound by latency and run as one CTA
 // that makes the rows too; large ones leave the rows (12 bytes each) to a second kernel over the whole machine.
 //
 // Bound by latency: 64 decoding requests take 4.8 us a call (a dependent chain of lengths, sums, stack, table and rows
@@ -203,40 +203,51 @@ __global__ void __launch_bounds__(THREADS, 1) kv_plan_kernel(const PlanParams p)
   const int rows_all = min(row_off[B], p.max_rows);
   const int stride = THREADS * ranks, first = rank * THREADS + tid;
 
-  // ---- pages: pops into the table, left-over returns onto the stack ----
-  auto returned = [&](int i) -> int {
+  // ---- pages: pops into the table, left-over returns onto the stack; who reads a returned entry, and only one does, clears it ----
+  auto returned = [&](int i) -> int* {
     const int b = owner(give_off, B, top, i);
-    const int entry = pages_of(p, s_new[b]) + i - give_off[b];
-    return __ldcg(p.table + (int64_t)b * p.pps + entry);
+    return p.table + (int64_t)b * p.pps + pages_of(p, s_new[b]) + i - give_off[b];
   };
   if (alloc) {
     for (int base = first; base < taken; base += FLIGHT * stride) {
-      int page[FLIGHT];
+      int page[FLIGHT], *from[FLIGHT];
 #pragma unroll
       for (int j = 0; j < FLIGHT; ++j) {
         const int i = base + j * stride;
         const long long v = avail - 1 - i;
-        page[j] = i >= taken ? -1 : v < have ? __ldcg(p.free_pages + v) : returned((int)(v - have));
+        page[j] = -1;
+        from[j] = i < taken && v >= have ? returned((int)(v - have)) : nullptr;
+        if (i < taken) page[j] = __ldcg(from[j] ? from[j] : p.free_pages + v);
       }
 #pragma unroll
       for (int j = 0; j < FLIGHT; ++j) {
         const int i = base + j * stride;
         if (i >= taken) break;
+        if (from[j]) *from[j] = -1;
         const int b = owner(need_off, B, top, i);
         p.table[(int64_t)b * p.pps + pages_of(p, s_old[b]) + i - need_off[b]] = page[j];
       }
     }
-    for (int i = first; i < given - taken; i += stride)
-      if (have + (long long)i < p.n_pages) p.free_pages[have + i] = returned(i);
+    for (int base = first; base < given - taken; base += FLIGHT * stride) {
+      int page[FLIGHT], *from[FLIGHT];
+#pragma unroll
+      for (int j = 0; j < FLIGHT; ++j) {
+        from[j] = base + j * stride < given - taken ? returned(base + j * stride) : nullptr;
+        if (from[j]) page[j] = __ldcg(from[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < FLIGHT; ++j) {
+        if (!from[j]) break;
+        *from[j] = -1;
+        const long long at = have + (long long)base + j * stride;
+        if (at < p.n_pages) p.free_pages[at] = page[j];
+      }
+    }
   }
 
-  // ---- the CTAs meet: table entries written above are read below, returned entries read above are cleared below ----
+  // ---- the CTAs meet: table entries written above are read below ----
   if (ranks > 1) cg::this_cluster().sync(); else __syncthreads();
 
-  for (int i = first; i < given; i += stride) {
-    const int b = owner(give_off, B, top, i);
-    p.table[(int64_t)b * p.pps + pages_of(p, s_new[b]) + i - give_off[b]] = -1;
-  }
   if (alloc && first == 0) *p.free_count = (int)min(avail - taken, (long long)p.n_pages);
   for (int b = first; b <= B; b += stride) p.row_offsets[b] = min(row_off[b], p.max_rows);
   for (int b = first; b < B; b += stride) p.len_out[b] = s_new[b];
