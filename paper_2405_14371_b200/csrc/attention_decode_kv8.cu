@@ -178,8 +178,6 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
     prefetch_tmap(&maps.k);
     prefetch_tmap(&maps.v);
   }
-  pdl_wait();
-  pdl_launch_dependents();               // only now: the merge kernel reads the lengths before it waits
   Cursor c, ahead;
   int begin, end, me = 0;                // tiles of this warp, and its place among the warps
   if constexpr (GROUPED) {
@@ -187,6 +185,8 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
     c.b = item / items;
     c.kvh = in_b / p.row_tiles;
     c.rt = in_b - c.kvh * p.row_tiles;
+    pdl_wait();
+    pdl_launch_dependents();
     c.tiles = tiles_of<TILE>(p.ctx_len[c.b], p.max_ctx);
     const int workers = p.group * AW, per_warp = stretch_of(c.tiles, workers);
     begin = min((warp * p.group + (int)blockIdx.x % p.group) * per_warp, c.tiles);
@@ -194,6 +194,8 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
     c.tile = begin;
     __syncthreads();
   } else {
+    pdl_wait();
+    pdl_launch_dependents();             // only now: the merge kernel reads the lengths before it waits
     int before = 0;
     if (p.B <= 32) {                     // every warp for itself, all writing the same
       const int v = lane < p.B ? tiles_of<TILE>(p.ctx_len[lane], p.max_ctx) : 0;

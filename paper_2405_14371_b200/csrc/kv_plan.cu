@@ -11,13 +11,13 @@
 //
 // One cluster does it all: every CTA scans the lengths for itself (a few KB out of L2, cheaper than handing sums around),
 // then the CTAs share the page work, meet once, and share the rest.  The meeting orders table writes before the rows that
-// read them.  Small calls are bound by latency and run as one CTA
-// that makes the rows too; large ones leave the rows (12 bytes each) to a second kernel over the whole machine.
+// read them.  Small calls are bound by latency and run as one CTA that makes the rows too; large ones leave the rows (12
+// bytes each) to a second kernel over the whole machine.
 //
-// Bound by latency: 64 decoding requests take 4.8 us a call (a dependent chain of lengths, sums, stack, table and rows
-// with five barriers in it).  1024 requests of which a tenth brings prompts (75 000 rows) and a tenth
-// returns 25 000 pages, and the same back (410 000 rows), take 33 us for both calls (7 MB, 1 us at the copy rate): 15 us
-// each in the cluster, most of it the searches for the owner of every page (issue slots of 16 SMs), the rest the rows.
+// Bound by latency: 64 decoding requests take 4.0 us a call (a dependent chain of lengths, sums, stack, table and rows
+// with barriers in it).  1024 requests of which a tenth brings prompts (75 000 rows) and a tenth returns 25 000 pages, and
+// the same back (410 000 rows), take 27 us for both calls (7 MB, 1 us at the copy rate): 9 us each in the cluster, sums and
+// three rounds of search, read and write, the rest the rows.
 #include <cooperative_groups.h>
 #include <limits.h>
 
@@ -310,7 +310,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) kv_plan_rows_kernel(const Pla
 }
 
 // CTAs of a large call's cluster: 16 where the device places such clusters (their shared work is bound by issue slots; a
-// call that returns 25 000 pages and one that takes as many: 33 us together, with 8 39 us), else the portable 8.
+// call that returns 25 000 pages and one that takes as many: 27 us together, with 8 30 us), else the portable 8.
 int plan_cluster() {
   static std::atomic<int> known[64];
   int dev = 0;
@@ -370,11 +370,11 @@ es_status_t es_op_kv_plan(const int32_t* old_len, const int32_t* new_len, int32_
   PlanParams p{old_len, new_len, block_table, free_pages, free_count, B, pages_per_seq, page_tokens, log2P, n_pages, max_rows,
                es_op_kv_plan_max_runs(B, max_rows, page_tokens), row_offsets, slot_map, positions, row_seq, runs, len_out};
   const size_t smem = (size_t)(6 * B + 4) * sizeof(int);
-  // One CTA as long as it writes the rows in about the time that a second launch costs: 1024 rows take 5.5 - 6.0 us by
-  // themselves and 6.9 - 7.4 us with the second kernel, 4096 rows 7.7 - 9.3 us and 7.2 - 8.2 us.  128 threads for the
-  // smallest: 64 requests of one row 4.8 us, with 1024 threads 6.0 us.
+  // One CTA as long as it writes the rows in less than the time that a cluster and a second launch cost: 1024 rows take 4.1 -
+  // 4.3 us in one CTA and 5.8 - 6.2 us in two kernels, 2048 4.9 - 5.2 and 6.2 - 6.4, 4096 5.7 - 7.2 and 6.0 - 6.7.  128
+  // threads for the smallest: 64 requests of one row 3.5 us, with 1024 threads 4.3 us; of eight rows 5.0 and 4.5 us.
   const bool small = max_rows <= 2048;
-  const bool few = small && max_rows <= 4 * PLAN_FEW && B <= PLAN_FEW;
+  const bool few = small && max_rows <= 2 * PLAN_FEW && B <= PLAN_FEW;
   auto kern = few ? kv_plan_kernel<true, PLAN_FEW> : small ? kv_plan_kernel<true, PLAN_THREADS> : kv_plan_kernel<false, PLAN_THREADS>;
   static std::atomic<uint64_t> allowed[2];
   if (smem > 48 * 1024) ES_CUDA_CHECK(allow_shared_memory(kern, (int)((6 * PLAN_MAX_B + 4) * sizeof(int)), &allowed[small]));
