@@ -28,10 +28,10 @@
 // bf16 queries are brought to fp16 by a power of two per row (largest magnitude to [1, 2)): 11 bits hold bf16's 8, and
 // what underflows is below 2^-24 of the row's largest.
 //
-// Measured: 32 sequences of 500 to 8191 tokens, 64 / 8 heads of 128 (286 MB): 59.4 us = 4.8 TB/s, of which the merge kernel
+// Measured: 32 sequences of 500 to 8191 tokens, 64 / 8 heads of 128 (286 MB): 59.0 us = 4.8 TB/s, of which the merge kernel
 // 6.4 us; in the loop an SM takes in 23.4 bytes a clock, the rate at which memory feeds it (with the multiplications of the
 // low halves and the conversions left out it took no less).  8 sequences of 3 to 2500 with 4 draft tokens, 40 heads (103 MB):
-// 30.1 us.  16 of 1025 to 1152 (36 MB): 14.4 us.  One of 1000, 32 heads (8 MB): 6.4 us, of which about 3 us are the launch
+// 30.1 us.  16 of 1025 to 1152 (36 MB): 13.7 us.  One of 1000, 32 heads (8 MB): 5.9 us, of which about 3 us are the launch
 // and the chain from length to table to the first tile.
 //
 // Codes behind the context are zeroed in V and masked by selection in the scores, so that garbage (NaN codes among it)

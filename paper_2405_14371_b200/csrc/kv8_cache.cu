@@ -9,7 +9,7 @@
 // Bound: append reads two bytes and writes one per value, gather the reverse.  8 prompts of up to 2600 tokens behind up to 300,
 // 32 heads of 128 (256 MB for append, 285 MB for gather), take 103 us together, 5.2 TB/s; append fills 60 % of the issue
 // slots beside that (two conversions, the scaling and the rounding of every value).  The newest token of 64 sequences of 8
-// heads, and all 3900 of theirs read back (24 MB), take 8.4 us: two launches and a chain of slot, scale and codes each.
+// heads, and all 3900 of theirs read back (24 MB), take 9.0 us: two launches and a chain of slot, scale and codes each.
 #include "es_internal.cuh"
 #include "kv8.cuh"
 #include "launch.cuh"

@@ -18,8 +18,8 @@
 // is exact whatever its order: thresholds and tokens depend on the inputs alone, and the borders are as sharp as the
 // exponential (2^-39).
 //
-// Measured, unrestricted / top_k 50 / top_p 0.9: one row of 32000 6.0 / 9.6 / 14.3 us, 64 rows 10.5 / 12.5 / 23.8 us, 256
-// rows of 128001 (131 MB, 20 us at the copy rate) 110 / 64 / 260 us.  Small calls are bound by the latency of the passes
+// Measured, unrestricted / top_k 50 / top_p 0.9: one row of 32000 5.6 / 9.1 / 13.7 us, 64 rows 10.0 / 12.2 / 24.0 us, 256
+// rows of 128001 (131 MB, 20 us at the copy rate) 111 / 64 / 260 us.  Small calls are bound by the latency of the passes
 // and the cluster's barriers between them; large ones by issue slots: a weight costs about 45 instructions, a third of
 // them 64-bit, and top-p asks for each twice (its histogram, and the draw), beside four additions to shared memory.
 //
