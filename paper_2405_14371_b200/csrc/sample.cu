@@ -25,7 +25,8 @@
 //
 // A row belongs to a cluster of 1 to 8 CTAs.  Where all CTAs of a call run at once, each holds its slice of the row in
 // shared memory as fp32: latency counts there.  Larger calls read the slice again from L2, which leaves room for four
-// CTAs on an SM, one's barriers under another's sums.
+// CTAs on an SM, one's barriers under another's sums (256 rows of 128001 with three and more registers each: 130 / 84 / 292
+// us).
 #include <cooperative_groups.h>
 #include <limits.h>
 
