@@ -67,6 +67,7 @@ struct Kv8AttnParams {
   int B, T, Hq, Hkv, G, P, log2P, pps, n_pages, max_ctx;
   int row_tiles, rows, bf16;             // rows = rows of a row tile that are stored
   int group;                             // CTAs of an item (groups)
+  int give_up;                           // every warp's first wait counts as run out
 };
 
 struct alignas(64) Kv8Maps { CUtensorMap k, v; };
@@ -283,7 +284,7 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
   uint32_t qa[NT][8 * J];
   float o[NT][NM][4], m_run[NT], l_run[NT];
   int ctx = 0, item_begin = 0;
-  bool fresh = false, running = true;
+  bool fresh = false, running = !p.give_up;
   // query rows of the item at hand; row r of the row tile is token r / G, head kv_head * G + r % G
   auto load_q = [&]() {
 #pragma unroll
@@ -337,7 +338,8 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
   if (SL == 3 && asked < n_half) ask(ks_a, vs_a);          // the second tile's K, whose scales wait in ks_a, vs_a
   start_item(begin);
 
-  for (int at = begin; at < end && running; ++at) {
+  int at = begin;
+  for (; at < end && running; ++at) {
     if (fresh) {
       fresh = false;
       load_q();
@@ -571,13 +573,38 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
     }
     c.next(pre, p.B, p.Hkv, p.row_tiles);
   }
-  // a wait that ran out: let this warp's copies that are under way land before its shared memory goes
-  if (!running)
+  // A wait ran out.  These calls have no status word: every row that this warp was to finish or to hand over becomes NaN (a
+  // sum that is NaN stays so through both joins), so that nothing it did not compute looks like a result.
+  if (!running) {
+    if constexpr (GROUPED) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) l_run[n] = NAN;
+    } else {
+      for (; at < end; ++at) {
+        const bool item_ends = c.tile + 1 == c.tiles;
+        if (item_ends || at + 1 == end) {
+          const int i = c.rt * ROWS + lane, token = i / p.G;
+          if (lane < ROWS && i < n_rows) {
+            if (item_ends && item_begin >= begin) {
+              uint32_t* to = reinterpret_cast<uint32_t*>(p.out) + (((int64_t)c.b * p.T + token) * p.Hq + c.kvh * p.G + (i - token * p.G)) * (HD / 2);
+              for (int k = 0; k < HD / 2; ++k) to[k] = two_outputs(NAN, NAN, p.bf16);
+            } else {
+              const int64_t part = 2 * (int64_t)me + (item_begin >= begin);
+              *reinterpret_cast<float2*>(p.part_ml + (part * p.rows + lane) * 2) = make_float2(0.f, NAN);
+            }
+          }
+          item_begin = at + 1;
+        }
+        c.next(pre, p.B, p.Hkv, p.row_tiles);
+      }
+    }
+    // and its copies that are under way land before its shared memory goes
     for (; used < asked; ++used) {
       int nobody = 0;
       mbar_wait(my_bars + slot * 8, parity, &nobody, nullptr, 1);
       if (++slot == SL) { slot = 0; parity ^= 1; }
     }
+  }
   if constexpr (GROUPED) {
     // ---- the warps of the CTA, then the CTAs of the item, join in order ----
     // a warp's part goes over its ring, which nothing writes any more: o [ROWS][HD] (zero where it had no tile)
@@ -892,7 +919,8 @@ es_status_t es_op_decode_attention_kv8(const void* q, int32_t dtype, int64_t q_s
   float* part = (float*)scratch;
   const size_t parts = parts_of(sh);
   Kv8AttnParams p{q, q_stride, k_scale, v_scale, block_table, ctx_len, out, part, part + parts * hd, B, T, Hq, Hkv, Hq / Hkv,
-                  page_tokens, log2P, pages_per_seq, n_pages, max_ctx, sh.row_tiles, sh.rows, dtype == ES_DTYPE_BF16, sh.group};
+                  page_tokens, log2P, pages_per_seq, n_pages, max_ctx, sh.row_tiles, sh.rows, dtype == ES_DTYPE_BF16, sh.group,
+                  tunables().kv8_give_up};
   cudaStream_t s = (cudaStream_t)stream;
   if (hd == 128) return code == CODE_I8 ? launch<128, CODE_I8>(maps, p, sh, s) : launch<128, CODE_E4M3>(maps, p, sh, s);
   return code == CODE_I8 ? launch<64, CODE_I8>(maps, p, sh, s) : launch<64, CODE_E4M3>(maps, p, sh, s);

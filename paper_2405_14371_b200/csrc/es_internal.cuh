@@ -41,6 +41,7 @@ struct Tunables {
   int ks_cols;             // ES_KS_COLS: column ranges per K slice of that kernel (0 = chosen per shape)
   int attn_split_tokens;   // ES_ATTN_SPLIT_TOKENS: smallest split of a decode-attention context (tokens; 0 = 256, or 384 for groups of 4-8 query heads)
   int debug_checks;        // ES_DEBUG: es_shard_device_status also verifies the guard bytes behind every scratch region and the ranges of the page table, context lengths and slot list (1) or not (0, default)
+  int kv8_give_up;         // ES_KV8_GIVE_UP: the waits inside the 8-bit decode attention count as run out (1, for the test of what follows) or not (0, default)
   int even_grid;           // ES_EVEN_GRID: weight-streaming kernels shrink their grid so that every CTA (warp) gets the same number of units (1) or fill the machine (0)
 };
 const Tunables& tunables();

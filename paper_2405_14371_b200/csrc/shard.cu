@@ -54,6 +54,7 @@ const Tunables& tunables() {
     v.ks_splits = env_int("ES_KS_SPLITS", 0);
     v.ks_cols = env_int("ES_KS_COLS", 0);
     v.attn_split_tokens = env_int("ES_ATTN_SPLIT_TOKENS", 0);
+    v.kv8_give_up = env_int("ES_KV8_GIVE_UP", 0);
     v.even_grid = env_int("ES_EVEN_GRID", 0);
     v.debug_checks = env_int("ES_DEBUG", 0);
     return v;

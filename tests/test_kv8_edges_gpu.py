@@ -1,0 +1,41 @@
+"""The operations over the 8-bit cache at the edges of their definitions.  References in 64 bits or exact fractions."""
+import os
+import subprocess
+import sys
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- attention: a wait that runs out -----------------------------------------------------------------------------
+
+_RUN_OUT = """
+import torch
+from paper_2405_14371_b200 import binding as B
+from tests.test_kv8_ops_gpu import _attn_case
+
+def rows(*a, **kw):
+    case = _attn_case(*a, **kw)
+    out = B.es_op_decode_attention_kv8(*[t.cuda() for t in case[:7]], case[7])
+    torch.cuda.synchronize()
+    return out
+
+for code, dtype in (("int8", "fp16"), ("e4m3", "bf16")):
+    for args in ((1, 1, 8, 8, 128, 64, [2000]), (1, 1, 40, 40, 64, 16, [70]), (3, 1, 8, 1, 128, 16, [0, 1, 40]), (2, 5, 8, 2, 128, 32, [90, 300]),
+                 (20, 1, 8, 8, 128, 64, [1 + 150 * i for i in range(20)]), (20, 3, 32, 8, 128, 64, [1 + 150 * i for i in range(20)]),
+                 (40, 1, 16, 8, 64, 16, [1 + i % 16 for i in range(40)]), (20, 1, 8, 8, 128, 16, [9000] + [0] * 19)):
+        got = rows(*args, code, dtype, 5)
+        assert bool(got.isnan().all()), (args, code, int((~got.isnan()).sum()))
+tok, _ = B.es_op_sample(torch.zeros(2, 50, device="cuda"), torch.full((2,), 0.5, device="cuda"))
+assert tok.tolist() == [25, 25]
+print("all rows without a result")
+"""
+
+
+def test_attention_a_wait_that_runs_out_leaves_no_result():
+    """ES_KV8_GIVE_UP (read once per process, hence a child process): every first wait counts as run out.  The copies under way
+    still land before a CTA ends, the rows become NaN in both ways of sharing the tiles, and the device goes on working."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", _RUN_OUT], cwd=root, env=dict(os.environ, ES_KV8_GIVE_UP="1"), capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "all rows without a result" in r.stdout, r.stdout[-2000:] + r.stderr[-2000:]
