@@ -35,7 +35,8 @@
 // and the chain from length to table to the first tile.
 //
 // Codes behind the context are zeroed in V and masked by selection in the scores, so that garbage (NaN codes among it)
-// never meets a product; a page whose scale is NaN makes the rows that see it NaN.
+// never meets a product; a page whose scale is NaN makes the rows that see it NaN, a V code that is no number its dimension
+// of them.
 #include <cooperative_groups.h>
 #include <cuda.h>
 
@@ -438,6 +439,52 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int i = 0; i < NM; ++i) { o[n][i][0] *= al[n][0]; o[n][i][1] *= al[n][1]; o[n][i][2] *= al[n][0]; o[n][i][3] *= al[n][1]; }
+      }
+      // ---- a V code that is no number shows in the rows that see its token, and in no others (0 * NaN would be NaN there):
+      // where rows differ in what they see, it is written into their sums and taken out of the tile ----
+      if constexpr (CODE == CODE_E4M3) {
+        if (!inner && p.T > 1) {
+          const int n_tok = min(SUB, ctx - T0);
+          auto place = [&](int j) -> uint32_t {            // dimensions D g .. of token j of the sub-tile
+            const uint32_t line = HD == 128 ? sub * SUB + j : sub * (SUB / 2) + (j >> 1);
+            const uint32_t piece = HD == 128 ? g : 4 * (j & 1) + (g >> 1);
+            return vbase + line * 128 + ((piece ^ (line & 7)) << 4) + (HD == 128 ? 0 : 8 * (g & 1));
+          };
+          auto no_number = [](uint32_t w) { return __vcmpeq4(w & 0x7f7f7f7fu, 0x7f7f7f7fu); };
+          uint32_t any = 0;
+          for (int j = t; j < n_tok; j += 4) {
+            const uint2 a = lds8(place(j)), b = HD == 128 ? lds8(place(j) + 8) : a;
+            any |= no_number(a.x) | no_number(a.y) | no_number(b.x) | no_number(b.y);
+          }
+          if (__any_sync(~0u, any != 0)) {
+            int lim[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) lim[n][e] = __shfl_sync(~0u, limit[n], (2 * t + e) * 4);
+#pragma unroll 1
+            for (int j = 0; j < n_tok; ++j) {
+              uint32_t w[D / 4];
+#pragma unroll
+              for (int i = 0; i < D / 4; i += 2) { const uint2 x = lds8(place(j) + 4 * i); w[i] = x.x; w[i + 1] = x.y; }
+              __syncwarp();
+#pragma unroll
+              for (int i = 0; i < D / 4; ++i) {
+                const uint32_t bad = no_number(w[i]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                  for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                      if (((bad >> (8 * k)) & 1) && T0 + j < lim[n][e]) o[n][(4 * i + k) % NM][2 * ((4 * i + k) / NM) + e] = NAN;
+                if (t == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(place(j) + 4 * i), "r"(w[i] & ~bad) : "memory");
+              }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");              // before the next copy into this place
+            __syncwarp();
+          }
+        }
       }
       // ---- output: MMA i gives dimensions D g + i (rows 0..7) and D g + D / 2 + i (rows 8..15) ----
       auto load_v = [&](int kk, uint32_t (&v)[4][D / 4]) {

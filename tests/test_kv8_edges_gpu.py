@@ -1,11 +1,55 @@
-"""The operations over the 8-bit cache at the edges of their definitions.  References in 64 bits or exact fractions."""
+"""The operations over the 8-bit cache at the edges of their definitions: codes that are no numbers, waits that run out.
+References in 64 bits or exact fractions."""
 import os
 import subprocess
 import sys
 
 import pytest
+import torch
+
+from tests import kv8_reference as R
+from tests.test_kv8_ops_gpu import _attn_case
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2405_14371_b200 import binding
+    return binding
+
+
+def _attend(B, case):
+    return B.es_op_decode_attention_kv8(*[t.cuda() for t in case[:7]], case[7]).cpu().double()
+
+
+def _inside(got, want, bound):
+    assert torch.equal(got.isnan(), want.isnan()), (got.isnan().nonzero()[:8].tolist(), want.isnan().nonzero()[:8].tolist())
+    ok = ~want.isnan()
+    over = ((got - want).abs() / bound)[ok]
+    assert float(over.max()) <= 1.0, float(over.max())
+
+
+# ---- attention: codes that are no numbers ------------------------------------------------------------------------
+
+@pytest.mark.parametrize("Bn,T,Hq,Hkv,hd,P,ctxs", [
+    (1, 3, 2, 2, 64, 16, [40]), (2, 3, 4, 2, 128, 32, [37, 3]), (1, 4, 16, 2, 128, 64, [70]), (2, 17, 1, 1, 64, 16, [60, 20]), (20, 3, 8, 8, 128, 64, [30 + 7 * i for i in range(20)]),
+    (20, 4, 32, 8, 64, 16, [30 + 7 * i for i in range(20)]), (20, 2, 8, 8, 128, 16, [600 + 3 * i for i in range(20)]), (20, 6, 16, 8, 128, 32, [90 + 7 * i for i in range(20)]),
+])
+def test_attention_a_value_that_is_no_number_shows_only_where_it_is_seen(B, Bn, T, Hq, Hkv, hd, P, ctxs):
+    """e4m3 NaN codes in V at draft tokens: the queries before such a token do not see it, the others are NaN in its dimension
+    alone (a sum with it has no other value)."""
+    case = _attn_case(Bn, T, Hq, Hkv, hd, P, ctxs, "e4m3", "fp16", 101)
+    vc, table = case[2].view(torch.int8), case[5]
+    for b, n in enumerate(ctxs):
+        for back, dim, code in ((1, 5, 0x7f), (2, hd - 1, -1), (T - 1, 17, 0x7f)):
+            pos = n - max(back, 1)
+            if b % 3 != 2 and pos >= 0:
+                vc[int(table[b, pos // P]), (b + back) % Hkv, pos % P, dim] = code
+    q, kc, _, ks, vs, table, ctx, max_ctx = case
+    want, bound = R.attend(q, kc, case[2], ks, vs, table, ctx, P, max_ctx)
+    assert bool(want.isnan().any())
+    _inside(_attend(B, case).reshape(want.shape), want, bound)
 
 
 # ---- attention: a wait that runs out -----------------------------------------------------------------------------
