@@ -339,8 +339,7 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
   if (SL == 3 && asked < n_half) ask(ks_a, vs_a);          // the second tile's K, whose scales wait in ks_a, vs_a
   start_item(begin);
 
-  int at = begin;
-  for (; at < end && running; ++at) {
+  for (int at = begin; at < end && running; ++at) {
     if (fresh) {
       fresh = false;
       load_q();
@@ -621,13 +620,16 @@ __global__ void __launch_bounds__(WARPS<HD, NT> * 32, 1) kv8_attn_kernel(const _
     c.next(pre, p.B, p.Hkv, p.row_tiles);
   }
   // A wait ran out.  These calls have no status word: every row that this warp was to finish or to hand over becomes NaN (a
-  // sum that is NaN stays so through both joins), so that nothing it did not compute looks like a result.
+  // sum that is NaN stays so through both joins), so that nothing it did not compute looks like a result.  All of its stretch,
+  // from the start, so that the loop need not keep anything for this.
   if (!running) {
     if constexpr (GROUPED) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) l_run[n] = NAN;
     } else {
-      for (; at < end; ++at) {
+      c.seek(begin, pre, p.B, p.Hkv, p.row_tiles);
+      item_begin = begin - c.tile;
+      for (int at = begin; at < end; ++at) {
         const bool item_ends = c.tile + 1 == c.tiles;
         if (item_ends || at + 1 == end) {
           const int i = c.rt * ROWS + lane, token = i / p.G;
