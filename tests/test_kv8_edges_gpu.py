@@ -1,4 +1,5 @@
-"""The operations over the 8-bit cache at the edges of their definitions: codes that are no numbers, waits that run out.
+"""The operations over the 8-bit cache at the edges of their definitions: codes that are no numbers, queries of very different
+magnitudes, waits that run out.
 References in 64 bits or exact fractions."""
 import os
 import subprocess
@@ -49,6 +50,26 @@ def test_attention_a_value_that_is_no_number_shows_only_where_it_is_seen(B, Bn, 
     q, kc, _, ks, vs, table, ctx, max_ctx = case
     want, bound = R.attend(q, kc, case[2], ks, vs, table, ctx, P, max_ctx)
     assert bool(want.isnan().any())
+    _inside(_attend(B, case).reshape(want.shape), want, bound)
+
+
+# ---- attention: queries of very different magnitudes -------------------------------------------------------------
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("big", [2.0 ** 15, 2.0 ** 20, 2.0 ** 23, -2.0 ** 23])
+@pytest.mark.parametrize("f", [1.0, 2.0 ** -60, 2.0 ** 90])
+def test_attention_keeps_the_small_elements_of_a_bf16_query(B, code, big, f):
+    """One element of the query is large and the keys are zero there, so the result is that of the others alone: nothing of
+    them may be lost beside it.  Tolerance: that of the reference for the query without the large element, to which the
+    products with zero add nothing; elements down to 2^-30 of the largest are held exactly."""
+    case = list(_attn_case(2, 2, 8, 2, 128, 16, [33, 150], code, "bf16", 103))
+    q, kc = case[0], case[1]
+    kc[..., 9] = 0
+    q[..., 9] = 0
+    q.copy_(torch.where(q.abs() < 2.0 ** -6, torch.zeros_like(q), q))         # 2^-6 / 2^23: within 2^-30 of the largest
+    case[0], case[3] = (q.float() * f).bfloat16(), case[3] / f
+    want, bound = R.attend(case[0], *case[1:6], case[6], 16, case[7])
+    case[0][..., 9] = big * f
     _inside(_attend(B, case).reshape(want.shape), want, bound)
 
 
