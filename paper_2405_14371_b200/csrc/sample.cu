@@ -76,7 +76,8 @@ struct Shared {
   int pick_bin, pick_count;                   // a bin, and how many elements it holds
   u64 pick_up_to;                             // elements up to and including that bin
   u64 pick_target;                            // rank (counts) or mass to reach within the bin
-  u64 pick_pair;                              // threshold found in the list
+  u64 pick_pair, pick_mass_pair;              // thresholds found in the list, of top-k and of top-p: nothing need stand between
+                                              // everybody's reading of the first and the first CTA's finding the second
   // this CTA's own
   u64 all_mass;
   int list_n;
@@ -462,9 +463,9 @@ struct Row {
       to->pick_bin = bin; to->pick_count = count; to->pick_target = target; to->pick_up_to = up_to;
     }
   }
-  __device__ __forceinline__ void publish_pair(u64 pair) {
+  __device__ __forceinline__ void publish_pair(u64 Shared::* to, u64 pair) {
     cg::cluster_group cl = cg::this_cluster();
-    for (int i = 0; i < ranks; ++i) cl.map_shared_rank(sm, i)->pick_pair = pair;
+    for (int i = 0; i < ranks; ++i) cl.map_shared_rank(sm, i)->*to = pair;
   }
 
   // The elements whose bin lies in [lo, hi] go to the first CTA's list: each CTA gathers its own out of the groups whose
@@ -713,7 +714,7 @@ __global__ void __launch_bounds__(RESIDENT ? 512 : 256, RESIDENT ? 2 : 4) sample
       to->best[rank] = best;
       to->least[rank] = least;
     }
-    if (lane == 0) { shared.few_n = 0; shared.pick_bin = 0; shared.pick_count = 0; shared.pick_target = 1; shared.pick_pair = 0; shared.top = INT_MAX; }
+    if (lane == 0) { shared.few_n = 0; shared.pick_bin = 0; shared.pick_count = 0; shared.pick_target = 1; shared.pick_pair = 0; shared.pick_mass_pair = 0; shared.top = INT_MAX; }
   }
   cl.sync();
   best = -INFINITY;
@@ -847,7 +848,7 @@ __global__ void __launch_bounds__(RESIDENT ? 512 : 256, RESIDENT ? 2 : 4) sample
         listed = bin;
         R.collect(bin, bin, &shared.few_n);
         if (rank == 0) {                      // the mass of the bin's kept elements joins that of the bins before
-          R.choose(m, false, by_mass, want, [&](u64 pair, u64 mass) { R.publish_pair(pair); shared.all_mass += mass; });
+          R.choose(m, false, by_mass, want, [&](u64 pair, u64 mass) { R.publish_pair(&Shared::pick_pair, pair); shared.all_mass += mass; });
           if (by_mass) pick_mass();
           if (tid == 0) shared.few_n = 0;
         }
@@ -879,9 +880,9 @@ __global__ void __launch_bounds__(RESIDENT ? 512 : 256, RESIDENT ? 2 : 4) sample
       const int bin = shared.pick_bin, m = shared.pick_count;
       if (m <= LIST) {
         if (listed != bin) R.collect(bin, bin, &shared.few_n);
-        if (rank == 0) R.choose(m, true, true, target, [&](u64 pair, u64) { R.publish_pair(pair); });
+        if (rank == 0) R.choose(m, true, true, target, [&](u64 pair, u64) { R.publish_pair(&Shared::pick_mass_pair, pair); });
         cl.sync();
-        R.keep = shared.pick_pair > R.keep ? shared.pick_pair : R.keep;
+        R.keep = shared.pick_mass_pair > R.keep ? shared.pick_mass_pair : R.keep;       // never below top-k's
       } else {
         u64 above, here;
         const uint32_t key = R.descend([&](float v, int) { return R.bin_of(v) == bin ? R.weight(v) : 0ull; }, target, &above, &here);

@@ -9,7 +9,7 @@ import pytest
 import torch
 
 from tests import kv8_reference as R
-from tests.test_kv8_ops_gpu import _attn_case
+from tests.test_kv8_ops_gpu import _attn_case, _check_sample, _gen
 
 pytestmark = pytest.mark.gpu
 
@@ -104,3 +104,22 @@ def test_attention_a_wait_that_runs_out_leaves_no_result():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", _RUN_OUT], cwd=root, env=dict(os.environ, ES_KV8_GIVE_UP="1"), capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "all rows without a result" in r.stdout, r.stdout[-2000:] + r.stderr[-2000:]
+
+
+# ---- sampling ----------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("n,V", [(3, 40000), (40, 9000), (400, 20000)])
+def test_sampling_both_thresholds_in_one_list(B, n, V):
+    """700 logits so close together that the borders of top-k and of top-p lie in one bin, whose elements are collected once
+    and searched twice: right, and the same tokens every time."""
+    g = _gen(n)
+    x = -10 - 10 * torch.rand(n, V, generator=g)
+    for r in range(n):
+        x[r, torch.randperm(V, generator=g)[:700]] = 0.001 * torch.rand(700, generator=g)
+    u = torch.rand(n, generator=g).tolist()
+    k = [300 + 7 * r % 350 for r in range(n)]
+    p = [(0.2, 0.5, 0.9, 0.97)[r % 4] for r in range(n)]
+    tokens, _ = _check_sample(B, x, u, k=k, p=p)
+    dev = [x.cuda(), torch.tensor(u).cuda(), None, torch.tensor(k, dtype=torch.int32).cuda(), torch.tensor(p).cuda()]
+    for _ in range(30):
+        assert B.es_op_sample(*dev)[0].tolist() == tokens
