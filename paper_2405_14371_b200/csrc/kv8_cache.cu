@@ -96,16 +96,24 @@ __device__ __forceinline__ uint2 encode(const uint4& x, float s, float inv) {
   return make_uint2(out[0], out[1]);
 }
 
-// four codes at the old scale -> four codes at the new one
+// Four codes at the old scale -> four codes at the new one, round(code * old / new) to nearest, ties to even.  int8: with
+// `ratio` rounded to 53 bits the product misses the middle between two codes by at most 2^-45, and what is not the middle
+// itself lies at least 2^-34 from it (32 bits over 24); so only there the remainder decides, which two 32-bit products give exactly.
 template <int CODE>
-__device__ __forceinline__ uint32_t rescale(uint32_t w, double ratio) {
+__device__ __forceinline__ uint32_t rescale(uint32_t w, double ratio, float s_old, float s) {
   uint32_t out = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint32_t c = (w >> (8 * i)) & 255u;
     uint32_t n;
     if (CODE == CODE_I8) {
-      n = (uint32_t)__double2int_rn((double)(int)(int8_t)c * ratio) & 255u;
+      const double code = (double)(int)(int8_t)c, to = code * ratio;
+      int q = __double2int_rn(to);
+      if (fabs(to - (double)q) > 0.4999999999) {
+        const double r = fma(code, (double)s_old, -(double)q * (double)s), twice = 2.0 * fabs(r);
+        if (twice > (double)s || (twice == (double)s && (q & 1))) q += r > 0.0 ? 1 : -1;
+      }
+      n = (uint32_t)q & 255u;
     } else {
       const __half_raw h = __nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)c, __NV_E4M3);
       n = e4m3_of(__half2float(__half(h)) * (float)ratio);
@@ -219,8 +227,8 @@ __global__ void __launch_bounds__(APPEND_THREADS, 4) kv8_append_kernel(const App
     uint4* front = reinterpret_cast<uint4*>(dst);
     for (int i = tid; i < off * HD / 16; i += GROUP) {
       uint4 w = front[i];
-      w.x = rescale<CODE>(w.x, ratio); w.y = rescale<CODE>(w.y, ratio);
-      w.z = rescale<CODE>(w.z, ratio); w.w = rescale<CODE>(w.w, ratio);
+      w.x = rescale<CODE>(w.x, ratio, s_old, s); w.y = rescale<CODE>(w.y, ratio, s_old, s);
+      w.z = rescale<CODE>(w.z, ratio, s_old, s); w.w = rescale<CODE>(w.w, ratio, s_old, s);
       front[i] = w;
     }
   }

@@ -1,15 +1,17 @@
 """The operations over the 8-bit cache at the edges of their definitions: codes that are no numbers, queries of very different
-magnitudes, waits that run out.
+magnitudes, waits that run out, exact ties.
 References in 64 bits or exact fractions."""
+import math
 import os
 import subprocess
 import sys
+from fractions import Fraction
 
 import pytest
 import torch
 
 from tests import kv8_reference as R
-from tests.test_kv8_ops_gpu import _attn_case, _check_sample, _gen
+from tests.test_kv8_ops_gpu import _attn_case, _check_sample, _gen, _i32
 
 pytestmark = pytest.mark.gpu
 
@@ -104,6 +106,61 @@ def test_attention_a_wait_that_runs_out_leaves_no_result():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", _RUN_OUT], cwd=root, env=dict(os.environ, ES_KV8_GIVE_UP="1"), capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "all rows without a result" in r.stdout, r.stdout[-2000:] + r.stderr[-2000:]
+
+
+# ---- append: rounding at ties, scales that another program chose ---------------------------------------------------
+
+def _e4m3_numbers():
+    c = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).float()
+    return sorted({Fraction(float(x)) for x in c[c.isfinite()]})
+
+
+E4M3 = _e4m3_numbers()
+
+
+def _nearest(x, int8):
+    """The code's number nearest to the fraction x, ties to even."""
+    if int8:
+        return round(x)
+    if abs(x) >= 448:
+        return Fraction(448) if x > 0 else Fraction(-448)
+    best = min(E4M3, key=lambda n: abs(n - x))
+    two = [n for n in E4M3 if abs(n - x) == abs(best - x)]
+    if len(two) == 1:
+        return best
+    # of two neighbours the one whose code is even
+    code = lambda n: int(torch.tensor(float(n)).to(torch.float8_e4m3fn).view(torch.uint8))  # noqa: E731
+    return next(n for n in two if code(n) % 2 == 0)
+
+
+def _append_into(B, held, s_old, new, dtype, code):
+    """One page, one head: `held` [n, 64] codes at scale s_old in front, rows `new` [m, 64] behind; (numbers, scale) after."""
+    P = 32
+    ct = torch.int8 if code == "int8" else torch.float8_e4m3fn
+    page = torch.zeros(1, 1, P, 64)
+    page[0, 0, :len(held)] = held
+    kp = page.to(ct).cuda()
+    vp, s = kp.clone(), torch.full((1, 1), s_old).cuda()
+    vs = s.clone()
+    x = new.to(dtype).view(-1, 1, 64).cuda()
+    B.es_op_kv8_append(x, x, _i32([len(held) + i for i in range(len(new))]).cuda(), kp, vp, s, vs)
+    assert torch.equal(kp.view(torch.int8), vp.view(torch.int8)) and torch.equal(s, vs)
+    return kp.cpu().float()[0, 0], float(s)
+
+
+@pytest.mark.parametrize("first,second", [(444.5, 635.0), (349.25, 635.0), (889.0, 635.0 * 2), (2.0 * 127, 7.0 * 127), (3.0 * 127, 11.0 * 127), (1.25 * 127, 13.0 * 127)])
+def test_append_brings_int8_codes_in_front_to_the_new_scale_with_ties_to_even(B, first, second):
+    """Scales that are small whole numbers (largest magnitude 127 times them), so that many codes fall in the middle of two."""
+    held = torch.zeros(2, 64)
+    held[0], held[1] = torch.arange(1, 65), -torch.arange(64, 128)
+    new = torch.zeros(1, 64)
+    new[0, 3] = second
+    old = first / 127
+    assert float(torch.tensor(first).half()) == first and float(torch.tensor(second).half()) == second
+    got, s = _append_into(B, held, old, new, torch.float16, "int8")
+    assert s == second / 127
+    want = [[int(_nearest(Fraction(float(c)) * Fraction(old) / Fraction(s), True)) for c in row] for row in held]
+    assert got[:2].long().tolist() == want
 
 
 # ---- sampling ----------------------------------------------------------------------------------------------------
