@@ -54,8 +54,6 @@ __device__ __forceinline__ int quotient_code(float x, float s, float inv) {
   return (int)q;
 }
 
-__device__ __forceinline__ uint32_t e4m3_of(float x) { return __nv_cvt_float_to_fp8(x, __NV_SATFINITE, __NV_E4M3); }
-
 // 8 values at scale s -> 8 codes.  int8: x * inv is within 127 * 2^-24 < 1e-5 of x / s (the product is not rounded
 // before it meets 1.5 * 2^23, which leaves the nearest integer in the low bits), so only where it comes that close to the
 // middle between two codes does the exact form decide: 6 instructions a value instead of 14.
@@ -96,9 +94,26 @@ __device__ __forceinline__ uint2 encode(const uint4& x, float s, float inv) {
   return make_uint2(out[0], out[1]);
 }
 
+// 8 values at an e4m3 scale that is no power of two (append makes none; a page another program filled may hold one): 1 / s
+// is not exact then.  A quotient of 11 and 24 bits that is not the middle between two codes lies more than 2^-30 of itself
+// from it, so the 64-bit one lies on its side, and is rounded once.  A division a value: only pages with such a scale come here.
+template <bool BF16>
+__device__ __forceinline__ uint2 encode_divided(const uint4& x, float s) {
+  uint2 out = make_uint2(0, 0);
+#pragma unroll 1
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t w = i < 2 ? x.x : i < 4 ? x.y : i < 6 ? x.z : x.w;
+    const float2 v = to_float2<BF16>(w);
+    const uint32_t c = __nv_cvt_double_to_fp8((double)(i & 1 ? v.y : v.x) / (double)s, __NV_SATFINITE, __NV_E4M3);
+    if (i < 4) out.x |= c << (8 * i); else out.y |= c << (8 * (i - 4));
+  }
+  return out;
+}
+
 // Four codes at the old scale -> four codes at the new one, round(code * old / new) to nearest, ties to even.  int8: with
 // `ratio` rounded to 53 bits the product misses the middle between two codes by at most 2^-45, and what is not the middle
 // itself lies at least 2^-34 from it (32 bits over 24); so only there the remainder decides, which two 32-bit products give exactly.
+// e4m3: the new scale is a power of two, so the product of 4 and 24 bits is exact in 64 bits, and in 32 where the old one is too.
 template <int CODE>
 __device__ __forceinline__ uint32_t rescale(uint32_t w, double ratio, float s_old, float s) {
   uint32_t out = 0;
@@ -116,7 +131,9 @@ __device__ __forceinline__ uint32_t rescale(uint32_t w, double ratio, float s_ol
       n = (uint32_t)q & 255u;
     } else {
       const __half_raw h = __nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)c, __NV_E4M3);
-      n = e4m3_of(__half2float(__half(h)) * (float)ratio);
+      const float number = __half2float(__half(h));
+      n = __float_as_uint(s_old) & 0x7fffffu ? __nv_cvt_double_to_fp8((double)number * ratio, __NV_SATFINITE, __NV_E4M3)
+                                             : __nv_cvt_float_to_fp8(number * (float)ratio, __NV_SATFINITE, __NV_E4M3);
     }
     out |= n << (8 * i);
   }
@@ -235,10 +252,14 @@ __global__ void __launch_bounds__(APPEND_THREADS, 4) kv8_append_kernel(const App
 
   // ---- new codes ----
   uint2* to = reinterpret_cast<uint2*>(dst + (int64_t)off * HD);
+  if (CODE == CODE_E4M3 && !bad && (__float_as_uint(s) & 0x7fffffu)) {
+    for (int j = 0; tid + j * GROUP < pieces; ++j) to[tid + j * GROUP] = encode_divided<BF16>(piece(j), s);
+  } else {
 #pragma unroll
-  for (int j = 0; j < KEEP; ++j)
-    if (tid + j * GROUP < pieces) to[tid + j * GROUP] = bad ? make_uint2(0, 0) : encode<CODE, BF16>(keep[j], s, inv);
-  for (int j = KEEP; tid + j * GROUP < pieces; ++j) to[tid + j * GROUP] = bad ? make_uint2(0, 0) : encode<CODE, BF16>(piece(j), s, inv);
+    for (int j = 0; j < KEEP; ++j)
+      if (tid + j * GROUP < pieces) to[tid + j * GROUP] = bad ? make_uint2(0, 0) : encode<CODE, BF16>(keep[j], s, inv);
+    for (int j = KEEP; tid + j * GROUP < pieces; ++j) to[tid + j * GROUP] = bad ? make_uint2(0, 0) : encode<CODE, BF16>(piece(j), s, inv);
+  }
   if (WARPS == 1) __syncwarp();                    // every thread has read the old scale (several warps have met since)
   if (tid == 0) *scale = s;
 }

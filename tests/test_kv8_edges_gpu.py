@@ -1,6 +1,5 @@
 """The operations over the 8-bit cache at the edges of their definitions: codes that are no numbers, queries of very different
-magnitudes, waits that run out, exact ties.
-References in 64 bits or exact fractions."""
+magnitudes, waits that run out, exact ties, pages whose scale another program chose.  References in 64 bits or exact fractions."""
 import math
 import os
 import subprocess
@@ -161,6 +160,42 @@ def test_append_brings_int8_codes_in_front_to_the_new_scale_with_ties_to_even(B,
     assert s == second / 127
     want = [[int(_nearest(Fraction(float(c)) * Fraction(old) / Fraction(s), True)) for c in row] for row in held]
     assert got[:2].long().tolist() == want
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("s_old", [3.0, 5.0, 7.0, 13.0, 0.40625, 41.0, 49.0, 61.0, 0.1, 1.0 / 3.0, 47.0 / 127.0])
+def test_append_rounds_to_e4m3_exactly_at_a_kept_scale_that_is_no_power_of_two(B, s_old, dtype):
+    """Values at and next to the middle between two codes, at scales that only another program can have left."""
+    s = Fraction(float(torch.tensor(s_old)))
+    mids = [(a + b) / 2 for a, b in zip(E4M3, E4M3[1:]) if abs(a) <= 240 and abs(b) <= 240]
+    x = torch.tensor([float(m * s) for m in mids]).to(dtype)
+    near = [torch.nextafter(x, torch.full_like(x, e)) for e in (math.inf, -math.inf)]
+    x = torch.cat([x, *near])
+    x = torch.cat([x, torch.zeros(-len(x) % 64, dtype=dtype)]).view(-1, 64)
+    for i in range(0, len(x), 24):
+        new = x[i:i + 24]
+        got, kept = _append_into(B, torch.ones(1, 64), s_old, new, dtype, "e4m3")
+        assert kept == float(s)
+        want = [[float(_nearest(Fraction(float(v)) / s, False)) for v in row] for row in new]
+        assert got[1:1 + len(new)].tolist() == want
+
+
+@pytest.mark.parametrize("number", [1.0, 1.125, 3.25, 15.0, 0.4375])
+def test_append_brings_e4m3_codes_to_the_new_scale_from_one_that_is_no_power_of_two(B, number):
+    """code * old / new next to the middle between two numbers: the product has more bits than 32-bit floats hold."""
+    new = torch.zeros(1, 64)
+    new[0, 0] = 448.0 * 64                                # a scale of 64
+    for mid in (1.0625, 1.1875, 5.25, 2.0 ** -8 * 3 / 2):
+        base = torch.tensor(mid * 64 / number)
+        for old in (base, *[torch.nextafter(base, torch.tensor(e)) for e in (math.inf, -math.inf)]):
+            if float(old) >= 64:
+                continue
+            held = torch.full((1, 64), number)
+            held[0, 1::2] *= -1
+            got, s = _append_into(B, held, float(old), new, torch.float16, "e4m3")
+            assert s == 64.0
+            want = [float(_nearest(Fraction(float(c)) * Fraction(float(old)) / 64, False)) for c in held[0]]
+            assert got[0].tolist() == want
 
 
 # ---- sampling ----------------------------------------------------------------------------------------------------
