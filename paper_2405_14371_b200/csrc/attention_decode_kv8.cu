@@ -887,9 +887,9 @@ es_status_t launch_sub(const Kv8Maps& maps, const Kv8AttnParams& p, cudaStream_t
   static std::atomic<uint64_t> allowed{0};
   ES_CUDA_CHECK(allow_shared_memory(kern, RINGS + (GROUPED ? INBOX : (KV8_MAX_B + 1) * (int)sizeof(int)), &allowed));
   ES_CUDA_CHECK(launch_clusters(kern, GROUPED && p.group > 1 ? p.group : 0, dim3(GROUPED ? p.B * p.Hkv * p.row_tiles * p.group : sm_count()), dim3(AW * 32),
-                                RINGS + (GROUPED ? (p.group > 1 ? INBOX : 0) : (size_t)(p.B + 1) * sizeof(int)), s, true, maps, p));
+                                RINGS + (GROUPED ? (p.group > 1 ? INBOX : 0) : (size_t)(p.B + 1) * sizeof(int)), s, tunables().pdl != 0, maps, p));
   if (!GROUPED && p.max_ctx > TILE)
-    ES_CUDA_CHECK(launch_kernel(kv8_merge_kernel<HD, TILE>, dim3(p.Hq, p.T, p.B), dim3(128), 0, s, true, p, AW * sm_count()));
+    ES_CUDA_CHECK(launch_kernel(kv8_merge_kernel<HD, TILE>, dim3(p.Hq, p.T, p.B), dim3(128), 0, s, tunables().pdl != 0, p, AW * sm_count()));
   return ES_OK;
 }
 

@@ -33,7 +33,7 @@ struct Tunables {
   int tc_pair;       // ES_TC_PAIR: CTA-pair tensor-core kernel for large prefill products (1, default) or never (0)
   int tc_pair_wide;  // ES_TC_PAIR_WIDE: 256 x 512 pair tiles: chosen per shape (1, default), never (0), always (2)
   int split_pairs;   // ES_SPLIT_PAIRS: split-K products with 256 or more rows run on CTA pairs (1, default) or on single CTAs (0)
-  int pdl;           // ES_PDL: programmatic dependent launch in decode steps (1, default) or plain stream order (0)
+  int pdl;           // ES_PDL: programmatic dependent launch in decode steps and in the calls of the 8-bit decode loop (1, default) or plain stream order (0)
   int attn_mma;      // ES_ATTN_MMA: tensor-core decode attention for launches with many items (1, default) or never (0)
   int split_k;       // ES_SPLIT_K: split-K for the O and down projections of short prefills (1, default) or never (0)
   int ks_min_slice;        // ES_KS_MIN_SLICE: smallest K slice of the K-sliced streaming kernel (elements, default 512)

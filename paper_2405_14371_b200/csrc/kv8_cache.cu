@@ -380,9 +380,9 @@ es_status_t launch_gather(const GatherParams& p, int out, cudaStream_t s) {
   if (blocks > INT32_MAX || p.n_items / (HD / 8) > UINT32_MAX) return fail(ES_ERR_RANGE, "too many rows for one launch");
   const dim3 grid((unsigned)blocks);
   switch (out) {
-    case ES_DTYPE_F16: ES_CUDA_CHECK(launch_kernel(kv8_gather_kernel<HD, CODE, ES_DTYPE_F16>, grid, dim3(GATHER_THREADS), 0, s, true, p)); break;
-    case ES_DTYPE_BF16: ES_CUDA_CHECK(launch_kernel(kv8_gather_kernel<HD, CODE, ES_DTYPE_BF16>, grid, dim3(GATHER_THREADS), 0, s, true, p)); break;
-    default: ES_CUDA_CHECK(launch_kernel(kv8_gather_kernel<HD, CODE, ES_DTYPE_F32>, grid, dim3(GATHER_THREADS), 0, s, true, p));
+    case ES_DTYPE_F16: ES_CUDA_CHECK(launch_kernel(kv8_gather_kernel<HD, CODE, ES_DTYPE_F16>, grid, dim3(GATHER_THREADS), 0, s, tunables().pdl != 0, p)); break;
+    case ES_DTYPE_BF16: ES_CUDA_CHECK(launch_kernel(kv8_gather_kernel<HD, CODE, ES_DTYPE_BF16>, grid, dim3(GATHER_THREADS), 0, s, tunables().pdl != 0, p)); break;
+    default: ES_CUDA_CHECK(launch_kernel(kv8_gather_kernel<HD, CODE, ES_DTYPE_F32>, grid, dim3(GATHER_THREADS), 0, s, tunables().pdl != 0, p));
   }
   ES_CUDA_CHECK(cudaGetLastError());
   return ES_OK;

@@ -379,12 +379,12 @@ es_status_t es_op_kv_plan(const int32_t* old_len, const int32_t* new_len, int32_
   static std::atomic<uint64_t> allowed[2];
   if (smem > 48 * 1024) ES_CUDA_CHECK(allow_shared_memory(kern, (int)((6 * PLAN_MAX_B + 4) * sizeof(int)), &allowed[small]));
   const int ranks = small ? 1 : plan_cluster();
-  ES_CUDA_CHECK(launch_clusters(kern, small ? 0 : ranks, dim3(ranks), dim3(few ? PLAN_FEW : PLAN_THREADS), smem, (cudaStream_t)stream, true, p));
+  ES_CUDA_CHECK(launch_clusters(kern, small ? 0 : ranks, dim3(ranks), dim3(few ? PLAN_FEW : PLAN_THREADS), smem, (cudaStream_t)stream, tunables().pdl != 0, p));
   if (!small) {
     const int blocks = (int)((max_rows + (long long)PLAN_THREADS - 1) / PLAN_THREADS);
     const int most = 2 * sm_count();
     ES_CUDA_CHECK(launch_kernel(kv_plan_rows_kernel, dim3(blocks < most ? blocks : most), dim3(PLAN_THREADS), (size_t)(B + 1) * sizeof(int),
-                                (cudaStream_t)stream, true, p));
+                                (cudaStream_t)stream, tunables().pdl != 0, p));
   }
   return ES_OK;
 }

@@ -919,7 +919,7 @@ es_status_t launch_kind(const SampleParams& p, int B, cudaStream_t s) {
   static std::atomic<uint64_t> allowed{0};
   ES_CUDA_CHECK(allow_shared_memory(sample_kernel<DT, ranks, RESIDENT>, (int)sample_smem(MAX_SLICE, RESIDENT), &allowed));
   ES_CUDA_CHECK(launch_clusters(sample_kernel<DT, ranks, RESIDENT>, ranks, dim3((unsigned)(B * ranks)), dim3(Row<DT, ranks, RESIDENT>::ST),
-                                sample_smem(p.slice, RESIDENT), s, true, p));
+                                sample_smem(p.slice, RESIDENT), s, tunables().pdl != 0, p));
   return ES_OK;
 }
 

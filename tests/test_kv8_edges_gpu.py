@@ -215,3 +215,51 @@ def test_sampling_both_thresholds_in_one_list(B, n, V):
     dev = [x.cuda(), torch.tensor(u).cuda(), None, torch.tensor(k, dtype=torch.int32).cuda(), torch.tensor(p).cuda()]
     for _ in range(30):
         assert B.es_op_sample(*dev)[0].tolist() == tokens
+
+
+# ---- launches ----------------------------------------------------------------------------------------------------
+
+_EDGES = """
+import torch
+from cuda.bindings import runtime as R
+from paper_2405_14371_b200 import binding as B
+from tests.test_kv8_ops_gpu import _attn_case, _gen, _i32
+
+long, short = [[t.cuda() if torch.is_tensor(t) else t for t in _attn_case(n, 1, 16, 8, 64, 16, [400] * n, "int8", "fp16", 3)] for n in (40, 1)]
+x, u = torch.randn(300, 9000, generator=_gen(5)).cuda(), torch.rand(300, generator=_gen(6)).cuda()
+lens, table = _i32([5, 6]).cuda(), _i32([[0, 1], [2, 3]]).cuda()
+slots, wide = _i32(list(range(16))).cuda(), _i32([[i] for i in range(2)]).repeat(1, 400).cuda()
+
+def calls():
+    out = [B.es_op_decode_attention_kv8(*c) for c in (long, short)]
+    out += [*B.es_op_kv_plan(lens, lens + 3, table, 16, 8, n_pages=4), *B.es_op_kv_plan(lens, lens + 3, wide, 16, 5000, n_pages=2)]
+    return out + [*B.es_op_kv8_gather(slots, *long[1:5]), *B.es_op_sample(x, u), *B.es_op_sample(x[:2], u[:2])]
+
+want = calls()
+graph = torch.cuda.CUDAGraph(keep_graph=True)
+with torch.cuda.graph(graph):
+    got = calls()
+raw = R.cudaGraph_t(graph.raw_cuda_graph())
+err, *_, n = R.cudaGraphGetEdges_v2(raw, 0)
+err, _, _, data, n = R.cudaGraphGetEdges_v2(raw, n)
+assert int(err) == 0
+graph.replay()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(got, want))
+print("early", sum(int(e.type) == int(R.cudaGraphDependencyType.cudaGraphDependencyTypeProgrammatic) for e in data), "of", n)
+print("sums", [float(t.double().nan_to_num().sum()) for t in want])
+"""
+
+
+def test_launches_follow_the_knob_for_dependent_launch():
+    """ES_PDL (read once per process, hence child processes): with 0 no launch of these calls begins before the one in front has
+    ended, and the results are the same."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    out = {}
+    for pdl in ("0", "1"):
+        r = subprocess.run([sys.executable, "-c", _EDGES], cwd=root, env=dict(os.environ, ES_PDL=pdl), capture_output=True, text=True, timeout=300)
+        assert r.returncode == 0, r.stdout[-2000:] + r.stderr[-2000:]
+        out[pdl] = [line.split(" ", 1) for line in r.stdout.splitlines() if line.startswith(("early", "sums"))]
+    early = {pdl: lines[0][1].split(" of ") for pdl, lines in out.items()}
+    assert early["0"][0] == "0" and int(early["1"][0]) > 0, early
+    assert early["0"][1] == early["1"][1] and out["0"][1] == out["1"][1]
