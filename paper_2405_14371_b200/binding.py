@@ -117,11 +117,6 @@ def _load() -> C.CDLL:
 
 
 lib = _load()
-try:
-    from . import _native_binding as _native
-except ImportError as e:
-    raise ImportError(f"{os.path.join(_HERE, '_native_binding.so')} is missing or does not fit this torch ({e}): build it "
-                      "with `python -m paper_2405_14371_b200.build`") from e
 EXPORTS = ("es_shard_workspace_bytes es_shard_create es_shard_prefill es_shard_prefill_ragged es_shard_prefill_packed es_shard_decode_step es_shard_handoff "
            "es_layer_profile es_shard_set_profiling es_shard_reset_slots es_shard_set_page_table es_shard_set_graphs "
            "es_partition_latency es_partition_throughput es_shard_device_status es_shard_wait_probe es_shard_launch_count es_shard_set_kernel_timing es_shard_kernel_timing es_shard_kernel_timing_detail es_shard_set_step_timing es_shard_step_timing es_shard_destroy es_last_error es_version es_op_rmsnorm "
@@ -434,9 +429,23 @@ def es_op_decode_attention_static(q: torch.Tensor, k_pages: torch.Tensor, v_page
 
 _VALUE_DTYPES = {torch.float16: ES_DTYPE_F16, torch.bfloat16: ES_DTYPE_BF16, torch.float32: ES_DTYPE_F32}
 
-# A decode step makes these calls once per layer, so their checks, result memory and stream are handled in the compiled
-# module (csrc_py/native_binding.cpp); every refusal is an EsError with the C ABI's status.
-_native.set_errors(EsError, torch.cuda.OutOfMemoryError)
+class _Native:
+    """The compiled module (csrc_py/native_binding.cpp).  A decode step makes these calls once per layer, so their checks,
+    result memory and stream are handled there; every refusal is an EsError with the C ABI's status.  It is loaded by the first
+    of them: everything else works without it."""
+
+    def __getattr__(self, name):
+        try:
+            from . import _native_binding as module
+        except ImportError as e:
+            raise ImportError(f"{os.path.join(_HERE, '_native_binding.so')} is missing or does not fit this torch ({e}): build it "
+                              "with `python -m paper_2405_14371_b200.build`") from e
+        module.set_errors(EsError, torch.cuda.OutOfMemoryError)
+        self.__dict__.update({n: getattr(module, n) for n in dir(module) if not n.startswith("_")})
+        return getattr(module, name)
+
+
+_native = _Native()
 
 
 def _call(stream, f, *args):
