@@ -106,6 +106,12 @@ class ShardPipeline:
             for name, t in sampling.items():
                 if tuple(t.shape[-2:]) != (len(self.slots), batch) or t.dim() != (3 if name == "u" else 2):
                     raise ValueError(f"sampling[{name!r}] must be [{'iterations, ' if name == 'u' else ''}micro_batches, batch]")
+                # what es_op_sample would refuse on the last shard, after the prefill
+                want = torch.int32 if name == "top_k" else torch.float32
+                if t.dtype != want or t.device != dev or (batch > 1 and t.stride(-1) != 1):
+                    raise ValueError(f"sampling[{name!r}] must be {want} on {dev} with dense rows")
+            if sampling["u"].shape[0] < 1:
+                raise ValueError("sampling['u'] must have a row for the prefill")
         self.events = {}
         self.iteration = 0
         self.outputs = [None] * len(self.slots)        # (hidden, logits, next_ids) views of the last shard, per micro-batch
