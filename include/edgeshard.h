@@ -392,7 +392,7 @@ ES_API es_status_t es_op_decode_attention_static(const void *q, const void *k_pa
  *   the table holds no page);  runs int32 [max_runs]: first rows of the served stretches that lie in one page, ascending
  *   (-1 for one whose page the table does not hold), max_runs = es_op_kv_plan_max_runs(...);
  *   entries behind the last row or run are -1;
- *   len_out int32 [B]: new_len where served, else old_len (may be old_len itself).
+ *   len_out int32 [B]: new_len where served, else old_len (may be old_len itself, not new_len).
  * Entries of the table below a request's length must be distinct pages in [0, n_pages) for the stack to stay
  * sound. */
 ES_API int32_t es_op_kv_plan_max_runs(int32_t B, int32_t max_rows, int32_t page_tokens);

@@ -365,6 +365,7 @@ es_status_t es_op_kv_plan(const int32_t* old_len, const int32_t* new_len, int32_
     return fail(ES_ERR_RANGE, "pages_per_seq or n_pages times page_tokens exceeds 2^31 - 1");
   if (max_rows > (1 << 30)) return fail(ES_ERR_RANGE, "max_rows exceeds 2^30");
   if ((long long)B * pages_per_seq > (1 << 30)) return fail(ES_ERR_RANGE, "the block table has more than 2^30 entries");
+  if (len_out == new_len) return fail(ES_ERR_INVALID_ARG, "len_out may be old_len, not new_len");      // a large call's rows compare the two
   int log2P = 0;
   while ((1 << log2P) < page_tokens) ++log2P;
   PlanParams p{old_len, new_len, block_table, free_pages, free_count, B, pages_per_seq, page_tokens, log2P, n_pages, max_rows,
