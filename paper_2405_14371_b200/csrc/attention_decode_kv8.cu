@@ -28,10 +28,10 @@
 // bf16 queries are brought to fp16 by a power of two per row, largest magnitude to [2^15, 2^16) (bf16's largest mantissa stays
 // below 65504): elements down to 2^-32 of the row's largest are exact, smaller ones are off by 2^-40 of it at most.
 //
-// Measured: 32 sequences of 500 to 8191 tokens, 64 / 8 heads of 128 (286 MB): 59.0 us = 4.8 TB/s, of which the merge kernel
+// Measured: 32 sequences of 500 to 8191 tokens, 64 / 8 heads of 128 (286 MB): 59.4 us = 4.8 TB/s, of which the merge kernel
 // 6.4 us; in the loop an SM takes in 23.4 bytes a clock, the rate at which memory feeds it (with the multiplications of the
 // low halves and the conversions left out it took no less).  8 sequences of 3 to 2500 with 4 draft tokens, 40 heads (103 MB):
-// 30.1 us.  16 of 1025 to 1152 (36 MB): 13.7 us.  One of 1000, 32 heads (8 MB): 5.9 us, of which about 3 us are the launch
+// 30.6 us.  16 of 1025 to 1152 (36 MB): 14.1 us.  One of 1000, 32 heads (8 MB): 6.0 us, of which about 3 us are the launch
 // and the chain from length to table to the first tile.
 //
 // Codes behind the context are zeroed in V and masked by selection in the scores, so that garbage (NaN codes among it)
@@ -854,7 +854,10 @@ Shape shape_of(int B, int T, int Hq, int Hkv, int hd, int max_ctx) {
   // more than half a megabyte for a CTA to read, so that an uneven batch, whose longest sequence then sets the time,
   // loses about what the second kernel costs.  With 32 KV heads of 128, groups and stretches take: 1 sequence of 700
   // 6.7 and 10.0 us, of 8192 (512 KB a CTA) 20.7 and 27.5 us; 4 of 2048 (512 KB) 20.2 and 23.1 us, of 1 to 2048 19.8 and
-  // 18.0 us; 4 of 4096 (1 MB) 32.9 and 32.6 us, of 1 to 4096 32.4 and 23.0 us.
+  // 18.0 us; 4 of 4096 (1 MB) 32.9 and 32.6 us, of 1 to 4096 32.4 and 23.0 us.  All of it goes by max_ctx, for the lengths are on
+  // the device: a cap far above them costs the way it leads to.  16 sequences of 1025 to 1152, 64 / 8 heads: 13.0 us with a cap up to
+  // 2048, 16.7 us from 4096 on (stretches); one of 1000, 32 heads: 6.0 us up to 8192, 9.6 us with 16384; two of 300, 8 KV heads:
+  // 5.7 us with their own length, 9.3 us with 2048 and more (clusters of 8 for 10 tiles; stretches 7.2 us).
   const long long items = (long long)B * Hkv * s.row_tiles;
   const int warps = s.nt == 1 ? WARPS<128, 1> : WARPS<128, 2>;
   int group = 1;

@@ -277,7 +277,11 @@ es_status_t launch_append_warps(const AppendParams& p, cudaStream_t s) {
 
 // A warp per item where stretches are short on average (a decode step: one row each); else as many as give a thread eight
 // 16-byte pieces of a whole page, up to eight.  Pages of 64 tokens, 1 / 2 / 4 / 8 warps: 8 prompts of up to 2600 tokens, 32 heads,
-// 139 / 118 / 103 / 118 us; a decode step of 64 sequences 8.9 / 9.3 / 10.0 / 11.3 us (with the gather that follows).
+// 139 / 118 / 103 / 118 us; a decode step of 64 sequences 8.9 / 9.3 / 10.0 / 11.3 us (with the gather that follows).  The
+// border is 8 rows an entry of `runs`, padding included, since the host knows no more.  64 sequences of 16 / 24 / 64 / 128 new
+// rows in pages of 64 (7 / 10 / 21 / 32 rows an entry), append alone: 8 heads 6.4 / 8.6 / 14.1 / 29.3 us with one warp, 5.9 / 6.5 /
+// 10.1 / 16.7 with four; 32 heads 9.6 / 15.5 / 36.4 / 66.0 and 16.1 / 19.1 / 33.6 / 51.4.  Without `runs` nothing tells prompts
+// from decode steps, and a prompt takes one warp an item.
 template <int HD, int CODE, bool BF16>
 es_status_t launch_append(const AppendParams& p, bool whole_pages, cudaStream_t s) {
   const int warps = whole_pages ? p.P * (HD / 8) / 256 : 1;

@@ -189,8 +189,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_plan_kernel(const PlanParams p)
     runs_before += total;
   }
   __syncthreads();
-  // from here row_off is capped, and need_off counts the served only: they are a prefix of those that need pages
-  // (need sums beyond avail belong to refused requests; so do all needs behind the first row sum beyond max_rows)
+  // The served requests that take pages are a prefix of those that need some (behind the first need sum beyond avail, or row sum
+  // beyond max_rows, all of these are refused), so the pages taken are the inclusive need of the last of them.
   {
     int most = 0;
     for (int b = tid; b < B; b += THREADS)
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) kv_plan_rows_kernel(const Pla
   for (int b = threadIdx.x; b <= B; b += PLAN_THREADS) row_off[b] = __ldcg(p.row_offsets + b);
   __syncthreads();
   const int rows_all = row_off[B];
-  // neighbouring threads take neighbouring rows, four rounds under way at a time
+  // neighbouring threads take neighbouring rows
   for (int64_t base = (int64_t)blockIdx.x * PLAN_THREADS + threadIdx.x; base < p.max_rows; base += (int64_t)gridDim.x * PLAN_THREADS) {
     const int r = (int)base;
     int slot = -1, pos = -1, seq = -1;
@@ -309,7 +309,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) kv_plan_rows_kernel(const Pla
   }
 }
 
-// CTAs of a large call's cluster: 16 where the device places such clusters (their shared work is bound by issue slots; a
+// CTAs of a large call's cluster: 16 where the device places such clusters (a
 // call that returns 25 000 pages and one that takes as many: 27 us together, with 8 30 us), else the portable 8.
 int plan_cluster() {
   static std::atomic<int> known[64];

@@ -20,8 +20,9 @@
 //
 // Measured, unrestricted / top_k 50 / top_p 0.9: one row of 32000 5.6 / 9.1 / 13.7 us, 64 rows 10.0 / 12.2 / 24.0 us, 256
 // rows of 128001 (131 MB, 20 us at the copy rate) 111 / 64 / 260 us.  Small calls are bound by the latency of the passes
-// and the cluster's barriers between them; large ones by issue slots: a weight costs about 45 instructions, a third of
-// them 64-bit, and top-p asks for each twice (its histogram, and the draw), beside four additions to shared memory.
+// and the cluster's barriers between them.  Large ones with mixed settings use a tenth of the memory's rate and 36 % of the
+// issue slots (61 % on the busiest SM): a weight costs about 45 instructions, a third of them 64-bit, and top-p asks for
+// each twice (its histogram, and the draw), beside four additions to shared memory, so rows are of very unequal length.
 //
 // A row belongs to a cluster of 1 to 8 CTAs.  Where all CTAs of a call run at once, each holds its slice of the row in
 // shared memory as fp32: latency counts there.  Larger calls read the slice again from L2, which leaves room for four
@@ -304,7 +305,7 @@ struct Row {
     }
     int at_index = ch * CHUNK;                // in steps of 32: ends where the chunk's sum passes the target
     unsigned hit = 0;
-#pragma unroll 1
+#pragma unroll 1                              // once a row, so a quarter of the code; unrolled it finds the same
     for (int j = 0; j < CHUNK / 32; ++j) {
       const u64 inc = run + warp_scan(f(get(at_index + lane), first + at_index + lane));
       hit = __ballot_sync(~0u, inc > target);
@@ -611,7 +612,7 @@ struct Row {
         }
         __syncthreads();
       }
-    const int each = size / ST, at = threadIdx.x * each;          // 1 or 2 elements a thread
+    const int each = size / ST, at = threadIdx.x * each;          // 1, 2 or 4 elements a thread
     u64 w = 0, nothing = 0;
     if (weights) for (int i = 0; i < each; ++i) w += lweight[at + i];
     u64 run = w;
