@@ -263,3 +263,41 @@ def test_launches_follow_the_knob_for_dependent_launch():
     early = {pdl: lines[0][1].split(" of ") for pdl, lines in out.items()}
     assert early["0"][0] == "0" and int(early["1"][0]) > 0, early
     assert early["0"][1] == early["1"][1] and out["0"][1] == out["1"][1]
+
+
+_FIRST = """
+import sys
+import torch
+from paper_2405_14371_b200 import binding as B
+from tests.test_kv8_ops_gpu import _attn_case, _gen, _i32
+
+long, short = [[t.cuda() if torch.is_tensor(t) else t for t in _attn_case(n, 1, 16, 8, 64, 16, [400] * n, "int8", "fp16", 3)] for n in (40, 1)]
+x, u = torch.randn(300, 9000, generator=_gen(5)).cuda(), torch.rand(300, generator=_gen(6)).cuda()
+n = 4000
+lens, more, table = _i32([0] * n).cuda(), _i32([5] * n).cuda(), _i32([[i] for i in range(n)]).cuda()
+rows, slots = torch.randn(32, 8, 64, generator=_gen(7)).half().cuda(), _i32(list(range(32))).cuda()
+pages, scales = [torch.zeros(2, 8, 16, 64, dtype=torch.int8, device="cuda") for _ in range(2)], [torch.zeros(2, 8, device="cuda") for _ in range(2)]
+calls = dict(attend=lambda: (B.es_op_decode_attention_kv8(*long),), joined=lambda: (B.es_op_decode_attention_kv8(*short),),
+             plan=lambda: B.es_op_kv_plan(lens, more, table, 16, 20000, n_pages=n), few=lambda: B.es_op_kv_plan(lens[:9], more[:9], table[:9], 16, 45, n_pages=n),
+             append=lambda: (B.es_op_kv8_append(rows, rows, slots, *pages, *scales),), gather=lambda: B.es_op_kv8_gather(slots, *pages, *scales),
+             sample=lambda: B.es_op_sample(x, u), sample_one=lambda: B.es_op_sample(x[:1], u[:1]))
+got = {}
+for name, call in calls.items():
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got[name] = graph, call()
+for name, call in calls.items():
+    graph, out = got[name]
+    graph.replay()
+    torch.cuda.synchronize()
+    for a, b in zip(out, call()):
+        assert a is None or torch.equal(a, b), name
+print("captured first")
+"""
+
+
+def test_the_first_call_of_a_process_may_be_a_captured_one():
+    """What a call sets up once (shared-memory limits, the cluster size of large plans) it may set up while capturing."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", _FIRST], cwd=root, env=dict(os.environ), capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "captured first" in r.stdout, r.stdout[-2000:] + r.stderr[-2000:]
