@@ -434,12 +434,13 @@ ES_API es_status_t es_op_kv8_gather(const int32_t *slot_map, int32_t n_rows, con
  *   of Hkv;  B <= 4096, T * Hq / Hkv <= 65535, max_ctx <= 2^30, and B * Hkv * ceil(T * Hq / Hkv / 8) *
  *   ceil(max_ctx / 32) <= 2^30;
  *   block_table int32 [B, pages_per_seq];  ctx_len int32 [B]: cached keys of the sequence, its T newest included.
- * Query t sees keys 0 .. ctx_len[b] - T + t, and nothing of the others reaches it, codes that are no numbers included (a page's
- * scale belongs to all its tokens: one that is NaN shows in every query that sees some of them); a query that sees none gives zeros.  Scale 1/sqrt(hd); scores, softmax
- * and sums in fp32; bf16 queries are exact down to 2^-32 of the largest element of their head's row (and within 2^-40 of it below),
- * probabilities enter the product as two fp16 halves.  Table entries outside [0, n_pages) are
- * pages that nobody sees; lengths above max_ctx (<= pages_per_seq * page_tokens) are read as max_ctx.  Should a wait for
- * keys or values inside the kernel run out (after a second), the rows it was for become NaN.
+ * Query t sees keys 0 .. ctx_len[b] - T + t, and nothing of the others reaches it, codes that are no numbers included
+ * (a page's scale belongs to all its tokens: one that is NaN shows in every query that sees some of them); a query
+ * that sees none gives zeros.  Scale 1/sqrt(hd); scores, softmax and sums in fp32; bf16 queries are exact down to 2^-32
+ * of the largest element of their head's row (and within 2^-40 of it below), probabilities enter the product as two
+ * fp16 halves.  Table entries outside [0, n_pages) are pages that nobody sees; lengths above max_ctx (<= pages_per_seq *
+ * page_tokens) are read as max_ctx.  Should a wait for keys or values inside the kernel run out (after a second), the
+ * rows it was for become NaN.
  *   scratch: dev, 16-byte aligned, es_op_decode_attention_kv8_scratch_bytes(...) bytes of the call's sizes, in use
  *   until the call's work is done (calls that overlap on the GPU need one each).  Uninitialised is fine. */
 ES_API size_t es_op_decode_attention_kv8_scratch_bytes(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t hd,

@@ -309,8 +309,8 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) kv_plan_rows_kernel(const Pla
   }
 }
 
-// CTAs of a large call's cluster: 16 where the device places such clusters (a
-// call that returns 25 000 pages and one that takes as many: 27 us together, with 8 30 us), else the portable 8.
+// CTAs of a large call's cluster: 16 where the device places such clusters (a call that returns 25 000 pages and one that
+// takes as many: 27 us together, with 8 30 us), else the portable 8.
 int plan_cluster() {
   static std::atomic<int> known[64];
   int dev = 0;
