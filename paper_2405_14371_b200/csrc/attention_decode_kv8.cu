@@ -28,10 +28,10 @@
 // bf16 queries are brought to fp16 by a power of two per row, largest magnitude to [2^15, 2^16) (bf16's largest mantissa stays
 // below 65504): elements down to 2^-32 of the row's largest are exact, smaller ones are off by 2^-40 of it at most.
 //
-// Measured: 32 sequences of 500 to 8191 tokens, 64 / 8 heads of 128 (286 MB): 59.4 us = 4.8 TB/s, of which the merge kernel
+// Measured: 32 sequences of 500 to 8191 tokens, 64 / 8 heads of 128 (286 MB): 59.1 us = 4.8 TB/s, of which the merge kernel
 // 6.4 us; in the loop an SM takes in 23.4 bytes a clock, the rate at which memory feeds it (with the multiplications of the
 // low halves and the conversions left out it took no less).  8 sequences of 3 to 2500 with 4 draft tokens, 40 heads (103 MB):
-// 30.6 us.  16 of 1025 to 1152 (36 MB): 14.1 us.  One of 1000, 32 heads (8 MB): 6.0 us, of which about 3 us are the launch
+// 30.3 us.  16 of 1025 to 1152 (36 MB): 13.7 us.  One of 1000, 32 heads (8 MB): 6.0 us, of which about 3 us are the launch
 // and the chain from length to table to the first tile.
 //
 // Codes behind the context are zeroed in V and masked by selection in the scores, so that garbage (NaN codes among it)
@@ -66,10 +66,14 @@ struct Kv8AttnParams {
   void* out;
   float *part_o, *part_ml;               // [2 * warps][rows][hd], [..][rows][2]
   int B, T, Hq, Hkv, G, P, log2P, pps, n_pages, max_ctx;
-  int row_tiles, rows, bf16;             // rows = rows of a row tile that are stored
+  int row_tiles, rows;                   // rows = rows of a row tile that are stored
+  int16_t bf16;
+  int16_t give_up;                       // every warp's first wait counts as run out
   int group;                             // CTAs of an item (groups)
-  int give_up;                           // every warp's first wait counts as run out
 };
+
+// With the maps 384 bytes of parameters; with 8 more every call took 0.1 to 0.2 us longer (drafts 30.5 and 30.3 us).
+static_assert(sizeof(Kv8AttnParams) <= 128, "parameters of the attention kernel");
 
 struct alignas(64) Kv8Maps { CUtensorMap k, v; };
 
@@ -971,8 +975,8 @@ es_status_t es_op_decode_attention_kv8(const void* q, int32_t dtype, int64_t q_s
   float* part = (float*)scratch;
   const size_t parts = parts_of(sh);
   Kv8AttnParams p{q, q_stride, k_scale, v_scale, block_table, ctx_len, out, part, part + parts * hd, B, T, Hq, Hkv, Hq / Hkv,
-                  page_tokens, log2P, pages_per_seq, n_pages, max_ctx, sh.row_tiles, sh.rows, dtype == ES_DTYPE_BF16, sh.group,
-                  tunables().kv8_give_up};
+                  page_tokens, log2P, pages_per_seq, n_pages, max_ctx, sh.row_tiles, sh.rows,
+                  (int16_t)(dtype == ES_DTYPE_BF16), (int16_t)(tunables().kv8_give_up != 0), sh.group};
   cudaStream_t s = (cudaStream_t)stream;
   if (hd == 128) return code == CODE_I8 ? launch<128, CODE_I8>(maps, p, sh, s) : launch<128, CODE_E4M3>(maps, p, sh, s);
   return code == CODE_I8 ? launch<64, CODE_I8>(maps, p, sh, s) : launch<64, CODE_E4M3>(maps, p, sh, s);
