@@ -167,7 +167,7 @@ def _run_linear(s):
     if own:
         from paper_2405_14371_b200 import binding as b
         codes, scale = b.es_op_quant_e4m3(s["x"])
-        return b.es_op_linear_fp8(codes, scale, s["w"], s["ws"], residual=s["r"], dtype=TYPE[s["out"]])
+        return b.es_op_linear_fp8(codes, scale, s["w"], s["ws"], residual=s["r"], dtype=TYPE[s["out"]], weights_ready=True)
     return _linear(s["x"], s["w"], s["ws"], s["r"], TYPE[s["out"]])
 
 
