@@ -60,8 +60,8 @@ typedef enum {
 
 typedef enum {
   ES_DTYPE_F16 = 0, ES_DTYPE_F32 = 1, ES_DTYPE_I32 = 2,
-  ES_DTYPE_BF16 = 3,                       /* operands of the 8-bit cache and sampling operations only */
-  ES_DTYPE_I8 = 4, ES_DTYPE_F8E4M3 = 5     /* codes of an 8-bit cache */
+  ES_DTYPE_BF16 = 3,                       /* operands of the operations after es_op_decode_attention_static only */
+  ES_DTYPE_I8 = 4, ES_DTYPE_F8E4M3 = 5     /* codes of an 8-bit cache; F8E4M3 also of 8-bit weights and activations */
 } es_dtype_t;
 
 /* Model and capacity description.  max_slots = number of sequences whose KV is kept at once;
@@ -470,6 +470,55 @@ ES_API es_status_t es_op_sample(const void *logits, int32_t dtype, int64_t row_s
                                 const float *temperature, const int32_t *top_k, const float *top_p,
                                 const float *min_p, int32_t *tokens, float *logprobs, int32_t B, int32_t V,
                                 void *stream);
+
+/* ---- an attention block with 8-bit weights, normalised heads and a shared prefix ------------------
+ * The other term of the paper's memory constraint, the parameters (Req_i), in one byte per weight; and what models
+ * and servers around it ask of the attention block.  All pointers dev; every call only enqueues on `stream`, on the
+ * current device, and may be captured into a graph. */
+
+/* Codes of type F8E4M3 with one fp32 scale per block of 128 columns (the last block of a row may be shorter) and
+ * block_rows rows: 1 (activations) or 128 (weights; the last rows may be fewer).
+ *   x (fp16, bf16 or fp32) [M, K], row r at x + r * row_stride elements, every row 16-byte aligned;  K % 16 == 0;
+ *   codes [M, K], dense, 16-byte aligned;  scale fp32: block_rows 1: [ceil(K / 128), M]; 128: [ceil(M / 128), ceil(K / 128)];
+ *   M <= 262140 (block_rows 1), 8388480 (128).
+ * scale = max(largest magnitude * fl(1 / 448), 2^-100); code = round(value / scale), to nearest, ties to even, of the
+ * fp32 quotient.  A block that holds an infinity or a NaN has the scale NaN and codes that are no numbers. */
+ES_API es_status_t es_op_quant_e4m3(const void *x, int32_t dtype, int64_t row_stride, int32_t M, int32_t K,
+                                    int32_t block_rows, void *codes, float *scale, void *stream);
+
+/* es_op_linear of such operands: C[m, n] = sum over blocks b of a_scale[b, m] * w_scale[n / 128, b] *
+ * sum over k in b of a[m, k] * w[n, k]   (+ R[m, n]); blocks are added in ascending order, in fp32 (few rows: in up to
+ * 8 ranges of blocks, then range by range; the order depends on the sizes and the device's SM count alone).
+ *   a codes [M, K], a_scale fp32 [ceil(K / 128), M];  w codes [N, K], w_scale fp32 [ceil(N / 128), ceil(K / 128)];
+ *   C [M, N], dense, fp16, bf16 or fp32;  R fp32 [M, N] or NULL, only with an fp32 C, may be C itself;
+ *   a, w 16-byte aligned;  K % 16 == 0;  M <= 262140, N <= 2^24.
+ * path: 0 = automatic, 1 = tiles of 128 weight rows, 2 = tiles of 256 x 256 on CTA pairs.
+ * weights_ready != 0: w and w_scale hold their values already when the call is made (when a captured call is
+ *   replayed), whatever still runs on the stream; with few rows they are then read while the kernel in front ends.
+ * Should a wait inside the kernel run out (after a second), the results it was for become NaN. */
+ES_API es_status_t es_op_linear_fp8(const void *a, const float *a_scale, const void *w, const float *w_scale,
+                                    const float *R, void *C, int32_t out_dtype, int32_t M, int32_t N, int32_t K,
+                                    int32_t path, int32_t weights_ready, void *stream);
+
+/* Norm of every query and key head, rotation by the position, and the keys' and values' way into the cache.
+ *   q [n, Hq, hd], k, v [n, Hkv, hd] (fp16 or bf16), token r at + r * its stride elements (heads contiguous; strides % 8
+ *   == 0, 16-byte aligned: slices of a fused QKV product serve); v may be NULL, with v_out;  hd 64, 128 or 256;
+ *   q_gain, k_gain [hd] (fp16, bf16 or fp32): x = x / sqrt(mean over the head of x^2 + eps) * gain; NULL: no norm;
+ *   cosines, sines fp32 [max_pos, rot / 2]: the first rot values of a head are rotated, pairs (2i, 2i + 1), or
+ *   (i, i + rot / 2) with halves != 0;  rot % 16 == 0, 0 <= rot <= hd;  positions int32 [n];
+ *   q_out [n, Hq, hd], dense.  Without slot_map k_out, v_out [n, Hkv, hd], dense; with slot_map int32 [n] they are the
+ *   pages [n_pages, Hkv, page_tokens, hd] of a cache in the layout of es_op_decode_attention, and token r goes to slot
+ *   slot_map[r] = page * page_tokens + offset (page_tokens a power of two >= 16); tokens with a slot outside
+ *   [0, n_pages * page_tokens) are not cached.  Two tokens of a call must not have the same slot.
+ * A token whose position is outside [0, max_pos) (padding) gives zeros in q_out and in dense k_out, v_out and is not
+ * cached.  Arithmetic in fp32, rounded once.  Results must not overlap q, k or v. */
+ES_API es_status_t es_op_qk_norm_rope(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
+                                      int64_t v_stride, int32_t dtype, const void *q_gain, const void *k_gain,
+                                      int32_t gain_dtype, float eps, const float *cosines, const float *sines,
+                                      int32_t max_pos, int32_t rot, int32_t halves, const int32_t *positions,
+                                      void *q_out, void *k_out, void *v_out, int32_t n, int32_t Hq, int32_t Hkv,
+                                      int32_t hd, const int32_t *slot_map, int32_t page_tokens, int32_t n_pages,
+                                      void *stream);
 
 #ifdef __cplusplus
 }

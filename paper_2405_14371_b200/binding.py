@@ -106,6 +106,9 @@ def _load() -> C.CDLL:
         "es_op_decode_attention_kv8_scratch_bytes": (sz, [i32] * 7),
         "es_op_decode_attention_kv8": (i32, [vp, i32, C.c_int64, vp, vp, i32] + [vp] * 5 + [i32] * 9 + [vp, sz, vp]),
         "es_op_sample": (i32, [vp, i32, C.c_int64] + [vp] * 7 + [i32, i32, vp]),
+        "es_op_quant_e4m3": (i32, [vp, i32, C.c_int64, i32, i32, i32, vp, vp, vp]),
+        "es_op_linear_fp8": (i32, [vp] * 6 + [i32] * 6 + [vp]),
+        "es_op_qk_norm_rope": (i32, [vp, C.c_int64] * 3 + [i32, vp, vp, i32, C.c_float, vp, vp, i32, i32, i32] + [vp] * 4 + [i32] * 4 + [vp, i32, i32, vp]),
         "es_op_decode_attention_static_capacity": (sz, []),
         "es_op_decode_attention_static": (i32, [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp]),
     }
@@ -122,7 +125,8 @@ EXPORTS = ("es_shard_workspace_bytes es_shard_create es_shard_prefill es_shard_p
            "es_partition_latency es_partition_throughput es_shard_device_status es_shard_wait_probe es_shard_launch_count es_shard_set_kernel_timing es_shard_kernel_timing es_shard_kernel_timing_detail es_shard_set_step_timing es_shard_step_timing es_shard_destroy es_last_error es_version es_op_rmsnorm "
            "es_op_linear es_op_linear_splitk_workspace_bytes es_op_linear_splitk es_op_prefill_attention es_op_decode_attention_scratch_bytes es_op_decode_attention "
            "es_op_decode_attention_static_capacity es_op_decode_attention_static es_op_kv_plan_max_runs es_op_kv_plan es_op_kv8_append "
-           "es_op_kv8_gather es_op_decode_attention_kv8_scratch_bytes es_op_decode_attention_kv8 es_op_sample").split()
+           "es_op_kv8_gather es_op_decode_attention_kv8_scratch_bytes es_op_decode_attention_kv8 es_op_sample "
+           "es_op_quant_e4m3 es_op_linear_fp8 es_op_qk_norm_rope").split()
 
 
 def es_last_error() -> str:
@@ -512,6 +516,35 @@ def es_op_sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[to
     """(tokens int32 [B], logprobs fp32 [B]) drawn from logits [B, V] (fp32, fp16 or bf16; rows may be spaced) with the random
     numbers u [B] in [0, 1) and per-row settings [B]: temperature, top_p, min_p fp32, top_k int32; None = off."""
     return _call(stream, _native.sample, logits, u, temperature, top_k, top_p, min_p, out)
+
+
+# ---- an attention block with 8-bit weights, normalised heads and a shared prefix -------------------
+
+def es_op_quant_e4m3(x: torch.Tensor, block_rows: int = 1, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
+                     stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(codes float8_e4m3fn [M, K], scale fp32) of x [M, K] (fp16, bf16 or fp32; rows may be spaced): a scale per row and 128
+    columns, [ceil(K / 128), M], or with block_rows = 128 (weights) per block of 128 x 128, [ceil(M / 128), ceil(K / 128)]."""
+    return _call(stream, _native.quant_e4m3, x, block_rows, out)
+
+
+def es_op_linear_fp8(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, residual: Optional[torch.Tensor] = None,
+                     dtype: torch.dtype = torch.float16, path: int = 0, weights_ready: bool = False, out: Optional[torch.Tensor] = None,
+                     stream=None) -> torch.Tensor:
+    """[M, N] = a w^T (+ residual) of codes and scales as es_op_quant_e4m3 gives them for a [M, K] (block_rows 1) and w [N, K]
+    (block_rows 128); residual fp32 [M, N], with dtype fp32 only.  weights_ready: w and w_scale are complete already, whatever
+    still runs on the stream."""
+    return _call(stream, _native.linear_fp8, a, a_scale, w, w_scale, residual, _VALUE_DTYPES.get(dtype, -1), path, int(weights_ready), out)
+
+
+def es_op_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_gain: Optional[torch.Tensor], k_gain: Optional[torch.Tensor], eps: float,
+                       cosines: torch.Tensor, sines: torch.Tensor, positions: torch.Tensor, halves: bool = False, v: Optional[torch.Tensor] = None,
+                       slot_map: Optional[torch.Tensor] = None, k_pages: Optional[torch.Tensor] = None, v_pages: Optional[torch.Tensor] = None,
+                       out: Optional[torch.Tensor] = None, stream=None):
+    """Norm and rotation of q [n, Hq, hd] and k [n, Hkv, hd] (fp16 or bf16; evenly spaced, e.g. slices of a fused projection).
+    cosines, sines fp32 [max_pos, rot / 2]; pairs (2i, 2i + 1), or (i, i + rot / 2) with `halves`.  With slot_map, k_pages (and
+    v, v_pages) the keys and values go into the cache and the result is q [n, Hq * hd]; without, it is (q, k) or
+    (q, k, v), k and v dense [n, Hkv, hd]."""
+    return _call(stream, _native.qk_norm_rope, q, k, q_gain, k_gain, eps, cosines, sines, positions, int(halves), v, slot_map, k_pages, v_pages, out)
 
 
 def _partition(fn, t_comp, O, Req, Mem, Bw):

@@ -1,0 +1,531 @@
+// Products with block-scaled e4m3 operands on the tensor cores (tcgen05 kind::f8f6f4, TMA, TMEM).
+//
+//   C[m, n] = sum over blocks b of 128 columns:  sa[b, m] * sw[n / 128, b] * sum over k in b:  A[m, k] * W[n, k]     (+ R[m, n])
+//
+// The codes of a block are multiplied and added by one accumulation of 4 MMAs in TMEM (K = 32 each); the scales differ from
+// block to block, so each block's sums are read back and join the running fp32 sums of the result in registers,
+// acc = fma(sums, sa * sw, acc), while the tensor cores work on the next block into another TMEM buffer.
+//
+// Two kernels:
+//
+//   * tiles of 128 weight rows (few tokens).  The weights are the M side of the MMA, 16 to 128 tokens its N side, so a decode
+//     batch wastes no tensor-core rows on absent tokens and a block costs a thread 16 to 128 multiply-adds.  Bound: reading
+//     the weights once.  The K range of a tile is shared by a cluster of 1 to 8 CTAs so that the machine is full in one wave;
+//     their sums meet in distributed shared memory and are added in rank order, so the result depends on the sizes alone.
+//   * 256 x 256 tiles on CTA pairs (many tokens): cta_group::2, each CTA stages 128 rows of A and 128 of W per block and
+//     keeps 128 x 256 running sums in the registers of 8 warps (128 each).  Bound: the tensor cores' e4m3 rate, and the
+//     power it draws.
+//
+// Every wait is bounded by a second; the tiles of a CTA whose wait ran out become NaN.
+#include <cooperative_groups.h>
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include "es_internal.cuh"
+#include "fp8.cuh"
+#include "launch.cuh"
+#include "sm100.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace es {
+namespace {
+
+struct alignas(64) Fp8Maps { CUtensorMap a, w; };
+
+struct Fp8Params {
+  const float *as, *ws;      // [K blocks, M], [N blocks, K blocks]
+  const float* R;            // [M, N] or nullptr
+  void* C;
+  int M, N, nkb;
+  int out;                   // ES_DTYPE_*
+  int ready;                 // the weights may be read before the kernel in front has ended
+  int vec;                   // rows of C (and R) start on multiples of 16 bytes
+};
+
+constexpr int BKB = 128;                         // bytes (= codes) of a row per block
+constexpr int W_TILE = 128 * BKB;
+
+__device__ __forceinline__ void store_one(const Fp8Params& p, int64_t at, float v) {
+  if (p.out == ES_DTYPE_F32) {
+    if (p.R) v += p.R[at];
+    ((float*)p.C)[at] = v;
+  } else if (p.out == ES_DTYPE_F16) {
+    ((__half*)p.C)[at] = __float2half_rn(v);
+  } else {
+    ((__nv_bfloat16*)p.C)[at] = __float2bfloat16_rn(v);
+  }
+}
+
+// ---- tiles of 128 weight rows x NT tokens ----------------------------------------------------------
+
+template <int NT> struct RowsCfg {
+  static constexpr int OCC = NT <= 64 ? 2 : 1;                       // CTAs per SM (registers: NT running sums a thread)
+  static constexpr int X_TILE = NT * BKB;
+  static constexpr int STAGE = W_TILE + X_TILE;
+  static constexpr int STAGES = (OCC == 2 ? 108 * 1024 : 200 * 1024) / STAGE;
+  static constexpr int BUFS = NT <= 32 ? 4 : 2;                      // TMEM buffers
+  static constexpr int COLS = BUFS * NT;                             // 64 to 256, a power of two
+  static constexpr int BARS = 2 * STAGES + 2 * BUFS;
+  static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + 2 * NT * 4 + BARS * 8 + 16;
+  static_assert(STAGES * STAGE >= 128 * NT * 4, "the running sums of a CTA go where the ring was");
+};
+
+constexpr int ROWS_THREADS = 192;                // TMA, MMA, four warps of sums
+
+template <int NT>
+__global__ void __launch_bounds__(ROWS_THREADS, RowsCfg<NT>::OCC) linear_fp8_rows_kernel(const __grid_constant__ Fp8Maps maps, const Fp8Params p, const int split) {
+  using L = RowsCfg<NT>;
+  pdl_launch_dependents();
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  unsigned char* ring = smem;                                          // stage: weight tile, token tile
+  float* factor = (float*)(smem + L::STAGES * L::STAGE);               // [2][NT] sa * sw of a block
+  uint64_t* bars = (uint64_t*)(factor + 2 * NT);
+  uint64_t *full = bars, *empty = full + L::STAGES, *acc_full = empty + L::STAGES, *acc_empty = acc_full + L::BUFS;
+  uint32_t* tmem_slot = (uint32_t*)(bars + L::BARS);
+  volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)blockIdx.x % split, n0 = ((int)blockIdx.x / split) * 128, m0 = (int)blockIdx.y * NT;
+  const int b0 = (int)((long long)p.nkb * rank / split), b1 = (int)((long long)p.nkb * (rank + 1) / split);
+
+  if (threadIdx.x == 0) {
+    prefetch_tmap(&maps.a);
+    prefetch_tmap(&maps.w);
+    for (int s = 0; s < L::STAGES; ++s) { mbar_init(smem_u32(&full[s]), 1); mbar_init(smem_u32(&empty[s]), 1); }
+    for (int s = 0; s < L::BUFS; ++s) { mbar_init(smem_u32(&acc_full[s]), 1); mbar_init(smem_u32(&acc_empty[s]), 4); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) tmem_alloc(smem_u32(tmem_slot), L::COLS);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  float acc[NT];
+  bool ok = true;
+  if (warp == 0) {
+    if (lane == 0) {
+      // ---- TMA: weights of the first stages ahead of the wait for the kernel in front, if they are known to be complete ----
+      const int early = min(b1 - b0, L::STAGES);
+      for (int i = 0; i < early; ++i) {
+        mbar_expect_tx(smem_u32(&full[i]), L::STAGE);
+        if (p.ready) tma_load_2d(smem_u32(ring + i * L::STAGE), &maps.w, (b0 + i) * (BKB / 2), n0, smem_u32(&full[i]));
+      }
+      pdl_wait();
+      for (int i = 0; i < early; ++i) {
+        if (!p.ready) tma_load_2d(smem_u32(ring + i * L::STAGE), &maps.w, (b0 + i) * (BKB / 2), n0, smem_u32(&full[i]));
+        tma_load_2d(smem_u32(ring + i * L::STAGE + W_TILE), &maps.a, (b0 + i) * (BKB / 2), m0, smem_u32(&full[i]));
+      }
+      for (int i = early; i < b1 - b0; ++i) {
+        const int s = i % L::STAGES;
+        if (!mbar_wait(smem_u32(&empty[s]), ((i / L::STAGES) & 1) ^ 1, abort_flag, nullptr, 0)) break;
+        const uint32_t fb = smem_u32(&full[s]);
+        mbar_expect_tx(fb, L::STAGE);
+        tma_load_2d(smem_u32(ring + s * L::STAGE), &maps.w, (b0 + i) * (BKB / 2), n0, fb);
+        tma_load_2d(smem_u32(ring + s * L::STAGE + W_TILE), &maps.a, (b0 + i) * (BKB / 2), m0, fb);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      // ---- MMA ----
+      constexpr uint32_t idesc = umma_idesc_f16(128, NT);
+      for (int i = 0; i < b1 - b0; ++i) {
+        const int s = i % L::STAGES, buf = i % L::BUFS;
+        if (!mbar_wait(smem_u32(&full[s]), (i / L::STAGES) & 1, abort_flag, nullptr, 0)) break;
+        if (!mbar_wait(smem_u32(&acc_empty[buf]), ((i / L::BUFS) & 1) ^ 1, abort_flag, nullptr, 0)) break;
+        tc_fence_after();
+        const uint32_t w = smem_u32(ring + s * L::STAGE), x = w + W_TILE;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          umma_f8(tmem + buf * NT, umma_desc_sw128(w + k * 32), umma_desc_sw128(x + k * 32), idesc, k > 0 ? 1u : 0u);
+        umma_commit(smem_u32(&empty[s]));
+        umma_commit(smem_u32(&acc_full[buf]));
+      }
+    }
+  } else {
+    // ---- sums: a thread has one weight row and every token ----
+    const int e = threadIdx.x - 64, quarter = warp & 3;
+    const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
+    const float* ws = p.ws + (int64_t)(n0 / FP8_BLOCK) * p.nkb;
+    const bool mine = e < NT && m0 + e < p.M;                           // this thread brings token e's factors
+    pdl_wait();
+    float next = 0.f;
+    if (mine) next = p.as[(int64_t)b0 * p.M + m0 + e] * ws[b0];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[j] = 0.f;
+    for (int i = 0; i < b1 - b0; ++i) {
+      const int buf = i % L::BUFS;
+      float* f = factor + (i & 1) * NT;
+      if (e < NT) f[e] = next;
+      if (mine && b0 + i + 1 < b1) next = p.as[(int64_t)(b0 + i + 1) * p.M + m0 + e] * ws[b0 + i + 1];
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+      if (ok) ok = mbar_wait(smem_u32(&acc_full[buf]), (i / L::BUFS) & 1, abort_flag, nullptr, 0);
+      if (!__all_sync(0xffffffffu, ok)) { ok = false; continue; }
+      tc_fence_after();
+      constexpr int CH = NT < 32 ? 16 : 32;
+#pragma unroll
+      for (int c = 0; c < NT; c += CH) {
+        uint32_t v[CH];
+        tmem_ld_issue(tmem + lane_off + buf * NT + c, v);
+        tmem_ld_wait(v);
+#pragma unroll
+        for (int j = 0; j < CH; j += 4) {
+          const float4 q = *reinterpret_cast<const float4*>(f + c + j);
+          acc[c + j] = fmaf(__uint_as_float(v[j]), q.x, acc[c + j]);
+          acc[c + j + 1] = fmaf(__uint_as_float(v[j + 1]), q.y, acc[c + j + 1]);
+          acc[c + j + 2] = fmaf(__uint_as_float(v[j + 2]), q.z, acc[c + j + 2]);
+          acc[c + j + 3] = fmaf(__uint_as_float(v[j + 3]), q.w, acc[c + j + 3]);
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&acc_empty[buf]));
+    }
+    if (!ok) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) acc[j] = __uint_as_float(0x7fffffffu);
+    }
+  }
+
+  // ---- teardown, and the sums of the cluster's CTAs ----
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    if (*abort_flag) __nanosleep(100000);
+    tmem_dealloc(tmem, L::COLS);
+  }
+  const int tokens = min(NT, p.M - m0);
+  const int e = (int)threadIdx.x - 64;
+  const int n = n0 + (warp & 3) * 32 + lane;                            // of the four warps of sums
+  if (split == 1) {
+    if (warp >= 2 && n < p.N) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        if (j < tokens) store_one(p, (int64_t)(m0 + j) * p.N + n, acc[j]);
+    }
+    return;
+  }
+  float* sums = (float*)ring;                                           // [NT][128]
+  const int at = (warp & 3) * 32 + lane;
+  if (e >= 0) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) sums[j * 128 + at] = acc[j];
+  }
+  cg::cluster_group cl = cg::this_cluster();
+  cl.sync();
+  if (e >= 0 && n < p.N) {
+    const int j1 = min(tokens, NT * (rank + 1) / split);
+    for (int j = NT * rank / split; j < j1; ++j) {
+      float v = 0.f;
+      for (int r = 0; r < split; ++r) v += cl.map_shared_rank(sums, r)[j * 128 + at];
+      store_one(p, (int64_t)(m0 + j) * p.N + n, v);
+    }
+  }
+  cl.sync();                                                            // nobody leaves while its sums are being read
+}
+
+template <int NT>
+es_status_t launch_rows(const Fp8Maps& maps, const Fp8Params& p, int split, cudaStream_t s) {
+  using L = RowsCfg<NT>;
+  static std::atomic<uint64_t> allowed{0};
+  auto kern = linear_fp8_rows_kernel<NT>;
+  ES_CUDA_CHECK(allow_shared_memory(kern, (int)L::SMEM, &allowed));
+  const dim3 grid((unsigned)((p.N + 127) / 128 * split), (unsigned)((p.M + NT - 1) / NT));
+  ES_CUDA_CHECK(launch_clusters(kern, split > 1 ? split : 0, grid, dim3(ROWS_THREADS), L::SMEM, s, tunables().pdl != 0, maps, p, split));
+  return ES_OK;
+}
+
+// ---- 256 x 256 tiles on CTA pairs ------------------------------------------------------------------
+
+constexpr int P_STAGES = 6, P_STAGE = 2 * W_TILE;                       // 128 rows of A, 128 of W
+constexpr int P_EPI = 8, P_THREADS = 128 + 32 * P_EPI;                  // TMA, MMA and two idle warps; eight warps of sums
+// Registers: 168 a thread at launch (64512 in all); the first four warps give theirs up, 128 * 72 + 256 * 216 = 64512.
+constexpr int P_REGS_FEW = 72, P_REGS_SUMS = 216;
+static_assert(128 * P_REGS_FEW + 32 * P_EPI * P_REGS_SUMS <= 168 * P_THREADS, "the register split must fit what the launch gets");
+constexpr int P_TURN = 32 * 128;                                        // a warp's store tile: 32 rows of 128 bytes
+constexpr size_t P_SMEM = 1024 + (size_t)P_STAGES * P_STAGE + P_EPI * P_TURN + (2 * P_STAGES + 4) * 8 + 16;
+
+__device__ __forceinline__ uint32_t two(float a, float b, int out) {
+  if (out == ES_DTYPE_F16) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// A warp's 32 rows x 128 columns of sums, 128 bytes of every row at a time through its store tile (16-byte pieces at place
+// piece ^ (row & 7): no bank conflicts either way), so that global stores cover whole row segments.
+template <bool WIDE>                                                    // fp32 results
+__device__ __forceinline__ void store_tile(const Fp8Params& p, unsigned char* turn, const uint64_t (&acc)[64], int row0, int n, int lane) {
+  constexpr int CH = WIDE ? 32 : 64;                                    // columns in 128 bytes
+#pragma unroll
+  for (int c = 0; c < 128; c += CH) {
+    __syncwarp();
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      uint4 u;
+      if (WIDE) {
+        const float2 a = unpack_f32x2(acc[(c + 4 * q) / 2]), b = unpack_f32x2(acc[(c + 4 * q) / 2 + 1]);
+        u = make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
+      } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 a = unpack_f32x2(acc[(c + 8 * q) / 2 + i]);
+          w[i] = two(a.x, a.y, p.out);
+        }
+        u = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+      *reinterpret_cast<uint4*>(turn + lane * 128 + ((q ^ (lane & 7)) << 4)) = u;
+    }
+    __syncwarp();
+    if (n + c >= p.N) continue;
+    if (p.vec && n + c + CH <= p.N) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = 4 * i + (lane >> 3), q = lane & 7;
+        if (row0 + r >= p.M) continue;
+        uint4 u = *reinterpret_cast<const uint4*>(turn + r * 128 + ((q ^ (r & 7)) << 4));
+        const int64_t at = (int64_t)(row0 + r) * p.N + n + c + q * (WIDE ? 4 : 8);
+        if (WIDE) {
+          if (p.R) {
+            const float4 x = *reinterpret_cast<const float4*>(p.R + at);
+            u.x = __float_as_uint(__uint_as_float(u.x) + x.x); u.y = __float_as_uint(__uint_as_float(u.y) + x.y);
+            u.z = __float_as_uint(__uint_as_float(u.z) + x.z); u.w = __float_as_uint(__uint_as_float(u.w) + x.w);
+          }
+          *reinterpret_cast<uint4*>((float*)p.C + at) = u;
+        } else {
+          *reinterpret_cast<uint4*>((uint16_t*)p.C + at) = u;
+        }
+      }
+    } else {
+      // ragged or unaligned rows: a column a lane
+      for (int r = 0; r < 32 && row0 + r < p.M; ++r) {
+#pragma unroll
+        for (int i = 0; i < CH / 32; ++i) {
+          const int col = lane + 32 * i;
+          if (n + c + col >= p.N) continue;
+          const int64_t at = (int64_t)(row0 + r) * p.N + n + c + col;
+          if (WIDE) {
+            float v = *reinterpret_cast<const float*>(turn + r * 128 + (((col >> 2) ^ (r & 7)) << 4) + (col & 3) * 4);
+            if (p.R) v += p.R[at];
+            ((float*)p.C)[at] = v;
+          } else {
+            ((uint16_t*)p.C)[at] = *reinterpret_cast<const uint16_t*>(turn + r * 128 + (((col >> 3) ^ (r & 7)) << 4) + (col & 7) * 2);
+          }
+        }
+      }
+    }
+  }
+}
+
+__global__ void __launch_bounds__(P_THREADS, 1) linear_fp8_pair_kernel(const __grid_constant__ Fp8Maps maps, const Fp8Params p, const int m_tiles, const int n_tiles) {
+  pdl_launch_dependents();
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  unsigned char* ring = smem;
+  unsigned char* turn = smem + P_STAGES * P_STAGE;
+  uint64_t* bars = (uint64_t*)(turn + P_EPI * P_TURN);
+  uint64_t *full = bars, *empty = full + P_STAGES, *acc_full = empty + P_STAGES, *acc_empty = acc_full + 2;   // full, acc_empty: rank 0's are used
+  uint32_t* tmem_slot = (uint32_t*)(bars + 2 * P_STAGES + 4);
+  volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  const int tiles = m_tiles * n_tiles;
+
+  // 16 row tiles share a column tile: what a wave of pairs reads then fits in L2
+  auto origin = [&](int tile, int& m0, int& n0) {
+    constexpr int GM = 16;
+    const int per_group = GM * n_tiles;
+    const int first_m = (tile / per_group) * GM;
+    const int gsz = min(GM, m_tiles - first_m);
+    m0 = (first_m + (tile % per_group) % gsz) * 256;
+    n0 = ((tile % per_group) / gsz) * 256;
+  };
+
+  if (threadIdx.x == 0) {
+    prefetch_tmap(&maps.a);
+    prefetch_tmap(&maps.w);
+    for (int s = 0; s < P_STAGES; ++s) { mbar_init(smem_u32(&full[s]), 1); mbar_init(smem_u32(&empty[s]), 1); }
+    for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&acc_full[s]), 1); mbar_init(smem_u32(&acc_empty[s]), 2 * P_EPI); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) tmem_alloc_pair(smem_u32(tmem_slot), 512);
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  pdl_wait();
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(P_REGS_FEW));
+    if (warp == 0 && lane == 0) {
+      int it = 0;
+      bool ok = true;
+      for (int tile = pair; tile < tiles && ok; tile += n_pairs) {
+        int m0, n0;
+        origin(tile, m0, n0);
+        for (int b = 0; b < p.nkb; ++b, ++it) {
+          const int s = it % P_STAGES;
+          if (!mbar_wait(smem_u32(&empty[s]), ((it / P_STAGES) & 1) ^ 1, abort_flag, nullptr, 0)) { ok = false; break; }
+          const uint32_t fb = smem_u32(&full[s]), dst = smem_u32(ring + s * P_STAGE);
+          if (rank == 0) mbar_expect_tx(fb, 2 * P_STAGE);               // both CTAs' bytes land on this barrier
+          tma_load_2d_pair(dst, &maps.a, b * (BKB / 2), m0 + (int)rank * 128, fb);
+          tma_load_2d_pair(dst + W_TILE, &maps.w, b * (BKB / 2), n0 + (int)rank * 128, fb);
+        }
+      }
+    }
+    if (warp == 1 && lane == 0 && rank == 0) {
+      constexpr uint32_t idesc = umma_idesc_f16(256, 256);
+      int it = 0;
+      bool ok = true;
+      for (int tile = pair; tile < tiles && ok; tile += n_pairs) {
+        for (int b = 0; b < p.nkb; ++b, ++it) {
+          const int s = it % P_STAGES, buf = it & 1;
+          ok = mbar_wait(smem_u32(&full[s]), (it / P_STAGES) & 1, abort_flag, nullptr, 0) &&
+               mbar_wait(smem_u32(&acc_empty[buf]), ((it >> 1) & 1) ^ 1, abort_flag, nullptr, 0);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t a = smem_u32(ring + s * P_STAGE), w = a + W_TILE;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            umma_f8_pair(tmem + buf * 256, umma_desc_sw128(a + k * 32), umma_desc_sw128(w + k * 32), idesc, k > 0 ? 1u : 0u);
+          umma_commit_pair(smem_u32(&empty[s]));
+          umma_commit_pair(smem_u32(&acc_full[buf]));
+        }
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(P_REGS_SUMS));
+    const int quarter = warp & 3, half = (warp - 4) >> 2;               // 32 rows, 128 columns
+    unsigned char* my_turn = turn + (warp - 4) * P_TURN;
+    int it = 0;
+    bool ok = true;
+    for (int tile = pair; tile < tiles; tile += n_pairs) {
+      int m0, n0;
+      origin(tile, m0, n0);
+      const int row0 = m0 + (int)rank * 128 + quarter * 32, n = n0 + half * 128;
+      const bool in = row0 + lane < p.M && n < p.N;
+      const float* as = p.as + row0 + lane;
+      const float* ws = p.ws + (int64_t)(n / FP8_BLOCK) * p.nkb;
+      uint64_t acc[64];
+#pragma unroll
+      for (int j = 0; j < 64; ++j) acc[j] = 0;
+      float sa = in ? as[0] : 0.f, sw = in ? ws[0] : 0.f;
+      for (int b = 0; b < p.nkb; ++b, ++it) {
+        const int buf = it & 1;
+        const float f = sa * sw;
+        if (in && b + 1 < p.nkb) { sa = as[(int64_t)(b + 1) * p.M]; sw = ws[b + 1]; }
+        if (ok) ok = mbar_wait(smem_u32(&acc_full[buf]), (it >> 1) & 1, abort_flag, nullptr, 0);
+        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        tc_fence_after();
+        const uint64_t ff = pack_f32x2(f, f);
+        const uint32_t t = tmem + buf * 256 + half * 128 + ((uint32_t)(quarter * 32) << 16);
+        uint32_t v[2][16];
+        tmem_ld_issue(t, v[0]);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          tmem_ld_wait(v[c & 1]);
+          if (c < 7) tmem_ld_issue(t + (c + 1) * 16, v[(c + 1) & 1]);
+          if (c == 7) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_rank0(smem_u32(&acc_empty[buf]));
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            acc[c * 8 + j] = fma_f32x2(pack_f32x2(__uint_as_float(v[c & 1][2 * j]), __uint_as_float(v[c & 1][2 * j + 1])), ff, acc[c * 8 + j]);
+        }
+      }
+      if (!ok) {
+#pragma unroll
+        for (int j = 0; j < 64; ++j) acc[j] = 0x7fffffff7fffffffull;
+      }
+      if (p.out == ES_DTYPE_F32) store_tile<true>(p, my_turn, acc, row0, n, lane);
+      else store_tile<false>(p, my_turn, acc, row0, n, lane);
+    }
+  }
+
+  // neither CTA leaves while its partner may still signal or read it
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  if (warp == 1) {
+    tc_fence_after();
+    if (*abort_flag) __nanosleep(100000);
+    tmem_dealloc_pair(tmem, 512);
+  }
+}
+
+es_status_t launch_pair(const Fp8Maps& maps, const Fp8Params& p, cudaStream_t s) {
+  static std::atomic<uint64_t> allowed{0};
+  ES_CUDA_CHECK(allow_shared_memory(linear_fp8_pair_kernel, (int)P_SMEM, &allowed));
+  const int m_tiles = (p.M + 255) / 256, n_tiles = (p.N + 255) / 256;
+  int pairs = sm_count() / 2;
+  if (pairs > (long long)m_tiles * n_tiles) pairs = m_tiles * n_tiles;
+  ES_CUDA_CHECK(launch_clusters(linear_fp8_pair_kernel, 2, dim3(2 * pairs), dim3(P_THREADS), P_SMEM, s, tunables().pdl != 0, maps, p, m_tiles, n_tiles));
+  return ES_OK;
+}
+
+// CTAs that share a tile's K range: as many as make the busiest SM's time shortest, counted in blocks; starting and joining
+// cost about 4 of them.
+int split_of(long long tiles, int nkb, int slots) {
+  int best = 1;
+  long long least = 0;
+  for (int s = 1; s <= 8 && s <= nkb; ++s) {
+    const long long cost = ((tiles * s + slots - 1) / slots) * ((nkb + s - 1) / s + 4);
+    if (s == 1 || cost < least) { best = s; least = cost; }
+  }
+  return best;
+}
+
+template <int NT>
+es_status_t rows_auto(const Fp8Maps& maps, const Fp8Params& p, cudaStream_t s) {
+  const long long tiles = (long long)((p.N + 127) / 128) * ((p.M + NT - 1) / NT);
+  return launch_rows<NT>(maps, p, split_of(tiles, p.nkb, RowsCfg<NT>::OCC * sm_count()), s);
+}
+
+}  // namespace
+}  // namespace es
+
+using namespace es;
+
+extern "C" es_status_t es_op_linear_fp8(const void* a, const float* a_scale, const void* w, const float* w_scale, const float* R, void* C, int32_t out_dtype, int32_t M,
+                                        int32_t N, int32_t K, int32_t path, int32_t weights_ready, void* stream) {
+  if (M < 0 || N <= 0 || K <= 0) return fail(ES_ERR_INVALID_ARG, "bad sizes");
+  if (out_dtype != ES_DTYPE_F16 && out_dtype != ES_DTYPE_BF16 && out_dtype != ES_DTYPE_F32) return fail(ES_ERR_INVALID_ARG, "the result must be fp16, bf16 or fp32");
+  if (R && out_dtype != ES_DTYPE_F32) return fail(ES_ERR_INVALID_ARG, "a residual needs an fp32 result");
+  if (path < 0 || path > 2) return fail(ES_ERR_INVALID_ARG, "unknown path %d", path);
+  if (K % 16) return fail(ES_ERR_SHAPE, "K = %d is no multiple of 16", K);
+  if (M > FP8_MAX_ROWS || N > (1 << 24)) return fail(ES_ERR_RANGE, "more than %d rows or 2^24 columns", FP8_MAX_ROWS);
+  if (M == 0) return ES_OK;
+  if (!a || !a_scale || !w || !w_scale || !C) return fail(ES_ERR_INVALID_ARG, "null argument");
+  const size_t esize = out_dtype == ES_DTYPE_F32 ? 4 : 2;
+  if (((uintptr_t)a | (uintptr_t)w) % 16 || ((uintptr_t)a_scale | (uintptr_t)w_scale | (uintptr_t)R) % 4 || (uintptr_t)C % esize)
+    return fail(ES_ERR_INVALID_ARG, "a and w must be 16-byte aligned, the others by their elements");
+  if (!tma_available()) return fail(ES_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+  // 256 x 256 tiles from the size on at which they are as good as full (below, more and smaller tiles on single CTAs)
+  const bool pairs = path == 2 || (path == 0 && M > 128 && (long long)((M + 255) / 256) * ((N + 255) / 256) * 2 >= sm_count());
+  const int NT = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
+  Fp8Params p{a_scale, w_scale, R, C, M, N, (K + FP8_BLOCK - 1) / FP8_BLOCK, out_dtype, weights_ready != 0, 0};
+  p.vec = ((size_t)N * esize) % 16 == 0 && ((uintptr_t)C | (uintptr_t)R) % 16 == 0;
+  Fp8Maps maps;
+  // two codes make one 16-bit element of the map: boxes of 64 elements are 128 bytes
+  ES_TRY(tma_encode_2d_f16(&maps.a, a, M, K / 2, K / 2, pairs ? 128 : NT));
+  ES_TRY(tma_encode_2d_f16(&maps.w, w, N, K / 2, K / 2, 128));
+  cudaStream_t s = (cudaStream_t)stream;
+  if (pairs) return launch_pair(maps, p, s);
+  if (NT == 16) return rows_auto<16>(maps, p, s);
+  if (NT == 32) return rows_auto<32>(maps, p, s);
+  if (NT == 64) return rows_auto<64>(maps, p, s);
+  return rows_auto<128>(maps, p, s);
+}

@@ -1,4 +1,5 @@
-// Python entry points of the calls that a decode step makes once per layer (8-bit cache, sampling): argument checks, result
+// Python entry points of the calls that a decode step makes once per layer (8-bit cache and weights, heads,
+// sampling): argument checks, result
 // memory and the current stream handled here, so that the host side of a call is a few microseconds.  The work itself is
 // the C ABI's; binding.py holds the signatures and their documentation.
 #define PY_SSIZE_T_CLEAN
@@ -341,6 +342,147 @@ PyObject* sample(PyObject* const* a) {
   return result;
 }
 
+PyObject* quant_e4m3(PyObject* const* a) {
+  const at::Tensor& x = tensor(a[0], "x");
+  const int block_rows = int_arg(a[1], "block_rows");
+  need_cuda_first(x, "x");
+  cudaStream_t stream = launch_stream({{&x, "x"}});
+  const int dtype = value_dtype(x);
+  if (x.dim() != 2 || dtype < 0 || (x.stride(1) != 1 && x.size(1) != 1)) refuse("x must be fp16, bf16 or fp32 [M, K] with dense rows");
+  if (block_rows != 1 && block_rows != 128) refuse("block_rows must be 1 or 128");
+  const int M = fit(x.size(0), "M"), K = fit(x.size(1), "K"), blocks = (int)(((int64_t)K + 127) / 128);
+  if (M > 1 && x.stride(0) < K) refuse("the rows of x must lie one after the other (no expanded dimensions)");
+  const int64_t s0 = block_rows == 1 ? blocks : ((int64_t)M + 127) / 128, s1 = block_rows == 1 ? M : blocks;
+  at::Tensor codes, scale;
+  if (a[2] == Py_None) {
+    codes = empty({M, K}, at::kFloat8_e4m3fn, x);
+    scale = empty({s0, s1}, at::kFloat, x);
+  } else {
+    if (!PyTuple_Check(a[2]) || PyTuple_GET_SIZE(a[2]) != 2) refuse("out must be two tensors");
+    codes = tensor(PyTuple_GET_ITEM(a[2], 0), "out[0]");
+    scale = tensor(PyTuple_GET_ITEM(a[2], 1), "out[1]");
+    launch_stream({{&codes, "out[0]"}, {&scale, "out[1]"}});
+    if (codes.scalar_type() != at::kFloat8_e4m3fn || scale.scalar_type() != at::kFloat || !codes.is_contiguous() || !scale.is_contiguous() || codes.dim() != 2 ||
+        scale.dim() != 2 || codes.size(0) != M || codes.size(1) != K || scale.size(0) != s0 || scale.size(1) != s1)
+      refuse("out must be contiguous float8_e4m3fn [M, K] and fp32 scales");
+  }
+  const int64_t stride = M > 1 ? x.stride(0) : K;
+  call([&] { return es_op_quant_e4m3(x.data_ptr(), dtype, stride, M, K, block_rows, codes.data_ptr(), (float*)scale.data_ptr(), stream); });
+  if (a[2] != Py_None) { Py_INCREF(a[2]); return a[2]; }
+  PyObject* result = PyTuple_New(2);
+  if (!result) throw PythonError{};
+  PyTuple_SET_ITEM(result, 0, THPVariable_Wrap(std::move(codes)));
+  PyTuple_SET_ITEM(result, 1, THPVariable_Wrap(std::move(scale)));
+  return result;
+}
+
+void need_scales(const at::Tensor& t, const char* name, int64_t s0, int64_t s1) {
+  if (t.scalar_type() != at::kFloat || !t.is_contiguous() || t.dim() != 2 || t.size(0) != s0 || t.size(1) != s1)
+    refuse(std::string(name) + " must be contiguous fp32 [" + std::to_string(s0) + ", " + std::to_string(s1) + "]");
+}
+
+PyObject* linear_fp8(PyObject* const* p) {
+  const at::Tensor &a = tensor(p[0], "a"), &as = tensor(p[1], "a_scale"), &w = tensor(p[2], "w"), &ws = tensor(p[3], "w_scale");
+  const at::Tensor* r = maybe_tensor(p[4], "residual");
+  const int dtype = int_arg(p[5], "dtype"), path = int_arg(p[6], "path"), ready = int_arg(p[7], "weights_ready");
+  const at::Tensor* given = maybe_tensor(p[8], "out");
+  need_cuda_first(a, "a");
+  cudaStream_t stream = launch_stream({{&a, "a"}, {&as, "a_scale"}, {&w, "w"}, {&ws, "w_scale"}, {r, "residual"}, {given, "out"}});
+  for (const Named& t : {Named{&a, "a"}, Named{&w, "w"}})
+    if (t.t->scalar_type() != at::kFloat8_e4m3fn || t.t->dim() != 2 || !t.t->is_contiguous()) refuse(std::string(t.name) + " must be contiguous float8_e4m3fn, two dimensions");
+  const int M = fit(a.size(0), "M"), K = fit(a.size(1), "K"), N = fit(w.size(0), "N");
+  if (w.size(1) != K) refuse("a and w must have the same number of columns");
+  need_scales(as, "a_scale", ((int64_t)K + 127) / 128, M);
+  need_scales(ws, "w_scale", ((int64_t)N + 127) / 128, ((int64_t)K + 127) / 128);
+  if (dtype != ES_DTYPE_F16 && dtype != ES_DTYPE_BF16 && dtype != ES_DTYPE_F32) refuse("dtype must be fp16, bf16 or fp32");
+  if (r && (r->scalar_type() != at::kFloat || !r->is_contiguous() || r->dim() != 2 || r->size(0) != M || r->size(1) != N)) refuse("residual must be contiguous fp32 [M, N]");
+  at::Tensor out;
+  if (given) {
+    if (given->scalar_type() != scalar_of(dtype) || !given->is_contiguous() || given->dim() != 2 || given->size(0) != M || given->size(1) != N)
+      refuse("out must be contiguous [M, N] of dtype");
+    out = *given;
+  } else {
+    out = empty({M, N}, scalar_of(dtype), a);
+  }
+  call([&] {
+    return es_op_linear_fp8(a.data_ptr(), (const float*)as.data_ptr(), w.data_ptr(), (const float*)ws.data_ptr(), r ? (const float*)r->data_ptr() : nullptr,
+                            out.data_ptr(), dtype, M, N, K, path, ready, stream);
+  });
+  return THPVariable_Wrap(std::move(out));
+}
+
+PyObject* qk_norm_rope(PyObject* const* a) {
+  const at::Tensor &q = tensor(a[0], "q"), &k = tensor(a[1], "k");
+  const at::Tensor *qg = maybe_tensor(a[2], "q_gain"), *kg = maybe_tensor(a[3], "k_gain");
+  const double eps = PyFloat_AsDouble(a[4]);
+  if (eps == -1.0 && PyErr_Occurred()) throw PythonError{};
+  const at::Tensor &cosines = tensor(a[5], "cosines"), &sines = tensor(a[6], "sines"), &positions = tensor(a[7], "positions");
+  const int halves = int_arg(a[8], "halves");
+  const at::Tensor *v = maybe_tensor(a[9], "v"), *slots = maybe_tensor(a[10], "slot_map"), *kp = maybe_tensor(a[11], "k_pages"), *vp = maybe_tensor(a[12], "v_pages"),
+                   *given = maybe_tensor(a[13], "out");
+  need_cuda_first(q, "q");
+  cudaStream_t stream = launch_stream({{&q, "q"}, {&k, "k"}, {qg, "q_gain"}, {kg, "k_gain"}, {&cosines, "cosines"}, {&sines, "sines"}, {&positions, "positions"}, {v, "v"},
+                                       {slots, "slot_map"}, {kp, "k_pages"}, {vp, "v_pages"}, {given, "out"}});
+  const int dtype = value_dtype(q);
+  if (q.dim() != 3 || dtype < 0 || dtype == ES_DTYPE_F32) refuse("q must be fp16 or bf16 [n, Hq, hd]");
+  const int n = fit(q.size(0), "n"), Hq = fit(q.size(1), "Hq"), hd = fit(q.size(2), "hd");
+  if (k.dim() != 3 || k.size(0) != n || k.size(2) != hd || k.scalar_type() != q.scalar_type()) refuse("k must be [n, Hkv, hd] of q's type");
+  const int Hkv = fit(k.size(1), "Hkv");
+  if (v && (v->sizes() != k.sizes() || v->scalar_type() != q.scalar_type())) refuse("v must be [n, Hkv, hd] of q's type");
+  int gain_dtype = ES_DTYPE_F32;
+  if (qg && kg && qg->scalar_type() != kg->scalar_type()) refuse("q_gain and k_gain must have the same type");
+  for (const Named& g : {Named{qg, "q_gain"}, Named{kg, "k_gain"}})
+    if (g.t) {
+      gain_dtype = value_dtype(*g.t);
+      if (gain_dtype < 0 || !g.t->is_contiguous() || g.t->dim() != 1 || g.t->size(0) != hd) refuse(std::string(g.name) + " must be contiguous fp16, bf16 or fp32 [hd]");
+    }
+  for (const Named& t : {Named{&cosines, "cosines"}, Named{&sines, "sines"}})
+    if (t.t->scalar_type() != at::kFloat || !t.t->is_contiguous() || t.t->dim() != 2 || t.t->sizes() != cosines.sizes())
+      refuse(std::string(t.name) + " must be contiguous fp32 [max_pos, rot / 2], both the same");
+  need_ints({{&positions, "positions"}, {slots, "slot_map"}});
+  if (positions.numel() < n || (slots && slots->numel() < n)) refuse("positions and slot_map must have an entry for every token");
+  const int max_pos = fit(cosines.size(0), "max_pos");
+  if (cosines.size(1) > hd) throw Refusal{ES_ERR_SHAPE, "rot must be at most the head dimension"};
+  const int rot = 2 * (int)cosines.size(1);
+  if (!slots != !kp || (kp && !v != !vp) || (!kp && vp)) refuse("slot_map, k_pages and, with v, v_pages go together");
+  int P = 0, n_pages = 0;
+  at::Tensor ko, vo;
+  if (kp) {
+    for (const Named& t : {Named{kp, "k_pages"}, Named{vp, "v_pages"}})
+      if (t.t && (t.t->scalar_type() != q.scalar_type() || !t.t->is_contiguous() || t.t->dim() != 4 || t.t->sizes() != kp->sizes() || t.t->size(1) != Hkv || t.t->size(3) != hd))
+        refuse(std::string(t.name) + " must be contiguous [n_pages, Hkv, P, hd] of q's type");
+    n_pages = fit(kp->size(0), "n_pages");
+    P = fit(kp->size(2), "page_tokens");
+    ko = *kp;
+    if (vp) vo = *vp;
+  } else {
+    ko = empty({n, Hkv, hd}, q.scalar_type(), q);
+    if (v) vo = empty({n, Hkv, hd}, q.scalar_type(), q);
+  }
+  const int64_t qs = row_stride(q, "q"), ks = row_stride(k, "k"), vs = v ? row_stride(*v, "v") : 0;
+  at::Tensor qo;
+  if (given) {
+    if (given->scalar_type() != q.scalar_type() || !given->is_contiguous() || given->dim() != 2 || given->size(0) != n || given->size(1) != (int64_t)Hq * hd)
+      refuse("out must be contiguous [n, Hq * hd] of q's type");
+    qo = *given;
+  } else {
+    qo = empty({n, (int64_t)Hq * hd}, q.scalar_type(), q);
+  }
+  call([&] {
+    return es_op_qk_norm_rope(q.data_ptr(), qs, k.data_ptr(), ks, v ? v->data_ptr() : nullptr, vs, dtype, qg ? qg->data_ptr() : nullptr, kg ? kg->data_ptr() : nullptr,
+                              gain_dtype, (float)eps, (const float*)cosines.data_ptr(), (const float*)sines.data_ptr(), max_pos, rot, halves,
+                              (const int32_t*)positions.data_ptr(), qo.data_ptr(), ko.data_ptr(), v ? vo.data_ptr() : nullptr, n, Hq, Hkv, hd,
+                              slots ? (const int32_t*)slots->data_ptr() : nullptr, P, n_pages, stream);
+  });
+  if (kp) return THPVariable_Wrap(std::move(qo));
+  PyObject* result = PyTuple_New(v ? 3 : 2);
+  if (!result) throw PythonError{};
+  PyTuple_SET_ITEM(result, 0, THPVariable_Wrap(std::move(qo)));
+  PyTuple_SET_ITEM(result, 1, THPVariable_Wrap(std::move(ko)));
+  if (v) PyTuple_SET_ITEM(result, 2, THPVariable_Wrap(std::move(vo)));
+  return result;
+}
+
 // ---- module ------------------------------------------------------------------------------------
 
 void raise_refusal(int status, const std::string& message) {
@@ -393,6 +535,7 @@ PyObject* set_errors(PyObject*, PyObject* args) {
 PyMethodDef g_methods[] = {
     ENTRY("kv_plan", kv_plan, 9), ENTRY("kv8_append", kv8_append, 8), ENTRY("kv8_gather", kv8_gather, 7),
     ENTRY("decode_attention_kv8", decode_attention_kv8, 10), ENTRY("sample", sample, 7),
+    ENTRY("quant_e4m3", quant_e4m3, 3), ENTRY("linear_fp8", linear_fp8, 9), ENTRY("qk_norm_rope", qk_norm_rope, 14),
     {"set_errors", set_errors, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
