@@ -520,6 +520,36 @@ ES_API es_status_t es_op_qk_norm_rope(const void *q, int64_t q_stride, const voi
                                       int32_t hd, const int32_t *slot_map, int32_t page_tokens, int32_t n_pages,
                                       void *stream);
 
+/* Decode attention of a batch whose sequences share prefixes: the newest T tokens of every sequence over the keys of its
+ * prefix and over its own, a prefix read once for all of its sequences.
+ *   q (fp16 or bf16) [B, T, Hq, hd], token b * T + t at q + (b * T + t) * q_stride elements (heads contiguous, q_stride
+ *   % 8 == 0, 16-byte aligned);  k_pages, v_pages of q's type [n_pages, Hkv, page_tokens, hd], 16-byte aligned, page_tokens
+ *   a power of two >= 16;  out [B, T, Hq * hd], dense, of q's type, 8-byte aligned;
+ *   group_begin int32 [groups + 1]: sequences group_begin[g] .. group_begin[g + 1] - 1 share prefix g; sequences outside
+ *   every group have none.  Entries are clamped to [0, B], and a group begins no earlier than those before it end;
+ *   prefix_table int32 [groups, prefix_pages], prefix_len int32 [groups];  block_table int32 [B, pages_per_seq], ctx_len
+ *   int32 [B]: a sequence's own keys, its T newest included.  groups = 0 (and NULL for the three) is a batch without
+ *   prefixes.
+ * Query t sees the whole prefix and its sequence's own keys 0 .. ctx_len[b] - T + t, and nothing of the others reaches it,
+ * infinities and NaN included; a query that sees none gives zeros.  Scale 1/sqrt(hd); scores, softmax and sums in fp32,
+ * probabilities enter the product with V in q's type.  Table entries outside [0, n_pages) are pages that nobody sees;
+ * lengths above max_prefix (<= prefix_pages * page_tokens) or max_ctx (<= pages_per_seq * page_tokens) are read as those.
+ *   hd 64 or 128;  Hq a multiple of Hkv, at most 128 times as many;  groups + B <= 8192;  B * T * Hq <= 2^26;  n_pages *
+ *   Hkv * page_tokens < 2^31 - 256;  Hkv * (tiles of 64 keys, of each sequence and of each prefix for every 128 rows) <= 2^30.
+ *   scratch: dev, 16-byte aligned, es_op_decode_attention_prefix_scratch_bytes(...) bytes of the call's sizes on the current
+ *   device, in use until the call's work is done (calls that overlap on the GPU need one each).  Uninitialised is fine.
+ * Should a wait inside the kernel run out (after a second), the rows it was for become NaN. */
+ES_API size_t es_op_decode_attention_prefix_scratch_bytes(int32_t groups, int32_t B, int32_t T, int32_t Hq, int32_t Hkv,
+                                                          int32_t hd);
+ES_API es_status_t es_op_decode_attention_prefix(const void *q, int32_t dtype, int64_t q_stride, const void *k_pages,
+                                                 const void *v_pages, const int32_t *prefix_table,
+                                                 const int32_t *prefix_len, const int32_t *group_begin, int32_t groups,
+                                                 int32_t prefix_pages, const int32_t *block_table,
+                                                 const int32_t *ctx_len, void *out, int32_t B, int32_t T, int32_t Hq,
+                                                 int32_t Hkv, int32_t hd, int32_t page_tokens, int32_t pages_per_seq,
+                                                 int32_t n_pages, int32_t max_prefix, int32_t max_ctx, void *scratch,
+                                                 size_t scratch_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -109,6 +109,8 @@ def _load() -> C.CDLL:
         "es_op_quant_e4m3": (i32, [vp, i32, C.c_int64, i32, i32, i32, vp, vp, vp]),
         "es_op_linear_fp8": (i32, [vp] * 6 + [i32] * 6 + [vp]),
         "es_op_qk_norm_rope": (i32, [vp, C.c_int64] * 3 + [i32, vp, vp, i32, C.c_float, vp, vp, i32, i32, i32] + [vp] * 4 + [i32] * 4 + [vp, i32, i32, vp]),
+        "es_op_decode_attention_prefix_scratch_bytes": (sz, [i32] * 6),
+        "es_op_decode_attention_prefix": (i32, [vp, i32, C.c_int64] + [vp] * 5 + [i32, i32] + [vp] * 3 + [i32] * 10 + [vp, sz, vp]),
         "es_op_decode_attention_static_capacity": (sz, []),
         "es_op_decode_attention_static": (i32, [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp]),
     }
@@ -126,7 +128,7 @@ EXPORTS = ("es_shard_workspace_bytes es_shard_create es_shard_prefill es_shard_p
            "es_op_linear es_op_linear_splitk_workspace_bytes es_op_linear_splitk es_op_prefill_attention es_op_decode_attention_scratch_bytes es_op_decode_attention "
            "es_op_decode_attention_static_capacity es_op_decode_attention_static es_op_kv_plan_max_runs es_op_kv_plan es_op_kv8_append "
            "es_op_kv8_gather es_op_decode_attention_kv8_scratch_bytes es_op_decode_attention_kv8 es_op_sample "
-           "es_op_quant_e4m3 es_op_linear_fp8 es_op_qk_norm_rope").split()
+           "es_op_quant_e4m3 es_op_linear_fp8 es_op_qk_norm_rope es_op_decode_attention_prefix_scratch_bytes es_op_decode_attention_prefix").split()
 
 
 def es_last_error() -> str:
@@ -545,6 +547,21 @@ def es_op_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_gain: Optional[torch.
     v, v_pages) the keys and values go into the cache and the result is q [n, Hq * hd]; without, it is (q, k) or
     (q, k, v), k and v dense [n, Hkv, hd]."""
     return _call(stream, _native.qk_norm_rope, q, k, q_gain, k_gain, eps, cosines, sines, positions, int(halves), v, slot_map, k_pages, v_pages, out)
+
+
+def es_op_decode_attention_prefix_scratch_bytes(groups: int, B: int, T: int, Hq: int, Hkv: int, hd: int) -> int:
+    return int(lib.es_op_decode_attention_prefix_scratch_bytes(groups, B, T, Hq, Hkv, hd))
+
+
+def es_op_decode_attention_prefix(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, prefix_table: Optional[torch.Tensor],
+                                  prefix_len: Optional[torch.Tensor], group_begin: Optional[torch.Tensor], block_table: torch.Tensor,
+                                  ctx_len: torch.Tensor, max_prefix: int, max_ctx: int, scratch: Optional[torch.Tensor] = None,
+                                  out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Attention of q [B, T, Hq, hd] (the T newest tokens of every sequence; [B, Hq, hd] for one) over pages of q's type: over the
+    prefix that sequences group_begin[g] .. group_begin[g + 1] - 1 share and over each one's own keys (block_table, ctx_len);
+    returns [B, T, Hq * hd] (or [B, Hq * hd]) of q's type.  q's tokens may be evenly spaced slices of larger rows."""
+    return _call(stream, _native.decode_attention_prefix, q, k_pages, v_pages, prefix_table, prefix_len, group_begin, block_table, ctx_len, max_prefix,
+                 max_ctx, scratch, out)
 
 
 def _partition(fn, t_comp, O, Req, Mem, Bw):

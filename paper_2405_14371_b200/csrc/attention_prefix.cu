@@ -1,0 +1,694 @@
+// Decode attention for a batch whose sequences share long prefixes (tcgen05 / TMEM / TMA): a prefix is read once per KV head
+// for all of its sequences' queries, a sequence's own keys once for its own.
+//
+//   out = sum_k exp(s_k - m) v_k / sum_k exp(s_k - m),   s_k = q . k / sqrt(hd),  over the prefix's keys and the own ones
+//
+// A segment is a prefix or the own keys of one sequence.  Its rows are the query heads of a KV head's group, of all tokens
+// that see it: a whole group of sequences makes one product with many rows where one sequence makes G.  An item is a segment,
+// a KV head and a row tile (as many whole tokens as 128 rows hold); its keys come in tiles of 64.  The tiles of all items form
+// one line, cut into equal stretches, one for each resident CTA (two per SM), whatever the lengths: the host knows none.
+// Every piece of an item that lies in a stretch leaves (o, m, l) in fp32 in the scratch, and a second kernel joins, for each row,
+// the pieces of its prefix and of its own keys in order of the line, so results do not depend on scheduling.
+//
+// Within a stretch, per tile (the roles of the prefill kernel):
+//   S = Q K^T      M = 128 rows, N = 64 keys, fp32 in TMEM, two buffers: the product of the next tile runs beside this softmax
+//   softmax        four warps, a row a thread: running maximum and sum in fp32; P in q's type takes K's place in the ring.  The
+//                  sum is of the rounded P, so rounding them moves no weight to or from other keys on average.  Warps
+//                  without rows (a single sequence has G) only keep the protocol.
+//   O += P V       fp32 in TMEM, rescaled when a row's maximum has grown by more than 8 (log2), as P stays below 256
+// The ring runs on over the items' borders, and the next item's Q is fetched while the last tile of the one before is finished.
+//
+// Nothing of a key that a row does not see reaches it: scores are masked by selection, V rows behind the length are zeroed
+// in shared memory, pages that do not exist are read as zeros (a TMA box outside the tensor).  Of a draft's last tokens, which
+// only later rows see, infinities and NaN in V are taken out of the product and added to the rows that see them at the end.
+//
+// Every wait is bounded by a second; the rows of a piece whose wait ran out become NaN.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <string.h>
+
+#include "es_internal.cuh"
+#include "launch.cuh"
+#include "sm100.cuh"
+
+namespace es {
+namespace {
+
+constexpr int KT = 64;                   // keys of a tile
+constexpr int THREADS = 192;             // TMA, MMA, four softmax warps
+constexpr int TMEM_COLS = 256;           // S: two buffers of 64 columns, O: up to 128
+constexpr float GAP = 8.0f;
+constexpr int MIN_UNITS = 2;             // tiles of a stretch, at least
+constexpr int MAX_SEGMENTS = 8192;
+
+struct alignas(64) PrefixMaps { CUtensorMap q, k, v; };
+
+struct PrefixParams {
+  const int *prefix_table, *prefix_len, *begin, *table, *ctx;
+  const void* v_pages;
+  void* out;
+  int *line, *group_of, *first;          // scratch: cumulative tiles [segments + 1], prefix of every sequence [B], first sequences [groups + 1]
+  float *ml_p, *o_p, *ml_o, *o_o;        // pieces of prefixes and of own keys: [rows][2], [rows][hd]
+  int B, T, Hq, Hkv, G, P, log2P, groups, prefix_pages, pps, n_pages, max_prefix, max_ctx;
+  int TT;                                // tokens of a row tile
+  int box;                               // tokens of a page that one copy brings
+  float scale_log2e;
+};
+
+// A piece of an item: what one CTA does of it.
+struct Piece {
+  int seg, group, kvh, rt;               // segment; group: it is a prefix
+  int tok0, ntok;                        // its tokens (token = sequence * T + t)
+  int len;                               // its keys
+  int j0, j1;                            // tiles of the piece
+};
+
+__device__ __forceinline__ int tiles_of(int len) { return (len + KT - 1) / KT; }
+
+// CTAs that share the line of `units` tiles, and which has which
+__device__ __forceinline__ int active(int units, int ctas) { return max(1, min(ctas, units / MIN_UNITS)); }
+__device__ __forceinline__ int start_of(int cta, int units, int n) { return (int)((long long)units * cta / n); }
+__device__ __forceinline__ int cta_of(int unit, int units, int n) { return (int)(((long long)(unit + 1) * n - 1) / units); }
+
+__device__ __forceinline__ Piece piece_at(const PrefixParams& p, const int* line, const int* lens, const int* first, int u, int end) {
+  Piece x;
+  int lo = 0, hi = p.groups + p.B;                      // line[lo] <= u < line[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (line[mid] <= u) lo = mid; else hi = mid;
+  }
+  x.seg = lo;
+  x.group = lo < p.groups;
+  x.len = lens[lo];
+  if (x.group) {
+    x.tok0 = first[lo] * p.T;
+    x.ntok = (first[lo + 1] - first[lo]) * p.T;
+  } else {
+    x.tok0 = (lo - p.groups) * p.T;
+    x.ntok = p.T;
+  }
+  const int row_tiles = (x.ntok + p.TT - 1) / p.TT, k = tiles_of(x.len), r = u - line[lo], item = r / k;
+  x.j0 = r - item * k;
+  x.j1 = min(k, x.j0 + (end - u));
+  x.kvh = item / row_tiles;
+  x.rt = item - x.kvh * row_tiles;
+  return x;
+}
+
+// First row of a piece's partials, in the prefixes' or the own keys' part of the scratch: the rows of the items before it, and
+// a tile's worth for each CTA before this one.
+__device__ __forceinline__ int64_t piece_row(const PrefixParams& p, const Piece& x, int cta) {
+  const int64_t before = (int64_t)x.tok0 * p.Hq + ((int64_t)x.kvh * x.ntok + (int64_t)x.rt * p.TT) * p.G;
+  return before + (int64_t)cta * ((x.group ? p.TT : min(p.TT, p.T)) * p.G);
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+
+// Two probabilities rounded to q's type, and what they became.
+template <bool BF16>
+__device__ __forceinline__ uint32_t round_pair(float a, float b, float& sum) {
+  if (BF16) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(&h);
+    sum += __uint_as_float(w << 16) + __uint_as_float(w & 0xffff0000u);
+    return w;
+  }
+  const __half2 h = __floats2half2_rn(a, b);
+  const float2 f = __half22float2(h);
+  sum += f.x + f.y;
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+template <int HD>
+struct Smem {
+  static constexpr int HALVES = HD / 64;
+  static constexpr int Q_BYTES = 128 * HD * 2, KV_BYTES = KT * HD * 2, P_BYTES = 128 * KT * 2;
+  static constexpr bool P_IN_K = KV_BYTES >= P_BYTES;
+  static constexpr int BARS = 12;
+  static constexpr size_t FIXED = 1024 + Q_BYTES + 4 * KV_BYTES + (P_IN_K ? 0 : 2 * P_BYTES) + BARS * 8 + 64;
+};
+
+template <int HD, bool BF16>
+__global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_constant__ PrefixMaps maps, const PrefixParams p) {
+  using L = Smem<HD>;
+  pdl_launch_dependents();
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  unsigned char* q_s = smem;                                   // [halves][128 rows][128 B]
+  unsigned char* k_s = q_s + L::Q_BYTES;                       // [2 stages][halves][64 rows][128 B]
+  unsigned char* v_s = k_s + 2 * L::KV_BYTES;
+  unsigned char* p_own = v_s + 2 * L::KV_BYTES;
+  uint64_t* bars = (uint64_t*)(p_own + (L::P_IN_K ? 0 : 2 * L::P_BYTES));
+  uint64_t *q_full = bars, *q_empty = bars + 1, *kv_full = bars + 2, *kv_empty = bars + 4, *s_full = bars + 6, *p_full = bars + 8, *pv_done = bars + 10;
+  uint32_t* tmem_slot = (uint32_t*)(bars + L::BARS);
+  volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
+  volatile int* pages_seen = (volatile int*)(tmem_slot + 2);   // [2] of a stage's tile: which 16 tokens lie in pages that exist
+  volatile int* tail_bad = (volatile int*)(tmem_slot + 4);     // piece whose last tokens hold a V that is no number
+  int* line = (int*)(tmem_slot + 8);                           // [segments + 1]
+  int* lens = line + p.groups + p.B + 1;                       // [segments]
+  int* first = lens + p.groups + p.B;                          // [groups + 1]
+  auto p_tile = [&](int s) -> unsigned char* { return L::P_IN_K ? k_s + s * L::KV_BYTES : p_own + s * L::P_BYTES; };
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    prefetch_tmap(&maps.q);
+    prefetch_tmap(&maps.k);
+    prefetch_tmap(&maps.v);
+    for (int i = 0; i < L::BARS; ++i) mbar_init(smem_u32(&bars[i]), (i == 8 || i == 9) ? 4 : 1);   // p_full: four warps
+    *abort_flag = 0;
+    *tail_bad = -1;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) tmem_alloc(smem_u32(tmem_slot), TMEM_COLS);
+  pdl_wait();
+
+  // ---- the line: cumulative tiles of the segments ----
+  const int segments = p.groups + p.B;
+  if (warp == 0) {
+    int units = 0, seen = 0;                                   // so far: tiles, sequences of earlier groups
+    for (int base = 0; base < segments; base += 32) {
+      const int s = base + lane;
+      const bool group = s < p.groups;
+      int len = 0, from = 0, to = 0;
+      if (s < segments) {
+        len = group ? min(max(p.prefix_len[s], 0), p.max_prefix) : min(max(p.ctx[s - p.groups], 0), p.max_ctx);
+        if (group) { from = min(max(p.begin[s], 0), p.B); to = min(max(p.begin[s + 1], 0), p.B); }
+      }
+      // groups in order: each begins where the ones before have ended, at least
+      int reach = max(from, to);
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, reach, o); if (lane >= o) reach = max(reach, x); }
+      reach = max(reach, seen);
+      int before = __shfl_up_sync(0xffffffffu, reach, 1);
+      if (lane == 0) before = seen;
+      before = max(before, from);                              // this group: [before, reach)
+      if (group) {
+        first[s] = before;
+        if (s == p.groups - 1) first[p.groups] = reach;
+      }
+      const int tokens = group ? (reach - before) * p.T : p.T;
+      int mine = s < segments ? p.Hkv * ((tokens + p.TT - 1) / p.TT) * tiles_of(len) : 0;
+      const int own = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, mine, o); if (lane >= o) mine += x; }
+      if (s < segments) { lens[s] = len; line[s] = units + mine - own; }
+      units += __shfl_sync(0xffffffffu, mine, 31);
+      seen = __shfl_sync(0xffffffffu, reach, 31);
+    }
+    if (lane == 0) line[segments] = units;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot, tmem_s = tmem_base, tmem_o = tmem_base + 128;
+  const int units = line[segments], ctas = active(units, (int)gridDim.x), cta = (int)blockIdx.x;
+  const int u0 = cta < ctas ? start_of(cta, units, ctas) : 0, u1 = cta < ctas ? start_of(cta + 1, units, ctas) : 0;
+
+  if (warp == 0) {
+    // ---- TMA: a lane per page of a tile ----
+    const int chunks = KT / p.box;                             // copies along the tile's keys
+    const int lines = p.n_pages * p.Hkv * p.P;                 // outside the tensor: zeros
+    int it = 0, pieces = 0;
+    bool ok = true;
+    for (int u = u0; u < u1 && ok; ++pieces) {
+      const Piece x = piece_at(p, line, lens, first, u, u1);
+      const int* pages = x.group ? p.prefix_table + (int64_t)x.seg * p.prefix_pages : p.table + (int64_t)(x.seg - p.groups) * p.pps;
+      for (int j = x.j0; j < x.j1; ++j, ++it) {
+        const int s = it & 1;
+        int row = lines, here = 0;
+        if (lane < chunks) {
+          const int t0 = j * KT + lane * p.box;
+          if (t0 < x.len) {
+            const int page = pages[t0 >> p.log2P];
+            if ((unsigned)page < (unsigned)p.n_pages) {
+              row = (page * p.Hkv + x.kvh) * p.P + (t0 & (p.P - 1));
+              here = ((1 << (p.box / 16)) - 1) << (lane * (p.box / 16));
+            }
+          }
+        }
+        here = __reduce_or_sync(0xffffffffu, here);
+        ok = mbar_wait(smem_u32(&kv_empty[s]), ((it >> 1) & 1) ^ 1, abort_flag, nullptr, 0);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        const uint32_t fb = smem_u32(&kv_full[s]);
+        if (lane == 0) {
+          pages_seen[s] = here;
+          mbar_expect_tx(fb, 2 * L::KV_BYTES);
+        }
+        __syncwarp();
+        if (lane < chunks) {
+#pragma unroll
+          for (int h = 0; h < L::HALVES; ++h) {
+            tma_load_2d(smem_u32(k_s + s * L::KV_BYTES + h * (KT * 128) + lane * p.box * 128), &maps.k, h * 64, row, fb);
+            tma_load_2d(smem_u32(v_s + s * L::KV_BYTES + h * (KT * 128) + lane * p.box * 128), &maps.v, h * 64, row, fb);
+          }
+        }
+        if (j == x.j0) {                                       // the first tile is under way before Q's place is free
+          ok = mbar_wait(smem_u32(q_empty), (pieces & 1) ^ 1, abort_flag, nullptr, 0);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          if (lane == 0) {
+            mbar_expect_tx(smem_u32(q_full), p.TT * p.G * HD * 2);
+#pragma unroll
+            for (int h = 0; h < L::HALVES; ++h)
+              tma_load_3d(smem_u32(q_s + h * (128 * 128)), &maps.q, h * 64, x.kvh * p.G, x.tok0 + x.rt * p.TT, smem_u32(q_full));
+          }
+        }
+      }
+      u += x.j1 - x.j0;
+    }
+    // what the second kernel needs to find the pieces
+    if (cta == 0) {
+      for (int s = lane; s <= segments; s += 32) p.line[s] = line[s];
+      for (int s = lane; s <= p.groups; s += 32) p.first[s] = p.groups ? first[s] : 0;
+      for (int b = lane; b < p.B; b += 32) {
+        int lo = -1, hi = p.groups;                            // first[lo] <= b < first[hi]
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (first[mid] <= b) lo = mid; else hi = mid;
+        }
+        p.group_of[b] = lo >= 0 && b < first[lo + 1] ? lo : -1;
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && u0 < u1) {
+      // ---- MMA: whichever of the next S product and the next P V is ready ----
+      constexpr uint32_t type = BF16 ? (1u << 7) | (1u << 10) : 0u;
+      constexpr uint32_t idesc_s = umma_idesc_f16(128, KT) | type;
+      constexpr uint32_t idesc_o = umma_idesc_f16(128, HD) | type | (1u << 16);        // V is MN-major
+      const int n = u1 - u0;
+      Piece xs = piece_at(p, line, lens, first, u0, u1), xo = xs;
+      int s_next = 0, s_end = xs.j1 - xs.j0, s_piece = 0, o_end = s_end;
+      bool s_first = true, o_first = true;
+      uint64_t t_start = global_timer_ns();
+      for (int j = 0; j < n;) {
+        bool progressed = false;
+        if (s_next < n && s_next <= j + 1 && mbar_test(smem_u32(&kv_full[s_next & 1]), (s_next >> 1) & 1) &&
+            (!s_first || mbar_test(smem_u32(q_full), s_piece & 1))) {
+          tc_fence_after();
+          const uint32_t kb = smem_u32(k_s + (s_next & 1) * L::KV_BYTES);
+#pragma unroll
+          for (int k = 0; k < HD / 16; ++k) {
+            const int hf = k / 4, kk = k % 4;
+            umma_f16(tmem_s + (uint32_t)((s_next & 1) * KT), umma_desc_sw128(smem_u32(q_s + hf * (128 * 128)) + kk * 32),
+                     umma_desc_sw128(kb + hf * (KT * 128) + kk * 32), idesc_s, k > 0 ? 1u : 0u);
+          }
+          umma_commit(smem_u32(&s_full[s_next & 1]));
+          ++s_next;
+          s_first = false;
+          if (s_next == s_end) {                               // the piece's last S product frees Q
+            umma_commit(smem_u32(q_empty));
+            if (s_next < n) {
+              xs = piece_at(p, line, lens, first, u0 + s_next, u1);
+              s_end += xs.j1 - xs.j0;
+              ++s_piece;
+              s_first = true;
+            }
+          }
+          progressed = true;
+        }
+        // P is complete (and with it, on a piece's first tile, the way of the earlier O out of TMEM: the same warps did both)
+        if (s_next > j && mbar_test(smem_u32(&p_full[j & 1]), (j >> 1) & 1)) {
+          tc_fence_after();
+          const int s = j & 1;
+          const uint32_t vb = smem_u32(v_s + s * L::KV_BYTES), pb = smem_u32(p_tile(s));
+#pragma unroll
+          for (int k = 0; k < KT / 16; ++k)
+            umma_f16(tmem_o, umma_desc_sw128(pb + k * 32), umma_desc_sw128_mn(vb + k * (16 * 128), KT * 128, 1024), idesc_o, (!o_first || k > 0) ? 1u : 0u);
+          umma_commit(smem_u32(&kv_empty[s]));
+          umma_commit(smem_u32(pv_done));
+          ++j;
+          o_first = false;
+          if (j == o_end && j < n) {
+            xo = piece_at(p, line, lens, first, u0 + j, u1);
+            o_end += xo.j1 - xo.j0;
+            o_first = true;
+          }
+          progressed = true;
+        }
+        if (progressed) {
+          t_start = 0;
+        } else {
+          if (*abort_flag) break;
+          const uint64_t now = global_timer_ns();
+          if (t_start == 0) t_start = now;
+          if (now - t_start > 1000000000ull) { *abort_flag = 1; break; }      // a second without progress
+        }
+      }
+    }
+  } else {
+    // ---- softmax: thread = row, TMEM lane quarter = warp % 4 ----
+    const int quarter = warp & 3, r = quarter * 32 + lane, e = (int)threadIdx.x - 64;
+    const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
+    int it = 0, pieces = 0;
+    bool ok = true;
+    for (int u = u0; u < u1; ++pieces) {
+      const Piece x = piece_at(p, line, lens, first, u, u1);
+      const int token = x.rt * p.TT + r / p.G;                 // of the segment
+      const bool real = r < p.TT * p.G && token < x.ntok;
+      const bool idle = !__any_sync(0xffffffffu, real);
+      const int lim = !real ? 0 : x.group ? x.len : min(x.len, x.len - p.T + token + 1);      // keys that the row sees
+      const int tail = x.group ? x.len : max(0, x.len - p.T + 1);                             // keys from here on are seen by some rows only
+      float m_ref = -INFINITY, l_run = 0.f;
+      for (int j = x.j0; j < x.j1 && ok; ++j, ++it) {
+        const int s = it & 1;
+        ok = mbar_wait(smem_u32(&s_full[s]), (it >> 1) & 1, abort_flag, nullptr, 0);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after();
+        const int k0 = j * KT;
+        unsigned char* vt = v_s + s * L::KV_BYTES;
+        if (x.len - k0 < KT || k0 + KT > tail) {               // V is touched below: its arrival, long over, is seen by this thread too
+          ok = mbar_wait(smem_u32(&kv_full[s]), (it >> 1) & 1, abort_flag, nullptr, 0);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+        }
+        if (x.len - k0 < KT) {                                 // V behind the last key: zeros
+          const int from = x.len - k0;
+          for (int i = e; i < (KT - from) * (HD / 8); i += 128) {
+            const int row = from + i / (HD / 8), c = i % (HD / 8);
+            *reinterpret_cast<uint4*>(vt + (c >> 3) * (KT * 128) + row * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+          }
+        }
+        if (tail < x.len && k0 + KT > tail) {
+          // keys that only later tokens see: what is no number leaves the product
+          const int from = max(0, tail - k0), to = min(KT, x.len - k0);
+          for (int i = e; i < (to - from) * (HD / 2); i += 128) {
+            const int row = from + i / (HD / 2), c = i % (HD / 2);
+            uint32_t* at = reinterpret_cast<uint32_t*>(vt + (c >> 5) * (KT * 128) + row * 128 + (c & 31) * 4);
+            const uint32_t w = *at, inf = BF16 ? 0x7f80u : 0x7c00u;
+            uint32_t keep = 0xffffffffu;
+            if ((w & inf) == inf) keep &= 0xffff0000u;
+            if (((w >> 16) & inf) == inf) keep &= 0xffffu;
+            if (keep != 0xffffffffu) { *at = w & keep; *tail_bad = pieces; }
+          }
+        }
+        bool move = false;
+        float alpha = 1.f;
+        if (!idle) {
+          uint32_t sr[2][32];
+          tmem_ld_issue(tmem_s + (uint32_t)(s * KT) + lane_off, sr[0]);
+          tmem_ld_issue(tmem_s + (uint32_t)(s * KT) + lane_off + 32, sr[1]);
+          tmem_ld_wait(sr[0]);
+          tmem_ld_wait(sr[1]);
+          float sc[KT];
+#pragma unroll
+          for (int c = 0; c < KT; ++c) sc[c] = __uint_as_float(sr[c / 32][c % 32]);
+          const int nk = lim - k0, seen = pages_seen[s];
+          if (__any_sync(0xffffffffu, nk < KT) || seen != 15) {
+#pragma unroll
+            for (int c = 0; c < KT; ++c) sc[c] = (c < nk && ((seen >> (c / 16)) & 1)) ? sc[c] : -INFINITY;
+          }
+          float mx = sc[0];
+#pragma unroll
+          for (int c = 1; c < KT; ++c) mx = fmaxf(mx, sc[c]);
+          mx *= p.scale_log2e;
+          move = mx > m_ref + GAP || (m_ref == -INFINITY && mx > -INFINITY);
+          const float m_new = move ? mx : m_ref, m_use = m_new == -INFINITY ? 0.f : m_new;
+          alpha = move ? ex2(m_ref - m_use) : 1.f;
+          float sum = 0.f;
+          uint32_t packed[KT / 2];
+#pragma unroll
+          for (int c = 0; c < KT; c += 2)
+            packed[c / 2] = round_pair<BF16>(ex2(fmaf(sc[c], p.scale_log2e, -m_use)), ex2(fmaf(sc[c + 1], p.scale_log2e, -m_use)), sum);
+          l_run = l_run * alpha + sum;
+          m_ref = m_new;
+          unsigned char* prow = p_tile(s) + r * 128;
+#pragma unroll
+          for (int c = 0; c < 8; ++c)
+            *reinterpret_cast<uint4*>(prow + ((c ^ (r & 7)) << 4)) = make_uint4(packed[4 * c], packed[4 * c + 1], packed[4 * c + 2], packed[4 * c + 3]);
+        }
+        // P V of the tile before has landed: its phases are followed one by one (a parity wait tells only neighbours apart)
+        if (it > 0) {
+          ok = mbar_wait(smem_u32(pv_done), (it - 1) & 1, abort_flag, nullptr, 0);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after();
+          if (j > x.j0 && __any_sync(0xffffffffu, move)) {
+#pragma unroll 1
+            for (int c = 0; c < HD; c += 32) {
+              float o[32];
+              tmem_ld32(tmem_o + lane_off + c, o);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] *= alpha;
+              tmem_st32(tmem_o + lane_off + c, o);
+            }
+          }
+        }
+        fence_proxy_async_smem();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&p_full[s]));
+      }
+      if (ok) {
+        ok = mbar_wait(smem_u32(pv_done), (it - 1) & 1, abort_flag, nullptr, 0);
+        ok = __all_sync(0xffffffffu, ok);
+        tc_fence_after();
+      }
+      // the piece's part of its rows
+      const int64_t row = piece_row(p, x, cta) + r;
+      float* ml = (x.group ? p.ml_p : p.ml_o) + row * 2;
+      float* po = (x.group ? p.o_p : p.o_o) + row * HD;
+      if (!idle) {
+        if (real) *reinterpret_cast<float2*>(ml) = ok ? make_float2(m_ref, l_run) : make_float2(0.f, __uint_as_float(0x7fffffffu));
+        const bool bad = *tail_bad == pieces;
+        if (ok) {
+#pragma unroll 1
+          for (int c = 0; c < HD; c += 32) {
+            float o[32];
+            __syncwarp();
+            tmem_ld32(tmem_o + lane_off + c, o);
+            if (bad) {
+              for (int key = max(tail, x.j0 * KT); key < min(lim, x.j1 * KT); ++key) {
+                const int page = p.table[(int64_t)(x.seg - p.groups) * p.pps + (key >> p.log2P)];
+                if ((unsigned)page >= (unsigned)p.n_pages) continue;
+                const uint16_t* v = (const uint16_t*)p.v_pages + (((int64_t)page * p.Hkv + x.kvh) * p.P + (key & (p.P - 1))) * HD + c;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                  const float f = BF16 ? __uint_as_float((uint32_t)v[i] << 16) : __half2float(*reinterpret_cast<const __half*>(v + i));
+                  if (!isfinite(f)) o[i] += f;
+                }
+              }
+            }
+            if (real) {
+#pragma unroll
+              for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(po + c + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+            }
+          }
+        }
+      }
+      tc_fence_before();
+      u += x.j1 - x.j0;
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    if (*abort_flag) __nanosleep(100000);
+    tmem_dealloc(tmem_base, TMEM_COLS);
+  }
+}
+
+// ---- the pieces of a row, joined in order of the line: a warp per token and head ------------------
+
+constexpr int JOIN_WARPS = 4;
+
+template <int HD, bool BF16>
+__global__ void __launch_bounds__(JOIN_WARPS * 32) prefix_join_kernel(const PrefixParams p, const int ctas) {
+  pdl_launch_dependents();
+  constexpr int D = HD / 32;                                   // values of a lane
+  const int lane = threadIdx.x & 31;
+  const int64_t at = (int64_t)blockIdx.x * JOIN_WARPS + (threadIdx.x >> 5);
+  pdl_wait();
+  if (at >= (int64_t)p.B * p.T * p.Hq) return;
+  const int token = (int)(at / p.Hq), h = (int)(at % p.Hq), kvh = h / p.G, g = h - kvh * p.G, b = token / p.T;
+  const int units = p.line[p.groups + p.B], n = active(units, ctas);
+  const int group = p.group_of[b];
+  float top = -INFINITY, sum = 0.f, o[D];
+#pragma unroll
+  for (int i = 0; i < D; ++i) o[i] = 0.f;
+#pragma unroll 1
+  for (int part = 0; part < 2; ++part) {
+    Piece x;
+    x.group = part == 0;
+    if (x.group && group < 0) continue;
+    x.seg = x.group ? group : p.groups + b;
+    x.tok0 = x.group ? p.first[group] * p.T : b * p.T;
+    x.ntok = x.group ? (p.first[group + 1] - p.first[group]) * p.T : p.T;
+    x.kvh = kvh;
+    const int local = token - x.tok0, row_tiles = (x.ntok + p.TT - 1) / p.TT;
+    x.rt = local / p.TT;
+    const int begin = p.line[x.seg], tiles = (p.line[x.seg + 1] - begin) / (p.Hkv * row_tiles);
+    if (tiles == 0) continue;
+    const int u = begin + (kvh * row_tiles + x.rt) * tiles, c0 = cta_of(u, units, n), c1 = cta_of(u + tiles - 1, units, n);
+    const int64_t row0 = piece_row(p, x, 0) + (local - x.rt * p.TT) * p.G + g, step = piece_row(p, x, 1) - piece_row(p, x, 0);
+    const float *ml = x.group ? p.ml_p : p.ml_o, *po = x.group ? p.o_p : p.o_o;
+    for (int base = c0; base <= c1; base += 32) {
+      const int c = base + lane;
+      float2 v = make_float2(-INFINITY, 0.f);
+      if (c <= c1) v = *reinterpret_cast<const float2*>(ml + (row0 + c * step) * 2);
+      float m = v.x;
+#pragma unroll
+      for (int w = 16; w > 0; w >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
+      const float m_new = fmaxf(top, m);
+      const float use = m_new == -INFINITY ? 0.f : m_new, old = ex2(top - use), f = ex2(v.x - use);
+      float l = v.y * f;
+#pragma unroll
+      for (int w = 16; w > 0; w >>= 1) l += __shfl_xor_sync(0xffffffffu, l, w);
+      sum = sum * old + l;
+      top = m_new;
+#pragma unroll
+      for (int i = 0; i < D; ++i) o[i] *= old;
+      const int k = min(32, c1 - base + 1);
+#pragma unroll 4
+      for (int q = 0; q < k; ++q) {
+        const float w = __shfl_sync(0xffffffffu, f, q);
+        const float* src = po + (row0 + (base + q) * step) * HD + lane * D;
+        if (D == 4) {
+          const float4 t = *reinterpret_cast<const float4*>(src);
+          o[0] = fmaf(t.x, w, o[0]); o[1] = fmaf(t.y, w, o[1]); o[2] = fmaf(t.z, w, o[2]); o[D - 1] = fmaf(t.w, w, o[D - 1]);
+        } else {
+          const float2 t = *reinterpret_cast<const float2*>(src);
+          o[0] = fmaf(t.x, w, o[0]); o[1] = fmaf(t.y, w, o[1]);
+        }
+      }
+    }
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  uint16_t* out = (uint16_t*)p.out + at * HD + lane * D;
+  uint32_t w[D / 2];
+#pragma unroll
+  for (int i = 0; i < D; i += 2) {
+    if (BF16) {
+      const __nv_bfloat162 v = __floats2bfloat162_rn(o[i] * inv, o[i + 1] * inv);
+      w[i / 2] = *reinterpret_cast<const uint32_t*>(&v);
+    } else {
+      const __half2 v = __floats2half2_rn(o[i] * inv, o[i + 1] * inv);
+      w[i / 2] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+  }
+  if (D == 4) *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[D / 2 - 1]);
+  else *reinterpret_cast<uint32_t*>(out) = w[0];
+}
+
+// ---- host ------------------------------------------------------------------------------------------
+
+struct Layout {
+  size_t line, group_of, first, ml_p, o_p, ml_o, o_o, bytes;
+};
+
+int tokens_of_tile(int G) { return 128 / G; }
+
+Layout layout_of(int groups, int B, int T, int Hq, int G, int hd) {
+  const int TT = tokens_of_tile(G);
+  const int64_t ctas = 2LL * sm_count(), rows = (int64_t)B * T * Hq;
+  const int64_t rows_p = groups ? rows + ctas * (TT * G) : 0, rows_o = rows + ctas * ((TT < T ? TT : T) * G);
+  Layout l;
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
+  l.line = take((size_t)(groups + B + 1) * 4);
+  l.group_of = take((size_t)B * 4);
+  l.first = take((size_t)(groups + 1) * 4);
+  l.ml_p = take((size_t)rows_p * 8);
+  l.o_p = take((size_t)rows_p * hd * 4);
+  l.ml_o = take((size_t)rows_o * 8);
+  l.o_o = take((size_t)rows_o * hd * 4);
+  l.bytes = at;
+  return l;
+}
+
+es_status_t check_sizes(int groups, int B, int T, int Hq, int Hkv, int hd) {
+  if (groups < 0 || B <= 0 || T <= 0 || Hq <= 0 || Hkv <= 0) return fail(ES_ERR_INVALID_ARG, "bad sizes");
+  if (Hq % Hkv || Hq / Hkv > 128) return fail(ES_ERR_SHAPE, "Hq must be a multiple of Hkv, at most 128 times as many");
+  if (hd != 64 && hd != 128) return fail(ES_ERR_SHAPE, "head_dim must be 64 or 128");
+  if ((long long)groups + B > MAX_SEGMENTS) return fail(ES_ERR_RANGE, "more than %d prefixes and sequences", MAX_SEGMENTS);
+  if ((long long)B * T * Hq > (1 << 26)) return fail(ES_ERR_RANGE, "more than 2^26 query heads");
+  return ES_OK;
+}
+
+template <int HD, bool BF16>
+es_status_t launch(const PrefixMaps& maps, const PrefixParams& p, cudaStream_t s) {
+  auto kern = prefix_attn_kernel<HD, BF16>;
+  const size_t smem = Smem<HD>::FIXED + (size_t)(2 * (p.groups + p.B) + p.groups + 2) * 4;
+  static std::atomic<uint64_t> allowed{0};
+  ES_CUDA_CHECK(allow_shared_memory(kern, 227 * 1024, &allowed));
+  const bool pdl = tunables().pdl != 0;
+  // two CTAs share an SM while both fit
+  const int ctas = (smem <= 112 * 1024 ? 2 : 1) * sm_count();
+  ES_CUDA_CHECK(launch_kernel(kern, dim3(ctas), dim3(THREADS), smem, s, pdl, maps, p));
+  const int64_t rows = (int64_t)p.B * p.T * p.Hq;
+  ES_CUDA_CHECK(launch_kernel(prefix_join_kernel<HD, BF16>, dim3((unsigned)((rows + JOIN_WARPS - 1) / JOIN_WARPS)), dim3(JOIN_WARPS * 32), 0, s, pdl, p, ctas));
+  return ES_OK;
+}
+
+}  // namespace
+}  // namespace es
+
+using namespace es;
+
+extern "C" size_t es_op_decode_attention_prefix_scratch_bytes(int32_t groups, int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t hd) {
+  if (check_sizes(groups, B, T, Hq, Hkv, hd) != ES_OK) return 0;
+  return layout_of(groups, B, T, Hq, Hq / Hkv, hd).bytes;
+}
+
+extern "C" es_status_t es_op_decode_attention_prefix(const void* q, int32_t dtype, int64_t q_stride, const void* k_pages, const void* v_pages,
+                                                     const int32_t* prefix_table, const int32_t* prefix_len, const int32_t* group_begin, int32_t groups,
+                                                     int32_t prefix_pages, const int32_t* block_table, const int32_t* ctx_len, void* out, int32_t B, int32_t T,
+                                                     int32_t Hq, int32_t Hkv, int32_t hd, int32_t page_tokens, int32_t pages_per_seq, int32_t n_pages,
+                                                     int32_t max_prefix, int32_t max_ctx, void* scratch, size_t scratch_bytes, void* stream) {
+  if (dtype != ES_DTYPE_F16 && dtype != ES_DTYPE_BF16) return fail(ES_ERR_INVALID_ARG, "q and pages must be fp16 or bf16");
+  ES_TRY(check_sizes(groups, B, T, Hq, Hkv, hd));
+  if (!q || !k_pages || !v_pages || !block_table || !ctx_len || !out || (groups && (!prefix_table || !prefix_len || !group_begin)))
+    return fail(ES_ERR_INVALID_ARG, "null argument");
+  if (page_tokens < 16 || (page_tokens & (page_tokens - 1))) return fail(ES_ERR_SHAPE, "page_tokens must be a power of two, at least 16");
+  if (n_pages <= 0 || pages_per_seq <= 0 || max_ctx <= 0 || (groups && (prefix_pages <= 0 || max_prefix <= 0))) return fail(ES_ERR_INVALID_ARG, "bad sizes");
+  if ((long long)max_ctx > (long long)page_tokens * pages_per_seq || (groups && (long long)max_prefix > (long long)page_tokens * prefix_pages))
+    return fail(ES_ERR_RANGE, "max_ctx or max_prefix exceeds its block table");
+  if ((long long)n_pages * Hkv * page_tokens > INT32_MAX - 256) return fail(ES_ERR_RANGE, "a page pool exceeds 2^31 rows");
+  if (max_ctx > (1 << 30) || max_prefix > (1 << 30)) return fail(ES_ERR_RANGE, "max_ctx or max_prefix exceeds 2^30");
+  if (q_stride % 8 || q_stride < (int64_t)Hq * hd || q_stride > (1LL << 38)) return fail(ES_ERR_INVALID_ARG, "q_stride must be a multiple of 8, at least Hq * hd");
+  if (((uintptr_t)q | (uintptr_t)k_pages | (uintptr_t)v_pages | (uintptr_t)scratch) % 16 || (uintptr_t)out % 8)
+    return fail(ES_ERR_INVALID_ARG, "q, pages and scratch must be 16-byte aligned, out 8-byte aligned");
+  const int G = Hq / Hkv, TT = tokens_of_tile(G);
+  // tiles on the line: every token's row tiles, a part of one more for each group
+  const long long own_tiles = (max_ctx + KT - 1) / KT, prefix_tiles = groups ? (max_prefix + KT - 1) / KT : 0;
+  const long long line = Hkv * (B * (long long)((T + TT - 1) / TT) * own_tiles + ((long long)B * T / TT + 1 + groups) * prefix_tiles);
+  if (line > (1LL << 30)) return fail(ES_ERR_RANGE, "heads * tokens * keys exceed one launch");
+  const Layout l = layout_of(groups, B, T, Hq, G, hd);
+  if (!scratch || scratch_bytes < l.bytes) return fail(ES_ERR_WORKSPACE, "scratch: %zu bytes given, %zu needed", scratch ? scratch_bytes : (size_t)0, l.bytes);
+
+  PrefixParams p{};
+  p.prefix_table = prefix_table; p.prefix_len = prefix_len; p.begin = group_begin; p.table = block_table; p.ctx = ctx_len;
+  p.v_pages = v_pages;
+  p.out = out;
+  char* base = (char*)scratch;
+  p.line = (int*)(base + l.line); p.group_of = (int*)(base + l.group_of); p.first = (int*)(base + l.first);
+  p.ml_p = (float*)(base + l.ml_p); p.o_p = (float*)(base + l.o_p); p.ml_o = (float*)(base + l.ml_o); p.o_o = (float*)(base + l.o_o);
+  p.B = B; p.T = T; p.Hq = Hq; p.Hkv = Hkv; p.G = G; p.P = page_tokens; p.groups = groups;
+  while ((1 << p.log2P) < page_tokens) ++p.log2P;
+  p.prefix_pages = prefix_pages; p.pps = pages_per_seq; p.n_pages = n_pages; p.max_prefix = groups ? max_prefix : 0; p.max_ctx = max_ctx;
+  p.TT = TT;
+  p.box = page_tokens < KT ? page_tokens : KT;
+  p.scale_log2e = 1.4426950408889634f / sqrtf((float)hd);
+  PrefixMaps maps;
+  ES_TRY(tma_encode_3d_f16(&maps.q, q, (int64_t)B * T, Hq, hd, q_stride, TT, G));
+  const int64_t lines = (int64_t)n_pages * Hkv * page_tokens;
+  ES_TRY(tma_encode_2d_f16(&maps.k, k_pages, lines, hd, hd, p.box));
+  ES_TRY(tma_encode_2d_f16(&maps.v, v_pages, lines, hd, hd, p.box));
+  cudaStream_t s = (cudaStream_t)stream;
+  if (dtype == ES_DTYPE_F16) return hd == 128 ? launch<128, false>(maps, p, s) : launch<64, false>(maps, p, s);
+  return hd == 128 ? launch<128, true>(maps, p, s) : launch<64, true>(maps, p, s);
+}

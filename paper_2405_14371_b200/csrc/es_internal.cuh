@@ -141,6 +141,8 @@ es_status_t tc_build_maps(const LinearParams& p, int epi, int64_t a_rows, TcMaps
 // TMA tensor map (128 bytes, 64-byte aligned) of an fp16 row-major matrix [rows, cols] with row stride
 // ld elements: boxes of 64 columns x box_rows rows, 128-byte swizzle, zero fill outside.
 es_status_t tma_encode_2d_f16(void* map, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows);
+// the same of [tokens, heads, cols] with tokens ld elements apart and heads dense; boxes of 64 columns, box_heads, box_tokens
+es_status_t tma_encode_3d_f16(void* map, const void* base, int64_t tokens, int64_t heads, int64_t cols, int64_t ld, int box_tokens, int box_heads);
 bool tma_available();
 
 // ---- element-wise / reductions ---------------------------------------------------------------

@@ -349,6 +349,20 @@ es_status_t tma_encode_2d_f16(void* map, const void* base, int64_t rows, int64_t
   return ES_OK;
 }
 
+es_status_t tma_encode_3d_f16(void* map, const void* base, int64_t tokens, int64_t heads, int64_t cols, int64_t ld, int box_tokens, int box_heads) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return fail(ES_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+  cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)heads, (cuuint64_t)tokens};
+  cuuint64_t strides[2] = {(cuuint64_t)cols * 2, (cuuint64_t)ld * 2};
+  cuuint32_t box[3] = {64u, (cuuint32_t)box_heads, (cuuint32_t)box_tokens};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = fn(reinterpret_cast<CUtensorMap*>(map), CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(base), dims,
+                  strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(ES_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
+  return ES_OK;
+}
+
 int linear_tc_splits(const LinearParams& p, int epi) {
   // Worth it when 256-wide tiles over the whole K range would leave at least half of the SMs idle;
   // every slice keeps at least four 64-element K blocks.

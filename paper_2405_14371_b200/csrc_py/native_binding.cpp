@@ -1,7 +1,6 @@
-// Python entry points of the calls that a decode step makes once per layer (8-bit cache and weights, heads,
-// sampling): argument checks, result
-// memory and the current stream handled here, so that the host side of a call is a few microseconds.  The work itself is
-// the C ABI's; binding.py holds the signatures and their documentation.
+// Python entry points of the calls that a decode step makes once per layer (8-bit cache, sampling, 8-bit weights, heads,
+// shared prefixes): argument checks, result memory and the current stream handled here, so that the host side of a call is a
+// few microseconds.  The work itself is the C ABI's; binding.py holds the signatures and their documentation.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -483,6 +482,64 @@ PyObject* qk_norm_rope(PyObject* const* a) {
   return result;
 }
 
+PyObject* decode_attention_prefix(PyObject* const* a) {
+  const at::Tensor &q = tensor(a[0], "q"), &kp = tensor(a[1], "k_pages"), &vp = tensor(a[2], "v_pages");
+  const at::Tensor *pt = maybe_tensor(a[3], "prefix_table"), *pl = maybe_tensor(a[4], "prefix_len"), *gb = maybe_tensor(a[5], "group_begin");
+  const at::Tensor &table = tensor(a[6], "block_table"), &ctx = tensor(a[7], "ctx_len");
+  const int max_prefix = int_arg(a[8], "max_prefix"), max_ctx = int_arg(a[9], "max_ctx");
+  const at::Tensor *scratch = maybe_tensor(a[10], "scratch"), *given = maybe_tensor(a[11], "out");
+  need_cuda_first(q, "q");
+  cudaStream_t stream = launch_stream({{&q, "q"}, {&kp, "k_pages"}, {&vp, "v_pages"}, {pt, "prefix_table"}, {pl, "prefix_len"}, {gb, "group_begin"},
+                                       {&table, "block_table"}, {&ctx, "ctx_len"}, {scratch, "scratch"}, {given, "out"}});
+  need_ints({{pt, "prefix_table"}, {pl, "prefix_len"}, {gb, "group_begin"}, {&table, "block_table"}, {&ctx, "ctx_len"}});
+  const int dims = (int)q.dim(), dtype = value_dtype(q);
+  if ((dims != 3 && dims != 4) || dtype < 0 || dtype == ES_DTYPE_F32) refuse("q must be fp16 or bf16 [B, T, Hq, hd] or [B, Hq, hd]");
+  for (const Named& t : {Named{&kp, "k_pages"}, Named{&vp, "v_pages"}})
+    if (t.t->scalar_type() != q.scalar_type() || !t.t->is_contiguous() || t.t->dim() != 4 || t.t->sizes() != kp.sizes() || t.t->size(3) != q.size(dims - 1))
+      refuse(std::string(t.name) + " must be contiguous [n_pages, Hkv, P, hd] of q's type");
+  const int n_pages = fit(kp.size(0), "n_pages"), Hkv = fit(kp.size(1), "Hkv"), P = fit(kp.size(2), "page_tokens"), hd = fit(kp.size(3), "hd");
+  const int B = fit(q.size(0), "B"), T = dims == 4 ? fit(q.size(1), "T") : 1, Hq = fit(q.size(dims - 2), "Hq");
+  if (table.dim() != 2 || table.size(0) != B || ctx.dim() != 1 || ctx.size(0) != B) refuse("block_table must be [B, pages], ctx_len [B]");
+  if (!pt != !pl || !pt != !gb) refuse("prefix_table, prefix_len and group_begin go together");
+  int groups = 0, prefix_pages = 0;
+  if (pt) {
+    if (pt->dim() != 2 || pl->dim() != 1 || gb->dim() != 1 || pl->size(0) != pt->size(0) || gb->size(0) != pt->size(0) + 1)
+      refuse("prefix_table must be [groups, pages], prefix_len [groups], group_begin [groups + 1]");
+    groups = fit(pt->size(0), "groups");
+    prefix_pages = fit(pt->size(1), "prefix_pages");
+  }
+  const int64_t stride = row_stride(q, "q"), width = (int64_t)Hq * hd;
+  at::Tensor own_scratch, out;
+  size_t bytes;
+  void* work = nullptr;
+  if (scratch) {
+    if (!scratch->is_contiguous()) refuse("scratch must be contiguous");
+    work = scratch->data_ptr();
+    bytes = scratch->nbytes();
+  } else {
+    bytes = es_op_decode_attention_prefix_scratch_bytes(groups, B, T, Hq, Hkv, hd);
+    if (bytes) {
+      own_scratch = empty({(int64_t)bytes}, at::kByte, q);
+      work = own_scratch.data_ptr();
+    }
+  }
+  if (given) {
+    if (given->scalar_type() != q.scalar_type() || !given->is_contiguous() || given->dim() != dims - 1 || given->size(0) != B || (dims == 4 && given->size(1) != T) ||
+        given->size(dims - 2) != width)
+      refuse("out must be contiguous [B, T, Hq * hd] (or [B, Hq * hd]) of q's type");
+    out = *given;
+  } else {
+    out = dims == 4 ? empty({B, T, width}, q.scalar_type(), q) : empty({B, width}, q.scalar_type(), q);
+  }
+  const int pps = fit(table.size(1), "pages_per_seq");
+  auto i = [](const at::Tensor* t) { return t ? (const int32_t*)t->data_ptr() : nullptr; };
+  call([&] {
+    return es_op_decode_attention_prefix(q.data_ptr(), dtype, stride, kp.data_ptr(), vp.data_ptr(), i(pt), i(pl), i(gb), groups, prefix_pages, i(&table), i(&ctx),
+                                         out.data_ptr(), B, T, Hq, Hkv, hd, P, pps, n_pages, max_prefix, max_ctx, work, bytes, stream);
+  });
+  return THPVariable_Wrap(std::move(out));
+}
+
 // ---- module ------------------------------------------------------------------------------------
 
 void raise_refusal(int status, const std::string& message) {
@@ -536,6 +593,7 @@ PyMethodDef g_methods[] = {
     ENTRY("kv_plan", kv_plan, 9), ENTRY("kv8_append", kv8_append, 8), ENTRY("kv8_gather", kv8_gather, 7),
     ENTRY("decode_attention_kv8", decode_attention_kv8, 10), ENTRY("sample", sample, 7),
     ENTRY("quant_e4m3", quant_e4m3, 3), ENTRY("linear_fp8", linear_fp8, 9), ENTRY("qk_norm_rope", qk_norm_rope, 14),
+    ENTRY("decode_attention_prefix", decode_attention_prefix, 12),
     {"set_errors", set_errors, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

@@ -66,3 +66,46 @@ def heads(x, gain, eps, cosines, sines, positions, halves):
 def heads_bound(out, size, hd, dtype):
     """Squares: hd / 8 + 5 additions, a root (2 units), 3 products and the rotation's 3 roundings, all fp32; one rounding."""
     return size * (hd / 8 + 5 + 2 + 6) * 2.0 ** -24 + out.abs() * HALF_STEP[dtype] + SMALLEST[dtype]
+
+
+def shared(q, k_pages, v_pages, prefix_table, prefix_len, begin, table, ctx):
+    """(attention [B, T, Hq, hd], sum over the keys of weight times |v|): query t of a sequence sees its prefix and own keys
+    0 .. ctx - T + t; pages that do not exist hold nothing.  `begin` is taken as it is given (in order)."""
+    B, T, Hq, hd = q.shape
+    n_pages, Hkv, P, _ = k_pages.shape
+    out = torch.zeros(B, T, Hq, hd, dtype=torch.float64, device=q.device)
+    size = torch.zeros_like(out)
+
+    def keys(row, n):
+        """Pages and offsets of the first n keys of a table's row that lie in pages that exist."""
+        at = torch.arange(n, device=q.device)
+        page = row.long()[at // P]
+        ok = (page >= 0) & (page < n_pages)
+        return page[ok], at[ok] % P, at[ok]
+
+    for b in range(B):
+        group = next((g for g in range(len(prefix_len)) if int(begin[g]) <= b < int(begin[g + 1])), None) if prefix_len is not None else None
+        mine = keys(table[b], int(ctx[b]))
+        front = (torch.empty(0, dtype=torch.long, device=q.device),) * 2 if group is None else keys(prefix_table[group], int(prefix_len[group]))[:2]
+        for t in range(T):
+            see = mine[2] <= int(ctx[b]) - T + t
+            page, off = torch.cat([front[0], mine[0][see]]), torch.cat([front[1], mine[1][see]])
+            if len(page) == 0:
+                continue
+            k, v = k_pages[page, :, off].double(), v_pages[page, :, off].double()
+            w = torch.softmax(torch.einsum("hgd,nhd->hgn", q[b, t].double().view(Hkv, -1, hd), k) / math.sqrt(hd), -1)
+            out[b, t] = torch.einsum("hgn,nhd->hgd", w, v).reshape(Hq, hd)
+            size[b, t] = torch.einsum("hgn,nhd->hgd", w, v.abs()).reshape(Hq, hd)
+    return out, size
+
+
+def shared_bound(q, k_pages, out, size):
+    """A score is a sum of hd products of magnitude |q||k| in fp32, its exponent in units of log2(e) / sqrt(hd) rounded once and
+    taken by a function good to 2^-22; a weight is rounded to q's type in the product (half a step of it) and joins with at most
+    a few fp32 roundings per tile; one rounding of the result.  The weights' common factor cancels against their sum's, so an
+    error of a weight counts at most twice."""
+    dtype, hd = q.dtype, q.shape[-1]
+    largest = q.double().norm(dim=-1).max() * torch.nan_to_num(k_pages.double(), 0.0, 0.0, 0.0).norm(dim=-1).max() / math.sqrt(hd)
+    score = float(largest) * (hd * 2.0 ** -24 + 2.0 ** -23)
+    weight = 2 * (score + 2.0 ** -20) + 2 * HALF_STEP[dtype]
+    return size * weight + out.abs() * HALF_STEP[dtype] + SMALLEST[dtype]

@@ -62,11 +62,36 @@ def test_heads(B, kw, status):
     assert _heads(B, **kw) == status
 
 
+def _shared(b, **kw):
+    a = dict(q=A, dtype=0, stride=512, k=A, v=A, pt=A, pl=A, gb=A, groups=2, pp=4, table=A, ctx=A, out=A, B=3, T=1, Hq=4, Hkv=2, hd=128, P=16, pps=4, n_pages=8,
+             max_prefix=64, max_ctx=64, scratch=A, bytes=1 << 30)
+    a.update(kw)
+    return b.lib.es_op_decode_attention_prefix(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    ({"q": None}, 1), ({"k": None}, 1), ({"v": None}, 1), ({"pt": None}, 1), ({"pl": None}, 1), ({"gb": None}, 1), ({"table": None}, 1), ({"ctx": None}, 1), ({"out": None}, 1),
+    ({"dtype": 1}, 1), ({"groups": -1}, 1), ({"B": 0}, 1), ({"T": 0}, 1), ({"Hq": 3}, 2), ({"Hq": 258, "stride": 1 << 20}, 2), ({"hd": 96}, 2), ({"P": 8}, 2), ({"P": 48}, 2),
+    ({"pps": 0}, 1), ({"pp": 0}, 1), ({"n_pages": 0}, 1), ({"max_ctx": 0}, 1), ({"max_prefix": 0}, 1), ({"max_ctx": 65}, 3), ({"max_prefix": 65}, 3), ({"stride": 511}, 1),
+    ({"stride": 504}, 1), ({"q": A + 8}, 1), ({"k": A + 2}, 1), ({"out": A + 4}, 1), ({"scratch": A + 8}, 1), ({"B": 8191}, 3), ({"n_pages": 1 << 26}, 3),
+    ({"max_ctx": (1 << 30) + 1, "pps": 1 << 27}, 3), ({"B": 8000, "max_ctx": 1 << 23, "pps": 1 << 19}, 3), ({"T": 1 << 24}, 3), ({"bytes": 100}, 6), ({"scratch": None}, 6),
+])
+def test_shared(B, kw, status):
+    assert _shared(B, **kw) == status
+
+
+def test_shared_scratch(B):
+    f = B.es_op_decode_attention_prefix_scratch_bytes
+    assert f(1, 0, 1, 4, 2, 128) == 0 and f(1, 1, 1, 4, 3, 128) == 0 and f(1, 3, 1, 4, 2, 96) == 0
+    assert f(0, 3, 1, 4, 2, 128) < f(1, 3, 1, 4, 2, 128)
+
+
 def test_binding_refuses_host_tensors(B):
     h, i = torch.zeros(2, 2, 64, dtype=torch.float16), torch.zeros(2, dtype=torch.int32)
     f, t = torch.zeros(2, 128), torch.zeros(4, 32)
     c = torch.zeros(2, 128, dtype=torch.float8_e4m3fn)
-    for call in (lambda: B.es_op_quant_e4m3(f), lambda: B.es_op_linear_fp8(c, f, c, f), lambda: B.es_op_qk_norm_rope(h, h, None, None, 0.0, t, t, i)):
+    for call in (lambda: B.es_op_quant_e4m3(f), lambda: B.es_op_linear_fp8(c, f, c, f), lambda: B.es_op_qk_norm_rope(h, h, None, None, 0.0, t, t, i),
+                 lambda: B.es_op_decode_attention_prefix(h, h, h, None, None, None, i.view(2, 1), i, 1, 1)):
         with pytest.raises(B.EsError) as e:
             call()
         assert e.value.status == 1
