@@ -60,41 +60,45 @@ __device__ __forceinline__ void store_one(const Fp8Params& p, int64_t at, float 
 // ---- tiles of 128 weight rows x NT tokens ----------------------------------------------------------
 
 template <int NT> struct RowsCfg {
-  static constexpr int OCC = NT <= 64 ? 2 : 1;                       // CTAs per SM (registers: NT running sums a thread)
+  static constexpr int OCC = NT <= 64 ? 2 : 1;                       // CTAs per SM
+  static constexpr int SUMS = NT <= 32 ? 4 : 8;                      // warps of sums; a thread has one weight row
+  static constexpr int MINE = NT * 4 / SUMS;                         // and so many tokens
+  static constexpr int THREADS = 128 + 32 * SUMS;                    // TMA, MMA, factors, an idle warp
   static constexpr int X_TILE = NT * BKB;
   static constexpr int STAGE = W_TILE + X_TILE;
   static constexpr int STAGES = (OCC == 2 ? 108 * 1024 : 200 * 1024) / STAGE;
-  static constexpr int BUFS = NT <= 32 ? 4 : 2;                      // TMEM buffers
-  static constexpr int COLS = BUFS * NT;                             // 64 to 256, a power of two
-  static constexpr int BARS = 2 * STAGES + 2 * BUFS;
-  static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + 2 * NT * 4 + BARS * 8 + 16;
+  static constexpr int BUFS = 4;                                     // TMEM buffers
+  static constexpr int COLS = BUFS * NT;                             // 64 to 512, a power of two
+  static constexpr int FACTORS = 8;                                  // blocks whose factors are in shared memory
+  static constexpr int BARS = 2 * STAGES + 2 * BUFS + 2 * FACTORS;
+  static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + FACTORS * NT * 4 + BARS * 8 + 16;
   static_assert(STAGES * STAGE >= 128 * NT * 4, "the running sums of a CTA go where the ring was");
 };
 
-constexpr int ROWS_THREADS = 192;                // TMA, MMA, four warps of sums
-
 template <int NT>
-__global__ void __launch_bounds__(ROWS_THREADS, RowsCfg<NT>::OCC) linear_fp8_rows_kernel(const __grid_constant__ Fp8Maps maps, const Fp8Params p, const int split) {
+__global__ void __launch_bounds__(RowsCfg<NT>::THREADS, RowsCfg<NT>::OCC) linear_fp8_rows_kernel(const __grid_constant__ Fp8Maps maps, const Fp8Params p, const int split) {
   using L = RowsCfg<NT>;
   pdl_launch_dependents();
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   unsigned char* ring = smem;                                          // stage: weight tile, token tile
-  float* factor = (float*)(smem + L::STAGES * L::STAGE);               // [2][NT] sa * sw of a block
-  uint64_t* bars = (uint64_t*)(factor + 2 * NT);
-  uint64_t *full = bars, *empty = full + L::STAGES, *acc_full = empty + L::STAGES, *acc_empty = acc_full + L::BUFS;
+  float* factor = (float*)(smem + L::STAGES * L::STAGE);               // [FACTORS][NT] sa * sw of a block
+  uint64_t* bars = (uint64_t*)(factor + L::FACTORS * NT);
+  uint64_t *full = bars, *empty = full + L::STAGES, *acc_full = empty + L::STAGES, *acc_empty = acc_full + L::BUFS, *fac_full = acc_empty + L::BUFS,
+           *fac_empty = fac_full + L::FACTORS;
   uint32_t* tmem_slot = (uint32_t*)(bars + L::BARS);
   volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = (int)blockIdx.x % split, n0 = ((int)blockIdx.x / split) * 128, m0 = (int)blockIdx.y * NT;
-  const int b0 = (int)((long long)p.nkb * rank / split), b1 = (int)((long long)p.nkb * (rank + 1) / split);
+  const int b0 = (int)((long long)p.nkb * rank / split), blocks = (int)((long long)p.nkb * (rank + 1) / split) - b0;
 
   if (threadIdx.x == 0) {
     prefetch_tmap(&maps.a);
     prefetch_tmap(&maps.w);
     for (int s = 0; s < L::STAGES; ++s) { mbar_init(smem_u32(&full[s]), 1); mbar_init(smem_u32(&empty[s]), 1); }
-    for (int s = 0; s < L::BUFS; ++s) { mbar_init(smem_u32(&acc_full[s]), 1); mbar_init(smem_u32(&acc_empty[s]), 4); }
+    for (int s = 0; s < L::BUFS; ++s) { mbar_init(smem_u32(&acc_full[s]), 1); mbar_init(smem_u32(&acc_empty[s]), L::SUMS); }
+    for (int s = 0; s < L::FACTORS; ++s) { mbar_init(smem_u32(&fac_full[s]), 1); mbar_init(smem_u32(&fac_empty[s]), L::SUMS); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -104,12 +108,12 @@ __global__ void __launch_bounds__(ROWS_THREADS, RowsCfg<NT>::OCC) linear_fp8_row
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
 
-  float acc[NT];
-  bool ok = true;
+  const int col0 = warp >= 4 ? ((warp - 4) >> 2) * L::MINE : 0;         // first token of a thread of sums
+  float acc[L::MINE];
   if (warp == 0) {
     if (lane == 0) {
       // ---- TMA: weights of the first stages ahead of the wait for the kernel in front, if they are known to be complete ----
-      const int early = min(b1 - b0, L::STAGES);
+      const int early = min(blocks, L::STAGES);
       for (int i = 0; i < early; ++i) {
         mbar_expect_tx(smem_u32(&full[i]), L::STAGE);
         if (p.ready) tma_load_2d(smem_u32(ring + i * L::STAGE), &maps.w, (b0 + i) * (BKB / 2), n0, smem_u32(&full[i]));
@@ -119,7 +123,7 @@ __global__ void __launch_bounds__(ROWS_THREADS, RowsCfg<NT>::OCC) linear_fp8_row
         if (!p.ready) tma_load_2d(smem_u32(ring + i * L::STAGE), &maps.w, (b0 + i) * (BKB / 2), n0, smem_u32(&full[i]));
         tma_load_2d(smem_u32(ring + i * L::STAGE + W_TILE), &maps.a, (b0 + i) * (BKB / 2), m0, smem_u32(&full[i]));
       }
-      for (int i = early; i < b1 - b0; ++i) {
+      for (int i = early; i < blocks; ++i) {
         const int s = i % L::STAGES;
         if (!mbar_wait(smem_u32(&empty[s]), ((i / L::STAGES) & 1) ^ 1, abort_flag, nullptr, 0)) break;
         const uint32_t fb = smem_u32(&full[s]);
@@ -132,7 +136,7 @@ __global__ void __launch_bounds__(ROWS_THREADS, RowsCfg<NT>::OCC) linear_fp8_row
     if (lane == 0) {
       // ---- MMA ----
       constexpr uint32_t idesc = umma_idesc_f16(128, NT);
-      for (int i = 0; i < b1 - b0; ++i) {
+      for (int i = 0; i < blocks; ++i) {
         const int s = i % L::STAGES, buf = i % L::BUFS;
         if (!mbar_wait(smem_u32(&full[s]), (i / L::STAGES) & 1, abort_flag, nullptr, 0)) break;
         if (!mbar_wait(smem_u32(&acc_empty[buf]), ((i / L::BUFS) & 1) ^ 1, abort_flag, nullptr, 0)) break;
@@ -145,49 +149,87 @@ __global__ void __launch_bounds__(ROWS_THREADS, RowsCfg<NT>::OCC) linear_fp8_row
         umma_commit(smem_u32(&acc_full[buf]));
       }
     }
-  } else {
-    // ---- sums: a thread has one weight row and every token ----
-    const int e = threadIdx.x - 64, quarter = warp & 3;
-    const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
-    const float* ws = p.ws + (int64_t)(n0 / FP8_BLOCK) * p.nkb;
-    const bool mine = e < NT && m0 + e < p.M;                           // this thread brings token e's factors
+  } else if (warp == 2) {
+    // ---- factors: fetched four blocks at a time, the next four on their way while these are handed on (with the loads in the
+    // loop of the sums, every block waited for memory: 113 x 5120 x 13824 70 us) ----
+    constexpr int PER = (NT + 31) / 32, BATCH = 4;
+    const float* ws = p.ws + (int64_t)(n0 / FP8_BLOCK) * p.nkb + b0;
+    const float* as = p.as + (int64_t)b0 * p.M + m0;
     pdl_wait();
-    float next = 0.f;
-    if (mine) next = p.as[(int64_t)b0 * p.M + m0 + e] * ws[b0];
+    float sa[2][BATCH][PER], sw[2][BATCH];
+    auto fetch = [&](int i0, float (&a)[BATCH][PER], float (&w)[BATCH]) {
 #pragma unroll
-    for (int j = 0; j < NT; ++j) acc[j] = 0.f;
-    for (int i = 0; i < b1 - b0; ++i) {
-      const int buf = i % L::BUFS;
-      float* f = factor + (i & 1) * NT;
-      if (e < NT) f[e] = next;
-      if (mine && b0 + i + 1 < b1) next = p.as[(int64_t)(b0 + i + 1) * p.M + m0 + e] * ws[b0 + i + 1];
-      asm volatile("bar.sync 1, 128;" ::: "memory");
-      if (ok) ok = mbar_wait(smem_u32(&acc_full[buf]), (i / L::BUFS) & 1, abort_flag, nullptr, 0);
-      if (!__all_sync(0xffffffffu, ok)) { ok = false; continue; }
-      tc_fence_after();
-      constexpr int CH = NT < 32 ? 16 : 32;
+      for (int q = 0; q < BATCH; ++q) {
+        const int i = i0 + q;
+        w[q] = i < blocks ? ws[i] : 0.f;
 #pragma unroll
-      for (int c = 0; c < NT; c += CH) {
-        uint32_t v[CH];
-        tmem_ld_issue(tmem + lane_off + buf * NT + c, v);
-        tmem_ld_wait(v);
-#pragma unroll
-        for (int j = 0; j < CH; j += 4) {
-          const float4 q = *reinterpret_cast<const float4*>(f + c + j);
-          acc[c + j] = fmaf(__uint_as_float(v[j]), q.x, acc[c + j]);
-          acc[c + j + 1] = fmaf(__uint_as_float(v[j + 1]), q.y, acc[c + j + 1]);
-          acc[c + j + 2] = fmaf(__uint_as_float(v[j + 2]), q.z, acc[c + j + 2]);
-          acc[c + j + 3] = fmaf(__uint_as_float(v[j + 3]), q.w, acc[c + j + 3]);
+        for (int t = 0; t < PER; ++t) {
+          const int token = lane + 32 * t;
+          a[q][t] = (i < blocks && token < NT && m0 + token < p.M) ? as[(int64_t)i * p.M + token] : 0.f;
         }
       }
+    };
+    auto hand_on = [&](int i0, const float (&a)[BATCH][PER], const float (&w)[BATCH]) {
+#pragma unroll
+      for (int q = 0; q < BATCH; ++q) {
+        const int i = i0 + q, slot = i % L::FACTORS;
+        if (i >= blocks) break;
+        if (!mbar_wait(smem_u32(&fac_empty[slot]), ((i / L::FACTORS) & 1) ^ 1, abort_flag, nullptr, 0)) return;
+#pragma unroll
+        for (int t = 0; t < PER; ++t)
+          if (lane + 32 * t < NT) factor[slot * NT + lane + 32 * t] = a[q][t] * w[q];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&fac_full[slot]));
+      }
+    };
+    fetch(0, sa[0], sw[0]);
+    for (int i = 0; i < blocks; i += 2 * BATCH) {
+      fetch(i + BATCH, sa[1], sw[1]);
+      hand_on(i, sa[0], sw[0]);
+      fetch(i + 2 * BATCH, sa[0], sw[0]);
+      hand_on(i + BATCH, sa[1], sw[1]);
+    }
+  } else if (warp >= 4) {
+    // ---- sums ----
+    const uint32_t taddr = tmem + col0 + ((uint32_t)((warp & 3) * 32) << 16);
+    bool ok = true;
+#pragma unroll
+    for (int j = 0; j < L::MINE; ++j) acc[j] = 0.f;
+    for (int i = 0; i < blocks; ++i) {
+      const int buf = i % L::BUFS, slot = i % L::FACTORS;
+      ok = mbar_wait(smem_u32(&fac_full[slot]), (i / L::FACTORS) & 1, abort_flag, nullptr, 0) &&
+           mbar_wait(smem_u32(&acc_full[buf]), (i / L::BUFS) & 1, abort_flag, nullptr, 0);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+      constexpr int CH = L::MINE < 32 ? 16 : 32, N = L::MINE / CH;
+      uint32_t v[N][CH];
+#pragma unroll
+      for (int c = 0; c < N; ++c) tmem_ld_issue(taddr + buf * NT + c * CH, v[c]);
+#pragma unroll
+      for (int c = 0; c < N; ++c) tmem_ld_wait(v[c]);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&acc_empty[buf]));
+      const float* f = factor + slot * NT + col0;
+#pragma unroll
+      for (int c = 0; c < N; ++c)
+#pragma unroll
+        for (int j = 0; j < CH; j += 4) {
+          const float4 q = *reinterpret_cast<const float4*>(f + c * CH + j);
+          acc[c * CH + j] = fmaf(__uint_as_float(v[c][j]), q.x, acc[c * CH + j]);
+          acc[c * CH + j + 1] = fmaf(__uint_as_float(v[c][j + 1]), q.y, acc[c * CH + j + 1]);
+          acc[c * CH + j + 2] = fmaf(__uint_as_float(v[c][j + 2]), q.z, acc[c * CH + j + 2]);
+          acc[c * CH + j + 3] = fmaf(__uint_as_float(v[c][j + 3]), q.w, acc[c * CH + j + 3]);
+        }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&fac_empty[slot]));
     }
     if (!ok) {
 #pragma unroll
-      for (int j = 0; j < NT; ++j) acc[j] = __uint_as_float(0x7fffffffu);
+      for (int j = 0; j < L::MINE; ++j) acc[j] = __uint_as_float(0x7fffffffu);
     }
+    pdl_wait();                                                         // long over; this thread writes the result
   }
 
   // ---- teardown, and the sums of the cluster's CTAs ----
@@ -199,27 +241,25 @@ __global__ void __launch_bounds__(ROWS_THREADS, RowsCfg<NT>::OCC) linear_fp8_row
     tmem_dealloc(tmem, L::COLS);
   }
   const int tokens = min(NT, p.M - m0);
-  const int e = (int)threadIdx.x - 64;
-  const int n = n0 + (warp & 3) * 32 + lane;                            // of the four warps of sums
+  const int at = (warp & 3) * 32 + lane, n = n0 + at;                   // of the warps of sums: the weight row
   if (split == 1) {
-    if (warp >= 2 && n < p.N) {
+    if (warp >= 4 && n < p.N) {
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
-        if (j < tokens) store_one(p, (int64_t)(m0 + j) * p.N + n, acc[j]);
+      for (int j = 0; j < L::MINE; ++j)
+        if (col0 + j < tokens) store_one(p, (int64_t)(m0 + col0 + j) * p.N + n, acc[j]);
     }
     return;
   }
   float* sums = (float*)ring;                                           // [NT][128]
-  const int at = (warp & 3) * 32 + lane;
-  if (e >= 0) {
+  if (warp >= 4) {
 #pragma unroll
-    for (int j = 0; j < NT; ++j) sums[j * 128 + at] = acc[j];
+    for (int j = 0; j < L::MINE; ++j) sums[(col0 + j) * 128 + at] = acc[j];
   }
   cg::cluster_group cl = cg::this_cluster();
   cl.sync();
-  if (e >= 0 && n < p.N) {
+  if (warp >= 4 && n < p.N) {
     const int j1 = min(tokens, NT * (rank + 1) / split);
-    for (int j = NT * rank / split; j < j1; ++j) {
+    for (int j = NT * rank / split + (warp - 4) / 4; j < j1; j += L::SUMS / 4) {
       float v = 0.f;
       for (int r = 0; r < split; ++r) v += cl.map_shared_rank(sums, r)[j * 128 + at];
       store_one(p, (int64_t)(m0 + j) * p.N + n, v);
@@ -235,7 +275,7 @@ es_status_t launch_rows(const Fp8Maps& maps, const Fp8Params& p, int split, cuda
   auto kern = linear_fp8_rows_kernel<NT>;
   ES_CUDA_CHECK(allow_shared_memory(kern, (int)L::SMEM, &allowed));
   const dim3 grid((unsigned)((p.N + 127) / 128 * split), (unsigned)((p.M + NT - 1) / NT));
-  ES_CUDA_CHECK(launch_clusters(kern, split > 1 ? split : 0, grid, dim3(ROWS_THREADS), L::SMEM, s, tunables().pdl != 0, maps, p, split));
+  ES_CUDA_CHECK(launch_clusters(kern, split > 1 ? split : 0, grid, dim3(L::THREADS), L::SMEM, s, tunables().pdl != 0, maps, p, split));
   return ES_OK;
 }
 

@@ -4,8 +4,9 @@
 //   (y_i, y_j) -> (y_i cos - y_j sin, y_j cos + y_i sin)   for the pairs (2i, 2i + 1) or (i, i + rot / 2) of the first rot values
 //
 // A head's hd values are 8 to a thread: 8, 16 or 32 lanes share a head, the squares are added by shuffles in fp32, and a
-// partner of the second pairing lies in another lane of the group.  A warp keeps to one token, whose cosines and sines it
-// holds in registers while it walks over the token's heads.  All arithmetic is fp32, rounded once when it is stored.
+// partner of the second pairing lies in another lane of the group.  A warp keeps to one token and one kind of head, asks for
+// all it reads at once, and holds the products of gains, cosines and sines in registers while it walks over its heads: a
+// value then costs a square, two multiply-adds and a product.  All arithmetic is fp32, rounded once when it is stored.
 //
 // Bound: reading every element once and writing it once.
 #include <cuda_bf16.h>
@@ -25,10 +26,8 @@ struct HeadsParams {
   void *q_out, *k_out, *v_out;               // dense rows, or pages
   float eps;
   int n, Hq, Hkv, rot, max_pos;
-  int heads;                                 // Hq + Hkv (+ Hkv with v)
   int paged, P, n_pages;
   int gain;                                  // ES_DTYPE_* of the gains
-  int per_warp;                              // groups of heads a warp walks over
 };
 
 template <typename T> struct Pair;
@@ -56,7 +55,6 @@ __device__ __forceinline__ void load4(const float* p, float (&v)[8], int at) {
   v[at] = f.x; v[at + 1] = f.y; v[at + 2] = f.z; v[at + 3] = f.w;
 }
 __device__ __forceinline__ void load_gain(const void* g, int dtype, int at, float (&v)[8]) {
-  if (!g) return;
   if (dtype == ES_DTYPE_F16) load8((const __half*)g + at, v);
   else if (dtype == ES_DTYPE_BF16) load8((const __nv_bfloat16*)g + at, v);
   else { load4((const float*)g + at, v, 0); load4((const float*)g + at + 4, v, 4); }
@@ -64,130 +62,138 @@ __device__ __forceinline__ void load_gain(const void* g, int dtype, int at, floa
 
 constexpr int WARPS = 8;
 
-template <typename T, int HD, bool HALVES>
+// PER_WARP groups of heads for each warp, all of one kind (query, key or value).
+template <typename T, int HD, bool HALVES, int PER_WARP>
 __global__ void __launch_bounds__(WARPS * 32) qk_norm_rope_kernel(const HeadsParams p) {
-  constexpr int LANES = HD / 8, PER = 32 / LANES;          // lanes of a head, heads a warp holds at a time
+  constexpr int LANES = HD / 8, PER = 32 / LANES, CHUNK = PER * PER_WARP;      // lanes of a head, heads at a time, heads of a warp
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, part = lane % LANES, sub = lane / LANES;
-  const int chunk = PER * p.per_warp;                      // heads of a warp
-  const int tasks = (p.heads + chunk - 1) / chunk;         // warps of a token
-  const int64_t task = (int64_t)blockIdx.x * WARPS + (threadIdx.x >> 5);
-  const int64_t token = task / tasks;
-  const int h0 = (int)(task % tasks) * chunk;
+  const int q_tasks = (p.Hq + CHUNK - 1) / CHUNK, k_tasks = (p.Hkv + CHUNK - 1) / CHUNK;
+  const int tasks = q_tasks + k_tasks * (p.v ? 2 : 1);       // warps of a token
+  const int64_t warp = (int64_t)blockIdx.x * WARPS + (threadIdx.x >> 5);
+  const int64_t token = warp / tasks;
+  int task = (int)(warp - token * tasks);
+  const int kind = task < q_tasks ? 0 : task < q_tasks + k_tasks ? 1 : 2;
+  task -= kind == 0 ? 0 : kind == 1 ? q_tasks : q_tasks + k_tasks;
+  const int heads = kind == 0 ? p.Hq : p.Hkv, h0 = task * CHUNK + sub, d0 = part * 8;
   pdl_wait();
   if (token >= p.n) return;
 
-  const int pos = p.positions[token];
-  const bool there = (unsigned)pos < (unsigned)p.max_pos;  // else a padded row: its queries are zeros, nothing is cached
-  int64_t page = -1;
-  int off = 0;
-  if (p.paged && there) {
-    const int slot = p.slots[token];
-    if (slot >= 0 && slot / p.P < p.n_pages) { page = slot / p.P; off = slot % p.P; }
+  // everything that this warp reads is asked for at once
+  const T* row = (const T*)(kind == 0 ? p.q : kind == 1 ? p.k : p.v) + token * (kind == 0 ? p.q_stride : kind == 1 ? p.k_stride : p.v_stride) + d0;
+  uint4 raw[PER_WARP];
+#pragma unroll
+  for (int i = 0; i < PER_WARP; ++i) {
+    const int h = h0 + i * PER;
+    raw[i] = h < heads ? *reinterpret_cast<const uint4*>(row + (int64_t)h * HD) : make_uint4(0, 0, 0, 0);
   }
-  // factors of this lane's values
-  const int d0 = part * 8, half = p.rot >> 1;
-  const bool turned = d0 < p.rot;
-  float c[8], s[8];
-  if (turned && there) {
-    if (HALVES) {
-      const int64_t at = (int64_t)pos * half + (d0 < half ? d0 : d0 - half);
+  const int pos = p.positions[token];
+  const bool there = (unsigned)pos < (unsigned)p.max_pos;    // else a padded row: its queries are zeros, nothing is cached
+  // where the first of the heads goes, and how far apart they are there
+  T* out;
+  int64_t step;
+  if (kind == 0 || !p.paged) {
+    out = (T*)(kind == 0 ? p.q_out : kind == 1 ? p.k_out : p.v_out) + token * heads * HD;
+    step = HD;
+  } else {
+    const int slot = there ? p.slots[token] : -1, page = slot / p.P;
+    if (slot < 0 || page >= p.n_pages) return;               // the whole warp: one token
+    out = (T*)(kind == 1 ? p.k_out : p.v_out) + ((int64_t)page * p.Hkv * p.P + slot % p.P) * HD;
+    step = (int64_t)p.P * HD;
+  }
+  out += d0;
+  if (kind == 2 || !there) {
+#pragma unroll
+    for (int i = 0; i < PER_WARP; ++i) {
+      const int h = h0 + i * PER;
+      if (h < heads) *reinterpret_cast<uint4*>(out + h * step) = there ? raw[i] : make_uint4(0, 0, 0, 0);
+    }
+    return;
+  }
+
+  // factors of this lane's values: y' = r * (x * own + partner's x * other), gains and rotation in one
+  const void* gain = kind == 0 ? p.q_gain : p.k_gain;
+  const int half = p.rot >> 1;
+  const bool turned = d0 < p.rot, first = d0 < half;
+  float own[8], other[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) { own[j] = 1.f; other[j] = 0.f; }
+  if (gain) load_gain(gain, p.gain, d0, own);
+  int from = lane;                                           // HALVES: the partner's lane
+  if (HALVES) {
+    if (turned) {
+      const int shift = first ? half : -half;
+      from = lane + shift / 8;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) other[j] = 1.f;
+      if (gain) load_gain(gain, p.gain, d0 + shift, other);
+      const int64_t at = (int64_t)pos * half + (first ? d0 : d0 - half);
+      float c[8], s[8];
       load4(p.cosines + at, c, 0); load4(p.cosines + at + 4, c, 4);
       load4(p.sines + at, s, 0); load4(p.sines + at + 4, s, 4);
-    } else {
-      const int64_t at = (int64_t)pos * half + (d0 >> 1);
-      load4(p.cosines + at, c, 0);
-      load4(p.sines + at, s, 0);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) { own[j] *= c[j]; other[j] *= first ? -s[j] : s[j]; }
+    }
+  } else if (turned) {
+    const int64_t at = (int64_t)pos * half + (d0 >> 1);
+    float c[8], s[8];
+    load4(p.cosines + at, c, 0);
+    load4(p.sines + at, s, 0);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      other[2 * j] = -s[j] * own[2 * j + 1];
+      other[2 * j + 1] = s[j] * own[2 * j];
+      own[2 * j] *= c[j];
+      own[2 * j + 1] *= c[j];
     }
   }
-  float qg[8], kg[8];
-  load_gain(p.q_gain, p.gain, d0, qg);
-  load_gain(p.k_gain, p.gain, d0, kg);
 
-#pragma unroll 2
-  for (int i = 0; i < p.per_warp; ++i) {
-    const int h = h0 + i * PER + sub;
-    const bool real = h < p.heads;
-    const int kind = h < p.Hq ? 0 : h < p.Hq + p.Hkv ? 1 : 2;           // query, key, value
-    const int hh = kind == 0 ? h : kind == 1 ? h - p.Hq : h - p.Hq - p.Hkv;
-    float y[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = 0.f;
-    uint4 raw = make_uint4(0, 0, 0, 0);
-    if (real && there) {
-      const T* row = kind == 0 ? (const T*)p.q + token * p.q_stride : kind == 1 ? (const T*)p.k + token * p.k_stride : (const T*)p.v + token * p.v_stride;
-      raw = *reinterpret_cast<const uint4*>(row + (int64_t)hh * HD + d0);
+  for (int i = 0; i < PER_WARP; ++i) {
+    const int h = h0 + i * PER;
+    const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+    uint32_t z[4];
+    float r = 1.f;
+    float2 y[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = Pair<T>::get(w[j]);
+    if (gain) {
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum = fmaf(y[j].x, y[j].x, fmaf(y[j].y, y[j].y, sum));
+#pragma unroll
+      for (int o = LANES / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      r = rsqrtf(sum * (1.0f / HD) + p.eps);
     }
-    {
-      const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) { const float2 f = Pair<T>::get(w[j]); y[2 * j] = f.x; y[2 * j + 1] = f.y; }
+    for (int j = 0; j < 4; ++j) {
+      const float2 m = HALVES ? Pair<T>::get(__shfl_sync(0xffffffffu, w[j], from)) : make_float2(y[j].y, y[j].x);
+      // a value without a partner takes nothing of the one that stands there, whatever it is
+      const float a = y[j].x * own[2 * j], b = y[j].y * own[2 * j + 1];
+      z[j] = turned ? Pair<T>::put(r * fmaf(m.x, other[2 * j], a), r * fmaf(m.y, other[2 * j + 1], b)) : Pair<T>::put(r * a, r * b);
     }
-    const void* gain = kind == 0 ? p.q_gain : p.k_gain;
-    float sum = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sum = fmaf(y[j], y[j], sum);
-#pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (gain && kind < 2) {
-      const float r = rsqrtf(sum * (1.0f / HD) + p.eps);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = y[j] * r * (kind == 0 ? qg[j] : kg[j]);
-    }
-    float z[8];
-    if (HALVES) {
-      const bool first = d0 < half;
-      const int from = first ? lane + half / 8 : lane - half / 8;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float other = __shfl_sync(0xffffffffu, y[j], from);
-        z[j] = first ? y[j] * c[j] - other * s[j] : y[j] * c[j] + other * s[j];
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        z[2 * j] = y[2 * j] * c[j] - y[2 * j + 1] * s[j];
-        z[2 * j + 1] = y[2 * j + 1] * c[j] + y[2 * j] * s[j];
-      }
-    }
-    if (!real) continue;
-    uint4 u = raw;
-    if (kind < 2 && there) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) if (turned) y[j] = z[j];
-      u = make_uint4(Pair<T>::put(y[0], y[1]), Pair<T>::put(y[2], y[3]), Pair<T>::put(y[4], y[5]), Pair<T>::put(y[6], y[7]));
-    }
-    T* out;
-    if (kind == 0) {
-      out = (T*)p.q_out + (token * p.Hq + hh) * HD;
-    } else {
-      T* base = (T*)(kind == 1 ? p.k_out : p.v_out);
-      if (p.paged) {
-        if (page < 0) continue;
-        out = base + ((page * p.Hkv + hh) * p.P + off) * HD;
-      } else {
-        out = base + (token * p.Hkv + hh) * HD;
-      }
-    }
-    *reinterpret_cast<uint4*>(out + d0) = u;
+    if (h < heads) *reinterpret_cast<uint4*>(out + h * step) = make_uint4(z[0], z[1], z[2], z[3]);
   }
 }
 
-template <typename T, int HD>
-es_status_t launch(const HeadsParams& p0, bool halves, cudaStream_t s) {
-  HeadsParams p = p0;
-  constexpr int PER = 32 / (HD / 8);
-  // A warp walks over several groups of heads once there are enough warps without it (about 16 for each of an SM's
-  // schedulers), which spares it the token's factors.
-  const int groups = (p.heads + PER - 1) / PER;
-  int per = 1;
-  while (per < 4 && (long long)p.n * ((groups + 2 * per - 1) / (2 * per)) >= 64LL * sm_count()) per *= 2;
-  p.per_warp = per;
-  const long long warps = (long long)p.n * ((groups + per - 1) / per), ctas = (warps + WARPS - 1) / WARPS;
+template <typename T, int HD, bool HALVES, int PER_WARP>
+es_status_t launch_per(const HeadsParams& p, cudaStream_t s) {
+  constexpr int CHUNK = 32 / (HD / 8) * PER_WARP;
+  const long long tasks = (p.Hq + CHUNK - 1) / CHUNK + (p.Hkv + CHUNK - 1) / CHUNK * (p.v ? 2 : 1);
+  const long long ctas = (p.n * tasks + WARPS - 1) / WARPS;
   if (ctas > INT32_MAX) return fail(ES_ERR_RANGE, "n * heads exceeds one launch");
-  if (halves) ES_CUDA_CHECK(launch_kernel(qk_norm_rope_kernel<T, HD, true>, dim3((unsigned)ctas), dim3(WARPS * 32), 0, s, tunables().pdl != 0, p));
-  else ES_CUDA_CHECK(launch_kernel(qk_norm_rope_kernel<T, HD, false>, dim3((unsigned)ctas), dim3(WARPS * 32), 0, s, tunables().pdl != 0, p));
+  ES_CUDA_CHECK(launch_kernel(qk_norm_rope_kernel<T, HD, HALVES, PER_WARP>, dim3((unsigned)ctas), dim3(WARPS * 32), 0, s, tunables().pdl != 0, p));
   return ES_OK;
+}
+
+template <typename T, int HD>
+es_status_t launch(const HeadsParams& p, bool halves, cudaStream_t s) {
+  // A warp walks over four groups of heads once that leaves enough warps (about 16 for each of an SM's schedulers), which
+  // spares it the token's factors.
+  constexpr int CHUNK = 32 / (HD / 8) * 4;
+  const bool many = (long long)p.n * (p.Hq + p.Hkv) >= 64LL * sm_count() * CHUNK;
+  if (halves) return many ? launch_per<T, HD, true, 4>(p, s) : launch_per<T, HD, true, 1>(p, s);
+  return many ? launch_per<T, HD, false, 4>(p, s) : launch_per<T, HD, false, 1>(p, s);
 }
 
 template <typename T>
@@ -250,7 +256,6 @@ extern "C" es_status_t es_op_qk_norm_rope(const void* q, int64_t q_stride, const
   p.q_out = q_out; p.k_out = k_out; p.v_out = v_out;
   p.eps = eps;
   p.n = n; p.Hq = Hq; p.Hkv = Hkv; p.rot = rot; p.max_pos = max_pos;
-  p.heads = Hq + Hkv * (v ? 2 : 1);
   p.paged = slot_map != nullptr; p.P = page_tokens > 0 ? page_tokens : 1; p.n_pages = n_pages;
   cudaStream_t s = (cudaStream_t)stream;
   return dtype == ES_DTYPE_F16 ? launch_hd<__half>(p, hd, halves != 0, s) : launch_hd<__nv_bfloat16>(p, hd, halves != 0, s);
