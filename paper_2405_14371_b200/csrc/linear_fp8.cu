@@ -257,12 +257,26 @@ __global__ void __launch_bounds__(RowsCfg<NT>::THREADS, RowsCfg<NT>::OCC) linear
   }
   cg::cluster_group cl = cg::this_cluster();
   cl.sync();
-  if (warp >= 4 && n < p.N) {
-    const int j1 = min(tokens, NT * (rank + 1) / split);
-    for (int j = NT * rank / split + (warp - 4) / 4; j < j1; j += L::SUMS / 4) {
-      float v = 0.f;
-      for (int r = 0; r < split; ++r) v += cl.map_shared_rank(sums, r)[j * 128 + at];
-      store_one(p, (int64_t)(m0 + j) * p.N + n, v);
+  // this CTA's share of the tokens, eight at a time: their sums of all ranks are under way together (one by one, the reads of
+  // 113 tokens took 15 us)
+  constexpr int TEAMS = L::SUMS / 4, MANY = 8;
+  const int j1 = min(tokens, NT * (rank + 1) / split);
+  if (warp >= 4) {
+    for (int j0 = NT * rank / split + (warp - 4) / 4; j0 < j1; j0 += TEAMS * MANY) {
+      float v[MANY];
+#pragma unroll
+      for (int q = 0; q < MANY; ++q) v[q] = 0.f;
+#pragma unroll 4
+      for (int r = 0; r < split; ++r) {
+        const float* from = cl.map_shared_rank(sums, r) + at;
+#pragma unroll
+        for (int q = 0; q < MANY; ++q) v[q] += from[min(j0 + q * TEAMS, NT - 1) * 128];
+      }
+      if (n < p.N) {
+#pragma unroll
+        for (int q = 0; q < MANY; ++q)
+          if (j0 + q * TEAMS < j1) store_one(p, (int64_t)(m0 + j0 + q * TEAMS) * p.N + n, v[q]);
+      }
     }
   }
   cl.sync();                                                            // nobody leaves while its sums are being read
@@ -271,9 +285,7 @@ __global__ void __launch_bounds__(RowsCfg<NT>::THREADS, RowsCfg<NT>::OCC) linear
 template <int NT>
 es_status_t launch_rows(const Fp8Maps& maps, const Fp8Params& p, int split, cudaStream_t s) {
   using L = RowsCfg<NT>;
-  static std::atomic<uint64_t> allowed{0};
   auto kern = linear_fp8_rows_kernel<NT>;
-  ES_CUDA_CHECK(allow_shared_memory(kern, (int)L::SMEM, &allowed));
   const dim3 grid((unsigned)((p.N + 127) / 128 * split), (unsigned)((p.M + NT - 1) / NT));
   ES_CUDA_CHECK(launch_clusters(kern, split > 1 ? split : 0, grid, dim3(L::THREADS), L::SMEM, s, tunables().pdl != 0, maps, p, split));
   return ES_OK;
@@ -516,22 +528,49 @@ es_status_t launch_pair(const Fp8Maps& maps, const Fp8Params& p, cudaStream_t s)
   return ES_OK;
 }
 
-// CTAs that share a tile's K range: as many as make the busiest SM's time shortest, counted in blocks; starting and joining
-// cost about 4 of them.
-int split_of(long long tiles, int nkb, int slots) {
-  int best = 1;
-  long long least = 0;
-  for (int s = 1; s <= 8 && s <= nkb; ++s) {
-    const long long cost = ((tiles * s + slots - 1) / slots) * ((nkb + s - 1) / s + 4);
-    if (s == 1 || cost < least) { best = s; least = cost; }
-  }
-  return best;
+// Clusters of 1 to 8 CTAs that the device holds at a time (fewer than its SMs' places divided by the size: a cluster lies in one
+// part of the device, and the parts differ).
+template <int NT>
+es_status_t places_of(int split, int* places) {
+  using L = RowsCfg<NT>;
+  static std::atomic<int> known[64][9];
+  int dev = 0;
+  ES_CUDA_CHECK(cudaGetDevice(&dev));
+  std::atomic<int>* at = dev < 64 ? &known[dev][split] : nullptr;
+  if (at && (*places = at->load(std::memory_order_relaxed)) > 0) return ES_OK;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(split);
+  cfg.blockDim = dim3(L::THREADS);
+  cfg.dynamicSmemBytes = L::SMEM;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = split;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int n = 0;
+  ES_CUDA_CHECK(cudaOccupancyMaxActiveClusters(&n, linear_fp8_rows_kernel<NT>, &cfg));
+  *places = n > 0 ? n : 1;
+  if (at) at->store(*places, std::memory_order_relaxed);
+  return ES_OK;
 }
 
+// CTAs that share a tile's K range: as many as make the time of the waves shortest, counted in blocks; starting and joining
+// cost about 4 of them.
 template <int NT>
 es_status_t rows_auto(const Fp8Maps& maps, const Fp8Params& p, cudaStream_t s) {
+  static std::atomic<uint64_t> allowed{0};
+  ES_CUDA_CHECK(allow_shared_memory(linear_fp8_rows_kernel<NT>, (int)RowsCfg<NT>::SMEM, &allowed));
   const long long tiles = (long long)((p.N + 127) / 128) * ((p.M + NT - 1) / NT);
-  return launch_rows<NT>(maps, p, split_of(tiles, p.nkb, RowsCfg<NT>::OCC * sm_count()), s);
+  int best = 1;
+  long long least = 0;
+  for (int split = 1; split <= 8 && split <= p.nkb; ++split) {
+    int places = 0;
+    ES_TRY(places_of<NT>(split, &places));
+    const long long cost = ((tiles + places - 1) / places) * ((p.nkb + split - 1) / split + 4);
+    if (split == 1 || cost < least) { best = split; least = cost; }
+  }
+  return launch_rows<NT>(maps, p, best, s);
 }
 
 }  // namespace

@@ -71,12 +71,12 @@ __device__ __forceinline__ void store8(uint8_t* p, const float (&v)[8], float s)
 // together), the 8 warps of a CTA 8 consecutive blocks.
 template <typename T>
 __global__ void __launch_bounds__(256) quant_rows_kernel(const QuantParams p) {
-  pdl_wait();
-  pdl_launch_dependents();          // behind the wait: whoever starts now knows that everything in front of this kernel is done
+  pdl_launch_dependents();
   const int lane = threadIdx.x & 31, part = lane & 7;
   const int b = blockIdx.x * 8 + (threadIdx.x >> 5);
   const int64_t row = (int64_t)blockIdx.y * 4 + (lane >> 3);
   const bool here = b < p.kb && row < p.M;
+  pdl_wait();
   const T* x = (const T*)p.x + row * p.stride;
   float v[2][8];
   uint32_t m = 0;
