@@ -6,17 +6,19 @@
 // A segment is a prefix or the own keys of one sequence.  Its rows are the query heads of a KV head's group, of all tokens
 // that see it: a whole group of sequences makes one product with many rows where one sequence makes G.  An item is a segment,
 // a KV head and a row tile (as many whole tokens as 128 rows hold); its keys come in tiles of 64.  The tiles of all items form
-// one line, cut into equal stretches, one for each resident CTA (two per SM), whatever the lengths: the host knows none.
-// Every piece of an item that lies in a stretch leaves (o, m, l) in fp32 in the scratch, and a second kernel joins, for each row,
-// the pieces of its prefix and of its own keys in order of the line, so results do not depend on scheduling.
+// one line, each item with OV places more for what starting and ending it costs, cut into equal stretches, one for each
+// resident CTA (two per SM), whatever the lengths: the host knows none.  Every piece of an item that lies in a stretch leaves
+// (o, m, l) in fp32 in the scratch, and a second kernel joins, for each row, the pieces of its prefix and of its own keys in
+// order of the line, so results do not depend on scheduling.
 //
-// Within a stretch, per tile (the roles of the prefill kernel):
+// Within a stretch, per tile:
 //   S = Q K^T      M = 128 rows, N = 64 keys, fp32 in TMEM, two buffers: the product of the next tile runs beside this softmax
-//   softmax        four warps, a row a thread: running maximum and sum in fp32; P in q's type takes K's place in the ring.  The
-//                  sum is of the rounded P, so rounding them moves no weight to or from other keys on average.  Warps
-//                  without rows (a single sequence has G) only keep the protocol.
-//   O += P V       fp32 in TMEM, rescaled when a row's maximum has grown by more than 8 (log2), as P stays below 256
-// The ring runs on over the items' borders, and the next item's Q is fetched while the last tile of the one before is finished.
+//   softmax        four warps, a row a thread: running maximum and sum in fp32; P in q's type goes into TMEM in place of S.
+//                  The sum is of the rounded P, so a row's weights still add up to one.  Warps without rows (a single
+//                  sequence has G) only keep the protocol.
+//   O += P V       P from TMEM; fp32 in TMEM, rescaled when a row's maximum has grown by more than 8 (log2), as P stays below 256
+// K's place in the ring is free once S is complete, V's after P V; each has a warp that asks for the next.  The ring runs on
+// over the items' borders, and the next item's Q is fetched while the last tile of the one before is finished.
 //
 // Nothing of a key that a row does not see reaches it: scores are masked by selection, V rows behind the length are zeroed
 // in shared memory, pages that do not exist are read as zeros (a TMA box outside the tensor).  Of a draft's last tokens, which
@@ -35,10 +37,11 @@ namespace es {
 namespace {
 
 constexpr int KT = 64;                   // keys of a tile
-constexpr int THREADS = 192;             // TMA, MMA, four softmax warps
+constexpr int THREADS = 256;             // K and Q, MMA, V, records, four softmax warps
 constexpr int TMEM_COLS = 256;           // S: two buffers of 64 columns, O: up to 128
 constexpr float GAP = 8.0f;
-constexpr int MIN_UNITS = 2;             // tiles of a stretch, at least
+constexpr int OV = 2;                    // places on the line that an item takes besides its tiles
+constexpr int MIN_UNITS = 2 + OV;        // places of a stretch, at least
 constexpr int MAX_SEGMENTS = 8192;
 
 struct alignas(64) PrefixMaps { CUtensorMap q, k, v; };
@@ -47,7 +50,7 @@ struct PrefixParams {
   const int *prefix_table, *prefix_len, *begin, *table, *ctx;
   const void* v_pages;
   void* out;
-  int *line, *group_of, *first;          // scratch: cumulative tiles [segments + 1], prefix of every sequence [B], first sequences [groups + 1]
+  int4* records;                         // scratch: two for every sequence, where its row's pieces are
   float *ml_p, *o_p, *ml_o, *o_o;        // pieces of prefixes and of own keys: [rows][2], [rows][hd]
   int B, T, Hq, Hkv, G, P, log2P, groups, prefix_pages, pps, n_pages, max_prefix, max_ctx;
   int TT;                                // tokens of a row tile
@@ -65,35 +68,48 @@ struct Piece {
 
 __device__ __forceinline__ int tiles_of(int len) { return (len + KT - 1) / KT; }
 
-// CTAs that share the line of `units` tiles, and which has which
+// CTAs that share the line of `units` places, and which has which
 __device__ __forceinline__ int active(int units, int ctas) { return max(1, min(ctas, units / MIN_UNITS)); }
 __device__ __forceinline__ int start_of(int cta, int units, int n) { return (int)((long long)units * cta / n); }
 __device__ __forceinline__ int cta_of(int unit, int units, int n) { return (int)(((long long)(unit + 1) * n - 1) / units); }
 
-__device__ __forceinline__ Piece piece_at(const PrefixParams& p, const int* line, const int* lens, const int* first, int u, int end) {
+// The pieces of a stretch, one after the other.
+struct Walk {
+  const PrefixParams& p;
+  const int *line, *lens, *first;
+  int u, end;
   Piece x;
-  int lo = 0, hi = p.groups + p.B;                      // line[lo] <= u < line[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (line[mid] <= u) lo = mid; else hi = mid;
+  __device__ __forceinline__ Walk(const PrefixParams& p_, const int* line_, const int* lens_, const int* first_, int u_, int end_)
+      : p(p_), line(line_), lens(lens_), first(first_), u(u_), end(end_) {}
+  __device__ __forceinline__ bool next() {
+    while (u < end) {
+      int lo = 0, hi = p.groups + p.B;                    // line[lo] <= u < line[hi]
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (line[mid] <= u) lo = mid; else hi = mid;
+      }
+      x.seg = lo;
+      x.group = lo < p.groups;
+      x.len = lens[lo];
+      if (x.group) {
+        x.tok0 = first[lo] * p.T;
+        x.ntok = (first[lo + 1] - first[lo]) * p.T;
+      } else {
+        x.tok0 = (lo - p.groups) * p.T;
+        x.ntok = p.T;
+      }
+      const int row_tiles = (x.ntok + p.TT - 1) / p.TT, k = tiles_of(x.len) + OV, r = u - line[lo], item = r / k, a = r - item * k;
+      const int take = min(k - a, end - u);
+      x.j0 = max(0, a - OV);
+      x.j1 = max(0, a + take - OV);
+      x.kvh = item / row_tiles;
+      x.rt = item - x.kvh * row_tiles;
+      u += take;
+      if (x.j1 > x.j0) return true;
+    }
+    return false;
   }
-  x.seg = lo;
-  x.group = lo < p.groups;
-  x.len = lens[lo];
-  if (x.group) {
-    x.tok0 = first[lo] * p.T;
-    x.ntok = (first[lo + 1] - first[lo]) * p.T;
-  } else {
-    x.tok0 = (lo - p.groups) * p.T;
-    x.ntok = p.T;
-  }
-  const int row_tiles = (x.ntok + p.TT - 1) / p.TT, k = tiles_of(x.len), r = u - line[lo], item = r / k;
-  x.j0 = r - item * k;
-  x.j1 = min(k, x.j0 + (end - u));
-  x.kvh = item / row_tiles;
-  x.rt = item - x.kvh * row_tiles;
-  return x;
-}
+};
 
 // First row of a piece's partials, in the prefixes' or the own keys' part of the scratch: the rows of the items before it, and
 // a tile's worth for each CTA before this one.
@@ -115,29 +131,43 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
       : "memory");
 }
 
-// Two probabilities rounded to q's type, and what they became.
+// Two probabilities rounded to q's type.
 template <bool BF16>
-__device__ __forceinline__ uint32_t round_pair(float a, float b, float& sum) {
+__device__ __forceinline__ uint32_t round_pair(float a, float b) {
   if (BF16) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(&h);
-    sum += __uint_as_float(w << 16) + __uint_as_float(w & 0xffff0000u);
-    return w;
+    return *reinterpret_cast<const uint32_t*>(&h);
   }
   const __half2 h = __floats2half2_rn(a, b);
-  const float2 f = __half22float2(h);
-  sum += f.x + f.y;
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
 template <int HD>
 struct Smem {
   static constexpr int HALVES = HD / 64;
-  static constexpr int Q_BYTES = 128 * HD * 2, KV_BYTES = KT * HD * 2, P_BYTES = 128 * KT * 2;
-  static constexpr bool P_IN_K = KV_BYTES >= P_BYTES;
-  static constexpr int BARS = 12;
-  static constexpr size_t FIXED = 1024 + Q_BYTES + 4 * KV_BYTES + (P_IN_K ? 0 : 2 * P_BYTES) + BARS * 8 + 64;
+  static constexpr int Q_BYTES = 128 * HD * 2, KV_BYTES = KT * HD * 2;
+  static constexpr int BARS = 16;
+  static constexpr size_t FIXED = 1024 + Q_BYTES + 4 * KV_BYTES + BARS * 8 + 128;
 };
+
+// Inclusive scan over the block of one value a thread, by `join`; the total goes to everyone.
+template <class Join>
+__device__ __forceinline__ int block_scan(int v, int* totals, int* all, Join join) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, v, o); if (lane >= o) v = join(v, x); }
+  __syncthreads();                                             // `totals` may still be read
+  if (lane == 31) totals[warp] = v;
+  __syncthreads();
+  int sum = totals[0], before = 0;
+#pragma unroll
+  for (int w = 1; w < THREADS / 32; ++w) {
+    if (w == warp) before = sum;
+    sum = join(sum, totals[w]);
+  }
+  *all = sum;
+  return warp ? join(before, v) : v;
+}
 
 template <int HD, bool BF16>
 __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_constant__ PrefixMaps maps, const PrefixParams p) {
@@ -148,24 +178,24 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
   unsigned char* q_s = smem;                                   // [halves][128 rows][128 B]
   unsigned char* k_s = q_s + L::Q_BYTES;                       // [2 stages][halves][64 rows][128 B]
   unsigned char* v_s = k_s + 2 * L::KV_BYTES;
-  unsigned char* p_own = v_s + 2 * L::KV_BYTES;
-  uint64_t* bars = (uint64_t*)(p_own + (L::P_IN_K ? 0 : 2 * L::P_BYTES));
-  uint64_t *q_full = bars, *q_empty = bars + 1, *kv_full = bars + 2, *kv_empty = bars + 4, *s_full = bars + 6, *p_full = bars + 8, *pv_done = bars + 10;
+  uint64_t* bars = (uint64_t*)(v_s + 2 * L::KV_BYTES);
+  uint64_t *q_full = bars, *q_empty = bars + 1, *k_full = bars + 2, *k_empty = bars + 4, *v_full = bars + 6, *v_empty = bars + 8, *s_full = bars + 10,
+           *p_full = bars + 12, *pv_done = bars + 14;           // [2] each but Q's, by the tile's parity
   uint32_t* tmem_slot = (uint32_t*)(bars + L::BARS);
   volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
-  volatile int* pages_seen = (volatile int*)(tmem_slot + 2);   // [2] of a stage's tile: which 16 tokens lie in pages that exist
-  volatile int* tail_bad = (volatile int*)(tmem_slot + 4);     // piece whose last tokens hold a V that is no number
-  int* line = (int*)(tmem_slot + 8);                           // [segments + 1]
-  int* lens = line + p.groups + p.B + 1;                       // [segments]
-  int* first = lens + p.groups + p.B;                          // [groups + 1]
-  auto p_tile = [&](int s) -> unsigned char* { return L::P_IN_K ? k_s + s * L::KV_BYTES : p_own + s * L::P_BYTES; };
+  volatile int* pages_seen = (volatile int*)(tmem_slot + 2);   // [4] of the latest tiles: which 16 tokens lie in pages that exist
+  volatile int* tail_bad = (volatile int*)(tmem_slot + 6);     // piece whose last tokens hold a V that is no number
+  int* totals = (int*)(tmem_slot + 8);                         // [8]
+  int* line = (int*)(tmem_slot + 16);                          // [segments + 1] places before
+  int* lens = line + p.groups + p.B + 1;                       // [segments] keys
+  int* first = lens + p.groups + p.B;                          // [groups + 1] first sequences
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     prefetch_tmap(&maps.q);
     prefetch_tmap(&maps.k);
     prefetch_tmap(&maps.v);
-    for (int i = 0; i < L::BARS; ++i) mbar_init(smem_u32(&bars[i]), (i == 8 || i == 9) ? 4 : 1);   // p_full: four warps
+    for (int i = 0; i < L::BARS; ++i) mbar_init(smem_u32(&bars[i]), (i == 12 || i == 13) ? 4 : 1);   // p_full: four warps
     *abort_flag = 0;
     *tail_bad = -1;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -173,40 +203,34 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
   if (warp == 1) tmem_alloc(smem_u32(tmem_slot), TMEM_COLS);
   pdl_wait();
 
-  // ---- the line: cumulative tiles of the segments ----
-  const int segments = p.groups + p.B;
-  if (warp == 0) {
-    int units = 0, seen = 0;                                   // so far: tiles, sequences of earlier groups
-    for (int base = 0; base < segments; base += 32) {
-      const int s = base + lane;
-      const bool group = s < p.groups;
-      int len = 0, from = 0, to = 0;
-      if (s < segments) {
-        len = group ? min(max(p.prefix_len[s], 0), p.max_prefix) : min(max(p.ctx[s - p.groups], 0), p.max_ctx);
-        if (group) { from = min(max(p.begin[s], 0), p.B); to = min(max(p.begin[s + 1], 0), p.B); }
-      }
-      // groups in order: each begins where the ones before have ended, at least
-      int reach = max(from, to);
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, reach, o); if (lane >= o) reach = max(reach, x); }
-      reach = max(reach, seen);
-      int before = __shfl_up_sync(0xffffffffu, reach, 1);
-      if (lane == 0) before = seen;
-      before = max(before, from);                              // this group: [before, reach)
-      if (group) {
-        first[s] = before;
-        if (s == p.groups - 1) first[p.groups] = reach;
-      }
-      const int tokens = group ? (reach - before) * p.T : p.T;
-      int mine = s < segments ? p.Hkv * ((tokens + p.TT - 1) / p.TT) * tiles_of(len) : 0;
-      const int own = mine;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, mine, o); if (lane >= o) mine += x; }
-      if (s < segments) { lens[s] = len; line[s] = units + mine - own; }
-      units += __shfl_sync(0xffffffffu, mine, 31);
-      seen = __shfl_sync(0xffffffffu, reach, 31);
-    }
-    if (lane == 0) line[segments] = units;
+  // ---- the line ----
+  const int segments = p.groups + p.B, per = (segments + THREADS) / THREADS, s0 = (int)threadIdx.x * per;      // `per` segments a thread
+  for (int s = threadIdx.x; s < segments; s += THREADS)
+    lens[s] = s < p.groups ? min(max(p.prefix_len[s], 0), p.max_prefix) : min(max(p.ctx[s - p.groups], 0), p.max_ctx);
+  if (p.groups)
+    for (int g = threadIdx.x; g <= p.groups; g += THREADS) first[g] = min(max(p.begin[g], 0), p.B);
+  __syncthreads();
+  {
+    // a group begins no earlier than those before it end
+    int top = 0, all;
+    for (int s = s0; s < min(s0 + per, p.groups + 1); ++s) if (p.groups) top = max(top, first[s]);
+    auto larger = [](int a, int b) { return max(a, b); };
+    const int mine = top;
+    top = block_scan(mine, totals, &all, larger);
+    int before = __shfl_up_sync(0xffffffffu, top, 1);
+    if (lane == 0) { before = 0; for (int w = 0; w < warp; ++w) before = max(before, totals[w]); }
+    for (int s = s0; s < min(s0 + per, p.groups + 1); ++s)
+      if (p.groups) { before = max(before, first[s]); first[s] = before; }
+    __syncthreads();
+    int sum = 0;
+    auto places = [&](int s) {
+      const int tokens = s < p.groups ? (first[s + 1] - first[s]) * p.T : p.T;
+      return lens[s] > 0 ? p.Hkv * ((tokens + p.TT - 1) / p.TT) * (tiles_of(lens[s]) + OV) : 0;
+    };
+    for (int s = s0; s < min(s0 + per, segments); ++s) sum += places(s);
+    int at = block_scan(sum, totals, &all, [](int a, int b) { return a + b; }) - sum;
+    for (int s = s0; s < min(s0 + per, segments); ++s) { line[s] = at; at += places(s); }
+    if (threadIdx.x == 0) line[segments] = all;
   }
   tc_fence_before();
   __syncthreads();
@@ -214,15 +238,20 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
   const uint32_t tmem_base = *tmem_slot, tmem_s = tmem_base, tmem_o = tmem_base + 128;
   const int units = line[segments], ctas = active(units, (int)gridDim.x), cta = (int)blockIdx.x;
   const int u0 = cta < ctas ? start_of(cta, units, ctas) : 0, u1 = cta < ctas ? start_of(cta + 1, units, ctas) : 0;
+  Walk walk(p, line, lens, first, u0, u1);
+  const Piece& x = walk.x;
 
-  if (warp == 0) {
-    // ---- TMA: a lane per page of a tile ----
+  if (warp == 0 || warp == 2) {
+    // ---- TMA: K (and Q) or V; a lane per page of a tile ----
+    const bool key = warp == 0;
     const int chunks = KT / p.box;                             // copies along the tile's keys
     const int lines = p.n_pages * p.Hkv * p.P;                 // outside the tensor: zeros
-    int it = 0, pieces = 0;
+    uint64_t *full = key ? k_full : v_full, *empty = key ? k_empty : v_empty;
+    unsigned char* ring = key ? k_s : v_s;
+    const CUtensorMap* map = key ? &maps.k : &maps.v;
+    int it = 0;
     bool ok = true;
-    for (int u = u0; u < u1 && ok; ++pieces) {
-      const Piece x = piece_at(p, line, lens, first, u, u1);
+    for (int pieces = 0; ok && walk.next(); ++pieces) {
       const int* pages = x.group ? p.prefix_table + (int64_t)x.seg * p.prefix_pages : p.table + (int64_t)(x.seg - p.groups) * p.pps;
       for (int j = x.j0; j < x.j1; ++j, ++it) {
         const int s = it & 1;
@@ -238,23 +267,20 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
           }
         }
         here = __reduce_or_sync(0xffffffffu, here);
-        ok = mbar_wait(smem_u32(&kv_empty[s]), ((it >> 1) & 1) ^ 1, abort_flag, nullptr, 0);
+        ok = mbar_wait(smem_u32(&empty[s]), ((it >> 1) & 1) ^ 1, abort_flag, nullptr, 0);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
-        const uint32_t fb = smem_u32(&kv_full[s]);
+        const uint32_t fb = smem_u32(&full[s]);
         if (lane == 0) {
-          pages_seen[s] = here;
-          mbar_expect_tx(fb, 2 * L::KV_BYTES);
+          if (key) pages_seen[it & 3] = here;                  // read by the softmax of this tile, which is over when K of it + 4 is asked for
+          mbar_expect_tx(fb, L::KV_BYTES);
         }
         __syncwarp();
         if (lane < chunks) {
 #pragma unroll
-          for (int h = 0; h < L::HALVES; ++h) {
-            tma_load_2d(smem_u32(k_s + s * L::KV_BYTES + h * (KT * 128) + lane * p.box * 128), &maps.k, h * 64, row, fb);
-            tma_load_2d(smem_u32(v_s + s * L::KV_BYTES + h * (KT * 128) + lane * p.box * 128), &maps.v, h * 64, row, fb);
-          }
+          for (int h = 0; h < L::HALVES; ++h) tma_load_2d(smem_u32(ring + s * L::KV_BYTES + h * (KT * 128) + lane * p.box * 128), map, h * 64, row, fb);
         }
-        if (j == x.j0) {                                       // the first tile is under way before Q's place is free
+        if (key && j == x.j0) {                                // the first tile is under way before Q's place is free
           ok = mbar_wait(smem_u32(q_empty), (pieces & 1) ^ 1, abort_flag, nullptr, 0);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
@@ -266,95 +292,92 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
           }
         }
       }
-      u += x.j1 - x.j0;
-    }
-    // what the second kernel needs to find the pieces
-    if (cta == 0) {
-      for (int s = lane; s <= segments; s += 32) p.line[s] = line[s];
-      for (int s = lane; s <= p.groups; s += 32) p.first[s] = p.groups ? first[s] : 0;
-      for (int b = lane; b < p.B; b += 32) {
-        int lo = -1, hi = p.groups;                            // first[lo] <= b < first[hi]
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (first[mid] <= b) lo = mid; else hi = mid;
-        }
-        p.group_of[b] = lo >= 0 && b < first[lo + 1] ? lo : -1;
-      }
     }
   } else if (warp == 1) {
-    if (lane == 0 && u0 < u1) {
+    if (lane == 0) {
       // ---- MMA: whichever of the next S product and the next P V is ready ----
       constexpr uint32_t type = BF16 ? (1u << 7) | (1u << 10) : 0u;
       constexpr uint32_t idesc_s = umma_idesc_f16(128, KT) | type;
       constexpr uint32_t idesc_o = umma_idesc_f16(128, HD) | type | (1u << 16);        // V is MN-major
-      const int n = u1 - u0;
-      Piece xs = piece_at(p, line, lens, first, u0, u1), xo = xs;
-      int s_next = 0, s_end = xs.j1 - xs.j0, s_piece = 0, o_end = s_end;
+      Walk ahead(p, line, lens, first, u0, u1);
+      bool more_s = ahead.next(), more_o = walk.next();
+      int s_it = 0, s_left = ahead.x.j1 - ahead.x.j0, s_piece = 0, o_it = 0, o_left = x.j1 - x.j0;
       bool s_first = true, o_first = true;
-      uint64_t t_start = global_timer_ns();
-      for (int j = 0; j < n;) {
+      uint64_t idle_since = 0;
+      while (more_o) {
         bool progressed = false;
-        if (s_next < n && s_next <= j + 1 && mbar_test(smem_u32(&kv_full[s_next & 1]), (s_next >> 1) & 1) &&
-            (!s_first || mbar_test(smem_u32(q_full), s_piece & 1))) {
+        if (more_s && s_it <= o_it + 1 && mbar_test(smem_u32(&k_full[s_it & 1]), (s_it >> 1) & 1) && (!s_first || mbar_test(smem_u32(q_full), s_piece & 1))) {
           tc_fence_after();
-          const uint32_t kb = smem_u32(k_s + (s_next & 1) * L::KV_BYTES);
+          const int s = s_it & 1;
+          const uint32_t kb = smem_u32(k_s + s * L::KV_BYTES);
 #pragma unroll
           for (int k = 0; k < HD / 16; ++k) {
             const int hf = k / 4, kk = k % 4;
-            umma_f16(tmem_s + (uint32_t)((s_next & 1) * KT), umma_desc_sw128(smem_u32(q_s + hf * (128 * 128)) + kk * 32),
-                     umma_desc_sw128(kb + hf * (KT * 128) + kk * 32), idesc_s, k > 0 ? 1u : 0u);
+            umma_f16(tmem_s + (uint32_t)(s * KT), umma_desc_sw128(smem_u32(q_s + hf * (128 * 128)) + kk * 32), umma_desc_sw128(kb + hf * (KT * 128) + kk * 32), idesc_s,
+                     k > 0 ? 1u : 0u);
           }
-          umma_commit(smem_u32(&s_full[s_next & 1]));
-          ++s_next;
+          umma_commit(smem_u32(&s_full[s]));
+          umma_commit(smem_u32(&k_empty[s]));
+          ++s_it;
           s_first = false;
-          if (s_next == s_end) {                               // the piece's last S product frees Q
+          if (--s_left == 0) {                                 // the piece's last S product frees Q
             umma_commit(smem_u32(q_empty));
-            if (s_next < n) {
-              xs = piece_at(p, line, lens, first, u0 + s_next, u1);
-              s_end += xs.j1 - xs.j0;
-              ++s_piece;
-              s_first = true;
-            }
+            more_s = ahead.next();
+            s_left = ahead.x.j1 - ahead.x.j0;
+            ++s_piece;
+            s_first = true;
           }
           progressed = true;
         }
         // P is complete (and with it, on a piece's first tile, the way of the earlier O out of TMEM: the same warps did both)
-        if (s_next > j && mbar_test(smem_u32(&p_full[j & 1]), (j >> 1) & 1)) {
+        if (s_it > o_it && mbar_test(smem_u32(&p_full[o_it & 1]), (o_it >> 1) & 1) && mbar_test(smem_u32(&v_full[o_it & 1]), (o_it >> 1) & 1)) {
           tc_fence_after();
-          const int s = j & 1;
-          const uint32_t vb = smem_u32(v_s + s * L::KV_BYTES), pb = smem_u32(p_tile(s));
+          const int s = o_it & 1;
+          const uint32_t vb = smem_u32(v_s + s * L::KV_BYTES);
 #pragma unroll
           for (int k = 0; k < KT / 16; ++k)
-            umma_f16(tmem_o, umma_desc_sw128(pb + k * 32), umma_desc_sw128_mn(vb + k * (16 * 128), KT * 128, 1024), idesc_o, (!o_first || k > 0) ? 1u : 0u);
-          umma_commit(smem_u32(&kv_empty[s]));
-          umma_commit(smem_u32(pv_done));
-          ++j;
+            umma_f16_ts(tmem_o, tmem_s + (uint32_t)(s * KT + k * 8), umma_desc_sw128_mn(vb + k * (16 * 128), KT * 128, 1024), idesc_o, (!o_first || k > 0) ? 1u : 0u);
+          umma_commit(smem_u32(&v_empty[s]));
+          umma_commit(smem_u32(&pv_done[s]));
+          ++o_it;
           o_first = false;
-          if (j == o_end && j < n) {
-            xo = piece_at(p, line, lens, first, u0 + j, u1);
-            o_end += xo.j1 - xo.j0;
+          if (--o_left == 0) {
+            more_o = walk.next();
+            o_left = x.j1 - x.j0;
             o_first = true;
           }
           progressed = true;
         }
         if (progressed) {
-          t_start = 0;
+          idle_since = 0;
         } else {
           if (*abort_flag) break;
           const uint64_t now = global_timer_ns();
-          if (t_start == 0) t_start = now;
-          if (now - t_start > 1000000000ull) { *abort_flag = 1; break; }      // a second without progress
+          if (idle_since == 0) idle_since = now;
+          if (now - idle_since > 1000000000ull) { *abort_flag = 1; break; }      // a second without progress
         }
       }
     }
+  } else if (warp == 3) {
+    // ---- for the second kernel: where the pieces of a sequence's rows are ----
+    for (int b = cta + lane * (int)gridDim.x; b < p.B; b += 32 * (int)gridDim.x) {
+      int lo = -1, hi = p.groups;                              // first[lo] <= b < first[hi]
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first[mid] <= b) lo = mid; else hi = mid;
+      }
+      int4 r = make_int4(0, 0, 0, 0);
+      if (p.groups && lo >= 0 && b < first[lo + 1]) r = make_int4(line[lo], tiles_of(lens[lo]), first[lo] * p.T, (first[lo + 1] - first[lo]) * p.T);
+      p.records[2 * b] = r;
+      p.records[2 * b + 1] = make_int4(line[p.groups + b], tiles_of(lens[p.groups + b]), units, 0);
+    }
   } else {
     // ---- softmax: thread = row, TMEM lane quarter = warp % 4 ----
-    const int quarter = warp & 3, r = quarter * 32 + lane, e = (int)threadIdx.x - 64;
+    const int quarter = warp & 3, r = quarter * 32 + lane, e = (int)threadIdx.x - 128;
     const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
-    int it = 0, pieces = 0;
+    int it = 0;
     bool ok = true;
-    for (int u = u0; u < u1; ++pieces) {
-      const Piece x = piece_at(p, line, lens, first, u, u1);
+    for (int pieces = 0; walk.next(); ++pieces) {
       const int token = x.rt * p.TT + r / p.G;                 // of the segment
       const bool real = r < p.TT * p.G && token < x.ntok;
       const bool idle = !__any_sync(0xffffffffu, real);
@@ -362,97 +385,100 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
       const int tail = x.group ? x.len : max(0, x.len - p.T + 1);                             // keys from here on are seen by some rows only
       float m_ref = -INFINITY, l_run = 0.f;
       for (int j = x.j0; j < x.j1 && ok; ++j, ++it) {
-        const int s = it & 1;
+        const int s = it & 1, k0 = j * KT;
         ok = mbar_wait(smem_u32(&s_full[s]), (it >> 1) & 1, abort_flag, nullptr, 0);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         tc_fence_after();
-        const int k0 = j * KT;
-        unsigned char* vt = v_s + s * L::KV_BYTES;
-        if (x.len - k0 < KT || k0 + KT > tail) {               // V is touched below: its arrival, long over, is seen by this thread too
-          ok = mbar_wait(smem_u32(&kv_full[s]), (it >> 1) & 1, abort_flag, nullptr, 0);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-        }
-        if (x.len - k0 < KT) {                                 // V behind the last key: zeros
-          const int from = x.len - k0;
-          for (int i = e; i < (KT - from) * (HD / 8); i += 128) {
-            const int row = from + i / (HD / 8), c = i % (HD / 8);
-            *reinterpret_cast<uint4*>(vt + (c >> 3) * (KT * 128) + row * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
-          }
-        }
-        if (tail < x.len && k0 + KT > tail) {
-          // keys that only later tokens see: what is no number leaves the product
-          const int from = max(0, tail - k0), to = min(KT, x.len - k0);
-          for (int i = e; i < (to - from) * (HD / 2); i += 128) {
-            const int row = from + i / (HD / 2), c = i % (HD / 2);
-            uint32_t* at = reinterpret_cast<uint32_t*>(vt + (c >> 5) * (KT * 128) + row * 128 + (c & 31) * 4);
-            const uint32_t w = *at, inf = BF16 ? 0x7f80u : 0x7c00u;
-            uint32_t keep = 0xffffffffu;
-            if ((w & inf) == inf) keep &= 0xffff0000u;
-            if (((w >> 16) & inf) == inf) keep &= 0xffffu;
-            if (keep != 0xffffffffu) { *at = w & keep; *tail_bad = pieces; }
-          }
-        }
         bool move = false;
         float alpha = 1.f;
         if (!idle) {
           uint32_t sr[2][32];
-          tmem_ld_issue(tmem_s + (uint32_t)(s * KT) + lane_off, sr[0]);
-          tmem_ld_issue(tmem_s + (uint32_t)(s * KT) + lane_off + 32, sr[1]);
+          const uint32_t ts = tmem_s + (uint32_t)(s * KT) + lane_off;
+          tmem_ld_issue(ts, sr[0]);
+          tmem_ld_issue(ts + 32, sr[1]);
           tmem_ld_wait(sr[0]);
           tmem_ld_wait(sr[1]);
           float sc[KT];
 #pragma unroll
           for (int c = 0; c < KT; ++c) sc[c] = __uint_as_float(sr[c / 32][c % 32]);
-          const int nk = lim - k0, seen = pages_seen[s];
+          const int nk = lim - k0, seen = pages_seen[it & 3];
           if (__any_sync(0xffffffffu, nk < KT) || seen != 15) {
 #pragma unroll
             for (int c = 0; c < KT; ++c) sc[c] = (c < nk && ((seen >> (c / 16)) & 1)) ? sc[c] : -INFINITY;
           }
-          float mx = sc[0];
+          float mx4[4] = {sc[0], sc[1], sc[2], sc[3]};
 #pragma unroll
-          for (int c = 1; c < KT; ++c) mx = fmaxf(mx, sc[c]);
+          for (int c = 4; c < KT - 4; c += 8)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) mx4[q] = max3(mx4[q], sc[c + 2 * q], sc[c + 2 * q + 1]);
+          float mx = max3(max3(mx4[0], mx4[1], mx4[2]), mx4[3], max3(max3(sc[KT - 4], sc[KT - 3], sc[KT - 2]), sc[KT - 1], -INFINITY));
           mx *= p.scale_log2e;
           move = mx > m_ref + GAP || (m_ref == -INFINITY && mx > -INFINITY);
           const float m_new = move ? mx : m_ref, m_use = m_new == -INFINITY ? 0.f : m_new;
           alpha = move ? ex2(m_ref - m_use) : 1.f;
-          float sum = 0.f;
+          const uint64_t scale2 = pack_f32x2(p.scale_log2e, p.scale_log2e), minus2 = pack_f32x2(-m_use, -m_use);
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
           uint32_t packed[KT / 2];
 #pragma unroll
-          for (int c = 0; c < KT; c += 2)
-            packed[c / 2] = round_pair<BF16>(ex2(fmaf(sc[c], p.scale_log2e, -m_use)), ex2(fmaf(sc[c + 1], p.scale_log2e, -m_use)), sum);
-          l_run = l_run * alpha + sum;
+          for (int c = 0; c < KT; c += 2) {
+            const float2 t = unpack_f32x2(fma_f32x2(pack_f32x2(sc[c], sc[c + 1]), scale2, minus2));
+            const uint32_t w = round_pair<BF16>(ex2(t.x), ex2(t.y));
+            packed[c / 2] = w;
+            float &a = sum[c & 2], &b = sum[(c & 2) + 1];
+            a = BF16 ? add_lo_bf16(w, a) : add_lo_f16(w, a);
+            b = BF16 ? add_hi_bf16(w, b) : add_hi_f16(w, b);
+          }
+          l_run = l_run * alpha + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
           m_ref = m_new;
-          unsigned char* prow = p_tile(s) + r * 128;
-#pragma unroll
-          for (int c = 0; c < 8; ++c)
-            *reinterpret_cast<uint4*>(prow + ((c ^ (r & 7)) << 4)) = make_uint4(packed[4 * c], packed[4 * c + 1], packed[4 * c + 2], packed[4 * c + 3]);
+          tmem_st32_words(ts, packed);
         }
-        // P V of the tile before has landed: its phases are followed one by one (a parity wait tells only neighbours apart)
-        if (it > 0) {
-          ok = mbar_wait(smem_u32(pv_done), (it - 1) & 1, abort_flag, nullptr, 0);
+        if (x.len - k0 < KT || k0 + KT > tail) {
+          // V is touched: keys behind the length become zeros; of keys that only later tokens see, what is no number leaves the product
+          ok = mbar_wait(smem_u32(&v_full[s]), (it >> 1) & 1, abort_flag, nullptr, 0);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          unsigned char* vt = v_s + s * L::KV_BYTES;
+          const int from = min(KT, x.len - k0);
+          for (int i = e; i < (KT - from) * (HD / 8); i += 128) {
+            const int row = from + i / (HD / 8), c = i % (HD / 8);
+            *reinterpret_cast<uint4*>(vt + (c >> 3) * (KT * 128) + row * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+          }
+          if (tail < x.len) {
+            const int f = max(0, tail - k0);
+            for (int i = e; i < (from - f) * (HD / 2); i += 128) {
+              const int row = f + i / (HD / 2), c = i % (HD / 2);
+              uint32_t* at = reinterpret_cast<uint32_t*>(vt + (c >> 5) * (KT * 128) + row * 128 + (c & 31) * 4);
+              const uint32_t w = *at, inf = BF16 ? 0x7f80u : 0x7c00u;
+              uint32_t keep = 0xffffffffu;
+              if ((w & inf) == inf) keep &= 0xffff0000u;
+              if (((w >> 16) & inf) == inf) keep &= 0xffffu;
+              if (keep != 0xffffffffu) { *at = w & keep; *tail_bad = pieces; }
+            }
+          }
+          fence_proxy_async_smem();
+        }
+        if (j > x.j0 && __any_sync(0xffffffffu, move)) {
+          // O is rescaled once P V of the tile before has landed
+          ok = mbar_wait(smem_u32(&pv_done[s ^ 1]), ((it - 1) >> 1) & 1, abort_flag, nullptr, 0);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           tc_fence_after();
-          if (j > x.j0 && __any_sync(0xffffffffu, move)) {
 #pragma unroll 1
-            for (int c = 0; c < HD; c += 32) {
-              float o[32];
-              tmem_ld32(tmem_o + lane_off + c, o);
+          for (int c = 0; c < HD; c += 32) {
+            float o[32];
+            tmem_ld32(tmem_o + lane_off + c, o);
 #pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] *= alpha;
-              tmem_st32(tmem_o + lane_off + c, o);
-            }
+            for (int i = 0; i < 32; ++i) o[i] *= alpha;
+            tmem_st32(tmem_o + lane_off + c, o);
           }
         }
-        fence_proxy_async_smem();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&p_full[s]));
       }
       if (ok) {
-        ok = mbar_wait(smem_u32(pv_done), (it - 1) & 1, abort_flag, nullptr, 0);
+        ok = mbar_wait(smem_u32(&pv_done[(it - 1) & 1]), ((it - 1) >> 1) & 1, abort_flag, nullptr, 0);
         ok = __all_sync(0xffffffffu, ok);
         tc_fence_after();
       }
@@ -489,7 +515,6 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
         }
       }
       tc_fence_before();
-      u += x.j1 - x.j0;
     }
   }
 
@@ -515,25 +540,23 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) prefix_join_kernel(const Pref
   pdl_wait();
   if (at >= (int64_t)p.B * p.T * p.Hq) return;
   const int token = (int)(at / p.Hq), h = (int)(at % p.Hq), kvh = h / p.G, g = h - kvh * p.G, b = token / p.T;
-  const int units = p.line[p.groups + p.B], n = active(units, ctas);
-  const int group = p.group_of[b];
+  const int4 shared = p.records[2 * b], mine = p.records[2 * b + 1];
+  const int units = mine.z, n = active(units, ctas);
   float top = -INFINITY, sum = 0.f, o[D];
 #pragma unroll
   for (int i = 0; i < D; ++i) o[i] = 0.f;
 #pragma unroll 1
   for (int part = 0; part < 2; ++part) {
+    const int tiles = part == 0 ? shared.y : mine.y;
+    if (tiles == 0) continue;
     Piece x;
     x.group = part == 0;
-    if (x.group && group < 0) continue;
-    x.seg = x.group ? group : p.groups + b;
-    x.tok0 = x.group ? p.first[group] * p.T : b * p.T;
-    x.ntok = x.group ? (p.first[group + 1] - p.first[group]) * p.T : p.T;
+    x.tok0 = x.group ? shared.z : b * p.T;
+    x.ntok = x.group ? shared.w : p.T;
     x.kvh = kvh;
     const int local = token - x.tok0, row_tiles = (x.ntok + p.TT - 1) / p.TT;
     x.rt = local / p.TT;
-    const int begin = p.line[x.seg], tiles = (p.line[x.seg + 1] - begin) / (p.Hkv * row_tiles);
-    if (tiles == 0) continue;
-    const int u = begin + (kvh * row_tiles + x.rt) * tiles, c0 = cta_of(u, units, n), c1 = cta_of(u + tiles - 1, units, n);
+    const int u = (x.group ? shared.x : mine.x) + (kvh * row_tiles + x.rt) * (tiles + OV) + OV, c0 = cta_of(u, units, n), c1 = cta_of(u + tiles - 1, units, n);
     const int64_t row0 = piece_row(p, x, 0) + (local - x.rt * p.TT) * p.G + g, step = piece_row(p, x, 1) - piece_row(p, x, 0);
     const float *ml = x.group ? p.ml_p : p.ml_o, *po = x.group ? p.o_p : p.o_o;
     for (int base = c0; base <= c1; base += 32) {
@@ -587,7 +610,7 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) prefix_join_kernel(const Pref
 // ---- host ------------------------------------------------------------------------------------------
 
 struct Layout {
-  size_t line, group_of, first, ml_p, o_p, ml_o, o_o, bytes;
+  size_t records, ml_p, o_p, ml_o, o_o, bytes;
 };
 
 int tokens_of_tile(int G) { return 128 / G; }
@@ -599,9 +622,7 @@ Layout layout_of(int groups, int B, int T, int Hq, int G, int hd) {
   Layout l;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
-  l.line = take((size_t)(groups + B + 1) * 4);
-  l.group_of = take((size_t)B * 4);
-  l.first = take((size_t)(groups + 1) * 4);
+  l.records = take((size_t)B * 2 * sizeof(int4));
   l.ml_p = take((size_t)rows_p * 8);
   l.o_p = take((size_t)rows_p * hd * 4);
   l.ml_o = take((size_t)rows_o * 8);
@@ -664,7 +685,7 @@ extern "C" es_status_t es_op_decode_attention_prefix(const void* q, int32_t dtyp
     return fail(ES_ERR_INVALID_ARG, "q, pages and scratch must be 16-byte aligned, out 8-byte aligned");
   const int G = Hq / Hkv, TT = tokens_of_tile(G);
   // tiles on the line: every token's row tiles, a part of one more for each group
-  const long long own_tiles = (max_ctx + KT - 1) / KT, prefix_tiles = groups ? (max_prefix + KT - 1) / KT : 0;
+  const long long own_tiles = (max_ctx + KT - 1) / KT + OV, prefix_tiles = groups ? (max_prefix + KT - 1) / KT + OV : 0;
   const long long line = Hkv * (B * (long long)((T + TT - 1) / TT) * own_tiles + ((long long)B * T / TT + 1 + groups) * prefix_tiles);
   if (line > (1LL << 30)) return fail(ES_ERR_RANGE, "heads * tokens * keys exceed one launch");
   const Layout l = layout_of(groups, B, T, Hq, G, hd);
@@ -675,7 +696,7 @@ extern "C" es_status_t es_op_decode_attention_prefix(const void* q, int32_t dtyp
   p.v_pages = v_pages;
   p.out = out;
   char* base = (char*)scratch;
-  p.line = (int*)(base + l.line); p.group_of = (int*)(base + l.group_of); p.first = (int*)(base + l.first);
+  p.records = (int4*)(base + l.records);
   p.ml_p = (float*)(base + l.ml_p); p.o_p = (float*)(base + l.o_p); p.ml_o = (float*)(base + l.ml_o); p.o_o = (float*)(base + l.o_o);
   p.B = B; p.T = T; p.Hq = Hq; p.Hkv = Hkv; p.G = G; p.P = page_tokens; p.groups = groups;
   while ((1 << p.log2P) < page_tokens) ++p.log2P;

@@ -109,6 +109,14 @@ __device__ __forceinline__ void umma_f16(uint32_t tmem_d, uint64_t adesc, uint64
       ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(acc)
       : "memory");
 }
+// the same with A in TMEM: lane = row, two K-elements to a column
+__device__ __forceinline__ void umma_f16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+      ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(acc)
+      : "memory");
+}
 __device__ __forceinline__ void umma_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
@@ -178,6 +186,33 @@ __device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c
   return d;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// c + the low (high) 16 bits of w as a number of that type
+__device__ __forceinline__ float add_lo_f16(uint32_t w, float c) {
+  float d;
+  asm("{\n.reg .b16 lo, hi;\nmov.b32 {lo, hi}, %1;\nadd.f32.f16 %0, lo, %2;\n}" : "=f"(d) : "r"(w), "f"(c));
+  return d;
+}
+__device__ __forceinline__ float add_hi_f16(uint32_t w, float c) {
+  float d;
+  asm("{\n.reg .b16 lo, hi;\nmov.b32 {lo, hi}, %1;\nadd.f32.f16 %0, hi, %2;\n}" : "=f"(d) : "r"(w), "f"(c));
+  return d;
+}
+__device__ __forceinline__ float add_lo_bf16(uint32_t w, float c) {
+  float d;
+  asm("{\n.reg .b16 lo, hi;\nmov.b32 {lo, hi}, %1;\nadd.f32.bf16 %0, lo, %2;\n}" : "=f"(d) : "r"(w), "f"(c));
+  return d;
+}
+__device__ __forceinline__ float add_hi_bf16(uint32_t w, float c) {
+  float d;
+  asm("{\n.reg .b16 lo, hi;\nmov.b32 {lo, hi}, %1;\nadd.f32.bf16 %0, hi, %2;\n}" : "=f"(d) : "r"(w), "f"(c));
+  return d;
+}
+
 // 32 consecutive fp32 accumulator columns of this thread's TMEM lane.
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32]) {
   uint32_t r[32];
@@ -230,6 +265,14 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&v)[32]) 
         "r"(__float_as_uint(v[31]))
       : "memory");
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
+// 32 words of this thread's TMEM lane.
+__device__ __forceinline__ void tmem_st32_words(uint32_t taddr, const uint32_t (&v)[32]) {
+  float f[32];
+#pragma unroll
+  for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(v[i]);
+  tmem_st32(taddr, f);
 }
 
 // ---- CTA pairs (cta_group::2): one MMA spans the tensor cores and shared memory of two CTAs ------
