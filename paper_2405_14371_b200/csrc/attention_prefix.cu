@@ -44,7 +44,7 @@ constexpr int OV = 2;                    // places on the line that an item take
 constexpr int MIN_UNITS = 2 + OV;        // places of a stretch, at least
 constexpr int MAX_SEGMENTS = 8192;
 
-struct alignas(64) PrefixMaps { CUtensorMap q, k, v; };
+struct alignas(64) PrefixMaps { CUtensorMap q, q_own, k, v; };   // q_own: boxes of one sequence's rows
 
 struct PrefixParams {
   const int *prefix_table, *prefix_len, *begin, *table, *ctx;
@@ -54,6 +54,8 @@ struct PrefixParams {
   float *ml_p, *o_p, *ml_o, *o_o;        // pieces of prefixes and of own keys: [rows][2], [rows][hd]
   int B, T, Hq, Hkv, G, P, log2P, groups, prefix_pages, pps, n_pages, max_prefix, max_ctx;
   int TT;                                // tokens of a row tile
+  int own_row_tiles, own_rows;           // of one sequence: row tiles; rows of the first (own_q: they fit a quarter of the tile)
+  int own_q;
   int box;                               // tokens of a page that one copy brings
   float scale_log2e;
 };
@@ -73,43 +75,65 @@ __device__ __forceinline__ int active(int units, int ctas) { return max(1, min(c
 __device__ __forceinline__ int start_of(int cta, int units, int n) { return (int)((long long)units * cta / n); }
 __device__ __forceinline__ int cta_of(int unit, int units, int n) { return (int)(((long long)(unit + 1) * n - 1) / units); }
 
-// The pieces of a stretch, one after the other.
+// The pieces of a stretch, one after the other.  Only the first is searched for.
 struct Walk {
   const PrefixParams& p;
   const int *line, *lens, *first;
-  int u, end;
+  int u, end, item, a, row_tiles;                         // place on the line; item of the segment, place in the item
   Piece x;
   __device__ __forceinline__ Walk(const PrefixParams& p_, const int* line_, const int* lens_, const int* first_, int u_, int end_)
-      : p(p_), line(line_), lens(lens_), first(first_), u(u_), end(end_) {}
+      : p(p_), line(line_), lens(lens_), first(first_), u(u_), end(end_), item(-1) {}
+  __device__ __forceinline__ void segment(int s) {
+    x.seg = s;
+    x.group = s < p.groups;
+    x.len = lens[s];
+    if (x.group) {
+      x.tok0 = first[s] * p.T;
+      x.ntok = (first[s + 1] - first[s]) * p.T;
+      row_tiles = (x.ntok + p.TT - 1) / p.TT;
+    } else {
+      x.tok0 = (s - p.groups) * p.T;
+      x.ntok = p.T;
+      row_tiles = p.own_row_tiles;
+    }
+  }
   __device__ __forceinline__ bool next() {
     while (u < end) {
-      int lo = 0, hi = p.groups + p.B;                    // line[lo] <= u < line[hi]
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (line[mid] <= u) lo = mid; else hi = mid;
+      if (item < 0) {
+        int lo = 0, hi = p.groups + p.B;                  // line[lo] <= u < line[hi]
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (line[mid] <= u) lo = mid; else hi = mid;
+        }
+        segment(lo);
+        const int k = tiles_of(x.len) + OV, r = u - line[lo];
+        item = r / k;
+        a = r - item * k;
+        x.kvh = item / row_tiles;
+        x.rt = item - x.kvh * row_tiles;
+      } else {                                            // the item before has ended: the stretch goes on
+        a = 0;
+        if (++x.rt == row_tiles) { x.rt = 0; ++x.kvh; }
+        if (x.kvh == p.Hkv) {
+          int s = x.seg + 1;
+          while (line[s + 1] == u) ++s;                   // segments without places; u < end <= line[segments]
+          segment(s);
+          x.kvh = x.rt = 0;
+        }
       }
-      x.seg = lo;
-      x.group = lo < p.groups;
-      x.len = lens[lo];
-      if (x.group) {
-        x.tok0 = first[lo] * p.T;
-        x.ntok = (first[lo + 1] - first[lo]) * p.T;
-      } else {
-        x.tok0 = (lo - p.groups) * p.T;
-        x.ntok = p.T;
-      }
-      const int row_tiles = (x.ntok + p.TT - 1) / p.TT, k = tiles_of(x.len) + OV, r = u - line[lo], item = r / k, a = r - item * k;
-      const int take = min(k - a, end - u);
+      const int take = min(tiles_of(x.len) + OV - a, end - u);
       x.j0 = max(0, a - OV);
       x.j1 = max(0, a + take - OV);
-      x.kvh = item / row_tiles;
-      x.rt = item - x.kvh * row_tiles;
       u += take;
       if (x.j1 > x.j0) return true;
     }
     return false;
   }
 };
+
+// Rows of a single sequence that fit a quarter of the tile go to one of the four by turns: the warp that has the quarter, and the
+// part of the SM it runs on, differ between the CTAs that share an SM.
+__device__ __forceinline__ int row_offset(const PrefixParams& p, const Piece& x) { return !x.group && p.own_q ? 32 * ((x.seg + x.kvh) & 3) : 0; }
 
 // First row of a piece's partials, in the prefixes' or the own keys' part of the scratch: the rows of the items before it, and
 // a tile's worth for each CTA before this one.
@@ -205,27 +229,29 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
 
   // ---- the line ----
   const int segments = p.groups + p.B, per = (segments + THREADS) / THREADS, s0 = (int)threadIdx.x * per;      // `per` segments a thread
-  for (int s = threadIdx.x; s < segments; s += THREADS)
-    lens[s] = s < p.groups ? min(max(p.prefix_len[s], 0), p.max_prefix) : min(max(p.ctx[s - p.groups], 0), p.max_ctx);
-  if (p.groups)
-    for (int g = threadIdx.x; g <= p.groups; g += THREADS) first[g] = min(max(p.begin[g], 0), p.B);
+  for (int s = threadIdx.x; s <= segments; s += THREADS) {     // both loads are under way together
+    const int g = p.groups && s <= p.groups ? p.begin[s] : 0;
+    const int n = s < p.groups ? p.prefix_len[s] : s < segments ? p.ctx[s - p.groups] : 0;
+    if (s < segments) lens[s] = min(max(n, 0), s < p.groups ? p.max_prefix : p.max_ctx);
+    if (p.groups && s <= p.groups) first[s] = min(max(g, 0), p.B);
+  }
   __syncthreads();
   {
-    // a group begins no earlier than those before it end
-    int top = 0, all;
-    for (int s = s0; s < min(s0 + per, p.groups + 1); ++s) if (p.groups) top = max(top, first[s]);
-    auto larger = [](int a, int b) { return max(a, b); };
-    const int mine = top;
-    top = block_scan(mine, totals, &all, larger);
-    int before = __shfl_up_sync(0xffffffffu, top, 1);
-    if (lane == 0) { before = 0; for (int w = 0; w < warp; ++w) before = max(before, totals[w]); }
-    for (int s = s0; s < min(s0 + per, p.groups + 1); ++s)
-      if (p.groups) { before = max(before, first[s]); first[s] = before; }
-    __syncthreads();
-    int sum = 0;
+    int all, sum = 0;
+    if (p.groups) {
+      // a group begins no earlier than those before it end
+      const int to = min(s0 + per, p.groups + 1);
+      int top = 0;
+      for (int s = s0; s < to; ++s) top = max(top, first[s]);
+      top = block_scan(top, totals, &all, [](int a, int b) { return max(a, b); });
+      int before = __shfl_up_sync(0xffffffffu, top, 1);
+      if (lane == 0) { before = 0; for (int w = 0; w < warp; ++w) before = max(before, totals[w]); }
+      for (int s = s0; s < to; ++s) { before = max(before, first[s]); first[s] = before; }
+      __syncthreads();
+    }
     auto places = [&](int s) {
-      const int tokens = s < p.groups ? (first[s + 1] - first[s]) * p.T : p.T;
-      return lens[s] > 0 ? p.Hkv * ((tokens + p.TT - 1) / p.TT) * (tiles_of(lens[s]) + OV) : 0;
+      const int row_tiles = s < p.groups ? ((first[s + 1] - first[s]) * p.T + p.TT - 1) / p.TT : p.own_row_tiles;
+      return lens[s] > 0 ? p.Hkv * row_tiles * (tiles_of(lens[s]) + OV) : 0;
     };
     for (int s = s0; s < min(s0 + per, segments); ++s) sum += places(s);
     int at = block_scan(sum, totals, &all, [](int a, int b) { return a + b; }) - sum;
@@ -285,10 +311,12 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           if (lane == 0) {
-            mbar_expect_tx(smem_u32(q_full), p.TT * p.G * HD * 2);
+            const bool few = !x.group && p.own_q;
+            mbar_expect_tx(smem_u32(q_full), (few ? p.own_rows : p.TT * p.G) * HD * 2);
 #pragma unroll
             for (int h = 0; h < L::HALVES; ++h)
-              tma_load_3d(smem_u32(q_s + h * (128 * 128)), &maps.q, h * 64, x.kvh * p.G, x.tok0 + x.rt * p.TT, smem_u32(q_full));
+              tma_load_3d(smem_u32(q_s + h * (128 * 128) + row_offset(p, x) * 128), few ? &maps.q_own : &maps.q, h * 64, x.kvh * p.G, x.tok0 + x.rt * p.TT,
+                          smem_u32(q_full));
           }
         }
       }
@@ -373,13 +401,15 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
     }
   } else {
     // ---- softmax: thread = row, TMEM lane quarter = warp % 4 ----
-    const int quarter = warp & 3, r = quarter * 32 + lane, e = (int)threadIdx.x - 128;
+    const int quarter = warp & 3, e = (int)threadIdx.x - 128;
     const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
+    const int token0 = (quarter * 32 + lane) / p.G, lane_token = lane / p.G;
     int it = 0;
     bool ok = true;
     for (int pieces = 0; walk.next(); ++pieces) {
-      const int token = x.rt * p.TT + r / p.G;                 // of the segment
-      const bool real = r < p.TT * p.G && token < x.ntok;
+      const int off = row_offset(p, x), r = quarter * 32 + lane - off;
+      const int token = x.rt * p.TT + (off ? lane_token : token0);                            // of the segment
+      const bool real = r >= 0 && r < (x.group ? p.TT * p.G : p.own_rows) && token < x.ntok;
       const bool idle = !__any_sync(0xffffffffu, real);
       const int lim = !real ? 0 : x.group ? x.len : min(x.len, x.len - p.T + token + 1);      // keys that the row sees
       const int tail = x.group ? x.len : max(0, x.len - p.T + 1);                             // keys from here on are seen by some rows only
@@ -702,10 +732,14 @@ extern "C" es_status_t es_op_decode_attention_prefix(const void* q, int32_t dtyp
   while ((1 << p.log2P) < page_tokens) ++p.log2P;
   p.prefix_pages = prefix_pages; p.pps = pages_per_seq; p.n_pages = n_pages; p.max_prefix = groups ? max_prefix : 0; p.max_ctx = max_ctx;
   p.TT = TT;
+  p.own_row_tiles = (T + TT - 1) / TT;
+  p.own_rows = (T < TT ? T : TT) * G;
+  p.own_q = p.own_rows <= 32;
   p.box = page_tokens < KT ? page_tokens : KT;
   p.scale_log2e = 1.4426950408889634f / sqrtf((float)hd);
-  PrefixMaps maps;
+  PrefixMaps maps = {};
   ES_TRY(tma_encode_3d_f16(&maps.q, q, (int64_t)B * T, Hq, hd, q_stride, TT, G));
+  if (p.own_q) ES_TRY(tma_encode_3d_f16(&maps.q_own, q, (int64_t)B * T, Hq, hd, q_stride, T, G));
   const int64_t lines = (int64_t)n_pages * Hkv * page_tokens;
   ES_TRY(tma_encode_2d_f16(&maps.k, k_pages, lines, hd, hd, p.box));
   ES_TRY(tma_encode_2d_f16(&maps.v, v_pages, lines, hd, hd, p.box));
