@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
           }
         }
         here = __reduce_or_sync(0xffffffffu, here);
-        ok = mbar_wait(smem_u32(&empty[s]), ((it >> 1) & 1) ^ 1, abort_flag, nullptr, 0);
+        ok = mbar_wait_soon(smem_u32(&empty[s]), ((it >> 1) & 1) ^ 1, abort_flag);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         const uint32_t fb = smem_u32(&full[s]);
@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
           for (int h = 0; h < L::HALVES; ++h) tma_load_2d(smem_u32(ring + s * L::KV_BYTES + h * (KT * 128) + lane * p.box * 128), map, h * 64, row, fb);
         }
         if (key && j == x.j0) {                                // the first tile is under way before Q's place is free
-          ok = mbar_wait(smem_u32(q_empty), (pieces & 1) ^ 1, abort_flag, nullptr, 0);
+          ok = mbar_wait_soon(smem_u32(q_empty), (pieces & 1) ^ 1, abort_flag);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           if (lane == 0) {
@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
       float m_ref = -INFINITY, l_run = 0.f;
       for (int j = x.j0; j < x.j1 && ok; ++j, ++it) {
         const int s = it & 1, k0 = j * KT;
-        ok = mbar_wait(smem_u32(&s_full[s]), (it >> 1) & 1, abort_flag, nullptr, 0);
+        ok = mbar_wait_soon(smem_u32(&s_full[s]), (it >> 1) & 1, abort_flag);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         tc_fence_after();
@@ -465,7 +465,7 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
         }
         if (x.len - k0 < KT || k0 + KT > tail) {
           // V is touched: keys behind the length become zeros; of keys that only later tokens see, what is no number leaves the product
-          ok = mbar_wait(smem_u32(&v_full[s]), (it >> 1) & 1, abort_flag, nullptr, 0);
+          ok = mbar_wait_soon(smem_u32(&v_full[s]), (it >> 1) & 1, abort_flag);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           unsigned char* vt = v_s + s * L::KV_BYTES;
@@ -490,7 +490,7 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
         }
         if (j > x.j0 && __any_sync(0xffffffffu, move)) {
           // O is rescaled once P V of the tile before has landed
-          ok = mbar_wait(smem_u32(&pv_done[s ^ 1]), ((it - 1) >> 1) & 1, abort_flag, nullptr, 0);
+          ok = mbar_wait_soon(smem_u32(&pv_done[s ^ 1]), ((it - 1) >> 1) & 1, abort_flag);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           tc_fence_after();
@@ -508,7 +508,7 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
         if (lane == 0) mbar_arrive(smem_u32(&p_full[s]));
       }
       if (ok) {
-        ok = mbar_wait(smem_u32(&pv_done[(it - 1) & 1]), ((it - 1) >> 1) & 1, abort_flag, nullptr, 0);
+        ok = mbar_wait_soon(smem_u32(&pv_done[(it - 1) & 1]), ((it - 1) >> 1) & 1, abort_flag);
         ok = __all_sync(0xffffffffu, ok);
         tc_fence_after();
       }

@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(RowsCfg<NT>::THREADS, RowsCfg<NT>::OCC) linear
       }
       for (int i = early; i < blocks; ++i) {
         const int s = i % L::STAGES;
-        if (!mbar_wait(smem_u32(&empty[s]), ((i / L::STAGES) & 1) ^ 1, abort_flag, nullptr, 0)) break;
+        if (!mbar_wait_soon(smem_u32(&empty[s]), ((i / L::STAGES) & 1) ^ 1, abort_flag)) break;
         const uint32_t fb = smem_u32(&full[s]);
         mbar_expect_tx(fb, L::STAGE);
         tma_load_2d(smem_u32(ring + s * L::STAGE), &maps.w, (b0 + i) * (BKB / 2), n0, fb);
@@ -136,17 +136,17 @@ __global__ void __launch_bounds__(RowsCfg<NT>::THREADS, RowsCfg<NT>::OCC) linear
     if (lane == 0) {
       // ---- MMA ----
       constexpr uint32_t idesc = umma_idesc_f16(128, NT);
-      for (int i = 0; i < blocks; ++i) {
-        const int s = i % L::STAGES, buf = i % L::BUFS;
-        if (!mbar_wait(smem_u32(&full[s]), (i / L::STAGES) & 1, abort_flag, nullptr, 0)) break;
-        if (!mbar_wait(smem_u32(&acc_empty[buf]), ((i / L::BUFS) & 1) ^ 1, abort_flag, nullptr, 0)) break;
+      const uint64_t w0 = umma_desc_sw128(smem_u32(ring)), x0 = umma_desc_sw128(smem_u32(ring) + W_TILE);
+      const uint32_t full0 = smem_u32(full), empty0 = smem_u32(empty), acc_full0 = smem_u32(acc_full), acc_empty0 = smem_u32(acc_empty);
+      uint32_t s = 0, ring_phase = 0, buf = 0, buf_phase = 1;
+      for (int left = blocks; left > 0; --left) {
+        if (!mbar_wait_soon(full0 + s * 8, ring_phase, abort_flag) || !mbar_wait_soon(acc_empty0 + buf * 8, buf_phase, abort_flag)) break;
         tc_fence_after();
-        const uint32_t w = smem_u32(ring + s * L::STAGE), x = w + W_TILE;
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          umma_f8(tmem + buf * NT, umma_desc_sw128(w + k * 32), umma_desc_sw128(x + k * 32), idesc, k > 0 ? 1u : 0u);
-        umma_commit(smem_u32(&empty[s]));
-        umma_commit(smem_u32(&acc_full[buf]));
+        umma_f8_block(tmem + buf * NT, w0 + s * (L::STAGE >> 4), x0 + s * (L::STAGE >> 4), idesc);
+        umma_commit(acc_full0 + buf * 8);
+        umma_commit(empty0 + s * 8);
+        if (++s == L::STAGES) { s = 0; ring_phase ^= 1; }
+        if (++buf == L::BUFS) { buf = 0; buf_phase ^= 1; }
       }
     }
   } else if (warp == 2) {
@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(RowsCfg<NT>::THREADS, RowsCfg<NT>::OCC) linear
       for (int q = 0; q < BATCH; ++q) {
         const int i = i0 + q, slot = i % L::FACTORS;
         if (i >= blocks) break;
-        if (!mbar_wait(smem_u32(&fac_empty[slot]), ((i / L::FACTORS) & 1) ^ 1, abort_flag, nullptr, 0)) return;
+        if (!mbar_wait_soon(smem_u32(&fac_empty[slot]), ((i / L::FACTORS) & 1) ^ 1, abort_flag)) return;
 #pragma unroll
         for (int t = 0; t < PER; ++t)
           if (lane + 32 * t < NT) factor[slot * NT + lane + 32 * t] = a[q][t] * w[q];
@@ -197,8 +197,8 @@ __global__ void __launch_bounds__(RowsCfg<NT>::THREADS, RowsCfg<NT>::OCC) linear
     for (int j = 0; j < L::MINE; ++j) acc[j] = 0.f;
     for (int i = 0; i < blocks; ++i) {
       const int buf = i % L::BUFS, slot = i % L::FACTORS;
-      ok = mbar_wait(smem_u32(&fac_full[slot]), (i / L::FACTORS) & 1, abort_flag, nullptr, 0) &&
-           mbar_wait(smem_u32(&acc_full[buf]), (i / L::BUFS) & 1, abort_flag, nullptr, 0);
+      ok = mbar_wait_soon(smem_u32(&fac_full[slot]), (i / L::FACTORS) & 1, abort_flag) &&
+           mbar_wait_soon(smem_u32(&acc_full[buf]), (i / L::BUFS) & 1, abort_flag);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
@@ -428,7 +428,7 @@ __global__ void __launch_bounds__(P_THREADS, 1) linear_fp8_pair_kernel(const __g
         origin(tile, m0, n0);
         for (int b = 0; b < p.nkb; ++b, ++it) {
           const int s = it % P_STAGES;
-          if (!mbar_wait(smem_u32(&empty[s]), ((it / P_STAGES) & 1) ^ 1, abort_flag, nullptr, 0)) { ok = false; break; }
+          if (!mbar_wait_soon(smem_u32(&empty[s]), ((it / P_STAGES) & 1) ^ 1, abort_flag)) { ok = false; break; }
           const uint32_t fb = smem_u32(&full[s]), dst = smem_u32(ring + s * P_STAGE);
           if (rank == 0) mbar_expect_tx(fb, 2 * P_STAGE);               // both CTAs' bytes land on this barrier
           tma_load_2d_pair(dst, &maps.a, b * (BKB / 2), m0 + (int)rank * 128, fb);
@@ -437,23 +437,21 @@ __global__ void __launch_bounds__(P_THREADS, 1) linear_fp8_pair_kernel(const __g
       }
     }
     if (warp == 1 && lane == 0 && rank == 0) {
+      // This thread's own instructions are on the path of every block: they are kept few.
       constexpr uint32_t idesc = umma_idesc_f16(256, 256);
-      int it = 0;
-      bool ok = true;
-      for (int tile = pair; tile < tiles && ok; tile += n_pairs) {
-        for (int b = 0; b < p.nkb; ++b, ++it) {
-          const int s = it % P_STAGES, buf = it & 1;
-          ok = mbar_wait(smem_u32(&full[s]), (it / P_STAGES) & 1, abort_flag, nullptr, 0) &&
-               mbar_wait(smem_u32(&acc_empty[buf]), ((it >> 1) & 1) ^ 1, abort_flag, nullptr, 0);
-          if (!ok) break;
-          tc_fence_after();
-          const uint32_t a = smem_u32(ring + s * P_STAGE), w = a + W_TILE;
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            umma_f8_pair(tmem + buf * 256, umma_desc_sw128(a + k * 32), umma_desc_sw128(w + k * 32), idesc, k > 0 ? 1u : 0u);
-          umma_commit_pair(smem_u32(&empty[s]));
-          umma_commit_pair(smem_u32(&acc_full[buf]));
-        }
+      const uint64_t a0 = umma_desc_sw128(smem_u32(ring)), w0 = umma_desc_sw128(smem_u32(ring) + W_TILE);
+      const uint32_t full0 = smem_u32(full), empty0 = smem_u32(empty), acc_full0 = smem_u32(acc_full), acc_empty0 = smem_u32(acc_empty);
+      int left = pair < tiles ? ((tiles - 1 - pair) / n_pairs + 1) * p.nkb : 0;
+      uint32_t s = 0, ring_phase = 0, buf = 0, buf_phase = 1;
+      for (; left > 0; --left) {
+        if (!mbar_wait_soon(full0 + s * 8, ring_phase, abort_flag) || !mbar_wait_soon(acc_empty0 + buf * 8, buf_phase, abort_flag)) break;
+        tc_fence_after();
+        umma_f8_block_pair(tmem + buf * 256, a0 + s * (P_STAGE >> 4), w0 + s * (P_STAGE >> 4), idesc);
+        umma_commit_pair(acc_full0 + buf * 8);
+        umma_commit_pair(empty0 + s * 8);
+        if (++s == P_STAGES) { s = 0; ring_phase ^= 1; }
+        buf ^= 1;
+        if (buf == 0) buf_phase ^= 1;
       }
     }
   } else {
@@ -477,7 +475,7 @@ __global__ void __launch_bounds__(P_THREADS, 1) linear_fp8_pair_kernel(const __g
         const int buf = it & 1;
         const float f = sa * sw;
         if (in && b + 1 < p.nkb) { sa = as[(int64_t)(b + 1) * p.M]; sw = ws[b + 1]; }
-        if (ok) ok = mbar_wait(smem_u32(&acc_full[buf]), (it >> 1) & 1, abort_flag, nullptr, 0);
+        if (ok) ok = mbar_wait_soon(smem_u32(&acc_full[buf]), (it >> 1) & 1, abort_flag);
         if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
         tc_fence_after();
         const uint64_t ff = pack_f32x2(f, f);

@@ -65,6 +65,20 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   }
 }
 
+// The same for waits that are short and many: the clock (whose reading takes about 480 cycles, which mbar_wait spends on every
+// wait that is not over at once) is left alone for the first 255 looks.
+__device__ __forceinline__ bool mbar_wait_soon(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  uint64_t t0 = 0;
+  for (uint32_t looks = 1; !mbar_test(bar, parity); ++looks) {
+    if ((looks & 255u) != 0) continue;
+    if (*abort_flag) return false;
+    const uint64_t now = global_timer_ns();
+    if (t0 == 0) t0 = now;
+    if (now - t0 > 1000000000ull) { *abort_flag = 1; return false; }
+  }
+  return true;
+}
+
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
@@ -121,13 +135,20 @@ __device__ __forceinline__ void umma_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
-// kind::f8f6f4 with e4m3 operands (type codes 0, so the instruction descriptor is umma_idesc_f16's): 32 K-elements of one
-// byte per instruction.
-__device__ __forceinline__ void umma_f8(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
+// kind::f8f6f4 with e4m3 operands (type codes 0, so the instruction descriptor is umma_idesc_f16's).
+// The four instructions that multiply tiles of 128 one-byte K-elements (128-byte swizzle), descriptors of the tiles given: a step
+// of 32 bytes is 2 in a descriptor's address field.  The sums start anew.
+__device__ __forceinline__ void umma_f8_block(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc) {
   asm volatile(
-      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}"
-      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(acc)
+      "{\n.reg .pred f, t;\n.reg .b64 a1, a2, a3, b1, b2, b3;\n"
+      "setp.ne.b32 f, 0, 0;\nsetp.eq.b32 t, 0, 0;\n"
+      "add.s64 a1, %1, 2;\nadd.s64 a2, %1, 4;\nadd.s64 a3, %1, 6;\n"
+      "add.s64 b1, %2, 2;\nadd.s64 b2, %2, 4;\nadd.s64 b3, %2, 6;\n"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, f;\n"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a1, b1, %3, t;\n"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a2, b2, %3, t;\n"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a3, b3, %3, t;\n}"
+      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc)
       : "memory");
 }
 
@@ -308,11 +329,18 @@ __device__ __forceinline__ void umma_f16_pair(uint32_t tmem_d, uint64_t adesc, u
       ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(acc)
       : "memory");
 }
-__device__ __forceinline__ void umma_f8_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
+// umma_f8_block by a pair
+__device__ __forceinline__ void umma_f8_block_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc) {
   asm volatile(
-      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}"
-      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(acc)
+      "{\n.reg .pred f, t;\n.reg .b64 a1, a2, a3, b1, b2, b3;\n"
+      "setp.ne.b32 f, 0, 0;\nsetp.eq.b32 t, 0, 0;\n"
+      "add.s64 a1, %1, 2;\nadd.s64 a2, %1, 4;\nadd.s64 a3, %1, 6;\n"
+      "add.s64 b1, %2, 2;\nadd.s64 b2, %2, 4;\nadd.s64 b3, %2, 6;\n"
+      "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, f;\n"
+      "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a1, b1, %3, t;\n"
+      "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a2, b2, %3, t;\n"
+      "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a3, b3, %3, t;\n}"
+      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc)
       : "memory");
 }
 // completion of the pair's MMAs, signalled on the barrier at this offset in both CTAs
