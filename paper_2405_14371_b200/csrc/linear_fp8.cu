@@ -46,14 +46,26 @@ struct Fp8Params {
 constexpr int BKB = 128;                         // bytes (= codes) of a row per block
 constexpr int W_TILE = 128 * BKB;
 
-__device__ __forceinline__ void store_one(const Fp8Params& p, int64_t at, float v) {
+// Results of one weight row, of tokens m, m + step, ... < m1.  The residual of all is asked for before the first is stored (it may
+// be where the result goes, so the compiler keeps the order: token by token, 113 of them waited 8 us).
+template <int MANY>
+__device__ __forceinline__ void store_many(const Fp8Params& p, int n, int m, int step, int m1, const float* v) {
+  const int64_t at = (int64_t)m * p.N + n, far = (int64_t)step * p.N;
   if (p.out == ES_DTYPE_F32) {
-    if (p.R) v += p.R[at];
-    ((float*)p.C)[at] = v;
+    float r[MANY];
+#pragma unroll
+    for (int q = 0; q < MANY; ++q) r[q] = p.R && m + q * step < m1 ? p.R[at + q * far] : 0.f;
+#pragma unroll
+    for (int q = 0; q < MANY; ++q)
+      if (m + q * step < m1) ((float*)p.C)[at + q * far] = p.R ? v[q] + r[q] : v[q];
   } else if (p.out == ES_DTYPE_F16) {
-    ((__half*)p.C)[at] = __float2half_rn(v);
+#pragma unroll
+    for (int q = 0; q < MANY; ++q)
+      if (m + q * step < m1) ((__half*)p.C)[at + q * far] = __float2half_rn(v[q]);
   } else {
-    ((__nv_bfloat16*)p.C)[at] = __float2bfloat16_rn(v);
+#pragma unroll
+    for (int q = 0; q < MANY; ++q)
+      if (m + q * step < m1) ((__nv_bfloat16*)p.C)[at + q * far] = __float2bfloat16_rn(v[q]);
   }
 }
 
@@ -202,26 +214,27 @@ __global__ void __launch_bounds__(RowsCfg<NT>::THREADS, RowsCfg<NT>::OCC) linear
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
-      constexpr int CH = L::MINE < 32 ? 16 : 32, N = L::MINE / CH;
-      uint32_t v[N][CH];
-#pragma unroll
-      for (int c = 0; c < N; ++c) tmem_ld_issue(taddr + buf * NT + c * CH, v[c]);
-#pragma unroll
-      for (int c = 0; c < N; ++c) tmem_ld_wait(v[c]);
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&acc_empty[buf]));
+      constexpr int CH = L::MINE < 32 ? 16 : 32;
       const float* f = factor + slot * NT + col0;
 #pragma unroll
-      for (int c = 0; c < N; ++c)
+      for (int c = 0; c < L::MINE; c += CH) {
+        uint32_t v[CH];
+        tmem_ld_issue(taddr + buf * NT + c, v);
+        tmem_ld_wait(v);
+        if (c + CH == L::MINE) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&acc_empty[buf]));
+        }
 #pragma unroll
         for (int j = 0; j < CH; j += 4) {
-          const float4 q = *reinterpret_cast<const float4*>(f + c * CH + j);
-          acc[c * CH + j] = fmaf(__uint_as_float(v[c][j]), q.x, acc[c * CH + j]);
-          acc[c * CH + j + 1] = fmaf(__uint_as_float(v[c][j + 1]), q.y, acc[c * CH + j + 1]);
-          acc[c * CH + j + 2] = fmaf(__uint_as_float(v[c][j + 2]), q.z, acc[c * CH + j + 2]);
-          acc[c * CH + j + 3] = fmaf(__uint_as_float(v[c][j + 3]), q.w, acc[c * CH + j + 3]);
+          const float4 q = *reinterpret_cast<const float4*>(f + c + j);
+          acc[c + j] = fmaf(__uint_as_float(v[j]), q.x, acc[c + j]);
+          acc[c + j + 1] = fmaf(__uint_as_float(v[j + 1]), q.y, acc[c + j + 1]);
+          acc[c + j + 2] = fmaf(__uint_as_float(v[j + 2]), q.z, acc[c + j + 2]);
+          acc[c + j + 3] = fmaf(__uint_as_float(v[j + 3]), q.w, acc[c + j + 3]);
         }
+      }
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&fac_empty[slot]));
     }
@@ -245,8 +258,7 @@ __global__ void __launch_bounds__(RowsCfg<NT>::THREADS, RowsCfg<NT>::OCC) linear
   if (split == 1) {
     if (warp >= 4 && n < p.N) {
 #pragma unroll
-      for (int j = 0; j < L::MINE; ++j)
-        if (col0 + j < tokens) store_one(p, (int64_t)(m0 + col0 + j) * p.N + n, acc[j]);
+      for (int j = 0; j < L::MINE; j += 16) store_many<16>(p, n, m0 + col0 + j, 1, m0 + tokens, acc + j);
     }
     return;
   }
@@ -272,11 +284,7 @@ __global__ void __launch_bounds__(RowsCfg<NT>::THREADS, RowsCfg<NT>::OCC) linear
 #pragma unroll
         for (int q = 0; q < MANY; ++q) v[q] += from[min(j0 + q * TEAMS, NT - 1) * 128];
       }
-      if (n < p.N) {
-#pragma unroll
-        for (int q = 0; q < MANY; ++q)
-          if (j0 + q * TEAMS < j1) store_one(p, (int64_t)(m0 + j0 + q * TEAMS) * p.N + n, v[q]);
-      }
+      if (n < p.N) store_many<MANY>(p, n, m0 + j0, TEAMS, m0 + j1, v);
     }
   }
   cl.sync();                                                            // nobody leaves while its sums are being read

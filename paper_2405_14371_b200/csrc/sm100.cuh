@@ -69,7 +69,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
 // wait that is not over at once) is left alone for the first 255 looks.
 __device__ __forceinline__ bool mbar_wait_soon(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
   uint64_t t0 = 0;
-  for (uint32_t looks = 1; !mbar_test(bar, parity); ++looks) {
+  for (uint32_t looks = 1; !mbar_try_wait(bar, parity); ++looks) {
     if ((looks & 255u) != 0) continue;
     if (*abort_flag) return false;
     const uint64_t now = global_timer_ns();
