@@ -549,16 +549,18 @@ es_status_t launch_pair(const Fp8Maps& maps, const Fp8Params& p, cudaStream_t s)
   return ES_OK;
 }
 
-// Clusters of 1 to 8 CTAs that the device holds at a time (fewer than its SMs' places divided by the size: a cluster lies in one
-// part of the device, and the parts differ).
-template <int NT>
+// Clusters of `split` CTAs that the device holds with a CTA on each SM, asked of the form that fits an SM once.  (Fewer than the
+// SMs divided by the size: a cluster lies in one part of the device, and the parts differ.)
 es_status_t places_of(int split, int* places) {
-  using L = RowsCfg<NT>;
+  using L = RowsCfg<128>;
+  static_assert(L::OCC == 1, "one CTA an SM");
   static std::atomic<int> known[64][9];
+  static std::atomic<uint64_t> allowed{0};
   int dev = 0;
   ES_CUDA_CHECK(cudaGetDevice(&dev));
   std::atomic<int>* at = dev < 64 ? &known[dev][split] : nullptr;
   if (at && (*places = at->load(std::memory_order_relaxed)) > 0) return ES_OK;
+  ES_CUDA_CHECK(allow_shared_memory(linear_fp8_rows_kernel<128>, (int)L::SMEM, &allowed));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(split);
   cfg.blockDim = dim3(L::THREADS);
@@ -570,14 +572,15 @@ es_status_t places_of(int split, int* places) {
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   int n = 0;
-  ES_CUDA_CHECK(cudaOccupancyMaxActiveClusters(&n, linear_fp8_rows_kernel<NT>, &cfg));
+  ES_CUDA_CHECK(cudaOccupancyMaxActiveClusters(&n, linear_fp8_rows_kernel<128>, &cfg));
   *places = n > 0 ? n : 1;
   if (at) at->store(*places, std::memory_order_relaxed);
   return ES_OK;
 }
 
 // CTAs that share a tile's K range: as many as make the time of the waves shortest, counted in blocks; starting and joining
-// cost about 4 of them.
+// cost about 4 of them.  Measured for 1, 2, 3, 4 CTAs: 1 x 12288 x 4096 15.2 / 12.7 / 17.9 / 16.1 us (2 taken: 3 no longer fit in
+// one wave), 16 x 10240 x 8192 28.5 / 18.7 / 18.0 / 25.6 (3), 113 x 5120 x 13824 74.6 / 43.4 / 32.5 / 49.7 (3).
 template <int NT>
 es_status_t rows_auto(const Fp8Maps& maps, const Fp8Params& p, cudaStream_t s) {
   static std::atomic<uint64_t> allowed{0};
@@ -587,7 +590,8 @@ es_status_t rows_auto(const Fp8Maps& maps, const Fp8Params& p, cudaStream_t s) {
   long long least = 0;
   for (int split = 1; split <= 8 && split <= p.nkb; ++split) {
     int places = 0;
-    ES_TRY(places_of<NT>(split, &places));
+    ES_TRY(places_of(split, &places));
+    places *= RowsCfg<NT>::OCC;
     const long long cost = ((tiles + places - 1) / places) * ((p.nkb + split - 1) / split + 4);
     if (split == 1 || cost < least) { best = split; least = cost; }
   }
