@@ -502,7 +502,7 @@ ES_API es_status_t es_op_linear_fp8(const void *a, const float *a_scale, const v
 
 /* Norm of every query and key head, rotation by the position, and the keys' and values' way into the cache.
  *   q [n, Hq, hd], k, v [n, Hkv, hd] (fp16 or bf16), token r at + r * its stride elements (heads contiguous; strides % 8
- *   == 0, 16-byte aligned: slices of a fused QKV product serve); v may be NULL, with v_out;  hd 64, 128 or 256;
+ *   == 0, 16-byte aligned: slices of a fused QKV product serve); v may be NULL, with v_out;  hd 64, 128 or 256;  Hq, Hkv <= 2^14;
  *   q_gain, k_gain [hd] (fp16, bf16 or fp32): x = x / sqrt(mean over the head of x^2 + eps) * gain; NULL: no norm;
  *   cosines, sines fp32 [max_pos, rot / 2]: the first rot values of a head are rotated, pairs (2i, 2i + 1), or
  *   (i, i + rot / 2) with halves != 0;  rot % 16 == 0, 0 <= rot <= hd;  positions int32 [n];

@@ -13,6 +13,7 @@
 
 #include "es_internal.cuh"
 #include "launch.cuh"
+#include "sm100.cuh"
 
 namespace es {
 namespace {
@@ -62,17 +63,16 @@ __device__ __forceinline__ void load_gain(const void* g, int dtype, int at, floa
 
 constexpr int WARPS = 8;
 
-// PER_WARP groups of heads for each warp, all of one kind (query, key or value).
-template <typename T, int HD, bool HALVES, int PER_WARP>
+// A warp has one token and PER_WARP groups of heads of one kind (query, key or value); the warps of a CTA have consecutive tokens.
+// FULL: every value of a head is rotated.
+template <typename T, int HD, bool HALVES, bool FULL, int PER_WARP>
 __global__ void __launch_bounds__(WARPS * 32) qk_norm_rope_kernel(const HeadsParams p) {
   constexpr int LANES = HD / 8, PER = 32 / LANES, CHUNK = PER * PER_WARP;      // lanes of a head, heads at a time, heads of a warp
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, part = lane % LANES, sub = lane / LANES;
   const int q_tasks = (p.Hq + CHUNK - 1) / CHUNK, k_tasks = (p.Hkv + CHUNK - 1) / CHUNK;
-  const int tasks = q_tasks + k_tasks * (p.v ? 2 : 1);       // warps of a token
-  const int64_t warp = (int64_t)blockIdx.x * WARPS + (threadIdx.x >> 5);
-  const int64_t token = warp / tasks;
-  int task = (int)(warp - token * tasks);
+  const int64_t token = (int64_t)blockIdx.x * WARPS + (threadIdx.x >> 5);
+  int task = blockIdx.y;
   const int kind = task < q_tasks ? 0 : task < q_tasks + k_tasks ? 1 : 2;
   task -= kind == 0 ? 0 : kind == 1 ? q_tasks : q_tasks + k_tasks;
   const int heads = kind == 0 ? p.Hq : p.Hkv, h0 = task * CHUNK + sub, d0 = part * 8;
@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(WARPS * 32) qk_norm_rope_kernel(const HeadsPar
   // factors of this lane's values: y' = r * (x * own + partner's x * other), gains and rotation in one
   const void* gain = kind == 0 ? p.q_gain : p.k_gain;
   const int half = p.rot >> 1;
-  const bool turned = d0 < p.rot, first = d0 < half;
+  const bool turned = FULL || d0 < p.rot, first = d0 < half;
   float own[8], other[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) { own[j] = 1.f; other[j] = 0.f; }
@@ -148,29 +148,40 @@ __global__ void __launch_bounds__(WARPS * 32) qk_norm_rope_kernel(const HeadsPar
     }
   }
 
+  uint64_t own2[4], other2[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) { own2[j] = pack_f32x2(own[2 * j], own[2 * j + 1]); other2[j] = pack_f32x2(other[2 * j], other[2 * j + 1]); }
 #pragma unroll
   for (int i = 0; i < PER_WARP; ++i) {
     const int h = h0 + i * PER;
     const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-    uint32_t z[4];
-    float r = 1.f;
     float2 y[4];
+    uint64_t y2[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) y[j] = Pair<T>::get(w[j]);
+    for (int j = 0; j < 4; ++j) { y[j] = Pair<T>::get(w[j]); y2[j] = pack_f32x2(y[j].x, y[j].y); }
+    float r = 1.f;
     if (gain) {
-      float sum = 0.f;
+      uint64_t sum2 = mul_f32x2(y2[0], y2[0]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) sum = fmaf(y[j].x, y[j].x, fmaf(y[j].y, y[j].y, sum));
+      for (int j = 1; j < 4; ++j) sum2 = fma_f32x2(y2[j], y2[j], sum2);
+      const float2 both = unpack_f32x2(sum2);
+      float sum = both.x + both.y;
 #pragma unroll
       for (int o = LANES / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
       r = rsqrtf(sum * (1.0f / HD) + p.eps);
     }
+    const uint64_t r2 = pack_f32x2(r, r);
+    uint32_t z[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float2 m = HALVES ? Pair<T>::get(__shfl_sync(0xffffffffu, w[j], from)) : make_float2(y[j].y, y[j].x);
+      float2 m = make_float2(y[j].y, y[j].x);
+      if (HALVES) m = Pair<T>::get(__shfl_sync(0xffffffffu, w[j], from));
       // a value without a partner takes nothing of the one that stands there, whatever it is
-      const float a = y[j].x * own[2 * j], b = y[j].y * own[2 * j + 1];
-      z[j] = turned ? Pair<T>::put(r * fmaf(m.x, other[2 * j], a), r * fmaf(m.y, other[2 * j + 1], b)) : Pair<T>::put(r * a, r * b);
+      uint64_t v = mul_f32x2(y2[j], own2[j]);
+      if (FULL) v = fma_f32x2(pack_f32x2(m.x, m.y), other2[j], v);
+      else if (turned) v = fma_f32x2(pack_f32x2(m.x, m.y), other2[j], v);
+      const float2 t = unpack_f32x2(mul_f32x2(v, r2));
+      z[j] = Pair<T>::put(t.x, t.y);
     }
     if (h < heads) *reinterpret_cast<uint4*>(out + h * step) = make_uint4(z[0], z[1], z[2], z[3]);
   }
@@ -179,10 +190,11 @@ __global__ void __launch_bounds__(WARPS * 32) qk_norm_rope_kernel(const HeadsPar
 template <typename T, int HD, bool HALVES, int PER_WARP>
 es_status_t launch_per(const HeadsParams& p, cudaStream_t s) {
   constexpr int CHUNK = 32 / (HD / 8) * PER_WARP;
-  const long long tasks = (p.Hq + CHUNK - 1) / CHUNK + (p.Hkv + CHUNK - 1) / CHUNK * (p.v ? 2 : 1);
-  const long long ctas = (p.n * tasks + WARPS - 1) / WARPS;
-  if (ctas > INT32_MAX) return fail(ES_ERR_RANGE, "n * heads exceeds one launch");
-  ES_CUDA_CHECK(launch_kernel(qk_norm_rope_kernel<T, HD, HALVES, PER_WARP>, dim3((unsigned)ctas), dim3(WARPS * 32), 0, s, tunables().pdl != 0, p));
+  const int tasks = (p.Hq + CHUNK - 1) / CHUNK + (p.Hkv + CHUNK - 1) / CHUNK * (p.v ? 2 : 1);
+  const dim3 grid((unsigned)((p.n - 1) / WARPS + 1), (unsigned)tasks);
+  const bool pdl = tunables().pdl != 0;
+  if (p.rot == HD) ES_CUDA_CHECK(launch_kernel(qk_norm_rope_kernel<T, HD, HALVES, true, PER_WARP>, grid, dim3(WARPS * 32), 0, s, pdl, p));
+  else ES_CUDA_CHECK(launch_kernel(qk_norm_rope_kernel<T, HD, HALVES, false, PER_WARP>, grid, dim3(WARPS * 32), 0, s, pdl, p));
   return ES_OK;
 }
 
@@ -225,7 +237,7 @@ extern "C" es_status_t es_op_qk_norm_rope(const void* q, int64_t q_stride, const
   if (dtype != ES_DTYPE_F16 && dtype != ES_DTYPE_BF16) return fail(ES_ERR_INVALID_ARG, "q, k and v must be fp16 or bf16");
   if (gain_dtype != ES_DTYPE_F16 && gain_dtype != ES_DTYPE_BF16 && gain_dtype != ES_DTYPE_F32) return fail(ES_ERR_INVALID_ARG, "gains must be fp16, bf16 or fp32");
   if (!(eps >= 0.f)) return fail(ES_ERR_INVALID_ARG, "eps must not be negative");
-  if (Hq > (1 << 16) || Hkv > (1 << 16)) return fail(ES_ERR_RANGE, "more than 2^16 heads");
+  if (Hq > (1 << 14) || Hkv > (1 << 14)) return fail(ES_ERR_RANGE, "more than 2^14 heads");
   if (slot_map) {
     if (page_tokens < 16 || (page_tokens & (page_tokens - 1))) return fail(ES_ERR_SHAPE, "page_tokens must be a power of two, at least 16");
     if (n_pages <= 0) return fail(ES_ERR_INVALID_ARG, "bad sizes");
