@@ -364,19 +364,21 @@ __device__ __forceinline__ void store_tile(const Fp8Params& p, unsigned char* tu
         }
       }
     } else {
-      // ragged or unaligned rows: a column a lane
-      for (int r = 0; r < 32 && row0 + r < p.M; ++r) {
+      // ragged or unaligned rows: a column a lane, eight rows under way at a time
+#pragma unroll 8
+      for (int r = 0; r < 32; ++r) {
 #pragma unroll
         for (int i = 0; i < CH / 32; ++i) {
           const int col = lane + 32 * i;
-          if (n + c + col >= p.N) continue;
           const int64_t at = (int64_t)(row0 + r) * p.N + n + c + col;
+          const bool here = row0 + r < p.M && n + c + col < p.N;
           if (WIDE) {
             float v = *reinterpret_cast<const float*>(turn + r * 128 + (((col >> 2) ^ (r & 7)) << 4) + (col & 3) * 4);
-            if (p.R) v += p.R[at];
-            ((float*)p.C)[at] = v;
+            if (here && p.R) v += p.R[at];
+            if (here) ((float*)p.C)[at] = v;
           } else {
-            ((uint16_t*)p.C)[at] = *reinterpret_cast<const uint16_t*>(turn + r * 128 + (((col >> 3) ^ (r & 7)) << 4) + (col & 7) * 2);
+            const uint16_t v = *reinterpret_cast<const uint16_t*>(turn + r * 128 + (((col >> 3) ^ (r & 7)) << 4) + (col & 7) * 2);
+            if (here) ((uint16_t*)p.C)[at] = v;
           }
         }
       }
@@ -579,23 +581,46 @@ es_status_t places_of(int split, int* places) {
 }
 
 // CTAs that share a tile's K range: as many as make the time of the waves shortest, counted in blocks; starting and joining
-// cost about 4 of them.  Measured for 1, 2, 3, 4 CTAs: 1 x 12288 x 4096 15.2 / 12.7 / 17.9 / 16.1 us (2 taken: 3 no longer fit in
+// cost about 4 of them (8 with 128 tokens: their sums take longer to join).  Measured for 1, 2, 3, 4 CTAs: 1 x 12288 x 4096 15.2 / 12.7 / 17.9 / 16.1 us (2 taken: 3 no longer fit in
 // one wave), 16 x 10240 x 8192 28.5 / 18.7 / 18.0 / 25.6 (3), 113 x 5120 x 13824 74.6 / 43.4 / 32.5 / 49.7 (3).
+template <int NT>
+es_status_t rows_split(const Fp8Params& p, int* split, long long* blocks) {
+  const long long tiles = (long long)((p.N + 127) / 128) * ((p.M + NT - 1) / NT);
+  *blocks = 0;
+  for (int s = 1; s <= 8 && s <= p.nkb; ++s) {
+    int places = 0;
+    ES_TRY(places_of(s, &places));
+    places *= RowsCfg<NT>::OCC;
+    const long long cost = ((tiles + places - 1) / places) * ((p.nkb + s - 1) / s + (RowsCfg<NT>::OCC == 1 ? 8 : 4));
+    if (s == 1 || cost < *blocks) { *split = s; *blocks = cost; }
+  }
+  return ES_OK;
+}
+
 template <int NT>
 es_status_t rows_auto(const Fp8Maps& maps, const Fp8Params& p, cudaStream_t s) {
   static std::atomic<uint64_t> allowed{0};
   ES_CUDA_CHECK(allow_shared_memory(linear_fp8_rows_kernel<NT>, (int)RowsCfg<NT>::SMEM, &allowed));
-  const long long tiles = (long long)((p.N + 127) / 128) * ((p.M + NT - 1) / NT);
-  int best = 1;
-  long long least = 0;
-  for (int split = 1; split <= 8 && split <= p.nkb; ++split) {
-    int places = 0;
-    ES_TRY(places_of(split, &places));
-    places *= RowsCfg<NT>::OCC;
-    const long long cost = ((tiles + places - 1) / places) * ((p.nkb + split - 1) / split + 4);
-    if (split == 1 || cost < least) { best = split; least = cost; }
-  }
-  return launch_rows<NT>(maps, p, best, s);
+  int split = 1;
+  long long blocks = 0;
+  ES_TRY(rows_split<NT>(p, &split, &blocks));
+  return launch_rows<NT>(maps, p, split, s);
+}
+
+// The kernel for more than 64 tokens: the one whose waves take fewer blocks, a block of a pair's tile costing 7 / 8 of one of a
+// single CTA's (0.55 and 0.62 us), its start and its stores 5.  Measured, us with tiles of 128 weight rows / on pairs:
+// 129 x 4096 x 4096 16.5 / 21.3, 320 x 4096 x 4096 24.8 / 21.4, 100 x 11008 x 4096 29.0 / 22.3, 512 x 5003 x 2064 37.9 / 18.1,
+// 1024 x 4096 x 4096 48.9 / 22.1, 256 x 28672 x 8192 187 / 79; up to 64 tokens the first is ahead everywhere (64 x 28672 x 8192
+// 65 / 78).
+es_status_t pairs_better(const Fp8Params& p, bool* pairs) {
+  *pairs = false;
+  if (p.M <= 64) return ES_OK;
+  int split = 1;
+  long long blocks = 0;
+  ES_TRY(rows_split<128>(p, &split, &blocks));
+  const long long tiles = (long long)((p.M + 255) / 256) * ((p.N + 255) / 256), n_pairs = sm_count() / 2 > 0 ? sm_count() / 2 : 1;
+  *pairs = (tiles + n_pairs - 1) / n_pairs * p.nkb * 7 + 5 * 8 < blocks * 8;
+  return ES_OK;
 }
 
 }  // namespace
@@ -617,10 +642,10 @@ extern "C" es_status_t es_op_linear_fp8(const void* a, const float* a_scale, con
   if (((uintptr_t)a | (uintptr_t)w) % 16 || ((uintptr_t)a_scale | (uintptr_t)w_scale | (uintptr_t)R) % 4 || (uintptr_t)C % esize)
     return fail(ES_ERR_INVALID_ARG, "a and w must be 16-byte aligned, the others by their elements");
   if (!tma_available()) return fail(ES_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
-  // 256 x 256 tiles from the size on at which they are as good as full (below, more and smaller tiles on single CTAs)
-  const bool pairs = path == 2 || (path == 0 && M > 128 && (long long)((M + 255) / 256) * ((N + 255) / 256) * 2 >= sm_count());
   const int NT = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
   Fp8Params p{a_scale, w_scale, R, C, M, N, (K + FP8_BLOCK - 1) / FP8_BLOCK, out_dtype, weights_ready != 0, 0};
+  bool pairs = path == 2;
+  if (path == 0) ES_TRY(pairs_better(p, &pairs));
   p.vec = ((size_t)N * esize) % 16 == 0 && ((uintptr_t)C | (uintptr_t)R) % 16 == 0;
   Fp8Maps maps;
   // two codes make one 16-bit element of the map: boxes of 64 elements are 128 bytes
