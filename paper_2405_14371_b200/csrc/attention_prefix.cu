@@ -73,7 +73,10 @@ __device__ __forceinline__ int tiles_of(int len) { return (len + KT - 1) / KT; }
 // CTAs that share the line of `units` places, and which has which
 __device__ __forceinline__ int active(int units, int ctas) { return max(1, min(ctas, units / MIN_UNITS)); }
 __device__ __forceinline__ int start_of(int cta, int units, int n) { return (int)((long long)units * cta / n); }
-__device__ __forceinline__ int cta_of(int unit, int units, int n) { return (int)(((long long)(unit + 1) * n - 1) / units); }
+__device__ __forceinline__ int cta_of(int unit, int units, int n) {
+  // below 2^39 over below 2^30: a double's quotient is off by less than its distance from the next whole number
+  return (int)(((double)(unit + 1) * n - 1.0) / (double)units);
+}
 
 // The pieces of a stretch, one after the other.  Only the first is searched for.
 struct Walk {
@@ -238,9 +241,11 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
   __syncthreads();
   {
     int all, sum = 0;
-    if (p.groups) {
+    const int to = p.groups ? min(s0 + per, p.groups + 1) : 0;
+    bool disorder = false;
+    for (int s = max(s0, 1); s < to; ++s) disorder |= first[s] < first[s - 1];
+    if (__syncthreads_or(disorder)) {
       // a group begins no earlier than those before it end
-      const int to = min(s0 + per, p.groups + 1);
       int top = 0;
       for (int s = s0; s < to; ++s) top = max(top, first[s]);
       top = block_scan(top, totals, &all, [](int a, int b) { return max(a, b); });
@@ -566,10 +571,10 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) prefix_join_kernel(const Pref
   pdl_launch_dependents();
   constexpr int D = HD / 32;                                   // values of a lane
   const int lane = threadIdx.x & 31;
-  const int64_t at = (int64_t)blockIdx.x * JOIN_WARPS + (threadIdx.x >> 5);
+  const unsigned at = blockIdx.x * JOIN_WARPS + (threadIdx.x >> 5);             // below 2^26 + 4
+  const int token = (int)(at / (unsigned)p.Hq), h = (int)(at - (unsigned)token * p.Hq), kvh = h / p.G, g = h - kvh * p.G, b = token / p.T;
   pdl_wait();
-  if (at >= (int64_t)p.B * p.T * p.Hq) return;
-  const int token = (int)(at / p.Hq), h = (int)(at % p.Hq), kvh = h / p.G, g = h - kvh * p.G, b = token / p.T;
+  if (b >= p.B) return;
   const int4 shared = p.records[2 * b], mine = p.records[2 * b + 1];
   const int units = mine.z, n = active(units, ctas);
   float top = -INFINITY, sum = 0.f, o[D];
@@ -621,7 +626,7 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) prefix_join_kernel(const Pref
     }
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  uint16_t* out = (uint16_t*)p.out + at * HD + lane * D;
+  uint16_t* out = (uint16_t*)p.out + (int64_t)at * HD + lane * D;
   uint32_t w[D / 2];
 #pragma unroll
   for (int i = 0; i < D; i += 2) {
