@@ -535,7 +535,7 @@ ES_API es_status_t es_op_qk_norm_rope(const void *q, int64_t q_stride, const voi
  * probabilities enter the product with V in q's type.  Table entries outside [0, n_pages) are pages that nobody sees;
  * lengths above max_prefix (<= prefix_pages * page_tokens) or max_ctx (<= pages_per_seq * page_tokens) are read as those.
  *   hd 64 or 128;  Hq a multiple of Hkv, at most 128 times as many;  groups + B <= 8192;  B * T * Hq <= 2^26;  n_pages *
- *   Hkv * page_tokens < 2^31 - 256;  Hkv * (tiles of 64 keys, of each sequence and of each prefix for every 128 rows) <= 2^30.
+ *   Hkv * page_tokens < 2^31 - 256;  Hkv * (tiles of 64 keys and 2 more, of each sequence and of each prefix for every 128 rows) <= 2^30.
  *   scratch: dev, 16-byte aligned, es_op_decode_attention_prefix_scratch_bytes(...) bytes of the call's sizes on the current
  *   device, in use until the call's work is done (calls that overlap on the GPU need one each).  Uninitialised is fine.
  * Should a wait inside the kernel run out (after a second), the rows it was for become NaN. */
