@@ -488,7 +488,8 @@ ES_API es_status_t es_op_quant_e4m3(const void *x, int32_t dtype, int64_t row_st
 
 /* es_op_linear of such operands: C[m, n] = sum over blocks b of a_scale[b, m] * w_scale[n / 128, b] *
  * sum over k in b of a[m, k] * w[n, k]   (+ R[m, n]); blocks are added in ascending order, in fp32 (few rows: in up to
- * 8 ranges of blocks, then range by range; the order depends on the sizes and the device's SM count alone).
+ * 8 ranges of blocks, then range by range; the order depends on the sizes and the device alone).  The product of two
+ * scales is formed in fp32 and must be finite there.
  *   a codes [M, K], a_scale fp32 [ceil(K / 128), M];  w codes [N, K], w_scale fp32 [ceil(N / 128), ceil(K / 128)];
  *   C [M, N], dense, fp16, bf16 or fp32;  R fp32 [M, N] or NULL, only with an fp32 C, may be C itself;
  *   a, w 16-byte aligned;  K % 16 == 0;  M <= 262140, N <= 2^24.

@@ -132,6 +132,14 @@ at::Tensor empty(at::IntArrayRef shape, at::ScalarType dtype, const at::Tensor& 
   return at::empty(shape, at::TensorOptions().dtype(dtype).device(like.device()));
 }
 
+// A dense tensor of another type inside a buffer of bytes, `offset` bytes from its start: two results, one allocation.
+at::Tensor within(const at::Tensor& bytes, at::IntArrayRef shape, at::ScalarType dtype, int64_t offset) {
+  auto impl = c10::make_intrusive<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(bytes.storage()), bytes.key_set(), c10::scalarTypeToTypeMeta(dtype));
+  impl->set_storage_offset(offset / (int64_t)c10::elementSize(dtype));
+  impl->set_sizes_contiguous(shape);
+  return at::Tensor(std::move(impl));
+}
+
 // The call itself, other Python threads running meanwhile.
 template <class F>
 void call(F f) {
@@ -354,8 +362,10 @@ PyObject* quant_e4m3(PyObject* const* a) {
   const int64_t s0 = block_rows == 1 ? blocks : ((int64_t)M + 127) / 128, s1 = block_rows == 1 ? M : blocks;
   at::Tensor codes, scale;
   if (a[2] == Py_None) {
-    codes = empty({M, K}, at::kFloat8_e4m3fn, x);
-    scale = empty({s0, s1}, at::kFloat, x);
+    const int64_t front = ((int64_t)M * K + 15) / 16 * 16;
+    const at::Tensor both = empty({front + s0 * s1 * 4}, at::kByte, x);
+    codes = within(both, {M, K}, at::kFloat8_e4m3fn, 0);
+    scale = within(both, {s0, s1}, at::kFloat, front);
   } else {
     if (!PyTuple_Check(a[2]) || PyTuple_GET_SIZE(a[2]) != 2) refuse("out must be two tensors");
     codes = tensor(PyTuple_GET_ITEM(a[2], 0), "out[0]");
