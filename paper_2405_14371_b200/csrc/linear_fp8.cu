@@ -386,7 +386,15 @@ __device__ __forceinline__ void store_tile(const Fp8Params& p, unsigned char* tu
   }
 }
 
-__global__ void __launch_bounds__(P_THREADS, 1) linear_fp8_pair_kernel(const __grid_constant__ Fp8Maps maps, const Fp8Params p, const int m_tiles, const int n_tiles) {
+// split > 1: a cluster of 2 or 4 pairs shares one tile's K range; their sums meet in distributed shared memory, where each pair
+// adds up and stores its share of the columns, in order of the ranges.
+constexpr int P_PITCH = 260;                                            // floats of a row of sums: 16-byte writes of 32 rows without bank conflicts
+static_assert(128 * P_PITCH * 4 <= P_STAGES * P_STAGE, "the sums go where the ring was");
+
+template <bool SPLIT>
+__global__ void __launch_bounds__(P_THREADS, 1) linear_fp8_pair_kernel(const __grid_constant__ Fp8Maps maps, const Fp8Params p, const int m_tiles, const int n_tiles,
+                                                                       const int pairs_of_tile) {
+  const int split = SPLIT ? pairs_of_tile : 1;
   pdl_launch_dependents();
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -398,9 +406,12 @@ __global__ void __launch_bounds__(P_THREADS, 1) linear_fp8_pair_kernel(const __g
   volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t rank = cluster_ctarank();
-  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  const uint32_t rank = cluster_ctarank() & 1;
+  const int ks = SPLIT ? (int)(cluster_ctarank() >> 1) : 0;             // range of K
+  const uint16_t both = (uint16_t)(3u << (2 * ks));                     // this pair in the cluster
+  const int pair = (int)blockIdx.x / (2 * split), n_pairs = (int)gridDim.x / (2 * split);
   const int tiles = m_tiles * n_tiles;
+  const int b0 = (int)((long long)p.nkb * ks / split), b1 = (int)((long long)p.nkb * (ks + 1) / split);
 
   // 16 row tiles share a column tile: what a wave of pairs reads then fits in L2
   auto origin = [&](int tile, int& m0, int& n0) {
@@ -436,7 +447,7 @@ __global__ void __launch_bounds__(P_THREADS, 1) linear_fp8_pair_kernel(const __g
       for (int tile = pair; tile < tiles && ok; tile += n_pairs) {
         int m0, n0;
         origin(tile, m0, n0);
-        for (int b = 0; b < p.nkb; ++b, ++it) {
+        for (int b = b0; b < b1; ++b, ++it) {
           const int s = it % P_STAGES;
           if (!mbar_wait_soon(smem_u32(&empty[s]), ((it / P_STAGES) & 1) ^ 1, abort_flag)) { ok = false; break; }
           const uint32_t fb = smem_u32(&full[s]), dst = smem_u32(ring + s * P_STAGE);
@@ -451,14 +462,14 @@ __global__ void __launch_bounds__(P_THREADS, 1) linear_fp8_pair_kernel(const __g
       constexpr uint32_t idesc = umma_idesc_f16(256, 256);
       const uint64_t a0 = umma_desc_sw128(smem_u32(ring)), w0 = umma_desc_sw128(smem_u32(ring) + W_TILE);
       const uint32_t full0 = smem_u32(full), empty0 = smem_u32(empty), acc_full0 = smem_u32(acc_full), acc_empty0 = smem_u32(acc_empty);
-      int left = pair < tiles ? ((tiles - 1 - pair) / n_pairs + 1) * p.nkb : 0;
+      int left = pair < tiles ? ((tiles - 1 - pair) / n_pairs + 1) * (b1 - b0) : 0;
       uint32_t s = 0, ring_phase = 0, buf = 0, buf_phase = 1;
       for (; left > 0; --left) {
         if (!mbar_wait_soon(full0 + s * 8, ring_phase, abort_flag) || !mbar_wait_soon(acc_empty0 + buf * 8, buf_phase, abort_flag)) break;
         tc_fence_after();
         umma_f8_block_pair(tmem + buf * 256, a0 + s * (P_STAGE >> 4), w0 + s * (P_STAGE >> 4), idesc);
-        umma_commit_pair(acc_full0 + buf * 8);
-        umma_commit_pair(empty0 + s * 8);
+        umma_commit_pair(acc_full0 + buf * 8, both);
+        umma_commit_pair(empty0 + s * 8, both);
         if (++s == P_STAGES) { s = 0; ring_phase ^= 1; }
         buf ^= 1;
         if (buf == 0) buf_phase ^= 1;
@@ -483,18 +494,18 @@ __global__ void __launch_bounds__(P_THREADS, 1) linear_fp8_pair_kernel(const __g
       // Factors are fetched four blocks at a time, the next four while these are used: one at a time, every block waited for
       // its load (8192 x 28672 x 8192 2.1 ms).
       float sa[4], sw[4], fac[4];
-      auto fetch = [&](int b0) {
+      auto fetch = [&](int b) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const bool have = in && b0 + q < p.nkb;
-          sa[q] = have ? as[(int64_t)(b0 + q) * p.M] : 0.f;
-          sw[q] = have ? ws[b0 + q] : 0.f;
+          const bool have = in && b + q < b1;
+          sa[q] = have ? as[(int64_t)(b + q) * p.M] : 0.f;
+          sw[q] = have ? ws[b + q] : 0.f;
         }
       };
-      fetch(0);
-      for (int b = 0; b < p.nkb; ++b, ++it) {
+      fetch(b0);
+      for (int b = b0; b < b1; ++b, ++it) {
         const int buf = it & 1;
-        if ((b & 3) == 0) {
+        if (((b - b0) & 3) == 0) {
 #pragma unroll
           for (int q = 0; q < 4; ++q) fac[q] = sa[q] * sw[q];
           fetch(b + 4);
@@ -525,8 +536,60 @@ __global__ void __launch_bounds__(P_THREADS, 1) linear_fp8_pair_kernel(const __g
 #pragma unroll
         for (int j = 0; j < 64; ++j) acc[j] = 0x7fffffff7fffffffull;
       }
-      if (p.out == ES_DTYPE_F32) store_tile<true>(p, my_turn, acc, row0, n, lane);
-      else store_tile<false>(p, my_turn, acc, row0, n, lane);
+      if (SPLIT) {
+        float* mine = (float*)ring + (quarter * 32 + lane) * P_PITCH + half * 128;
+#pragma unroll
+        for (int j = 0; j < 64; j += 2) {
+          const float2 u = unpack_f32x2(acc[j]), w = unpack_f32x2(acc[j + 1]);
+          *reinterpret_cast<float4*>(mine + 2 * j) = make_float4(u.x, u.y, w.x, w.y);
+        }
+      } else if (p.out == ES_DTYPE_F32) {
+        store_tile<true>(p, my_turn, acc, row0, n, lane);
+      } else {
+        store_tile<false>(p, my_turn, acc, row0, n, lane);
+      }
+    }
+  }
+  if (SPLIT) {
+    __syncwarp();
+    cluster_sync_all();
+    if (warp >= 4) {
+      cg::cluster_group cl = cg::this_cluster();
+      int m0, n0;
+      origin(pair, m0, n0);
+      const int lanes = 64 / split, e = (int)threadIdx.x - 128, c = ks * (256 / split) + e % lanes * 4, n = n0 + c;      // lanes of a row, first of four columns
+#pragma unroll 4
+      for (int r = e / lanes; r < 128; r += 32 * P_EPI / lanes) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          if (s >= split) break;
+          const float4 x = *reinterpret_cast<const float4*>(cl.map_shared_rank((float*)ring, 2 * s + (int)rank) + r * P_PITCH + c);
+          v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+        }
+        const int m = m0 + (int)rank * 128 + r;
+        if (m >= p.M || n >= p.N) continue;
+        const int64_t at = (int64_t)m * p.N + n;
+        if (p.vec) {                                                    // then n + 4 <= N
+          if (p.out == ES_DTYPE_F32) {
+            if (p.R) {
+              const float4 x = *reinterpret_cast<const float4*>(p.R + at);
+              v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+            }
+            *reinterpret_cast<float4*>((float*)p.C + at) = v;
+          } else {
+            *reinterpret_cast<uint2*>((uint16_t*)p.C + at) = make_uint2(two(v.x, v.y, p.out), two(v.z, v.w, p.out));
+          }
+        } else {
+          const float x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (n + i >= p.N) break;
+            if (p.out == ES_DTYPE_F32) ((float*)p.C)[at + i] = p.R ? x[i] + p.R[at + i] : x[i];
+            else ((uint16_t*)p.C)[at + i] = (uint16_t)two(x[i], 0.f, p.out);
+          }
+        }
+      }
     }
   }
 
@@ -541,14 +604,21 @@ __global__ void __launch_bounds__(P_THREADS, 1) linear_fp8_pair_kernel(const __g
   }
 }
 
-es_status_t launch_pair(const Fp8Maps& maps, const Fp8Params& p, cudaStream_t s) {
+template <bool SPLIT>
+es_status_t launch_pair_form(const Fp8Maps& maps, const Fp8Params& p, int split, cudaStream_t s) {
   static std::atomic<uint64_t> allowed{0};
-  ES_CUDA_CHECK(allow_shared_memory(linear_fp8_pair_kernel, (int)P_SMEM, &allowed));
+  auto kern = linear_fp8_pair_kernel<SPLIT>;
+  ES_CUDA_CHECK(allow_shared_memory(kern, (int)P_SMEM, &allowed));
   const int m_tiles = (p.M + 255) / 256, n_tiles = (p.N + 255) / 256;
-  int pairs = sm_count() / 2;
-  if (pairs > (long long)m_tiles * n_tiles) pairs = m_tiles * n_tiles;
-  ES_CUDA_CHECK(launch_clusters(linear_fp8_pair_kernel, 2, dim3(2 * pairs), dim3(P_THREADS), P_SMEM, s, tunables().pdl != 0, maps, p, m_tiles, n_tiles));
+  const long long tiles = (long long)m_tiles * n_tiles;
+  long long pairs = sm_count() / 2 > 0 ? sm_count() / 2 : 1;
+  if (SPLIT || pairs > tiles) pairs = tiles;
+  ES_CUDA_CHECK(launch_clusters(kern, 2 * split, dim3((unsigned)(2 * split * pairs)), dim3(P_THREADS), P_SMEM, s, tunables().pdl != 0, maps, p, m_tiles, n_tiles, split));
   return ES_OK;
+}
+
+es_status_t launch_pair(const Fp8Maps& maps, const Fp8Params& p, int split, cudaStream_t s) {
+  return split > 1 ? launch_pair_form<true>(maps, p, split, s) : launch_pair_form<false>(maps, p, 1, s);
 }
 
 // Clusters of `split` CTAs that the device holds with a CTA on each SM, asked of the form that fits an SM once.  (Fewer than the
@@ -607,19 +677,33 @@ es_status_t rows_auto(const Fp8Maps& maps, const Fp8Params& p, cudaStream_t s) {
   return launch_rows<NT>(maps, p, split, s);
 }
 
-// The kernel for more than 64 tokens: the one whose waves take fewer blocks, a block of a pair's tile costing 7 / 8 of one of a
-// single CTA's (0.55 and 0.62 us), its start and its stores 5.  Measured, us with tiles of 128 weight rows / on pairs:
-// 129 x 4096 x 4096 16.5 / 21.3, 320 x 4096 x 4096 24.8 / 21.4, 100 x 11008 x 4096 29.0 / 22.3, 512 x 5003 x 2064 37.9 / 18.1,
-// 1024 x 4096 x 4096 48.9 / 22.1, 256 x 28672 x 8192 187 / 79; up to 64 tokens the first is ahead everywhere (64 x 28672 x 8192
-// 65 / 78).
+// Pairs that share a tile's K range, and eighths of the blocks (of a single CTA's) that the rounds take: a block of a pair's tile
+// costs 7 / 8 of one of a single CTA's (0.55 and 0.62 us), start and stores 5, joining SPLIT_JOIN.
+constexpr int SPLIT_JOIN = 5;          // measured with two pairs a tile: 320 x 4096 x 4096 21.2 -> 19.1 us, 129 x 5003 x 2064 16.3 -> 16.5
+es_status_t pairs_split(const Fp8Params& p, int* split, long long* eighths) {
+  const long long tiles = (long long)((p.M + 255) / 256) * ((p.N + 255) / 256), n_pairs = sm_count() / 2 > 0 ? sm_count() / 2 : 1;
+  *split = 1;
+  *eighths = (tiles + n_pairs - 1) / n_pairs * p.nkb * 7 + 5 * 8;
+  for (int s = 2; s <= 4 && s <= p.nkb && tiles * s <= n_pairs; s *= 2) {
+    int places = 0;
+    ES_TRY(places_of(2 * s, &places));
+    const long long cost = (tiles + places - 1) / places * ((p.nkb + s - 1) / s) * 7 + (5 + SPLIT_JOIN) * 8;
+    if (cost < *eighths) { *split = s; *eighths = cost; }
+  }
+  return ES_OK;
+}
+
+// The kernel for more than 64 tokens: the one whose waves take fewer blocks.  Measured, us with tiles of 128 weight rows / on
+// pairs: 320 x 4096 x 4096 24.8 / 21.4, 100 x 11008 x 4096 29.0 / 22.3, 512 x 5003 x 2064 37.9 / 18.1, 1024 x 4096 x 4096
+// 48.9 / 22.1, 256 x 28672 x 8192 187 / 79; up to 64 tokens the first is ahead everywhere (64 x 28672 x 8192 65 / 78).
 es_status_t pairs_better(const Fp8Params& p, bool* pairs) {
   *pairs = false;
   if (p.M <= 64) return ES_OK;
   int split = 1;
-  long long blocks = 0;
+  long long blocks = 0, eighths = 0;
   ES_TRY(rows_split<128>(p, &split, &blocks));
-  const long long tiles = (long long)((p.M + 255) / 256) * ((p.N + 255) / 256), n_pairs = sm_count() / 2 > 0 ? sm_count() / 2 : 1;
-  *pairs = (tiles + n_pairs - 1) / n_pairs * p.nkb * 7 + 5 * 8 < blocks * 8;
+  ES_TRY(pairs_split(p, &split, &eighths));
+  *pairs = eighths < blocks * 8;
   return ES_OK;
 }
 
@@ -652,7 +736,12 @@ extern "C" es_status_t es_op_linear_fp8(const void* a, const float* a_scale, con
   ES_TRY(tma_encode_2d_f16(&maps.a, a, M, K / 2, K / 2, pairs ? 128 : NT));
   ES_TRY(tma_encode_2d_f16(&maps.w, w, N, K / 2, K / 2, 128));
   cudaStream_t s = (cudaStream_t)stream;
-  if (pairs) return launch_pair(maps, p, s);
+  if (pairs) {
+    int split = 1;
+    long long eighths = 0;
+    ES_TRY(pairs_split(p, &split, &eighths));
+    return launch_pair(maps, p, split, s);
+  }
   if (NT == 16) return rows_auto<16>(maps, p, s);
   if (NT == 32) return rows_auto<32>(maps, p, s);
   if (NT == 64) return rows_auto<64>(maps, p, s);

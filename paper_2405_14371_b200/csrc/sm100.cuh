@@ -386,6 +386,12 @@ __device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
                ::"r"(bar), "h"((unsigned short)3)
                : "memory");
 }
+// the same for the CTAs of `mask` in a cluster of several pairs
+__device__ __forceinline__ void umma_commit_pair(uint32_t bar, uint16_t mask) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+               ::"r"(bar), "h"(mask)
+               : "memory");
+}
 // arrive on the rank-0 CTA's copy of a barrier, from either CTA of the pair
 __device__ __forceinline__ void mbar_arrive_rank0(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar & kPeerBitMask) : "memory");
