@@ -199,7 +199,6 @@ __device__ __forceinline__ int block_scan(int v, int* totals, int* all, Join joi
 template <int HD, bool BF16>
 __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_constant__ PrefixMaps maps, const PrefixParams p) {
   using L = Smem<HD>;
-  pdl_launch_dependents();
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   unsigned char* q_s = smem;                                   // [halves][128 rows][128 B]
@@ -265,6 +264,7 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
   }
   tc_fence_before();
   __syncthreads();
+  pdl_launch_dependents();          // every CTA has its TMEM before a kernel behind this one can take any and then wait for this one's end
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot, tmem_s = tmem_base, tmem_o = tmem_base + 128;
   const int units = line[segments], ctas = active(units, (int)gridDim.x), cta = (int)blockIdx.x;
