@@ -533,7 +533,8 @@ ES_API es_status_t es_op_qk_norm_rope(const void *q, int64_t q_stride, const voi
  *   prefixes.
  * Query t sees the whole prefix and its sequence's own keys 0 .. ctx_len[b] - T + t, and nothing of the others reaches it,
  * infinities and NaN included; a query that sees none gives zeros.  Scale 1/sqrt(hd); scores, softmax and sums in fp32,
- * probabilities enter the product with V in q's type.  Table entries outside [0, n_pages) are pages that nobody sees;
+ * probabilities enter the product with V as two numbers of q's type (16 bits of bf16; 22 of fp16, good to 2^-32 of a query's
+ * largest), the result is rounded once.  Table entries outside [0, n_pages) are pages that nobody sees;
  * lengths above max_prefix (<= prefix_pages * page_tokens) or max_ctx (<= pages_per_seq * page_tokens) are read as those.
  *   hd 64 or 128;  Hq a multiple of Hkv, at most 128 times as many;  groups + B <= 8192;  B * T * Hq <= 2^26;  n_pages *
  *   Hkv * page_tokens < 2^31 - 256;  Hkv * (tiles of 64 keys and 2 more, of each sequence and of each prefix for every 128 rows) <= 2^30.

@@ -13,16 +13,19 @@
 //
 // Within a stretch, per tile:
 //   S = Q K^T      M = 128 rows, N = 64 keys, fp32 in TMEM, two buffers: the product of the next tile runs beside this softmax
-//   softmax        four warps, a row a thread: running maximum and sum in fp32; P in q's type goes into TMEM in place of S.
-//                  The sum is of the rounded P, so a row's weights still add up to one.  Warps without rows (a single
-//                  sequence has G) only keep the protocol.
-//   O += P V       P from TMEM; fp32 in TMEM, rescaled when a row's maximum has grown by more than 8 (log2), as P stays below 256
+//   softmax        four warps, a row a thread: running maximum and sum in fp32.  P goes into TMEM in place of S, as two numbers of
+//                  q's type (the rounded P and what that left, 16 and 22 bits: one alone is as coarse as the result, and its error
+//                  shows where the terms of a row cancel); the two fill exactly the columns that S had.  Warps without rows (a
+//                  single sequence has G) only keep the protocol.
+//   O += P V       P from TMEM; fp32 in TMEM, rescaled when a row's maximum has grown by more than 8 (log2).  P is below 256; fp16
+//                  has it 2^7 times as large (O and the sum too, so it cancels): good to 2^-32 of a row's largest weight.
 // K's place in the ring is free once S is complete, V's after P V; each has a warp that asks for the next.  The ring runs on
 // over the items' borders, and the next item's Q is fetched while the last tile of the one before is finished.
 //
 // Nothing of a key that a row does not see reaches it: scores are masked by selection, V rows behind the length are zeroed
 // in shared memory, pages that do not exist are read as zeros (a TMA box outside the tensor).  Of a draft's last tokens, which
-// only later rows see, infinities and NaN in V are taken out of the product and added to the rows that see them at the end.
+// only later rows see, infinities and NaN in V are taken out of the product and added to the rows that see them at the end.  A sum
+// that is no number, since either half of a weight may be zero or negative, is made anew from such values: see repair().
 //
 // Every wait is bounded by a second; the rows of a piece whose wait ran out become NaN.
 #include <cuda.h>
@@ -158,7 +161,7 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
       : "memory");
 }
 
-// Two probabilities rounded to q's type.
+// Two values rounded to q's type, and what that left of them.
 template <bool BF16>
 __device__ __forceinline__ uint32_t round_pair(float a, float b) {
   if (BF16) {
@@ -167,6 +170,40 @@ __device__ __forceinline__ uint32_t round_pair(float a, float b) {
   }
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+template <bool BF16>
+__device__ __forceinline__ uint32_t rest_pair(uint32_t w, float a, float b) {
+  const float x = BF16 ? add_lo_bf16(w, -a) : add_lo_f16(w, -a), y = BF16 ? add_hi_bf16(w, -b) : add_hi_f16(w, -b);
+  return round_pair<BF16>(-x, -y);
+}
+
+// The sums o of 32 columns, of keys k0 .. k1 - 1: infinities and NaN in V are added of the keys from `tail` on, which the product did
+// not get.  Columns that are no number (the weights are) are made anew over all of these keys: the values that are not finite
+// decide them alone; without one they stay what they are.  v: these columns of the KV head's first row in the pool.
+template <int HD, bool BF16>
+__device__ __noinline__ void repair(const int* pages, const uint16_t* v, int n_pages, int Hkv, int log2P, int k0, int k1, int tail, float* o) {
+  uint32_t unknown = 0, found = 0;
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    if (o[i] != o[i]) { unknown |= 1u << i; o[i] = 0.f; }
+  uint32_t open = unknown;                                     // not yet NaN for good
+  for (int key = k1 - 1; key >= k0 && (key >= tail || open); --key) {
+    const int page = pages[key >> log2P];
+    if ((unsigned)page >= (unsigned)n_pages) continue;
+    const uint16_t* at = v + ((((int64_t)page * Hkv) << log2P) + (key & ((1 << log2P) - 1))) * HD;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const float f = BF16 ? __uint_as_float((uint32_t)at[i] << 16) : __half2float(*reinterpret_cast<const __half*>(at + i));
+      if (isfinite(f)) continue;
+      o[i] += f;
+      found |= 1u << i;
+      if (o[i] != o[i]) open &= ~(1u << i);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    if ((unknown & ~found) >> i & 1) o[i] = __uint_as_float(0x7fffffffu);
 }
 
 template <int HD>
@@ -368,8 +405,9 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
           const int s = o_it & 1;
           const uint32_t vb = smem_u32(v_s + s * L::KV_BYTES);
 #pragma unroll
-          for (int k = 0; k < KT / 16; ++k)
-            umma_f16_ts(tmem_o, tmem_s + (uint32_t)(s * KT + k * 8), umma_desc_sw128_mn(vb + k * (16 * 128), KT * 128, 1024), idesc_o, (!o_first || k > 0) ? 1u : 0u);
+          for (int k = 0; k < KT / 8; ++k)                     // 16 keys, their weights' first halves and then the second
+            umma_f16_ts(tmem_o, tmem_s + (uint32_t)(s * KT + k * 8), umma_desc_sw128_mn(vb + (k >> 1) * (16 * 128), KT * 128, 1024), idesc_o,
+                        (!o_first || k > 0) ? 1u : 0u);
           umma_commit(smem_u32(&v_empty[s]));
           umma_commit(smem_u32(&pv_done[s]));
           ++o_it;
@@ -452,21 +490,27 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
           move = mx > m_ref + GAP || (m_ref == -INFINITY && mx > -INFINITY);
           const float m_new = move ? mx : m_ref, m_use = m_new == -INFINITY ? 0.f : m_new;
           alpha = move ? ex2(m_ref - m_use) : 1.f;
-          const uint64_t scale2 = pack_f32x2(p.scale_log2e, p.scale_log2e), minus2 = pack_f32x2(-m_use, -m_use);
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
-          uint32_t packed[KT / 2];
+          constexpr float LIFT = BF16 ? 0.f : 7.f;
+          const uint64_t scale2 = pack_f32x2(p.scale_log2e, p.scale_log2e), minus2 = pack_f32x2(LIFT - m_use, LIFT - m_use), one2 = pack_f32x2(1.f, 1.f);
+          uint64_t sum[2] = {0, 0};
 #pragma unroll
-          for (int c = 0; c < KT; c += 2) {
-            const float2 t = unpack_f32x2(fma_f32x2(pack_f32x2(sc[c], sc[c + 1]), scale2, minus2));
-            const uint32_t w = round_pair<BF16>(ex2(t.x), ex2(t.y));
-            packed[c / 2] = w;
-            float &a = sum[c & 2], &b = sum[(c & 2) + 1];
-            a = BF16 ? add_lo_bf16(w, a) : add_lo_f16(w, a);
-            b = BF16 ? add_hi_bf16(w, b) : add_hi_f16(w, b);
+          for (int half = 0; half < 2; ++half) {               // 16 keys take 8 columns for their weights and 8 for the rest of them
+            uint32_t packed[32];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int c = half * 32 + 2 * i, at = (i >> 3) * 16 + (i & 7);
+              const float2 t = unpack_f32x2(fma_f32x2(pack_f32x2(sc[c], sc[c + 1]), scale2, minus2));
+              const float a = ex2(t.x), b = ex2(t.y);
+              packed[at] = round_pair<BF16>(a, b);
+              packed[at + 8] = rest_pair<BF16>(packed[at], a, b);
+              sum[i & 1] = fma_f32x2(pack_f32x2(a, b), one2, sum[i & 1]);
+            }
+            tmem_st32_words_issue(ts + half * 32, packed);
           }
-          l_run = l_run * alpha + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
+          const float2 s0 = unpack_f32x2(sum[0]), s1 = unpack_f32x2(sum[1]);
+          l_run = l_run * alpha + ((s0.x + s0.y) + (s1.x + s1.y));
+          tmem_st_wait();
           m_ref = m_new;
-          tmem_st32_words(ts, packed);
         }
         if (x.len - k0 < KT || k0 + KT > tail) {
           // V is touched: keys behind the length become zeros; of keys that only later tokens see, what is no number leaves the product
@@ -530,17 +574,18 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
             float o[32];
             __syncwarp();
             tmem_ld32(tmem_o + lane_off + c, o);
-            if (bad) {
-              for (int key = max(tail, x.j0 * KT); key < min(lim, x.j1 * KT); ++key) {
-                const int page = p.table[(int64_t)(x.seg - p.groups) * p.pps + (key >> p.log2P)];
-                if ((unsigned)page >= (unsigned)p.n_pages) continue;
-                const uint16_t* v = (const uint16_t*)p.v_pages + (((int64_t)page * p.Hkv + x.kvh) * p.P + (key & (p.P - 1))) * HD + c;
+            uint64_t z = 0;                                    // no number if one of them is none
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                  const float f = BF16 ? __uint_as_float((uint32_t)v[i] << 16) : __half2float(*reinterpret_cast<const __half*>(v + i));
-                  if (!isfinite(f)) o[i] += f;
-                }
-              }
+            for (int i = 0; i < 32; i += 2) z = fma_f32x2(pack_f32x2(o[i], o[i + 1]), 0, z);
+            const float2 zz = unpack_f32x2(z);
+            if ((bad || !(zz.x + zz.y == 0.f)) && l_run < INFINITY) {
+              float t[32];
+#pragma unroll
+              for (int i = 0; i < 32; ++i) t[i] = o[i];
+              repair<HD, BF16>(x.group ? p.prefix_table + (int64_t)x.seg * p.prefix_pages : p.table + (int64_t)(x.seg - p.groups) * p.pps,
+                               (const uint16_t*)p.v_pages + (int64_t)x.kvh * p.P * HD + c, p.n_pages, p.Hkv, p.log2P, x.j0 * KT, min(lim, x.j1 * KT), tail, t);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] = t[i];
             }
             if (real) {
 #pragma unroll

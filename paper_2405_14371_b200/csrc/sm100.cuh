@@ -306,8 +306,8 @@ __device__ __forceinline__ uint64_t umma_desc_sw128_mn(uint32_t saddr, uint32_t 
   return d;
 }
 
-// 32 consecutive fp32 columns of this thread's TMEM lane, written back.
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&v)[32]) {
+// 32 consecutive fp32 columns of this thread's TMEM lane, written back; tmem_st_wait must follow the last of several.
+__device__ __forceinline__ void tmem_st32_issue(uint32_t taddr, const float (&v)[32]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
       "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
@@ -322,15 +322,19 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&v)[32]) 
         "r"(__float_as_uint(v[27])), "r"(__float_as_uint(v[28])), "r"(__float_as_uint(v[29])), "r"(__float_as_uint(v[30])),
         "r"(__float_as_uint(v[31]))
       : "memory");
-  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&v)[32]) {
+  tmem_st32_issue(taddr, v);
+  tmem_st_wait();
 }
 
-// 32 words of this thread's TMEM lane.
-__device__ __forceinline__ void tmem_st32_words(uint32_t taddr, const uint32_t (&v)[32]) {
+// the same of words
+__device__ __forceinline__ void tmem_st32_words_issue(uint32_t taddr, const uint32_t (&v)[32]) {
   float f[32];
 #pragma unroll
   for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(v[i]);
-  tmem_st32(taddr, f);
+  tmem_st32_issue(taddr, f);
 }
 
 // ---- CTA pairs (cta_group::2): one MMA spans the tensor cores and shared memory of two CTAs ------
