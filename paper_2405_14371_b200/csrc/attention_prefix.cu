@@ -247,7 +247,8 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
   uint32_t* tmem_slot = (uint32_t*)(bars + L::BARS);
   volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
   volatile int* pages_seen = (volatile int*)(tmem_slot + 2);   // [4] of the latest tiles: which 16 tokens lie in pages that exist
-  volatile int* tail_bad = (volatile int*)(tmem_slot + 6);     // piece whose last tokens hold a V that is no number
+  volatile int* tail_bad = (volatile int*)(tmem_slot + 6);     // [2] of the latest pieces: the piece, if its last tokens hold a V that is no number.
+                                                               // A warp may be one piece ahead of another, not two: p_full takes all four
   int* totals = (int*)(tmem_slot + 8);                         // [8]
   int* line = (int*)(tmem_slot + 16);                          // [segments + 1] places before
   int* lens = line + p.groups + p.B + 1;                       // [segments] keys
@@ -260,7 +261,7 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
     prefetch_tmap(&maps.v);
     for (int i = 0; i < L::BARS; ++i) mbar_init(smem_u32(&bars[i]), (i == 12 || i == 13) ? 4 : 1);   // p_full: four warps
     *abort_flag = 0;
-    *tail_bad = -1;
+    tail_bad[0] = tail_bad[1] = -1;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) tmem_alloc(smem_u32(tmem_slot), TMEM_COLS);
@@ -532,7 +533,7 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
               uint32_t keep = 0xffffffffu;
               if ((w & inf) == inf) keep &= 0xffff0000u;
               if (((w >> 16) & inf) == inf) keep &= 0xffffu;
-              if (keep != 0xffffffffu) { *at = w & keep; *tail_bad = pieces; }
+              if (keep != 0xffffffffu) { *at = w & keep; tail_bad[pieces & 1] = pieces; }
             }
           }
           fence_proxy_async_smem();
@@ -567,7 +568,7 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
       float* po = (x.group ? p.o_p : p.o_o) + row * HD;
       if (!idle) {
         if (real) *reinterpret_cast<float2*>(ml) = ok ? make_float2(m_ref, l_run) : make_float2(0.f, __uint_as_float(0x7fffffffu));
-        const bool bad = *tail_bad == pieces;
+        const bool bad = tail_bad[pieces & 1] == pieces;
         if (ok) {
 #pragma unroll 1
           for (int c = 0; c < HD; c += 32) {
