@@ -151,6 +151,7 @@ __global__ void __launch_bounds__(RowsCfg<NT>::THREADS, RowsCfg<NT>::OCC) linear
       const uint64_t w0 = umma_desc_sw128(smem_u32(ring)), x0 = umma_desc_sw128(smem_u32(ring) + W_TILE);
       const uint32_t full0 = smem_u32(full), empty0 = smem_u32(empty), acc_full0 = smem_u32(acc_full), acc_empty0 = smem_u32(acc_empty);
       uint32_t s = 0, ring_phase = 0, buf = 0, buf_phase = 1;
+      pdl_wait();                                                       // the second that a wait may last is this kernel's alone
       for (int left = blocks; left > 0; --left) {
         if (!mbar_wait_soon(full0 + s * 8, ring_phase, abort_flag) || !mbar_wait_soon(acc_empty0 + buf * 8, buf_phase, abort_flag)) break;
         tc_fence_after();
@@ -205,6 +206,7 @@ __global__ void __launch_bounds__(RowsCfg<NT>::THREADS, RowsCfg<NT>::OCC) linear
     // ---- sums ----
     const uint32_t taddr = tmem + col0 + ((uint32_t)((warp & 3) * 32) << 16);
     bool ok = true;
+    pdl_wait();
 #pragma unroll
     for (int j = 0; j < L::MINE; ++j) acc[j] = 0.f;
     for (int i = 0; i < blocks; ++i) {
@@ -242,7 +244,6 @@ __global__ void __launch_bounds__(RowsCfg<NT>::THREADS, RowsCfg<NT>::OCC) linear
 #pragma unroll
       for (int j = 0; j < L::MINE; ++j) acc[j] = __uint_as_float(0x7fffffffu);
     }
-    pdl_wait();                                                         // long over; this thread writes the result
   }
 
   // ---- teardown, and the sums of the cluster's CTAs ----
