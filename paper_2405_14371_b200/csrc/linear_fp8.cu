@@ -622,16 +622,16 @@ es_status_t launch_pair(const Fp8Maps& maps, const Fp8Params& p, int split, cuda
 }
 
 // Clusters of `split` CTAs that the device holds with a CTA on each SM, asked of the form that fits an SM once.  (Fewer than the
-// SMs divided by the size: a cluster lies in one part of the device, and the parts differ.)
+// SMs divided by the size: a cluster lies in one part of the device, and the parts differ.  0: it holds none of this size.)
 es_status_t places_of(int split, int* places) {
   using L = RowsCfg<128>;
   static_assert(L::OCC == 1, "one CTA an SM");
-  static std::atomic<int> known[64][9];
+  static std::atomic<int> known[64][9];                                 // one more than the answer; 0: not asked yet
   static std::atomic<uint64_t> allowed{0};
   int dev = 0;
   ES_CUDA_CHECK(cudaGetDevice(&dev));
   std::atomic<int>* at = dev < 64 ? &known[dev][split] : nullptr;
-  if (at && (*places = at->load(std::memory_order_relaxed)) > 0) return ES_OK;
+  if (at && (*places = at->load(std::memory_order_relaxed) - 1) >= 0) return ES_OK;
   ES_CUDA_CHECK(allow_shared_memory(linear_fp8_rows_kernel<128>, (int)L::SMEM, &allowed));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(split);
@@ -645,25 +645,36 @@ es_status_t places_of(int split, int* places) {
   cfg.numAttrs = 1;
   int n = 0;
   ES_CUDA_CHECK(cudaOccupancyMaxActiveClusters(&n, linear_fp8_rows_kernel<128>, &cfg));
-  *places = n > 0 ? n : 1;
-  if (at) at->store(*places, std::memory_order_relaxed);
+  *places = n;
+  if (at) at->store(n + 1, std::memory_order_relaxed);
   return ES_OK;
 }
 
 // CTAs that share a tile's K range: as many as make the time of the waves shortest, counted in blocks; starting and joining
 // cost about 4 of them (8 with 128 tokens: their sums take longer to join).  Measured for 1, 2, 3, 4 CTAs: 1 x 12288 x 4096 15.2 / 12.7 / 17.9 / 16.1 us (2 taken: 3 no longer fit in
 // one wave), 16 x 10240 x 8192 28.5 / 18.7 / 18.0 / 25.6 (3), 113 x 5120 x 13824 74.6 / 43.4 / 32.5 / 49.7 (3).
+struct Split { int n; long long cost; };
+constexpr Split rows_split_of(long long tiles, int nkb, const int (&places)[9], int occ, int start) {
+  Split best{1, 0};
+  for (int s = 1; s <= 8 && s <= nkb; ++s) {
+    const long long at_once = (long long)(s == 1 && places[1] < 1 ? 1 : places[s]) * occ;       // a single CTA remains, whatever was answered
+    if (at_once == 0) continue;
+    const long long cost = ((tiles + at_once - 1) / at_once) * ((nkb + s - 1) / s + start);
+    if (s == 1 || cost < best.cost) best = Split{s, cost};
+  }
+  return best;
+}
+constexpr int EVEN[9] = {0, 148, 74, 48, 36, 26, 24, 20, 16}, SMALL_PARTS[9] = {0, 148, 74, 48, 0, 0, 0, 0, 0}, NOTHING[9] = {};
+static_assert(rows_split_of(1, 512, EVEN, 1, 8).n == 8 && rows_split_of(1, 512, SMALL_PARTS, 1, 8).n == 3 && rows_split_of(1, 512, NOTHING, 1, 8).n == 1,
+              "one tile is shared by the most CTAs that the device holds as a cluster");
+
 template <int NT>
 es_status_t rows_split(const Fp8Params& p, int* split, long long* blocks) {
-  const long long tiles = (long long)((p.N + 127) / 128) * ((p.M + NT - 1) / NT);
-  *blocks = 0;
-  for (int s = 1; s <= 8 && s <= p.nkb; ++s) {
-    int places = 0;
-    ES_TRY(places_of(s, &places));
-    places *= RowsCfg<NT>::OCC;
-    const long long cost = ((tiles + places - 1) / places) * ((p.nkb + s - 1) / s + (RowsCfg<NT>::OCC == 1 ? 8 : 4));
-    if (s == 1 || cost < *blocks) { *split = s; *blocks = cost; }
-  }
+  int places[9] = {};
+  for (int s = 1; s <= 8 && s <= p.nkb; ++s) ES_TRY(places_of(s, &places[s]));
+  const Split best = rows_split_of((long long)((p.N + 127) / 128) * ((p.M + NT - 1) / NT), p.nkb, places, RowsCfg<NT>::OCC, RowsCfg<NT>::OCC == 1 ? 8 : 4);
+  *split = best.n;
+  *blocks = best.cost;
   return ES_OK;
 }
 
@@ -680,16 +691,26 @@ es_status_t rows_auto(const Fp8Maps& maps, const Fp8Params& p, cudaStream_t s) {
 // Pairs that share a tile's K range, and eighths of the blocks (of a single CTA's) that the rounds take: a block of a pair's tile
 // costs 7 / 8 of one of a single CTA's (0.55 and 0.62 us), start and stores 5, joining SPLIT_JOIN.
 constexpr int SPLIT_JOIN = 5;          // measured with two pairs a tile: 320 x 4096 x 4096 21.2 -> 19.1 us, 129 x 5003 x 2064 16.3 -> 16.5
-es_status_t pairs_split(const Fp8Params& p, int* split, long long* eighths) {
-  const long long tiles = (long long)((p.M + 255) / 256) * ((p.N + 255) / 256), n_pairs = sm_count() / 2 > 0 ? sm_count() / 2 : 1;
-  *split = 1;
-  *eighths = (tiles + n_pairs - 1) / n_pairs * p.nkb * 7 + 5 * 8;
-  for (int s = 2; s <= 4 && s <= p.nkb && tiles * s <= n_pairs; s *= 2) {
-    int places = 0;
-    ES_TRY(places_of(2 * s, &places));
-    const long long cost = (tiles + places - 1) / places * ((p.nkb + s - 1) / s) * 7 + (5 + SPLIT_JOIN) * 8;
-    if (cost < *eighths) { *split = s; *eighths = cost; }
+constexpr Split pairs_split_of(long long tiles, int nkb, long long n_pairs, int places4, int places8) {
+  Split best{1, (tiles + n_pairs - 1) / n_pairs * nkb * 7 + 5 * 8};
+  for (int s = 2; s <= 4 && s <= nkb && tiles * s <= n_pairs; s *= 2) {
+    const int places = s == 2 ? places4 : places8;
+    if (places < 1) continue;
+    const long long cost = (tiles + places - 1) / places * ((nkb + s - 1) / s) * 7 + (5 + SPLIT_JOIN) * 8;
+    if (cost < best.cost) best = Split{s, cost};
   }
+  return best;
+}
+static_assert(pairs_split_of(4, 64, 74, 36, 16).n == 4 && pairs_split_of(4, 64, 74, 36, 0).n == 2 && pairs_split_of(4, 64, 74, 0, 0).n == 1,
+              "pairs share a tile only in clusters that the device holds");
+
+es_status_t pairs_split(const Fp8Params& p, int* split, long long* eighths) {
+  int places4 = 0, places8 = 0;
+  ES_TRY(places_of(4, &places4));
+  ES_TRY(places_of(8, &places8));
+  const Split best = pairs_split_of((long long)((p.M + 255) / 256) * ((p.N + 255) / 256), p.nkb, sm_count() / 2 > 0 ? sm_count() / 2 : 1, places4, places8);
+  *split = best.n;
+  *eighths = best.cost;
   return ES_OK;
 }
 
