@@ -748,7 +748,7 @@ extern "C" es_status_t es_op_linear_fp8(const void* a, const float* a_scale, con
     return fail(ES_ERR_INVALID_ARG, "a and w must be 16-byte aligned, the others by their elements");
   if (!tma_available()) return fail(ES_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
   const int NT = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
-  Fp8Params p{a_scale, w_scale, R, C, M, N, (K + FP8_BLOCK - 1) / FP8_BLOCK, out_dtype, weights_ready != 0, 0};
+  Fp8Params p{a_scale, w_scale, R, C, M, N, fp8_blocks(K), out_dtype, weights_ready != 0, 0};
   bool pairs = path == 2;
   if (path == 0) ES_TRY(pairs_better(p, &pairs));
   p.vec = ((size_t)N * esize) % 16 == 0 && ((uintptr_t)C | (uintptr_t)R) % 16 == 0;

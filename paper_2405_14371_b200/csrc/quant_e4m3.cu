@@ -165,7 +165,7 @@ extern "C" es_status_t es_op_quant_e4m3(const void* x, int32_t dtype, int64_t ro
   if (!x || !codes || !scale) return fail(ES_ERR_INVALID_ARG, "null argument");
   if (row_stride < K || row_stride % (dtype == ES_DTYPE_F32 ? 4 : 8)) return fail(ES_ERR_INVALID_ARG, "rows of x must start every multiple of 16 bytes, at least K elements apart");
   if (((uintptr_t)x | (uintptr_t)codes) % 16 || (uintptr_t)scale % 4) return fail(ES_ERR_INVALID_ARG, "x and codes must be 16-byte aligned, scale 4-byte aligned");
-  QuantParams p{x, row_stride, (uint8_t*)codes, scale, M, K, (K + FP8_BLOCK - 1) / FP8_BLOCK};
+  QuantParams p{x, row_stride, (uint8_t*)codes, scale, M, K, fp8_blocks(K)};
   cudaStream_t s = (cudaStream_t)stream;
   if (dtype == ES_DTYPE_F16) return launch<__half>(p, block_rows, s);
   if (dtype == ES_DTYPE_BF16) return launch<__nv_bfloat16>(p, block_rows, s);
