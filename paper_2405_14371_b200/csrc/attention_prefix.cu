@@ -603,7 +603,7 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    if (*abort_flag) __nanosleep(100000);
+    if (*abort_flag) settle();
     tmem_dealloc(tmem_base, TMEM_COLS);
   }
 }

@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(RowsCfg<NT>::THREADS, RowsCfg<NT>::OCC) linear
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    if (*abort_flag) __nanosleep(100000);
+    if (*abort_flag) settle();
     tmem_dealloc(tmem, L::COLS);
   }
   const int tokens = min(NT, p.M - m0);
@@ -275,6 +275,8 @@ __global__ void __launch_bounds__(RowsCfg<NT>::THREADS, RowsCfg<NT>::OCC) linear
   constexpr int TEAMS = L::SUMS / 4, MANY = 8;
   const int j1 = min(tokens, NT * (rank + 1) / split);
   if (warp >= 4) {
+    // sums of a CTA whose wait ran out are not read: copies that were under way may have landed on them
+    const bool lost = lane < split && *cl.map_shared_rank((int*)abort_flag, lane) != 0;
     for (int j0 = NT * rank / split + (warp - 4) / 4; j0 < j1; j0 += TEAMS * MANY) {
       float v[MANY];
 #pragma unroll
@@ -284,6 +286,10 @@ __global__ void __launch_bounds__(RowsCfg<NT>::THREADS, RowsCfg<NT>::OCC) linear
         const float* from = cl.map_shared_rank(sums, r) + at;
 #pragma unroll
         for (int q = 0; q < MANY; ++q) v[q] += from[min(j0 + q * TEAMS, NT - 1) * 128];
+      }
+      if (__any_sync(0xffffffffu, lost)) {
+#pragma unroll
+        for (int q = 0; q < MANY; ++q) v[q] = __uint_as_float(0x7fffffffu);
       }
       if (n < p.N) store_many<MANY>(p, n, m0 + j0, TEAMS, m0 + j1, v);
     }
@@ -557,6 +563,10 @@ __global__ void __launch_bounds__(P_THREADS, 1) linear_fp8_pair_kernel(const __g
       cg::cluster_group cl = cg::this_cluster();
       int m0, n0;
       origin(pair, m0, n0);
+      int lost = 0;                                                     // as above
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        if (s < split) lost |= *cl.map_shared_rank((int*)abort_flag, 2 * s + (int)rank);
       const int lanes = 64 / split, e = (int)threadIdx.x - 128, c = ks * (256 / split) + e % lanes * 4, n = n0 + c;      // lanes of a row, first of four columns
 #pragma unroll 4
       for (int r = e / lanes; r < 128; r += 32 * P_EPI / lanes) {
@@ -567,6 +577,7 @@ __global__ void __launch_bounds__(P_THREADS, 1) linear_fp8_pair_kernel(const __g
           const float4 x = *reinterpret_cast<const float4*>(cl.map_shared_rank((float*)ring, 2 * s + (int)rank) + r * P_PITCH + c);
           v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
         }
+        if (lost) v.x = v.y = v.z = v.w = __uint_as_float(0x7fffffffu);
         const int m = m0 + (int)rank * 128 + r;
         if (m >= p.M || n >= p.N) continue;
         const int64_t at = (int64_t)m * p.N + n;
@@ -599,7 +610,7 @@ __global__ void __launch_bounds__(P_THREADS, 1) linear_fp8_pair_kernel(const __g
   cluster_sync_all();
   if (warp == 1) {
     tc_fence_after();
-    if (*abort_flag) __nanosleep(100000);
+    if (*abort_flag) settle();
     tmem_dealloc_pair(tmem, 512);
   }
 }

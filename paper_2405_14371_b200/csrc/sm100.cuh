@@ -79,6 +79,12 @@ __device__ __forceinline__ bool mbar_wait_soon(uint32_t bar, uint32_t parity, vo
   return true;
 }
 
+// After a wait that ran out: time for copies and products under way to land, 200 us by the clock (a sleep may be over at once).
+__device__ __forceinline__ void settle() {
+  const uint64_t t0 = global_timer_ns();
+  while (global_timer_ns() - t0 < 200000ull) __nanosleep(20000);
+}
+
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
