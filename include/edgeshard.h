@@ -482,7 +482,8 @@ ES_API es_status_t es_op_sample(const void *logits, int32_t dtype, int64_t row_s
  *   codes [M, K], dense, 16-byte aligned;  scale fp32: block_rows 1: [ceil(K / 128), M]; 128: [ceil(M / 128), ceil(K / 128)];
  *   M <= 262140 (block_rows 1), 8388480 (128).
  * scale = max(largest magnitude * fl(1 / 448), 2^-100); code = round(value / scale), to nearest, ties to even, of the
- * fp32 quotient.  A block that holds an infinity or a NaN has the scale NaN and codes that are no numbers. */
+ * fp32 quotient.  A block that holds an infinity or a NaN has the scale NaN and codes that are no numbers.  x, codes and
+ * scale must not overlap. */
 ES_API es_status_t es_op_quant_e4m3(const void *x, int32_t dtype, int64_t row_stride, int32_t M, int32_t K,
                                     int32_t block_rows, void *codes, float *scale, void *stream);
 
@@ -491,7 +492,8 @@ ES_API es_status_t es_op_quant_e4m3(const void *x, int32_t dtype, int64_t row_st
  * 8 ranges of blocks, then range by range; the order depends on the sizes and the device alone).  The product of two
  * scales is formed in fp32 and must be finite there.
  *   a codes [M, K], a_scale fp32 [ceil(K / 128), M];  w codes [N, K], w_scale fp32 [ceil(N / 128), ceil(K / 128)];
- *   C [M, N], dense, fp16, bf16 or fp32;  R fp32 [M, N] or NULL, only with an fp32 C, may be C itself;
+ *   C [M, N], dense, fp16, bf16 or fp32;  R fp32 [M, N] or NULL, only with an fp32 C, may be C itself;  C must
+ *   not overlap anything else that is read;
  *   a, w 16-byte aligned;  K % 16 == 0;  M <= 262140, N <= 2^24.
  * path: 0 = automatic, 1 = tiles of 128 weight rows, 2 = tiles of 256 x 256 on CTA pairs.
  * weights_ready != 0: w and w_scale hold their values already when the call is made (when a captured call is
@@ -512,7 +514,7 @@ ES_API es_status_t es_op_linear_fp8(const void *a, const float *a_scale, const v
  *   slot_map[r] = page * page_tokens + offset (page_tokens a power of two >= 16); tokens with a slot outside
  *   [0, n_pages * page_tokens) are not cached.  Two tokens of a call must not have the same slot.
  * A token whose position is outside [0, max_pos) (padding) gives zeros in q_out and in dense k_out, v_out and is not
- * cached.  Arithmetic in fp32, rounded once.  Results must not overlap q, k or v. */
+ * cached.  Arithmetic in fp32, rounded once.  Results must not overlap q, k, v or one another. */
 ES_API es_status_t es_op_qk_norm_rope(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
                                       int64_t v_stride, int32_t dtype, const void *q_gain, const void *k_gain,
                                       int32_t gain_dtype, float eps, const float *cosines, const float *sines,

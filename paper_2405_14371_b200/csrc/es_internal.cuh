@@ -27,6 +27,12 @@ es_status_t fail(es_status_t st, const char* fmt, ...);
     if (_s != ES_OK) return _s;      \
   } while (0)
 
+// Whether two ranges of memory share a byte; ranges without an address or without bytes share none.
+inline bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return a && b && a_bytes > 0 && b_bytes > 0 && (x < y ? y - x < (uintptr_t)a_bytes : x - y < (uintptr_t)b_bytes);
+}
+
 // ---- tuning knobs (read once from the environment; defaults are the measured best) -----------
 struct Tunables {
   int stream_deep;   // ES_STREAM_DEEP: weight-streaming kernel chunk depth, 1 = 4 KB per warp per buffer (default), 0 = 2 KB

@@ -757,6 +757,11 @@ extern "C" es_status_t es_op_linear_fp8(const void* a, const float* a_scale, con
   const size_t esize = out_dtype == ES_DTYPE_F32 ? 4 : 2;
   if (((uintptr_t)a | (uintptr_t)w) % 16 || ((uintptr_t)a_scale | (uintptr_t)w_scale | (uintptr_t)R) % 4 || (uintptr_t)C % esize)
     return fail(ES_ERR_INVALID_ARG, "a and w must be 16-byte aligned, the others by their elements");
+  // a tile may be stored while another has yet to read what its results would lie on; the residual is read where its result goes
+  const int64_t c_bytes = (int64_t)M * N * esize, kb = fp8_blocks(K);
+  if (overlap(C, c_bytes, a, (int64_t)M * K) || overlap(C, c_bytes, w, (int64_t)N * K) || overlap(C, c_bytes, a_scale, kb * M * 4) ||
+      overlap(C, c_bytes, w_scale, kb * fp8_blocks(N) * 4) || (R != C && overlap(C, c_bytes, R, c_bytes)))
+    return fail(ES_ERR_INVALID_ARG, "the result overlaps what is read");
   if (!tma_available()) return fail(ES_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
   const int NT = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
   Fp8Params p{a_scale, w_scale, R, C, M, N, fp8_blocks(K), out_dtype, weights_ready != 0, 0};

@@ -217,11 +217,6 @@ es_status_t launch_hd(const HeadsParams& p, int hd, bool halves, cudaStream_t s)
 
 bool stride_ok(int64_t stride, int64_t least, int64_t n) { return stride % 8 == 0 && (n <= 1 || stride >= least); }
 
-bool overlap(const void* a, int64_t a_elems, const void* b, int64_t b_elems) {
-  const char *x = (const char*)a, *y = (const char*)b;
-  return a && b && x < y + 2 * b_elems && y < x + 2 * a_elems;
-}
-
 }  // namespace
 }  // namespace es
 
@@ -251,14 +246,16 @@ extern "C" es_status_t es_op_qk_norm_rope(const void* q, int64_t q_stride, const
   if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)q_out | (uintptr_t)k_out | (uintptr_t)v_out | (uintptr_t)q_gain | (uintptr_t)k_gain | (uintptr_t)cosines |
        (uintptr_t)sines) % 16)
     return fail(ES_ERR_INVALID_ARG, "tensors must be 16-byte aligned");
-  // a warp may write a head while another has yet to read its own: results lie apart from what is read
+  // a warp may write a head while another has yet to read its own: results lie apart from what is read, and from one another
   const int64_t qs = (int64_t)(n - 1) * q_stride + (int64_t)Hq * hd, ks = (int64_t)(n - 1) * k_stride + (int64_t)Hkv * hd,
                 vs = (int64_t)(n - 1) * v_stride + (int64_t)Hkv * hd, qo = (int64_t)n * Hq * hd,
                 ko = slot_map ? (int64_t)n_pages * Hkv * page_tokens * hd : (int64_t)n * Hkv * hd;
   const struct { const void* p; int64_t n; } in[3] = {{q, qs}, {k, ks}, {v, vs}}, out[3] = {{q_out, qo}, {k_out, ko}, {v_out, ko}};
   for (auto& i : in)
     for (auto& o : out)
-      if (overlap(i.p, i.n, o.p, o.n)) return fail(ES_ERR_INVALID_ARG, "a result overlaps what is read");
+      if (overlap(i.p, 2 * i.n, o.p, 2 * o.n)) return fail(ES_ERR_INVALID_ARG, "a result overlaps what is read");
+  for (int i = 0; i < 3; ++i)
+    if (overlap(out[i].p, 2 * out[i].n, out[(i + 1) % 3].p, 2 * out[(i + 1) % 3].n)) return fail(ES_ERR_INVALID_ARG, "two results overlap");
   HeadsParams p{};
   p.q = q; p.k = k; p.v = v;
   p.q_stride = q_stride; p.k_stride = k_stride; p.v_stride = v_stride;

@@ -165,6 +165,12 @@ extern "C" es_status_t es_op_quant_e4m3(const void* x, int32_t dtype, int64_t ro
   if (!x || !codes || !scale) return fail(ES_ERR_INVALID_ARG, "null argument");
   if (row_stride < K || row_stride % (dtype == ES_DTYPE_F32 ? 4 : 8)) return fail(ES_ERR_INVALID_ARG, "rows of x must start every multiple of 16 bytes, at least K elements apart");
   if (((uintptr_t)x | (uintptr_t)codes) % 16 || (uintptr_t)scale % 4) return fail(ES_ERR_INVALID_ARG, "x and codes must be 16-byte aligned, scale 4-byte aligned");
+  if (M > 1 && row_stride > (1LL << 40)) return fail(ES_ERR_RANGE, "row_stride exceeds 2^40");
+  // a warp may write codes while another has yet to read what they would lie on
+  const int64_t x_bytes = ((int64_t)(M - 1) * (M > 1 ? row_stride : 0) + K) * (dtype == ES_DTYPE_F32 ? 4 : 2), code_bytes = (int64_t)M * K;
+  const int64_t scale_bytes = (int64_t)fp8_blocks(K) * (block_rows == 1 ? M : fp8_blocks(M)) * 4;
+  if (overlap(x, x_bytes, codes, code_bytes) || overlap(x, x_bytes, scale, scale_bytes) || overlap(codes, code_bytes, scale, scale_bytes))
+    return fail(ES_ERR_INVALID_ARG, "codes, scale and x must lie apart");
   QuantParams p{x, row_stride, (uint8_t*)codes, scale, M, K, fp8_blocks(K)};
   cudaStream_t s = (cudaStream_t)stream;
   if (dtype == ES_DTYPE_F16) return launch<__half>(p, block_rows, s);
