@@ -67,14 +67,14 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
 
 // The same for waits that are short and many: the clock (whose reading takes about 480 cycles, which mbar_wait spends on every
 // wait that is not over at once) is left alone for the first 255 looks.
-__device__ __forceinline__ bool mbar_wait_soon(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+__device__ __forceinline__ bool mbar_wait_soon(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint64_t limit_ns = 1000000000ull) {
   uint64_t t0 = 0;
   for (uint32_t looks = 1; !mbar_try_wait(bar, parity); ++looks) {
     if ((looks & 255u) != 0) continue;
     if (*abort_flag) return false;
     const uint64_t now = global_timer_ns();
     if (t0 == 0) t0 = now;
-    if (now - t0 > 1000000000ull) { *abort_flag = 1; return false; }
+    if (now - t0 > limit_ns) { *abort_flag = 1; return false; }
   }
   return true;
 }
