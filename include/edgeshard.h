@@ -488,16 +488,16 @@ ES_API es_status_t es_op_quant_e4m3(const void *x, int32_t dtype, int64_t row_st
                                     int32_t block_rows, void *codes, float *scale, void *stream);
 
 /* es_op_linear of such operands: C[m, n] = sum over blocks b of a_scale[b, m] * w_scale[n / 128, b] *
- * sum over k in b of a[m, k] * w[n, k]   (+ R[m, n]); blocks are added in ascending order, in fp32 (few rows: in up to
- * 8 ranges of blocks, then range by range; the order depends on the sizes and the device alone).  The product of two
- * scales is formed in fp32 and must be finite there.
+ * sum over k in b of a[m, k] * w[n, k]   (+ R[m, n]); blocks are added in ascending order, in fp32, in up to 8 ranges of
+ * blocks (tiles of 128 weight rows) or 1, 2 or 4 (pairs), then range by range; their number depends on the sizes and the
+ * device alone.  The product of two scales is formed in fp32 and must be finite there.
  *   a codes [M, K], a_scale fp32 [ceil(K / 128), M];  w codes [N, K], w_scale fp32 [ceil(N / 128), ceil(K / 128)];
  *   C [M, N], dense, fp16, bf16 or fp32;  R fp32 [M, N] or NULL, only with an fp32 C, may be C itself;  C must
  *   not overlap anything else that is read;
  *   a, w 16-byte aligned;  K % 16 == 0;  M <= 262140, N <= 2^24.
- * path: 0 = automatic, 1 = tiles of 128 weight rows, 2 = tiles of 256 x 256 on CTA pairs.
+ * path: 0 = automatic (up to 64 rows: 1), 1 = tiles of 128 weight rows, 2 = tiles of 256 x 256 on CTA pairs.
  * weights_ready != 0: w and w_scale hold their values already when the call is made (when a captured call is
- *   replayed), whatever still runs on the stream; with few rows they are then read while the kernel in front ends.
+ *   replayed), whatever still runs on the stream; on path 1 they are then read while the kernel in front ends.
  * Should a wait inside the kernel run out (after a second), the results it was for become NaN. */
 ES_API es_status_t es_op_linear_fp8(const void *a, const float *a_scale, const void *w, const float *w_scale,
                                     const float *R, void *C, int32_t out_dtype, int32_t M, int32_t N, int32_t K,

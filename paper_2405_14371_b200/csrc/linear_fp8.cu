@@ -9,12 +9,13 @@
 // Two kernels:
 //
 //   * tiles of 128 weight rows (few tokens).  The weights are the M side of the MMA, 16 to 128 tokens its N side, so a decode
-//     batch wastes no tensor-core rows on absent tokens and a block costs a thread 16 to 128 multiply-adds.  Bound: reading
+//     batch wastes no tensor-core rows on absent tokens and a block costs a thread 16 to 64 multiply-adds.  Bound: reading
 //     the weights once.  The K range of a tile is shared by a cluster of 1 to 8 CTAs so that the machine is full in one wave;
-//     their sums meet in distributed shared memory and are added in rank order, so the result depends on the sizes alone.
+//     their sums meet in distributed shared memory and are added in rank order, so the result depends on the sizes and the
+//     device (how many clusters it holds) alone.
 //   * 256 x 256 tiles on CTA pairs (many tokens): cta_group::2, each CTA stages 128 rows of A and 128 of W per block and
-//     keeps 128 x 256 running sums in the registers of 8 warps (128 each).  Bound: the tensor cores' e4m3 rate, and the
-//     power it draws.
+//     keeps 128 x 256 running sums in the registers of 8 warps (128 each).  Where tiles are few, two or four pairs share a
+//     tile's K range and join their sums the same way.  Bound: the tensor cores' e4m3 rate, and the power it draws.
 //
 // Every wait is bounded by a second; the tiles of a CTA whose wait ran out become NaN.
 #include <cooperative_groups.h>
@@ -271,7 +272,7 @@ __global__ void __launch_bounds__(RowsCfg<NT>::THREADS, RowsCfg<NT>::OCC) linear
   cg::cluster_group cl = cg::this_cluster();
   cl.sync();
   // this CTA's share of the tokens, eight at a time: their sums of all ranks are under way together (one by one, the reads of
-  // 113 tokens took 15 us)
+  // 113 tokens took 15 us; the whole product takes 33)
   constexpr int TEAMS = L::SUMS / 4, MANY = 8;
   const int j1 = min(tokens, NT * (rank + 1) / split);
   if (warp >= 4) {
@@ -662,8 +663,9 @@ es_status_t places_of(int split, int* places) {
 }
 
 // CTAs that share a tile's K range: as many as make the time of the waves shortest, counted in blocks; starting and joining
-// cost about 4 of them (8 with 128 tokens: their sums take longer to join).  Measured for 1, 2, 3, 4 CTAs: 1 x 12288 x 4096 15.2 / 12.7 / 17.9 / 16.1 us (2 taken: 3 no longer fit in
-// one wave), 16 x 10240 x 8192 28.5 / 18.7 / 18.0 / 25.6 (3), 113 x 5120 x 13824 74.6 / 43.4 / 32.5 / 49.7 (3).
+// cost about 4 of them (8 with 128 tokens: their sums take longer to join).  Measured for 1, 2, 3, 4 CTAs: 1 x 12288 x 4096
+// 15.2 / 12.7 / 17.9 / 16.1 us (2 taken: 3 no longer fit in one wave), 16 x 10240 x 8192 28.5 / 18.7 / 18.0 / 25.6 (3),
+// 113 x 5120 x 13824 74.6 / 43.4 / 32.5 / 49.7 (3).
 struct Split { int n; long long cost; };
 constexpr Split rows_split_of(long long tiles, int nkb, const int (&places)[9], int occ, int start) {
   Split best{1, 0};
