@@ -18,7 +18,8 @@
 //                  shows where the terms of a row cancel); the two fill exactly the columns that S had.  Warps without rows (a
 //                  single sequence has G) only keep the protocol.
 //   O += P V       P from TMEM; fp32 in TMEM, rescaled when a row's maximum has grown by more than 8 (log2).  P is below 256; fp16
-//                  has it 2^7 times as large (O and the sum too, so it cancels): good to 2^-32 of a row's largest weight.
+//                  has it 2^7 times as large (O and the sum too, so it cancels): good to 2^-32 of a row's largest weight.  The tensor cores'
+//                  additions are cut off rather than rounded: 256 requests behind 16000 keys come out 2e-5 too small.
 // K's place in the ring is free once S is complete, V's after P V; each has a warp that asks for the next.  The ring runs on
 // over the items' borders, and the next item's Q is fetched while the last tile of the one before is finished.
 //
