@@ -30,7 +30,7 @@ def test_linear(B, kw):  # noqa: F811
 
 
 @pytest.mark.parametrize("kw", [
-    # q_out 3 x 4 x 128 fp16: 3072 bytes; pages 8 x 2 x 16 x 128: 65536 bytes each
+    # q_out 3 x 4 x 128 fp16; pages 8 x 2 x 16 x 128, 65536 bytes each
     {"ko": 128 * MiB + 3056}, {"ko": 128 * MiB - 65520}, {"vo": 256 * MiB + 65520}, {"vo": 256 * MiB}, {"vo": 128 * MiB - 65520}, {"vo": 128 * MiB + 3056},
 ])
 def test_heads(B, kw):  # noqa: F811
