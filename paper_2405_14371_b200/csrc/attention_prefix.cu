@@ -18,8 +18,8 @@
 //                  shows where the terms of a row cancel); the two fill exactly the columns that S had.  Warps without rows (a
 //                  single sequence has G) only keep the protocol.
 //   O += P V       P from TMEM; fp32 in TMEM, rescaled when a row's maximum has grown by more than 8 (log2).  P is below 256; fp16
-//                  has it 2^7 times as large (O and the sum too, so it cancels): good to 2^-32 of a row's largest weight.  The tensor cores'
-//                  additions are cut off rather than rounded: 256 requests behind 16000 keys come out 2e-5 too small.
+//                  has it 2^7 times as large (O and the sum too, so it cancels): good to 2^-32 of a row's largest weight.  The
+//                  tensor cores' additions are cut off rather than rounded: 256 requests behind 16000 keys come out 2e-5 too small.
 // K's place in the ring is free once S is complete, V's after P V; each has a warp that asks for the next.  The ring runs on
 // over the items' borders, and the next item's Q is fetched while the last tile of the one before is finished.
 //
@@ -62,6 +62,7 @@ struct PrefixParams {
   int own_q;
   int box;                               // tokens of a page that one copy brings
   float scale_log2e;
+  float one;                             // 1, which the compiler does not know: with a known factor it makes one fused operation of two packed ones
 };
 
 // A piece of an item: what one CTA does of it.
@@ -488,12 +489,14 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
 #pragma unroll
             for (int q = 0; q < 4; ++q) mx4[q] = max3(mx4[q], sc[c + 2 * q], sc[c + 2 * q + 1]);
           float mx = max3(max3(mx4[0], mx4[1], mx4[2]), mx4[3], max3(max3(sc[KT - 4], sc[KT - 3], sc[KT - 2]), sc[KT - 1], -INFINITY));
-          mx *= p.scale_log2e;
-          move = mx > m_ref + GAP || (m_ref == -INFINITY && mx > -INFINITY);
-          const float m_new = move ? mx : m_ref, m_use = m_new == -INFINITY ? 0.f : m_new;
-          alpha = move ? ex2(m_ref - m_use) : 1.f;
+          mx = __fmul_rn(mx, p.scale_log2e);                   // rounded, as the scores below are
+          // m_ref: what exponents are counted from, LIFT below the maximum that it was taken of.  An exponent is the rounded score's
+          // distance from it, as the maximum's is: it exceeds LIFT + GAP for no score, however large a score's own step is.
           constexpr float LIFT = BF16 ? 0.f : 7.f;
-          const uint64_t scale2 = pack_f32x2(p.scale_log2e, p.scale_log2e), minus2 = pack_f32x2(LIFT - m_use, LIFT - m_use), one2 = pack_f32x2(1.f, 1.f);
+          move = mx - m_ref > LIFT + GAP;
+          const float m_new = move ? mx - LIFT : m_ref, m_use = m_new == -INFINITY ? 0.f : m_new;
+          alpha = move ? ex2(m_ref - m_use) : 1.f;
+          const uint64_t scale2 = pack_f32x2(p.scale_log2e, p.scale_log2e), minus2 = pack_f32x2(-m_use, -m_use), one2 = pack_f32x2(p.one, p.one);
           uint64_t sum[2] = {0, 0};
 #pragma unroll
           for (int half = 0; half < 2; ++half) {               // 16 keys take 8 columns for their weights and 8 for the rest of them
@@ -501,7 +504,7 @@ __global__ void __launch_bounds__(THREADS, 2) prefix_attn_kernel(const __grid_co
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const int c = half * 32 + 2 * i, at = (i >> 3) * 16 + (i & 7);
-              const float2 t = unpack_f32x2(fma_f32x2(pack_f32x2(sc[c], sc[c + 1]), scale2, minus2));
+              const float2 t = unpack_f32x2(fma_f32x2(mul_f32x2(pack_f32x2(sc[c], sc[c + 1]), scale2), one2, minus2));
               const float a = ex2(t.x), b = ex2(t.y);
               packed[at] = round_pair<BF16>(a, b);
               packed[at + 8] = rest_pair<BF16>(packed[at], a, b);
@@ -789,6 +792,7 @@ extern "C" es_status_t es_op_decode_attention_prefix(const void* q, int32_t dtyp
   p.own_q = p.own_rows <= 32;
   p.box = page_tokens < KT ? page_tokens : KT;
   p.scale_log2e = 1.4426950408889634f / sqrtf((float)hd);
+  p.one = 1.f;
   PrefixMaps maps = {};
   ES_TRY(tma_encode_3d_f16(&maps.q, q, (int64_t)B * T, Hq, hd, q_stride, TT, G));
   if (p.own_q) ES_TRY(tma_encode_3d_f16(&maps.q_own, q, (int64_t)B * T, Hq, hd, q_stride, T, G));

@@ -130,3 +130,20 @@ def test_infinities_that_a_row_sees_reach_it_as_infinities(prefix, dtype):
     assert bool(torch.isnan(got[:, [4, 6]]).all())
     rest = [c for c in range(hd) if c not in range(1, 7)]
     assert bool(torch.isfinite(got[:, rest]).all()) and bool(torch.isfinite(clean).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("prefix", [0, 70])
+@pytest.mark.parametrize("large", [2.0 ** 9, 2.0 ** 12, 2.0 ** 14, 2.0 ** 15])
+def test_scores_whose_own_steps_are_large(prefix, large, dtype):
+    """Scores of 2^21 to 2^33, which fp32 holds in steps of 1/4 to 2^10: no weight is larger than the largest key's by more than
+    such a step makes it, so every result is finite and lies among the values."""
+    n, hd = 200, 64
+    g = torch.Generator().manual_seed(5)
+    q = large * (1 + 0.01 * torch.rand(40, 1, 1, hd, generator=g))
+    k = large * (1 + 0.001 * torch.rand(n, hd, generator=g))
+    v = 1 + torch.rand(n, hd, generator=g)
+    q, k, v = [t.to(dtype).cuda() for t in (q, k, v)]
+    got = attend(q, k, v, prefix)
+    assert bool(torch.isfinite(got).all()) and float(got.min()) >= 1 - 2 * ref.HALF_STEP[dtype] and float(got.max()) <= 2 + 4 * ref.HALF_STEP[dtype]
